@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_HERE, "_lib", "libsa_sketch.so")
 SA_F32, SA_BF16 = 0, 1
 SA_KERNEL_FWD_MAIN, SA_KERNEL_BWD_MAIN, SA_KERNEL_AUX, SA_KERNEL_FWD_LSE, SA_KERNEL_BWD_DQ = 0, 1, 2, 3, 4
 STATUS = {0: "SA_OK", 1: "SA_ERR_INVALID_ARG", 2: "SA_ERR_UNSUPPORTED", 3: "SA_ERR_WORKSPACE",
-          4: "SA_ERR_CUDA", 5: "SA_ERR_TIMEOUT", 6: "SA_ERR_BAD_SEQLENS"}
+          4: "SA_ERR_CUDA", 5: "SA_ERR_TIMEOUT", 6: "SA_ERR_BAD_SEQLENS", 7: "SA_ERR_BAD_PAGE"}
 
 _lib = None
 
@@ -98,6 +98,22 @@ def load() -> ctypes.CDLL:
     lib.sa_plan_host.restype = i32
     lib.sa_walk_host.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, ctypes.c_int64]
     lib.sa_walk_host.restype = i32
+    lib.sa_cache_page_bytes.argtypes = [i32, i32, i32]
+    lib.sa_cache_page_bytes.restype = sz
+    lib.sa_cache_write.argtypes = [vp, vp, i64, i64, i64, vp, i32, i64, vp, i32, i32, i32, vp, i64, i32, vp, i32, vp,
+                                   sz, vp]
+    lib.sa_cache_write.restype = i32
+    lib.sa_cache_read.argtypes = [vp, i64, i32, vp, i32, vp, i32, i64, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+    lib.sa_cache_read.restype = i32
+    lib.sa_cache_attn_workspace_size.argtypes = [i32, i64, i32, i32, i32, i32, i64, i32]
+    lib.sa_cache_attn_workspace_size.restype = sz
+    attn = [vp, i64, i64, vp, i32, i64, i32, vp, i64, i32, vp, i32, vp, i32, i32, vp, vp, f32, i32]
+    lib.sa_cache_attn_fwd.argtypes = attn + [vp, vp, vp, sz, vp]
+    lib.sa_cache_attn_fwd.restype = i32
+    lib.sa_cache_attn_bwd.argtypes = attn + [vp, vp, vp, vp, vp, sz, vp]
+    lib.sa_cache_attn_bwd.restype = i32
+    lib.sa_cache_attn_kernel_name.argtypes = [i32, i64, i32, i32, i32, f32, i32, i32]
+    lib.sa_cache_attn_kernel_name.restype = ctypes.c_char_p
     _lib = lib
     return lib
 
@@ -532,3 +548,198 @@ def sa_sketch(K, V, cu_seqlens, Q, scale: Optional[float] = None):
     """Differentiable sketch [B,H,P,d] (fp32) of packed ragged histories."""
     scale = 1.0 / math.sqrt(K.shape[-1]) if scale is None else float(scale)
     return SketchAttention.apply(K, V, cu_seqlens, Q, scale)
+
+
+# ------------------------------------------------------- the 4-bit cache
+# (include/sa_cache.h).  `pool` is uint8 [n_pages, H, 2, page * (d/2 + d/16)] and
+# `block_table` int32 [B, max_pages]; the page size follows from the pool's shape
+# and the width d of the rows.
+
+_stream_ws_cache = {}
+
+
+def _stream_workspace(nbytes: int, device) -> torch.Tensor:
+    """A cached workspace of the current stream (calls on other streams may run at the same time)."""
+    key = (device.index, torch.cuda.current_stream(device).cuda_stream)
+    buf = _stream_ws_cache.get(key)
+    if buf is None or buf.numel() < nbytes:
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _stream_ws_cache[key] = buf
+    return buf
+
+
+def sa_cache_page_bytes(H: int, d: int, page: int) -> int:
+    """Bytes of one page of ``page`` tokens (0 for unsupported sizes)."""
+    return int(load().sa_cache_page_bytes(H, d, page))
+
+
+def sa_cache_alloc(n_pages: int, H: int, d: int, page: int = 64, device="cuda") -> torch.Tensor:
+    """An empty pool of ``n_pages`` pages (its bytes are not initialised; nothing reads what was not written)."""
+    if sa_cache_page_bytes(H, d, page) == 0:
+        raise SketchError(2, "sa_cache_page_bytes")
+    return torch.empty((n_pages, H, 2, page * (d // 2 + d // 16)), dtype=torch.uint8, device=device)
+
+
+def _cache_args(pool, block_table, d: int):
+    """(n_pages, H, page, B, max_pages) after the checks that every cache call makes."""
+    for name, t in (("pool", pool), ("block_table", block_table)):
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous CUDA tensor")
+    if pool.dtype != torch.uint8 or pool.dim() != 4 or pool.shape[2] != 2:
+        raise ValueError("pool must be uint8 [n_pages, H, 2, page * (d/2 + d/16)]")
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.device != pool.device:
+        raise ValueError("block_table must be int32 [B, max_pages] on the pool's device")
+    page, rest = divmod(pool.shape[3] * 16, 9 * d)
+    if rest:
+        raise ValueError(f"records of {pool.shape[3]} bytes hold no whole page of rows of width {d}")
+    return pool.shape[0], pool.shape[1], page, block_table.shape[0], block_table.shape[1]
+
+
+def _offsets_arg(name, t, n, device):
+    if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or t.device != device
+                          or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous int32 [{n}] on the pool's device")
+
+
+def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
+                   cu_seqlens: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
+                   ws: Optional[torch.Tensor] = None) -> None:
+    """Write rows into the cache in 4 bits: user b's row i to position start[b] + i.
+
+    K, V are packed rows [N, H, d] with ``cu_seqlens`` [B+1], or [B, H, n, d] (a
+    batch of sketches) without; fp32 or bf16, any strides with contiguous rows."""
+    lib = load()
+    packed = cu_seqlens is not None
+    if K.dim() != (3 if packed else 4) or K.shape != V.shape or K.dtype != V.dtype:
+        raise ValueError("K and V must be [N, H, d] with cu_seqlens, or [B, H, n, d] without, of one dtype")
+    d = K.shape[-1]
+    n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
+    if not K.is_cuda or K.device != pool.device or V.device != pool.device:
+        raise ValueError("K and V must be on the pool's device")
+    if K.stride(-1) != 1 or V.stride() != K.stride():
+        raise ValueError("K and V must have contiguous rows and equal strides")
+    if K.shape[1] != H or (not packed and K.shape[0] != B):
+        raise ValueError(f"K{tuple(K.shape)} does not fit a cache of {H} heads and {B} users")
+    _offsets_arg("cu_seqlens", cu_seqlens, B + 1, pool.device)
+    _offsets_arg("start", start, B, pool.device)
+    if packed:
+        N, strides = K.shape[0], (0, K.stride(0), K.stride(1))
+    else:
+        N, strides = B * K.shape[2], (K.stride(0), K.stride(2), K.stride(1))
+    with torch.cuda.device(pool.device):
+        w = ws if ws is not None else _stream_workspace(256, pool.device)
+        st = lib.sa_cache_write(_ptr(K), _ptr(V), *strides, _ptr(cu_seqlens), B, N, _ptr(start), H, d, _dt(K),
+                                _ptr(pool), n_pages, page, _ptr(block_table), max_pages, _ptr(w), w.numel(),
+                                _stream(pool.device))
+    _check(st, "sa_cache_write")
+
+
+def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: torch.Tensor, n_rows: int, d: int,
+                  start: Optional[torch.Tensor] = None, dtype=torch.bfloat16, ws: Optional[torch.Tensor] = None):
+    """(K, V) [n_rows, H, d]: positions start[b] .. of every user, n_rows = cu_seqlens[B] in all."""
+    lib = load()
+    n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
+    _offsets_arg("cu_seqlens", cu_seqlens, B + 1, pool.device)
+    _offsets_arg("start", start, B, pool.device)
+    K = torch.empty((n_rows, H, d), dtype=dtype, device=pool.device)
+    V = torch.empty_like(K)
+    with torch.cuda.device(pool.device):
+        w = ws if ws is not None else _stream_workspace(256, pool.device)
+        st = lib.sa_cache_read(_ptr(pool), n_pages, page, _ptr(block_table), max_pages, _ptr(cu_seqlens), B, n_rows,
+                               _ptr(start), H, d, _dt(K), _ptr(K), _ptr(V), _ptr(w), w.numel(), _stream(pool.device))
+    _check(st, "sa_cache_read")
+    return K, V
+
+
+def sa_cache_attn_workspace_size(B: int, T: int, Hq: int, H: int, d: int, dt: int, max_tokens: int, bwd: bool) -> int:
+    return int(load().sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_tokens, int(bool(bwd))))
+
+
+def sa_cache_attn_kernel_name(B: int, T: int, Hq: int, H: int, d: int, scale: float, dt: int, bwd: bool) -> str:
+    return load().sa_cache_attn_kernel_name(B, T, Hq, H, d, float(scale), dt, int(bool(bwd))).decode()
+
+
+def _cache_attn(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, bwd: bool):
+    """What both directions check and pass: (leading C arguments, workspace)."""
+    if q.dim() != 3 or not q.is_cuda or q.stride(-1) != 1:
+        raise ValueError("q must be a CUDA tensor [T, Hq, d] with contiguous rows")
+    T, Hq, d = q.shape
+    n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
+    dev = pool.device
+    if q.device != dev:
+        raise ValueError("q must be on the pool's device")
+    if Hq % H:
+        raise ValueError(f"{Hq} query heads over {H} cached heads")
+    _offsets_arg("cu_q", cu_q, B + 1, dev)
+    _offsets_arg("cache_lens", cache_lens, B, dev)
+    _offsets_arg("kv_begin", kv_begin, T, dev)
+    _offsets_arg("kv_end", kv_end, T, dev)
+    dt = _dt(q)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    need = load().sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_pages * page, int(bwd))
+    if need == 0:
+        raise SketchError(2, "sa_cache_attn_workspace_size")
+    w = ws if ws is not None else _stream_workspace(need, dev)
+    return (_ptr(q), q.stride(0), q.stride(1), _ptr(cu_q), B, T, Hq, _ptr(pool), n_pages, page, _ptr(block_table),
+            max_pages, _ptr(cache_lens), H, d, _ptr(kv_begin), _ptr(kv_end), scale, dt), w
+
+
+def sa_cache_attn_fwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor,
+                      cache_lens: torch.Tensor, kv_begin: Optional[torch.Tensor] = None,
+                      kv_end: Optional[torch.Tensor] = None, scale: Optional[float] = None, want_lse: bool = False,
+                      ws: Optional[torch.Tensor] = None):
+    """Attention of packed queries q [T, Hq, d] (user b's are cu_q[b] .. cu_q[b+1]-1) over the cache:
+    out [T, Hq, d] like q (and lse [T, Hq] fp32).  Query t sees positions kv_begin[t] <= i < kv_end[t] below
+    cache_lens[b] (all of them by default); one that sees nothing gets zeros and -inf."""
+    lib = load()
+    with torch.cuda.device(pool.device):
+        args, w = _cache_attn(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, False)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+        st = lib.sa_cache_attn_fwd(*args, _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
+    _check(st, "sa_cache_attn_fwd")
+    return (out, lse) if want_lse else out
+
+
+def sa_cache_attn_bwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor,
+                      cache_lens: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                      kv_begin: Optional[torch.Tensor] = None, kv_end: Optional[torch.Tensor] = None,
+                      scale: Optional[float] = None, ws: Optional[torch.Tensor] = None):
+    """dq [T, Hq, d] like q for the gradient dout of ``sa_cache_attn_fwd``'s out; out and lse are that call's.
+    The cached rows are constants and get no gradient."""
+    lib = load()
+    for name, t, shape, dtype in (("out", out, q.shape, q.dtype), ("dout", dout, q.shape, q.dtype),
+                                  ("lse", lse, q.shape[:2], torch.float32)):
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != q.device:
+            raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on q's device")
+    with torch.cuda.device(pool.device):
+        args, w = _cache_attn(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, True)
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        st = lib.sa_cache_attn_bwd(*args, _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(w), w.numel(),
+                                   _stream(q.device))
+    _check(st, "sa_cache_attn_bwd")
+    return dq
+
+
+class CacheAttention(torch.autograd.Function):
+    """out = softmax(scale q K^T) V over each user's cached rows; gradient for q only."""
+
+    @staticmethod
+    def forward(ctx, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale):
+        out, lse = sa_cache_attn_fwd(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, want_lse=True)
+        ctx.save_for_backward(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, out, lse)
+        ctx.scale = scale
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, out, lse = ctx.saved_tensors
+        dq = sa_cache_attn_bwd(q, cu_q, pool, block_table, cache_lens, out, lse, dout.contiguous(), kv_begin, kv_end,
+                               ctx.scale)
+        return dq, None, None, None, None, None, None, None
+
+
+def sa_cache_attention(q, cu_q, pool, block_table, cache_lens, kv_begin=None, kv_end=None,
+                       scale: Optional[float] = None):
+    """Differentiable (in q) attention of packed queries over the 4-bit cache: [T, Hq, d]."""
+    return CacheAttention.apply(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale)

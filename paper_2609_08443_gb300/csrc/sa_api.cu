@@ -9,6 +9,7 @@
 
 #include <cuda.h>
 
+#include "../../include/sa_cache.h"
 #include "sa_kernels.cuh"
 #include "sa_tc.cuh"
 #include "sa_tc_common.cuh"
@@ -200,6 +201,7 @@ namespace sa {
 
 bool tc_path_enabled() { return g_path.load() != 1; }
 uint64_t wait_limit_ns() { return g_wait_ns.load(); }
+void count_launches(int n) { g_launches.fetch_add(uint64_t(n), std::memory_order_relaxed); }
 bool tc_fwd_sliced_selected() { return g_path.load() == 2; }
 bool tc_narrow_selected() { return g_path.load() == 3; }
 
@@ -599,7 +601,9 @@ const char* sa_status_string(sa_status s) {
     case SA_ERR_CUDA: return "CUDA runtime error";
     case SA_ERR_TIMEOUT: return "a device pipeline wait gave up (bounded wait expired)";
     case SA_ERR_BAD_SEQLENS: return "cu_seqlens is not 0..N non-decreasing";
+    default: break;
   }
+  if (s == SA_ERR_BAD_PAGE) return "a used block_table entry is outside [0, n_pages)";
   return "unknown status";
 }
 

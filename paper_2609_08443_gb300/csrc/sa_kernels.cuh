@@ -31,6 +31,8 @@ SA_HD int q_row(const Args& a, int b, int h) { return a.uq ? b * a.H + h : h; }
 // Limit of the bounded pipeline waits for calls enqueued from now on
 // (sa_set_wait_limit_ns; the planner copies it into each call's workspace).
 uint64_t wait_limit_ns();
+// Adds to sa_launch_count() (for host files other than sa_api.cu).
+void count_launches(int n);
 
 // planner / finalize (sa_simt.cu)
 cudaError_t launch_plan(const Args& a, int T, cudaStream_t st);
