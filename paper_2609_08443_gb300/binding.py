@@ -7,7 +7,9 @@ built or cannot be loaded, every call raises: there is no CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import math
 import os
 from typing import Optional, Tuple
@@ -558,9 +560,18 @@ def sa_sketch(K, V, cu_seqlens, Q, scale: Optional[float] = None):
 _stream_ws_cache = {}
 
 
-def _stream_workspace(nbytes: int, device) -> torch.Tensor:
-    """A cached workspace of the current stream (calls on other streams may run at the same time)."""
-    key = (device.index, torch.cuda.current_stream(device).cuda_stream)
+def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _on(device):
+    """Makes ``device`` current for a call (nothing to do, and no cost, where it is)."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _stream_workspace(nbytes: int, device, stream: int) -> torch.Tensor:
+    """A cached workspace of this stream (calls on other streams may run at the same time)."""
+    key = (device.index, stream)
     buf = _stream_ws_cache.get(key)
     if buf is None or buf.numel() < nbytes:
         buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -626,11 +637,12 @@ def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tenso
         N, strides = K.shape[0], (0, K.stride(0), K.stride(1))
     else:
         N, strides = B * K.shape[2], (K.stride(0), K.stride(2), K.stride(1))
-    with torch.cuda.device(pool.device):
-        w = ws if ws is not None else _stream_workspace(256, pool.device)
-        st = lib.sa_cache_write(_ptr(K), _ptr(V), *strides, _ptr(cu_seqlens), B, N, _ptr(start), H, d, _dt(K),
-                                _ptr(pool), n_pages, page, _ptr(block_table), max_pages, _ptr(w), w.numel(),
-                                _stream(pool.device))
+    with _on(pool.device):
+        stream = torch.cuda.current_stream().cuda_stream
+        w = ws if ws is not None else _stream_workspace(256, pool.device, stream)
+        st = lib.sa_cache_write(K.data_ptr(), V.data_ptr(), *strides, _addr(cu_seqlens), B, N, _addr(start), H, d,
+                                _dt(K), pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
+                                w.data_ptr(), w.numel(), stream)
     _check(st, "sa_cache_write")
 
 
@@ -643,14 +655,17 @@ def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: tor
     _offsets_arg("start", start, B, pool.device)
     K = torch.empty((n_rows, H, d), dtype=dtype, device=pool.device)
     V = torch.empty_like(K)
-    with torch.cuda.device(pool.device):
-        w = ws if ws is not None else _stream_workspace(256, pool.device)
-        st = lib.sa_cache_read(_ptr(pool), n_pages, page, _ptr(block_table), max_pages, _ptr(cu_seqlens), B, n_rows,
-                               _ptr(start), H, d, _dt(K), _ptr(K), _ptr(V), _ptr(w), w.numel(), _stream(pool.device))
+    with _on(pool.device):
+        stream = torch.cuda.current_stream().cuda_stream
+        w = ws if ws is not None else _stream_workspace(256, pool.device, stream)
+        st = lib.sa_cache_read(pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
+                               cu_seqlens.data_ptr(), B, n_rows, _addr(start), H, d, _dt(K), K.data_ptr(),
+                               V.data_ptr(), w.data_ptr(), w.numel(), stream)
     _check(st, "sa_cache_read")
     return K, V
 
 
+@functools.lru_cache(maxsize=1024)
 def sa_cache_attn_workspace_size(B: int, T: int, Hq: int, H: int, d: int, dt: int, max_tokens: int, bwd: bool) -> int:
     return int(load().sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_tokens, int(bool(bwd))))
 
@@ -659,8 +674,8 @@ def sa_cache_attn_kernel_name(B: int, T: int, Hq: int, H: int, d: int, scale: fl
     return load().sa_cache_attn_kernel_name(B, T, Hq, H, d, float(scale), dt, int(bool(bwd))).decode()
 
 
-def _cache_attn(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, bwd: bool):
-    """What both directions check and pass: (leading C arguments, workspace)."""
+def _cache_attn(entry, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, bwd: bool, *tensors):
+    """What both directions check and pass; ``tensors``: the entry point's own."""
     if q.dim() != 3 or not q.is_cuda or q.stride(-1) != 1:
         raise ValueError("q must be a CUDA tensor [T, Hq, d] with contiguous rows")
     T, Hq, d = q.shape
@@ -676,12 +691,17 @@ def _cache_attn(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale,
     _offsets_arg("kv_end", kv_end, T, dev)
     dt = _dt(q)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    need = load().sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_pages * page, int(bwd))
-    if need == 0:
-        raise SketchError(2, "sa_cache_attn_workspace_size")
-    w = ws if ws is not None else _stream_workspace(need, dev)
-    return (_ptr(q), q.stride(0), q.stride(1), _ptr(cu_q), B, T, Hq, _ptr(pool), n_pages, page, _ptr(block_table),
-            max_pages, _ptr(cache_lens), H, d, _ptr(kv_begin), _ptr(kv_end), scale, dt), w
+    with _on(dev):
+        stream = torch.cuda.current_stream().cuda_stream
+        if ws is None:
+            need = sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_pages * page, bwd)
+            if need == 0:
+                raise SketchError(2, "sa_cache_attn_workspace_size")
+            ws = _stream_workspace(need, dev, stream)
+        st = entry(q.data_ptr(), q.stride(0), q.stride(1), cu_q.data_ptr(), B, T, Hq, pool.data_ptr(), n_pages, page,
+                   block_table.data_ptr(), max_pages, cache_lens.data_ptr(), H, d, _addr(kv_begin), _addr(kv_end),
+                   scale, dt, *[_addr(t) for t in tensors], ws.data_ptr(), ws.numel(), stream)
+    _check(st, "sa_cache_attn_bwd" if bwd else "sa_cache_attn_fwd")
 
 
 def sa_cache_attn_fwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor,
@@ -691,13 +711,10 @@ def sa_cache_attn_fwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, b
     """Attention of packed queries q [T, Hq, d] (user b's are cu_q[b] .. cu_q[b+1]-1) over the cache:
     out [T, Hq, d] like q (and lse [T, Hq] fp32).  Query t sees positions kv_begin[t] <= i < kv_end[t] below
     cache_lens[b] (all of them by default); one that sees nothing gets zeros and -inf."""
-    lib = load()
-    with torch.cuda.device(pool.device):
-        args, w = _cache_attn(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, False)
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
-        st = lib.sa_cache_attn_fwd(*args, _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
-    _check(st, "sa_cache_attn_fwd")
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+    _cache_attn(load().sa_cache_attn_fwd, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, False,
+                out, lse)
     return (out, lse) if want_lse else out
 
 
@@ -707,17 +724,13 @@ def sa_cache_attn_bwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, b
                       scale: Optional[float] = None, ws: Optional[torch.Tensor] = None):
     """dq [T, Hq, d] like q for the gradient dout of ``sa_cache_attn_fwd``'s out; out and lse are that call's.
     The cached rows are constants and get no gradient."""
-    lib = load()
     for name, t, shape, dtype in (("out", out, q.shape, q.dtype), ("dout", dout, q.shape, q.dtype),
                                   ("lse", lse, q.shape[:2], torch.float32)):
         if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != q.device:
             raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on q's device")
-    with torch.cuda.device(pool.device):
-        args, w = _cache_attn(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, True)
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        st = lib.sa_cache_attn_bwd(*args, _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(w), w.numel(),
-                                   _stream(q.device))
-    _check(st, "sa_cache_attn_bwd")
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _cache_attn(load().sa_cache_attn_bwd, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, True,
+                out, lse, dout, dq)
     return dq
 
 

@@ -92,15 +92,64 @@ __device__ __forceinline__ uint32_t scale_code(float big) {
   return c;
 }
 
-// |x| / s to the nearest whole number, halves down, at most 7.  The quotient by the
-// rounded reciprocal may sit on the wrong side of a half; the remainder x - q s is
-// exact there (both are within a factor of two of each other), so it decides.
-__device__ __forceinline__ uint32_t level_of(float ax, float s, float inv_s) {
-  float q = fminf(rintf(ax * inv_s), 8.f);
-  const float r = fmaf(-q, s, ax);
-  if (r > 0.5f * s) q += 1.f;
-  if (r <= -0.5f * s) q -= 1.f;
-  return uint32_t(fminf(q, 7.f));
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t m, uint32_t o) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(m), "r"(o));  // (a & m) | o
+  return d;
+}
+
+// bf16 scales of the codes in the two halves of `cc`, as (s / 8, -24 s): a level field
+// u at mantissa bits 3..6 of 128.0 reads 128 + 8 u, and (128 + 8 u) s/8 - 24 s =
+// (u - 8) s in one rounding, which is exact (24 s has six significant bits).
+struct ScaleB {
+  uint32_t s8, c;
+};
+__device__ __forceinline__ ScaleB scale_bf16(uint32_t cc) {
+  ScaleB r;
+  r.s8 = cc * 16u + 0x36803680u;
+  r.c = mul_bf16x2(r.s8, 0xC340C340u);  // -192
+  return r;
+}
+// word of codes -> four bf16 pairs
+__device__ __forceinline__ void values_bf16(uint32_t w, ScaleB s, uint32_t* r) {
+  r[0] = fma_bf16x2(and_or(w << 3, 0x00780078u, 0x43004300u), s.s8, s.c);
+  r[1] = fma_bf16x2(and_or(w >> 1, 0x00780078u, 0x43004300u), s.s8, s.c);
+  r[2] = fma_bf16x2(and_or(w >> 5, 0x00780078u, 0x43004300u), s.s8, s.c);
+  r[3] = fma_bf16x2(and_or(w >> 9, 0x00780078u, 0x43004300u), s.s8, s.c);
+}
+// word of codes -> four float16 pairs, times the float16 scales s2.  The level comes
+// first and alone (72 s would pass float16's range), then one exact product.
+__device__ __forceinline__ void values_f16(uint32_t w, uint32_t s2, uint32_t* r) {
+  const uint32_t v = w >> 8;
+  r[0] = mul_f16x2(add_f16x2(and_or(w, 0x000F000Fu, 0x64006400u), 0xE408E408u), s2);               // 1024 + u - 1032
+  r[1] = mul_f16x2(fma_f16x2(and_or(w, 0x00F000F0u, 0x64006400u), 0x2C002C00u, 0xD480D480u), s2);  // (1024 + 16 u) / 16 - 72
+  r[2] = mul_f16x2(add_f16x2(and_or(v, 0x000F000Fu, 0x64006400u), 0xE408E408u), s2);
+  r[3] = mul_f16x2(fma_f16x2(and_or(v, 0x00F000F0u, 0x64006400u), 0x2C002C00u, 0xD480D480u), s2);
 }
 #endif
 

@@ -64,6 +64,9 @@ struct Cfg {
 // Partial of one piece: 16 rows of D sums, then 16 (max, sum) pairs.
 __host__ __device__ constexpr int partial_floats(int D) { return ROWS * D + ROWS * 2; }
 
+// Shares of a call with `total` tiles: none is empty.
+__device__ __forceinline__ int shares(const AttnArgs& a, int64_t total) { return int(total < a.workers ? total : a.workers); }
+
 struct Piece {  // what a worker's first segment is, for the join
   int64_t seg0, seg1;
   int b, h, rt, pad;
@@ -81,66 +84,6 @@ __device__ __forceinline__ void mma_f16(float* c, const uint32_t* a, uint32_t b0
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t m, uint32_t o) {
-  uint32_t d;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(m), "r"(o));  // (a & m) | o
-  return d;
-}
-
-// bf16 scales of the codes in the two halves of `cc`, as (s / 8, -24 s): a level field
-// u at mantissa bits 3..6 of 128.0 reads 128 + 8 u, and (128 + 8 u) s/8 - 24 s =
-// (u - 8) s in one rounding, which is exact (24 s has six significant bits).
-struct ScaleB {
-  uint32_t s8, c;
-};
-__device__ __forceinline__ ScaleB scale_bf16(uint32_t cc) {
-  ScaleB r;
-  r.s8 = cc * 16u + 0x36803680u;
-  r.c = mul_bf16x2(r.s8, 0xC340C340u);  // -192
-  return r;
-}
-// word of codes -> four bf16 pairs
-__device__ __forceinline__ void values_bf16(uint32_t w, ScaleB s, uint32_t* r) {
-  r[0] = fma_bf16x2(and_or(w << 3, 0x00780078u, 0x43004300u), s.s8, s.c);
-  r[1] = fma_bf16x2(and_or(w >> 1, 0x00780078u, 0x43004300u), s.s8, s.c);
-  r[2] = fma_bf16x2(and_or(w >> 5, 0x00780078u, 0x43004300u), s.s8, s.c);
-  r[3] = fma_bf16x2(and_or(w >> 9, 0x00780078u, 0x43004300u), s.s8, s.c);
-}
-// word of codes -> four float16 pairs, times the float16 scales s2.  The level comes
-// first and alone (72 s would pass float16's range), then one exact product.
-__device__ __forceinline__ void values_f16(uint32_t w, uint32_t s2, uint32_t* r) {
-  const uint32_t v = w >> 8;
-  r[0] = mul_f16x2(add_f16x2(and_or(w, 0x000F000Fu, 0x64006400u), 0xE408E408u), s2);               // 1024 + u - 1032
-  r[1] = mul_f16x2(fma_f16x2(and_or(w, 0x00F000F0u, 0x64006400u), 0x2C002C00u, 0xD480D480u), s2);  // (1024 + 16 u) / 16 - 72
-  r[2] = mul_f16x2(add_f16x2(and_or(v, 0x000F000Fu, 0x64006400u), 0xE408E408u), s2);
-  r[3] = mul_f16x2(fma_f16x2(and_or(v, 0x00F000F0u, 0x64006400u), 0x2C002C00u, 0xD480D480u), s2);
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -598,10 +541,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
   if (total <= 0) return;
 
   // Worker order runs over the CTAs first, so that little work still spreads over the SMs.
-  const int wk = int(blockIdx.x) + warp * int(gridDim.x);
-  if (wk >= a.workers) return;
-  const int64_t tb = range_begin(total, a.workers, wk), te = range_begin(total, a.workers, wk + 1);
-  if (tb >= te) return;
+  const int wk = int(blockIdx.x) + warp * int(gridDim.x), W = shares(a, total);
+  if (wk >= W) return;
+  const int64_t tb = range_begin(total, W, wk), te = range_begin(total, W, wk + 1);
 
   uint8_t* mine = smem + warp * C::WARP_SMEM;
   Warp<C, FULL> x{a, lane, lane >> 2, lane & 3, mine, mine + C::FRAGS, bar, ctl, slot};
@@ -843,18 +785,22 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
 
 // Adds the pieces of segments that share borders cut, in worker order, and gathers
 // the CTAs' status.  Block w handles the segment whose first cut is where worker w
-// starts; its warps take the segment's rows.
+// starts.  Eight warps take rp rows at a time and split each row's pieces 8 / rp
+// ways: with one row (a single token over a long history) a segment has many pieces,
+// with sixteen it has few.
+constexpr int kJoinWarps = 8;
+
 template <class C>
-__global__ void __launch_bounds__(128) cache_join_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __grid_constant__ AttnArgs a) {
   using T = typename std::conditional<C::F32, float, __nv_bfloat16>::type;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w = blockIdx.x;
   if (w == 0) {
-    int e = 0;
-    for (int i = threadIdx.x; i < a.ctas; i += blockDim.x) e = max(e, int(a.slots[i].err));
     __shared__ int all;
     if (threadIdx.x == 0) all = 0;
     __syncthreads();
+    int e = 0;
+    for (int i = threadIdx.x; i < a.ctas; i += blockDim.x) e = max(e, int(a.slots[i].err));
     if (e) atomicMax(&all, e);
     __syncthreads();
     if (threadIdx.x == 0) ws_header(a.ws)->err = uint32_t(all);
@@ -862,50 +808,90 @@ __global__ void __launch_bounds__(128) cache_join_kernel(const __grid_constant__
   }
   const int64_t total = ws_header(a.ws)->tiles_per_head;
   if (total <= 0) return;
-  const int64_t tb = range_begin(total, a.workers, w), te = range_begin(total, a.workers, w + 1);
-  if (tb >= te) return;
+  const int W = shares(a, total);
+  if (w >= W) return;
+  const int64_t tb = range_begin(total, W, w);
   const Piece p = static_cast<const Piece*>(a.piece)[w];
   if (p.seg0 >= tb) return;
-  const int first = owner_of(total, a.workers, tb - 1);
-  const int64_t fb = range_begin(total, a.workers, first);
-  if (fb > p.seg0) return;  // an earlier border already cut this segment
-  const int last = owner_of(total, a.workers, p.seg1 - 1);
+  if (range_begin(total, W, w - 1) > p.seg0) return;  // an earlier border already cut this segment
+  const int first = w - 1, n = owner_of(total, W, p.seg1 - 1) - first + 1;
   constexpr int PF = partial_floats(C::D);
-  const float* base = a.partial;
+  // the first worker's piece is its second one unless its share begins with the segment
+  const float* base = a.partial + int64_t(first) * 2 * PF;
+  const int first_off = range_begin(total, W, first) >= p.seg0 ? 0 : PF;
   const int64_t q0 = a.cu_q[p.b];
   const int rows = min(ROWS, int((a.cu_q[p.b + 1] - q0) * a.G - p.rt * ROWS));
-  const int d = a.c.d;
-  for (int r = warp; r < rows; r += 4) {
-    auto piece = [&](int k) { return base + (int64_t(k) * 2 + (k == first ? (fb >= p.seg0 ? 0 : 1) : 0)) * PF; };
-    float m = -INFINITY;
-    if constexpr (!C::BWD) {
-      for (int k = first + lane; k <= last; k += 32)
-        if (range_begin(total, a.workers, k) < range_begin(total, a.workers, k + 1))
-          m = fmaxf(m, piece(k)[ROWS * C::D + 2 * r]);
+  const int rp = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, ns = kJoinWarps / rp;
+  const int split = warp / rp, d = a.c.d;
+  constexpr int V = C::D / 32;
+  __shared__ float part[kJoinWarps][C::D];
+  __shared__ float2 stat[kJoinWarps];
+  for (int r0 = 0; r0 < rows; r0 += rp) {
+    const int r = r0 + warp % rp;
+    float m = -INFINITY, l = 0.f, y[V] = {};
+    if (r < rows) {
+      for (int k0 = split * 32; k0 < n; k0 += ns * 32) {  // 32 pieces at a time, one lane each for the weights
+        const int k = k0 + lane;
+        float f = 1.f;
+        if constexpr (!C::BWD) {
+          float2 ml = make_float2(-INFINITY, 0.f);
+          if (k < n)
+            ml = *reinterpret_cast<const float2*>(base + int64_t(k) * 2 * PF + (k == 0 ? first_off : 0) + ROWS * C::D + 2 * r);
+          float bm = ml.x;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    }
-    float y[C::D / 32] = {}, l = 0.f;
-    for (int k = first; k <= last; ++k) {
-      if (range_begin(total, a.workers, k) >= range_begin(total, a.workers, k + 1)) continue;
-      const float* s = piece(k);
-      float f = 1.f;
-      if constexpr (!C::BWD) {
-        const float2 ml = *reinterpret_cast<const float2*>(s + ROWS * C::D + 2 * r);
-        f = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
-        l = fmaf(ml.y, f, l);
+          for (int o = 16; o; o >>= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
+          const float nm = fmaxf(m, bm), z = nm == -INFINITY ? 0.f : nm, back = ex2(m - z);
+          f = ex2(ml.x - z);
+          float bl = ml.y * f;
+#pragma unroll
+          for (int o = 16; o; o >>= 1) bl += __shfl_xor_sync(0xffffffffu, bl, o);
+          l = fmaf(l, back, bl);
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[i] *= back;
+          m = nm;
+        }
+        const int cnt = min(32, n - k0);
+#pragma unroll 4
+        for (int j = 0; j < cnt; ++j) {
+          const float* s = base + int64_t(k0 + j) * 2 * PF + (k0 + j == 0 ? first_off : 0) + r * C::D + lane;
+          const float fj = __shfl_sync(0xffffffffu, f, j);
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[i] = fmaf(s[32 * i], fj, y[i]);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < C::D / 32; ++i) y[i] = fmaf(s[r * C::D + 32 * i + lane], f, y[i]);
     }
-    const int row = p.rt * ROWS + r;
-    const int64_t o = (q0 + row / a.G) * a.Hq + p.h * a.G + row % a.G;
-    const float f = C::BWD ? a.scale : (l > 0.f ? 1.f / l : 0.f);
-    T* dst = static_cast<T*>(C::BWD ? a.dq : a.out) + o * d;
+    if (ns > 1) {
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < C::D / 32; ++i)
-      if (32 * i + lane < d) st_from_f32(dst + 32 * i + lane, y[i] * f);
-    if (!C::BWD && a.lse && lane == 0) a.lse[o] = l > 0.f ? (m + log2f(l) - kLift) * kLn2 : -INFINITY;
+      for (int i = 0; i < V; ++i) part[warp][32 * i + lane] = y[i];
+      if (lane == 0) stat[warp] = make_float2(m, l);
+      __syncthreads();
+      if (split == 0)
+        for (int s = 1; s < ns; ++s) {
+          const int o = warp + s * rp;
+          float f = 1.f, back = 1.f;
+          if constexpr (!C::BWD) {
+            const float2 ml = stat[o];
+            const float nm = fmaxf(m, ml.x), z = nm == -INFINITY ? 0.f : nm;
+            back = ex2(m - z);
+            f = ex2(ml.x - z);
+            l = fmaf(l, back, ml.y * f);
+            m = nm;
+          }
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[i] = fmaf(part[o][32 * i + lane], f, y[i] * back);
+        }
+    }
+    if (split == 0 && r < rows) {
+      const int row = p.rt * ROWS + r;
+      const int64_t o = (q0 + row / a.G) * a.Hq + p.h * a.G + row % a.G;
+      const float f = C::BWD ? a.scale : (l > 0.f ? 1.f / l : 0.f);
+      T* dst = static_cast<T*>(C::BWD ? a.dq : a.out) + o * d;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (32 * i + lane < d) st_from_f32(dst + 32 * i + lane, y[i] * f);
+      if (!C::BWD && a.lse && lane == 0) a.lse[o] = l > 0.f ? (m + log2f(l) - kLift) * kLn2 : -INFINITY;
+    }
   }
 }
 
@@ -924,7 +910,7 @@ static cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(a.workers));
-  cfg.blockDim = dim3(128);
+  cfg.blockDim = dim3(32 * kJoinWarps);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

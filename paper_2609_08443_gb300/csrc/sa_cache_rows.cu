@@ -3,9 +3,11 @@
 // One thread handles one group of 16 features of one key or value row: writing, it
 // takes the largest magnitude, picks the scale, rounds to levels and stores 8 code
 // bytes and a scale byte; reading, it does the reverse.  Both are bound by memory
-// (per feature 2 or 4 bytes of the row and 9/16 of the cache).  A block takes a run
-// of tokens of one head, so that what it touches in a page is contiguous, and keys
-// and values side by side (blockIdx.z).
+// (per feature 2 or 4 bytes of the row and 9/16 of the cache), so a thread has several
+// groups' loads in flight and the arithmetic is kept to a few instructions a feature.
+// A block takes up to 32 consecutive rows, looks up their pages once, and goes through
+// them head by head with the groups of a row, then the rows, over its threads: what a
+// warp touches is contiguous in the page and in runs of a row on the other side.
 #include "sa_cache.cuh"
 #include "sa_kernels.cuh"
 #include "sa_simt_util.cuh"
@@ -39,13 +41,6 @@ __device__ __forceinline__ RowRef find_row(const RowArgs& a, int64_t row) {
   r.pos = s + r.i;
   r.ok = r.ok && s >= 0 && (r.pos >> a.c.log2page) < a.c.max_pages;
   return r;
-}
-
-// Byte offset of the row's record (K or V: kv), or -1 where there is no page.
-__device__ __forceinline__ int64_t find_record(const RowArgs& a, const RowRef& r, int h, int kv) {
-  const int p = a.c.table[int64_t(r.b) * a.c.max_pages + (r.pos >> a.c.log2page)];
-  if (p < 0 || p >= a.c.n_pages) return -1;
-  return a.c.record(p, h) + int64_t(kv) * a.c.rec;
 }
 
 // Checks of what the host cannot see, by one more block: writes the call's status.
@@ -91,121 +86,248 @@ __device__ __forceinline__ bool offsets_ok(const RowArgs& a) {
   return !__syncthreads_or(bad);
 }
 
-// grid: x = runs of tokens (+ 1 for the checks), y = heads, z = keys / values
-template <typename T>
-__global__ void __launch_bounds__(kThreads) cache_write_kernel(RowArgs a, int rows_per_block) {
+// ------------------------------------------------------------------ a block's rows
+constexpr int kRows = 32;
+
+struct Rows {
+  int64_t rec[kRows];  // byte offset of head 0's key record, or -1: nothing to do
+  int64_t at[kRows];   // element offset of head 0 on the other side
+  int slot[kRows];     // token within the page
+};
+
+// Rows [row0, row0 + n) of the call, looked up by the first threads.  The last block
+// only checks; false: leave.
+template <bool WRITE>
+__device__ __forceinline__ bool find_rows(const RowArgs& a, int n, Rows& s) {
   if (blockIdx.x == gridDim.x - 1) {
-    if (blockIdx.y == 0 && blockIdx.z == 0) check_rows(a);
-    return;
+    check_rows(a);
+    return false;
   }
-  if (!offsets_ok(a)) return;
-  const int ng = a.c.d / kGroup, h = blockIdx.y, kv = blockIdx.z;
-  const int64_t row0 = int64_t(blockIdx.x) * rows_per_block;
-  const T* src = static_cast<const T*>(kv ? a.V : a.K) + int64_t(h) * a.head_stride;
+  if (!offsets_ok(a)) return false;
+  if (threadIdx.x < n) {
+    const int64_t row = int64_t(blockIdx.x) * n + threadIdx.x;
+    int64_t rec = -1;
+    if (row < a.N) {
+      const RowRef r = find_row(a, row);
+      if (r.ok) {
+        const int p = a.c.table[int64_t(r.b) * a.c.max_pages + (r.pos >> a.c.log2page)];
+        if (p >= 0 && p < a.c.n_pages) rec = a.c.record(p, 0);
+        s.slot[threadIdx.x] = int(r.pos & (a.c.page - 1));
+        if (!WRITE)
+          s.at[threadIdx.x] = row * a.c.H * a.c.d;
+        else if (a.cu)
+          s.at[threadIdx.x] = row * a.row_stride;
+        else
+          s.at[threadIdx.x] = r.b * a.user_stride + r.i * a.row_stride;
+      }
+    }
+    s.rec[threadIdx.x] = rec;
+  }
+  __syncthreads();
+  return true;
+}
+
+// Group e of the block: its group of features, row, head and side (0 keys, 1 values).
+struct GroupRef {
+  int g, r, h, kv;
+};
+__device__ __forceinline__ GroupRef group_of(int e, int ng, int n, int H) {
+  GroupRef x;
+  const int u = e / ng, hk = u / n;
+  x.g = e - u * ng;
+  x.r = u - hk * n;
+  x.kv = hk >= H;
+  x.h = x.kv ? hk - H : hk;
+  return x;
+}
+
+// ------------------------------------------------------------------- quantising
+// 16 features as they came.
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> {
+  static constexpr int kAtOnce = 4;  // groups in flight per thread
+  uint4 v[2];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    v[0] = __ldcs(reinterpret_cast<const uint4*>(p));
+    v[1] = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+  }
+  __device__ __forceinline__ uint32_t word(int i) const {
+    const uint4& q = v[i >> 2];
+    return (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
+  }
+  // bits of the largest magnitude as fp32 (a NaN is larger than infinity)
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, word(i) & 0x7FFF7FFFu);
+    return max(m & 0xFFFF0000u, m << 16);
+  }
+  __device__ __forceinline__ float get(int k) const {
+    const uint32_t w = word(k >> 1);
+    return __uint_as_float(k & 1 ? w & 0xFFFF0000u : w << 16);
+  }
+};
+template <> struct Raw<float> {
+  static constexpr int kAtOnce = 2;
+  float4 v[4];
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __ldcs(reinterpret_cast<const float4*>(p) + i);
+  }
+  __device__ __forceinline__ float get(int k) const {
+    const float4& q = v[k >> 2];
+    return (k & 3) == 0 ? q.x : (k & 3) == 1 ? q.y : (k & 3) == 2 ? q.z : q.w;
+  }
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) m = max(m, __float_as_uint(get(k)) & 0x7FFFFFFFu);
+    return m;
+  }
+};
+
+// 1.5 x 2^23 + 8: adding it leaves level + 8 in the low bits of the sum
+constexpr float kRound = 12582920.f;
+constexpr uint32_t kRoundBits = 0x4B400000u;
+__host__ __device__ constexpr int shift_of(int k) { return 4 * (((k & 7) >> 1) + 4 * (k & 1)); }
+__host__ __device__ constexpr uint32_t round_bits_sum() {
+  uint32_t s = 0;
+  for (int k = 0; k < 8; ++k) s += kRoundBits << shift_of(k);
+  return s;
+}
+
+// Levels of a group.  The quotient by a reciprocal made smaller by 2^-20 (its own
+// rounding and the product's are under 2^-22) lies below the true one, so a half always
+// rounds towards zero.  It can come out a level too low only for a quotient within
+// 2^-19 above a half: impossible for bf16 (eight significant bits against the scale's
+// four), and seen for fp32 from the remainder x - q s, which is exact there.
+template <typename T>
+__device__ __forceinline__ uint2 levels(const Raw<T>& x, uint32_t code, bool odd_values) {
+  const float s = scale_value(code), inv = __frcp_rn(s) * (1.f - 0x1p-20f);
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int k = 0; k < kGroup; ++k) {
+    float v = x.get(k);
+    if (odd_values) {  // NaN to zero, beyond the largest scale saturates
+      if (isnan(v)) v = 0.f;
+      v = fminf(fmaxf(v, -7.f * s), 7.f * s);
+    }
+    float u = fmaf(v, inv, kRound);
+    if constexpr (sizeof(T) == 4) {
+      const float r = fmaf(kRound - u, s, v);
+      if (fabsf(r) > 0.5f * s) u += copysignf(1.f, v);
+    }
+    w[k >> 3] += __float_as_uint(u) << shift_of(k);
+  }
+  return make_uint2(w[0] - round_bits_sum(), w[1] - round_bits_sum());
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_constant__ RowArgs a, int n) {
+  __shared__ Rows rows;
+  if (!find_rows<true>(a, n, rows)) return;
+  constexpr int U = Raw<T>::kAtOnce;
+  const int ng = a.c.d / kGroup, count = ng * n * a.c.H * 2;
+  const T* src[2] = {static_cast<const T*>(a.K), static_cast<const T*>(a.V)};
   uint8_t* pool = const_cast<uint8_t*>(a.c.pool);
-  for (int e = threadIdx.x; e < rows_per_block * ng; e += kThreads) {
-    const int64_t row = row0 + e / ng;
-    const int g = e % ng;
-    if (row >= a.N) break;
-    const RowRef r = find_row(a, row);
-    if (!r.ok) continue;
-    const int64_t rec = find_record(a, r, h, kv);
-    if (rec < 0) continue;
-    const T* p = src + (a.cu ? row : int64_t(0)) * a.row_stride +
-                 (a.cu ? int64_t(0) : r.b * a.user_stride + r.i * a.row_stride) + g * kGroup;
-    float x[kGroup];
+  for (int e0 = threadIdx.x; e0 < count; e0 += U * kThreads) {
+    Raw<T> x[U];
+    GroupRef ref[U];
+    bool on[U];
 #pragma unroll
-    for (int k = 0; k < kGroup; k += Vec<T>::n) Vec<T>::load(p + k, x + k);
-    float big = 0.f;
-#pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
-      if (isnan(x[k])) x[k] = 0.f;
-      big = fmaxf(big, fabsf(x[k]));
+    for (int i = 0; i < U; ++i) {
+      const int e = e0 + i * kThreads;
+      ref[i] = group_of(e, ng, n, a.c.H);
+      on[i] = e < count && rows.rec[ref[i].r] >= 0;
+      if (on[i]) x[i].load((ref[i].kv ? src[1] : src[0]) + rows.at[ref[i].r] + ref[i].h * a.head_stride + ref[i].g * kGroup);
     }
-    const uint32_t code = scale_code(big);
-    const float s = scale_value(code), inv = 1.f / s;
-    uint32_t w[2] = {0u, 0u};
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
-      const uint32_t l = level_of(fabsf(x[k]), s, inv);
-      const uint32_t u = x[k] < 0.f ? 8u - l : 8u + l;
-      w[k >> 3] |= u << (4 * (((k & 7) >> 1) + 4 * (k & 1)));
+    for (int i = 0; i < U; ++i) {
+      if (!on[i]) continue;
+      uint32_t big = x[i].largest();
+      if (big > 0x7F800000u) {  // a NaN: the largest of the others
+        big = 0;
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+          const float v = x[i].get(k);
+          if (!isnan(v)) big = max(big, __float_as_uint(v) & 0x7FFFFFFFu);
+        }
+        big |= 1u << 31;
+      }
+      const uint32_t code = scale_code(__uint_as_float(big & 0x7FFFFFFFu));
+      const uint2 w = levels<T>(x[i], code, code == kCodeMax || (big >> 31));
+      const int64_t rec = rows.rec[ref[i].r] + int64_t(2 * ref[i].h + ref[i].kv) * a.c.rec;
+      const int slot = rows.slot[ref[i].r];
+      *reinterpret_cast<uint2*>(pool + rec + slot * (a.c.d / 2) + ref[i].g * 8) = w;
+      pool[rec + a.c.page * (a.c.d / 2) + slot * ng + ref[i].g] = uint8_t(code);
     }
-    const int slot = int(r.pos & (a.c.page - 1));
-    *reinterpret_cast<uint2*>(pool + rec + int64_t(slot) * (a.c.d / 2) + g * 8) = make_uint2(w[0], w[1]);
-    pool[rec + int64_t(a.c.page) * (a.c.d / 2) + slot * ng + g] = uint8_t(code);
-  }
-}
-
-template <typename T> __device__ __forceinline__ void store16(T* p, const float* x);
-template <> __device__ __forceinline__ void store16<float>(float* p, const float* x) {
-#pragma unroll
-  for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(p + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-}
-template <> __device__ __forceinline__ void store16<__nv_bfloat16>(__nv_bfloat16* p, const float* x) {
-#pragma unroll
-  for (int k = 0; k < 16; k += 8) {
-    __nv_bfloat162 v[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = __floats2bfloat162_rn(x[k + 2 * j], x[k + 2 * j + 1]);
-    *reinterpret_cast<uint4*>(p + k) = *reinterpret_cast<const uint4*>(v);
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(RowArgs a, int rows_per_block) {
-  if (blockIdx.x == gridDim.x - 1) {
-    if (blockIdx.y == 0 && blockIdx.z == 0) check_rows(a);
-    return;
-  }
-  if (!offsets_ok(a)) return;
-  const int ng = a.c.d / kGroup, h = blockIdx.y, kv = blockIdx.z;
-  const int64_t row0 = int64_t(blockIdx.x) * rows_per_block;
-  T* dst = static_cast<T*>(kv ? a.Vo : a.Ko) + int64_t(h) * a.c.d;
-  for (int e = threadIdx.x; e < rows_per_block * ng; e += kThreads) {
-    const int64_t row = row0 + e / ng;
-    const int g = e % ng;
-    if (row >= a.N) break;
-    const RowRef r = find_row(a, row);
-    if (!r.ok) continue;
-    const int64_t rec = find_record(a, r, h, kv);
-    if (rec < 0) continue;
-    const int slot = int(r.pos & (a.c.page - 1));
-    const uint2 w2 = *reinterpret_cast<const uint2*>(a.c.pool + rec + int64_t(slot) * (a.c.d / 2) + g * 8);
-    const float s = scale_value(a.c.pool[rec + int64_t(a.c.page) * (a.c.d / 2) + slot * ng + g]);
-    float x[kGroup];
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ RowArgs a, int n) {
+  __shared__ Rows rows;
+  if (!find_rows<false>(a, n, rows)) return;
+  constexpr int U = 4;
+  const int ng = a.c.d / kGroup, count = ng * n * a.c.H * 2;
+  T* dst[2] = {static_cast<T*>(a.Ko), static_cast<T*>(a.Vo)};
+  for (int e0 = threadIdx.x; e0 < count; e0 += U * kThreads) {
+    uint2 w[U];
+    uint32_t code[U];
+    GroupRef ref[U];
+    bool on[U];
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
-      const uint32_t w = k < 8 ? w2.x : w2.y;
-      x[k] = s * float(int((w >> (4 * (((k & 7) >> 1) + 4 * (k & 1)))) & 15u) - 8);
+    for (int i = 0; i < U; ++i) {
+      const int e = e0 + i * kThreads;
+      ref[i] = group_of(e, ng, n, a.c.H);
+      on[i] = e < count && rows.rec[ref[i].r] >= 0;
+      if (!on[i]) continue;
+      const uint8_t* rec = a.c.pool + rows.rec[ref[i].r] + int64_t(2 * ref[i].h + ref[i].kv) * a.c.rec;
+      const int slot = rows.slot[ref[i].r];
+      w[i] = __ldcs(reinterpret_cast<const uint2*>(rec + slot * (a.c.d / 2) + ref[i].g * 8));
+      code[i] = __ldcs(rec + a.c.page * (a.c.d / 2) + slot * ng + ref[i].g);
     }
-    store16(dst + row * a.c.H * a.c.d + g * kGroup, x);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (!on[i]) continue;
+      uint32_t v[8];
+      const ScaleB s = scale_bf16(code[i] * 0x00010001u);
+      values_bf16(w[i].x, s, v);
+      values_bf16(w[i].y, s, v + 4);
+      T* p = (ref[i].kv ? dst[1] : dst[0]) + rows.at[ref[i].r] + ref[i].h * a.c.d + ref[i].g * kGroup;
+      if constexpr (sizeof(T) == 2) {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          reinterpret_cast<float4*>(p)[k] =
+              make_float4(__uint_as_float(v[2 * k] << 16), __uint_as_float(v[2 * k] & 0xFFFF0000u),
+                          __uint_as_float(v[2 * k + 1] << 16), __uint_as_float(v[2 * k + 1] & 0xFFFF0000u));
+      }
+    }
   }
 }
 
-// Rows a block takes: enough groups for its threads.
-static int rows_per_block(const RowArgs& a) { return kThreads / (a.c.d / kGroup) > 0 ? kThreads / (a.c.d / kGroup) : 1; }
+// Rows a block takes: 32, fewer (a power of two) where that would leave SMs without work.
+static int rows_per_block(const RowArgs& a) {
+  int n = kRows;
+  while (n > 1 && a.N / n < 608) n >>= 1;
+  return n;
+}
 
-static dim3 row_grid(const RowArgs& a, int rpb) {
-  return dim3(unsigned((a.N + rpb - 1) / rpb + 1), unsigned(a.c.H), 2);
+static cudaError_t launch_rows(void (*kernel)(RowArgs, int), const RowArgs& a, cudaStream_t st) {
+  const int n = rows_per_block(a);
+  kernel<<<unsigned((a.N + n - 1) / n + 1), kThreads, 0, st>>>(a, n);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_write(const RowArgs& a, cudaStream_t st) {
-  const int rpb = rows_per_block(a);
-  if (a.dt == SA_BF16)
-    cache_write_kernel<__nv_bfloat16><<<row_grid(a, rpb), kThreads, 0, st>>>(a, rpb);
-  else
-    cache_write_kernel<float><<<row_grid(a, rpb), kThreads, 0, st>>>(a, rpb);
-  return cudaGetLastError();
+  return a.dt == SA_BF16 ? launch_rows(cache_write_kernel<__nv_bfloat16>, a, st) : launch_rows(cache_write_kernel<float>, a, st);
 }
 
 cudaError_t launch_read(const RowArgs& a, cudaStream_t st) {
-  const int rpb = rows_per_block(a);
-  if (a.dt == SA_BF16)
-    cache_read_kernel<__nv_bfloat16><<<row_grid(a, rpb), kThreads, 0, st>>>(a, rpb);
-  else
-    cache_read_kernel<float><<<row_grid(a, rpb), kThreads, 0, st>>>(a, rpb);
-  return cudaGetLastError();
+  return a.dt == SA_BF16 ? launch_rows(cache_read_kernel<__nv_bfloat16>, a, st) : launch_rows(cache_read_kernel<float>, a, st);
 }
 
 }  // namespace cache
