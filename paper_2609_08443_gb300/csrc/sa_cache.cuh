@@ -69,9 +69,11 @@ cudaError_t launch_write(const RowArgs& a, cudaStream_t st);
 cudaError_t launch_read(const RowArgs& a, cudaStream_t st);
 
 // Warp-level kernels (sa_cache_mma.cu)
-int mma_workers(int sms, int d, sa_dtype dt, bool bwd, int* ctas);
-size_t mma_piece_bytes();
-size_t mma_partial_floats(int d);
+struct MmaPlan {
+  int ctas, workers;
+  size_t piece_bytes, partial_floats;  // per worker; per worker and slot
+};
+MmaPlan mma_plan(int sms, int B, int64_t T, int G, int d, sa_dtype dt, bool bwd);
 cudaError_t launch_mma(const AttnArgs& a, bool bwd, cudaStream_t st);
 
 // ------------------------------------------------------------------ arithmetic

@@ -67,15 +67,17 @@ struct Layout {
 
 Layout attn_layout(int B, int64_t T, int G, int H, int d, sa_dtype dt, int64_t max_tokens, bool bwd) {
   Layout l{};
-  l.workers = sa::cache::mma_workers(sa::tcc::device_sm_count(), d, dt, bwd, &l.ctas);
-  (void)B, (void)T, (void)G, (void)H, (void)max_tokens;
+  const sa::cache::MmaPlan p = sa::cache::mma_plan(sa::tcc::device_sm_count(), B, T, G, d, dt, bwd);
+  (void)H, (void)max_tokens;
+  l.ctas = p.ctas;
+  l.workers = p.workers;
   size_t off = sizeof(sa::WsHeader);
   l.slots = off;
   off += size_t(l.ctas) * sizeof(sa::WsHeader);
   l.piece = off;
-  off = sa::align256(off + size_t(l.workers) * sa::cache::mma_piece_bytes());
+  off = sa::align256(off + size_t(l.workers) * p.piece_bytes);
   l.partial = off;
-  off = sa::align256(off + size_t(l.workers) * 2 * sa::cache::mma_partial_floats(d) * sizeof(float));
+  off = sa::align256(off + size_t(l.workers) * 2 * p.partial_floats * sizeof(float));
   l.total = off;
   return l;
 }

@@ -1,21 +1,24 @@
 // Attention over the 4-bit cache with warp-level tensor-core products: the form for
 // few queries (serving's single tokens), for fp32 and for every width.
 //
-// One warp is one worker.  It owns 16 query rows (a user's queries times the query
-// heads that share a cached head) and walks 64 cached positions at a time:
-//     S = Q K^T  (m16n8k16)  ->  online softmax in registers  ->  O += P V  (m16n8k16)
-// The 4-bit words go from shared memory straight into the B operands' registers:
-//   - for Q K^T lane (g, t) = (lane / 4, lane % 4) takes key g's features
-//     [D/4 t, D/4 (t+1)): the contraction order is free, so Q's fragments are laid
-//     out the same way once per segment;
-//   - for P V it takes four keys' features of column group g; a byte permute puts
-//     two keys' words side by side and the same masks give the pairs (k, k+1) that
-//     the operand wants.  S's accumulators are P's A operand as they stand.
+// One warp is one worker.  It owns 8 NR query rows (a user's queries times the query
+// heads that share a cached head) and walks KB cached positions at a time, everything
+// transposed so that the cache is the 16-row operand and a few queries the 8-column one:
+//     S^T = K Q^T  (m16n8k16)  ->  online softmax in registers  ->  O^T += V^T P^T
+// The 4-bit words go from shared memory straight into the A operands' registers:
+//   - for K Q^T lane (g, t) = (lane / 4, lane % 4) takes keys g and g + 8 and features
+//     [D/4 t, D/4 (t+1)): the contraction order is free, so Q's fragments are laid out
+//     the same way once per segment;
+//   - for V^T P^T it takes four keys' features of column group g; a byte permute puts
+//     two keys' words side by side and the same masks give the pairs (k, k+1) that the
+//     operand wants.  S^T's accumulators become P^T's operand by a transpose of 8 x 8
+//     tiles between registers.
 // So nothing is stored dequantised, and a cached byte costs one bulk copy and one
 // shared-memory read per product.  With one query per user the call is bound by
-// reading the cache: 144 bytes a key and head at d = 128.
+// reading the cache, 144 bytes a key and head at d = 128, and next by issuing about
+// 20 instructions a key and head and warp, four fifths of them dequantisation.
 //
-// Work is the list of (user, cached head, 16-row tile, 64-position block), cut into
+// Work is the list of (user, cached head, row tile, block of positions), cut into
 // equal contiguous shares; a segment cut by share borders leaves unfinished
 // (O, max, sum) pieces that the join kernel adds in order.  Every CTA scans the
 // users' lengths itself, so a call is two launches.
@@ -24,35 +27,37 @@
 #include "sa_cache.cuh"
 #include "sa_kernels.cuh"
 #include "sa_ptx.cuh"
+#include "sa_simt_util.cuh"
 
 namespace sa {
 namespace cache {
 
 using namespace ptx;
 
-constexpr int KB = 64;       // positions per block
-constexpr int ROWS = 16;     // query rows per tile
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // Weights are kept as 2^12 exp(S - max): float16 then holds weights down to 2^-26 of
 // the largest in full precision.
 constexpr float kLift = 12.f;
 
-template <int D_, bool F32_, bool BWD_>
+template <int D_, bool F32_, bool BWD_, int NR_>
 struct Cfg {
   static constexpr int D = D_;
   static constexpr bool F32 = F32_, BWD = BWD_;
+  static constexpr int NR = NR_;           // column tiles of 8 query rows
+  static constexpr int ROWS = 8 * NR;
+  static constexpr int KB = 64;            // positions per block
   static constexpr int NS = F32 ? 3 : 1;   // bf16 terms of a query or gradient element
   static constexpr int NP = F32 ? 2 : 1;   // float16 terms of a weight
   static constexpr int LW = D / 32;        // words of 8 features a lane holds of a key
-  static constexpr int KS = D / 16;        // contraction steps
-  static constexpr int NT = D / 8;         // column tiles of the output
-  static constexpr int FRAG = KS * 32 * 16;
+  static constexpr int MT = D / 16;        // row tiles of the transposed output
+  static constexpr int FRAG = LW * 32 * 16 * NR;
   static constexpr int FRAGS = FRAG * NS * (BWD ? 2 : 1);
   static constexpr int STAGE = KB * 2 * (D / 2 + D / 16);
   static constexpr int WARP_SMEM = FRAGS + 2 * STAGE;
-  static constexpr int NWARP = BWD ? (F32 ? (D == 128 ? 4 : 8) : (D == 128 ? 8 : 12))
-                                   : (F32 ? (D == 128 ? 6 : 8) : (D == 128 ? 8 : 12));
+  static constexpr int FIT = (232448 - 8192) / WARP_SMEM;  // warps that shared memory holds
+  static constexpr int WANT = D == 128 ? (BWD || F32 || NR > 1 ? 8 : 10) : (F32 && NR > 1 ? 8 : BWD || F32 || NR > 1 ? 12 : 14);
+  static constexpr int NWARP = FIT < WANT ? FIT : WANT;
   static constexpr int THREADS = NWARP * 32;
   static constexpr int OFF_BAR = NWARP * WARP_SMEM + 128;  // the last lanes of a narrow row may read past a stage
   static constexpr int OFF_SCAN = OFF_BAR + NWARP * 16;
@@ -61,8 +66,8 @@ struct Cfg {
   static_assert(SMEM <= 232448, "shared memory budget");
 };
 
-// Partial of one piece: 16 rows of D sums, then 16 (max, sum) pairs.
-__host__ __device__ constexpr int partial_floats(int D) { return ROWS * D + ROWS * 2; }
+// Partial of one piece: its rows' D sums, then their (max, sum) pairs.
+__host__ __device__ constexpr int partial_floats(int rows, int D) { return rows * D + rows * 2; }
 
 // Shares of a call with `total` tiles: none is empty.
 __device__ __forceinline__ int shares(const AttnArgs& a, int64_t total) { return int(total < a.workers ? total : a.workers); }
@@ -86,6 +91,14 @@ __device__ __forceinline__ void mma_f16(float* c, const uint32_t* a, uint32_t b0
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// 8 x 8 tile of 16-bit values: lane (g, t) gives row g, columns 2t and 2t + 1, and gets
+// column g, rows 2t and 2t + 1.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -102,8 +115,8 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// Column c of an 8-key tile is this key of the tile: pairs differ in parity and the
-// even columns hold two even and two odd keys, so the reads of K (two keys a phase)
+// Row c of an 8-key tile is this key of the tile: pairs differ in parity and the
+// even rows hold two even and two odd keys, so the reads of K (two keys a phase)
 // and of V (four keys a phase) spread over the shared-memory banks.
 __device__ __forceinline__ int key_of(int c) { return c ^ ((c >> 1) & 1); }
 
@@ -124,14 +137,15 @@ struct Sizes {
   int nrt, nkb, rows, len;
   int64_t q0;
 };
+template <class C>
 __device__ __forceinline__ Sizes user_sizes(const AttnArgs& a, int b) {
   Sizes s;
   const int c0 = a.cu_q[b], c1 = a.cu_q[b + 1];
   s.q0 = c0;
   s.len = a.lens[b];
   s.rows = (c1 - c0) * a.G;
-  s.nrt = (s.rows + ROWS - 1) / ROWS;
-  s.nkb = s.len > 0 ? (s.len + KB - 1) / KB : 1;  // a user with nothing cached still gets its zeros
+  s.nrt = (s.rows + C::ROWS - 1) / C::ROWS;
+  s.nkb = s.len > 0 ? (s.len + C::KB - 1) / C::KB : 1;  // a user with nothing cached still gets its zeros
   s.tiles = int64_t(s.nrt) * s.nkb * a.c.H;
   return s;
 }
@@ -142,6 +156,7 @@ __device__ __forceinline__ void row_window(const AttnArgs& a, int64_t t, int len
 }
 
 // The piece that starts at tile w.t of user w.b (sizes in s).
+template <class C>
 __device__ __forceinline__ void set_piece(const AttnArgs& a, Walk& w, const Sizes& s, int64_t rem, int lane) {
   w.nrt = s.nrt;
   w.nkb = s.nkb;
@@ -159,7 +174,7 @@ __device__ __forceinline__ void set_piece(const AttnArgs& a, Walk& w, const Size
   w.vis1 = w.len;
   if (a.begin || a.end) {
     int lo = 0x7fffffff, hi = 0;
-    const int r = w.rt * ROWS + (lane & (ROWS - 1));
+    const int r = w.rt * C::ROWS + (lane & (C::ROWS - 1));
     if (r < w.rows) {
       int l, e;
       row_window(a, w.q0 + r / a.G, w.len, l, e);
@@ -172,12 +187,13 @@ __device__ __forceinline__ void set_piece(const AttnArgs& a, Walk& w, const Size
     w.vis1 = __reduce_max_sync(0xffffffffu, hi);
   }
   const int64_t last = w.te < w.seg1 ? w.te : w.seg1;
-  w.kb0 = max(kb, w.vis0 / KB);
-  w.kb1 = min(int(last - w.seg0), (w.vis1 + KB - 1) / KB);
+  w.kb0 = max(kb, w.vis0 / C::KB);
+  w.kb1 = min(int(last - w.seg0), (w.vis1 + C::KB - 1) / C::KB);
   if (w.vis0 >= w.vis1) w.kb1 = w.kb0;
 }
 
 // Move to the next piece of the share; false at its end.
+template <class C>
 __device__ __forceinline__ bool next_piece(const AttnArgs& a, Walk& w, int lane) {
   w.t = w.te < w.seg1 ? w.te : w.seg1;
   if (w.t >= w.te) return false;
@@ -204,17 +220,17 @@ __device__ __forceinline__ bool next_piece(const AttnArgs& a, Walk& w, int lane)
       if (b >= a.B) return false;
     }
     w.b = b;
-    s = user_sizes(a, b);
+    s = user_sizes<C>(a, b);
     rem = 0;
   }
-  set_piece(a, w, s, rem, lane);
+  set_piece<C>(a, w, s, rem, lane);
   return true;
 }
 
 // Exclusive scan of the users' tiles over the CTA's threads (each takes `chunk`
-// consecutive users) into pre[0..THREADS]; returns the total, or -1 where offsets or
+// consecutive users) into pre[0..C::THREADS]; returns the total, or -1 where offsets or
 // lengths are out of order.
-template <int THREADS>
+template <class C>
 __device__ int64_t scan_users(const AttnArgs& a, int64_t* pre, int chunk) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b0 = tid * chunk, b1 = min(a.B, b0 + chunk);
@@ -224,7 +240,7 @@ __device__ int64_t scan_users(const AttnArgs& a, int64_t* pre, int chunk) {
   for (int b = b0; b < b1; ++b) {
     const int c0 = a.cu_q[b], c1 = a.cu_q[b + 1], len = a.lens[b];
     if (c0 > c1 || (b == 0 && c0 != 0) || (b == a.B - 1 && int64_t(c1) != a.T) || len < 0 || len > most) bad = 1;
-    sum += user_sizes(a, b).tiles;
+    sum += user_sizes<C>(a, b).tiles;
   }
   int64_t inc = sum;
 #pragma unroll
@@ -236,20 +252,20 @@ __device__ int64_t scan_users(const AttnArgs& a, int64_t* pre, int chunk) {
   if (lane == 31) warp_sum[warp] = inc;
   bad = __syncthreads_or(bad);
   int64_t before = 0, total = 0;
-  for (int i = 0; i < THREADS / 32; ++i) {
+  for (int i = 0; i < C::NWARP; ++i) {
     if (i < warp) before += warp_sum[i];
     total += warp_sum[i];
   }
   pre[tid] = before + inc - sum;
-  if (tid == 0) pre[THREADS] = total;
+  if (tid == 0) pre[C::THREADS] = total;
   __syncthreads();
   return bad ? -1 : total;
 }
 
 // The user of tile t and the tile's rank among the user's.
-template <int THREADS>
+template <class C>
 __device__ void find_tile(const AttnArgs& a, const int64_t* pre, int chunk, int64_t t, int lane, int& b, int64_t& rem) {
-  int lo = 0, hi = THREADS - 1;
+  int lo = 0, hi = C::THREADS - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (pre[mid] <= t) lo = mid; else hi = mid - 1;
@@ -257,7 +273,7 @@ __device__ void find_tile(const AttnArgs& a, const int64_t* pre, int chunk, int6
   int64_t at = pre[lo];
   for (int b0 = lo * chunk;; b0 += 32) {
     const int u = b0 + lane;
-    const int64_t mine = u < a.B && u < (lo + 1) * chunk ? user_sizes(a, u).tiles : 0;
+    const int64_t mine = u < a.B && u < (lo + 1) * chunk ? user_sizes<C>(a, u).tiles : 0;
     int64_t inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -290,65 +306,52 @@ struct Warp {
   const uint32_t bar;        // two barriers
   volatile int* const ctl;
   WsHeader* const slot;
-  int pe, log2pe, recS;      // positions and bytes of a record in shared memory
+  static constexpr int KB = C::KB;
   uint32_t issued = 0, used = 0;
   bool ok = true;
 
-  // What lane `lane` copies of block kb of the piece, and the page it comes from.
-  __device__ __forceinline__ int copies() const { return a.c.page <= KB ? KB / a.c.page : 4; }
+  // A stage holds the block's key codes, key scales, value codes and value scales, each
+  // contiguous over the positions whatever the page size.  Lane 4 p + i copies part i of
+  // the block's p-th page (all of it, or KB positions of a larger one).
+  __device__ __forceinline__ int width() const { return FULL ? C::D : a.c.d; }
   __device__ __forceinline__ bool wanted(const Walk& w, int kb) const {
-    if (lane >= copies()) return false;
-    const int p0 = kb * KB + (a.c.page <= KB ? lane * a.c.page : 0);
-    return p0 < w.vis1 && p0 + pe > w.vis0;
+    const int n = min(a.c.page, KB), off = (lane >> 2) * n, p0 = kb * KB + off;
+    return off < KB && p0 < w.vis1 && p0 + n > w.vis0;
   }
   __device__ __forceinline__ int page_id(const Walk& w, int kb) const {
     if (!wanted(w, kb)) return 0;
-    const int p0 = kb * KB + (a.c.page <= KB ? lane * a.c.page : 0);
+    const int p0 = kb * KB + (lane >> 2) * min(a.c.page, KB);
     return a.c.table[int64_t(w.b) * a.c.max_pages + (p0 >> a.c.log2page)];
   }
   __device__ __forceinline__ void issue(const Walk& w, int kb, int pid) {
     const uint32_t s = issued & 1u;
-    const uint32_t dst = smem_u32(ring) + s * C::STAGE, b = bar + 8u * s;
+    const uint32_t b = bar + 8u * s;
     bool want = wanted(w, kb);
     if (want && (pid < 0 || pid >= a.c.n_pages)) {
       atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
       want = false;
     }
-    uint32_t bytes = 0, off = 0;
-    int64_t src = 0;
-    if (want) {
-      src = a.c.record(pid, w.h);
-      if (a.c.page <= KB) {
-        bytes = 2u * a.c.rec;
-        off = lane * bytes;
-      } else {
-        const int sub = (kb * KB) & (a.c.page - 1), kv = lane >> 1;
-        src += int64_t(kv) * a.c.rec;
-        off = kv * recS;
-        if (lane & 1) {
-          src += int64_t(a.c.page) * (a.c.d / 2) + sub * (a.c.d / 16);
-          off += KB * (a.c.d / 2);
-          bytes = KB * (a.c.d / 16);
-        } else {
-          src += int64_t(sub) * (a.c.d / 2);
-          bytes = KB * (a.c.d / 2);
-        }
-      }
-    }
+    const int n = min(a.c.page, KB), off = (lane >> 2) * n, first = (kb * KB + off) & (a.c.page - 1);
+    const int kv = (lane >> 1) & 1, rb = lane & 1 ? a.c.d / 16 : a.c.d / 2;  // bytes of a row of this part
+    const uint32_t bytes = want ? uint32_t(n * rb) : 0u;
     const uint32_t total = __reduce_add_sync(0xffffffffu, bytes);
     if (lane == 0) mbar_arrive_expect_tx(b, total);
     __syncwarp();
-    if (want) bulk_load(dst + off, a.c.pool + src, bytes, b);
+    if (want) {
+      const uint8_t* src = a.c.pool + a.c.record(pid, w.h) + kv * a.c.rec + (lane & 1 ? a.c.page * (a.c.d / 2) : 0) + first * rb;
+      const uint32_t dst = smem_u32(ring) + s * C::STAGE + (kv * (KB * (a.c.d / 2 + a.c.d / 16))) +
+                           (lane & 1 ? KB * (a.c.d / 2) : 0) + off * rb;
+      bulk_load(dst, src, bytes, b);
+    }
     ++issued;
   }
 
-  // Address of key k's code row (kv = 0) or value row (kv = 1) within the stage.
+  // Code row and scales of key k (kv = 0) or value k (kv = 1) within the stage.
   __device__ __forceinline__ const uint8_t* row(const uint8_t* st, int k, int kv) const {
-    return st + ((k >> log2pe) * 2 + kv) * recS + (k & (pe - 1)) * (FULL ? C::D / 2 : a.c.d / 2);
+    return st + kv * (KB * (width() / 2 + width() / 16)) + k * (width() / 2);
   }
   __device__ __forceinline__ const uint8_t* scales(const uint8_t* st, int k, int kv) const {
-    const int d = FULL ? C::D : a.c.d;
-    return st + ((k >> log2pe) * 2 + kv) * recS + pe * (d / 2) + (k & (pe - 1)) * (d / 16);
+    return st + kv * (KB * (width() / 2 + width() / 16)) + KB * (width() / 2) + k * (width() / 16);
   }
   // This lane's words of key row k in the contraction layout, and its scale codes.
   __device__ __forceinline__ void load_words(const uint8_t* st, int k, int kv, uint32_t* w, uint32_t& codes) const {
@@ -370,42 +373,53 @@ struct Warp {
       codes = sp[0];
     }
   }
-  // acc[j] += rows x key tile j, j < NJ, keys 8 (j0 + j) + key_of(c); `fr` the rows' fragments
-  template <int NJ>
-  __device__ __forceinline__ void contract(const uint8_t* st, int j0, int kv, const uint8_t* fr, float (*acc)[4]) const {
-    uint32_t w[NJ][C::LW], codes[NJ];
+  // acc[m][n] = key tile m (16 keys from 16 (m0 + m)) x query rows 8 n ..; `fr` their fragments
+  template <int NM>
+  __device__ __forceinline__ void contract(const uint8_t* st, int m0, int kv, const uint8_t* fr,
+                                           float (*acc)[C::NR][4]) const {
+    uint32_t w[NM][2][C::LW], codes[NM][2];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      load_words(st, 8 * (j0 + j) + key_of(g), kv, w[j], codes[j]);
-      acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+    for (int m = 0; m < NM; ++m) {
+      load_words(st, 16 * (m0 + m) + key_of(g), kv, w[m][0], codes[m][0]);
+      load_words(st, 16 * (m0 + m) + 8 + key_of(g), kv, w[m][1], codes[m][1]);
+#pragma unroll
+      for (int n = 0; n < C::NR; ++n) acc[m][n][0] = acc[m][n][1] = acc[m][n][2] = acc[m][n][3] = 0.f;
     }
+    ScaleB sc[NM][2];
 #pragma unroll
     for (int i = 0; i < C::LW; ++i) {
-      uint32_t A[C::NS][2][4];
+      uint4 q[C::NS][C::NR];
 #pragma unroll
       for (int s = 0; s < C::NS; ++s)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-          *reinterpret_cast<uint4*>(A[s][k]) =
-              *reinterpret_cast<const uint4*>(fr + s * C::FRAG + ((2 * i + k) * 32 + lane) * 16);
+        for (int n = 0; n < C::NR; ++n)
+          q[s][n] = *reinterpret_cast<const uint4*>(fr + s * C::FRAG + ((n * C::LW + i) * 32 + lane) * 16);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        uint32_t v[4];
-        values_bf16(w[j][i], scale_bf16(((codes[j] >> (8 * (i / 2))) & 255u) * 0x00010001u), v);
-#pragma unroll
-        for (int s = C::NS - 1; s >= 0; --s) {  // the smallest terms first
-          mma_bf16(acc[j], A[s][0], v[0], v[1]);
-          mma_bf16(acc[j], A[s][1], v[2], v[3]);
+      for (int m = 0; m < NM; ++m) {
+        if (i % 2 == 0) {  // two words share a scale
+          sc[m][0] = scale_bf16(((codes[m][0] >> (8 * (i / 2))) & 255u) * 0x00010001u);
+          sc[m][1] = scale_bf16(((codes[m][1] >> (8 * (i / 2))) & 255u) * 0x00010001u);
         }
+        uint32_t lo[4], hi[4];
+        values_bf16(w[m][0][i], sc[m][0], lo);
+        values_bf16(w[m][1][i], sc[m][1], hi);
+        const uint32_t A0[4] = {lo[0], hi[0], lo[1], hi[1]}, A1[4] = {lo[2], hi[2], lo[3], hi[3]};
+#pragma unroll
+        for (int s = C::NS - 1; s >= 0; --s)  // the smallest terms first
+#pragma unroll
+          for (int n = 0; n < C::NR; ++n) {
+            mma_bf16(acc[m][n], A0, q[s][n].x, q[s][n].y);
+            mma_bf16(acc[m][n], A1, q[s][n].z, q[s][n].w);
+          }
       }
     }
   }
-  // acc += weights x rows of 16 keys 16 jj ..: WT terms of A operands; F16 or bf16 values.
-  // Keys outside [first, last) of the block count as zero: what nobody wrote can read as
-  // an infinity in float16, and 0 x inf is not 0.
+  // acc += (rows of 16 keys from 16 jj, transposed) x weights B, WT terms each; F16 or bf16
+  // values.  Keys outside [first, last) of the block count as zero: what nobody wrote can
+  // read as an infinity in float16, and 0 x inf is not 0.
   template <bool F16, int WT>
-  __device__ __forceinline__ void combine(const uint8_t* st, int jj, int kv, const uint32_t (*A)[4], float (*acc)[4],
-                                          bool inside, int first, int last) const {
+  __device__ __forceinline__ void combine(const uint8_t* st, int jj, int kv, const uint32_t (*B)[WT][2],
+                                          float (*acc)[C::NR][4], bool inside, int first, int last) const {
     int k[4];
     k[0] = 16 * jj + key_of(2 * t4);
     k[1] = 16 * jj + key_of(2 * t4 + 1);
@@ -428,50 +442,50 @@ struct Warp {
     }
     const uint32_t c01 = code[0] | code[1] << 16, c23 = code[2] | code[3] << 16;
     const ScaleB sb01 = scale_bf16(c01), sb23 = scale_bf16(c23);
+    auto values = [&](uint32_t x, bool second, uint32_t* r) {
+      if constexpr (F16)
+        values_f16(x, (second ? c23 : c01) << 7, r);
+      else
+        values_bf16(x, second ? sb23 : sb01, r);
+    };
 #pragma unroll
-    for (int n = 0; n < NW; ++n) {
+    for (int i = 0; i < NW; ++i) {
+      uint32_t e01[4], e23[4], o01[4], o23[4];  // even and odd features, keys 0 1 and 2 3
+      values(__byte_perm(w[0][i], w[1][i], 0x5410u), false, e01);
+      values(__byte_perm(w[0][i], w[1][i], 0x7632u), false, o01);
+      values(__byte_perm(w[2][i], w[3][i], 0x5410u), true, e23);
+      values(__byte_perm(w[2][i], w[3][i], 0x7632u), true, o23);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {  // even, then odd features
-        const uint32_t sel = half ? 0x7632u : 0x5410u;
-        const uint32_t x = __byte_perm(w[0][n], w[1][n], sel), y = __byte_perm(w[2][n], w[3][n], sel);
-        uint32_t b0[4], b1[4];
-        if constexpr (F16) {
-          values_f16(x, c01 << 7, b0);
-          values_f16(y, c23 << 7, b1);
-        } else {
-          values_bf16(x, sb01, b0);
-          values_bf16(y, sb23, b1);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t A[4] = {e01[e], o01[e], e23[e], o23[e]};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int n = 0; n < C::NR; ++n)
 #pragma unroll
           for (int s = WT - 1; s >= 0; --s) {
             if constexpr (F16)
-              mma_f16(acc[8 * n + 2 * e + half], A[s], b0[e], b1[e]);
+              mma_f16(acc[4 * i + e][n], A, B[n][s][0], B[n][s][1]);
             else
-              mma_bf16(acc[8 * n + 2 * e + half], A[s], b0[e], b1[e]);
+              mma_bf16(acc[4 * i + e][n], A, B[n][s][0], B[n][s][1]);
           }
       }
     }
   }
 
-  // Rows g and g + 8 of src (element offsets r0, r1; negative: no row) as fragments.
+  // Rows g of src (element offsets r[n]; negative: no row) as fragments.
   template <typename T>
-  __device__ __forceinline__ void load_frags(const T* src, int64_t r0, int64_t r1, uint8_t* fr) const {
+  __device__ __forceinline__ void load_frags(const T* src, const int64_t* r, uint8_t* fr) const {
     const int base = (C::D / 4) * t4, d = FULL ? C::D : a.c.d;
 #pragma unroll
-    for (int i = 0; i < C::LW; ++i) {
-      const int c = base + 8 * i;
-      uint32_t A[C::NS][2][4];
+    for (int n = 0; n < C::NR; ++n)
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int64_t r = half ? r1 : r0;
+      for (int i = 0; i < C::LW; ++i) {
+        const int c = base + 8 * i;
         uint32_t p[C::NS][4] = {};
-        if (r >= 0 && c < d) {
+        if (r[n] >= 0 && c < d) {
           if constexpr (C::F32) {
             float x[8];
-            *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(src + r + c);
-            *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(src + r + c + 4);
+            *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(src + r[n] + c);
+            *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(src + r[n] + c + 4);
 #pragma unroll
             for (int s = 0; s < C::NS; ++s)
 #pragma unroll
@@ -482,21 +496,14 @@ struct Warp {
                 x[2 * k + 1] -= f.y;
               }
           } else {
-            *reinterpret_cast<uint4*>(p[0]) = *reinterpret_cast<const uint4*>(src + r + c);
+            *reinterpret_cast<uint4*>(p[0]) = *reinterpret_cast<const uint4*>(src + r[n] + c);
           }
         }
 #pragma unroll
         for (int s = 0; s < C::NS; ++s)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) A[s][k >> 1][half + 2 * (k & 1)] = p[s][k];
+          *reinterpret_cast<uint4*>(fr + s * C::FRAG + ((n * C::LW + i) * 32 + lane) * 16) =
+              *reinterpret_cast<const uint4*>(p[s]);
       }
-#pragma unroll
-      for (int s = 0; s < C::NS; ++s)
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          *reinterpret_cast<uint4*>(fr + s * C::FRAG + ((2 * i + k) * 32 + lane) * 16) =
-              *reinterpret_cast<const uint4*>(A[s][k]);
-    }
   }
 };
 
@@ -532,7 +539,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
   fence_mbar_init();
   int64_t* pre = reinterpret_cast<int64_t*>(smem + C::OFF_SCAN);
   const int chunk = (a.B + C::THREADS - 1) / C::THREADS;
-  const int64_t total = scan_users<C::THREADS>(a, pre, chunk);
+  const int64_t total = scan_users<C>(a, pre, chunk);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     ws_header(a.ws)->tiles_per_head = total;
     if (total < 0) slot->err = uint32_t(SA_ERR_BAD_SEQLENS);
@@ -547,9 +554,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
 
   uint8_t* mine = smem + warp * C::WARP_SMEM;
   Warp<C, FULL> x{a, lane, lane >> 2, lane & 3, mine, mine + C::FRAGS, bar, ctl, slot};
-  x.pe = min(a.c.page, KB);
-  x.log2pe = min(a.c.log2page, 6);
-  x.recS = x.pe * (a.c.d / 2 + a.c.d / 16);
+  constexpr int KB = C::KB, NR = C::NR;
   const int g = x.g, t4 = x.t4, d = FULL ? C::D : a.c.d;
   const float c2 = a.scale * kLog2e;
 
@@ -558,8 +563,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
   cur.te = te;
   {
     int64_t rem;
-    find_tile<C::THREADS>(a, pre, chunk, tb, lane, cur.b, rem);
-    set_piece(a, cur, user_sizes(a, cur.b), rem, lane);
+    find_tile<C>(a, pre, chunk, tb, lane, cur.b, rem);
+    set_piece<C>(a, cur, user_sizes<C>(a, cur.b), rem, lane);
   }
   if (lane == 0) {
     Piece p{cur.seg0, cur.seg1, cur.b, cur.h, cur.rt, 0};
@@ -570,7 +575,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
   bool more = true;
   auto settle = [&]() {  // move `ahead` to a block that exists
     while (more && akb >= ahead.kb1) {
-      more = next_piece(a, ahead, lane);
+      more = next_piece<C>(a, ahead, lane);
       akb = ahead.kb0;
     }
   };
@@ -586,45 +591,75 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
   produce();
   produce();
 
+  const T* q = static_cast<const T*>(a.q);
   for (bool have = true; have && x.ok;) {
-    // rows of this piece
-    const int r0 = cur.rt * ROWS + g, r1 = r0 + 8;
-    const int64_t q_t0 = cur.q0 + r0 / a.G, q_t1 = cur.q0 + r1 / a.G;
-    const int hd0 = cur.h * a.G + r0 % a.G, hd1 = cur.h * a.G + r1 % a.G;
-    const bool v0 = r0 < cur.rows, v1 = r1 < cur.rows;
-    int lo0 = 0, hi0 = 0x7fffffff, lo1 = 0, hi1 = 0x7fffffff;
-    if (v0) row_window(a, q_t0, cur.len, lo0, hi0);
-    if (v1) row_window(a, q_t1, cur.len, lo1, hi1);
-    const int lo_most = __reduce_max_sync(0xffffffffu, max(lo0, lo1));
-    const int hi_least = __reduce_min_sync(0xffffffffu, min(hi0, hi1));
-    __syncwarp();
-    if (cur.kb0 < cur.kb1) {
-      const T* q = static_cast<const T*>(a.q);
-      x.load_frags(q, v0 ? q_t0 * a.q_row + hd0 * a.q_head : -1, v1 ? q_t1 * a.q_row + hd1 * a.q_head : -1, x.frag);
-    }
-    const int64_t o0 = (q_t0 * a.Hq + hd0) * d, o1 = (q_t1 * a.Hq + hd1) * d;  // rows of the dense tensors
-    float D0 = 0.f, D1 = 0.f, L0 = 0.f, L1 = 0.f;
-    if constexpr (C::BWD) {
-      const T* dout = static_cast<const T*>(a.dout);
-      const T* out = static_cast<const T*>(a.out);
-      if (cur.kb0 < cur.kb1) x.load_frags(dout, v0 ? o0 : -1, v1 ? o1 : -1, x.frag + C::NS * C::FRAG);
-      for (int c = (C::D / 4) * t4; c < (C::D / 4) * (t4 + 1) && c < d; ++c) {
-        if (v0) D0 = fmaf(ld_f32(dout + o0 + c), ld_f32(out + o0 + c), D0);
-        if (v1) D1 = fmaf(ld_f32(dout + o1 + c), ld_f32(out + o1 + c), D1);
-      }
-      D0 += __shfl_xor_sync(0xffffffffu, D0, 1);
-      D0 += __shfl_xor_sync(0xffffffffu, D0, 2);
-      D1 += __shfl_xor_sync(0xffffffffu, D1, 1);
-      D1 += __shfl_xor_sync(0xffffffffu, D1, 2);
-      if (v0) L0 = a.lse[q_t0 * a.Hq + hd0] * kLog2e;
-      if (v1) L1 = a.lse[q_t1 * a.Hq + hd1] * kLog2e;
-    }
-    __syncwarp();
-
-    float acc[C::NT][4];
+    // Row g of each column tile feeds the products; rows 2t and 2t + 1 are this lane's in
+    // the accumulators (their windows, statistics and sums).
+    int64_t q_at[NR];
+    int lo[NR][2], hi[NR][2];
+    float D_[NR][2], L[NR][2];
+    int lo_most = 0, hi_least = 0x7fffffff;
 #pragma unroll
-    for (int i = 0; i < C::NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    for (int n = 0; n < NR; ++n) {
+      const int r = cur.rt * C::ROWS + 8 * n + g;
+      q_at[n] = r < cur.rows ? (cur.q0 + r / a.G) * a.q_row + (cur.h * a.G + r % a.G) * a.q_head : -1;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int s = cur.rt * C::ROWS + 8 * n + 2 * t4 + e;
+        lo[n][e] = 0, hi[n][e] = 0x7fffffff;
+        if (s < cur.rows) row_window(a, cur.q0 + s / a.G, cur.len, lo[n][e], hi[n][e]);
+        lo_most = max(lo_most, lo[n][e]);
+        hi_least = min(hi_least, hi[n][e]);
+        D_[n][e] = L[n][e] = 0.f;
+      }
+    }
+    lo_most = __reduce_max_sync(0xffffffffu, lo_most);
+    hi_least = __reduce_min_sync(0xffffffffu, hi_least);
+    // row i of this lane's: element offset in the dense tensors / d, or -1
+    auto dense = [&](int i) {
+      const int r = cur.rt * C::ROWS + i;
+      return r < cur.rows ? (cur.q0 + r / a.G) * a.Hq + cur.h * a.G + r % a.G : int64_t(-1);
+    };
+    if (cur.kb0 < cur.kb1) {
+      x.load_frags(q, q_at, x.frag);
+      if constexpr (C::BWD) {
+        const T* dout = static_cast<const T*>(a.dout);
+        const T* out = static_cast<const T*>(a.out);
+        int64_t o_at[NR];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          const int64_t o = dense(8 * n + g);
+          o_at[n] = o < 0 ? -1 : o * d;
+          float s = 0.f;
+          if (o >= 0)
+            for (int c = (C::D / 4) * t4; c < (C::D / 4) * (t4 + 1) && c < d; c += Vec<T>::n) {
+              float u[Vec<T>::n], v[Vec<T>::n];
+              Vec<T>::load(dout + o * d + c, u);
+              Vec<T>::load(out + o * d + c, v);
+#pragma unroll
+              for (int k = 0; k < Vec<T>::n; ++k) s = fmaf(u[k], v[k], s);
+            }
+          s += __shfl_xor_sync(0xffffffffu, s, 1);
+          s += __shfl_xor_sync(0xffffffffu, s, 2);  // row g's sum in its four lanes
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            D_[n][e] = __shfl_sync(0xffffffffu, s, 4 * (2 * t4 + e));
+            const int64_t oe = dense(8 * n + 2 * t4 + e);
+            if (oe >= 0) L[n][e] = a.lse[oe] * kLog2e;
+          }
+        }
+        x.load_frags(dout, o_at, x.frag + C::NS * C::FRAG);
+      }
+    }
+
+    float acc[C::MT][NR][4], m[NR][2], l[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+    }
 
     for (int kb = cur.kb0; kb < cur.kb1; ++kb) {
       const uint32_t s = x.used & 1u;
@@ -633,96 +668,104 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
       const uint8_t* st = x.ring + s * C::STAGE;
       const int k0 = kb * KB;
       const bool inside = k0 >= lo_most && k0 + KB <= hi_least;
+      // accumulator element e of key tile i: key 16 i + 8 (e / 2) + key_of(g), row 2t + e % 2
+      auto key = [&](int i, int e) { return k0 + 16 * i + 8 * (e >> 1) + key_of(g); };
       if constexpr (!C::BWD) {
-        float S[KB / 8][4];
-        x.template contract<KB / 8>(st, 0, 0, x.frag, S);
-        float b0 = -INFINITY, b1 = -INFINITY;
+        float S[KB / 16][NR][4];
+        x.template contract<KB / 16>(st, 0, 0, x.frag, S);
+        bool moved = false;
+        float nm[NR][2], z[NR][2];
 #pragma unroll
-        for (int j = 0; j < KB / 8; ++j) {
+        for (int n = 0; n < NR; ++n) {
+          float b[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) S[j][e] *= c2;
-          if (!inside) {
+          for (int i = 0; i < KB / 16; ++i) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int k = k0 + 8 * j + key_of(2 * t4 + e);
-              if (k < lo0 || k >= hi0) S[j][e] = -INFINITY;
-              if (k < lo1 || k >= hi1) S[j][2 + e] = -INFINITY;
+            for (int e = 0; e < 4; ++e) {
+              S[i][n][e] *= c2;
+              if (!inside && (key(i, e) < lo[n][e & 1] || key(i, e) >= hi[n][e & 1])) S[i][n][e] = -INFINITY;
             }
+            b[0] = fmax3(b[0], S[i][n][0], S[i][n][2]);
+            b[1] = fmax3(b[1], S[i][n][1], S[i][n][3]);
           }
-          b0 = fmax3(b0, S[j][0], S[j][1]);
-          b1 = fmax3(b1, S[j][2], S[j][3]);
-        }
-        b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 1));
-        b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 2));
-        b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 1));
-        b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 2));
-        const float n0 = fmaxf(m0, b0), n1 = fmaxf(m1, b1);
-        // nothing seen yet: shift by zero, so that 2^(-inf) = 0 and no inf - inf appears
-        const float z0 = n0 == -INFINITY ? 0.f : n0, z1 = n1 == -INFINITY ? 0.f : n1;
-        if (__any_sync(0xffffffffu, n0 != m0 || n1 != m1)) {
-          const float f0 = ex2(m0 - z0), f1 = ex2(m1 - z1);
-          l0 *= f0;
-          l1 *= f1;
 #pragma unroll
-          for (int i = 0; i < C::NT; ++i) {
-            acc[i][0] *= f0, acc[i][1] *= f0;
-            acc[i][2] *= f1, acc[i][3] *= f1;
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int o = 4; o <= 16; o <<= 1) b[e] = fmaxf(b[e], __shfl_xor_sync(0xffffffffu, b[e], o));
+            nm[n][e] = fmaxf(m[n][e], b[e]);
+            // nothing seen yet: shift by zero, so that 2^(-inf) = 0 and no inf - inf appears
+            z[n][e] = nm[n][e] == -INFINITY ? 0.f : nm[n][e];
+            moved = moved || nm[n][e] != m[n][e];
           }
-          m0 = n0;
-          m1 = n1;
         }
-        const float sh0 = z0 - kLift, sh1 = z1 - kLift;
+        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-        for (int jj = 0; jj < KB / 16; ++jj) {
-          uint32_t A[C::NP][4];
+          for (int n = 0; n < NR; ++n) {
+            const float f0 = ex2(m[n][0] - z[n][0]), f1 = ex2(m[n][1] - z[n][1]);
+            l[n][0] *= f0;
+            l[n][1] *= f1;
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            float* p = S[2 * jj + u];
-            p[0] = ex2(p[0] - sh0), p[1] = ex2(p[1] - sh0);
-            p[2] = ex2(p[2] - sh1), p[3] = ex2(p[3] - sh1);
-            l0 += p[0] + p[1];
-            l1 += p[2] + p[3];
-            A[0][2 * u] = pack_f16(p[0], p[1]);
-            A[0][2 * u + 1] = pack_f16(p[2], p[3]);
-            if constexpr (C::NP == 2) {
-              const float2 f = unpack_f16(A[0][2 * u]), e = unpack_f16(A[0][2 * u + 1]);
-              A[1][2 * u] = pack_f16(p[0] - f.x, p[1] - f.y);
-              A[1][2 * u + 1] = pack_f16(p[2] - e.x, p[3] - e.y);
+            for (int i = 0; i < C::MT; ++i) {
+              acc[i][n][0] *= f0, acc[i][n][1] *= f1;
+              acc[i][n][2] *= f0, acc[i][n][3] *= f1;
             }
+            m[n][0] = nm[n][0];
+            m[n][1] = nm[n][1];
           }
-          x.template combine<true, C::NP>(st, jj, 1, A, acc, inside, cur.vis0 - k0, cur.vis1 - k0);
         }
-      } else {
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          float S[4][4], P[4][4];
-          x.template contract<4>(st, 4 * half, 0, x.frag, S);
-          x.template contract<4>(st, 4 * half, 1, x.frag + C::NS * C::FRAG, P);
 #pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            uint32_t A[C::NS][4];
+        for (int i = 0; i < KB / 16; ++i) {
+          uint32_t B[NR][C::NP][2];
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            float* p = S[i][n];
+            const float sh0 = z[n][0] - kLift, sh1 = z[n][1] - kLift;
+            p[0] = ex2(p[0] - sh0), p[1] = ex2(p[1] - sh1);
+            p[2] = ex2(p[2] - sh0), p[3] = ex2(p[3] - sh1);
+            l[n][0] += p[0] + p[2];
+            l[n][1] += p[1] + p[3];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              const int j = 2 * jj + u;
+              const uint32_t h = pack_f16(p[2 * u], p[2 * u + 1]);
+              B[n][0][u] = transpose8x8(h);
+              if constexpr (C::NP == 2) {
+                const float2 f = unpack_f16(h);
+                B[n][1][u] = transpose8x8(pack_f16(p[2 * u] - f.x, p[2 * u + 1] - f.y));
+              }
+            }
+          }
+          x.template combine<true, C::NP>(st, i, 1, B, acc, inside, cur.vis0 - k0, cur.vis1 - k0);
+        }
+      } else {
+        constexpr int HM = KB / 32;  // half a block at a time: two products' scores are live
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          float S[HM][NR][4], P[HM][NR][4];
+          x.template contract<HM>(st, HM * half, 0, x.frag, S);
+          x.template contract<HM>(st, HM * half, 1, x.frag + C::NS * C::FRAG, P);
+#pragma unroll
+          for (int i = 0; i < HM; ++i) {
+            uint32_t B[NR][C::NS][2];
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
               float p[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const int k = k0 + 32 * half + 8 * j + key_of(2 * t4 + (e & 1));
-                const bool see = inside || (e < 2 ? k >= lo0 && k < hi0 : k >= lo1 && k < hi1);
-                const float w = ex2(fmaf(S[j][e], c2, e < 2 ? -L0 : -L1));
-                p[e] = see ? w * (P[j][e] - (e < 2 ? D0 : D1)) : 0.f;
+                const int k = key(HM * half + i, e);
+                const float w = ex2(fmaf(S[i][n][e], c2, -L[n][e & 1])) * (P[i][n][e] - D_[n][e & 1]);
+                p[e] = inside || (k >= lo[n][e & 1] && k < hi[n][e & 1]) ? w : 0.f;
               }
 #pragma unroll
-              for (int s2 = 0; s2 < C::NS; ++s2) {
-                A[s2][2 * u] = pack_bf16(p[0], p[1]);
-                A[s2][2 * u + 1] = pack_bf16(p[2], p[3]);
-                if (s2 + 1 < C::NS) {
-                  const float2 f = unpack_bf16(A[s2][2 * u]), e = unpack_bf16(A[s2][2 * u + 1]);
-                  p[0] -= f.x, p[1] -= f.y, p[2] -= e.x, p[3] -= e.y;
+              for (int s2 = 0; s2 < C::NS; ++s2)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                  const uint32_t h = pack_bf16(p[2 * u], p[2 * u + 1]);
+                  B[n][s2][u] = transpose8x8(h);
+                  const float2 f = unpack_bf16(h);
+                  p[2 * u] -= f.x, p[2 * u + 1] -= f.y;
                 }
-              }
             }
-            x.template combine<false, C::NS>(st, 2 * half + jj, 0, A, acc, true, 0, KB);
+            x.template combine<false, C::NS>(st, HM * half + i, 0, B, acc, true, 0, KB);
           }
         }
       }
@@ -732,47 +775,47 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
     }
     if (!x.ok) break;
 
-    // the piece's end
+    // the piece's end: this lane has features [per g, per (g + 1)) of rows 2t and 2t + 1
     const bool whole = cur.seg0 >= tb && cur.seg1 <= te;
-    if constexpr (!C::BWD) {
-      l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
-      l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
-      l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
-      l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
-    }
-    float* part = a.partial + (int64_t(wk) * 2 + (tb >= cur.seg0 ? 0 : 1)) * partial_floats(C::D);
-    const float f0 = C::BWD ? a.scale : (l0 > 0.f ? 1.f / l0 : 0.f), f1 = C::BWD ? a.scale : (l1 > 0.f ? 1.f / l1 : 0.f);
+    constexpr int PER = C::D / 8;
+    float* part = a.partial + (int64_t(wk) * 2 + (tb >= cur.seg0 ? 0 : 1)) * partial_floats(C::ROWS, C::D);
     T* dst = static_cast<T*>(C::BWD ? a.dq : a.out);
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      if (!(half ? v1 : v0)) continue;
+    for (int n = 0; n < NR; ++n) {
 #pragma unroll
-      for (int i = 0; i < C::LW; ++i) {
-        // columns 2 t4 (the first half of the lane's features) and 2 t4 + 1 (the second)
-        float y[8];
-        constexpr int PER = C::NT / 8;  // words per column
-        const int col = i / PER, n = i % PER;
-        const float f = whole ? (half ? f1 : f0) : 1.f;
+      for (int e = 0; e < 2; ++e) {
+        float sum = l[n][e];
+        if constexpr (!C::BWD) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = acc[8 * n + e][2 * half + col] * f;
-        const int c = (C::D / 4) * t4 + 8 * i;
-        if (c >= d) continue;
-        if (whole)
-          store8(dst + (half ? o1 : o0) + c, y);
-        else
-          store8(part + (g + 8 * half) * C::D + c, y);
-      }
-      if constexpr (!C::BWD) {
-        const float m = half ? m1 : m0, l = half ? l1 : l0;
-        if (t4 == 0) {
-          if (!whole)
-            *reinterpret_cast<float2*>(part + ROWS * C::D + 2 * (g + 8 * half)) = make_float2(m, l);
-          else if (a.lse)
-            a.lse[half ? q_t1 * a.Hq + hd1 : q_t0 * a.Hq + hd0] = l > 0.f ? (m + log2f(l) - kLift) * kLn2 : -INFINITY;
+          for (int o = 4; o <= 16; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        }
+        const int i = 8 * n + 2 * t4 + e;
+        const int64_t o = dense(i);
+        if (o < 0) continue;
+        const float f = !whole ? 1.f : C::BWD ? a.scale : sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int w = 0; w < PER / 8; ++w) {
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = acc[4 * w + k / 2][n][2 * (k & 1) + e] * f;
+          const int c = PER * g + 8 * w;
+          if (c >= d) continue;
+          if (whole)
+            store8(dst + o * d + c, y);
+          else
+            store8(part + i * C::D + c, y);
+        }
+        if constexpr (!C::BWD) {
+          if (g == 0) {
+            if (!whole)
+              *reinterpret_cast<float2*>(part + C::ROWS * C::D + 2 * i) = make_float2(m[n][e], sum);
+            else if (a.lse)
+              a.lse[o] = sum > 0.f ? (m[n][e] + log2f(sum) - kLift) * kLn2 : -INFINITY;
+          }
         }
       }
     }
-    have = next_piece(a, cur, lane);
+    have = next_piece<C>(a, cur, lane);
   }
   if (!x.ok) {  // no copy may still be in flight when the CTA's shared memory goes
     for (; x.used != x.issued; ++x.used) {
@@ -815,7 +858,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
   if (p.seg0 >= tb) return;
   if (range_begin(total, W, w - 1) > p.seg0) return;  // an earlier border already cut this segment
   const int first = w - 1, n = owner_of(total, W, p.seg1 - 1) - first + 1;
-  constexpr int PF = partial_floats(C::D);
+  constexpr int ROWS = C::ROWS, PF = partial_floats(ROWS, C::D);
   // the first worker's piece is its second one unless its share begins with the segment
   const float* base = a.partial + int64_t(first) * 2 * PF;
   const int first_off = range_begin(total, W, first) >= p.seg0 ? 0 : PF;
@@ -920,29 +963,35 @@ static cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, cache_join_kernel<C>, a);
 }
 
-template <int D>
-static cudaError_t run_d(const AttnArgs& a, bool bwd, cudaStream_t st) {
-  if (a.dt == SA_F32) return bwd ? run<Cfg<D, true, true>>(a, st) : run<Cfg<D, true, false>>(a, st);
-  return bwd ? run<Cfg<D, false, true>>(a, st) : run<Cfg<D, false, false>>(a, st);
+// Rows of a tile: 8 where a user's rows fit (the average over the call decides: half the
+// products and registers of 16), else 16, which reads the cache half as often.
+static bool two_tiles(int B, int64_t T, int G) { return T * G > int64_t(8) * B; }
+
+// f(configuration) for a call's sizes
+template <class F>
+static auto with_config(int d, sa_dtype dt, bool bwd, bool two, F&& f) {
+  auto rows = [&](auto D, auto f32, auto back) {
+    constexpr int W = decltype(D)::value;
+    constexpr bool X = decltype(f32)::value, Y = decltype(back)::value;
+    return two ? f(Cfg<W, X, Y, 2>{}) : f(Cfg<W, X, Y, 1>{});
+  };
+  auto dir = [&](auto D, auto f32) { return bwd ? rows(D, f32, std::true_type{}) : rows(D, f32, std::false_type{}); };
+  auto type = [&](auto D) { return dt == SA_F32 ? dir(D, std::true_type{}) : dir(D, std::false_type{}); };
+  return d > 64 ? type(std::integral_constant<int, 128>{}) : type(std::integral_constant<int, 64>{});
 }
 
-template <int D>
-static int warps(bool f32, bool bwd) {
-  if (f32) return bwd ? Cfg<D, true, true>::NWARP : Cfg<D, true, false>::NWARP;
-  return bwd ? Cfg<D, false, true>::NWARP : Cfg<D, false, false>::NWARP;
+MmaPlan mma_plan(int sms, int B, int64_t T, int G, int d, sa_dtype dt, bool bwd) {
+  MmaPlan p;
+  p.ctas = sms;
+  p.workers = sms * with_config(d, dt, bwd, two_tiles(B, T, G), [](auto c) { return decltype(c)::NWARP; });
+  p.piece_bytes = sizeof(Piece);
+  p.partial_floats =
+      with_config(d, dt, bwd, two_tiles(B, T, G), [](auto c) { return partial_floats(decltype(c)::ROWS, decltype(c)::D); });
+  return p;
 }
-
-static bool wide(int d) { return d > 64; }
-
-int mma_workers(int sms, int d, sa_dtype dt, bool bwd, int* ctas) {
-  *ctas = sms;
-  return sms * (wide(d) ? warps<128>(dt == SA_F32, bwd) : warps<64>(dt == SA_F32, bwd));
-}
-size_t mma_piece_bytes() { return sizeof(Piece); }
-size_t mma_partial_floats(int d) { return size_t(partial_floats(wide(d) ? 128 : 64)); }
 
 cudaError_t launch_mma(const AttnArgs& a, bool bwd, cudaStream_t st) {
-  return wide(a.c.d) ? run_d<128>(a, bwd, st) : run_d<64>(a, bwd, st);
+  return with_config(a.c.d, a.dt, bwd, two_tiles(a.B, a.T, a.G), [&](auto c) { return run<decltype(c)>(a, st); });
 }
 
 }  // namespace cache
