@@ -69,12 +69,17 @@ cudaError_t launch_write(const RowArgs& a, cudaStream_t st);
 cudaError_t launch_read(const RowArgs& a, cudaStream_t st);
 
 // Warp-level kernels (sa_cache_mma.cu)
-struct MmaPlan {
+struct AttnPlan {
   int ctas, workers;
   size_t piece_bytes, partial_floats;  // per worker; per worker and slot
 };
-MmaPlan mma_plan(int sms, int B, int64_t T, int G, int d, sa_dtype dt, bool bwd);
+AttnPlan mma_plan(int sms, int B, int64_t T, int G, int d, sa_dtype dt, bool bwd);
 cudaError_t launch_mma(const AttnArgs& a, bool bwd, cudaStream_t st);
+
+// tcgen05 kernels (sa_cache_tc.cu)
+bool tc_supported(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd);
+AttnPlan tc_plan(int sms, int d);
+cudaError_t launch_tc(const AttnArgs& a, bool bwd, cudaStream_t st);
 
 // ------------------------------------------------------------------ arithmetic
 #ifdef __CUDACC__

@@ -65,10 +65,10 @@ struct Layout {
   int workers, ctas;
 };
 
-Layout attn_layout(int B, int64_t T, int G, int H, int d, sa_dtype dt, int64_t max_tokens, bool bwd) {
+Layout attn_layout(int B, int64_t T, int G, int d, sa_dtype dt, bool bwd, bool tc) {
   Layout l{};
-  const sa::cache::MmaPlan p = sa::cache::mma_plan(sa::tcc::device_sm_count(), B, T, G, d, dt, bwd);
-  (void)H, (void)max_tokens;
+  const int sms = sa::tcc::device_sm_count();
+  const sa::cache::AttnPlan p = tc ? sa::cache::tc_plan(sms, d) : sa::cache::mma_plan(sms, B, T, G, d, dt, bwd);
   l.ctas = p.ctas;
   l.workers = p.workers;
   size_t off = sizeof(sa::WsHeader);
@@ -96,7 +96,8 @@ sa_status attn(AttnArgs& a, const void* q, int64_t q_row, int64_t q_head, const 
   if (!attn_sizes_ok(B, T, Hq, H, d, dt)) return SA_ERR_UNSUPPORTED;
   if (T > 0 && (!q || !aligned(q, 16))) return SA_ERR_INVALID_ARG;
   if (!stride_ok(q_row, dt) || !stride_ok(q_head, dt)) return SA_ERR_INVALID_ARG;
-  const Layout l = attn_layout(B, T, Hq / H, H, d, dt, int64_t(max_pages) * page, bwd);
+  const bool tc = sa::cache::tc_supported(B, T, Hq / H, d, dt, scale, bwd);
+  const Layout l = attn_layout(B, T, Hq / H, d, dt, bwd, tc);
   SA_TRY(check_workspace(ws, ws_bytes, l.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* base = static_cast<char*>(ws);
@@ -121,7 +122,7 @@ sa_status attn(AttnArgs& a, const void* q, int64_t q_row, int64_t q_head, const 
   a.piece = base + l.piece;
   a.partial = reinterpret_cast<float*>(base + l.partial);
   a.wait_limit_ns = sa::wait_limit_ns();
-  const cudaError_t e = sa::cache::launch_mma(a, bwd, st);
+  const cudaError_t e = tc ? sa::cache::launch_tc(a, bwd, st) : sa::cache::launch_mma(a, bwd, st);
   sa::count_launches(2);
   return e == cudaSuccess ? SA_OK : SA_ERR_CUDA;
 }
@@ -188,7 +189,11 @@ sa_status sa_cache_read(const void* pool, int64_t n_pages, int page, const int32
 
 size_t sa_cache_attn_workspace_size(int B, int64_t T, int Hq, int H, int d, sa_dtype dt, int64_t max_tokens, int bwd) {
   if (!attn_sizes_ok(B, T, Hq, H, d, dt) || max_tokens < 0) return 0;
-  return attn_layout(B, T, Hq / H, H, d, dt, max_tokens, bwd != 0).total;
+  // enough for either kernel: the scale, not known here, has a say
+  const size_t x = attn_layout(B, T, Hq / H, d, dt, bwd != 0, false).total;
+  if (!sa::cache::tc_supported(B, T, Hq / H, d, dt, 1.f, bwd != 0)) return x;
+  const size_t y = attn_layout(B, T, Hq / H, d, dt, bwd != 0, true).total;
+  return x > y ? x : y;
 }
 
 sa_status sa_cache_attn_fwd(const void* q, int64_t q_row_stride, int64_t q_head_stride, const int32_t* cu_q, int B,
@@ -222,6 +227,7 @@ sa_status sa_cache_attn_bwd(const void* q, int64_t q_row_stride, int64_t q_head_
 
 const char* sa_cache_attn_kernel_name(int B, int64_t T, int Hq, int H, int d, float scale, sa_dtype dt, int bwd) {
   if (!attn_sizes_ok(B, T, Hq, H, d, dt) || !std::isfinite(scale)) return "unsupported";
+  if (sa::cache::tc_supported(B, T, Hq / H, d, dt, scale, bwd != 0)) return bwd ? "tc5_cache_attn_bwd" : "tc5_cache_attn_fwd";
   return bwd ? "mma_cache_attn_bwd" : "mma_cache_attn_fwd";
 }
 

@@ -1,0 +1,575 @@
+// Attention over the 4-bit cache on tcgen05, for many queries of a user (the candidates
+// of a request, the requests of a training group times the query heads of a cached
+// head): bf16, d in {64, 128}, a positive scale.
+//
+// A CTA holds up to 256 query rows as two halves of 128 and walks 128 cached positions
+// at a time.  The products need 16-bit operands in shared memory, so four warps turn a
+// block's 4-bit words into them once for all the rows:
+//     S = Q K^T   (M = 128 rows, N = 128 positions, bf16)       accumulated in TMEM
+//     P = 2^(S - shift) in registers, float16, back over S in TMEM
+//     O += P V    (M = 128, N = d, K = 128 positions, float16; P read from TMEM)
+// Dequantising costs about 16 instructions a word of 8 features; spread over 256 rows it
+// stays below the products.  The two warpgroups of the softmax take the units (block,
+// half) in turn, so that one's exponentials run under the other's products.  A row tile
+// of at most 128 rows has one half only: its blocks alternate between the warpgroups,
+// each with its own O and shift, and the two are added at the end.
+//
+// The shift of a row is changed lazily, when a block's maximum passes the shift in use
+// by more than 3 (log2 units), and only then is the row of O rescaled in TMEM; S of a
+// block is issued after the product that read the warpgroup's last weights, so when it
+// arrives O is at rest.
+//
+// Warp roles: 0 copies pages' codes and scales into a ring (bulk copies), 1 issues the
+// products, 2 and 3 load the halves' query rows, 4..7 dequantise, 8..15 softmax and
+// results.  Every wait is bounded (sa_ptx.cuh).
+#include "sa_cache.cuh"
+#include "sa_cache_walk.cuh"
+#include "sa_tc_common.cuh"
+
+namespace sa {
+namespace cache {
+
+using namespace ptx;
+
+constexpr float kLazy = 3.f;  // with kLift = 12 a weight stays below 2^15, inside float16
+
+template <int D_>
+struct TcFwd {
+  static constexpr int D = D_;
+  static constexpr bool F32 = false, BWD = false;
+  static constexpr int ROWS = 256, HALF = 128, KB = 128;
+  static constexpr int NWARP = 16, THREADS = 512;
+  static constexpr int TILE = 128 * D * 2;  // 128 rows of 16-bit values, [D / 64][128][128 bytes]
+  static constexpr int NSLOT = 3, NRAW = 5;
+  static constexpr int RAW = KB * (D / 2 + D / 16);
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_RING = OFF_Q + 2 * TILE;
+  static constexpr int OFF_RAW = OFF_RING + NSLOT * TILE;
+  static constexpr int OFF_X = OFF_RAW + NRAW * RAW;  // exchange between the warpgroups: 32 columns + statistics
+  static constexpr int X_BYTES = 128 * 32 * 4 + 128 * 8;
+  static constexpr int OFF_SCAN = OFF_X;  // used before anything is exchanged
+  static_assert((THREADS + 2) * 8 <= X_BYTES, "the scan shares the exchange area");
+  static constexpr int OFF_BAR = OFF_X + X_BYTES;
+  static constexpr int NBAR = 2 * NSLOT + 2 * NRAW + 2 * 6 + 3;
+  static constexpr int OFF_CTL = OFF_BAR + NBAR * 8;
+  static constexpr int SMEM = OFF_CTL + 32;
+  static_assert(SMEM <= 232448, "shared memory budget");
+  static constexpr int S_COL = 0, O_COL = 256;  // two halves each
+};
+
+// Instruction descriptor of kind::f16 with float16 A and B, fp32 D.
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) {
+  return (1u << 4) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// What all roles derive from a piece: its blocks, and which warpgroup takes what.  Units
+// alternate between the warpgroups over the whole share; `parity` is the first one's.
+struct Units {
+  int n;        // blocks
+  int halves;   // 1 or 2
+  int parity;
+  __device__ __forceinline__ Units(const Walk& w, int parity_)
+      : n(w.kb1 > w.kb0 ? w.kb1 - w.kb0 : 0), halves(w.weight), parity(parity_) {}
+  __device__ __forceinline__ int count() const { return n * halves; }
+  // warpgroup wg's blocks: first, first + step, ...
+  __device__ __forceinline__ int first(int wg) const { return halves == 2 ? 0 : wg ^ parity; }
+  __device__ __forceinline__ int step() const { return halves == 2 ? 1 : 2; }
+  __device__ __forceinline__ int mine(int wg) const { return n > first(wg) ? (n - first(wg) + step() - 1) / step() : 0; }
+  // the half of the rows that warpgroup wg has
+  __device__ __forceinline__ int half(int wg) const { return halves == 2 ? wg ^ parity : 0; }
+  __device__ __forceinline__ int next_parity() const { return (parity + count()) & 1; }
+};
+
+template <int D>
+__global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_constant__ AttnArgs a) {
+  using C = TcFwd<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  WsHeader* slot = a.slots + blockIdx.x;
+  volatile int* ctl = reinterpret_cast<volatile int*>(smem + C::OFF_CTL);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_CTL + 16);
+  const uint32_t sb = smem_u32(smem), bar0 = sb + C::OFF_BAR;
+  auto slot_full = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto slot_empty = [&](uint32_t s) { return bar0 + 8u * (C::NSLOT + s); };
+  auto raw_full = [&](uint32_t s) { return bar0 + 8u * (2 * C::NSLOT + s); };
+  auto raw_empty = [&](uint32_t s) { return bar0 + 8u * (2 * C::NSLOT + C::NRAW + s); };
+  const uint32_t per = bar0 + 8u * (2 * C::NSLOT + 2 * C::NRAW);
+  auto s_full = [&](int g) { return per + 8u * g; };
+  auto p_full = [&](int g) { return per + 8u * (2 + g); };
+  auto o_full = [&](int g) { return per + 8u * (4 + g); };
+  auto o_empty = [&](int g) { return per + 8u * (6 + g); };
+  auto q_full = [&](int g) { return per + 8u * (8 + g); };
+  auto q_empty = [&](int g) { return per + 8u * (10 + g); };
+  const uint32_t x_full = per + 8u * 12, x_empty = per + 8u * 13, drain = per + 8u * 14;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::NBAR; ++i) {
+      const int p = i - 2 * C::NSLOT - 2 * C::NRAW;  // barriers of the halves
+      uint32_t n = 1;
+      if (i < C::NSLOT) n = 4;                                                       // slot_full: the dequantising warps
+      if (i >= 2 * C::NSLOT + C::NRAW && i < 2 * C::NSLOT + 2 * C::NRAW) n = 4;      // raw_empty
+      if (p == 2 || p == 3 || p == 6 || p == 7 || p == 12 || p == 13) n = 4;         // a softmax warpgroup's warps
+      mbar_init(bar0 + 8u * i, n);
+    }
+    slot->err = 0;
+    slot->timeout_site = 0;
+    slot->wait_limit_ns = a.wait_limit_ns;
+    wait_ctl_init(ctl, slot);
+    fence_mbar_init();
+  }
+  int64_t* pre = reinterpret_cast<int64_t*>(smem + C::OFF_SCAN);
+  const int chunk = (a.B + C::THREADS - 1) / C::THREADS;
+  const int64_t total = scan_users<C>(a, pre, chunk);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    ws_header(a.ws)->tiles_per_head = total;
+    if (total < 0) slot->err = uint32_t(SA_ERR_BAD_SEQLENS);
+  }
+  asm volatile("griddepcontrol.launch_dependents;");
+  if (total <= 0) return;
+  const int W = shares(a, total), wk = int(blockIdx.x);
+  if (wk >= W) return;
+  if (sb & 1023u) {  // the swizzled operands need 1024-byte alignment
+    if (threadIdx.x == 0) slot->err = uint32_t(SA_ERR_CUDA);
+    return;
+  }
+  const int64_t tb = range_begin(total, W, wk), te = range_begin(total, W, wk + 1);
+  Walk cur;
+  cur.t = tb;
+  cur.te = te;
+  {
+    int64_t rem;
+    find_tile<C>(a, pre, chunk, tb, lane, cur.b, rem);
+    set_piece<C>(a, cur, user_sizes<C>(a, cur.b), rem, lane);
+  }
+  if (threadIdx.x == 0) {
+    Piece p{cur.seg0, cur.seg1, cur.b, cur.h, cur.rt, 0};
+    static_cast<Piece*>(a.piece)[wk] = p;
+  }
+  if (warp == 2) tmem_alloc(smem_u32(tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  bool ok = true;
+  auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site) {
+    ok = __all_sync(0xffffffffu, mbar_wait(bar, parity & 1u, ctl, slot, site));
+    return ok;
+  };
+
+  if (warp < 4) {
+    setmaxnreg_dec<80>();
+    if (warp == 0) {
+      // ------------------------------------------------------------- copies
+      // lane 2 p + i copies the codes (i = 0) or scales of the block's p-th page
+      uint32_t c = 0;  // keys and values of block after block
+      const int n = min(a.c.page, C::KB), part = lane & 1, off = (lane >> 1) * n;
+      const int rb = part ? D / 16 : D / 2;
+      auto page_of = [&](const Walk& w, int kb) {
+        const int p0 = kb * C::KB + off;
+        if (off >= C::KB || p0 >= w.vis1 || p0 + n <= w.vis0) return -2;  // nothing to copy
+        return a.c.table[int64_t(w.b) * a.c.max_pages + (p0 >> a.c.log2page)];
+      };
+      for (bool have = true; have && ok;) {
+        int pid = cur.kb0 < cur.kb1 ? page_of(cur, cur.kb0) : -2;
+        for (int kb = cur.kb0; kb < cur.kb1 && ok; ++kb) {
+          bool want = pid != -2;
+          if (want && (pid < 0 || pid >= a.c.n_pages)) {
+            atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
+            want = false;
+          }
+          const int64_t rec = want ? a.c.record(pid, cur.h) : 0;
+          const int first = (kb * C::KB + off) & (a.c.page - 1);
+          const uint32_t bytes = want ? uint32_t(n * rb) : 0u;
+          const uint32_t sum = __reduce_add_sync(0xffffffffu, bytes);
+          if (kb + 1 < cur.kb1) pid = page_of(cur, kb + 1);
+          for (int kv = 0; kv < 2; ++kv, ++c) {
+            const uint32_t s = c % C::NRAW;
+            if (c >= C::NRAW && !wait(raw_empty(s), c / C::NRAW + 1, 0xD01u)) break;
+            if (lane == 0) mbar_arrive_expect_tx(raw_full(s), sum);
+            __syncwarp();
+            if (want)
+              bulk_copy(sb + C::OFF_RAW + s * C::RAW + (part ? C::KB * (D / 2) : 0) + off * rb,
+                        a.c.pool + rec + kv * a.c.rec + (part ? a.c.page * (D / 2) : 0) + first * rb, bytes, raw_full(s));
+          }
+        }
+        have = next_piece<C>(a, cur, lane);
+      }
+      if (!ok)  // no copy may be in flight when the CTA's shared memory goes
+        for (uint32_t k = c > C::NRAW ? c - C::NRAW : 0; k < c; ++k)
+          tcc::mbar_wait_bounded(raw_full(k % C::NRAW), (k / C::NRAW) & 1u, 200000000ull);
+    } else if (warp == 1) {
+      // ----------------------------------------------------------- products
+      constexpr uint32_t idS = idesc_bf16(128, C::KB, 0, 0);  // Q (K-major) x K^T (K-major)
+      constexpr uint32_t idO = idesc_f16(128, D, 0, 1);       // P (TMEM) x V (MN-major)
+      // What the second product of a unit needs to know, kept until its weights are there.
+      struct Unit {
+        uint32_t v;  // count of its value tile in the ring
+        bool first, last, last_v, on;
+      };
+      Unit q0{}, q1{};
+      uint32_t u = 0, pv = 0, tile = 0;  // units issued, units finished, blocks begun
+      uint32_t qn[2] = {0, 0}, on[2] = {0, 0}, pn[2] = {0, 0};
+      int i = 0;  // unit within the piece
+      bool have = true;
+      Units un(cur, 0);
+      auto settle = [&]() {
+        while (have && i >= un.count()) {
+          have = next_piece<C>(a, cur, lane);
+          un = Units(cur, un.next_parity());
+          i = 0;
+        }
+      };
+      settle();
+      auto scores = [&](Unit& f) {  // S of the next unit
+        f.on = false;
+        if (!have) return;
+        const int g = int(u & 1u), blk = un.halves == 2 ? i >> 1 : i;
+        const bool first_k = un.halves == 1 || !(i & 1), last_k = un.halves == 1 || (i & 1);
+        f.first = blk == un.first(g);
+        f.last = blk + un.step() >= un.n;
+        f.last_v = last_k;
+        f.v = 2 * tile + 1;
+        f.on = true;
+        const uint32_t k = 2 * tile;
+        if (first_k && !wait(slot_full(k % C::NSLOT), k / C::NSLOT, 0xD11u)) return;
+        if (f.first && !wait(q_full(g), qn[g]++, 0xD12u)) return;
+        tc_fence_after();
+        if (lane == 0) {
+          const uint32_t kq = sb + C::OFF_Q + g * C::TILE, kk = sb + C::OFF_RING + (k % C::NSLOT) * C::TILE;
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s)
+            umma_ss(tmem + C::S_COL + g * 128, sdesc(kq + (s >> 2) * 16384 + (s & 3) * 32, 16, 1024),
+                    sdesc(kk + (s >> 2) * 16384 + (s & 3) * 32, 16, 1024), idS, s > 0 ? 1u : 0u);
+          umma_commit(s_full(g));
+          if (last_k) umma_commit(slot_empty(k % C::NSLOT));
+          if (f.last) umma_commit(q_empty(g));
+        }
+        if (last_k) ++tile;
+        ++u;
+        ++i;
+        settle();
+      };
+      scores(q0);
+      if (ok) scores(q1);
+      while (ok && q0.on) {
+        const int g = int(pv & 1u);
+        if (!wait(p_full(g), pn[g]++, 0xD13u)) break;
+        if (!wait(slot_full(q0.v % C::NSLOT), q0.v / C::NSLOT, 0xD14u)) break;
+        if (q0.first) {
+          if (on[g] > 0 && !wait(o_empty(g), on[g] - 1, 0xD15u)) break;
+          ++on[g];
+        }
+        tc_fence_after();
+        if (lane == 0) {
+          const uint32_t vv = sb + C::OFF_RING + (q0.v % C::NSLOT) * C::TILE;
+#pragma unroll
+          for (int s = 0; s < C::KB / 16; ++s)
+            umma_ts(tmem + C::O_COL + g * 128, tmem + C::S_COL + g * 128 + 8 * s, sdesc(vv + s * 2048, 16384, 1024), idO,
+                    q0.first && s == 0 ? 0u : 1u);
+          if (q0.last_v) umma_commit(slot_empty(q0.v % C::NSLOT));
+          if (q0.last) umma_commit(o_full(g));
+        }
+        ++pv;
+        q0 = q1;
+        scores(q1);
+      }
+      if (lane == 0) {
+        umma_commit(drain);  // no product may still run when TMEM is released
+        tcc::mbar_wait_bounded(drain, 0, 200000000ull);
+      }
+    } else {
+      // ------------------------------------------------- query rows of half `g`
+      const int g = warp - 2;
+      uint32_t loads = 0;
+      Units un(cur, 0);
+      for (bool have = true; have && ok;) {
+        if (un.mine(g) > 0) {
+          if (loads > 0 && !wait(q_empty(g), loads - 1, 0xD21u)) break;
+          constexpr int CH = D / 8;  // 16-byte pieces of a row
+          const int r0 = cur.rt * C::ROWS + un.half(g) * 128;
+          const uint32_t dst = sb + C::OFF_Q + g * C::TILE;
+          const char* q = static_cast<const char*>(a.q);
+          const int c = lane % CH;
+#pragma unroll 4
+          for (int r = lane / CH; r < 128; r += 32 / CH) {
+            const int row = r0 + r;
+            const bool v = row < cur.s.rows;
+            const int t = v ? row / a.G : 0, h = v ? row - t * a.G : 0;
+            cp_async16(dst + (c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4),
+                       q + 2 * ((cur.s.q0 + t) * a.q_row + (cur.h * a.G + h) * a.q_head + 8 * c), v);
+          }
+          cp_async_wait_all();
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(q_full(g));
+          ++loads;
+        }
+        have = next_piece<C>(a, cur, lane);
+        un = Units(cur, un.next_parity());
+      }
+    }
+  } else if (warp < 8) {
+    setmaxnreg_dec<64>();
+    // ------------------------------------------------------- dequantisation
+    // Lane (r, q) = (lane / 4, lane % 4) takes a quarter of row 8 w + r: two or four
+    // words.  With 128 features the quarters of the two 64-feature halves go in
+    // swapped order, so that a store's eight lanes hit eight different banks.
+    const int w = warp - 4, q4 = lane & 3;
+    uint32_t c = 0;
+    for (bool have = true; have && ok;) {
+      for (int kb = cur.kb0; kb < cur.kb1 && ok; ++kb) {
+        for (int kv = 0; kv < 2; ++kv, ++c) {
+          const uint32_t rs = c % C::NRAW, s = c % C::NSLOT;
+          if (!wait(raw_full(rs), c / C::NRAW, 0xD31u)) break;
+          if (c >= C::NSLOT && !wait(slot_empty(s), c / C::NSLOT + 1, 0xD32u)) break;
+          const uint8_t* raw = smem + C::OFF_RAW + rs * C::RAW;
+          uint8_t* out = smem + C::OFF_RING + s * C::TILE;
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const int r = 32 * p + 8 * w + (lane >> 2);
+            constexpr int NW = D / 32;
+            uint32_t x[NW], code;
+            if constexpr (D == 128) {
+              const uint4 v = *reinterpret_cast<const uint4*>(raw + r * (D / 2) + q4 * 16);
+              x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+              code = *reinterpret_cast<const uint16_t*>(raw + C::KB * (D / 2) + r * (D / 16) + 2 * q4);
+              if (q4 & 2) {
+                x[0] = v.z, x[1] = v.w, x[2] = v.x, x[3] = v.y;
+                code = __byte_perm(code, 0, 0x4401);
+              }
+            } else {
+              const uint2 v = *reinterpret_cast<const uint2*>(raw + r * (D / 2) + q4 * 8);
+              x[0] = v.x, x[1] = v.y;
+              code = raw[C::KB * (D / 2) + r * (D / 16) + q4];
+            }
+            // positions that no row of the tile sees count as zero values: what nobody
+            // wrote can read as an infinity in float16, and 0 x inf is not 0
+            const int pos = kb * C::KB + r;
+            if (kv && (pos < cur.vis0 || pos >= cur.vis1)) code = 0;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+              const int word = D == 128 ? (i ^ (q4 & 2)) : i;  // of the lane's quarter
+              const int chunk = q4 * NW + word;                // of the row: 8 features, 16 bytes
+              const uint32_t cc = ((code >> (8 * (i / 2))) & 255u) * 0x00010001u;
+              uint32_t y[4];
+              if (kv == 0)
+                values_bf16(x[i], scale_bf16(cc), y);
+              else
+                values_f16(x[i], cc << 7, y);
+              *reinterpret_cast<uint4*>(out + (chunk >> 3) * 16384 + r * 128 + (((chunk & 7) ^ (r & 7)) << 4)) =
+                  make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(slot_full(s));
+            mbar_arrive(raw_empty(rs));
+          }
+        }
+      }
+      have = next_piece<C>(a, cur, lane);
+    }
+  } else {
+    setmaxnreg_inc<184>();
+    // ----------------------------------------------------- softmax and results
+    const int g = (warp - 8) >> 2, quad = warp & 3, rr = 32 * quad + lane;
+    const uint32_t lane_off = uint32_t(32 * quad) << 16;
+    const uint32_t tS = tmem + lane_off + C::S_COL + g * 128, tO = tmem + lane_off + C::O_COL + g * 128;
+    const float c2 = a.scale * kLog2e;
+    float* X = reinterpret_cast<float*>(smem + C::OFF_X);
+    float2* Xs = reinterpret_cast<float2*>(smem + C::OFF_X + 128 * 32 * 4);
+    uint32_t sn = 0, pieces = 0, xn = 0;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
+    Units un(cur, 0);
+    for (bool have = true; have && ok;) {
+      const int mine = un.mine(g);
+      const bool whole = cur.seg0 >= tb && cur.seg1 <= te;
+      float* part = a.partial + (int64_t(wk) * 2 + (tb >= cur.seg0 ? 0 : 1)) * partial_floats(C::ROWS, D);
+      // row i of the tile: its index among the (query, head) pairs, or -1
+      auto dense = [&](int i) {
+        const int r = cur.rt * C::ROWS + i;
+        return r < cur.s.rows ? (cur.s.q0 + r / a.G) * a.Hq + cur.h * a.G + r % a.G : int64_t(-1);
+      };
+      // 32 columns of one row, unnormalised or final
+      auto put = [&](int i, int64_t o, int col, const float* y, float f) {
+        if (o < 0) return;
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+          float z[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[e] = y[k + e] * f;
+          if (whole)
+            store8(out + o * D + col + k, z);
+          else
+            store8(part + i * D + col + k, z);
+        }
+      };
+      auto put_stat = [&](int i, int64_t o, float m, float l) {
+        if (o < 0) return;
+        if (!whole)
+          *reinterpret_cast<float2*>(part + C::ROWS * D + 2 * i) = make_float2(m, l);
+        else if (a.lse)
+          a.lse[o] = l > 0.f ? (m + log2f(l) - kLift) * kLn2 : -INFINITY;
+      };
+      if (un.n == 0 && g == 0) {  // nobody sees anything
+        float zero[32] = {};
+        for (int hf = 0; hf < un.halves; ++hf) {
+          const int i = 128 * hf + rr;
+          const int64_t o = dense(i);
+          for (int col = 0; col < D; col += 32) put(i, o, col, zero, 0.f);
+          put_stat(i, o, -INFINITY, 0.f);
+        }
+      }
+      if (mine > 0) {
+        const int i = 128 * un.half(g) + rr;
+        int lo = 0, hi = 0x7fffffff;
+        const int64_t o = dense(i);
+        if (o >= 0) row_window(a, cur.s.q0 + (cur.rt * C::ROWS + i) / a.G, cur.s.len, lo, hi);
+        float msh = -INFINITY, l = 0.f;
+        for (int b = 0; b < mine; ++b) {
+          const int k0 = (cur.kb0 + un.first(g) + b * un.step()) * C::KB;
+          if (!wait(s_full(g), sn++, 0xD41u)) break;
+          tc_fence_after();
+          float v[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, v + 32 * c);
+          tmem_ld_wait();
+          if (__any_sync(0xffffffffu, k0 < lo || k0 + C::KB > hi)) {
+            const int from = lo - k0, to = hi - k0;
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c < from || c >= to) v[c] = -INFINITY;
+          }
+          const float mt = row_max<128>(v) * c2;
+          float alpha = 1.f;
+          if (msh == -INFINITY) {
+            msh = mt;  // O and l are zero so far
+          } else if (mt > msh + kLazy) {
+            alpha = ex2(msh - mt);
+            msh = mt;
+          }
+          // nothing seen yet: any shift gives zeros
+          const float sh = msh == -INFINITY ? 0.f : msh - kLift;
+          l = l * alpha + exp2_shift_sum<128>(v, c2, sh);
+          uint32_t p[64];
+#pragma unroll
+          for (int k = 0; k < 64; ++k) {
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(v[2 * k + 1]), "f"(v[2 * k]));
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_st16(tS + 16 * c, p + 16 * c);
+          if (b > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              float y[32];
+              tmem_ld32(tO + c, y);
+              tmem_ld_wait();
+#pragma unroll
+              for (int k = 0; k < 32; ++k) y[k] *= alpha;
+              tmem_st16(tO + c, reinterpret_cast<const uint32_t*>(y));
+              tmem_st16(tO + c + 16, reinterpret_cast<const uint32_t*>(y) + 16);
+            }
+          }
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full(g));
+        }
+        if (!ok || !wait(o_full(g), pieces, 0xD42u)) break;
+        ++pieces;
+        tc_fence_after();
+        const bool both = un.halves == 1 && un.n > 1;  // the other warpgroup has the other blocks' share
+        const bool gives = both && un.first(g) == 1;
+        float m = msh, f0 = 1.f, f1 = 0.f;
+        for (int c = 0; c < D && ok; c += 32) {
+          float y[32];
+          tmem_ld32(tO + c, y);
+          tmem_ld_wait();
+          if (gives) {
+            if (xn > 0 && !wait(x_empty, xn - 1, 0xD43u)) break;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) X[k * 128 + rr] = y[k];
+            if (c == 0) Xs[rr] = make_float2(msh, l);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(x_full);
+            ++xn;
+            continue;
+          }
+          if (both) {
+            if (!wait(x_full, xn, 0xD44u)) break;
+            ++xn;
+            if (c == 0) {
+              const float2 s = Xs[rr];
+              m = fmaxf(msh, s.x);
+              f0 = msh == -INFINITY ? 0.f : ex2(msh - m);
+              f1 = s.x == -INFINITY ? 0.f : ex2(s.x - m);
+              l = l * f0 + s.y * f1;
+            }
+#pragma unroll
+            for (int k = 0; k < 32; ++k) y[k] = y[k] * f0 + X[k * 128 + rr] * f1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(x_empty);
+          }
+          put(i, o, c, y, !whole ? 1.f : l > 0.f ? 1.f / l : 0.f);
+        }
+        if (!ok) break;
+        if (!gives) put_stat(i, o, m, l);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_empty(g));
+      }
+      have = next_piece<C>(a, cur, lane);
+      un = Units(cur, un.next_parity());
+    }
+  }
+  __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int D>
+static cudaError_t run_fwd(const AttnArgs& a, cudaStream_t st) {
+  using C = TcFwd<D>;
+  const cudaError_t e =
+      cudaFuncSetAttribute(cache_tc_fwd_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  cache_tc_fwd_kernel<D><<<a.ctas, C::THREADS, C::SMEM, st>>>(a);
+  const cudaError_t e2 = cudaGetLastError();
+  return e2 != cudaSuccess ? e2 : launch_join<C>(a, st);
+}
+
+// Taken where the average user has at least 64 rows for a cached head: below that most of
+// the 128 rows of a product are padding.
+bool tc_supported(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd) {
+  if (bwd || dt != SA_BF16 || (d != 64 && d != 128) || !(scale > 0.f) || T * G < int64_t(64) * B) return false;
+  return tcc::device_is_sm103();
+}
+
+AttnPlan tc_plan(int sms, int d) {
+  AttnPlan p;
+  p.ctas = p.workers = sms;
+  p.piece_bytes = sizeof(Piece);
+  p.partial_floats = d == 128 ? partial_floats(256, 128) : partial_floats(256, 64);
+  return p;
+}
+
+cudaError_t launch_tc(const AttnArgs& a, bool, cudaStream_t st) {
+  return a.c.d == 128 ? run_fwd<128>(a, st) : run_fwd<64>(a, st);
+}
+
+}  // namespace cache
+}  // namespace sa
