@@ -19,8 +19,8 @@
 // block is issued after the product that read the warpgroup's last weights, so when it
 // arrives O is at rest.
 //
-// Warp roles: 0 copies pages' codes and scales into a ring (bulk copies), 1 issues the
-// products, 2 and 3 load the halves' query rows, 4..7 dequantise, 8..15 softmax and
+// Warp roles: 0 walks the share, publishes its pieces to the other roles and copies the
+// pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 and 3 load the halves' query rows, 4..7 dequantise, 8..15 softmax and
 // results.  Every wait is bounded (sa_ptx.cuh).
 #include "sa_cache.cuh"
 #include "sa_cache_walk.cuh"
@@ -50,8 +50,11 @@ struct TcFwd {
   static constexpr int OFF_SCAN = OFF_X;  // used before anything is exchanged
   static_assert((THREADS + 2) * 8 <= X_BYTES, "the scan shares the exchange area");
   static constexpr int OFF_BAR = OFF_X + X_BYTES;
-  static constexpr int NBAR = 2 * NSLOT + 2 * NRAW + 2 * 6 + 3;
-  static constexpr int OFF_CTL = OFF_BAR + NBAR * 8;
+  static constexpr int NPIECE = 4;    // pieces published ahead
+  static constexpr int NREADER = 15;  // warps that read them
+  static constexpr int NBAR = 2 * NSLOT + 2 * NRAW + 2 * 6 + 3 + 2 * NPIECE;
+  static constexpr int OFF_PIECE = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
+  static constexpr int OFF_CTL = OFF_PIECE + NPIECE * 64;
   static constexpr int SMEM = OFF_CTL + 32;
   static_assert(SMEM <= 232448, "shared memory budget");
   static constexpr int S_COL = 0, O_COL = 256;  // two halves each
@@ -73,14 +76,20 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// What all roles derive from a piece: its blocks, and which warpgroup takes what.  Units
+// A piece as the roles see it (64 bytes of shared memory).  Units, (block, half) pairs,
 // alternate between the warpgroups over the whole share; `parity` is the first one's.
 struct Units {
-  int n;        // blocks
-  int halves;   // 1 or 2
+  int n;         // blocks; -1: the share is done
+  int halves;    // 1 or 2
   int parity;
-  __device__ __forceinline__ Units(const Walk& w, int parity_)
-      : n(w.kb1 > w.kb0 ? w.kb1 - w.kb0 : 0), halves(w.weight), parity(parity_) {}
+  int kb0;       // first block
+  int vis0, vis1;
+  int rows;      // of the tile
+  int row0;      // of the tile within the user's rows of this head
+  int h, len;
+  int whole;     // the segment lies within this share
+  int second;    // which of the worker's two unfinished pieces it is, if not whole
+  int64_t q0;    // the user's first query
   __device__ __forceinline__ int count() const { return n * halves; }
   // warpgroup wg's blocks: first, first + step, ...
   __device__ __forceinline__ int first(int wg) const { return halves == 2 ? 0 : wg ^ parity; }
@@ -88,8 +97,79 @@ struct Units {
   __device__ __forceinline__ int mine(int wg) const { return n > first(wg) ? (n - first(wg) + step() - 1) / step() : 0; }
   // the half of the rows that warpgroup wg has
   __device__ __forceinline__ int half(int wg) const { return halves == 2 ? wg ^ parity : 0; }
-  __device__ __forceinline__ int next_parity() const { return (parity + count()) & 1; }
 };
+static_assert(sizeof(Units) <= 64, "one slot of the piece ring");
+
+// Every 64 polls of a wait: the time of the first check, or 0 to give up.  Out of line,
+// like all that the roles do rarely: their loops share one instruction cache, and with
+// the waits' slow paths inlined the kernel spent a third of its time refilling it.
+__device__ __noinline__ uint64_t still_waiting(uint64_t t0, volatile int* ctl, WsHeader* slot, uint32_t site) {
+  if (*ctl) return 0;
+  const uint64_t now = globaltimer();
+  if (t0 == 0) return now;
+  return mbar_wait_timed_out(ctl, slot, site, t0) ? 0 : t0;
+}
+
+// The forms below run on a whole warp in uniform control flow, with `e` true in one
+// lane: operands then stay in uniform registers and a product costs a few instructions
+// to issue instead of twenty, which the issuing warp cannot hide.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t e;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(e));
+  return e;
+}
+// Low word of sdesc(); the high words are constants of the operand's layout.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lbo_bytes) {
+  return ((saddr & 0x3FFFFu) >> 4) | ((lbo_bytes >> 4) << 16);
+}
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);  // 1024 bytes between 8-row groups
+__device__ __forceinline__ void mma_ss(uint32_t e, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "mov.b64 da, {%1, %6};\n\tmov.b64 db, {%2, %6};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(e), "r"(kDescHi));
+}
+__device__ __forceinline__ void mma_ts(uint32_t e, uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "mov.b64 db, {%2, %6};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(e), "r"(kDescHi));
+}
+__device__ __forceinline__ void commit_if(uint32_t e, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(e)
+      : "memory");
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* ctl, WsHeader* slot,
+                                          uint32_t site) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity & 1u)); ++it)
+    if ((it & 63u) == 0u) {
+      t0 = still_waiting(t0, ctl, slot, site);
+      if (__any_sync(0xffffffffu, t0 == 0)) return false;
+    }
+  return true;
+}
+
+__device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, volatile int* ctl, WsHeader* slot,
+                                             uint32_t site) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1; !mbar_try_wait(bar, parity); ++it)
+    if ((it & 63u) == 0u && (t0 = still_waiting(t0, ctl, slot, site)) == 0) return false;
+  return true;
+}
 
 template <int D>
 __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_constant__ AttnArgs a) {
@@ -112,6 +192,8 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
   auto q_full = [&](int g) { return per + 8u * (8 + g); };
   auto q_empty = [&](int g) { return per + 8u * (10 + g); };
   const uint32_t x_full = per + 8u * 12, x_empty = per + 8u * 13, drain = per + 8u * 14;
+  auto piece_full = [&](uint32_t s) { return per + 8u * (15 + s); };
+  auto piece_empty = [&](uint32_t s) { return per + 8u * (15 + C::NPIECE + s); };
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NBAR; ++i) {
@@ -120,6 +202,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
       if (i < C::NSLOT) n = 4;                                                       // slot_full: the dequantising warps
       if (i >= 2 * C::NSLOT + C::NRAW && i < 2 * C::NSLOT + 2 * C::NRAW) n = 4;      // raw_empty
       if (p == 2 || p == 3 || p == 6 || p == 7 || p == 12 || p == 13) n = 4;         // a softmax warpgroup's warps
+      if (p >= 15 + C::NPIECE) n = C::NREADER;                                       // piece_empty
       mbar_init(bar0 + 8u * i, n);
     }
     slot->err = 0;
@@ -144,17 +227,17 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
     return;
   }
   const int64_t tb = range_begin(total, W, wk), te = range_begin(total, W, wk + 1);
-  Walk cur;
-  cur.t = tb;
-  cur.te = te;
-  {
+  Walk cur;  // warp 0 walks
+  if (warp == 0) {
+    cur.t = tb;
+    cur.te = te;
     int64_t rem;
     find_tile<C>(a, pre, chunk, tb, lane, cur.b, rem);
     set_piece<C>(a, cur, user_sizes<C>(a, cur.b), rem, lane);
-  }
-  if (threadIdx.x == 0) {
-    Piece p{cur.seg0, cur.seg1, cur.b, cur.h, cur.rt, 0};
-    static_cast<Piece*>(a.piece)[wk] = p;
+    if (lane == 0) {
+      Piece p{cur.seg0, cur.seg1, cur.b, cur.h, cur.rt, 0};
+      static_cast<Piece*>(a.piece)[wk] = p;
+    }
   }
   if (warp == 2) tmem_alloc(smem_u32(tmem_slot), 512);
   tc_fence_before();
@@ -163,12 +246,26 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
   const uint32_t tmem = *tmem_slot;
   bool ok = true;
   auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site) {
-    ok = __all_sync(0xffffffffu, mbar_wait(bar, parity & 1u, ctl, slot, site));
+    ok = ok && __all_sync(0xffffffffu, bounded_wait(bar, parity & 1u, ctl, slot, site));
     return ok;
   };
 
+  Units* ring = reinterpret_cast<Units*>(smem + C::OFF_PIECE);
+  uint32_t np = 0;  // pieces read (or published) so far
+  // the next piece; done() gives its place back
+  auto next = [&](Units& u) {
+    if (!wait(piece_full(np % C::NPIECE), np / C::NPIECE, 0xD51u)) return false;
+    u = *reinterpret_cast<const Units*>(reinterpret_cast<const uint8_t*>(ring) + 64 * (np % C::NPIECE));
+    return u.n >= 0;
+  };
+  auto done = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(piece_empty(np % C::NPIECE));
+    ++np;
+  };
+
   if (warp < 4) {
-    setmaxnreg_dec<80>();
+    setmaxnreg_dec<96>();
     if (warp == 0) {
       // ------------------------------------------------------------- copies
       // lane 2 p + i copies the codes (i = 0) or scales of the block's p-th page
@@ -180,7 +277,34 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
         if (off >= C::KB || p0 >= w.vis1 || p0 + n <= w.vis0) return -2;  // nothing to copy
         return a.c.table[int64_t(w.b) * a.c.max_pages + (p0 >> a.c.log2page)];
       };
+      int parity = 0;
+      auto publish = [&](bool end) {
+        const uint32_t s = np % C::NPIECE;
+        if (np >= C::NPIECE && !wait(piece_empty(s), np / C::NPIECE + 1, 0xD52u)) return;
+        if (lane == 0) {
+          Units u;
+          u.n = end ? -1 : max(cur.kb1 - cur.kb0, 0);
+          u.halves = cur.weight;
+          u.parity = parity;
+          u.kb0 = cur.kb0;
+          u.vis0 = cur.vis0;
+          u.vis1 = cur.vis1;
+          u.row0 = cur.rt * C::ROWS;
+          u.rows = min(cur.s.rows - u.row0, C::ROWS);
+          u.h = cur.h;
+          u.len = cur.s.len;
+          u.whole = cur.seg0 >= tb && cur.seg1 <= te;
+          u.second = tb >= cur.seg0 ? 0 : 1;
+          u.q0 = cur.s.q0;
+          *reinterpret_cast<Units*>(reinterpret_cast<uint8_t*>(ring) + 64 * s) = u;
+          mbar_arrive(piece_full(s));
+        }
+        __syncwarp();
+        ++np;
+        if (!end) parity = (parity + max(cur.kb1 - cur.kb0, 0) * cur.weight) & 1;
+      };
       for (bool have = true; have && ok;) {
+        publish(false);
         int pid = cur.kb0 < cur.kb1 ? page_of(cur, cur.kb0) : -2;
         for (int kb = cur.kb0; kb < cur.kb1 && ok; ++kb) {
           bool want = pid != -2;
@@ -205,6 +329,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
         }
         have = next_piece<C>(a, cur, lane);
       }
+      if (ok) publish(true);
       if (!ok)  // no copy may be in flight when the CTA's shared memory goes
         for (uint32_t k = c > C::NRAW ? c - C::NRAW : 0; k < c; ++k)
           tcc::mbar_wait_bounded(raw_full(k % C::NRAW), (k / C::NRAW) & 1u, 200000000ull);
@@ -212,130 +337,148 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
       // ----------------------------------------------------------- products
       constexpr uint32_t idS = idesc_bf16(128, C::KB, 0, 0);  // Q (K-major) x K^T (K-major)
       constexpr uint32_t idO = idesc_f16(128, D, 0, 1);       // P (TMEM) x V (MN-major)
-      // What the second product of a unit needs to know, kept until its weights are there.
-      struct Unit {
-        uint32_t v;  // count of its value tile in the ring
-        bool first, last, last_v, on;
+      const uint32_t e = elect_one();
+      const uint32_t lo_q = desc_lo(sb + C::OFF_Q, 16), lo_k = desc_lo(sb + C::OFF_RING, 16);
+      const uint32_t lo_v = desc_lo(sb + C::OFF_RING, 16384);
+      // Ring places and phases of the block whose scores, and of the one whose weights,
+      // come next: keys of block t are at 2 t, values at 2 t + 1.
+      uint32_t ks = 0, kph = 0, vs = 1, vph = 0;
+      auto advance = [](uint32_t& s, uint32_t& ph) {  // two places on in a ring of three
+        s += 2;
+        if (s >= 3) {
+          s -= 3;
+          ph ^= 1;
+        }
       };
-      Unit q0{}, q1{};
-      uint32_t u = 0, pv = 0, tile = 0;  // units issued, units finished, blocks begun
-      uint32_t qn[2] = {0, 0}, on[2] = {0, 0}, pn[2] = {0, 0};
-      int i = 0;  // unit within the piece
+      uint32_t u = 0, pv = 0;                  // units whose scores are issued, units finished
+      uint32_t qph = 0, oph = 3, pph = 0;      // phases, bit g for warpgroup g; nobody waits for O at first
+      uint32_t f0 = 0, f1 = 0;                 // flags of the units between the two products
+      constexpr uint32_t kFirst = 1, kLast = 2, kLastV = 4;
+      uint32_t seen = 0;                       // warpgroups that have had a piece
+      int i = 0, count = 0, n = 0, two = 0, parity = 0;  // unit within the piece
       bool have = true;
-      Units un(cur, 0);
       auto settle = [&]() {
-        while (have && i >= un.count()) {
-          have = next_piece<C>(a, cur, lane);
-          un = Units(cur, un.next_parity());
+        while (ok && have && i >= count) {
+          if (np > 0 && e) mbar_arrive(piece_empty((np - 1) % C::NPIECE));
+          ok = warp_wait(piece_full(np % C::NPIECE), np / C::NPIECE, ctl, slot, 0xD10u);
+          const int* un = reinterpret_cast<const int*>(reinterpret_cast<const uint8_t*>(ring) + 64 * (np % C::NPIECE));
+          n = __shfl_sync(0xffffffffu, un[0], 0);
+          two = __shfl_sync(0xffffffffu, un[1], 0) - 1;
+          parity = __shfl_sync(0xffffffffu, un[2], 0);
+          have = n >= 0;
+          count = n << two;
           i = 0;
+          ++np;
         }
       };
       settle();
-      auto scores = [&](Unit& f) {  // S of the next unit
-        f.on = false;
-        if (!have) return;
-        const int g = int(u & 1u), blk = un.halves == 2 ? i >> 1 : i;
-        const bool first_k = un.halves == 1 || !(i & 1), last_k = un.halves == 1 || (i & 1);
-        f.first = blk == un.first(g);
-        f.last = blk + un.step() >= un.n;
-        f.last_v = last_k;
-        f.v = 2 * tile + 1;
-        f.on = true;
-        const uint32_t k = 2 * tile;
-        if (first_k && !wait(slot_full(k % C::NSLOT), k / C::NSLOT, 0xD11u)) return;
-        if (f.first && !wait(q_full(g), qn[g]++, 0xD12u)) return;
-        tc_fence_after();
-        if (lane == 0) {
-          const uint32_t kq = sb + C::OFF_Q + g * C::TILE, kk = sb + C::OFF_RING + (k % C::NSLOT) * C::TILE;
+      while (ok) {
+        if (have && u - pv < 2) {  // S runs two units ahead of O
+          const uint32_t g = u & 1u;
+          const int blk = i >> two;
+          const bool first_k = !two || !(i & 1), last_k = !two || (i & 1);
+          const bool first = two ? blk == 0 : i < 2, last = two ? blk == n - 1 : i >= n - 2;
+          if (first_k && !(ok = warp_wait(slot_full(ks), kph, ctl, slot, 0xD11u))) break;
+          if (first) {
+            if (!(ok = warp_wait(q_full(g), qph >> g, ctl, slot, 0xD12u))) break;
+            qph ^= 1u << g;
+          }
+          tc_fence_after();
+          const uint32_t dq = lo_q + g * (C::TILE >> 4), dk = lo_k + ks * (C::TILE >> 4), dst = tmem + C::S_COL + g * 128;
 #pragma unroll
-          for (int s = 0; s < D / 16; ++s)
-            umma_ss(tmem + C::S_COL + g * 128, sdesc(kq + (s >> 2) * 16384 + (s & 3) * 32, 16, 1024),
-                    sdesc(kk + (s >> 2) * 16384 + (s & 3) * 32, 16, 1024), idS, s > 0 ? 1u : 0u);
-          umma_commit(s_full(g));
-          if (last_k) umma_commit(slot_empty(k % C::NSLOT));
-          if (f.last) umma_commit(q_empty(g));
+          for (int s = 0; s < D / 16; ++s) {
+            const uint32_t at = ((s >> 2) * 16384 + (s & 3) * 32) >> 4;
+            mma_ss(e, dst, dq + at, dk + at, idS, s > 0 ? 1u : 0u);
+          }
+          commit_if(e, s_full(g));
+          if (last) commit_if(e, q_empty(g));
+          if (last_k) {
+            commit_if(e, slot_empty(ks));
+            advance(ks, kph);
+          }
+          const uint32_t f = (first ? kFirst : 0u) | (last ? kLast : 0u) | (last_k ? kLastV : 0u);
+          if (u == pv)
+            f0 = f;
+          else
+            f1 = f;
+          ++u;
+          ++i;
+          settle();
+          continue;
         }
-        if (last_k) ++tile;
-        ++u;
-        ++i;
-        settle();
-      };
-      scores(q0);
-      if (ok) scores(q1);
-      while (ok && q0.on) {
-        const int g = int(pv & 1u);
-        if (!wait(p_full(g), pn[g]++, 0xD13u)) break;
-        if (!wait(slot_full(q0.v % C::NSLOT), q0.v / C::NSLOT, 0xD14u)) break;
-        if (q0.first) {
-          if (on[g] > 0 && !wait(o_empty(g), on[g] - 1, 0xD15u)) break;
-          ++on[g];
+        if (u == pv) break;
+        const uint32_t g = pv & 1u;
+        if (!(ok = warp_wait(slot_full(vs), vph, ctl, slot, 0xD14u))) break;
+        if (f0 & kFirst) {
+          if ((seen >> g) & 1u) {
+            if (!(ok = warp_wait(o_empty(g), oph >> g, ctl, slot, 0xD15u))) break;
+          }
+          seen |= 1u << g;
+          oph ^= 1u << g;
         }
+        if (!(ok = warp_wait(p_full(g), pph >> g, ctl, slot, 0xD13u))) break;
+        pph ^= 1u << g;
         tc_fence_after();
-        if (lane == 0) {
-          const uint32_t vv = sb + C::OFF_RING + (q0.v % C::NSLOT) * C::TILE;
+        const uint32_t dv = lo_v + vs * (C::TILE >> 4), dst = tmem + C::O_COL + g * 128, src = tmem + C::S_COL + g * 128;
 #pragma unroll
-          for (int s = 0; s < C::KB / 16; ++s)
-            umma_ts(tmem + C::O_COL + g * 128, tmem + C::S_COL + g * 128 + 8 * s, sdesc(vv + s * 2048, 16384, 1024), idO,
-                    q0.first && s == 0 ? 0u : 1u);
-          if (q0.last_v) umma_commit(slot_empty(q0.v % C::NSLOT));
-          if (q0.last) umma_commit(o_full(g));
+        for (int s = 0; s < C::KB / 16; ++s)
+          mma_ts(e, dst, src + 8 * s, dv + ((s * 2048) >> 4), idO, s == 0 ? ~f0 & kFirst : 1u);
+        if (f0 & kLastV) {
+          commit_if(e, slot_empty(vs));
+          advance(vs, vph);
         }
+        if (f0 & kLast) commit_if(e, o_full(g));
         ++pv;
-        q0 = q1;
-        scores(q1);
+        f0 = f1;
       }
-      if (lane == 0) {
-        umma_commit(drain);  // no product may still run when TMEM is released
-        tcc::mbar_wait_bounded(drain, 0, 200000000ull);
-      }
+      commit_if(e, drain);  // no product may still run when TMEM is released
+      if (e) tcc::mbar_wait_bounded(drain, 0, 200000000ull);
+      __syncwarp();
     } else {
       // ------------------------------------------------- query rows of half `g`
       const int g = warp - 2;
       uint32_t loads = 0;
-      Units un(cur, 0);
-      for (bool have = true; have && ok;) {
-        if (un.mine(g) > 0) {
-          if (loads > 0 && !wait(q_empty(g), loads - 1, 0xD21u)) break;
-          constexpr int CH = D / 8;  // 16-byte pieces of a row
-          const int r0 = cur.rt * C::ROWS + un.half(g) * 128;
-          const uint32_t dst = sb + C::OFF_Q + g * C::TILE;
-          const char* q = static_cast<const char*>(a.q);
-          const int c = lane % CH;
-#pragma unroll 4
-          for (int r = lane / CH; r < 128; r += 32 / CH) {
-            const int row = r0 + r;
-            const bool v = row < cur.s.rows;
-            const int t = v ? row / a.G : 0, h = v ? row - t * a.G : 0;
-            cp_async16(dst + (c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4),
-                       q + 2 * ((cur.s.q0 + t) * a.q_row + (cur.h * a.G + h) * a.q_head + 8 * c), v);
-          }
-          cp_async_wait_all();
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(q_full(g));
-          ++loads;
+      for (Units un; next(un); done()) {
+        if (un.mine(g) == 0) continue;
+        if (loads > 0 && !wait(q_empty(g), loads - 1, 0xD21u)) break;
+        constexpr int CH = D / 8;  // 16-byte pieces of a row
+        const int r0 = un.half(g) * 128;
+        const uint32_t dst = sb + C::OFF_Q + g * C::TILE;
+        const char* q = static_cast<const char*>(a.q);
+        const int c = lane % CH;
+#pragma unroll 2
+        for (int r = lane / CH; r < 128; r += 32 / CH) {
+          const bool v = r0 + r < un.rows;
+          const int row = v ? un.row0 + r0 + r : 0, t = row / a.G, h = row - t * a.G;
+          cp_async16(dst + (c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4),
+                     q + 2 * ((un.q0 + t) * a.q_row + (un.h * a.G + h) * a.q_head + 8 * c), v);
         }
-        have = next_piece<C>(a, cur, lane);
-        un = Units(cur, un.next_parity());
+        cp_async_wait_all();
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full(g));
+        ++loads;
       }
     }
   } else if (warp < 8) {
-    setmaxnreg_dec<64>();
+    setmaxnreg_dec<96>();
     // ------------------------------------------------------- dequantisation
     // Lane (r, q) = (lane / 4, lane % 4) takes a quarter of row 8 w + r: two or four
     // words.  With 128 features the quarters of the two 64-feature halves go in
     // swapped order, so that a store's eight lanes hit eight different banks.
     const int w = warp - 4, q4 = lane & 3;
     uint32_t c = 0;
-    for (bool have = true; have && ok;) {
-      for (int kb = cur.kb0; kb < cur.kb1 && ok; ++kb) {
+    for (Units un; next(un); done()) {
+      for (int kb = un.kb0; kb < un.kb0 + un.n && ok; ++kb) {
+        const bool edge = kb * C::KB < un.vis0 || (kb + 1) * C::KB > un.vis1;
+#pragma unroll 1
         for (int kv = 0; kv < 2; ++kv, ++c) {
           const uint32_t rs = c % C::NRAW, s = c % C::NSLOT;
           if (!wait(raw_full(rs), c / C::NRAW, 0xD31u)) break;
           if (c >= C::NSLOT && !wait(slot_empty(s), c / C::NSLOT + 1, 0xD32u)) break;
           const uint8_t* raw = smem + C::OFF_RAW + rs * C::RAW;
           uint8_t* out = smem + C::OFF_RING + s * C::TILE;
-#pragma unroll
+#pragma unroll 1
           for (int p = 0; p < 4; ++p) {
             const int r = 32 * p + 8 * w + (lane >> 2);
             constexpr int NW = D / 32;
@@ -356,7 +499,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
             // positions that no row of the tile sees count as zero values: what nobody
             // wrote can read as an infinity in float16, and 0 x inf is not 0
             const int pos = kb * C::KB + r;
-            if (kv && (pos < cur.vis0 || pos >= cur.vis1)) code = 0;
+            if (kv && edge && (pos < un.vis0 || pos >= un.vis1)) code = 0;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
               const int word = D == 128 ? (i ^ (q4 & 2)) : i;  // of the lane's quarter
@@ -379,10 +522,9 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
           }
         }
       }
-      have = next_piece<C>(a, cur, lane);
     }
   } else {
-    setmaxnreg_inc<184>();
+    setmaxnreg_inc<160>();
     // ----------------------------------------------------- softmax and results
     const int g = (warp - 8) >> 2, quad = warp & 3, rr = 32 * quad + lane;
     const uint32_t lane_off = uint32_t(32 * quad) << 16;
@@ -392,15 +534,14 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
     float2* Xs = reinterpret_cast<float2*>(smem + C::OFF_X + 128 * 32 * 4);
     uint32_t sn = 0, pieces = 0, xn = 0;
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
-    Units un(cur, 0);
-    for (bool have = true; have && ok;) {
+    for (Units un; next(un); done()) {
       const int mine = un.mine(g);
-      const bool whole = cur.seg0 >= tb && cur.seg1 <= te;
-      float* part = a.partial + (int64_t(wk) * 2 + (tb >= cur.seg0 ? 0 : 1)) * partial_floats(C::ROWS, D);
+      const bool whole = un.whole;
+      float* part = a.partial + (int64_t(wk) * 2 + un.second) * partial_floats(C::ROWS, D);
       // row i of the tile: its index among the (query, head) pairs, or -1
       auto dense = [&](int i) {
-        const int r = cur.rt * C::ROWS + i;
-        return r < cur.s.rows ? (cur.s.q0 + r / a.G) * a.Hq + cur.h * a.G + r % a.G : int64_t(-1);
+        const int r = un.row0 + i;
+        return i < un.rows ? (un.q0 + r / a.G) * a.Hq + un.h * a.G + r % a.G : int64_t(-1);
       };
       // 32 columns of one row, unnormalised or final
       auto put = [&](int i, int64_t o, int col, const float* y, float f) {
@@ -425,9 +566,11 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
       };
       if (un.n == 0 && g == 0) {  // nobody sees anything
         float zero[32] = {};
+#pragma unroll 1
         for (int hf = 0; hf < un.halves; ++hf) {
           const int i = 128 * hf + rr;
           const int64_t o = dense(i);
+#pragma unroll 1
           for (int col = 0; col < D; col += 32) put(i, o, col, zero, 0.f);
           put_stat(i, o, -INFINITY, 0.f);
         }
@@ -436,23 +579,34 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
         const int i = 128 * un.half(g) + rr;
         int lo = 0, hi = 0x7fffffff;
         const int64_t o = dense(i);
-        if (o >= 0) row_window(a, cur.s.q0 + (cur.rt * C::ROWS + i) / a.G, cur.s.len, lo, hi);
+        if (o >= 0) row_window(a, un.q0 + (un.row0 + i) / a.G, un.len, lo, hi);
         float msh = -INFINITY, l = 0.f;
         for (int b = 0; b < mine; ++b) {
-          const int k0 = (cur.kb0 + un.first(g) + b * un.step()) * C::KB;
+          const int k0 = (un.kb0 + un.first(g) + b * un.step()) * C::KB;
           if (!wait(s_full(g), sn++, 0xD41u)) break;
           tc_fence_after();
-          float v[128];
+          const bool masked = __any_sync(0xffffffffu, k0 < lo || k0 + C::KB > hi);
+          // 64 columns at a time, twice: for the maximum and for the weights (a second
+          // read of TMEM costs less than the registers and the code of a whole row)
+          float v[64];
+          auto load = [&](int hf) {
+            tmem_ld32(tS + 64 * hf, v);
+            tmem_ld32(tS + 64 * hf + 32, v + 32);
+            tmem_ld_wait();
+            if (masked) {
+              const int from = lo - k0 - 64 * hf, to = hi - k0 - 64 * hf;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, v + 32 * c);
-          tmem_ld_wait();
-          if (__any_sync(0xffffffffu, k0 < lo || k0 + C::KB > hi)) {
-            const int from = lo - k0, to = hi - k0;
-#pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (c < from || c >= to) v[c] = -INFINITY;
+              for (int c = 0; c < 64; ++c)
+                if (c < from || c >= to) v[c] = -INFINITY;
+            }
+          };
+          float mt = -INFINITY;
+#pragma unroll 1
+          for (int hf = 0; hf < 2; ++hf) {
+            load(hf);
+            mt = fmaxf(mt, row_max<64>(v));
           }
-          const float mt = row_max<128>(v) * c2;
+          mt *= c2;
           float alpha = 1.f;
           if (msh == -INFINITY) {
             msh = mt;  // O and l are zero so far
@@ -462,14 +616,18 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
           }
           // nothing seen yet: any shift gives zeros
           const float sh = msh == -INFINITY ? 0.f : msh - kLift;
-          l = l * alpha + exp2_shift_sum<128>(v, c2, sh);
-          uint32_t p[64];
+          l *= alpha;
+#pragma unroll 1
+          for (int hf = 0; hf < 2; ++hf) {
+            load(hf);
+            l += exp2_shift_sum<64>(v, c2, sh);
+            uint32_t p[32];
 #pragma unroll
-          for (int k = 0; k < 64; ++k) {
-            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(v[2 * k + 1]), "f"(v[2 * k]));
+            for (int k = 0; k < 32; ++k)
+              asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(v[2 * k + 1]), "f"(v[2 * k]));
+            tmem_st16(tS + 32 * hf, p);  // over columns that have been read
+            tmem_st16(tS + 32 * hf + 16, p + 16);
           }
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_st16(tS + 16 * c, p + 16 * c);
           if (b > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
@@ -493,6 +651,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
         const bool both = un.halves == 1 && un.n > 1;  // the other warpgroup has the other blocks' share
         const bool gives = both && un.first(g) == 1;
         float m = msh, f0 = 1.f, f1 = 0.f;
+#pragma unroll 1
         for (int c = 0; c < D && ok; c += 32) {
           float y[32];
           tmem_ld32(tO + c, y);
@@ -530,8 +689,6 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
         __syncwarp();
         if (lane == 0) mbar_arrive(o_empty(g));
       }
-      have = next_piece<C>(a, cur, lane);
-      un = Units(cur, un.next_parity());
     }
   }
   __syncthreads();
