@@ -3,7 +3,7 @@
 // head): bf16, d in {64, 128}, a positive scale.
 //
 // A CTA holds up to 256 query rows as two halves of 128 and walks 128 cached positions
-// at a time.  The products need 16-bit operands in shared memory, so four warps turn a
+// at a time.  The products need 16-bit operands in shared memory, so eight warps turn a
 // block's 4-bit words into them once for all the rows:
 //     S = Q K^T   (M = 128 rows, N = 128 positions, bf16)       accumulated in TMEM
 //     P = 2^(S - shift) in registers, float16, back over S in TMEM
@@ -20,8 +20,8 @@
 // arrives O is at rest.
 //
 // Warp roles: 0 walks the share, publishes its pieces to the other roles and copies the
-// pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 and 3 load the halves' query rows, 4..7 dequantise, 8..15 softmax and
-// results.  Every wait is bounded (sa_ptx.cuh).
+// pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 and 3 load the halves' query rows, 4..7 dequantise keys, 8..11 values,
+// 12..19 softmax and results.  Every wait is bounded (sa_ptx.cuh).
 #include "sa_cache.cuh"
 #include "sa_cache_walk.cuh"
 #include "sa_tc_common.cuh"
@@ -38,21 +38,22 @@ struct TcFwd {
   static constexpr int D = D_;
   static constexpr bool F32 = false, BWD = false;
   static constexpr int ROWS = 256, HALF = 128, KB = 128;
-  static constexpr int NWARP = 16, THREADS = 512;
+  static constexpr int NWARP = 20, THREADS = 640;
   static constexpr int TILE = 128 * D * 2;  // 128 rows of 16-bit values, [D / 64][128][128 bytes]
-  static constexpr int NSLOT = 3, NRAW = 5;
+  // Keys of block t are in place 2 (t % 2) of the ring, its values in the next: a lone
+  // half runs two blocks of scores ahead of its weights.
+  static constexpr int NSLOT = 4, NRAW = D == 128 ? 3 : 8;
   static constexpr int RAW = KB * (D / 2 + D / 16);
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_RING = OFF_Q + 2 * TILE;
+  static constexpr int OFF_SCAN = OFF_RING;  // used before anything is dequantised
   static constexpr int OFF_RAW = OFF_RING + NSLOT * TILE;
-  static constexpr int OFF_X = OFF_RAW + NRAW * RAW;  // exchange between the warpgroups: 32 columns + statistics
-  static constexpr int X_BYTES = 128 * 32 * 4 + 128 * 8;
-  static constexpr int OFF_SCAN = OFF_X;  // used before anything is exchanged
-  static_assert((THREADS + 2) * 8 <= X_BYTES, "the scan shares the exchange area");
+  static constexpr int OFF_X = OFF_RAW + NRAW * RAW;  // a warpgroup's shifts and sums for the other
+  static constexpr int X_BYTES = 128 * 8;
   static constexpr int OFF_BAR = OFF_X + X_BYTES;
   static constexpr int NPIECE = 4;    // pieces published ahead
-  static constexpr int NREADER = 15;  // warps that read them
-  static constexpr int NBAR = 2 * NSLOT + 2 * NRAW + 2 * 6 + 3 + 2 * NPIECE;
+  static constexpr int NREADER = 19;  // warps that read them
+  static constexpr int NBAR = 2 * NSLOT + 2 * NRAW + 2 * 6 + 2 + 2 * NPIECE;
   static constexpr int OFF_PIECE = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
   static constexpr int OFF_CTL = OFF_PIECE + NPIECE * 64;
   static constexpr int SMEM = OFF_CTL + 32;
@@ -74,6 +75,10 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(src), "r"(bytes), "r"(bar)
                : "memory");
+}
+
+__device__ __forceinline__ void l2_prefetch(const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 
 // A piece as the roles see it (64 bytes of shared memory).  Units, (block, half) pairs,
@@ -172,7 +177,7 @@ __device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, vola
 }
 
 template <int D>
-__global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_constant__ AttnArgs a) {
   using C = TcFwd<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -191,9 +196,9 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
   auto o_empty = [&](int g) { return per + 8u * (6 + g); };
   auto q_full = [&](int g) { return per + 8u * (8 + g); };
   auto q_empty = [&](int g) { return per + 8u * (10 + g); };
-  const uint32_t x_full = per + 8u * 12, x_empty = per + 8u * 13, drain = per + 8u * 14;
-  auto piece_full = [&](uint32_t s) { return per + 8u * (15 + s); };
-  auto piece_empty = [&](uint32_t s) { return per + 8u * (15 + C::NPIECE + s); };
+  const uint32_t x_full = per + 8u * 12, drain = per + 8u * 13;
+  auto piece_full = [&](uint32_t s) { return per + 8u * (14 + s); };
+  auto piece_empty = [&](uint32_t s) { return per + 8u * (14 + C::NPIECE + s); };
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NBAR; ++i) {
@@ -201,8 +206,8 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
       uint32_t n = 1;
       if (i < C::NSLOT) n = 4;                                                       // slot_full: the dequantising warps
       if (i >= 2 * C::NSLOT + C::NRAW && i < 2 * C::NSLOT + 2 * C::NRAW) n = 4;      // raw_empty
-      if (p == 2 || p == 3 || p == 6 || p == 7 || p == 12 || p == 13) n = 4;         // a softmax warpgroup's warps
-      if (p >= 15 + C::NPIECE) n = C::NREADER;                                       // piece_empty
+      if (p == 2 || p == 3 || p == 6 || p == 7 || p == 12) n = 4;         // a softmax warpgroup's warps
+      if (p >= 14 + C::NPIECE) n = C::NREADER;                                       // piece_empty
       mbar_init(bar0 + 8u * i, n);
     }
     slot->err = 0;
@@ -265,7 +270,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
   };
 
   if (warp < 4) {
-    setmaxnreg_dec<96>();
+    setmaxnreg_dec<80>();
     if (warp == 0) {
       // ------------------------------------------------------------- copies
       // lane 2 p + i copies the codes (i = 0) or scales of the block's p-th page
@@ -274,7 +279,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
       const int rb = part ? D / 16 : D / 2;
       auto page_of = [&](const Walk& w, int kb) {
         const int p0 = kb * C::KB + off;
-        if (off >= C::KB || p0 >= w.vis1 || p0 + n <= w.vis0) return -2;  // nothing to copy
+        if (off >= C::KB || kb >= w.kb1 || p0 >= w.vis1 || p0 + n <= w.vis0) return -2;  // nothing to copy
         return a.c.table[int64_t(w.b) * a.c.max_pages + (p0 >> a.c.log2page)];
       };
       int parity = 0;
@@ -305,7 +310,8 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
       };
       for (bool have = true; have && ok;) {
         publish(false);
-        int pid = cur.kb0 < cur.kb1 ? page_of(cur, cur.kb0) : -2;
+        // the pages of this block and the next two; two blocks ahead go to L2
+        int pid = page_of(cur, cur.kb0), pid1 = page_of(cur, cur.kb0 + 1), pid2 = page_of(cur, cur.kb0 + 2);
         for (int kb = cur.kb0; kb < cur.kb1 && ok; ++kb) {
           bool want = pid != -2;
           if (want && (pid < 0 || pid >= a.c.n_pages)) {
@@ -316,7 +322,15 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
           const int first = (kb * C::KB + off) & (a.c.page - 1);
           const uint32_t bytes = want ? uint32_t(n * rb) : 0u;
           const uint32_t sum = __reduce_add_sync(0xffffffffu, bytes);
-          if (kb + 1 < cur.kb1) pid = page_of(cur, kb + 1);
+          if (pid2 >= 0 && pid2 < a.c.n_pages) {
+            const uint8_t* p = a.c.pool + a.c.record(pid2, cur.h) + (part ? a.c.page * (D / 2) : 0) +
+                               (((kb + 2) * C::KB + off) & (a.c.page - 1)) * rb;
+            l2_prefetch(p, n * rb);
+            l2_prefetch(p + a.c.rec, n * rb);
+          }
+          pid = pid1;
+          pid1 = pid2;
+          pid2 = page_of(cur, kb + 3);
           for (int kv = 0; kv < 2; ++kv, ++c) {
             const uint32_t s = c % C::NRAW;
             if (c >= C::NRAW && !wait(raw_empty(s), c / C::NRAW + 1, 0xD01u)) break;
@@ -340,45 +354,46 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
       const uint32_t e = elect_one();
       const uint32_t lo_q = desc_lo(sb + C::OFF_Q, 16), lo_k = desc_lo(sb + C::OFF_RING, 16);
       const uint32_t lo_v = desc_lo(sb + C::OFF_RING, 16384);
-      // Ring places and phases of the block whose scores, and of the one whose weights,
-      // come next: keys of block t are at 2 t, values at 2 t + 1.
-      uint32_t ks = 0, kph = 0, vs = 1, vph = 0;
-      auto advance = [](uint32_t& s, uint32_t& ph) {  // two places on in a ring of three
-        s += 2;
-        if (s >= 3) {
-          s -= 3;
-          ph ^= 1;
-        }
-      };
+      uint32_t kt = 0, vt = 0;                 // blocks whose scores, and whose weights, are issued
       uint32_t u = 0, pv = 0;                  // units whose scores are issued, units finished
       uint32_t qph = 0, oph = 3, pph = 0;      // phases, bit g for warpgroup g; nobody waits for O at first
       uint32_t f0 = 0, f1 = 0;                 // flags of the units between the two products
       constexpr uint32_t kFirst = 1, kLast = 2, kLastV = 4;
       uint32_t seen = 0;                       // warpgroups that have had a piece
-      int i = 0, count = 0, n = 0, two = 0, parity = 0;  // unit within the piece
+      int i = 0, count = 0, n = 0, two = 0;  // unit within the piece
       bool have = true;
-      auto settle = [&]() {
+      bool held = false;  // a piece whose place in the ring is not given back yet
+      // Moves on to a piece with units; false if it is not published yet.  With weights
+      // outstanding this must not block: the walk waits for pieces that they finish.
+      auto fetch = [&](bool block) {
         while (ok && have && i >= count) {
-          if (np > 0 && e) mbar_arrive(piece_empty((np - 1) % C::NPIECE));
-          ok = warp_wait(piece_full(np % C::NPIECE), np / C::NPIECE, ctl, slot, 0xD10u);
+          if (held && e) mbar_arrive(piece_empty((np - 1) % C::NPIECE));
+          held = false;
+          const uint32_t bar = piece_full(np % C::NPIECE), ph = (np / C::NPIECE) & 1u;
+          if (block)
+            ok = warp_wait(bar, ph, ctl, slot, 0xD10u);
+          else if (!__all_sync(0xffffffffu, mbar_try_wait(bar, ph)))
+            return false;
           const int* un = reinterpret_cast<const int*>(reinterpret_cast<const uint8_t*>(ring) + 64 * (np % C::NPIECE));
           n = __shfl_sync(0xffffffffu, un[0], 0);
           two = __shfl_sync(0xffffffffu, un[1], 0) - 1;
-          parity = __shfl_sync(0xffffffffu, un[2], 0);
           have = n >= 0;
           count = n << two;
           i = 0;
+          held = true;
           ++np;
         }
+        return true;
       };
-      settle();
       while (ok) {
-        if (have && u - pv < 2) {  // S runs two units ahead of O
+        if (have && u - pv < 2 && (i < count || fetch(u == pv)) && have) {  // S runs two units ahead of O
+          if (!ok) break;
           const uint32_t g = u & 1u;
           const int blk = i >> two;
           const bool first_k = !two || !(i & 1), last_k = !two || (i & 1);
           const bool first = two ? blk == 0 : i < 2, last = two ? blk == n - 1 : i >= n - 2;
-          if (first_k && !(ok = warp_wait(slot_full(ks), kph, ctl, slot, 0xD11u))) break;
+          const uint32_t ks = 2 * (kt & 1u);
+          if (first_k && !(ok = warp_wait(slot_full(ks), kt >> 1, ctl, slot, 0xD11u))) break;
           if (first) {
             if (!(ok = warp_wait(q_full(g), qph >> g, ctl, slot, 0xD12u))) break;
             qph ^= 1u << g;
@@ -394,7 +409,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
           if (last) commit_if(e, q_empty(g));
           if (last_k) {
             commit_if(e, slot_empty(ks));
-            advance(ks, kph);
+            ++kt;
           }
           const uint32_t f = (first ? kFirst : 0u) | (last ? kLast : 0u) | (last_k ? kLastV : 0u);
           if (u == pv)
@@ -403,12 +418,12 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
             f1 = f;
           ++u;
           ++i;
-          settle();
           continue;
         }
-        if (u == pv) break;
+        if (u == pv) break;  // nothing published is left, nothing outstanding
         const uint32_t g = pv & 1u;
-        if (!(ok = warp_wait(slot_full(vs), vph, ctl, slot, 0xD14u))) break;
+        const uint32_t vs = 2 * (vt & 1u) + 1;
+        if (!(ok = warp_wait(slot_full(vs), vt >> 1, ctl, slot, 0xD14u))) break;
         if (f0 & kFirst) {
           if ((seen >> g) & 1u) {
             if (!(ok = warp_wait(o_empty(g), oph >> g, ctl, slot, 0xD15u))) break;
@@ -425,7 +440,7 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
           mma_ts(e, dst, src + 8 * s, dv + ((s * 2048) >> 4), idO, s == 0 ? ~f0 & kFirst : 1u);
         if (f0 & kLastV) {
           commit_if(e, slot_empty(vs));
-          advance(vs, vph);
+          ++vt;
         }
         if (f0 & kLast) commit_if(e, o_full(g));
         ++pv;
@@ -460,25 +475,27 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
         ++loads;
       }
     }
-  } else if (warp < 8) {
-    setmaxnreg_dec<96>();
+  } else if (warp < 12) {
+    setmaxnreg_dec<64>();
     // ------------------------------------------------------- dequantisation
     // Lane (r, q) = (lane / 4, lane % 4) takes a quarter of row 8 w + r: two or four
     // words.  With 128 features the quarters of the two 64-feature halves go in
     // swapped order, so that a store's eight lanes hit eight different banks.
-    const int w = warp - 4, q4 = lane & 3;
-    uint32_t c = 0;
+    const int kv = warp >= 8, w = warp & 3, q4 = lane & 3;
+    uint32_t c = kv;
     for (Units un; next(un); done()) {
-      for (int kb = un.kb0; kb < un.kb0 + un.n && ok; ++kb) {
-        const bool edge = kb * C::KB < un.vis0 || (kb + 1) * C::KB > un.vis1;
 #pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv, ++c) {
-          const uint32_t rs = c % C::NRAW, s = c % C::NSLOT;
-          if (!wait(raw_full(rs), c / C::NRAW, 0xD31u)) break;
-          if (c >= C::NSLOT && !wait(slot_empty(s), c / C::NSLOT + 1, 0xD32u)) break;
-          const uint8_t* raw = smem + C::OFF_RAW + rs * C::RAW;
-          uint8_t* out = smem + C::OFF_RING + s * C::TILE;
-#pragma unroll 1
+      for (int kb = un.kb0; kb < un.kb0 + un.n; ++kb, c += 2) {
+        const uint32_t rs = c % C::NRAW, s = c % C::NSLOT;
+        if (!wait(raw_full(rs), c / C::NRAW, 0xD31u)) break;
+        if (c >= C::NSLOT && !wait(slot_empty(s), c / C::NSLOT + 1, 0xD32u)) break;
+        const uint8_t* raw = smem + C::OFF_RAW + rs * C::RAW;
+        uint8_t* out = smem + C::OFF_RING + s * C::TILE;
+        // positions that no row of the tile sees count as zero values: what nobody
+        // wrote can read as an infinity in float16, and 0 x inf is not 0
+        const int from = kv ? un.vis0 - kb * C::KB : 0, to = kv ? un.vis1 - kb * C::KB : C::KB;
+        auto rows = [&](auto values) {
+#pragma unroll 2
           for (int p = 0; p < 4; ++p) {
             const int r = 32 * p + 8 * w + (lane >> 2);
             constexpr int NW = D / 32;
@@ -496,42 +513,38 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
               x[0] = v.x, x[1] = v.y;
               code = raw[C::KB * (D / 2) + r * (D / 16) + q4];
             }
-            // positions that no row of the tile sees count as zero values: what nobody
-            // wrote can read as an infinity in float16, and 0 x inf is not 0
-            const int pos = kb * C::KB + r;
-            if (kv && edge && (pos < un.vis0 || pos >= un.vis1)) code = 0;
+            if (r < from || r >= to) code = 0;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
               const int word = D == 128 ? (i ^ (q4 & 2)) : i;  // of the lane's quarter
               const int chunk = q4 * NW + word;                // of the row: 8 features, 16 bytes
-              const uint32_t cc = ((code >> (8 * (i / 2))) & 255u) * 0x00010001u;
               uint32_t y[4];
-              if (kv == 0)
-                values_bf16(x[i], scale_bf16(cc), y);
-              else
-                values_f16(x[i], cc << 7, y);
+              values(x[i], __byte_perm(code, 0, i < 2 ? 0x4040 : 0x4141), y);
               *reinterpret_cast<uint4*>(out + (chunk >> 3) * 16384 + r * 128 + (((chunk & 7) ^ (r & 7)) << 4)) =
                   make_uint4(y[0], y[1], y[2], y[3]);
             }
           }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(slot_full(s));
-            mbar_arrive(raw_empty(rs));
-          }
+        };
+        if (kv)
+          rows([](uint32_t x, uint32_t cc, uint32_t* y) { values_f16(x, cc << 7, y); });
+        else
+          rows([](uint32_t x, uint32_t cc, uint32_t* y) { values_bf16(x, scale_bf16(cc), y); });
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(slot_full(s));
+          mbar_arrive(raw_empty(rs));
         }
       }
     }
   } else {
-    setmaxnreg_inc<160>();
+    setmaxnreg_inc<136>();
     // ----------------------------------------------------- softmax and results
-    const int g = (warp - 8) >> 2, quad = warp & 3, rr = 32 * quad + lane;
+    const int g = (warp - 12) >> 2, quad = warp & 3, rr = 32 * quad + lane;
     const uint32_t lane_off = uint32_t(32 * quad) << 16;
     const uint32_t tS = tmem + lane_off + C::S_COL + g * 128, tO = tmem + lane_off + C::O_COL + g * 128;
     const float c2 = a.scale * kLog2e;
-    float* X = reinterpret_cast<float*>(smem + C::OFF_X);
-    float2* Xs = reinterpret_cast<float2*>(smem + C::OFF_X + 128 * 32 * 4);
+    float2* X = reinterpret_cast<float2*>(smem + C::OFF_X);
     uint32_t sn = 0, pieces = 0, xn = 0;
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
     for (Units un; next(un); done()) {
@@ -648,46 +661,51 @@ __global__ void __launch_bounds__(512, 1) cache_tc_fwd_kernel(const __grid_const
         if (!ok || !wait(o_full(g), pieces, 0xD42u)) break;
         ++pieces;
         tc_fence_after();
-        const bool both = un.halves == 1 && un.n > 1;  // the other warpgroup has the other blocks' share
-        const bool gives = both && un.first(g) == 1;
+        // The other warpgroup has the other blocks' share of these rows: one of the two
+        // leaves its shifts and sums in X, and the other, whose warps read the same lanes
+        // of TMEM, adds and stores.
+        const bool both = un.halves == 1 && un.n > 1;
+        if (both && un.first(g) == 1) {
+          X[rr] = make_float2(msh, l);
+          ++xn;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(x_full);
+          continue;  // the other warpgroup gives O back
+        }
         float m = msh, f0 = 1.f, f1 = 0.f;
+        if (both) {
+          if (!wait(x_full, xn++, 0xD44u)) break;
+          tc_fence_after();
+          const float2 s = X[rr];
+          m = fmaxf(msh, s.x);
+          f0 = msh == -INFINITY ? 0.f : ex2(msh - m);
+          f1 = s.x == -INFINITY ? 0.f : ex2(s.x - m);
+          l = l * f0 + s.y * f1;
+        }
+        const float f = !whole ? 1.f : l > 0.f ? 1.f / l : 0.f;
+        f0 *= f;
+        f1 *= f;
 #pragma unroll 1
-        for (int c = 0; c < D && ok; c += 32) {
+        for (int c = 0; c < D; c += 32) {
           float y[32];
           tmem_ld32(tO + c, y);
           tmem_ld_wait();
-          if (gives) {
-            if (xn > 0 && !wait(x_empty, xn - 1, 0xD43u)) break;
-#pragma unroll
-            for (int k = 0; k < 32; ++k) X[k * 128 + rr] = y[k];
-            if (c == 0) Xs[rr] = make_float2(msh, l);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(x_full);
-            ++xn;
-            continue;
-          }
           if (both) {
-            if (!wait(x_full, xn, 0xD44u)) break;
-            ++xn;
-            if (c == 0) {
-              const float2 s = Xs[rr];
-              m = fmaxf(msh, s.x);
-              f0 = msh == -INFINITY ? 0.f : ex2(msh - m);
-              f1 = s.x == -INFINITY ? 0.f : ex2(s.x - m);
-              l = l * f0 + s.y * f1;
-            }
+            float z[32];
+            tmem_ld32(tmem + lane_off + C::O_COL + (g ^ 1) * 128 + c, z);
+            tmem_ld_wait();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) y[k] = y[k] * f0 + X[k * 128 + rr] * f1;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(x_empty);
+            for (int k = 0; k < 32; ++k) y[k] = y[k] * f0 + z[k] * f1;
           }
-          put(i, o, c, y, !whole ? 1.f : l > 0.f ? 1.f / l : 0.f);
+          put(i, o, c, y, both ? 1.f : f0);
         }
-        if (!ok) break;
-        if (!gives) put_stat(i, o, m, l);
+        put_stat(i, o, m, l);
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(o_empty(g));
+        if (lane == 0) {
+          mbar_arrive(o_empty(g));
+          if (both) mbar_arrive(o_empty(g ^ 1));
+        }
       }
     }
   }

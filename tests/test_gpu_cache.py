@@ -169,6 +169,30 @@ def test_long_history_is_shared_out_and_joined(cuda_lib, dt, R):
     run_both(cuda_lib, cache, [R, 1, 1], 1, dt)
 
 
+@pytest.mark.parametrize("d,R,L", [(128, 100, 300), (64, 100, 300), (64, 256, 130), (128, 140, 129)])
+def test_many_segments_a_worker(cuda_lib, d, R, L):
+    """More (user, head, row tile) segments than workers, of odd and even numbers of blocks, some empty."""
+    lens = [(L * (3 + b % 5)) // 7 if b % 9 else 0 for b in range(200)]
+    cache = cc.Cache(lens, 2, d, 64, seed=14)
+    rng = np.random.default_rng(15)
+    q = cc.queries(200 * R, 2, d, "bf16", 16)
+    do = cc.queries(200 * R, 2, d, "bf16", 17)
+    pool, table, tl = cache.tensors()
+    cu = gpu(cc.offsets([R] * 200))
+    tq = cc.to_gpu(q, "bf16")
+    out, lse = cuda_lib.sa_cache_attn_fwd(tq, cu, pool, table, tl, want_lse=True)
+    dq = cuda_lib.sa_cache_attn_bwd(tq, cu, pool, table, tl, out, lse, cc.to_gpu(do, "bf16"))
+    torch.cuda.synchronize()
+    for b in [int(x) for x in rng.choice(200, 12, replace=False)] + [0, 199]:
+        rows = slice(b * R, (b + 1) * R)
+        one = cc.Cache([0], 2, d, 64)
+        one.lens, one.kv = [lens[b]], [[part[b]] for part in cache.kv]
+        r = cc.reference(one, q[rows], [R], 1, cc.default_scale(d), dout=do[rows],
+                         out=out[rows].double().cpu().numpy(), lse=lse[rows].double().cpu().numpy())
+        for name, got, m in zip(("out", "lse", "dq"), (out, lse, dq), cc.limits(r, d, "bf16", max(1, lens[b]))):
+            cc.check(name, got[rows], r[name], m)
+
+
 @pytest.mark.parametrize("R", [1, 160])
 def test_unwritten_and_hidden_positions_never_matter(cuda_lib, R):
     """Pages outside every query's window may be gone (-1) or hold anything."""
