@@ -133,22 +133,29 @@ struct Warp {
   __device__ __forceinline__ void issue(const Walk& w, int kb, int pid) {
     const uint32_t s = issued & 1u;
     const uint32_t b = bar + 8u * s;
+    const uint32_t dst = smem_u32(ring) + s * C::STAGE;
     bool want = wanted(w, kb);
     if (want && (pid < 0 || pid >= a.c.n_pages)) {
       atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
       want = false;
     }
-    const int n = min(a.c.page, KB), off = (lane >> 2) * n, first = (kb * KB + off) & (a.c.page - 1);
-    const int kv = (lane >> 1) & 1, rb = lane & 1 ? a.c.d / 16 : a.c.d / 2;  // bytes of a row of this part
-    const uint32_t bytes = want ? uint32_t(n * rb) : 0u;
-    const uint32_t total = __reduce_add_sync(0xffffffffu, bytes);
-    if (lane == 0) mbar_arrive_expect_tx(b, total);
-    __syncwarp();
-    if (want) {
-      const uint8_t* src = a.c.pool + a.c.record(pid, w.h) + kv * a.c.rec + (lane & 1 ? a.c.page * (a.c.d / 2) : 0) + first * rb;
-      const uint32_t dst = smem_u32(ring) + s * C::STAGE + (kv * (KB * (a.c.d / 2 + a.c.d / 16))) +
-                           (lane & 1 ? KB * (a.c.d / 2) : 0) + off * rb;
-      bulk_load(dst, src, bytes, b);
+    if (a.c.page == KB) {  // a block is a page, and a page's records lie as the stage does
+      if (lane == 0) {
+        const uint32_t bytes = want ? 2u * a.c.rec : 0u;
+        mbar_arrive_expect_tx(b, bytes);
+        if (want) bulk_load(dst, a.c.pool + a.c.record(pid, w.h), bytes, b);
+      }
+    } else {
+      const int n = min(a.c.page, KB), off = (lane >> 2) * n, first = (kb * KB + off) & (a.c.page - 1);
+      const int kv = (lane >> 1) & 1, rb = lane & 1 ? a.c.d / 16 : a.c.d / 2;  // bytes of a row of this part
+      const uint32_t bytes = want ? uint32_t(n * rb) : 0u;
+      const uint32_t total = __reduce_add_sync(0xffffffffu, bytes);
+      if (lane == 0) mbar_arrive_expect_tx(b, total);
+      __syncwarp();
+      if (want) {
+        const uint8_t* src = a.c.pool + a.c.record(pid, w.h) + kv * a.c.rec + (lane & 1 ? a.c.page * (a.c.d / 2) : 0) + first * rb;
+        bulk_load(dst + (kv * (KB * (a.c.d / 2 + a.c.d / 16))) + (lane & 1 ? KB * (a.c.d / 2) : 0) + off * rb, src, bytes, b);
+      }
     }
     ++issued;
   }
