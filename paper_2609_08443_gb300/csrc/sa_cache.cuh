@@ -76,9 +76,10 @@ struct AttnPlan {
 AttnPlan mma_plan(int sms, int B, int64_t T, int G, int d, sa_dtype dt, bool bwd);
 cudaError_t launch_mma(const AttnArgs& a, bool bwd, cudaStream_t st);
 
-// tcgen05 kernels (sa_cache_tc.cu)
+// tcgen05 kernels (sa_cache_tc.cu, sa_cache_tc_bwd.cu)
 bool tc_supported(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd);
-AttnPlan tc_plan(int sms, int d);
+AttnPlan tc_plan(int sms, int d, bool bwd);
+cudaError_t launch_tc_bwd(const AttnArgs& a, cudaStream_t st);
 cudaError_t launch_tc(const AttnArgs& a, bool bwd, cudaStream_t st);
 
 // ------------------------------------------------------------------ arithmetic

@@ -68,7 +68,7 @@ struct Layout {
 Layout attn_layout(int B, int64_t T, int G, int d, sa_dtype dt, bool bwd, bool tc) {
   Layout l{};
   const int sms = sa::tcc::device_sm_count();
-  const sa::cache::AttnPlan p = tc ? sa::cache::tc_plan(sms, d) : sa::cache::mma_plan(sms, B, T, G, d, dt, bwd);
+  const sa::cache::AttnPlan p = tc ? sa::cache::tc_plan(sms, d, bwd) : sa::cache::mma_plan(sms, B, T, G, d, dt, bwd);
   l.ctas = p.ctas;
   l.workers = p.workers;
   size_t off = sizeof(sa::WsHeader);

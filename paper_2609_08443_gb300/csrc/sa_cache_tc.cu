@@ -21,15 +21,12 @@
 //
 // Warp roles: 0 walks the share, publishes its pieces to the other roles and copies the
 // pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 and 3 load the halves' query rows, 4..7 dequantise keys, 8..11 values,
-// 12..19 softmax and results.  Every wait is bounded (sa_ptx.cuh).
-#include "sa_cache.cuh"
-#include "sa_cache_walk.cuh"
-#include "sa_tc_common.cuh"
+// 12..19 softmax and results.  Every wait is bounded: past the limit
+// the CTA's roles leave, its copies and products drain and the error is reported.
+#include "sa_cache_tc.cuh"
 
 namespace sa {
 namespace cache {
-
-using namespace ptx;
 
 constexpr float kLazy = 3.f;  // with kLift = 12 a weight stays below 2^15, inside float16
 
@@ -56,30 +53,11 @@ struct TcFwd {
   static constexpr int NBAR = 2 * NSLOT + 2 * NRAW + 2 * 6 + 2 + 2 * NPIECE;
   static constexpr int OFF_PIECE = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
   static constexpr int OFF_CTL = OFF_PIECE + NPIECE * 64;
-  static constexpr int SMEM = OFF_CTL + 32;
+  static constexpr int OFF_TMEM = OFF_CTL + 16;
+  static constexpr int SMEM = OFF_TMEM + 16;
   static_assert(SMEM <= 232448, "shared memory budget");
   static constexpr int S_COL = 0, O_COL = 256;  // two halves each
 };
-
-// Instruction descriptor of kind::f16 with float16 A and B, fp32 D.
-__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) {
-  return (1u << 4) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
-}
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
-
-__device__ __forceinline__ void l2_prefetch(const void* src, uint32_t bytes) {
-  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
-}
 
 // A piece as the roles see it (64 bytes of shared memory).  Units, (block, half) pairs,
 // alternate between the warpgroups over the whole share; `parity` is the first one's.
@@ -105,85 +83,14 @@ struct Units {
 };
 static_assert(sizeof(Units) <= 64, "one slot of the piece ring");
 
-// Every 64 polls of a wait: the time of the first check, or 0 to give up.  Out of line,
-// like all that the roles do rarely: their loops share one instruction cache, and with
-// the waits' slow paths inlined the kernel spent a third of its time refilling it.
-__device__ __noinline__ uint64_t still_waiting(uint64_t t0, volatile int* ctl, WsHeader* slot, uint32_t site) {
-  if (*ctl) return 0;
-  const uint64_t now = globaltimer();
-  if (t0 == 0) return now;
-  return mbar_wait_timed_out(ctl, slot, site, t0) ? 0 : t0;
-}
-
-// The forms below run on a whole warp in uniform control flow, with `e` true in one
-// lane: operands then stay in uniform registers and a product costs a few instructions
-// to issue instead of twenty, which the issuing warp cannot hide.
-__device__ __forceinline__ uint32_t elect_one() {
-  uint32_t e;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(e));
-  return e;
-}
-// Low word of sdesc(); the high words are constants of the operand's layout.
-__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lbo_bytes) {
-  return ((saddr & 0x3FFFFu) >> 4) | ((lbo_bytes >> 4) << 16);
-}
-constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);  // 1024 bytes between 8-row groups
-__device__ __forceinline__ void mma_ss(uint32_t e, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
-                                       uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-      "mov.b64 da, {%1, %6};\n\tmov.b64 db, {%2, %6};\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
-      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(e), "r"(kDescHi));
-}
-__device__ __forceinline__ void mma_ts(uint32_t e, uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc,
-                                       uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-      "mov.b64 db, {%2, %6};\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(e), "r"(kDescHi));
-}
-__device__ __forceinline__ void commit_if(uint32_t e, uint32_t bar) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
-      "r"(e)
-      : "memory");
-}
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* ctl, WsHeader* slot,
-                                          uint32_t site) {
-  uint64_t t0 = 0;
-  for (uint32_t it = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity & 1u)); ++it)
-    if ((it & 63u) == 0u) {
-      t0 = still_waiting(t0, ctl, slot, site);
-      if (__any_sync(0xffffffffu, t0 == 0)) return false;
-    }
-  return true;
-}
-
-__device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, volatile int* ctl, WsHeader* slot,
-                                             uint32_t site) {
-  uint64_t t0 = 0;
-  for (uint32_t it = 1; !mbar_try_wait(bar, parity); ++it)
-    if ((it & 63u) == 0u && (t0 = still_waiting(t0, ctl, slot, site)) == 0) return false;
-  return true;
-}
-
 template <int D>
 __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_constant__ AttnArgs a) {
   using C = TcFwd<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   WsHeader* slot = a.slots + blockIdx.x;
-  volatile int* ctl = reinterpret_cast<volatile int*>(smem + C::OFF_CTL);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_CTL + 16);
+  Ctl* ctl = reinterpret_cast<Ctl*>(smem + C::OFF_CTL);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_TMEM);
   const uint32_t sb = smem_u32(smem), bar0 = sb + C::OFF_BAR;
   auto slot_full = [&](uint32_t s) { return bar0 + 8u * s; };
   auto slot_empty = [&](uint32_t s) { return bar0 + 8u * (C::NSLOT + s); };
@@ -212,8 +119,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
     }
     slot->err = 0;
     slot->timeout_site = 0;
-    slot->wait_limit_ns = a.wait_limit_ns;
-    wait_ctl_init(ctl, slot);
+    ctl->abort = 0;
     fence_mbar_init();
   }
   int64_t* pre = reinterpret_cast<int64_t*>(smem + C::OFF_SCAN);
@@ -249,9 +155,10 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  const uint32_t limit = a.wait_limit_ns > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(a.wait_limit_ns);
   bool ok = true;
   auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site) {
-    ok = ok && __all_sync(0xffffffffu, bounded_wait(bar, parity & 1u, ctl, slot, site));
+    ok = ok && warp_wait(bar, parity, ctl, limit, site);
     return ok;
   };
 
@@ -371,7 +278,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
           held = false;
           const uint32_t bar = piece_full(np % C::NPIECE), ph = (np / C::NPIECE) & 1u;
           if (block)
-            ok = warp_wait(bar, ph, ctl, slot, 0xD10u);
+            ok = warp_wait(bar, ph, ctl, limit, 0xD10u);
           else if (!__all_sync(0xffffffffu, mbar_try_wait(bar, ph)))
             return false;
           const int* un = reinterpret_cast<const int*>(reinterpret_cast<const uint8_t*>(ring) + 64 * (np % C::NPIECE));
@@ -393,9 +300,9 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
           const bool first_k = !two || !(i & 1), last_k = !two || (i & 1);
           const bool first = two ? blk == 0 : i < 2, last = two ? blk == n - 1 : i >= n - 2;
           const uint32_t ks = 2 * (kt & 1u);
-          if (first_k && !(ok = warp_wait(slot_full(ks), kt >> 1, ctl, slot, 0xD11u))) break;
+          if (first_k && !(ok = warp_wait(slot_full(ks), kt >> 1, ctl, limit, 0xD11u))) break;
           if (first) {
-            if (!(ok = warp_wait(q_full(g), qph >> g, ctl, slot, 0xD12u))) break;
+            if (!(ok = warp_wait(q_full(g), qph >> g, ctl, limit, 0xD12u))) break;
             qph ^= 1u << g;
           }
           tc_fence_after();
@@ -423,15 +330,15 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
         if (u == pv) break;  // nothing published is left, nothing outstanding
         const uint32_t g = pv & 1u;
         const uint32_t vs = 2 * (vt & 1u) + 1;
-        if (!(ok = warp_wait(slot_full(vs), vt >> 1, ctl, slot, 0xD14u))) break;
+        if (!(ok = warp_wait(slot_full(vs), vt >> 1, ctl, limit, 0xD14u))) break;
         if (f0 & kFirst) {
           if ((seen >> g) & 1u) {
-            if (!(ok = warp_wait(o_empty(g), oph >> g, ctl, slot, 0xD15u))) break;
+            if (!(ok = warp_wait(o_empty(g), oph >> g, ctl, limit, 0xD15u))) break;
           }
           seen |= 1u << g;
           oph ^= 1u << g;
         }
-        if (!(ok = warp_wait(p_full(g), pph >> g, ctl, slot, 0xD13u))) break;
+        if (!(ok = warp_wait(p_full(g), pph >> g, ctl, limit, 0xD13u))) break;
         pph ^= 1u << g;
         tc_fence_after();
         const uint32_t dv = lo_v + vs * (C::TILE >> 4), dst = tmem + C::O_COL + g * 128, src = tmem + C::S_COL + g * 128;
@@ -495,7 +402,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
         // wrote can read as an infinity in float16, and 0 x inf is not 0
         const int from = kv ? un.vis0 - kb * C::KB : 0, to = kv ? un.vis1 - kb * C::KB : C::KB;
         auto rows = [&](auto values) {
-#pragma unroll 2
+#pragma unroll 1
           for (int p = 0; p < 4; ++p) {
             const int r = 32 * p + 8 * w + (lane >> 2);
             constexpr int NW = D / 32;
@@ -599,25 +506,24 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
           if (!wait(s_full(g), sn++, 0xD41u)) break;
           tc_fence_after();
           const bool masked = __any_sync(0xffffffffu, k0 < lo || k0 + C::KB > hi);
-          // 64 columns at a time, twice: for the maximum and for the weights (a second
+          // 32 columns at a time, twice: for the maximum and for the weights (a second
           // read of TMEM costs less than the registers and the code of a whole row)
-          float v[64];
-          auto load = [&](int hf) {
-            tmem_ld32(tS + 64 * hf, v);
-            tmem_ld32(tS + 64 * hf + 32, v + 32);
+          float v[32];
+          auto load = [&](int c) {
+            tmem_ld32(tS + c, v);
             tmem_ld_wait();
             if (masked) {
-              const int from = lo - k0 - 64 * hf, to = hi - k0 - 64 * hf;
+              const int from = lo - k0 - c, to = hi - k0 - c;
 #pragma unroll
-              for (int c = 0; c < 64; ++c)
-                if (c < from || c >= to) v[c] = -INFINITY;
+              for (int k = 0; k < 32; ++k)
+                if (k < from || k >= to) v[k] = -INFINITY;
             }
           };
           float mt = -INFINITY;
 #pragma unroll 1
-          for (int hf = 0; hf < 2; ++hf) {
-            load(hf);
-            mt = fmaxf(mt, row_max<64>(v));
+          for (int c = 0; c < C::KB; c += 32) {
+            load(c);
+            mt = fmaxf(mt, row_max<32>(v));
           }
           mt *= c2;
           float alpha = 1.f;
@@ -631,15 +537,14 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
           const float sh = msh == -INFINITY ? 0.f : msh - kLift;
           l *= alpha;
 #pragma unroll 1
-          for (int hf = 0; hf < 2; ++hf) {
-            load(hf);
-            l += exp2_shift_sum<64>(v, c2, sh);
-            uint32_t p[32];
+          for (int c = 0; c < C::KB; c += 32) {
+            load(c);
+            l += exp2_shift_sum<32>(v, c2, sh);
+            uint32_t p[16];
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
+            for (int k = 0; k < 16; ++k)
               asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(v[2 * k + 1]), "f"(v[2 * k]));
-            tmem_st16(tS + 32 * hf, p);  // over columns that have been read
-            tmem_st16(tS + 32 * hf + 16, p + 16);
+            tmem_st16(tS + c / 2, p);  // over columns that have been read
           }
           if (b > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
 #pragma unroll 1
@@ -710,6 +615,10 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
     }
   }
   __syncthreads();
+  if (threadIdx.x == 0 && ctl->abort) {
+    slot->err = uint32_t(SA_ERR_TIMEOUT);
+    slot->timeout_site = ctl->site;
+  }
   if (warp == 2) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
@@ -728,21 +637,23 @@ static cudaError_t run_fwd(const AttnArgs& a, cudaStream_t st) {
 }
 
 // Taken where the average user has at least 64 rows for a cached head: below that most of
-// the 128 rows of a product are padding.
+// the 128 rows of a product are padding.  The forward takes its maximum on the raw scores,
+// so its scale is positive.
 bool tc_supported(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd) {
-  if (bwd || dt != SA_BF16 || (d != 64 && d != 128) || !(scale > 0.f) || T * G < int64_t(64) * B) return false;
+  if (dt != SA_BF16 || (d != 64 && d != 128) || (!bwd && !(scale > 0.f)) || T * G < int64_t(64) * B) return false;
   return tcc::device_is_sm103();
 }
 
-AttnPlan tc_plan(int sms, int d) {
+AttnPlan tc_plan(int sms, int d, bool bwd) {
   AttnPlan p;
   p.ctas = p.workers = sms;
   p.piece_bytes = sizeof(Piece);
-  p.partial_floats = d == 128 ? partial_floats(256, 128) : partial_floats(256, 64);
+  p.partial_floats = partial_floats(bwd ? 128 : 256, d);
   return p;
 }
 
-cudaError_t launch_tc(const AttnArgs& a, bool, cudaStream_t st) {
+cudaError_t launch_tc(const AttnArgs& a, bool bwd, cudaStream_t st) {
+  if (bwd) return launch_tc_bwd(a, st);
   return a.c.d == 128 ? run_fwd<128>(a, st) : run_fwd<64>(a, st);
 }
 
