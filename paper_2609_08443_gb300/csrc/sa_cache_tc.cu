@@ -111,8 +111,8 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
     for (int i = 0; i < C::NBAR; ++i) {
       const int p = i - 2 * C::NSLOT - 2 * C::NRAW;  // barriers of the halves
       uint32_t n = 1;
-      if (i < C::NSLOT) n = 4;                                                       // slot_full: the dequantising warps
-      if (i >= 2 * C::NSLOT + C::NRAW && i < 2 * C::NSLOT + 2 * C::NRAW) n = 4;      // raw_empty
+      if (i < C::NSLOT) n = 8;                                                       // slot_full: the dequantising warps
+      if (i >= 2 * C::NSLOT + C::NRAW && i < 2 * C::NSLOT + 2 * C::NRAW) n = 8;      // raw_empty
       if (p == 2 || p == 3 || p == 6 || p == 7 || p == 12) n = 4;         // a softmax warpgroup's warps
       if (p >= 14 + C::NPIECE) n = C::NREADER;                                       // piece_empty
       mbar_init(bar0 + 8u * i, n);
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const uint32_t limit = a.wait_limit_ns > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(a.wait_limit_ns);
+  const uint32_t limit = wait_limit(a);
   bool ok = true;
   auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site) {
     ok = ok && warp_wait(bar, parity, ctl, limit, site);
@@ -261,97 +261,62 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
       const uint32_t e = elect_one();
       const uint32_t lo_q = desc_lo(sb + C::OFF_Q, 16), lo_k = desc_lo(sb + C::OFF_RING, 16);
       const uint32_t lo_v = desc_lo(sb + C::OFF_RING, 16384);
-      uint32_t kt = 0, vt = 0;                 // blocks whose scores, and whose weights, are issued
-      uint32_t u = 0, pv = 0;                  // units whose scores are issued, units finished
-      uint32_t qph = 0, oph = 3, pph = 0;      // phases, bit g for warpgroup g; nobody waits for O at first
-      uint32_t f0 = 0, f1 = 0;                 // flags of the units between the two products
-      constexpr uint32_t kFirst = 1, kLast = 2, kLastV = 4;
-      uint32_t seen = 0;                       // warpgroups that have had a piece
-      int i = 0, count = 0, n = 0, two = 0;  // unit within the piece
-      bool have = true;
-      bool held = false;  // a piece whose place in the ring is not given back yet
-      // Moves on to a piece with units; false if it is not published yet.  With weights
-      // outstanding this must not block: the walk waits for pieces that they finish.
-      auto fetch = [&](bool block) {
-        while (ok && have && i >= count) {
-          if (held && e) mbar_arrive(piece_empty((np - 1) % C::NPIECE));
-          held = false;
-          const uint32_t bar = piece_full(np % C::NPIECE), ph = (np / C::NPIECE) & 1u;
-          if (block)
-            ok = warp_wait(bar, ph, ctl, limit, 0xD10u);
-          else if (!__all_sync(0xffffffffu, mbar_try_wait(bar, ph)))
-            return false;
-          const int* un = reinterpret_cast<const int*>(reinterpret_cast<const uint8_t*>(ring) + 64 * (np % C::NPIECE));
-          n = __shfl_sync(0xffffffffu, un[0], 0);
-          two = __shfl_sync(0xffffffffu, un[1], 0) - 1;
-          have = n >= 0;
-          count = n << two;
-          i = 0;
-          held = true;
-          ++np;
-        }
-        return true;
-      };
-      while (ok) {
-        if (have && u - pv < 2 && (i < count || fetch(u == pv)) && have) {  // S runs two units ahead of O
-          if (!ok) break;
-          const uint32_t g = u & 1u;
-          const int blk = i >> two;
-          const bool first_k = !two || !(i & 1), last_k = !two || (i & 1);
-          const bool first = two ? blk == 0 : i < 2, last = two ? blk == n - 1 : i >= n - 2;
-          const uint32_t ks = 2 * (kt & 1u);
-          if (first_k && !(ok = warp_wait(slot_full(ks), kt >> 1, ctl, limit, 0xD11u))) break;
-          if (first) {
-            if (!(ok = warp_wait(q_full(g), qph >> g, ctl, limit, 0xD12u))) break;
-            qph ^= 1u << g;
-          }
-          tc_fence_after();
-          const uint32_t dq = lo_q + g * (C::TILE >> 4), dk = lo_k + ks * (C::TILE >> 4), dst = tmem + C::S_COL + g * 128;
+      uint32_t kt = 0, vt = 0;            // blocks whose scores, and whose weights, are issued
+      uint32_t qph = 0, pph = 0, oph = 3; // phases, bit g for warpgroup g
+      uint32_t seen = 0;                  // warpgroups that have had a piece: the first does not wait for O
+      for (Units un; next(un); done()) {
+        // Units alternate between the warpgroups; S runs two units ahead of O, and the last
+        // two units' products are issued before the next piece is looked at: the walk may
+        // be waiting for what they release.
+        const int total = un.count(), two = un.halves == 2;
+#pragma unroll 1
+        for (int i = 0; i < total + 2 && total > 0; ++i) {
+          const uint32_t g = uint32_t(un.parity + i) & 1u;  // also of unit i - 2
+          if (i >= 2) {  // O of unit i - 2
+            const int j = i - 2;
+            const uint32_t vs = 2 * (vt & 1u) + 1;
+            if (!wait(slot_full(vs), vt >> 1, 0xD14u)) break;
+            if (j < 2) {  // the warpgroup's first of the piece
+              if (((seen >> g) & 1u) && !wait(o_empty(g), oph >> g, 0xD15u)) break;
+              seen |= 1u << g;
+              oph ^= 1u << g;
+            }
+            if (!wait(p_full(g), pph >> g, 0xD13u)) break;
+            pph ^= 1u << g;
+            tc_fence_after();
+            const uint32_t dv = lo_v + vs * (C::TILE >> 4), dst = tmem + C::O_COL + g * 128, src = tmem + C::S_COL + g * 128;
 #pragma unroll
-          for (int s = 0; s < D / 16; ++s) {
-            const uint32_t at = ((s >> 2) * 16384 + (s & 3) * 32) >> 4;
-            mma_ss(e, dst, dq + at, dk + at, idS, s > 0 ? 1u : 0u);
+            for (int s = 0; s < C::KB / 16; ++s)
+              mma_ts(e, dst, src + 8 * s, dv + ((s * 2048) >> 4), idO, s == 0 ? uint32_t(j >= 2) : 1u);
+            if (!two || (j & 1)) {
+              commit_if(e, slot_empty(vs));
+              ++vt;
+            }
+            if (j + 2 >= total) commit_if(e, o_full(g));
           }
-          commit_if(e, s_full(g));
-          if (last) commit_if(e, q_empty(g));
-          if (last_k) {
-            commit_if(e, slot_empty(ks));
-            ++kt;
-          }
-          const uint32_t f = (first ? kFirst : 0u) | (last ? kLast : 0u) | (last_k ? kLastV : 0u);
-          if (u == pv)
-            f0 = f;
-          else
-            f1 = f;
-          ++u;
-          ++i;
-          continue;
-        }
-        if (u == pv) break;  // nothing published is left, nothing outstanding
-        const uint32_t g = pv & 1u;
-        const uint32_t vs = 2 * (vt & 1u) + 1;
-        if (!(ok = warp_wait(slot_full(vs), vt >> 1, ctl, limit, 0xD14u))) break;
-        if (f0 & kFirst) {
-          if ((seen >> g) & 1u) {
-            if (!(ok = warp_wait(o_empty(g), oph >> g, ctl, limit, 0xD15u))) break;
-          }
-          seen |= 1u << g;
-          oph ^= 1u << g;
-        }
-        if (!(ok = warp_wait(p_full(g), pph >> g, ctl, limit, 0xD13u))) break;
-        pph ^= 1u << g;
-        tc_fence_after();
-        const uint32_t dv = lo_v + vs * (C::TILE >> 4), dst = tmem + C::O_COL + g * 128, src = tmem + C::S_COL + g * 128;
+          if (i < total) {  // S of unit i
+            const uint32_t ks = 2 * (kt & 1u);
+            if ((!two || !(i & 1)) && !wait(slot_full(ks), kt >> 1, 0xD11u)) break;
+            if (i < 2) {
+              if (!wait(q_full(g), qph >> g, 0xD12u)) break;
+              qph ^= 1u << g;
+            }
+            tc_fence_after();
+            const uint32_t dq = lo_q + g * (C::TILE >> 4), dk = lo_k + ks * (C::TILE >> 4), dst = tmem + C::S_COL + g * 128;
 #pragma unroll
-        for (int s = 0; s < C::KB / 16; ++s)
-          mma_ts(e, dst, src + 8 * s, dv + ((s * 2048) >> 4), idO, s == 0 ? ~f0 & kFirst : 1u);
-        if (f0 & kLastV) {
-          commit_if(e, slot_empty(vs));
-          ++vt;
+            for (int s = 0; s < D / 16; ++s) {
+              const uint32_t at = ((s >> 2) * 16384 + (s & 3) * 32) >> 4;
+              mma_ss(e, dst, dq + at, dk + at, idS, s > 0 ? 1u : 0u);
+            }
+            commit_if(e, s_full(g));
+            if (i + 2 >= total) commit_if(e, q_empty(g));
+            if (!two || (i & 1)) {
+              commit_if(e, slot_empty(ks));
+              ++kt;
+            }
+          }
         }
-        if (f0 & kLast) commit_if(e, o_full(g));
-        ++pv;
-        f0 = f1;
+        if (!ok) break;
       }
       commit_if(e, drain);  // no product may still run when TMEM is released
       if (e) tcc::mbar_wait_bounded(drain, 0, 200000000ull);
@@ -363,21 +328,11 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
       for (Units un; next(un); done()) {
         if (un.mine(g) == 0) continue;
         if (loads > 0 && !wait(q_empty(g), loads - 1, 0xD21u)) break;
-        constexpr int CH = D / 8;  // 16-byte pieces of a row
         const int r0 = un.half(g) * 128;
-        const uint32_t dst = sb + C::OFF_Q + g * C::TILE;
-        const char* q = static_cast<const char*>(a.q);
-        const int c = lane % CH;
-#pragma unroll 2
-        for (int r = lane / CH; r < 128; r += 32 / CH) {
-          const bool v = r0 + r < un.rows;
-          const int row = v ? un.row0 + r0 + r : 0, t = row / a.G, h = row - t * a.G;
-          cp_async16(dst + (c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4),
-                     q + 2 * ((un.q0 + t) * a.q_row + (un.h * a.G + h) * a.q_head + 8 * c), v);
-        }
-        cp_async_wait_all();
-        fence_proxy_async_smem();
-        __syncwarp();
+        load_rows<D>(a.q, sb + C::OFF_Q + g * C::TILE, lane, [&](int r) {
+          const int row = un.row0 + r0 + r;
+          return r0 + r < un.rows ? (un.q0 + row / a.G) * a.q_row + (un.h * a.G + row % a.G) * a.q_head : int64_t(-1);
+        });
         if (lane == 0) mbar_arrive(q_full(g));
         ++loads;
       }
@@ -385,14 +340,18 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
   } else if (warp < 12) {
     setmaxnreg_dec<64>();
     // ------------------------------------------------------- dequantisation
-    // Lane (r, q) = (lane / 4, lane % 4) takes a quarter of row 8 w + r: two or four
+    // Lane (r, q) = (lane / 4, lane % 4) takes a quarter of rows 8 w + r, 64 on: two or four
     // words.  With 128 features the quarters of the two 64-feature halves go in
     // swapped order, so that a store's eight lanes hit eight different banks.
-    const int kv = warp >= 8, w = warp & 3, q4 = lane & 3;
-    uint32_t c = kv;
+    // All eight warps take each place of the ring in turn, keys, then values: the places
+    // are shared, and a warpgroup that left every other one to its neighbour could take a
+    // place's last phase but one for the one it waits for.
+    const int w = warp - 4, q4 = lane & 3;
+    uint32_t c = 0;
     for (Units un; next(un); done()) {
 #pragma unroll 1
-      for (int kb = un.kb0; kb < un.kb0 + un.n; ++kb, c += 2) {
+      for (int i = 0; i < 2 * un.n; ++i, ++c) {
+        const int kv = i & 1, kb = un.kb0 + (i >> 1);
         const uint32_t rs = c % C::NRAW, s = c % C::NSLOT;
         if (!wait(raw_full(rs), c / C::NRAW, 0xD31u)) break;
         if (c >= C::NSLOT && !wait(slot_empty(s), c / C::NSLOT + 1, 0xD32u)) break;
@@ -403,8 +362,8 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
         const int from = kv ? un.vis0 - kb * C::KB : 0, to = kv ? un.vis1 - kb * C::KB : C::KB;
         auto rows = [&](auto values) {
 #pragma unroll 1
-          for (int p = 0; p < 4; ++p) {
-            const int r = 32 * p + 8 * w + (lane >> 2);
+          for (int p = 0; p < 2; ++p) {
+            const int r = 64 * p + 8 * w + (lane >> 2);
             constexpr int NW = D / 32;
             uint32_t x[NW], code;
             if constexpr (D == 128) {

@@ -56,7 +56,15 @@ struct Ctl {
   uint32_t site;   // where
 };
 
-// Polls until the phase is complete, the limit (ns) is over or the CTA aborts.  A few
+// Limit of a wait in ns: never below two seconds, whatever sa_set_wait_limit_ns asks for its
+// tests of the sketch's kernels.  A correct pipeline waits microseconds.
+__device__ __forceinline__ uint32_t wait_limit(const AttnArgs& a) {
+  const uint64_t ns = a.wait_limit_ns < 2000000000ull ? 2000000000ull : a.wait_limit_ns;
+  return ns > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(ns);
+}
+
+// Polls until the phase is complete, the limit (ns) is over or the CTA aborts.  (A try-wait may
+// sleep until its phase completes: it is no way to ask whether one has.)  A few
 // instructions and no call: a dozen of these sit in the roles' loops.
 __device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity, uint32_t abort_addr, uint32_t limit_ns) {
   uint32_t ok;
@@ -132,5 +140,29 @@ __device__ __forceinline__ void commit_if(uint32_t e, uint32_t bar) {
       "r"(e)
       : "memory");
 }
+// 128 rows of D bf16 values into the swizzled layout [D / 64][128][128 bytes], by one
+// warp: each lane works out four rows' places (offset(row), in elements; negative: zeros),
+// and the copies take them from it.
+template <int D, class F>
+__device__ __forceinline__ void load_rows(const void* src, uint32_t dst, int lane, F&& offset) {
+  constexpr int CH = D / 8;  // 16-byte pieces of a row
+  const int c = lane % CH, sub = lane / CH;
+  const char* base = static_cast<const char*>(src) + 16 * c;
+  const uint32_t to = dst + (c >> 3) * 16384;
+#pragma unroll 1
+  for (int j = 0; j < 4; ++j) {
+    const int64_t mine = offset(32 * j + lane);
+#pragma unroll 4
+    for (int r = sub; r < 32; r += 32 / CH) {
+      const int64_t o = __shfl_sync(0xffffffffu, mine, r);
+      const int row = 32 * j + r;
+      cp_async16(to + row * 128 + (((c & 7) ^ (row & 7)) << 4), base + 2 * (o < 0 ? 0 : o), o >= 0);
+    }
+  }
+  cp_async_wait_all();
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+
 }  // namespace cache
 }  // namespace sa

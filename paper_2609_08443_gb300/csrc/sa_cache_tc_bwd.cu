@@ -13,8 +13,8 @@
 // under the other's exponentials.
 //
 // Warp roles: 0 walks the share, publishes its pieces to the other roles and copies the
-// pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 loads the
-// rows of Q and dO, 4..7 dequantise keys, 8..11 values, 12..19 dS and results.  Every
+// pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 and 3
+// load the rows of Q and dO, 4..7 dequantise keys, 8..11 values, 12..19 dS and results.  Every
 // wait is bounded: past the limit the CTA's roles leave, its copies and products drain
 // and the error is reported.
 #include "sa_cache_tc.cuh"
@@ -41,7 +41,7 @@ struct TcBwd {
   static constexpr int OFF_RAW = OFF_RING + NSLOT * TILE;
   static constexpr int OFF_BAR = OFF_RAW + NRAW * RAW;
   static constexpr int NPIECE = 4;    // pieces published ahead
-  static constexpr int NREADER = 18;  // warps that read them
+  static constexpr int NREADER = 19;  // warps that read them
   static constexpr int NBAR = 2 * NSLOT + 2 * NRAW + 9 + 2 * NPIECE;
   static constexpr int OFF_PIECE = (OFF_BAR + NBAR * 8 + 15) / 16 * 16;
   static constexpr int OFF_CTL = OFF_PIECE + NPIECE * 64;
@@ -91,6 +91,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_bwd_kernel(const __grid_const
       uint32_t n = 1;
       if (i < C::NSLOT || (p < 0 && p >= -C::NRAW)) n = 4;  // slot_full, raw_empty: the dequantising warps
       if (p == 2 || p == 3) n = 4;                          // p_full: a warpgroup
+      if (p == 6) n = 2;                                    // q_full: both loaders
       if (p == 5) n = 8;                                    // o_empty: both
       if (p >= 9 + C::NPIECE) n = C::NREADER;               // piece_empty
       mbar_init(bar0 + 8u * i, n);
@@ -133,7 +134,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_bwd_kernel(const __grid_const
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const uint32_t limit = a.wait_limit_ns > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(a.wait_limit_ns);
+  const uint32_t limit = wait_limit(a);
   bool ok = true;
   auto wait = [&](uint32_t bar, uint32_t parity, uint32_t site) {
     ok = ok && warp_wait(bar, parity, ctl, limit, site);
@@ -308,29 +309,18 @@ __global__ void __launch_bounds__(640, 1) cache_tc_bwd_kernel(const __grid_const
       commit_if(e, drain);  // no product may still run when TMEM is released
       if (e) tcc::mbar_wait_bounded(drain, 0, 200000000ull);
       __syncwarp();
-    } else if (warp == 2) {
-      // --------------------------------------------------------- query rows
+    } else {
+      // ---------------------------------------- query rows (2), their gradients (3)
       uint32_t loads = 0;
       for (Part un; next(un); done()) {
         if (un.n == 0) continue;
         if (loads > 0 && !wait(q_empty, loads - 1, 0xD21u)) break;
         ++loads;
-        constexpr int CH = D / 8;  // 16-byte pieces of a row
-        const char* q = static_cast<const char*>(a.q);
-        const char* dout = static_cast<const char*>(a.dout);
-        const int c = lane % CH;
-#pragma unroll 2
-        for (int r = lane / CH; r < 128; r += 32 / CH) {
-          const bool v = r < un.rows;
-          const int row = v ? un.row0 + r : 0, t = row / a.G, h = row - t * a.G;
-          const uint32_t at = (c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-          const int64_t qt = un.q0 + t, hq = un.h * a.G + h;
-          cp_async16(sb + C::OFF_Q + at, q + 2 * (qt * a.q_row + hq * a.q_head + 8 * c), v);
-          cp_async16(sb + C::OFF_DO + at, dout + 2 * ((qt * a.Hq + hq) * D + 8 * c), v);
-        }
-        cp_async_wait_all();
-        fence_proxy_async_smem();
-        __syncwarp();
+        load_rows<D>(warp == 2 ? a.q : a.dout, sb + (warp == 2 ? C::OFF_Q : C::OFF_DO), lane, [&](int r) {
+          const int row = un.row0 + r;
+          const int64_t t = un.q0 + row / a.G, h = un.h * a.G + row % a.G;
+          return r >= un.rows ? int64_t(-1) : warp == 2 ? t * a.q_row + h * a.q_head : (t * a.Hq + h) * D;
+        });
         if (lane == 0) mbar_arrive(q_full);
       }
     }

@@ -296,6 +296,26 @@ def test_same_bits_every_time_on_other_streams_and_in_a_graph(cuda_lib):
             assert torch.equal(o, ref) and torch.equal(l, lse) and torch.equal(dq, dref)
 
 
+@pytest.mark.parametrize("R,G,lens", [(300, 1, [6000, 5100, 0, 2049]), (40, 16, [1024] * 6), (1, 1, [20000, 3, 900]),
+                                      (100, 1, [700, 0, 130, 64] * 60)])
+def test_many_calls_give_the_same_bits(cuda_lib, R, G, lens):
+    """A wait on the wrong phase or a lost copy shows in one call of many."""
+    cache = cc.Cache(lens, 1, 128, 64, seed=18)
+    pool, table, tl = cache.tensors()
+    B = len(lens)
+    cu = gpu(cc.offsets([R] * B))
+    q = torch.randn((B * R, G, 128), device="cuda").bfloat16()
+    do = torch.randn((B * R, G, 128), device="cuda").bfloat16()
+    ref, lse = cuda_lib.sa_cache_attn_fwd(q, cu, pool, table, tl, want_lse=True)
+    dref = cuda_lib.sa_cache_attn_bwd(q, cu, pool, table, tl, ref, lse, do)
+    for _ in range(150):
+        o, l = cuda_lib.sa_cache_attn_fwd(q, cu, pool, table, tl, want_lse=True)
+        dq = cuda_lib.sa_cache_attn_bwd(q, cu, pool, table, tl, ref, lse, do)
+        assert torch.equal(o, ref) and torch.equal(l, lse) and torch.equal(dq, dref)
+    for w in cuda_lib._stream_ws_cache.values():
+        assert cuda_lib.sa_get_device_error(w) == 0
+
+
 def test_offsets_past_32_bits(cuda_lib):
     """Pages beyond 4 GiB of the pool."""
     H, d, page = 8, 128, 256
