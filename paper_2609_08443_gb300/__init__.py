@@ -5,4 +5,4 @@ C ABI declared in ``include/sa_sketch.h``); ``binding`` is a thin ctypes layer
 that passes torch's device pointers and current stream to it.  The library is
 loaded lazily on first use and its absence is an error, never a fallback.
 """
-__all__ = ["binding", "workloads", "roofline"]
+__all__ = ["binding", "workloads", "roofline", "cached_targets"]

@@ -560,21 +560,33 @@ def sa_sketch(K, V, cu_seqlens, Q, scale: Optional[float] = None):
 _stream_ws_cache = {}
 
 
+# These calls answer single tokens, so their checks avoid what costs a microsecond in
+# Python: device and stream objects, and properties read twice.
+
 def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _on(device):
-    """Makes ``device`` current for a call (nothing to do, and no cost, where it is)."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+def _on(index: int):
+    """Makes device ``index`` current for a call (nothing to do, and no cost, where it is)."""
+    return _STAY if torch.cuda.current_device() == index else torch.cuda.device(index)
 
 
-def _stream_workspace(nbytes: int, device, stream: int) -> torch.Tensor:
+_STAY = contextlib.nullcontext()
+
+
+def _stream_handle(index: int) -> int:
+    """The current stream of a device, without building its Python object where torch lets us."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
+def _stream_workspace(nbytes: int, index: int, stream: int) -> torch.Tensor:
     """A cached workspace of this stream (calls on other streams may run at the same time)."""
-    key = (device.index, stream)
+    key = (index, stream)
     buf = _stream_ws_cache.get(key)
     if buf is None or buf.numel() < nbytes:
-        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
         _stream_ws_cache[key] = buf
     return buf
 
@@ -592,23 +604,24 @@ def sa_cache_alloc(n_pages: int, H: int, d: int, page: int = 64, device="cuda") 
 
 
 def _cache_args(pool, block_table, d: int):
-    """(n_pages, H, page, B, max_pages) after the checks that every cache call makes."""
-    for name, t in (("pool", pool), ("block_table", block_table)):
-        if not t.is_cuda or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous CUDA tensor")
-    if pool.dtype != torch.uint8 or pool.dim() != 4 or pool.shape[2] != 2:
-        raise ValueError("pool must be uint8 [n_pages, H, 2, page * (d/2 + d/16)]")
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.device != pool.device:
-        raise ValueError("block_table must be int32 [B, max_pages] on the pool's device")
-    page, rest = divmod(pool.shape[3] * 16, 9 * d)
-    if rest:
-        raise ValueError(f"records of {pool.shape[3]} bytes hold no whole page of rows of width {d}")
-    return pool.shape[0], pool.shape[1], page, block_table.shape[0], block_table.shape[1]
+    """(device index, n_pages, H, page, B, max_pages) after the checks that every cache call makes."""
+    index = pool.get_device() if pool.is_cuda else -1
+    if index < 0 or not pool.is_contiguous() or pool.dtype is not torch.uint8 or pool.dim() != 4:
+        raise ValueError("pool must be a contiguous CUDA tensor, uint8 [n_pages, H, 2, page * (d/2 + d/16)]")
+    if not block_table.is_cuda or block_table.get_device() != index or not block_table.is_contiguous() or \
+            block_table.dtype is not torch.int32 or block_table.dim() != 2:
+        raise ValueError("block_table must be contiguous int32 [B, max_pages] on the pool's device")
+    n_pages, H, two, record = pool.shape
+    page, rest = divmod(record * 16, 9 * d) if d > 0 else (0, 1)
+    if two != 2 or rest:
+        raise ValueError(f"a pool of shape {tuple(pool.shape)} holds no whole pages of rows of width {d}")
+    B, max_pages = block_table.shape
+    return index, n_pages, H, page, B, max_pages
 
 
-def _offsets_arg(name, t, n, device):
-    if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or t.device != device
-                          or not t.is_contiguous()):
+def _offsets_arg(name, t, n, index):
+    if t is not None and (not t.is_cuda or t.get_device() != index or t.dtype is not torch.int32 or t.dim() != 1
+                          or t.numel() != n or not t.is_contiguous()):
         raise ValueError(f"{name} must be contiguous int32 [{n}] on the pool's device")
 
 
@@ -624,22 +637,22 @@ def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tenso
     if K.dim() != (3 if packed else 4) or K.shape != V.shape or K.dtype != V.dtype:
         raise ValueError("K and V must be [N, H, d] with cu_seqlens, or [B, H, n, d] without, of one dtype")
     d = K.shape[-1]
-    n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
-    if not K.is_cuda or K.device != pool.device or V.device != pool.device:
+    index, n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
+    if not K.is_cuda or K.get_device() != index or not V.is_cuda or V.get_device() != index:
         raise ValueError("K and V must be on the pool's device")
     if K.stride(-1) != 1 or V.stride() != K.stride():
         raise ValueError("K and V must have contiguous rows and equal strides")
     if K.shape[1] != H or (not packed and K.shape[0] != B):
         raise ValueError(f"K{tuple(K.shape)} does not fit a cache of {H} heads and {B} users")
-    _offsets_arg("cu_seqlens", cu_seqlens, B + 1, pool.device)
-    _offsets_arg("start", start, B, pool.device)
+    _offsets_arg("cu_seqlens", cu_seqlens, B + 1, index)
+    _offsets_arg("start", start, B, index)
     if packed:
         N, strides = K.shape[0], (0, K.stride(0), K.stride(1))
     else:
         N, strides = B * K.shape[2], (K.stride(0), K.stride(2), K.stride(1))
-    with _on(pool.device):
-        stream = torch.cuda.current_stream().cuda_stream
-        w = ws if ws is not None else _stream_workspace(256, pool.device, stream)
+    with _on(index):
+        stream = _stream_handle(index)
+        w = ws if ws is not None else _stream_workspace(256, index, stream)
         st = lib.sa_cache_write(K.data_ptr(), V.data_ptr(), *strides, _addr(cu_seqlens), B, N, _addr(start), H, d,
                                 _dt(K), pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
                                 w.data_ptr(), w.numel(), stream)
@@ -650,14 +663,15 @@ def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: tor
                   start: Optional[torch.Tensor] = None, dtype=torch.bfloat16, ws: Optional[torch.Tensor] = None):
     """(K, V) [n_rows, H, d]: positions start[b] .. of every user, n_rows = cu_seqlens[B] in all."""
     lib = load()
-    n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
-    _offsets_arg("cu_seqlens", cu_seqlens, B + 1, pool.device)
-    _offsets_arg("start", start, B, pool.device)
-    K = torch.empty((n_rows, H, d), dtype=dtype, device=pool.device)
-    V = torch.empty_like(K)
-    with _on(pool.device):
-        stream = torch.cuda.current_stream().cuda_stream
-        w = ws if ws is not None else _stream_workspace(256, pool.device, stream)
+    index, n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
+    _offsets_arg("cu_seqlens", cu_seqlens, B + 1, index)
+    _offsets_arg("start", start, B, index)
+    if n_rows < 0:
+        raise ValueError("n_rows must not be negative")
+    K, V = torch.empty((2, n_rows, H, d), dtype=dtype, device=pool.device)
+    with _on(index):
+        stream = _stream_handle(index)
+        w = ws if ws is not None else _stream_workspace(256, index, stream)
         st = lib.sa_cache_read(pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
                                cu_seqlens.data_ptr(), B, n_rows, _addr(start), H, d, _dt(K), K.data_ptr(),
                                V.data_ptr(), w.data_ptr(), w.numel(), stream)
@@ -679,26 +693,28 @@ def _cache_attn(entry, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end,
     if q.dim() != 3 or not q.is_cuda or q.stride(-1) != 1:
         raise ValueError("q must be a CUDA tensor [T, Hq, d] with contiguous rows")
     T, Hq, d = q.shape
-    n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
-    dev = pool.device
-    if q.device != dev:
+    index, n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
+    if q.get_device() != index:
         raise ValueError("q must be on the pool's device")
     if Hq % H:
         raise ValueError(f"{Hq} query heads over {H} cached heads")
-    _offsets_arg("cu_q", cu_q, B + 1, dev)
-    _offsets_arg("cache_lens", cache_lens, B, dev)
-    _offsets_arg("kv_begin", kv_begin, T, dev)
-    _offsets_arg("kv_end", kv_end, T, dev)
+    _offsets_arg("cu_q", cu_q, B + 1, index)
+    _offsets_arg("cache_lens", cache_lens, B, index)
+    if kv_begin is not None:
+        _offsets_arg("kv_begin", kv_begin, T, index)
+    if kv_end is not None:
+        _offsets_arg("kv_end", kv_end, T, index)
     dt = _dt(q)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    with _on(dev):
-        stream = torch.cuda.current_stream().cuda_stream
+    with _on(index):
+        stream = _stream_handle(index)
         if ws is None:
             need = sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_pages * page, bwd)
             if need == 0:
                 raise SketchError(2, "sa_cache_attn_workspace_size")
-            ws = _stream_workspace(need, dev, stream)
-        st = entry(q.data_ptr(), q.stride(0), q.stride(1), cu_q.data_ptr(), B, T, Hq, pool.data_ptr(), n_pages, page,
+            ws = _stream_workspace(need, index, stream)
+        row, head, _ = q.stride()
+        st = entry(q.data_ptr(), row, head, cu_q.data_ptr(), B, T, Hq, pool.data_ptr(), n_pages, page,
                    block_table.data_ptr(), max_pages, cache_lens.data_ptr(), H, d, _addr(kv_begin), _addr(kv_end),
                    scale, dt, *[_addr(t) for t in tensors], ws.data_ptr(), ws.numel(), stream)
     _check(st, "sa_cache_attn_bwd" if bwd else "sa_cache_attn_fwd")
@@ -726,7 +742,7 @@ def sa_cache_attn_bwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, b
     The cached rows are constants and get no gradient."""
     for name, t, shape, dtype in (("out", out, q.shape, q.dtype), ("dout", dout, q.shape, q.dtype),
                                   ("lse", lse, q.shape[:2], torch.float32)):
-        if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.device != q.device:
+        if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != q.get_device():
             raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on q's device")
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     _cache_attn(load().sa_cache_attn_bwd, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale, ws, True,

@@ -425,3 +425,23 @@ def test_no_queries_at_all(cuda_lib, R):
     q = torch.randn((R, 2, 64), device="cuda").bfloat16()
     out, lse = cuda_lib.sa_cache_attn_fwd(q, gpu(np.array([0, 0, R], np.int32)), pool, table, lens, want_lse=True)
     assert out.shape == (R, 2, 64) and lse.shape == (R, 2) and torch.isfinite(out.float()).all()
+
+
+def test_the_example_runs_the_operators_together(cuda_lib):
+    from paper_2609_08443_gb300 import cached_targets
+
+    res = cached_targets.run(lengths=(900, 300, 130), H=2, P=128, d=64, candidates=70)
+    # a group's step is at most 1.125 / 7.5 of its largest value, its error uniform within half a step: under a
+    # tenth of a row's norm in keys and in values together
+    assert res["error"] < 0.2
+    assert torch.isfinite(res["z"].float()).all() and res["dq"].abs().sum() > 0
+    none = res["times"] == 0
+    assert torch.isinf(res["lse"][none]).all() and not res["recent"][none].any()
+    assert torch.isfinite(res["lse"][~none]).all()
+    pages = res["recents"]
+    held = [int(p) for p in pages.table.flatten() if p >= 0]
+    assert len(held) == len(set(held)) and not set(held) & set(pages.free)
+    pages.evict(0)
+    assert pages.lens[0] == 0 and int(pages.table[0].max()) == -1
+    with pytest.raises(RuntimeError):
+        pages.grow(1, 10 ** 6)
