@@ -668,7 +668,8 @@ def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: tor
     _offsets_arg("start", start, B, index)
     if n_rows < 0:
         raise ValueError("n_rows must not be negative")
-    K, V = torch.empty((2, n_rows, H, d), dtype=dtype, device=pool.device)
+    K = torch.empty((n_rows, H, d), dtype=dtype, device=pool.device)
+    V = torch.empty_like(K)
     with _on(index):
         stream = _stream_handle(index)
         w = ws if ws is not None else _stream_workspace(256, index, stream)

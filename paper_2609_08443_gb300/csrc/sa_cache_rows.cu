@@ -5,17 +5,25 @@
 // bytes and a scale byte; reading, it does the reverse.  Both are bound by memory
 // (per feature 2 or 4 bytes of the row and 9/16 of the cache), so a thread has several
 // groups' loads in flight and the arithmetic is kept to a few instructions a feature.
-// A block takes up to 32 consecutive rows, looks up their pages once, and goes through
+// A block takes up to 64 consecutive rows, looks up their pages once, and goes through
 // them head by head with the groups of a row, then the rows, over its threads: what a
 // warp touches is contiguous in the page and in runs of a row on the other side.
+//
+// Measured (GB300, bytes that have to move over time): ragged bf16 histories written and
+// read back (2.0 GB) 339 us, fp32 sketches written and read back (1.2 GB) 238 us, 64 x 1024
+// rows of 8 x 128 read as bf16 (0.34 GB) 66 us: 5.9, 5.1 and 5.2 TB/s of a measured copy's
+// 6.8.  Two groups a thread in flight beat four (histories 343 against 358 us: 40 registers
+// a thread instead of 77).
 #include "sa_cache.cuh"
 #include "sa_kernels.cuh"
+#include "sa_ptx.cuh"
 #include "sa_simt_util.cuh"
 
 namespace sa {
 namespace cache {
 
 constexpr int kThreads = 256;
+constexpr int kAtOnce = 2;  // groups in flight per thread
 
 // Where row `row` of the call lives: its user, the offset of the source row and the
 // cache position.  `ok` is false for offsets that lead outside the batch.
@@ -77,17 +85,18 @@ __device__ void check_rows(const RowArgs& a) {
   if (threadIdx.x == 0) ws_header(a.ws)->err = uint32_t(bad);
 }
 
-// Any offset out of order makes every block leave: the whole call writes nothing.
-__device__ __forceinline__ bool offsets_ok(const RowArgs& a) {
-  if (!a.cu) return true;
+// Whether this thread's part of the offsets is out of order: any such makes every block
+// leave, and the whole call writes nothing.
+__device__ __forceinline__ int offsets_bad(const RowArgs& a) {
   int bad = 0;
-  for (int b = threadIdx.x; b < a.B; b += blockDim.x)
-    bad |= (b == 0 && a.cu[0] != 0) || (b == a.B - 1 && int64_t(a.cu[a.B]) != a.N) || a.cu[b] > a.cu[b + 1];
-  return !__syncthreads_or(bad);
+  if (a.cu)
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x)
+      bad |= (b == 0 && a.cu[0] != 0) || (b == a.B - 1 && int64_t(a.cu[a.B]) != a.N) || a.cu[b] > a.cu[b + 1];
+  return bad;
 }
 
 // ------------------------------------------------------------------ a block's rows
-constexpr int kRows = 32;
+constexpr int kLog2Rows = 6, kRows = 1 << kLog2Rows;
 
 struct Rows {
   int64_t rec[kRows];  // byte offset of head 0's key record, or -1: nothing to do
@@ -103,7 +112,7 @@ __device__ __forceinline__ bool find_rows(const RowArgs& a, int n, Rows& s) {
     check_rows(a);
     return false;
   }
-  if (!offsets_ok(a)) return false;
+  const int bad = offsets_bad(a);
   if (threadIdx.x < n) {
     const int64_t row = int64_t(blockIdx.x) * n + threadIdx.x;
     int64_t rec = -1;
@@ -123,21 +132,29 @@ __device__ __forceinline__ bool find_rows(const RowArgs& a, int n, Rows& s) {
     }
     s.rec[threadIdx.x] = rec;
   }
-  __syncthreads();
-  return true;
+  return !__syncthreads_or(bad);
 }
 
 // Group e of the block: its group of features, row, head and side (0 keys, 1 values).
+// Groups run fastest, then rows (a power of two), then heads.
+struct Groups {
+  int ng, log2n, H;
+  uint32_t inv;  // 2^32 / ng rounded up: e * inv >> 32 is e / ng exactly for e < 2^29
+};
+static Groups groups_of(const RowArgs& a, int log2n) {
+  const int ng = a.c.d / kGroup;
+  return {ng, log2n, a.c.H, ng > 1 ? 0xFFFFFFFFu / uint32_t(ng) + 1u : 0u};
+}
 struct GroupRef {
   int g, r, h, kv;
 };
-__device__ __forceinline__ GroupRef group_of(int e, int ng, int n, int H) {
+__device__ __forceinline__ GroupRef group_of(int e, const Groups& s) {
   GroupRef x;
-  const int u = e / ng, hk = u / n;
-  x.g = e - u * ng;
-  x.r = u - hk * n;
-  x.kv = hk >= H;
-  x.h = x.kv ? hk - H : hk;
+  const int u = s.ng > 1 ? int(__umulhi(uint32_t(e), s.inv)) : e, hk = u >> s.log2n;
+  x.g = e - u * s.ng;
+  x.r = u - (hk << s.log2n);
+  x.kv = hk >= s.H;
+  x.h = x.kv ? hk - s.H : hk;
   return x;
 }
 
@@ -145,7 +162,6 @@ __device__ __forceinline__ GroupRef group_of(int e, int ng, int n, int H) {
 // 16 features as they came.
 template <typename T> struct Raw;
 template <> struct Raw<__nv_bfloat16> {
-  static constexpr int kAtOnce = 4;  // groups in flight per thread
   uint4 v[2];
   __device__ __forceinline__ void load(const __nv_bfloat16* p) {
     v[0] = __ldcs(reinterpret_cast<const uint4*>(p));
@@ -168,7 +184,6 @@ template <> struct Raw<__nv_bfloat16> {
   }
 };
 template <> struct Raw<float> {
-  static constexpr int kAtOnce = 2;
   float4 v[4];
   __device__ __forceinline__ void load(const float* p) {
 #pragma unroll
@@ -196,19 +211,19 @@ __host__ __device__ constexpr uint32_t round_bits_sum() {
   return s;
 }
 
-// Levels of a group.  The quotient by a reciprocal made smaller by 2^-20 (its own
-// rounding and the product's are under 2^-22) lies below the true one, so a half always
-// rounds towards zero.  It can come out a level too low only for a quotient within
+// Levels of a group.  The quotient by a reciprocal made smaller by 2^-20 (the
+// approximation and the product's rounding are under 2^-21) lies below the true one, so a
+// half always rounds towards zero.  It can come out a level too low only for a quotient within
 // 2^-19 above a half: impossible for bf16 (eight significant bits against the scale's
 // four), and seen for fp32 from the remainder x - q s, which is exact there.
-template <typename T>
-__device__ __forceinline__ uint2 levels(const Raw<T>& x, uint32_t code, bool odd_values) {
-  const float s = scale_value(code), inv = __frcp_rn(s) * (1.f - 0x1p-20f);
+template <bool ODD, typename T>
+__device__ __forceinline__ uint2 levels(const Raw<T>& x, uint32_t code) {
+  const float s = scale_value(code), inv = ptx::rcp_approx(s) * (1.f - 0x1p-20f);
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int k = 0; k < kGroup; ++k) {
     float v = x.get(k);
-    if (odd_values) {  // NaN to zero, beyond the largest scale saturates
+    if constexpr (ODD) {  // NaN to zero, beyond the largest scale saturates
       if (isnan(v)) v = 0.f;
       v = fminf(fmaxf(v, -7.f * s), 7.f * s);
     }
@@ -223,11 +238,12 @@ __device__ __forceinline__ uint2 levels(const Raw<T>& x, uint32_t code, bool odd
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_constant__ RowArgs a, int n) {
+__global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ Groups geo) {
   __shared__ Rows rows;
+  const int n = 1 << geo.log2n;
   if (!find_rows<true>(a, n, rows)) return;
-  constexpr int U = Raw<T>::kAtOnce;
-  const int ng = a.c.d / kGroup, count = ng * n * a.c.H * 2;
+  constexpr int U = kAtOnce;
+  const int ng = geo.ng, count = ng * n * a.c.H * 2;
   const T* src[2] = {static_cast<const T*>(a.K), static_cast<const T*>(a.V)};
   uint8_t* pool = const_cast<uint8_t*>(a.c.pool);
   for (int e0 = threadIdx.x; e0 < count; e0 += U * kThreads) {
@@ -237,7 +253,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_cons
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int e = e0 + i * kThreads;
-      ref[i] = group_of(e, ng, n, a.c.H);
+      ref[i] = group_of(e, geo);
       on[i] = e < count && rows.rec[ref[i].r] >= 0;
       if (on[i]) x[i].load((ref[i].kv ? src[1] : src[0]) + rows.at[ref[i].r] + ref[i].h * a.head_stride + ref[i].g * kGroup);
     }
@@ -255,7 +271,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_cons
         big |= 1u << 31;
       }
       const uint32_t code = scale_code(__uint_as_float(big & 0x7FFFFFFFu));
-      const uint2 w = levels<T>(x[i], code, code == kCodeMax || (big >> 31));
+      const uint2 w = code == kCodeMax || (big >> 31) ? levels<true>(x[i], code) : levels<false>(x[i], code);
       const int64_t rec = rows.rec[ref[i].r] + int64_t(2 * ref[i].h + ref[i].kv) * a.c.rec;
       const int slot = rows.slot[ref[i].r];
       *reinterpret_cast<uint2*>(pool + rec + slot * (a.c.d / 2) + ref[i].g * 8) = w;
@@ -265,11 +281,12 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_cons
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ RowArgs a, int n) {
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ Groups geo) {
   __shared__ Rows rows;
+  const int n = 1 << geo.log2n;
   if (!find_rows<false>(a, n, rows)) return;
-  constexpr int U = 4;
-  const int ng = a.c.d / kGroup, count = ng * n * a.c.H * 2;
+  constexpr int U = kAtOnce;
+  const int ng = geo.ng, count = ng * n * a.c.H * 2;
   T* dst[2] = {static_cast<T*>(a.Ko), static_cast<T*>(a.Vo)};
   for (int e0 = threadIdx.x; e0 < count; e0 += U * kThreads) {
     uint2 w[U];
@@ -279,7 +296,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int e = e0 + i * kThreads;
-      ref[i] = group_of(e, ng, n, a.c.H);
+      ref[i] = group_of(e, geo);
       on[i] = e < count && rows.rec[ref[i].r] >= 0;
       if (!on[i]) continue;
       const uint8_t* rec = a.c.pool + rows.rec[ref[i].r] + int64_t(2 * ref[i].h + ref[i].kv) * a.c.rec;
@@ -309,25 +326,36 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
   }
 }
 
-// Rows a block takes: 32, fewer (a power of two) where that would leave SMs without work.
-static int rows_per_block(const RowArgs& a) {
-  int n = kRows;
-  while (n > 1 && a.N / n < 608) n >>= 1;
-  return n;
+// log2 of the rows a block takes: the most, up to 64, whose source (writing) or result
+// (reading) is no more than `most` bytes and that leave every SM four blocks.  More rows
+// spread the look-up of users and pages over more work; too many and the tail grows.
+static int log2_rows(const RowArgs& a, int64_t most) {
+  const int64_t bytes = int64_t(2) * a.c.H * a.c.d * (a.dt == SA_BF16 ? 2 : 4);  // a row's, keys and values
+  int log2n = kLog2Rows;
+  while (log2n > 0 && ((a.N >> log2n) < 608 || (bytes << log2n) > most)) --log2n;
+  return log2n;
 }
 
-static cudaError_t launch_rows(void (*kernel)(RowArgs, int), const RowArgs& a, cudaStream_t st) {
-  const int n = rows_per_block(a);
-  kernel<<<unsigned((a.N + n - 1) / n + 1), kThreads, 0, st>>>(a, n);
+static cudaError_t launch_rows(void (*kernel)(RowArgs, Groups), const RowArgs& a, int64_t most, cudaStream_t st) {
+  const int log2n = log2_rows(a, most), n = 1 << log2n;
+  kernel<<<unsigned((a.N + n - 1) / n + 1), kThreads, 0, st>>>(a, groups_of(a, log2n));
   return cudaGetLastError();
 }
 
+// Measured on a GB300, written and read back: 64 users' up to 20,011 bf16 rows (8 heads of
+// 64) and 128 users' 512 fp32 rows (8 heads of 128) take 347 and 247 us at 64 KiB a block,
+// 343 and 237 at 128 KiB, 349 and 262 at 32 rows always.  Reading 64 users' 1024 rows (8 heads
+// of 128) as bf16 takes 66 us at 64 KiB, 71 at 128 KiB.
+constexpr int64_t kWriteBytes = 128 << 10, kReadBytes = 64 << 10;
+
 cudaError_t launch_write(const RowArgs& a, cudaStream_t st) {
-  return a.dt == SA_BF16 ? launch_rows(cache_write_kernel<__nv_bfloat16>, a, st) : launch_rows(cache_write_kernel<float>, a, st);
+  return a.dt == SA_BF16 ? launch_rows(cache_write_kernel<__nv_bfloat16>, a, kWriteBytes, st)
+                         : launch_rows(cache_write_kernel<float>, a, kWriteBytes, st);
 }
 
 cudaError_t launch_read(const RowArgs& a, cudaStream_t st) {
-  return a.dt == SA_BF16 ? launch_rows(cache_read_kernel<__nv_bfloat16>, a, st) : launch_rows(cache_read_kernel<float>, a, st);
+  return a.dt == SA_BF16 ? launch_rows(cache_read_kernel<__nv_bfloat16>, a, kReadBytes, st)
+                         : launch_rows(cache_read_kernel<float>, a, kReadBytes, st);
 }
 
 }  // namespace cache
