@@ -18,6 +18,12 @@
 // reading the cache, 144 bytes a key and head at d = 128, and next by issuing about
 // 20 instructions a key and head and warp, four fifths of them dequantisation.
 //
+// Measured (GB300): one query of 16 users over up to 100,000 positions, 8 heads of 128
+// (0.82 GB of cache), 215 us: 3.8 TB/s of a measured copy's 6.8, DRAM busy 56 %, the integer
+// pipe and issue 55 % each.  A lone query over 512 positions takes 15 us, two launches and
+// a walk of one block a warp.  Three or four tiles of rows a warp for the gradient
+// spilled and were slower, plain asynchronous copies instead of bulk copies the same.
+//
 // Work is the list of (user, cached head, row tile, block of positions), cut into
 // equal contiguous shares; a segment cut by share borders leaves unfinished
 // (O, max, sum) pieces that the join kernel adds in order.  Every CTA scans the
@@ -595,7 +601,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
         const int i = 8 * n + 2 * t4 + e;
         const int64_t o = dense(i);
         if (o < 0) continue;
-        const float f = !whole ? 1.f : C::BWD ? a.scale : sum > 0.f ? 1.f / sum : 0.f;
+        const float f = !whole ? 1.f : C::BWD ? a.scale : sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int w = 0; w < PER / 8; ++w) {
           float y[8];
@@ -613,7 +619,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
             if (!whole)
               *reinterpret_cast<float2*>(part + C::ROWS * C::D + 2 * i) = make_float2(m[n][e], sum);
             else if (a.lse)
-              a.lse[o] = sum > 0.f ? (m[n][e] + log2f(sum) - kLift) * kLn2 : -INFINITY;
+              a.lse[o] = sum == 0.f ? -INFINITY : (m[n][e] + log2f(sum) - kLift) * kLn2;
           }
         }
       }

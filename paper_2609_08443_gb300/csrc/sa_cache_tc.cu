@@ -20,9 +20,17 @@
 // arrives O is at rest.
 //
 // Warp roles: 0 walks the share, publishes its pieces to the other roles and copies the
-// pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 and 3 load the halves' query rows, 4..7 dequantise keys, 8..11 values,
-// 12..19 softmax and results.  Every wait is bounded: past the limit
-// the CTA's roles leave, its copies and products drain and the error is reported.
+// pages' codes and scales into a ring (bulk copies), 1 issues the products, 2 and 3 load
+// the halves' query rows, 4..11 dequantise, 12..19 softmax and results.  Every wait is
+// bounded: past the limit the CTA's roles leave, its copies and products drain and the
+// error is reported.
+//
+// Measured (GB300): 300 queries of 16 users over 10,000 positions, 8 heads of 128, 276 us, 713
+// TFLOP/s of a library product's 1894; the warp-level kernel takes 988.  No resource is
+// full (tensor pipe about 40 %): a block of 128 positions x 256 rows takes about 2,700
+// cycles, and dequantising, exponentials and issue each fill most of them with one
+// warp's instructions in a row.  Two issuers, 64 positions with twice the score buffers,
+// two CTAs an SM, and loads straight from the pages into registers were all slower.
 #include "sa_cache_tc.cuh"
 
 namespace sa {
@@ -441,7 +449,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
         if (!whole)
           *reinterpret_cast<float2*>(part + C::ROWS * D + 2 * i) = make_float2(m, l);
         else if (a.lse)
-          a.lse[o] = l > 0.f ? (m + log2f(l) - kLift) * kLn2 : -INFINITY;
+          a.lse[o] = l == 0.f ? -INFINITY : (m + log2f(l) - kLift) * kLn2;
       };
       if (un.n == 0 && g == 0) {  // nobody sees anything
         float zero[32] = {};
@@ -546,7 +554,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
           f1 = s.x == -INFINITY ? 0.f : ex2(s.x - m);
           l = l * f0 + s.y * f1;
         }
-        const float f = !whole ? 1.f : l > 0.f ? 1.f / l : 0.f;
+        const float f = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
         f0 *= f;
         f1 *= f;
 #pragma unroll 1
@@ -595,12 +603,20 @@ static cudaError_t run_fwd(const AttnArgs& a, cudaStream_t st) {
   return e2 != cudaSuccess ? e2 : launch_join<C>(a, st);
 }
 
-// Taken where the average user has at least 64 rows for a cached head: below that most of
-// the 128 rows of a product are padding.  The forward takes its maximum on the raw scores,
-// so its scale is positive.
+// Taken from so many rows (queries times query heads) of an average user for a cached
+// head: the tcgen05 kernels take about the same time up to 128 rows, the warp-level ones go up by
+// 16.  Measured on a GB300, us (tcgen05 | warp-level), 16 users x 8 heads x 10,000 positions:
+//     rows                 16          32          48          64          128
+//     forward, d = 128     114 |  83   115 | 128   116 | 178   118 | 229   126 | 428
+//     forward, d = 64      104 |  57   104 |  87   106 | 119   106 | 149   112 | 277
+//     gradient, d = 128    180 | 105   182 | 166   183 | 233   186 | 300   193 | 566
+//     gradient, d = 64     168 |  68   169 | 103   169 | 141   171 | 178   174 | 334
+// and the same order at 64 users x 4 heads x 1024 (forward, d = 128: 43 | 47 at 32 rows; gradient: 55
+// | 57).  The forward takes its maximum on the raw scores, so its scale is positive.
 bool tc_supported(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd) {
-  if (dt != SA_BF16 || (d != 64 && d != 128) || (!bwd && !(scale > 0.f)) || T * G < int64_t(64) * B) return false;
-  return tcc::device_is_sm103();
+  if (dt != SA_BF16 || (d != 64 && d != 128) || (!bwd && !(scale > 0.f))) return false;
+  const int64_t rows = d == 128 ? (bwd ? 40 : 32) : (bwd ? 56 : 40);
+  return T * G >= rows * B && tcc::device_is_sm103();
 }
 
 AttnPlan tc_plan(int sms, int d, bool bwd) {

@@ -48,7 +48,7 @@ __device__ __forceinline__ void l2_prefetch_if(uint32_t e, const void* src, uint
 // The roles share one instruction cache, whose first level is small; a role that runs
 // straight through cold code takes about ten cycles an instruction, and with the waits'
 // slow paths inlined the issuing warp alone was slower than its products.  So the loops
-// below are kept short, and what is rare is out of line.
+// below are kept short and not unrolled.
 
 // Control words of a CTA in shared memory.
 struct Ctl {

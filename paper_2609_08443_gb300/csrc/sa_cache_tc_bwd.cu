@@ -17,6 +17,13 @@
 // load the rows of Q and dO, 4..7 dequantise keys, 8..11 values, 12..19 dS and results.  Every
 // wait is bounded: past the limit the CTA's roles leave, its copies and products drain
 // and the error is reported.
+//
+// Measured (GB300): 40 queries x 16 heads of 64 users over one shared head of 1024 x 128,
+// 74 us (435 TFLOP/s of a library product's 1894; the warp-level kernel 171); up to 300 windowed
+// queries of 16 users over up to 10,000 positions, 8 heads of 128, 264 us (warp-level 585;
+// windows hide two thirds of the products that the blocks make).  Bound like the forward, by
+// the roles' own instructions: without exponentials 250, with an eighth of the products
+// 240, with a quarter of the dequantisation 248, with a quarter of the copies' code 262.
 #include "sa_cache_tc.cuh"
 #include "sa_simt_util.cuh"
 

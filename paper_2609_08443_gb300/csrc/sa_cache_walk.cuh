@@ -335,12 +335,12 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
     if (split == 0 && r < rows) {
       const int row = p.rt * ROWS + r;
       const int64_t o = (q0 + row / a.G) * a.Hq + p.h * a.G + row % a.G;
-      const float f = C::BWD ? a.scale : (l > 0.f ? 1.f / l : 0.f);
+      const float f = C::BWD ? a.scale : (l == 0.f ? 0.f : 1.f / l);
       T* dst = static_cast<T*>(C::BWD ? a.dq : a.out) + o * d;
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (32 * i + lane < d) st_from_f32(dst + 32 * i + lane, y[i] * f);
-      if (!C::BWD && a.lse && lane == 0) a.lse[o] = l > 0.f ? (m + log2f(l) - kLift) * kLn2 : -INFINITY;
+      if (!C::BWD && a.lse && lane == 0) a.lse[o] = l == 0.f ? -INFINITY : (m + log2f(l) - kLift) * kLn2;
     }
   }
 }

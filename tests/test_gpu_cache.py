@@ -445,3 +445,32 @@ def test_the_example_runs_the_operators_together(cuda_lib):
     assert pages.lens[0] == 0 and int(pages.table[0].max()) == -1
     with pytest.raises(RuntimeError):
         pages.grow(1, 10 ** 6)
+
+
+@pytest.mark.parametrize("dt,R,L", [("bf16", 1, 70), ("f32", 2, 70), ("bf16", 160, 70), ("bf16", 1, 60000),
+                                    ("bf16", 130, 60000)])
+def test_a_nan_query_has_nan_for_its_sum_and_gradient(cuda_lib, dt, R, L):
+    cache = cc.Cache([L], 1, 64, 64, seed=9)
+    pool, table, lens = cache.tensors()
+    cu = gpu(np.array([0, R + 1], np.int32))
+    q = torch.randn((R + 1, 1, 64), device="cuda").to(cc.TORCH[dt])
+    q[R, 0, 5] = float("nan")
+    end = torch.full((R + 1,), L, dtype=torch.int32, device="cuda")
+    for sees, value in ((True, float("nan")), (False, float("-inf"))):
+        end[R] = L if sees else 0
+        out, lse = cuda_lib.sa_cache_attn_fwd(q, cu, pool, table, lens, kv_end=end, want_lse=True)
+        dq = cuda_lib.sa_cache_attn_bwd(q, cu, pool, table, lens, out, lse, torch.ones_like(q), kv_end=end)
+        assert torch.isfinite(lse[:R]).all() and torch.isfinite(dq[:R]).all()
+        if sees:
+            assert torch.isnan(lse[R]).all() and torch.isnan(out[R]).all() and torch.isnan(dq[R]).all()
+        else:
+            assert lse[R].item() == value and not out[R].any() and not dq[R].any()
+
+
+@pytest.mark.parametrize("d,bwd,rows", [(128, False, 32), (64, False, 40), (128, True, 40), (64, True, 56)])
+def test_both_sides_of_the_choice_of_kernels(cuda_lib, d, bwd, rows):
+    names = [cuda_lib.sa_cache_attn_kernel_name(3, 3 * r, 2, 2, d, 0.1, cuda_lib.SA_BF16, bwd) for r in (rows - 1, rows)]
+    assert names[0].startswith("mma") and names[1].startswith("tc5")
+    cache = cc.Cache([300, 77, 512], 2, d, 64, seed=rows)
+    for r in (rows - 1, rows):
+        run_both(cuda_lib, cache, [r, r, r], 1, "bf16", seed=r)
