@@ -83,7 +83,10 @@ sa_status sa_cache_read(const void* pool, int64_t n_pages, int page, const int32
  * bf16 queries exactly (fp32 queries as three bf16 terms) and accumulate in fp32;
  * the weights are rounded to float16 before they meet the values (two float16
  * terms for fp32; a weight below 2^-37 of the largest counts as nothing), their
- * sum is kept in fp32. */
+ * sum is kept in fp32.
+ * The workspace is a few MB to tens of MB of unfinished pieces, one or two per worker; its
+ * size depends on neither the lengths nor max_tokens, the most cached positions of a
+ * user, which may not be negative. */
 size_t sa_cache_attn_workspace_size(int B, int64_t T, int Hq, int H, int d, sa_dtype dt, int64_t max_tokens, int bwd);
 sa_status sa_cache_attn_fwd(const void* q, int64_t q_row_stride, int64_t q_head_stride, const int32_t* cu_q, int B,
                             int64_t T, int Hq, const void* pool, int64_t n_pages, int page,

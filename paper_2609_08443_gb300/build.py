@@ -83,11 +83,14 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
 
 
 def source_hash() -> str:
-    """Hash of the CUDA sources and the ABI header (ties profiles to a build)."""
+    """Hash of the sketching step's CUDA sources and its ABI header (ties its traffic record to a
+    build; the cache's kernels, csrc/sa_cache*, have no part in that step)."""
     import hashlib
 
     h = hashlib.sha256()
     for f in sorted(os.listdir(CSRC)):
+        if f.startswith("sa_cache"):
+            continue
         with open(os.path.join(CSRC, f), "rb") as fh:
             h.update(f.encode() + b"\0" + fh.read())
     with open(os.path.join(ROOT, "include", "sa_sketch.h"), "rb") as fh:

@@ -21,7 +21,7 @@
 // Measured (GB300): one query of 16 users over up to 100,000 positions, 8 heads of 128
 // (0.82 GB of cache), 215 us: 3.8 TB/s of a measured copy's 6.8, DRAM busy 56 %, the integer
 // pipe and issue 55 % each.  A lone query over 512 positions takes 15 us, two launches and
-// a walk of one block a warp.  Three or four tiles of rows a warp for the gradient
+// a walk of one block a warp.  Four tiles of 8 rows a warp for the bf16 gradient
 // spilled and were slower, plain asynchronous copies instead of bulk copies the same.
 //
 // Work is the list of (user, cached head, row tile, block of positions), cut into
@@ -652,8 +652,17 @@ static cudaError_t run(const AttnArgs& a, cudaStream_t st) {
 }
 
 // Rows of a tile: 8 where a user's rows fit (the average over the call decides: half the
-// products and registers of 16), else 16, which reads the cache half as often.
-static bool two_tiles(int B, int64_t T, int G) { return T * G > int64_t(8) * B; }
+// products and registers of 16), else 16, which dequantises half as often; always 8 for the
+// fp32 gradient, whose 16 rows spill.  Measured on a GB300, us (8 | 16 a tile), 16 users x 8
+// heads x 10,000 positions:
+//                          8 rows        16 rows
+//     forward, bf16        67 | 76      107 |  84    (d = 128; 64: 48 | 54 and 71 | 58)
+//     forward, fp32        75 | 110     122 | 119    (d = 64: 49 | 69 and 77 | 74)
+//     gradient, bf16       80 | 96      127 | 106    (d = 64: 49 | 61 and 76 | 68)
+//     gradient, fp32      111 | 223     195 | 230    (d = 64: 64 | 95 and 104 | 104)
+static bool two_tiles(int B, int64_t T, int G, sa_dtype dt, bool bwd) {
+  return T * G > int64_t(8) * B && !(bwd && dt == SA_F32);
+}
 
 // f(configuration) for a call's sizes
 template <class F>
@@ -661,7 +670,10 @@ static auto with_config(int d, sa_dtype dt, bool bwd, bool two, F&& f) {
   auto rows = [&](auto D, auto f32, auto back) {
     constexpr int W = decltype(D)::value;
     constexpr bool X = decltype(f32)::value, Y = decltype(back)::value;
-    return two ? f(Cfg<W, X, Y, 2>{}) : f(Cfg<W, X, Y, 1>{});
+    if constexpr (!(X && Y)) {
+      if (two) return f(Cfg<W, X, Y, 2>{});
+    }
+    return f(Cfg<W, X, Y, 1>{});
   };
   auto dir = [&](auto D, auto f32) { return bwd ? rows(D, f32, std::true_type{}) : rows(D, f32, std::false_type{}); };
   auto type = [&](auto D) { return dt == SA_F32 ? dir(D, std::true_type{}) : dir(D, std::false_type{}); };
@@ -671,15 +683,15 @@ static auto with_config(int d, sa_dtype dt, bool bwd, bool two, F&& f) {
 AttnPlan mma_plan(int sms, int B, int64_t T, int G, int d, sa_dtype dt, bool bwd) {
   AttnPlan p;
   p.ctas = sms;
-  p.workers = sms * with_config(d, dt, bwd, two_tiles(B, T, G), [](auto c) { return decltype(c)::NWARP; });
+  p.workers = sms * with_config(d, dt, bwd, two_tiles(B, T, G, dt, bwd), [](auto c) { return decltype(c)::NWARP; });
   p.piece_bytes = sizeof(Piece);
   p.partial_floats =
-      with_config(d, dt, bwd, two_tiles(B, T, G), [](auto c) { return partial_floats(decltype(c)::ROWS, decltype(c)::D); });
+      with_config(d, dt, bwd, two_tiles(B, T, G, dt, bwd), [](auto c) { return partial_floats(decltype(c)::ROWS, decltype(c)::D); });
   return p;
 }
 
 cudaError_t launch_mma(const AttnArgs& a, bool bwd, cudaStream_t st) {
-  return with_config(a.c.d, a.dt, bwd, two_tiles(a.B, a.T, a.G), [&](auto c) { return run<decltype(c)>(a, st); });
+  return with_config(a.c.d, a.dt, bwd, two_tiles(a.B, a.T, a.G, a.dt, bwd), [&](auto c) { return run<decltype(c)>(a, st); });
 }
 
 }  // namespace cache
