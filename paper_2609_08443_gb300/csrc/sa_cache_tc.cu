@@ -27,7 +27,7 @@
 //
 // Measured (GB300): 300 queries of 16 users over 10,000 positions, 8 heads of 128, 276 us, 713
 // TFLOP/s of a library product's 1894; the warp-level kernel takes 988.  No resource is
-// full (tensor pipe 35 %, integer pipe 36 %): a block of 128 positions x 256 rows takes about 2,700
+// full (tensor pipe 44 %, integer pipe 41 %): a block of 128 positions x 256 rows takes about 2,700
 // cycles, and dequantising, exponentials and issue each fill most of them with one
 // warp's instructions in a row.  Two issuers, 64 positions with twice the score buffers,
 // two CTAs an SM, and loads straight from the pages into registers were all slower.
