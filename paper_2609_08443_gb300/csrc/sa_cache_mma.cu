@@ -19,8 +19,8 @@
 // 20 instructions a key and head and warp, four fifths of them dequantisation.
 //
 // Measured (GB300): one query of 16 users over up to 100,000 positions, 8 heads of 128
-// (0.82 GB of cache), 215 us: 3.8 TB/s of a measured copy's 6.8, DRAM busy 56 %, the integer
-// pipe and issue 55 % each.  A lone query over 512 positions takes 15 us, two launches and
+// (0.82 GB of cache), 211 us: 3.9 TB/s of a measured copy's 6.8, DRAM busy 52 %, the integer
+// pipe 54 %, issue slots 67 %.  A lone query over 512 positions takes 13 us, two launches and
 // a walk of one block a warp.  Four tiles of 8 rows a warp for the bf16 gradient
 // spilled and were slower, plain asynchronous copies instead of bulk copies the same.
 //

@@ -238,7 +238,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
 // time and split each row's pieces 8 / rp ways: with one row (a single token over a long
 // history) a segment has many pieces, with sixteen it has few.  Its launch overlaps the main
 // kernel's tail; what it adds is latency: one query of 16 users over up to 100,000 positions
-// takes 215 us, the main kernel alone 210 (GB300).
+// takes 210 us, the main kernel alone 201 (GB300).
 constexpr int kJoinWarps = 8;
 
 template <class C>
@@ -262,20 +262,26 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
   if (total <= 0) return;
   const int W = shares(a, total);
   if (w >= W) return;
-  const int64_t tb = range_begin(total, W, w);
+  // one unit a share in a small call: no divisions (each costs about as much as a load)
+  auto begin = [&](int x) { return W == total ? int64_t(x) : range_begin(total, W, x); };
   const Piece p = static_cast<const Piece*>(a.piece)[w];
-  if (p.seg0 >= tb) return;
-  if (range_begin(total, W, w - 1) > p.seg0) return;  // an earlier border already cut this segment
-  const int first = w - 1, n = owner_of(total, W, p.seg1 - 1) - first + 1;
+  if (p.seg0 >= begin(w)) return;
+  if (begin(w - 1) > p.seg0) return;  // an earlier border already cut this segment
+  const int first = w - 1;
+  const int n = (W == total ? int(p.seg1 - 1) : owner_of(total, W, p.seg1 - 1)) - first + 1;
   constexpr int ROWS = C::ROWS, PF = partial_floats(ROWS, C::D);
   // the first worker's piece is its second one unless its share begins with the segment
   const float* base = a.partial + int64_t(first) * 2 * PF;
-  const int first_off = range_begin(total, W, first) >= p.seg0 ? 0 : PF;
+  const int first_off = begin(first) >= p.seg0 ? 0 : PF;
   const int64_t q0 = a.cu_q[p.b];
   const int rows = min(ROWS, int((a.cu_q[p.b + 1] - q0) * a.G - p.rt * ROWS));
   const int rp = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, ns = kJoinWarps / rp;
   const int split = warp / rp, d = a.c.d;
-  constexpr int V = C::D / 32;
+  // Pieces whose loads are in flight: they come from L2, and their latency is the time.  A
+  // tall tile's segments are cut into few (300 queries over 10,000 positions: the call takes
+  // 274 us with two, 277 with four, 281 with eight; up to 7 windowed queries over 3001: 20 us
+  // with eight, 27 with four).
+  constexpr int V = C::D / 32, AT = ROWS > 16 ? 2 : 8;
   __shared__ float part[kJoinWarps][C::D];
   __shared__ float2 stat[kJoinWarps];
   for (int r0 = blockIdx.y * rp; r0 < rows; r0 += gridDim.y * rp) {
@@ -303,12 +309,21 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_join_kernel(const __gri
           m = nm;
         }
         const int cnt = min(32, n - k0);
-#pragma unroll 4
-        for (int j = 0; j < cnt; ++j) {
-          const float* s = base + int64_t(k0 + j) * 2 * PF + (k0 + j == 0 ? first_off : 0) + r * C::D + lane;
-          const float fj = __shfl_sync(0xffffffffu, f, j);
+        for (int j0 = 0; j0 < cnt; j0 += AT) {
+          float s[AT][V];
 #pragma unroll
-          for (int i = 0; i < V; ++i) y[i] = fmaf(s[32 * i], fj, y[i]);
+          for (int j = 0; j < AT; ++j) {
+            const int k = k0 + j0 + j;
+            const float* src = base + int64_t(k) * 2 * PF + (k == 0 ? first_off : 0) + r * C::D + lane;
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[j][i] = k < n ? src[32 * i] : 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < AT; ++j) {
+            const float fj = __shfl_sync(0xffffffffu, f, j0 + j);
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = fmaf(s[j][i], fj, y[i]);
+          }
         }
       }
     }
