@@ -159,6 +159,18 @@ __device__ __forceinline__ void values_f16(uint32_t w, uint32_t s2, uint32_t* r)
   r[2] = mul_f16x2(add_f16x2(and_or(v, 0x000F000Fu, 0x64006400u), 0xE408E408u), s2);
   r[3] = mul_f16x2(fma_f16x2(and_or(v, 0x00F000F0u, 0x64006400u), 0x2C002C00u, 0xD480D480u), s2);
 }
+
+// What no written row has, but bytes that nobody wrote can: a code above kCodeMax, which
+// float16 reads as an infinity, a NaN or a value past the format's range, and level -8
+// with one of the two scales (codes 224, 225) whose eighth multiple float16 does not hold.
+// A hidden position's weight is 0, and 0 x inf is not 0, so such codes count as 0 and
+// such levels as -7; written rows come out as they are.
+constexpr uint32_t kCodeSafe = 223;  // up to it 8 x scale is finite
+__device__ __forceinline__ uint32_t level_min7(uint32_t w) {
+  uint32_t any = w | w >> 1;
+  any |= any >> 2;  // the lowest bit of each nibble: whether it has one set
+  return w | (~any & 0x11111111u);
+}
 #endif
 
 }  // namespace cache

@@ -235,11 +235,11 @@ struct Warp {
     }
   }
   // acc += (rows of 16 keys from 16 jj, transposed) x weights B, WT terms each; F16 or bf16
-  // values.  Keys outside [first, last) of the block count as zero: what nobody wrote can
-  // read as an infinity in float16, and 0 x inf is not 0.
+  // values.  `inside`: every row sees the whole block.  Where one does not, the hidden keys'
+  // bytes may be nobody's, which float16 may read as infinities (bf16 never does).
   template <bool F16, int WT>
   __device__ __forceinline__ void combine(const uint8_t* st, int jj, int kv, const uint32_t (*B)[WT][2],
-                                          float (*acc)[C::NR][4], bool inside, int first, int last) const {
+                                          float (*acc)[C::NR][4], bool inside) const {
     int k[4];
     k[0] = 16 * jj + key_of(2 * t4);
     k[1] = 16 * jj + key_of(2 * t4 + 1);
@@ -258,7 +258,11 @@ struct Warp {
         w[i][0] = *reinterpret_cast<const uint32_t*>(p);
         code[i] = scales(st, k[i], kv)[g >> 1];
       }
-      if (!inside && (k[i] < first || k[i] >= last)) code[i] = 0;
+      if (F16 && !inside && code[i] > kCodeSafe) {
+        if (code[i] > kCodeMax) code[i] = 0;
+#pragma unroll
+        for (int j = 0; j < NW; ++j) w[i][j] = level_min7(w[i][j]);
+      }
     }
     const uint32_t c01 = code[0] | code[1] << 16, c23 = code[2] | code[3] << 16;
     const ScaleB sb01 = scale_bf16(c01), sb23 = scale_bf16(c23);
@@ -543,7 +547,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
               }
             }
           }
-          x.template combine<true, C::NP>(st, i, 1, B, acc, inside, cur.vis0 - k0, cur.vis1 - k0);
+          x.template combine<true, C::NP>(st, i, 1, B, acc, inside);
         }
       } else {
         constexpr int HM = KB / 32;  // half a block at a time: two products' scores are live
@@ -574,7 +578,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
                   p[2 * u] -= f.x, p[2 * u + 1] -= f.y;
                 }
             }
-            x.template combine<false, C::NS>(st, HM * half + i, 0, B, acc, true, 0, KB);
+            x.template combine<false, C::NS>(st, HM * half + i, 0, B, acc, true);
           }
         }
       }

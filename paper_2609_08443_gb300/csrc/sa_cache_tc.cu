@@ -74,7 +74,6 @@ struct Units {
   int halves;    // 1 or 2
   int parity;
   int kb0;       // first block
-  int vis0, vis1;
   int rows;      // of the tile
   int row0;      // of the tile within the user's rows of this head
   int h, len;
@@ -207,8 +206,6 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
           u.halves = cur.weight;
           u.parity = parity;
           u.kb0 = cur.kb0;
-          u.vis0 = cur.vis0;
-          u.vis1 = cur.vis1;
           u.row0 = cur.rt * C::ROWS;
           u.rows = min(cur.s.rows - u.row0, C::ROWS);
           u.h = cur.h;
@@ -359,16 +356,14 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
     for (Units un; next(un); done()) {
 #pragma unroll 1
       for (int i = 0; i < 2 * un.n; ++i, ++c) {
-        const int kv = i & 1, kb = un.kb0 + (i >> 1);
+        const int kv = i & 1;
         const uint32_t rs = c % C::NRAW, s = c % C::NSLOT;
         if (!wait(raw_full(rs), c / C::NRAW, 0xD31u)) break;
         if (c >= C::NSLOT && !wait(slot_empty(s), c / C::NSLOT + 1, 0xD32u)) break;
         const uint8_t* raw = smem + C::OFF_RAW + rs * C::RAW;
         uint8_t* out = smem + C::OFF_RING + s * C::TILE;
-        // positions that no row of the tile sees count as zero values: what nobody
-        // wrote can read as an infinity in float16, and 0 x inf is not 0
-        const int from = kv ? un.vis0 - kb * C::KB : 0, to = kv ? un.vis1 - kb * C::KB : C::KB;
-        auto rows = [&](auto values) {
+        // hidden positions' bytes may be nobody's, which float16 may read as infinities
+        auto rows = [&](auto f16, auto values) {
 #pragma unroll 1
           for (int p = 0; p < 2; ++p) {
             const int r = 64 * p + 8 * w + (lane >> 2);
@@ -387,7 +382,11 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
               x[0] = v.x, x[1] = v.y;
               code = raw[C::KB * (D / 2) + r * (D / 16) + q4];
             }
-            if (r < from || r >= to) code = 0;
+            if (f16 && ((code & 255u) > kCodeSafe || (code >> 8) > kCodeSafe)) {
+              code = ((code & 255u) > kCodeMax ? 0u : code & 255u) | ((code >> 8) > kCodeMax ? 0u : code & 0xFF00u);
+#pragma unroll
+              for (int i = 0; i < NW; ++i) x[i] = level_min7(x[i]);
+            }
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
               const int word = D == 128 ? (i ^ (q4 & 2)) : i;  // of the lane's quarter
@@ -400,9 +399,9 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
           }
         };
         if (kv)
-          rows([](uint32_t x, uint32_t cc, uint32_t* y) { values_f16(x, cc << 7, y); });
+          rows(std::true_type{}, [](uint32_t x, uint32_t cc, uint32_t* y) { values_f16(x, cc << 7, y); });
         else
-          rows([](uint32_t x, uint32_t cc, uint32_t* y) { values_bf16(x, scale_bf16(cc), y); });
+          rows(std::false_type{}, [](uint32_t x, uint32_t cc, uint32_t* y) { values_bf16(x, scale_bf16(cc), y); });
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
