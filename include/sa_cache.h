@@ -27,7 +27,8 @@
  *   - d is a multiple of 16, 16..128; 1 <= H <= 64 cached heads.
  *   - block_table : int32 [B, max_pages].  Entries outside a user's positions are
  *     not looked at.  A used entry outside [0, n_pages) is skipped and reported
- *     (SA_ERR_BAD_PAGE); the results of that call are then undefined.
+ *     (SA_ERR_BAD_PAGE); the results of that call are then undefined.  Attention
+ *     uses an entry where a query sees one of the page's positions.
  *   - `workspace` is 256-byte aligned and need not be cleared.  Its error word is
  *     read by sa_get_device_error(); bad offsets give SA_ERR_BAD_SEQLENS and the
  *     call writes nothing.

@@ -140,10 +140,10 @@ struct Warp {
     const uint32_t s = issued & 1u;
     const uint32_t b = bar + 8u * s;
     const uint32_t dst = smem_u32(ring) + s * C::STAGE;
-    bool want = wanted(w, kb);
-    if (want && (pid < 0 || pid >= a.c.n_pages)) {
-      atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
-      want = false;
+    const bool there = pid >= 0 && pid < a.c.n_pages, want = wanted(w, kb) && there;
+    for (uint32_t m = __ballot_sync(0xffffffffu, wanted(w, kb) && !there && (lane & 3) == 0); m; m &= m - 1) {
+      const int n = min(a.c.page, KB), p0 = kb * KB + ((__ffs(m) - 1) >> 2) * n;
+      if (tile_sees<C>(a, w, p0, p0 + n, lane) && lane == 0) atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
     }
     if (a.c.page == KB) {  // a block is a page, and a page's records lie as the stage does
       if (lane == 0) {

@@ -225,10 +225,10 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
         // the pages of this block and the next two; two blocks ahead go to L2
         int pid = page_of(cur, cur.kb0), pid1 = page_of(cur, cur.kb0 + 1), pid2 = page_of(cur, cur.kb0 + 2);
         for (int kb = cur.kb0; kb < cur.kb1 && ok; ++kb) {
-          bool want = pid != -2;
-          if (want && (pid < 0 || pid >= a.c.n_pages)) {
-            atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
-            want = false;
+          const bool want = pid >= 0 && pid < a.c.n_pages;
+          for (uint32_t m = __ballot_sync(0xffffffffu, pid != -2 && !want && !part); m; m &= m - 1) {
+            const int p0 = kb * C::KB + ((__ffs(m) - 1) >> 1) * n;
+            if (tile_sees<C>(a, cur, p0, p0 + n, lane) && lane == 0) atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
           }
           const int64_t rec = want ? a.c.record(pid, cur.h) : 0;
           const int first = (kb * C::KB + off) & (a.c.page - 1);

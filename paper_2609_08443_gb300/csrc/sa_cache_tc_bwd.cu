@@ -222,7 +222,8 @@ __global__ void __launch_bounds__(640, 1) cache_tc_bwd_kernel(const __grid_const
           uint32_t sum = 0;
           for (int i = 0; i < pages; ++i) {
             const int id = page_of(p0 + i * n);
-            if (id != -2 && !usable(id) && e) atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
+            if (id != -2 && !usable(id) && tile_sees<C>(a, cur, p0 + i * n, p0 + (i + 1) * n, lane) && e)
+              atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
             if (usable(id)) sum += per_page;
             const int ahead = kb + 4 < cur.kb1 ? page_of(p0 + 4 * C::KB + i * n) : -2;
             if (usable(ahead)) {

@@ -120,6 +120,22 @@ __device__ __forceinline__ void set_piece(const AttnArgs& a, Walk& w, const Size
   if (w.vis0 >= w.vis1) w.kb1 = w.kb0;
 }
 
+// Whether some row of the walk's tile sees one of positions [p0, p1), p0 within the user's
+// length.  Asked only where a page is missing, by the whole warp: between the windows of a
+// tile's rows a page may be nobody's, and is then no error.
+template <class C>
+__device__ __forceinline__ bool tile_sees(const AttnArgs& a, const Walk& w, int p0, int p1, int lane) {
+  if (!a.begin && !a.end) return true;
+  bool any = false;
+#pragma unroll 1
+  for (int r = w.rt * C::ROWS + lane; r < min(w.s.rows, (w.rt + 1) * C::ROWS); r += 32) {
+    int l, e;
+    row_window(a, w.s.q0 + r / a.G, w.s.len, l, e);
+    any = any || max(l, p0) < min(e, p1);
+  }
+  return __any_sync(0xffffffffu, any);
+}
+
 // Move to the next piece of the share; false at its end.
 template <class C>
 __device__ __forceinline__ bool next_piece(const AttnArgs& a, Walk& w, int lane) {

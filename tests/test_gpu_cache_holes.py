@@ -1,5 +1,5 @@
-"""Positions between the windows of a user's queries that no query sees: never written, or holding
-bytes that no written row has."""
+"""Positions between the windows of a user's queries that no query sees: never written, without a page, or
+holding bytes that no written row has."""
 import numpy as np
 import pytest
 import torch
@@ -43,6 +43,44 @@ def test_bytes_between_the_windows_never_matter(cuda_lib, dt, d, page, R, L):
         got = run_both(cuda_lib, cache, [R], 1, dt, begin=begin, end=end)
         for a, b in zip(base, got):
             assert torch.equal(a, b), (code, scale)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 16), (128, 64), (128, 256), (96, 32)])
+@pytest.mark.parametrize("R,L", [(2, 700), (13, 700), (160, 700), (2, 6000), (160, 6000)])
+def test_pages_between_the_windows_may_be_missing(cuda_lib, dt, d, page, R, L):
+    """run_both asserts that the call reported nothing."""
+    cache = cc.Cache([L], 1, d, page, seed=22)
+    begin, end = windows(L, R)
+    base = run_both(cuda_lib, cache, [R], 1, dt, begin=begin, end=end)
+    first, last = -(-12 // page), (L - 50) // page  # whole pages that nobody sees
+    assert first < last
+    for gone in (-1, cache.n_pages):
+        cache.table[0, first:last] = gone
+        got = run_both(cuda_lib, cache, [R], 1, dt, begin=begin, end=end)
+        for a, b in zip(base, got):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("R", [3, 160])
+@pytest.mark.parametrize("page", [16, 64, 128])
+def test_a_missing_page_that_one_query_sees_is_reported(cuda_lib, dt, R, page):
+    cache = cc.Cache([700], 1, 128, page, seed=23)
+    begin, end = windows(700, R)
+    begin[R // 2], end[R // 2] = 300, 301
+    cache.table[0, 300 // page] = -1
+    pool, table, lens = cache.tensors()
+    cu = gpu(cc.offsets([R]))
+    q = cc.to_gpu(cc.queries(R, 1, 128, dt, 1), dt)
+    kw = {"kv_begin": gpu(begin.astype(np.int32)), "kv_end": gpu(end.astype(np.int32))}
+    size = [cuda_lib.sa_cache_attn_workspace_size(1, R, 1, 1, 128, cuda_lib.SA_BF16 if dt == "bf16" else cuda_lib.SA_F32,
+                                                  700, bwd) for bwd in (False, True)]
+    ws = torch.empty(max(size), dtype=torch.uint8, device="cuda")
+    out, lse = cuda_lib.sa_cache_attn_fwd(q, cu, pool, table, lens, want_lse=True, ws=ws, **kw)
+    assert cuda_lib.sa_get_device_error(ws) == 7
+    cuda_lib.sa_cache_attn_bwd(q, cu, pool, table, lens, out, lse, q, ws=ws, **kw)
+    assert cuda_lib.sa_get_device_error(ws) == 7
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
