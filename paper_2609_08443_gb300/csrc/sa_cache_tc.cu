@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
       auto page_of = [&](const Walk& w, int kb) {
         const int p0 = kb * C::KB + off;
         if (off >= C::KB || kb >= w.kb1 || p0 >= w.vis1 || p0 + n <= w.vis0) return -2;  // nothing to copy
-        return a.c.table[int64_t(w.b) * a.c.max_pages + (p0 >> a.c.log2page)];
+        return max(a.c.table[int64_t(w.b) * a.c.max_pages + (p0 >> a.c.log2page)], -1);
       };
       int parity = 0;
       auto publish = [&](bool end) {

@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_bwd_kernel(const __grid_const
       int base = 0, ids0 = 0, ids1 = 0;
       auto ids_from = [&](int first) {
         const int i = first + lane;
-        return i < a.c.max_pages && (int64_t(i) << a.c.log2page) < cur.vis1 ? a.c.table[int64_t(cur.b) * a.c.max_pages + i] : -1;
+        return i < a.c.max_pages && (int64_t(i) << a.c.log2page) < cur.vis1 ? max(a.c.table[int64_t(cur.b) * a.c.max_pages + i], -1) : -1;
       };
       auto page_of = [&](int p0) {  // of position p0; -2: nobody sees these positions
         const int i = (p0 >> a.c.log2page) - base;

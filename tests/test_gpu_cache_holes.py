@@ -83,6 +83,26 @@ def test_a_missing_page_that_one_query_sees_is_reported(cuda_lib, dt, R, page):
     assert cuda_lib.sa_get_device_error(ws) == 7
 
 
+@pytest.mark.parametrize("entry", [-1, -2, -3, -(1 << 31), 3, (1 << 31) - 1])
+@pytest.mark.parametrize("R", [3, 160])
+@pytest.mark.parametrize("bwd", [False, True])
+def test_every_entry_outside_the_pool_is_reported(cuda_lib, entry, R, bwd):
+    cache = cc.Cache([130], 1, 64, 64, seed=25, spare=0)
+    assert cache.n_pages == 3
+    cache.table[0, 1] = entry
+    pool, table, lens = cache.tensors()
+    cu = gpu(cc.offsets([R]))
+    q = cc.to_gpu(cc.queries(R, 1, 64, "bf16", 1), "bf16")
+    ws = torch.empty(cuda_lib.sa_cache_attn_workspace_size(1, R, 1, 1, 64, cuda_lib.SA_BF16, 130, bwd), dtype=torch.uint8,
+                     device="cuda")
+    if bwd:
+        lse = torch.zeros((R, 1), device="cuda")
+        cuda_lib.sa_cache_attn_bwd(q, cu, pool, table, lens, q, lse, q, ws=ws)
+    else:
+        cuda_lib.sa_cache_attn_fwd(q, cu, pool, table, lens, ws=ws)
+    assert cuda_lib.sa_get_device_error(ws) == 7
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("d,R", [(64, 3), (128, 3), (64, 160), (128, 160)])
 def test_values_near_the_largest_in_partly_hidden_blocks(cuda_lib, dt, d, R):
