@@ -30,7 +30,7 @@
  *     (SA_ERR_BAD_PAGE); the results of that call are then undefined.  Attention
  *     uses an entry where a query sees one of the page's positions.
  *   - `workspace` is 256-byte aligned and need not be cleared.  Its error word is
- *     read by sa_get_device_error(); bad offsets give SA_ERR_BAD_SEQLENS and the
+ *     read by sa_get_device_error(); bad offsets or starts give SA_ERR_BAD_SEQLENS and the
  *     call writes nothing.
  *   - The pool and every base pointer are 16-byte aligned; row and head strides
  *     are in elements and keep rows 16-byte aligned.

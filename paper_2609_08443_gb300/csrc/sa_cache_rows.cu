@@ -51,24 +51,30 @@ __device__ __forceinline__ RowRef find_row(const RowArgs& a, int64_t row) {
   return r;
 }
 
+// Whether this thread's part of the users' offsets and starts is out of order or leads past
+// the table: any such makes every block leave, and the whole call writes nothing.
+__device__ __forceinline__ int offsets_bad(const RowArgs& a) {
+  const int64_t most = int64_t(a.c.max_pages) << a.c.log2page;
+  int bad = 0;
+  if (a.cu || a.start) {
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+      const int64_t c0 = a.cu ? int64_t(a.cu[b]) : b * a.per_user;
+      const int64_t c1 = a.cu ? int64_t(a.cu[b + 1]) : c0 + a.per_user;
+      const int64_t s = a.start ? a.start[b] : 0;
+      bad |= (b == 0 && c0 != 0) || (b == a.B - 1 && c1 != a.N) || c0 > c1 || s < 0 || s + (c1 - c0) > most;
+    }
+  } else {
+    bad = a.per_user > most;
+  }
+  return bad;
+}
+
 // Checks of what the host cannot see, by one more block: writes the call's status.
 __device__ void check_rows(const RowArgs& a) {
-  __shared__ int bad;
-  if (threadIdx.x == 0) bad = 0;
-  __syncthreads();
-  int mine = 0;
-  for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
-    const int64_t c0 = a.cu ? int64_t(a.cu[b]) : b * a.per_user;
-    const int64_t c1 = a.cu ? int64_t(a.cu[b + 1]) : (b + 1) * a.per_user;
-    const int64_t s = a.start ? a.start[b] : 0;
-    if ((b == 0 && c0 != 0) || (b == a.B - 1 && c1 != a.N) || c0 > c1 || s < 0 ||
-        s + (c1 - c0) > (int64_t(a.c.max_pages) << a.c.log2page))
-      mine = max(mine, int(SA_ERR_BAD_SEQLENS));
-  }
-  if (mine) atomicMax(&bad, mine);
-  __syncthreads();
-  if (bad == 0) {
+  int status = __syncthreads_or(offsets_bad(a)) ? int(SA_ERR_BAD_SEQLENS) : 0;
+  if (!status) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int bad = 0;
     for (int b = warp; b < a.B; b += blockDim.x >> 5) {
       const int64_t n = a.cu ? a.cu[b + 1] - a.cu[b] : a.per_user;
       if (n == 0) continue;
@@ -76,23 +82,12 @@ __device__ void check_rows(const RowArgs& a) {
       const int p0 = int(s >> a.c.log2page), p1 = int((s + n - 1) >> a.c.log2page);
       for (int p = p0 + lane; p <= p1; p += 32) {
         const int e = a.c.table[int64_t(b) * a.c.max_pages + p];
-        if (e < 0 || e >= a.c.n_pages) mine = int(SA_ERR_BAD_PAGE);
+        bad |= e < 0 || e >= a.c.n_pages;
       }
     }
-    if (mine) atomicMax(&bad, mine);
-    __syncthreads();
+    if (__syncthreads_or(bad)) status = int(SA_ERR_BAD_PAGE);
   }
-  if (threadIdx.x == 0) ws_header(a.ws)->err = uint32_t(bad);
-}
-
-// Whether this thread's part of the offsets is out of order: any such makes every block
-// leave, and the whole call writes nothing.
-__device__ __forceinline__ int offsets_bad(const RowArgs& a) {
-  int bad = 0;
-  if (a.cu)
-    for (int b = threadIdx.x; b < a.B; b += blockDim.x)
-      bad |= (b == 0 && a.cu[0] != 0) || (b == a.B - 1 && int64_t(a.cu[a.B]) != a.N) || a.cu[b] > a.cu[b + 1];
-  return bad;
+  if (threadIdx.x == 0) ws_header(a.ws)->err = uint32_t(status);
 }
 
 // ------------------------------------------------------------------ a block's rows
