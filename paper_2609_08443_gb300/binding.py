@@ -12,6 +12,7 @@ import ctypes
 import functools
 import math
 import os
+import threading
 from typing import Optional, Tuple
 
 import torch
@@ -557,7 +558,12 @@ def sa_sketch(K, V, cu_seqlens, Q, scale: Optional[float] = None):
 # `block_table` int32 [B, max_pages]; the page size follows from the pool's shape
 # and the width d of the rows.
 
+# A thread's workspaces, one for each of the streams that it used last, and, for their status,
+# the workspaces of each stream's latest call from any thread.
+_own_ws = threading.local()
 _stream_ws_cache = {}
+_STREAMS_KEPT = 8
+_ws_lock = threading.Lock()
 
 
 # These calls answer single tokens, so their checks avoid what costs a microsecond in
@@ -581,13 +587,29 @@ def _stream_handle(index: int) -> int:
     return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
+def _keep(kept: dict, key, buf: torch.Tensor) -> None:
+    with _ws_lock:
+        kept.pop(key, None)
+        while len(kept) >= _STREAMS_KEPT:
+            del kept[next(iter(kept))]
+        kept[key] = buf
+
+
 def _stream_workspace(nbytes: int, index: int, stream: int) -> torch.Tensor:
-    """A cached workspace of this stream (calls on other streams may run at the same time)."""
+    """Memory for one call on the current stream.  A thread's calls on a stream come one after the other and
+    share one buffer.  Two threads' calls may interleave, a call being two launches, and have their own; so has
+    a captured call, whose graph may run at any time and on any stream (its pool keeps what the call took)."""
     key = (index, stream)
-    buf = _stream_ws_cache.get(key)
-    if buf is None or buf.numel() < nbytes:
+    if torch.cuda.is_current_stream_capturing():
         buf = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
-        _stream_ws_cache[key] = buf
+    else:
+        own = _own_ws.__dict__
+        buf = own.get(key)
+        if buf is None or buf.numel() < nbytes:
+            buf = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
+            _keep(own, key, buf)
+    if _stream_ws_cache.get(key) is not buf:
+        _keep(_stream_ws_cache, key, buf)
     return buf
 
 
