@@ -608,9 +608,24 @@ def _stream_workspace(nbytes: int, index: int, stream: int) -> torch.Tensor:
         if buf is None or buf.numel() < nbytes:
             buf = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
             _keep(own, key, buf)
-    if _stream_ws_cache.get(key) is not buf:
-        _keep(_stream_ws_cache, key, buf)
     return buf
+
+
+def _note_call(buf: torch.Tensor, index: int, stream: int) -> None:
+    """``buf`` holds the status of the stream's latest call."""
+    if _stream_ws_cache.get((index, stream)) is not buf:
+        _keep(_stream_ws_cache, (index, stream), buf)
+
+
+def sa_cache_get_device_error(device=None) -> int:
+    """Status of the latest sa_cache_* call on the current stream (from any thread) that was given no ``ws``:
+    0, or what the device found (SA_ERR_TIMEOUT, SA_ERR_BAD_SEQLENS, SA_ERR_BAD_PAGE).  Waits for the stream.
+    A captured call's status is that of its graph's last replay: wait for the stream that ran it first."""
+    index = torch.device("cuda" if device is None else device).index
+    index = torch.cuda.current_device() if index is None else index
+    with _on(index):
+        buf = _stream_ws_cache.get((index, _stream_handle(index)))
+        return 0 if buf is None else sa_get_device_error(buf)
 
 
 def sa_cache_page_bytes(H: int, d: int, page: int) -> int:
@@ -679,6 +694,8 @@ def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tenso
                                 _dt(K), pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
                                 w.data_ptr(), w.numel(), stream)
     _check(st, "sa_cache_write")
+    if ws is None:
+        _note_call(w, index, stream)
 
 
 def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: torch.Tensor, n_rows: int, d: int,
@@ -699,6 +716,8 @@ def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: tor
                                cu_seqlens.data_ptr(), B, n_rows, _addr(start), H, d, _dt(K), K.data_ptr(),
                                V.data_ptr(), w.data_ptr(), w.numel(), stream)
     _check(st, "sa_cache_read")
+    if ws is None:
+        _note_call(w, index, stream)
     return K, V
 
 
@@ -731,16 +750,19 @@ def _cache_attn(entry, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end,
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     with _on(index):
         stream = _stream_handle(index)
-        if ws is None:
+        w = ws
+        if w is None:
             need = sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_pages * page, bwd)
             if need == 0:
                 raise SketchError(2, "sa_cache_attn_workspace_size")
-            ws = _stream_workspace(need, index, stream)
+            w = _stream_workspace(need, index, stream)
         row, head, _ = q.stride()
         st = entry(q.data_ptr(), row, head, cu_q.data_ptr(), B, T, Hq, pool.data_ptr(), n_pages, page,
                    block_table.data_ptr(), max_pages, cache_lens.data_ptr(), H, d, _addr(kv_begin), _addr(kv_end),
-                   scale, dt, *[_addr(t) for t in tensors], ws.data_ptr(), ws.numel(), stream)
+                   scale, dt, *[_addr(t) for t in tensors], w.data_ptr(), w.numel(), stream)
     _check(st, "sa_cache_attn_bwd" if bwd else "sa_cache_attn_fwd")
+    if ws is None:
+        _note_call(w, index, stream)
 
 
 def sa_cache_attn_fwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, block_table: torch.Tensor,
