@@ -664,11 +664,15 @@ def _offsets_arg(name, t, n, index):
 
 def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
                    cu_seqlens: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
-                   ws: Optional[torch.Tensor] = None) -> None:
+                   ws: Optional[torch.Tensor] = None, appends: bool = False) -> None:
     """Write rows into the cache in 4 bits: user b's row i to position start[b] + i.
 
     K, V are packed rows [N, H, d] with ``cu_seqlens`` [B+1], or [B, H, n, d] (a
-    batch of sketches) without; fp32 or bf16, any strides with contiguous rows."""
+    batch of sketches) without; fp32 or bf16, any strides with contiguous rows.
+
+    To autograd this is an in-place change of the pool: the backward of an earlier
+    ``sa_cache_attention`` over it is refused from then on.  ``appends`` is the caller's
+    word that no such forward has seen the positions written, and leaves it allowed."""
     lib = load()
     packed = cu_seqlens is not None
     if K.dim() != (3 if packed else 4) or K.shape != V.shape or K.dtype != V.dtype:
@@ -694,6 +698,8 @@ def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tenso
                                 _dt(K), pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
                                 w.data_ptr(), w.numel(), stream)
     _check(st, "sa_cache_write")
+    if not appends:
+        torch.autograd.graph.increment_version(pool)
     if ws is None:
         _note_call(w, index, stream)
 
