@@ -802,7 +802,7 @@ def sa_cache_attn_bwd(q: torch.Tensor, cu_q: torch.Tensor, pool: torch.Tensor, b
 
 
 class CacheAttention(torch.autograd.Function):
-    """out = softmax(scale q K^T) V over each user's cached rows; gradient for q only."""
+    """out = softmax(scale q K^T) V over each user's cached rows; gradient for q only, and once."""
 
     @staticmethod
     def forward(ctx, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale):
@@ -812,6 +812,7 @@ class CacheAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
         q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, out, lse = ctx.saved_tensors
         dq = sa_cache_attn_bwd(q, cu_q, pool, block_table, cache_lens, out, lse, dout.contiguous(), kv_begin, kv_end,

@@ -1,4 +1,4 @@
-"""What autograd has to refuse: a gradient over pages that were rewritten."""
+"""What autograd has to refuse: a gradient over pages that were rewritten, and a second derivative."""
 import numpy as np
 import pytest
 import torch
@@ -59,3 +59,10 @@ def test_a_write_before_the_forward_changes_nothing(cuda_lib):
     assert torch.isfinite(q.grad).all()
     with torch.inference_mode():
         cuda_lib.sa_cache_write(pool, table, K, K, n)
+
+def test_a_second_derivative_is_refused(cuda_lib):
+    pool, table, lens, cu, q = setup()
+    out = cuda_lib.sa_cache_attention(q, cu, pool, table, lens)
+    dq, = torch.autograd.grad(out.square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dq.sum().backward()
