@@ -108,7 +108,9 @@ sa_status sa_cache_attn_bwd(const void* q, int64_t q_row_stride, int64_t q_head_
                             size_t ws_bytes, void* stream);
 
 /* Name of the kernel a call with these sizes runs on ("tc5..." = tcgen05, "mma..."
- * = warp-level tensor-core products, the cached rows dequantised in registers). */
+ * = warp-level tensor-core products, the cached rows dequantised in registers).
+ * sa_select_path(1) takes the warp-level kernels for every call (a cross-check: there
+ * are no CUDA-core ones); workspaces do not depend on it. */
 const char* sa_cache_attn_kernel_name(int B, int64_t T, int Hq, int H, int d, float scale, sa_dtype dt, int bwd);
 
 #ifdef __cplusplus

@@ -82,6 +82,12 @@ Layout attn_layout(int B, int64_t T, int G, int d, sa_dtype dt, bool bwd, bool t
   return l;
 }
 
+// The kernel of a call: tcgen05 where its sizes are worth it (tc_supported) and sa_select_path
+// leaves it.  A workspace's size asks for the sizes alone: it serves either kernel.
+bool takes_tc(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd) {
+  return sa::tc_path_enabled() && sa::cache::tc_supported(B, T, G, d, dt, scale, bwd);
+}
+
 bool attn_sizes_ok(int B, int64_t T, int Hq, int H, int d, sa_dtype dt) {
   return B >= 1 && T >= 0 && H >= 1 && H <= sa::kMaxH && Hq >= H && Hq % H == 0 && width_ok(d) &&
          (dt == SA_F32 || dt == SA_BF16) && T * (Hq / H) < kMost && Hq < 65536;
@@ -96,7 +102,7 @@ sa_status attn(AttnArgs& a, const void* q, int64_t q_row, int64_t q_head, const 
   if (!attn_sizes_ok(B, T, Hq, H, d, dt)) return SA_ERR_UNSUPPORTED;
   if (T > 0 && (!q || !aligned(q, 16))) return SA_ERR_INVALID_ARG;
   if (!stride_ok(q_row, dt) || !stride_ok(q_head, dt)) return SA_ERR_INVALID_ARG;
-  const bool tc = sa::cache::tc_supported(B, T, Hq / H, d, dt, scale, bwd);
+  const bool tc = takes_tc(B, T, Hq / H, d, dt, scale, bwd);
   const Layout l = attn_layout(B, T, Hq / H, d, dt, bwd, tc);
   SA_TRY(check_workspace(ws, ws_bytes, l.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -189,7 +195,7 @@ sa_status sa_cache_read(const void* pool, int64_t n_pages, int page, const int32
 
 size_t sa_cache_attn_workspace_size(int B, int64_t T, int Hq, int H, int d, sa_dtype dt, int64_t max_tokens, int bwd) {
   if (!attn_sizes_ok(B, T, Hq, H, d, dt) || max_tokens < 0) return 0;
-  // enough for either kernel: the scale, not known here, has a say
+  // enough for either kernel: the scale and the path, which may change, have a say
   const size_t x = attn_layout(B, T, Hq / H, d, dt, bwd != 0, false).total;
   if (!sa::cache::tc_supported(B, T, Hq / H, d, dt, 1.f, bwd != 0)) return x;
   const size_t y = attn_layout(B, T, Hq / H, d, dt, bwd != 0, true).total;
@@ -227,7 +233,7 @@ sa_status sa_cache_attn_bwd(const void* q, int64_t q_row_stride, int64_t q_head_
 
 const char* sa_cache_attn_kernel_name(int B, int64_t T, int Hq, int H, int d, float scale, sa_dtype dt, int bwd) {
   if (!attn_sizes_ok(B, T, Hq, H, d, dt) || !std::isfinite(scale)) return "unsupported";
-  if (sa::cache::tc_supported(B, T, Hq / H, d, dt, scale, bwd != 0)) return bwd ? "tc5_cache_attn_bwd" : "tc5_cache_attn_fwd";
+  if (takes_tc(B, T, Hq / H, d, dt, scale, bwd != 0)) return bwd ? "tc5_cache_attn_bwd" : "tc5_cache_attn_fwd";
   return bwd ? "mma_cache_attn_bwd" : "mma_cache_attn_fwd";
 }
 
