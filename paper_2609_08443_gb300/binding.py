@@ -728,7 +728,13 @@ def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: tor
 
 
 @functools.lru_cache(maxsize=1024)
+def _attn_workspace_size(index: int, *sizes) -> int:
+    """The size on device ``index``, which is current."""
+    return int(load().sa_cache_attn_workspace_size(*sizes))
+
+
 def sa_cache_attn_workspace_size(B: int, T: int, Hq: int, H: int, d: int, dt: int, max_tokens: int, bwd: bool) -> int:
+    """Bytes of workspace that an attention call (``bwd``: its gradient) of these sizes needs on the current device."""
     return int(load().sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_tokens, int(bool(bwd))))
 
 
@@ -758,7 +764,7 @@ def _cache_attn(entry, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end,
         stream = _stream_handle(index)
         w = ws
         if w is None:
-            need = sa_cache_attn_workspace_size(B, T, Hq, H, d, dt, max_pages * page, bwd)
+            need = _attn_workspace_size(index, B, T, Hq, H, d, dt, max_pages * page, int(bwd))
             if need == 0:
                 raise SketchError(2, "sa_cache_attn_workspace_size")
             w = _stream_workspace(need, index, stream)

@@ -60,3 +60,23 @@ def test_few_streams_keep_a_buffer(capturing):
         return len(binding._own_ws.__dict__)
 
     assert in_a_thread(after_many) <= 16
+
+
+def test_a_size_is_remembered_for_the_device_it_holds_on(monkeypatch):
+    """It follows the current device's SM count."""
+    class Library:
+        def sa_cache_attn_workspace_size(self, *sizes):
+            return 1000 + device
+
+    monkeypatch.setattr(binding, "load", Library)
+    sizes = []
+    for device in (0, 1, 0):
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: device)
+        sizes.append(binding.sa_cache_attn_workspace_size(7001, 3, 2, 1, 64, 1, 128, False))
+    assert sizes == [1000, 1001, 1000]
+    binding._attn_workspace_size.cache_clear()
+    device = 0
+    assert binding._attn_workspace_size(0, 7001, 3, 2, 1, 64, 1, 128, 0) == 1000
+    device = 1
+    assert binding._attn_workspace_size(1, 7001, 3, 2, 1, 64, 1, 128, 0) == 1001
+    binding._attn_workspace_size.cache_clear()
