@@ -662,6 +662,12 @@ def _offsets_arg(name, t, n, index):
         raise ValueError(f"{name} must be contiguous int32 [{n}] on the pool's device")
 
 
+def _ws_arg(ws, index):
+    if not isinstance(ws, torch.Tensor) or not ws.is_cuda or ws.get_device() != index or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor (uint8) on the pool's device")
+    return ws
+
+
 def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
                    cu_seqlens: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
                    ws: Optional[torch.Tensor] = None, appends: bool = False) -> None:
@@ -693,7 +699,7 @@ def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tenso
         N, strides = B * K.shape[2], (K.stride(0), K.stride(2), K.stride(1))
     with _on(index):
         stream = _stream_handle(index)
-        w = ws if ws is not None else _stream_workspace(256, index, stream)
+        w = _ws_arg(ws, index) if ws is not None else _stream_workspace(256, index, stream)
         st = lib.sa_cache_write(K.data_ptr(), V.data_ptr(), *strides, _addr(cu_seqlens), B, N, _addr(start), H, d,
                                 _dt(K), pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
                                 w.data_ptr(), w.numel(), stream)
@@ -717,7 +723,7 @@ def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: tor
     V = torch.empty_like(K)
     with _on(index):
         stream = _stream_handle(index)
-        w = ws if ws is not None else _stream_workspace(256, index, stream)
+        w = _ws_arg(ws, index) if ws is not None else _stream_workspace(256, index, stream)
         st = lib.sa_cache_read(pool.data_ptr(), n_pages, page, block_table.data_ptr(), max_pages,
                                cu_seqlens.data_ptr(), B, n_rows, _addr(start), H, d, _dt(K), K.data_ptr(),
                                V.data_ptr(), w.data_ptr(), w.numel(), stream)
@@ -762,8 +768,9 @@ def _cache_attn(entry, q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end,
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     with _on(index):
         stream = _stream_handle(index)
-        w = ws
-        if w is None:
+        if ws is not None:
+            w = _ws_arg(ws, index)
+        else:
             need = _attn_workspace_size(index, B, T, Hq, H, d, dt, max_pages * page, int(bwd))
             if need == 0:
                 raise SketchError(2, "sa_cache_attn_workspace_size")
