@@ -657,8 +657,8 @@ def _cache_args(pool, block_table, d: int):
 
 
 def _offsets_arg(name, t, n, index):
-    if t is not None and (not t.is_cuda or t.get_device() != index or t.dtype is not torch.int32 or t.dim() != 1
-                          or t.numel() != n or not t.is_contiguous()):
+    if t is None or not t.is_cuda or t.get_device() != index or t.dtype is not torch.int32 or t.dim() != 1 \
+            or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous int32 [{n}] on the pool's device")
 
 
@@ -691,8 +691,10 @@ def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tenso
         raise ValueError("K and V must have contiguous rows and equal strides")
     if K.shape[1] != H or (not packed and K.shape[0] != B):
         raise ValueError(f"K{tuple(K.shape)} does not fit a cache of {H} heads and {B} users")
-    _offsets_arg("cu_seqlens", cu_seqlens, B + 1, index)
-    _offsets_arg("start", start, B, index)
+    if packed:
+        _offsets_arg("cu_seqlens", cu_seqlens, B + 1, index)
+    if start is not None:
+        _offsets_arg("start", start, B, index)
     if packed:
         N, strides = K.shape[0], (0, K.stride(0), K.stride(1))
     else:
@@ -716,7 +718,8 @@ def sa_cache_read(pool: torch.Tensor, block_table: torch.Tensor, cu_seqlens: tor
     lib = load()
     index, n_pages, H, page, B, max_pages = _cache_args(pool, block_table, d)
     _offsets_arg("cu_seqlens", cu_seqlens, B + 1, index)
-    _offsets_arg("start", start, B, index)
+    if start is not None:
+        _offsets_arg("start", start, B, index)
     if n_rows < 0:
         raise ValueError("n_rows must not be negative")
     K = torch.empty((n_rows, H, d), dtype=dtype, device=pool.device)

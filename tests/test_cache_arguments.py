@@ -90,3 +90,11 @@ def test_a_workspace_that_is_no_device_memory_is_refused(lib, name, ws):
     with pytest.raises(ValueError, match="ws"):
         calls(ws=ws)[name]()
     assert lib.calls == 0
+
+
+@pytest.mark.parametrize("name,arg", [("read", "cu_seqlens"), ("fwd", "cu_q"), ("fwd", "cache_lens"), ("bwd", "cu_q"),
+                                      ("bwd", "cache_lens")])
+def test_offsets_and_lengths_are_required(lib, name, arg):
+    with pytest.raises(ValueError, match=arg):
+        calls(**{arg: None})[name]()
+    assert lib.calls == 0
