@@ -24,7 +24,8 @@
  *
  * Conventions (otherwise those of sa_sketch.h: device pointers, the caller's
  * stream and memory, no synchronisation, bitwise reproducible results)
- *   - d is a multiple of 16, 16..128; 1 <= H <= 64 cached heads.
+ *   - d is a multiple of 16, 16..128; 1 <= H <= 64 cached heads.  max_pages * page and
+ *     T * Hq / H are at most 2^31 - 256.
  *   - block_table : int32 [B, max_pages].  Entries outside a user's positions are
  *     not looked at.  A used entry outside [0, n_pages) is skipped and reported
  *     (SA_ERR_BAD_PAGE); the results of that call are then undefined.  Attention

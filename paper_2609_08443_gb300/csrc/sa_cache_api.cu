@@ -20,6 +20,9 @@ using sa::cache::RowArgs;
   } while (0)
 
 constexpr int64_t kMost = int64_t(1) << 31;
+// A user's positions, and its rows for a cached head, are counted in int32 and rounded up to
+// tiles of at most 256.
+constexpr int64_t kMostTiled = kMost - 256;
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -30,7 +33,7 @@ sa_status set_pages(Pages* c, const void* pool, int64_t n_pages, int page, const
                     int d) {
   if (!pool || !table || !aligned(pool, 16)) return SA_ERR_INVALID_ARG;
   if (n_pages < 1 || max_pages < 1 || H < 1 || d < 1 || page < 1) return SA_ERR_INVALID_ARG;
-  if (!page_ok(page) || !width_ok(d) || H > sa::kMaxH || n_pages >= kMost || int64_t(max_pages) * page >= kMost)
+  if (!page_ok(page) || !width_ok(d) || H > sa::kMaxH || n_pages >= kMost || int64_t(max_pages) * page > kMostTiled)
     return SA_ERR_UNSUPPORTED;
   c->pool = static_cast<const uint8_t*>(pool);
   c->n_pages = n_pages;
@@ -90,7 +93,7 @@ bool takes_tc(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd
 
 bool attn_sizes_ok(int B, int64_t T, int Hq, int H, int d, sa_dtype dt) {
   return B >= 1 && T >= 0 && H >= 1 && H <= sa::kMaxH && Hq >= H && Hq % H == 0 && width_ok(d) &&
-         (dt == SA_F32 || dt == SA_BF16) && T * (Hq / H) < kMost && Hq < 65536;
+         (dt == SA_F32 || dt == SA_BF16) && T <= kMostTiled / (Hq / H) && Hq < 65536;
 }
 
 sa_status attn(AttnArgs& a, const void* q, int64_t q_row, int64_t q_head, const int32_t* cu_q, int B, int64_t T, int Hq,
