@@ -76,9 +76,10 @@ __device__ __forceinline__ Sizes user_sizes(const AttnArgs& a, int b) {
   return s;
 }
 
+// Query t's positions; neither end is negative, so that differences with positions stay in range.
 __device__ __forceinline__ void row_window(const AttnArgs& a, int64_t t, int len, int& lo, int& hi) {
   lo = a.begin ? max(a.begin[t], 0) : 0;
-  hi = a.end ? min(a.end[t], len) : len;
+  hi = a.end ? max(min(a.end[t], len), 0) : len;
 }
 
 // The piece that starts at unit w.t of user w.b (sizes in s).
