@@ -140,10 +140,11 @@ struct Warp {
     const uint32_t s = issued & 1u;
     const uint32_t b = bar + 8u * s;
     const uint32_t dst = smem_u32(ring) + s * C::STAGE;
-    const bool there = pid >= 0 && pid < a.c.n_pages, want = wanted(w, kb) && there;
-    for (uint32_t m = __ballot_sync(0xffffffffu, wanted(w, kb) && !there && (lane & 3) == 0); m; m &= m - 1) {
-      const int n = min(a.c.page, KB), p0 = kb * KB + ((__ffs(m) - 1) >> 2) * n;
-      if (tile_sees<C>(a, w, p0, p0 + n, lane) && lane == 0) atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
+    bool want = wanted(w, kb);
+    if (want && (pid < 0 || pid >= a.c.n_pages)) {
+      const int n = min(a.c.page, KB), p0 = kb * KB + (lane >> 2) * n;
+      if (tile_sees<C>(a, w, p0, p0 + n, 0, 1)) atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
+      want = false;
     }
     if (a.c.page == KB) {  // a block is a page, and a page's records lie as the stage does
       if (lane == 0) {
@@ -234,12 +235,33 @@ struct Warp {
       }
     }
   }
+  // A block that some row does not see whole may hold bytes that nobody wrote (see
+  // level_min7): seen to in the stage, before its values are read as float16.
+  __device__ __forceinline__ void make_finite(uint8_t* st) const {
+    uint8_t* codes = st + KB * (width() / 2 + width() / 16);
+    uint8_t* sc = codes + KB * (width() / 2);
+    uint32_t high = 0;
+    for (int i = lane; i < width(); i += 32) {  // four scales a word
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(sc + 4 * i);
+      high |= v & v << 1 & v << 2;  // bit 7 of a byte: its upper three bits are set
+    }
+    static_assert(kCodeSafe == 0xDF, "the codes above it are those with three upper bits");
+    if (!__any_sync(0xffffffffu, high & 0x80808080u)) return;
+#pragma unroll 1
+    for (int i = lane; i < 4 * width(); i += 32) {  // groups, 8 bytes of codes each
+      if (sc[i] <= kCodeSafe) continue;
+      uint2* w = reinterpret_cast<uint2*>(codes + 8 * i);
+      *w = make_uint2(level_min7(w->x), level_min7(w->y));
+      if (sc[i] > kCodeMax) sc[i] = 0;
+    }
+    fence_proxy_async_smem();  // before the next copy into the stage
+    __syncwarp();
+  }
   // acc += (rows of 16 keys from 16 jj, transposed) x weights B, WT terms each; F16 or bf16
-  // values.  `inside`: every row sees the whole block.  Where one does not, the hidden keys'
-  // bytes may be nobody's, which float16 may read as infinities (bf16 never does).
+  // values.
   template <bool F16, int WT>
   __device__ __forceinline__ void combine(const uint8_t* st, int jj, int kv, const uint32_t (*B)[WT][2],
-                                          float (*acc)[C::NR][4], bool inside) const {
+                                          float (*acc)[C::NR][4]) const {
     int k[4];
     k[0] = 16 * jj + key_of(2 * t4);
     k[1] = 16 * jj + key_of(2 * t4 + 1);
@@ -257,11 +279,6 @@ struct Warp {
       } else {
         w[i][0] = *reinterpret_cast<const uint32_t*>(p);
         code[i] = scales(st, k[i], kv)[g >> 1];
-      }
-      if (F16 && !inside && code[i] > kCodeSafe) {
-        if (code[i] > kCodeMax) code[i] = 0;
-#pragma unroll
-        for (int j = 0; j < NW; ++j) w[i][j] = level_min7(w[i][j]);
       }
     }
     const uint32_t c01 = code[0] | code[1] << 16, c23 = code[2] | code[3] << 16;
@@ -478,12 +495,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
       const uint32_t s = x.used & 1u;
       x.ok = __all_sync(0xffffffffu, mbar_wait(bar + 8 * s, (x.used >> 1) & 1u, ctl, slot, 0xC01u));
       if (!x.ok) break;
-      const uint8_t* st = x.ring + s * C::STAGE;
+      uint8_t* st = x.ring + s * C::STAGE;
       const int k0 = kb * KB;
       const bool inside = k0 >= lo_most && k0 + KB <= hi_least;
       // accumulator element e of key tile i: key 16 i + 8 (e / 2) + key_of(g), row 2t + e % 2
       auto key = [&](int i, int e) { return k0 + 16 * i + 8 * (e >> 1) + key_of(g); };
       if constexpr (!C::BWD) {
+        if (!inside) x.make_finite(st);
         float S[KB / 16][NR][4];
         x.template contract<KB / 16>(st, 0, 0, x.frag, S);
         bool moved = false;
@@ -547,7 +565,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
               }
             }
           }
-          x.template combine<true, C::NP>(st, i, 1, B, acc, inside);
+          x.template combine<true, C::NP>(st, i, 1, B, acc);
         }
       } else {
         constexpr int HM = KB / 32;  // half a block at a time: two products' scores are live
@@ -578,7 +596,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
                   p[2 * u] -= f.x, p[2 * u + 1] -= f.y;
                 }
             }
-            x.template combine<false, C::NS>(st, HM * half + i, 0, B, acc, true);
+            x.template combine<false, C::NS>(st, HM * half + i, 0, B, acc);
           }
         }
       }

@@ -191,10 +191,12 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
       uint32_t c = 0;  // keys and values of block after block
       const int n = min(a.c.page, C::KB), part = lane & 1, off = (lane >> 1) * n;
       const int rb = part ? D / 16 : D / 2;
-      auto page_of = [&](const Walk& w, int kb) {
+      auto holds = [&](const Walk& w, int kb) {  // whether the lane's page of the block has positions that may be seen
         const int p0 = kb * C::KB + off;
-        if (off >= C::KB || kb >= w.kb1 || p0 >= w.vis1 || p0 + n <= w.vis0) return -2;  // nothing to copy
-        return max(a.c.table[int64_t(w.b) * a.c.max_pages + (p0 >> a.c.log2page)], -1);
+        return off < C::KB && kb < w.kb1 && p0 < w.vis1 && p0 + n > w.vis0;
+      };
+      auto page_of = [&](const Walk& w, int kb) {
+        return holds(w, kb) ? a.c.table[int64_t(w.b) * a.c.max_pages + ((kb * C::KB + off) >> a.c.log2page)] : -1;
       };
       int parity = 0;
       auto publish = [&](bool end) {
@@ -226,14 +228,20 @@ __global__ void __launch_bounds__(640, 1) cache_tc_fwd_kernel(const __grid_const
         int pid = page_of(cur, cur.kb0), pid1 = page_of(cur, cur.kb0 + 1), pid2 = page_of(cur, cur.kb0 + 2);
         for (int kb = cur.kb0; kb < cur.kb1 && ok; ++kb) {
           const bool want = pid >= 0 && pid < a.c.n_pages;
-          for (uint32_t m = __ballot_sync(0xffffffffu, pid != -2 && !want && !part); m; m &= m - 1) {
-            const int p0 = kb * C::KB + ((__ffs(m) - 1) >> 1) * n;
-            if (tile_sees<C>(a, cur, p0, p0 + n, lane) && lane == 0) atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
-          }
           const int64_t rec = want ? a.c.record(pid, cur.h) : 0;
           const int first = (kb * C::KB + off) & (a.c.page - 1);
           const uint32_t bytes = want ? uint32_t(n * rb) : 0u;
-          const uint32_t sum = __reduce_add_sync(0xffffffffu, bytes);
+          // the block's bytes, and above them how many of its pages are missing
+          const bool missing = !want && !part && holds(cur, kb);
+          uint32_t sum = __reduce_add_sync(0xffffffffu, bytes | uint32_t(missing) << 24);
+          if (sum >> 24) {
+            for (uint32_t m = __ballot_sync(0xffffffffu, missing); m; m &= m - 1) {
+              const int p0 = kb * C::KB + ((__ffs(m) - 1) >> 1) * n;
+              if (__any_sync(0xffffffffu, tile_sees<C>(a, cur, p0, p0 + n, lane, 32)) && lane == 0)
+                atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
+            }
+            sum &= 0xFFFFFFu;
+          }
           if (pid2 >= 0 && pid2 < a.c.n_pages) {
             const uint8_t* p = a.c.pool + a.c.record(pid2, cur.h) + (part ? a.c.page * (D / 2) : 0) +
                                (((kb + 2) * C::KB + off) & (a.c.page - 1)) * rb;

@@ -177,12 +177,12 @@ __global__ void __launch_bounds__(640, 1) cache_tc_bwd_kernel(const __grid_const
       int base = 0, ids0 = 0, ids1 = 0;
       auto ids_from = [&](int first) {
         const int i = first + lane;
-        return i < a.c.max_pages && (int64_t(i) << a.c.log2page) < cur.vis1 ? max(a.c.table[int64_t(cur.b) * a.c.max_pages + i], -1) : -1;
+        return i < a.c.max_pages && (int64_t(i) << a.c.log2page) < cur.vis1 ? a.c.table[int64_t(cur.b) * a.c.max_pages + i] : -1;
       };
       auto page_of = [&](int p0) {  // of position p0; -2: nobody sees these positions
         const int i = (p0 >> a.c.log2page) - base;
         const int x = __shfl_sync(0xffffffffu, ids0, i & 31), y = __shfl_sync(0xffffffffu, ids1, i & 31);
-        return p0 >= cur.vis1 || p0 + n <= cur.vis0 ? -2 : i < 32 ? x : y;
+        return p0 >= cur.vis1 || p0 + n <= cur.vis0 ? -2 : max(i < 32 ? x : y, -1);
       };
       auto usable = [&](int id) { return id >= 0 && id < a.c.n_pages; };
       auto publish = [&](bool end) {
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(640, 1) cache_tc_bwd_kernel(const __grid_const
           uint32_t sum = 0;
           for (int i = 0; i < pages; ++i) {
             const int id = page_of(p0 + i * n);
-            if (id != -2 && !usable(id) && tile_sees<C>(a, cur, p0 + i * n, p0 + (i + 1) * n, lane) && e)
+            if (id != -2 && !usable(id) && __any_sync(0xffffffffu, tile_sees<C>(a, cur, p0 + i * n, p0 + (i + 1) * n, lane, 32)) && e)
               atomicCAS(&slot->err, 0u, uint32_t(SA_ERR_BAD_PAGE));
             if (usable(id)) sum += per_page;
             const int ahead = kb + 4 < cur.kb1 ? page_of(p0 + 4 * C::KB + i * n) : -2;

@@ -121,20 +121,25 @@ __device__ __forceinline__ void set_piece(const AttnArgs& a, Walk& w, const Size
   if (w.vis0 >= w.vis1) w.kb1 = w.kb0;
 }
 
-// Whether some row of the walk's tile sees one of positions [p0, p1), p0 within the user's
-// length.  Asked only where a page is missing, by the whole warp: between the windows of a
-// tile's rows a page may be nobody's, and is then no error.
-template <class C>
-__device__ __forceinline__ bool tile_sees(const AttnArgs& a, const Walk& w, int p0, int p1, int lane) {
+// Whether one of rows r, r + step, ... below `end` of a user sees one of positions [p0, p1), p0
+// within the user's length.  Asked only where a page is missing: between the windows of a
+// tile's rows a page may be nobody's, and is then no error.  Out of line, for the loops that
+// ask are bound by the code they run through (inlined, 300 queries over 10,000 positions
+// take 276 us instead of 273).
+static __device__ __noinline__ bool rows_see(const AttnArgs& a, int64_t q0, int len, int r, int end, int step, int p0,
+                                             int p1) {
   if (!a.begin && !a.end) return true;
-  bool any = false;
-#pragma unroll 1
-  for (int r = w.rt * C::ROWS + lane; r < min(w.s.rows, (w.rt + 1) * C::ROWS); r += 32) {
+  for (; r < end; r += step) {
     int l, e;
-    row_window(a, w.s.q0 + r / a.G, w.s.len, l, e);
-    any = any || max(l, p0) < min(e, p1);
+    row_window(a, q0 + r / a.G, len, l, e);
+    if (max(l, p0) < min(e, p1)) return true;
   }
-  return __any_sync(0xffffffffu, any);
+  return false;
+}
+// The same of rows first, first + step, ... of the walk's tile.
+template <class C>
+__device__ __forceinline__ bool tile_sees(const AttnArgs& a, const Walk& w, int p0, int p1, int first, int step) {
+  return rows_see(a, w.s.q0, w.s.len, w.rt * C::ROWS + first, min(w.s.rows, (w.rt + 1) * C::ROWS), step, p0, p1);
 }
 
 // Move to the next piece of the share; false at its end.
