@@ -237,20 +237,25 @@ struct Warp {
   }
   // A block that some row does not see whole may hold bytes that nobody wrote (see
   // level_min7): seen to in the stage, before its values are read as float16.
-  __device__ __forceinline__ void make_finite(uint8_t* st) const {
-    uint8_t* codes = st + KB * (width() / 2 + width() / 16);
-    uint8_t* sc = codes + KB * (width() / 2);
+  __device__ __forceinline__ uint8_t* value_codes(uint8_t* st) const { return st + KB * (width() / 2 + width() / 16); }
+  __device__ __forceinline__ uint8_t* value_scales(uint8_t* st) const { return value_codes(st) + KB * (width() / 2); }
+  // Not 0 where this lane's part of the scales has a code above kCodeSafe.
+  __device__ __forceinline__ uint32_t high_scales(uint8_t* st) const {
+    static_assert(kCodeSafe == 0xDF, "the codes above it are those with their upper three bits set");
     uint32_t high = 0;
-    for (int i = lane; i < width(); i += 32) {  // four scales a word
-      const uint32_t v = *reinterpret_cast<const uint32_t*>(sc + 4 * i);
-      high |= v & v << 1 & v << 2;  // bit 7 of a byte: its upper three bits are set
+#pragma unroll
+    for (int i = lane; i < C::D; i += 32) {  // four scales a word
+      const uint32_t v = i < width() ? reinterpret_cast<const uint32_t*>(value_scales(st))[i] : 0u;
+      high |= v & v << 1 & v << 2;
     }
-    static_assert(kCodeSafe == 0xDF, "the codes above it are those with three upper bits");
-    if (!__any_sync(0xffffffffu, high & 0x80808080u)) return;
+    return high & 0x80808080u;
+  }
+  __device__ __forceinline__ void make_finite(uint8_t* st) const {
+    uint8_t* sc = value_scales(st);
 #pragma unroll 1
     for (int i = lane; i < 4 * width(); i += 32) {  // groups, 8 bytes of codes each
       if (sc[i] <= kCodeSafe) continue;
-      uint2* w = reinterpret_cast<uint2*>(codes + 8 * i);
+      uint2* w = reinterpret_cast<uint2*>(value_codes(st) + 8 * i);
       *w = make_uint2(level_min7(w->x), level_min7(w->y));
       if (sc[i] > kCodeMax) sc[i] = 0;
     }
@@ -501,9 +506,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) cache_mma_kernel(const __grid_c
       // accumulator element e of key tile i: key 16 i + 8 (e / 2) + key_of(g), row 2t + e % 2
       auto key = [&](int i, int e) { return k0 + 16 * i + 8 * (e >> 1) + key_of(g); };
       if constexpr (!C::BWD) {
-        if (!inside) x.make_finite(st);
         float S[KB / 16][NR][4];
+        const uint32_t high = inside ? 0u : x.high_scales(st);
         x.template contract<KB / 16>(st, 0, 0, x.frag, S);
+        if (!inside && __any_sync(0xffffffffu, high != 0)) x.make_finite(st);
         bool moved = false;
         float nm[NR][2], z[NR][2];
 #pragma unroll
