@@ -19,8 +19,8 @@
 // 20 instructions a key and head and warp, four fifths of them dequantisation.
 //
 // Measured (GB300): one query of 16 users over up to 100,000 positions, 8 heads of 128
-// (0.82 GB of cache), 211 us: 3.9 TB/s of a measured copy's 6.8, DRAM busy 52 %, the integer
-// pipe 54 %, issue slots 67 %.  A lone query over 512 positions takes 13 us, two launches and
+// (0.82 GB of cache), 204 us: 4.0 TB/s of a measured copy's 6.8, DRAM busy 53 %, the integer
+// pipe 48 %, issue slots 64 %.  A lone query over 512 positions takes 11 us, two launches and
 // a walk of one block a warp.  Four tiles of 8 rows a warp for the bf16 gradient
 // spilled and were slower, plain asynchronous copies instead of bulk copies the same.
 //
@@ -47,7 +47,9 @@ struct Cfg {
   static constexpr int ROWS = 8 * NR;
   static constexpr int KB = 64;            // positions per block
   static constexpr int HALF = ROWS;        // every block of work costs the same
-  static constexpr int NS = F32 ? 3 : 1;   // bf16 terms of a query or gradient element
+  // bf16 terms of a query element, of dO's and of dS's.  One for bf16 calls: q and dO are bf16,
+  // and dS takes the rounding that the tcgen05 gradient's dS takes, for the same reason.
+  static constexpr int NS = F32 ? 3 : 1;
   static constexpr int NP = F32 ? 2 : 1;   // float16 terms of a weight
   static constexpr int LW = D / 32;        // words of 8 features a lane holds of a key
   static constexpr int MT = D / 16;        // row tiles of the transposed output
@@ -681,13 +683,13 @@ static cudaError_t run(const AttnArgs& a, cudaStream_t st) {
 
 // Rows of a tile: 8 where a user's rows fit (the average over the call decides: half the
 // products and registers of 16), else 16, which dequantises half as often; always 8 for the
-// fp32 gradient, whose 16 rows spill.  Measured on a GB300, us (8 | 16 a tile), 16 users x 8
-// heads x 10,000 positions:
+// fp32 gradient, whose 16 rows spill (their times: when they existed).  Measured on a GB300,
+// us (8 | 16 a tile), 16 users x 8 heads x 10,000 positions:
 //                          8 rows        16 rows
-//     forward, bf16        67 | 76      107 |  84    (d = 128; 64: 48 | 54 and 71 | 58)
-//     forward, fp32        75 | 110     122 | 119    (d = 64: 49 | 69 and 77 | 74)
-//     gradient, bf16       80 | 96      127 | 106    (d = 64: 49 | 61 and 76 | 68)
-//     gradient, fp32      111 | 223     195 | 230    (d = 64: 64 | 95 and 104 | 104)
+//     forward, bf16        63 | 71      103 |  76    (d = 128; 64: 42 | 48 and 66 | 51)
+//     forward, fp32        71 | 104     115 | 111    (d = 64: 43 | 61 and 70 | 66)
+//     gradient, bf16       76 | 93      126 | 101    (d = 64: 45 | 56 and 73 | 61)
+//     gradient, fp32      109 | 223     192 | 230    (d = 64: 60 | 95 and 102 | 104)
 static bool two_tiles(int B, int64_t T, int G, sa_dtype dt, bool bwd) {
   return T * G > int64_t(8) * B && !(bwd && dt == SA_F32);
 }

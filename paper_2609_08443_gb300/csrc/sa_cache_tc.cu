@@ -6,7 +6,8 @@
 // at a time.  The products need 16-bit operands in shared memory, so eight warps turn a
 // block's 4-bit words into them once for all the rows:
 //     S = Q K^T   (M = 128 rows, N = 128 positions, bf16)       accumulated in TMEM
-//     P = 2^(S - shift) in registers, float16, back over S in TMEM
+//     P = 2^(S - shift) in registers, float16, back over S in TMEM (its 11 bits leave the
+//         result's error where the result's own rounding to bf16 puts it, at 1.7e-3)
 //     O += P V    (M = 128, N = d, K = 128 positions, float16; P read from TMEM)
 // Dequantising costs about 16 instructions a word of 8 features; spread over 256 rows it
 // stays below the products.  The two warpgroups of the softmax take the units (block,
@@ -25,8 +26,8 @@
 // bounded: past the limit the CTA's roles leave, its copies and products drain and the
 // error is reported.
 //
-// Measured (GB300): 300 queries of 16 users over 10,000 positions, 8 heads of 128, 276 us, 713
-// TFLOP/s of a library product's 1894; the warp-level kernel takes 988.  No resource is
+// Measured (GB300): 300 queries of 16 users over 10,000 positions, 8 heads of 128, 274 us, 718
+// TFLOP/s of a library product's 1894; the warp-level kernel takes 944.  No resource is
 // full (tensor pipe 44 %, integer pipe 41 %): a block of 128 positions x 256 rows takes about 2,700
 // cycles, and dequantising, exponentials and issue each fill most of them with one
 // warp's instructions in a row.  Two issuers, 64 positions with twice the score buffers,
@@ -614,12 +615,12 @@ static cudaError_t run_fwd(const AttnArgs& a, cudaStream_t st) {
 // head: the tcgen05 kernels take about the same time up to 128 rows, the warp-level ones go up by
 // 16.  Measured on a GB300, us (tcgen05 | warp-level), 16 users x 8 heads x 10,000 positions:
 //     rows                 16          32          48          64          128
-//     forward, d = 128     114 |  83   115 | 128   116 | 178   118 | 229   126 | 428
-//     forward, d = 64      104 |  57   104 |  87   106 | 119   106 | 149   112 | 277
-//     gradient, d = 128    180 | 105   182 | 166   183 | 233   186 | 300   193 | 566
-//     gradient, d = 64     168 |  68   169 | 103   169 | 141   171 | 178   174 | 334
-// and the same order at 64 users x 4 heads x 1024 (forward, d = 128: 43 | 47 at 32 rows; gradient: 55
-// | 57).  The forward takes its maximum on the raw scores, so its scale is positive.
+//     forward, d = 128     112 |  76   113 | 122   115 | 173   116 | 224   123 | 423
+//     forward, d = 64      104 |  51   104 |  82   105 | 113   106 | 144   111 | 269
+//     gradient, d = 128    177 | 101   178 | 164   180 | 233   182 | 302   188 | 571
+//     gradient, d = 64     169 |  60   169 |  99   169 | 139   170 | 177   174 | 333
+// and the same order at 64 users x 4 heads x 1024 (forward, d = 128: 42 | 46 at 32 rows; gradient: 52
+// | 55).  The forward takes its maximum on the raw scores, so its scale is positive.
 bool tc_supported(int B, int64_t T, int G, int d, sa_dtype dt, float scale, bool bwd) {
   if (dt != SA_BF16 || (d != 64 && d != 128) || (!bwd && !(scale > 0.f))) return false;
   const int64_t rows = d == 128 ? (bwd ? 40 : 32) : (bwd ? 56 : 40);

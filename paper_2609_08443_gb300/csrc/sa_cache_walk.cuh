@@ -260,7 +260,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
 // time and split each row's pieces 8 / rp ways: with one row (a single token over a long
 // history) a segment has many pieces, with sixteen it has few.  Its launch overlaps the main
 // kernel's tail; what it adds is latency: one query of 16 users over up to 100,000 positions
-// takes 210 us, the main kernel alone 201 (GB300).
+// takes 204 us, the main kernel alone 199 (GB300).
 constexpr int kJoinWarps = 8;
 
 template <class C>
