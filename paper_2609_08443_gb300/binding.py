@@ -691,11 +691,10 @@ def sa_cache_write(pool: torch.Tensor, block_table: torch.Tensor, K: torch.Tenso
         raise ValueError("K and V must have contiguous rows and equal strides")
     if K.shape[1] != H or (not packed and K.shape[0] != B):
         raise ValueError(f"K{tuple(K.shape)} does not fit a cache of {H} heads and {B} users")
-    if packed:
-        _offsets_arg("cu_seqlens", cu_seqlens, B + 1, index)
     if start is not None:
         _offsets_arg("start", start, B, index)
     if packed:
+        _offsets_arg("cu_seqlens", cu_seqlens, B + 1, index)
         N, strides = K.shape[0], (0, K.stride(0), K.stride(1))
     else:
         N, strides = B * K.shape[2], (K.stride(0), K.stride(2), K.stride(1))

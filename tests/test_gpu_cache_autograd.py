@@ -60,6 +60,7 @@ def test_a_write_before_the_forward_changes_nothing(cuda_lib):
     with torch.inference_mode():
         cuda_lib.sa_cache_write(pool, table, K, K, n)
 
+
 def test_a_second_derivative_is_refused(cuda_lib):
     pool, table, lens, cu, q = setup()
     out = cuda_lib.sa_cache_attention(q, cu, pool, table, lens)
