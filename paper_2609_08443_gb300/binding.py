@@ -1,7 +1,7 @@
 """ctypes binding of libsa_sketch.so (argument marshalling only).
 
 Every function here has the name of the C entry point it calls (see
-``include/sa_sketch.h``).  Torch supplies device memory and the current CUDA
+``include/sa_sketch.h``, ``sa_cache.h`` and ``sa_dense.h``).  Torch supplies device memory and the current CUDA
 stream; all arithmetic runs in the library's kernels.  If the library is not
 built or cannot be loaded, every call raises: there is no CPU fallback.
 """
@@ -117,6 +117,21 @@ def load() -> ctypes.CDLL:
     lib.sa_cache_attn_bwd.restype = i32
     lib.sa_cache_attn_kernel_name.argtypes = [i32, i64, i32, i32, i32, f32, i32, i32]
     lib.sa_cache_attn_kernel_name.restype = ctypes.c_char_p
+    lib.sa_layer_norm_fwd.argtypes = [vp, i64, i32, vp, i64, i32, vp, vp, i32, i64, i32, f32, vp, i32, vp, vp]
+    lib.sa_layer_norm_fwd.restype = i32
+    lib.sa_layer_norm_workspace_size.argtypes = [i64, i32]
+    lib.sa_layer_norm_workspace_size.restype = sz
+    lib.sa_layer_norm_bwd.argtypes = [vp, i64, i32, vp, i64, i32, vp, i64, i32, vp, i32, vp, i64, i32, vp, vp, vp, vp,
+                                      vp, sz, vp]
+    lib.sa_layer_norm_bwd.restype = i32
+    lib.sa_linear_workspace_size.argtypes = [i64, i32, i32, i32, i32, i32, i32]
+    lib.sa_linear_workspace_size.restype = sz
+    lib.sa_linear_fwd.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+    lib.sa_linear_fwd.restype = i32
+    lib.sa_linear_bwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.sa_linear_bwd.restype = i32
+    lib.sa_linear_kernel_name.argtypes = [i64, i32, i32, i32, i32, i32]
+    lib.sa_linear_kernel_name.restype = ctypes.c_char_p
     _lib = lib
     return lib
 
@@ -595,7 +610,7 @@ def _keep(kept: dict, key, buf: torch.Tensor) -> None:
         kept[key] = buf
 
 
-def _stream_workspace(nbytes: int, index: int, stream: int) -> torch.Tensor:
+def _stream_workspace(nbytes: int, index: int, stream: int, kept: threading.local = _own_ws) -> torch.Tensor:
     """Memory for one call on the current stream.  A thread's calls on a stream come one after the other and
     share one buffer.  Two threads' calls may interleave, a call being two launches, and have their own; so has
     a captured call, whose graph may run at any time and on any stream (its pool keeps what the call took)."""
@@ -603,7 +618,7 @@ def _stream_workspace(nbytes: int, index: int, stream: int) -> torch.Tensor:
     if torch.cuda.is_current_stream_capturing():
         buf = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
     else:
-        own = _own_ws.__dict__
+        own = kept.__dict__
         buf = own.get(key)
         if buf is None or buf.numel() < nbytes:
             buf = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
@@ -611,20 +626,24 @@ def _stream_workspace(nbytes: int, index: int, stream: int) -> torch.Tensor:
     return buf
 
 
-def _note_call(buf: torch.Tensor, index: int, stream: int) -> None:
+def _note_call(buf: torch.Tensor, index: int, stream: int, kept: dict = _stream_ws_cache) -> None:
     """``buf`` holds the status of the stream's latest call."""
-    if _stream_ws_cache.get((index, stream)) is not buf:
-        _keep(_stream_ws_cache, (index, stream), buf)
+    if kept.get((index, stream)) is not buf:
+        _keep(kept, (index, stream), buf)
 
 
 def sa_cache_get_device_error(device=None) -> int:
     """Status of the latest sa_cache_* call on the current stream (from any thread) that was given no ``ws``:
     0, or what the device found (SA_ERR_TIMEOUT, SA_ERR_BAD_SEQLENS, SA_ERR_BAD_PAGE).  Waits for the stream.
     A captured call's status is that of its graph's last replay: wait for the stream that ran it first."""
+    return _kept_status(device, _stream_ws_cache)
+
+
+def _kept_status(device, kept: dict) -> int:
     index = torch.device("cuda" if device is None else device).index
     index = torch.cuda.current_device() if index is None else index
     with _on(index):
-        buf = _stream_ws_cache.get((index, _stream_handle(index)))
+        buf = kept.get((index, _stream_handle(index)))
         return 0 if buf is None else sa_get_device_error(buf)
 
 
@@ -839,3 +858,305 @@ def sa_cache_attention(q, cu_q, pool, block_table, cache_lens, kv_begin=None, kv
                        scale: Optional[float] = None):
     """Differentiable (in q) attention of packed queries over the 4-bit cache: [T, Hq, d]."""
     return CacheAttention.apply(q, cu_q, pool, block_table, cache_lens, kv_begin, kv_end, scale)
+
+
+# ------------------------------------------- layer norm and linear layers
+# (include/sa_dense.h).  Rows are a tensor's last axis; the axes before it may have any shape
+# whose rows lie a constant distance apart.
+
+SA_ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "swiglu": 4}
+
+# Workspaces of these calls, apart from the cache's: reading one family's status must not depend on the other's calls.
+_dense_ws = threading.local()
+_dense_ws_cache = {}
+
+
+def sa_linear_get_device_error(device=None) -> int:
+    """Status of the latest sa_linear_* call on the current stream (from any thread) that was given no ``ws``: 0, or
+    SA_ERR_TIMEOUT where a wait gave up.  As ``sa_cache_get_device_error`` otherwise."""
+    return _kept_status(device, _dense_ws_cache)
+
+
+def _row_stride(name: str, t: torch.Tensor, n: int, index: int, dtype=None) -> int:
+    """Elements between the rows of ``t`` [..., n] (its last axis contiguous)."""
+    if not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} must be a CUDA tensor on the call's device")
+    if t.dim() < 1 or t.shape[-1] != n or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{name} must be {dtype or 'bf16 or fp32'} [..., {n}], not {t.dtype} {tuple(t.shape)}")
+    if t.is_contiguous():
+        return n
+    if n > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    stride = rows = None
+    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if stride is None:
+            stride, rows = step, size
+        elif step != stride * rows:
+            raise ValueError(f"{name}'s rows must lie a constant distance apart")
+        else:
+            rows *= size
+    return n if stride is None else stride
+
+
+def _vector(name: str, t: Optional[torch.Tensor], n: int, index: int, dtype) -> Optional[int]:
+    if t is None:
+        return None
+    if not t.is_cuda or t.get_device() != index or t.dtype is not dtype or tuple(t.shape) != (n,) or \
+            not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} [{n}] on the call's device")
+    return t.data_ptr()
+
+
+def _on_device(name: str, t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return t.get_device()
+
+
+def sa_layer_norm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                      residual: Optional[torch.Tensor] = None, eps: float = 1e-5, dtype=None,
+                      want_stats: bool = False):
+    """Layer norm over the last axis of x + residual: y [..., n] of ``dtype`` (x's by default), and with
+    ``want_stats`` the rows' (mean, 1/sqrt(var + eps)), fp32 [..., 2], which the gradient takes.  x, residual,
+    the parameters (of one type) and y are bf16 or fp32 each."""
+    lib = load()
+    index = _on_device("x", x)
+    if x.dim() < 1:
+        raise ValueError("x must be [..., n]")
+    n = x.shape[-1]
+    xs = _row_stride("x", x, n, index)
+    rs, r_dt = 0, 0
+    if residual is not None:
+        if residual.shape != x.shape:
+            raise ValueError(f"residual{tuple(residual.shape)} must have the shape of x{tuple(x.shape)}")
+        rs, r_dt = _row_stride("residual", residual, n, index), _dt(residual)
+    w_t = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
+    w, b = _vector("weight", weight, n, index, w_t), _vector("bias", bias, n, index, w_t)
+    y = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
+    stats = torch.empty((*x.shape[:-1], 2), dtype=torch.float32, device=x.device) if want_stats else None
+    with _on(index):
+        st = lib.sa_layer_norm_fwd(x.data_ptr(), xs, _dt(x), _addr(residual), rs, r_dt, w, b,
+                                   _dt_of(w_t), x.numel() // max(n, 1), n,
+                                   float(eps), y.data_ptr(), _dt(y), _addr(stats), _stream_handle(index))
+    _check(st, "sa_layer_norm_fwd")
+    return (y, stats) if want_stats else y
+
+
+def _dt_of(dtype) -> int:
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype} (bf16 or fp32)")
+    return SA_BF16 if dtype is torch.bfloat16 else SA_F32
+
+
+def sa_layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                      residual: Optional[torch.Tensor] = None, want_dx: bool = True, want_params: bool = True,
+                      ws: Optional[torch.Tensor] = None):
+    """(dx, dr, dw, db) for the gradient dy of ``sa_layer_norm_fwd``'s y; ``stats`` are that call's.  dx is of x's
+    type and dr of residual's (the same tensor where the types agree, None without a residual); dw and db [n] are of
+    weight's type (fp32 without one).  What is not wanted is None."""
+    lib = load()
+    index = _on_device("x", x)
+    if x.dim() < 1 or dy.shape != x.shape:
+        raise ValueError(f"dy{tuple(dy.shape)} must have the shape of x{tuple(x.shape)}, [..., n]")
+    n = x.shape[-1]
+    xs, ys = _row_stride("x", x, n, index), _row_stride("dy", dy, n, index)
+    rs, r_dt = 0, 0
+    if residual is not None:
+        if residual.shape != x.shape:
+            raise ValueError(f"residual{tuple(residual.shape)} must have the shape of x{tuple(x.shape)}")
+        rs, r_dt = _row_stride("residual", residual, n, index), _dt(residual)
+    if not stats.is_cuda or stats.get_device() != index or stats.dtype is not torch.float32 or \
+            tuple(stats.shape) != (*x.shape[:-1], 2) or not stats.is_contiguous():
+        raise ValueError(f"stats must be contiguous fp32 {(*x.shape[:-1], 2)} on x's device")
+    w_t = weight.dtype if weight is not None else torch.float32
+    w = _vector("weight", weight, n, index, w_t)
+    rows = x.numel() // max(n, 1)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
+    dr = None
+    if residual is not None and want_dx:
+        dr = dx if residual.dtype is x.dtype else torch.empty(x.shape, dtype=residual.dtype, device=x.device)
+    dw = torch.empty(n, dtype=w_t, device=x.device) if want_params else None
+    db = torch.empty(n, dtype=w_t, device=x.device) if want_params else None
+    with _on(index):
+        stream = _stream_handle(index)
+        at, size = None, 0
+        if want_params:
+            need = _norm_workspace_size(index, rows, n)
+            if need == 0:
+                raise SketchError(2, "sa_layer_norm_workspace_size")
+            w_buf = _ws_arg(ws, index) if ws is not None else _stream_workspace(need, index, stream, _dense_ws)
+            at, size = w_buf.data_ptr(), w_buf.numel() * w_buf.element_size()
+        st = lib.sa_layer_norm_bwd(dy.data_ptr(), ys, _dt(dy), x.data_ptr(), xs, _dt(x), _addr(residual), rs, r_dt, w,
+                                   _dt_of(w_t), stats.data_ptr(), rows, n, _addr(dx), None if dr is dx else _addr(dr),
+                                   _addr(dw), _addr(db), at, size, stream)
+    _check(st, "sa_layer_norm_bwd")
+    return dx, dr, dw, db
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace_size(index: int, rows: int, n: int) -> int:
+    """The size on device ``index``, which is current."""
+    return int(load().sa_layer_norm_workspace_size(rows, n))
+
+
+class LayerNorm(torch.autograd.Function):
+    """y = LN(x + residual) weight + bias over the last axis; differentiable once."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, eps, dtype):
+        y, stats = sa_layer_norm_fwd(x, weight, bias, residual, eps, dtype, want_stats=True)
+        ctx.save_for_backward(x, weight, bias, residual, stats)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, residual, stats = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx, dr, dw, db = sa_layer_norm_bwd(dy.contiguous(), x, stats, weight, residual, need[0] or need[3],
+                                           need[1] or need[2])
+        if db is not None and bias is not None:
+            db = db.to(bias.dtype)
+        return dx if need[0] else None, dw if need[1] else None, db if need[2] else None, dr if need[3] else None, \
+            None, None
+
+
+def sa_layer_norm(x, weight=None, bias=None, residual=None, eps: float = 1e-5, dtype=None):
+    """Differentiable layer norm of x + residual over the last axis, [..., n] of ``dtype`` (x's by default)."""
+    return LayerNorm.apply(x, weight, bias, residual, eps, dtype)
+
+
+def _act(activation: Optional[str]) -> int:
+    code = SA_ACT.get("none" if activation is None else activation)
+    if code is None:
+        raise ValueError(f"unknown activation {activation!r}: one of {', '.join(SA_ACT)}")
+    return code
+
+
+def _repack(t: torch.Tensor, stride: int, n: int) -> bool:
+    return t.data_ptr() % 16 != 0 or stride * t.element_size() % 16 != 0 or stride < n
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_workspace_size(index: int, *sizes) -> int:
+    """The size on device ``index``, which is current."""
+    return int(load().sa_linear_workspace_size(*sizes))
+
+
+def sa_linear_kernel_name(M: int, N: int, K: int, activation: Optional[str], dt: int, which: int) -> str:
+    return load().sa_linear_kernel_name(M, N, K, _act(activation), dt, which).decode()
+
+
+def _linear_args(x, weight, activation):
+    index = _on_device("x", x)
+    act = _act(activation)
+    if weight.dim() != 2 or x.dim() < 1 or weight.dtype is not x.dtype:
+        raise ValueError("want x [..., K] and weight [N, K] (swiglu: [2 N, K]) of one dtype")
+    Z, K = weight.shape
+    if act == 4 and Z % 2:
+        raise ValueError("swiglu takes a weight [2 N, K], the gate's N rows first")
+    dt = _dt(x)
+    xs, wt = _row_stride("x", x, K, index, x.dtype), _row_stride("weight", weight, K, index, x.dtype)
+    return index, act, dt, x.numel() // max(K, 1), Z // 2 if act == 4 else Z, Z, K, xs, wt
+
+
+def sa_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                  activation: Optional[str] = None, residual: Optional[torch.Tensor] = None, want_pre: bool = False,
+                  ws: Optional[torch.Tensor] = None):
+    """y = act(x weight^T + bias) + residual, [..., N] of x's type: x [..., K], weight [Z, K], bias [Z], residual
+    [..., N].  ``activation``: none, relu, gelu (with the normal distribution function), silu, or swiglu, where the
+    weight's first half of the rows makes the gate: silu(first) * second, N = Z / 2; else N = Z.  With ``want_pre``
+    also what the activation is taken of, [..., Z], which the gradient takes (None for no activation)."""
+    lib = load()
+    index, act, dt, M, N, Z, K, xs, wt = _linear_args(x, weight, activation)
+    lead = x.shape[:-1]
+    b, rs = _vector("bias", bias, Z, index, x.dtype), 0
+    if residual is not None:
+        if tuple(residual.shape) != (*lead, N):
+            raise ValueError(f"residual{tuple(residual.shape)} must be {(*lead, N)}")
+        rs = _row_stride("residual", residual, N, index, x.dtype)
+    y = torch.empty((*lead, N), dtype=x.dtype, device=x.device)
+    z = torch.empty((*lead, Z), dtype=x.dtype, device=x.device) if want_pre and act else None
+    with _on(index):
+        stream = _stream_handle(index)
+        if ws is not None:
+            w = _ws_arg(ws, index)
+        else:
+            need = _linear_workspace_size(index, M, N, K, act, dt, 0,
+                                          _repack(x, xs, K) + 2 * _repack(weight, wt, K))
+            if need == 0:
+                raise SketchError(2, "sa_linear_workspace_size")
+            w = _stream_workspace(need, index, stream, _dense_ws)
+        st = lib.sa_linear_fwd(x.data_ptr(), xs, weight.data_ptr(), wt, b, _addr(residual), rs, M, N, K, act, dt,
+                               y.data_ptr(), _addr(z), w.data_ptr(), w.numel() * w.element_size(), stream)
+    _check(st, "sa_linear_fwd")
+    if ws is None:
+        _note_call(w, index, stream, _dense_ws_cache)
+    return (y, z) if want_pre else y
+
+
+def sa_linear_bwd(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: Optional[torch.Tensor] = None,
+                  activation: Optional[str] = None, want_dx: bool = True, want_dw: bool = True, want_db: bool = True,
+                  ws: Optional[torch.Tensor] = None):
+    """(dx [..., K], dw [Z, K], db [Z]) of x's type for the gradient dy [..., N] of ``sa_linear_fwd``'s y; ``pre`` is
+    that call's.  The residual's gradient is dy itself.  What is not wanted is None."""
+    lib = load()
+    index, act, dt, M, N, Z, K, xs, wt = _linear_args(x, weight, activation)
+    lead = x.shape[:-1]
+    if tuple(dy.shape) != (*lead, N):
+        raise ValueError(f"dy{tuple(dy.shape)} must be {(*lead, N)}")
+    ys = _row_stride("dy", dy, N, index, x.dtype)
+    if act:
+        if pre is None or tuple(pre.shape) != (*lead, Z) or pre.dtype is not x.dtype or not pre.is_contiguous() or \
+                not pre.is_cuda or pre.get_device() != index:
+            raise ValueError(f"pre must be contiguous {x.dtype} {(*lead, Z)} on x's device")
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
+    dw = torch.empty((Z, K), dtype=x.dtype, device=x.device) if want_dw else None
+    db = torch.empty(Z, dtype=x.dtype, device=x.device) if want_db else None
+    with _on(index):
+        stream = _stream_handle(index)
+        if ws is not None:
+            w = _ws_arg(ws, index)
+        else:
+            need = _linear_workspace_size(index, M, N, K, act, dt, 1, _repack(x, xs, K) +
+                                          2 * _repack(weight, wt, K) + 4 * _repack(dy, ys, N))
+            if need == 0:
+                raise SketchError(2, "sa_linear_workspace_size")
+            w = _stream_workspace(need, index, stream, _dense_ws)
+        st = lib.sa_linear_bwd(dy.data_ptr(), ys, x.data_ptr(), xs, weight.data_ptr(), wt, _addr(pre) if act else None,
+                               M, N, K, act, dt, _addr(dx), _addr(dw), _addr(db), w.data_ptr(),
+                               w.numel() * w.element_size(), stream)
+    _check(st, "sa_linear_bwd")
+    if ws is None:
+        _note_call(w, index, stream, _dense_ws_cache)
+    return dx, dw, db
+
+
+class Linear(torch.autograd.Function):
+    """y = act(x weight^T + bias) + residual; differentiable once."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, activation, residual):
+        need = any(ctx.needs_input_grad[:3])
+        y, pre = sa_linear_fwd(x, weight, bias, activation, residual, want_pre=need) if need else \
+            (sa_linear_fwd(x, weight, bias, activation, residual), None)
+        ctx.save_for_backward(x, weight, pre)
+        ctx.activation = activation
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, pre = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(need[:3]):
+            dx, dw, db = sa_linear_bwd(dy.contiguous(), x, weight, pre, ctx.activation, *need[:3])
+        return dx, dw, db, None, dy if need[4] else None
+
+
+def sa_linear(x, weight, bias=None, activation: Optional[str] = None, residual=None):
+    """Differentiable act(x weight^T + bias) + residual (see ``sa_linear_fwd``)."""
+    return Linear.apply(x, weight, bias, activation, residual)

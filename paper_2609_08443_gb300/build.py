@@ -20,7 +20,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_lib")
 LIB = os.path.join(OUT, "libsa_sketch.so")
 SOURCES = ["sa_api.cu", "sa_simt.cu", "sa_tc_fwd.cu", "sa_tc_fwd_wide.cu", "sa_tc_bwd.cu", "sa_noalloc.cu", "sa_xproj.cu", "sa_tokenwise.cu", "sa_tc_tw.cu", "sa_host_step.cu",
-           "sa_cache_api.cu", "sa_cache_rows.cu", "sa_cache_mma.cu", "sa_cache_tc.cu", "sa_cache_tc_bwd.cu"]
+           "sa_cache_api.cu", "sa_cache_rows.cu", "sa_cache_mma.cu", "sa_cache_tc.cu", "sa_cache_tc_bwd.cu",
+           "sa_dense_api.cu", "sa_dense_norm.cu", "sa_dense_simt.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2", "--expt-relaxed-constexpr",
          "-Xptxas", "-warn-spills"]
@@ -38,7 +39,7 @@ def nvcc() -> str:
 
 def _inputs():
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    files += [os.path.join(ROOT, "include", f) for f in ("sa_sketch.h", "sa_cache.h")]
+    files += [os.path.join(ROOT, "include", f) for f in ("sa_sketch.h", "sa_cache.h", "sa_dense.h")]
     files.append(os.path.abspath(__file__))
     return files
 
@@ -84,12 +85,13 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
 
 def source_hash() -> str:
     """Hash of the sketching step's CUDA sources and its ABI header (ties its traffic record to a
-    build; the cache's kernels, csrc/sa_cache*, have no part in that step)."""
+    build; the cache's and the dense operators' kernels, csrc/sa_cache* and csrc/sa_dense*, have no part
+    in that step)."""
     import hashlib
 
     h = hashlib.sha256()
     for f in sorted(os.listdir(CSRC)):
-        if f.startswith("sa_cache"):
+        if f.startswith(("sa_cache", "sa_dense")):
             continue
         with open(os.path.join(CSRC, f), "rb") as fh:
             h.update(f.encode() + b"\0" + fh.read())

@@ -1,0 +1,79 @@
+// Interface of the dense operators' kernels (include/sa_dense.h): layer norm and linear layers.
+#pragma once
+#include "sa_common.cuh"
+
+#include "../../include/sa_dense.h"
+
+namespace sa {
+namespace dense {
+
+constexpr int kMaxNorm = 16384;  // features of a normalised row
+constexpr int kMaxWidth = 1 << 20;  // K and Z of a linear layer
+
+// A matrix of contiguous rows.
+struct Mat {
+  const void* p;
+  int64_t stride;  // elements between rows
+  sa_dtype dt;
+};
+
+struct NormArgs {
+  Mat x, r, dy;  // r.p NULL: no second summand
+  const void* w;
+  const void* b;
+  sa_dtype w_dt;
+  int64_t rows;
+  int n;
+  float eps;
+  void* y;
+  sa_dtype y_dt;
+  float* stats;
+  void *dx, *dr, *dw, *db;
+  float* partial;  // [blocks][2][n]: column sums of the blocks (backward)
+};
+
+cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t st);
+cudaError_t launch_norm_bwd(const NormArgs& a, cudaStream_t st, int* launches);
+int norm_bwd_blocks(int64_t rows, int n);  // blocks that leave partial column sums
+
+// dst[c] = sum over g < G of partial[g * pitch + c], c < n, in order of g, rounded to dt.
+cudaError_t launch_join_columns(const float* partial, int G, int64_t pitch, int64_t n, void* dst, sa_dtype dt,
+                                cudaStream_t st);
+
+// C[m, n] = sum_k A(m, k) B(n, k) and what follows it.
+struct GemmArgs {
+  const void* A;
+  const void* B;
+  int64_t a_m, a_k, b_n, b_k;  // element strides
+  int64_t M;
+  int N;  // columns of y (SwiGLU: B has 2 N rows)
+  int64_t K;
+  const void* bias;
+  Mat r;
+  int act;
+  sa_dtype dt;
+  void* y;
+  void* z;
+};
+
+cudaError_t launch_simt_gemm(const GemmArgs& g, cudaStream_t st);
+
+// dz = dy act'(z) as [M, Z] rows of type dt, `pitch` elements apart (dz NULL: not stored), and
+// column sums of the unrounded dz into partial[g * Z + c] (NULL: none).
+struct ActGradArgs {
+  Mat dy;
+  const void* z;
+  int64_t M;
+  int N, Z;
+  int act;
+  void* dz;
+  int64_t pitch;
+  float* partial;
+};
+cudaError_t launch_act_grad(const ActGradArgs& a, cudaStream_t st);
+int act_grad_blocks(int64_t M, int N);
+
+int sm_count();
+
+}  // namespace dense
+}  // namespace sa

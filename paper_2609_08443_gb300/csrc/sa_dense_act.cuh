@@ -1,0 +1,89 @@
+// Activations of the linear layer and their slopes, in fp32.
+#pragma once
+#include "sa_dense.cuh"
+#include "sa_ptx.cuh"
+
+namespace sa {
+namespace dense {
+
+// Eight neighbours, 16-byte aligned.
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* v) {
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = __uint_as_float(w[j] << 16);
+    v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float* v) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* v) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(ptx::pack_bf16(v[0], v[1]), ptx::pack_bf16(v[2], v[3]),
+                                            ptx::pack_bf16(v[4], v[5]), ptx::pack_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float* p, const float* v) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// 1 / (1 + e^-z).  Results that end in bf16 take the hardware's approximations of 2^x and 1/x (a few
+// 2^-23); fp32 results the full-precision functions.
+template <bool FULL>
+__device__ __forceinline__ float sigmoid(float z) {
+  return FULL ? 1.f / (1.f + expf(-z)) : ptx::rcp_approx(1.f + ptx::ex2(-1.4426950409f * z));
+}
+
+// Phi(z) and e^(-z^2/2), Phi the normal distribution function.
+// FULL: from CUDA's erfc.  Else Phi(-x) = e^(-x^2/2) R(1 / (1 + 0.31 x)) for x >= 0, R of degree 6 without a constant
+// term: a least-squares fit with weights that level the relative error over 0 <= x <= 20 (Lawson's
+// iteration), 7.5e-6 at most; bf16's half step is 2e-3.
+template <bool FULL>
+__device__ __forceinline__ float normal_cdf(float z, float* density) {
+  const float e = FULL ? expf(-0.5f * z * z) : ptx::ex2(-0.72134752f * z * z);
+  if (density) *density = e;
+  if (FULL) return 0.5f * erfcf(-0.70710678f * z);
+  const float t = ptx::rcp_approx(fmaf(0.31f, fabsf(z), 1.f));
+  float r = fmaf(-0.07230377f, t, 0.17592333f);
+  r = fmaf(r, t, 0.020491485f);
+  r = fmaf(r, t, 0.13110992f);
+  r = fmaf(r, t, 0.120964423f);
+  r = fmaf(r, t, 0.12381754f) * t * e;
+  return z < 0.f ? r : 1.f - r;
+}
+
+// act(z) of one value (SA_ACT_SWIGLU: of the gate's half)
+template <bool FULL>
+__device__ __forceinline__ float activate(int act, float z) {
+  switch (act) {
+    case SA_ACT_RELU: return z < 0.f ? 0.f : z;  // a NaN stays one
+    case SA_ACT_GELU: return z * normal_cdf<FULL>(z, nullptr);
+    case SA_ACT_SILU:
+    case SA_ACT_SWIGLU: return z * sigmoid<FULL>(z);
+    default: return z;
+  }
+}
+
+// act'(z)
+template <bool FULL>
+__device__ __forceinline__ float slope(int act, float z) {
+  switch (act) {
+    case SA_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+    case SA_ACT_GELU: {
+      float e;
+      const float p = normal_cdf<FULL>(z, &e);
+      return fmaf(z * 0.39894228f, e, p);  // Phi + z phi, phi = e^(-z^2/2) / sqrt(2 pi)
+    }
+    case SA_ACT_SILU:
+    case SA_ACT_SWIGLU: {
+      const float p = sigmoid<FULL>(z);
+      return p * fmaf(z, 1.f - p, 1.f);
+    }
+    default: return 1.f;
+  }
+}
+
+}  // namespace dense
+}  // namespace sa

@@ -1,0 +1,287 @@
+// Host side of the dense operators: argument checks, workspace layout, the choice of kernels and
+// launches on the caller's stream.  Declarations and the meaning of every argument: include/sa_dense.h.
+#include <cmath>
+
+#include "sa_dense.cuh"
+#include "sa_kernels.cuh"
+#include "sa_tc_common.cuh"
+
+namespace {
+
+using sa::dense::Mat;
+
+constexpr int64_t kMostRows = (int64_t(1) << 31) - 256;
+
+#define SA_TRY(x)               \
+  do {                          \
+    const sa_status s_ = (x);   \
+    if (s_ != SA_OK) return s_; \
+  } while (0)
+
+bool type_ok(sa_dtype dt) { return dt == SA_F32 || dt == SA_BF16; }
+size_t size_of(sa_dtype dt) { return dt == SA_BF16 ? 2 : 4; }
+bool to_element(const void* p, sa_dtype dt) { return reinterpret_cast<uintptr_t>(p) % size_of(dt) == 0; }
+
+sa_status check_mat(const Mat& m, bool needed) {
+  if (!type_ok(m.dt)) return SA_ERR_UNSUPPORTED;
+  if ((needed && !m.p) || !to_element(m.p, m.dt) || m.stride < 0) return SA_ERR_INVALID_ARG;
+  return SA_OK;
+}
+
+sa_status check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0) return SA_ERR_INVALID_ARG;
+  return bytes < need ? SA_ERR_WORKSPACE : SA_OK;
+}
+
+sa_status status(cudaError_t e) { return e == cudaSuccess ? SA_OK : SA_ERR_CUDA; }
+
+// ------------------------------------------------------------- layer norm
+
+sa_status check_norm(const sa::dense::NormArgs& a) {
+  if (a.rows < 0 || a.n < 1) return SA_ERR_INVALID_ARG;
+  if (a.rows > kMostRows || a.n > sa::dense::kMaxNorm || !type_ok(a.w_dt) || !type_ok(a.y_dt)) return SA_ERR_UNSUPPORTED;
+  SA_TRY(check_mat(a.x, a.rows > 0));
+  SA_TRY(check_mat(a.r, false));
+  if (!to_element(a.w, a.w_dt) || !to_element(a.b, a.w_dt)) return SA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(a.stats) % 8 != 0) return SA_ERR_INVALID_ARG;
+  return SA_OK;
+}
+
+// ----------------------------------------------------------------- linear
+
+struct Linear {
+  int64_t M;
+  int N, K, Z;
+  int act;
+  sa_dtype dt;
+};
+
+bool linear_sizes_ok(int64_t M, int N, int K, int act, sa_dtype dt) {
+  return M >= 0 && N >= 1 && K >= 1 && M <= kMostRows && act >= SA_ACT_NONE && act <= SA_ACT_SWIGLU && type_ok(dt) &&
+         K <= sa::dense::kMaxWidth && N <= sa::dense::kMaxWidth / (act == SA_ACT_SWIGLU ? 2 : 1);
+}
+
+sa_status make_linear(Linear* l, int64_t M, int N, int K, sa_act act, sa_dtype dt) {
+  if (M < 0 || N < 1 || K < 1 || act < SA_ACT_NONE || act > SA_ACT_SWIGLU) return SA_ERR_INVALID_ARG;
+  if (!linear_sizes_ok(M, N, K, act, dt)) return SA_ERR_UNSUPPORTED;
+  *l = Linear{M, N, K, act == SA_ACT_SWIGLU ? 2 * N : N, act, dt};
+  return SA_OK;
+}
+
+// Sections of a linear call's workspace.
+struct Layout {
+  size_t dz, partial, total;
+  int64_t dz_pitch;
+};
+
+Layout linear_layout(const Linear& l, bool bwd, int repack) {
+  Layout w{};
+  size_t off = sizeof(sa::WsHeader);
+  w.dz_pitch = (l.Z + 7) / 8 * 8;
+  w.dz = off;
+  if (bwd && l.act != SA_ACT_NONE) off = sa::align256(off + size_t(l.M) * size_t(w.dz_pitch) * size_of(l.dt));
+  w.partial = off;
+  if (bwd) off = sa::align256(off + size_t(sa::dense::act_grad_blocks(l.M, l.N)) * size_t(l.Z) * sizeof(float));
+  (void)repack;
+  w.total = off;
+  return w;
+}
+
+int repack_bits(const Mat& x, const Mat& w, const Mat& dy, const Linear& l) {
+  auto need = [&](const Mat& m, int64_t len) {
+    return reinterpret_cast<uintptr_t>(m.p) % 16 != 0 || m.stride * int64_t(size_of(m.dt)) % 16 != 0 || m.stride < len;
+  };
+  return (need(x, l.K) ? 1 : 0) | (need(w, l.K) ? 2 : 0) | (dy.p && need(dy, l.N) ? 4 : 0);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sa_layer_norm_workspace_size(int64_t rows, int n) {
+  if (rows < 0 || rows > kMostRows || n < 1 || n > sa::dense::kMaxNorm) return 0;
+  return sizeof(sa::WsHeader) +
+         sa::align256(size_t(sa::dense::norm_bwd_blocks(rows, n)) * 2 * size_t(n) * sizeof(float));
+}
+
+sa_status sa_layer_norm_fwd(const void* x, int64_t x_stride, sa_dtype x_dt, const void* r, int64_t r_stride,
+                            sa_dtype r_dt, const void* w, const void* b, sa_dtype w_dt, int64_t rows, int n, float eps,
+                            void* y, sa_dtype y_dt, float* stats, void* stream) {
+  sa::dense::NormArgs a{};
+  a.x = Mat{x, x_stride, x_dt};
+  a.r = Mat{r, r_stride, r ? r_dt : SA_F32};
+  a.dy = Mat{nullptr, 0, SA_F32};
+  a.w = w;
+  a.b = b;
+  a.w_dt = w_dt;
+  a.rows = rows;
+  a.n = n;
+  a.eps = eps;
+  a.y = y;
+  a.y_dt = y_dt;
+  a.stats = stats;
+  SA_TRY(check_norm(a));
+  if (!(eps > 0.f) || !std::isfinite(eps)) return SA_ERR_INVALID_ARG;
+  if (!to_element(y, y_dt) || (rows > 0 && !y)) return SA_ERR_INVALID_ARG;
+  if (rows == 0) return SA_OK;
+  const cudaError_t e = sa::dense::launch_norm_fwd(a, static_cast<cudaStream_t>(stream));
+  sa::count_launches(1);
+  return status(e);
+}
+
+sa_status sa_layer_norm_bwd(const void* dy, int64_t dy_stride, sa_dtype y_dt, const void* x, int64_t x_stride,
+                            sa_dtype x_dt, const void* r, int64_t r_stride, sa_dtype r_dt, const void* w,
+                            sa_dtype w_dt, const float* stats, int64_t rows, int n, void* dx, void* dr, void* dw,
+                            void* db, void* workspace, size_t ws_bytes, void* stream) {
+  sa::dense::NormArgs a{};
+  a.x = Mat{x, x_stride, x_dt};
+  a.r = Mat{r, r_stride, r ? r_dt : SA_F32};
+  a.dy = Mat{dy, dy_stride, y_dt};
+  a.w = w;
+  a.w_dt = w_dt;
+  a.rows = rows;
+  a.n = n;
+  a.y_dt = y_dt;
+  a.stats = const_cast<float*>(stats);
+  a.dx = dx;
+  a.dr = dr;
+  a.dw = dw;
+  a.db = db;
+  SA_TRY(check_norm(a));
+  SA_TRY(check_mat(a.dy, rows > 0));
+  if (rows > 0 && !stats) return SA_ERR_INVALID_ARG;
+  if ((dr && !r) || !to_element(dx, x_dt) || !to_element(dr, a.r.dt) || !to_element(dw, w_dt) || !to_element(db, w_dt))
+    return SA_ERR_INVALID_ARG;
+  if (dw || db) {
+    SA_TRY(check_workspace(workspace, ws_bytes, sa_layer_norm_workspace_size(rows, n)));
+    a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + sizeof(sa::WsHeader));
+  } else if (rows == 0 || (!dx && !dr)) {
+    return SA_OK;
+  }
+  int launches = 0;
+  const cudaError_t e = sa::dense::launch_norm_bwd(a, static_cast<cudaStream_t>(stream), &launches);
+  sa::count_launches(launches);
+  return status(e);
+}
+
+size_t sa_linear_workspace_size(int64_t M, int N, int K, sa_act act, sa_dtype dt, int bwd, int repack) {
+  Linear l;
+  if (make_linear(&l, M, N, K, act, dt) != SA_OK) return 0;
+  return linear_layout(l, bwd != 0, repack).total;
+}
+
+sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* w, int64_t w_stride, const void* b,
+                        const void* r, int64_t r_stride, int64_t M, int N, int K, sa_act act, sa_dtype dt, void* y,
+                        void* z, void* workspace, size_t ws_bytes, void* stream) {
+  Linear l;
+  SA_TRY(make_linear(&l, M, N, K, act, dt));
+  const Mat mx{x, x_stride, dt}, mw{w, w_stride, dt}, mr{r, r_stride, dt};
+  SA_TRY(check_mat(mx, M > 0));
+  SA_TRY(check_mat(mw, true));
+  SA_TRY(check_mat(mr, false));
+  if ((M > 0 && !y) || !to_element(y, dt) || !to_element(z, dt) || !to_element(b, dt)) return SA_ERR_INVALID_ARG;
+  const Layout lay = linear_layout(l, false, repack_bits(mx, mw, Mat{nullptr, 0, dt}, l));
+  SA_TRY(check_workspace(workspace, ws_bytes, lay.total));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
+  if (M == 0) return SA_OK;
+  sa::dense::GemmArgs g{};
+  g.A = x;
+  g.a_m = x_stride;
+  g.a_k = 1;
+  g.B = w;
+  g.b_n = w_stride;
+  g.b_k = 1;
+  g.M = M;
+  g.N = N;
+  g.K = K;
+  g.bias = b;
+  g.r = mr;
+  g.act = act;
+  g.dt = dt;
+  g.y = y;
+  g.z = z;
+  const cudaError_t e = sa::dense::launch_simt_gemm(g, st);
+  sa::count_launches(1);
+  return status(e);
+}
+
+sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* w,
+                        int64_t w_stride, const void* z, int64_t M, int N, int K, sa_act act, sa_dtype dt, void* dx,
+                        void* dw, void* db, void* workspace, size_t ws_bytes, void* stream) {
+  Linear l;
+  SA_TRY(make_linear(&l, M, N, K, act, dt));
+  const Mat mx{x, x_stride, dt}, mw{w, w_stride, dt}, mdy{dy, dy_stride, dt};
+  SA_TRY(check_mat(mx, M > 0));
+  SA_TRY(check_mat(mw, true));
+  SA_TRY(check_mat(mdy, M > 0));
+  if ((M > 0 && act != SA_ACT_NONE && !z) || !to_element(z, dt) || !to_element(dx, dt) || !to_element(dw, dt) ||
+      !to_element(db, dt))
+    return SA_ERR_INVALID_ARG;
+  const Layout lay = linear_layout(l, true, repack_bits(mx, mw, mdy, l));
+  SA_TRY(check_workspace(workspace, ws_bytes, lay.total));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  char* base = static_cast<char*>(workspace);
+  if (cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
+
+  // dz and the columns' sums
+  sa::dense::ActGradArgs a{};
+  a.dy = mdy;
+  a.z = act == SA_ACT_NONE ? nullptr : z;
+  a.M = M;
+  a.N = N;
+  a.Z = l.Z;
+  a.act = act;
+  a.dz = act == SA_ACT_NONE || (!dx && !dw) ? nullptr : base + lay.dz;
+  a.pitch = lay.dz_pitch;
+  a.partial = db ? reinterpret_cast<float*>(base + lay.partial) : nullptr;
+  int launches = 0;
+  cudaError_t e = cudaSuccess;
+  if (M > 0 && (a.dz || a.partial)) {
+    e = sa::dense::launch_act_grad(a, st);
+    ++launches;
+  }
+  if (e == cudaSuccess && db) {
+    e = sa::dense::launch_join_columns(a.partial, sa::dense::act_grad_blocks(M, N), l.Z, l.Z, db, dt, st);
+    ++launches;
+  }
+  sa::dense::GemmArgs g{};
+  g.A = a.dz ? a.dz : dy;
+  const int64_t pitch = a.dz ? lay.dz_pitch : dy_stride;
+  g.dt = dt;
+  if (e == cudaSuccess && dx && M > 0) {  // dx = dz W
+    g.a_m = pitch;
+    g.a_k = 1;
+    g.B = w;
+    g.b_n = 1;
+    g.b_k = w_stride;
+    g.M = M;
+    g.N = K;
+    g.K = l.Z;
+    g.y = dx;
+    e = sa::dense::launch_simt_gemm(g, st);
+    ++launches;
+  }
+  if (e == cudaSuccess && dw) {  // dW = dz^T x
+    g.a_m = 1;
+    g.a_k = pitch;
+    g.B = x;
+    g.b_n = 1;
+    g.b_k = x_stride;
+    g.M = l.Z;
+    g.N = K;
+    g.K = M;
+    g.y = dw;
+    e = sa::dense::launch_simt_gemm(g, st);
+    ++launches;
+  }
+  sa::count_launches(launches);
+  return status(e);
+}
+
+const char* sa_linear_kernel_name(int64_t M, int N, int K, sa_act act, sa_dtype dt, int pass) {
+  if (!linear_sizes_ok(M, N, K, act, dt) || pass < 0 || pass > 2) return "unsupported";
+  return "simt_linear";
+}
+
+}  // extern "C"
