@@ -73,6 +73,42 @@ struct ActGradArgs {
 cudaError_t launch_act_grad(const ActGradArgs& a, cudaStream_t st);
 int act_grad_blocks(int64_t M, int N);
 
+// A matrix of bf16 rows `pitch` elements apart, 16-byte aligned, as TMA reads it; of fp32 values three planes of
+// terms, one behind the other.
+struct TcOperand {
+  const void* p;
+  int64_t rows, cols, pitch;
+};
+
+// How a product's tiles are dealt out (sa_dense_tc.cu).
+struct TcPlan {
+  int ctas, W;  // CTAs of a worker, workers
+  int64_t mt, nt, KB, whole, cut;
+  size_t piece_bytes;
+};
+
+// C[m, n] = sum_k A(m, k) B(n, k) on tcgen05.  K-major operands have k along their rows (a_mn, b_mn 0).
+struct TcGemm {
+  TcOperand A, B;
+  int a_mn, b_mn;
+  int64_t M;
+  int N;
+  const void* bias;
+  Mat r;
+  int act;
+  sa_dtype dt;
+  void* y;
+  void* z;
+  float* piece;
+  void* ws;
+  int clear;
+};
+
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32);
+cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches);
+// bf16 rows, or fp32 rows as three planes of bf16 terms
+cudaError_t launch_repack(const Mat& src, int64_t rows, int cols, void* dst, int64_t pitch, cudaStream_t st);
+
 int sm_count();
 
 }  // namespace dense

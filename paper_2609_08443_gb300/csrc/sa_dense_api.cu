@@ -68,30 +68,63 @@ sa_status make_linear(Linear* l, int64_t M, int N, int K, sa_act act, sa_dtype d
   return SA_OK;
 }
 
-// Sections of a linear call's workspace.
+// Which matrices TMA cannot read as they are (include/sa_dense.h): copied into aligned rows first.
+enum { COPY_X = 1, COPY_W = 2, COPY_DY = 4 };
+
+// Sections of a linear call's workspace: the operands' copies (fp32: their terms), dz, the pieces of cut tiles (of
+// one product at a time) and the partial column sums.
 struct Layout {
-  size_t dz, partial, total;
-  int64_t dz_pitch;
+  size_t x, w, dz, dz_terms, piece, partial, total;
 };
 
+int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
+
 Layout linear_layout(const Linear& l, bool bwd, int repack) {
-  Layout w{};
+  Layout s{};
+  const bool f32 = l.dt == SA_F32;
+  if (f32) repack = COPY_X | COPY_W | COPY_DY;
   size_t off = sizeof(sa::WsHeader);
-  w.dz_pitch = (l.Z + 7) / 8 * 8;
-  w.dz = off;
-  if (bwd && l.act != SA_ACT_NONE) off = sa::align256(off + size_t(l.M) * size_t(w.dz_pitch) * size_of(l.dt));
-  w.partial = off;
-  if (bwd) off = sa::align256(off + size_t(sa::dense::act_grad_blocks(l.M, l.N)) * size_t(l.Z) * sizeof(float));
-  (void)repack;
-  w.total = off;
-  return w;
+  auto section = [&](bool there, size_t bytes) {
+    const size_t at = off;
+    if (there) off = sa::align256(off + bytes);
+    return at;
+  };
+  const size_t each = f32 ? 6 : 2;  // bytes of an element's terms
+  s.x = section(repack & COPY_X, size_t(l.M) * pitch_of(l.K) * each);
+  s.w = section(repack & COPY_W, size_t(l.Z) * pitch_of(l.K) * each);
+  size_t piece = sa::dense::tc_plan(l.M, l.N, l.K, l.act == SA_ACT_SWIGLU, f32).piece_bytes;
+  if (bwd) {
+    const bool act = l.act != SA_ACT_NONE;
+    s.dz = section(act, size_t(l.M) * pitch_of(l.Z) * size_of(l.dt));
+    s.dz_terms = section(f32 || (!act && (repack & COPY_DY)), size_t(l.M) * pitch_of(l.Z) * each);
+    const size_t dx = sa::dense::tc_plan(l.M, l.K, l.Z, false, f32).piece_bytes;
+    const size_t dw = sa::dense::tc_plan(l.Z, l.K, l.M, false, f32).piece_bytes;
+    piece = dx > dw ? dx : dw;
+  }
+  s.piece = section(piece > 0, piece);
+  s.partial = section(bwd, size_t(sa::dense::act_grad_blocks(l.M, l.N)) * size_t(l.Z) * sizeof(float));
+  s.total = off;
+  return s;
 }
+
+bool on_tensor_cores() { return sa::tc_path_enabled() && sa::tcc::device_is_sm103(); }
 
 int repack_bits(const Mat& x, const Mat& w, const Mat& dy, const Linear& l) {
   auto need = [&](const Mat& m, int64_t len) {
     return reinterpret_cast<uintptr_t>(m.p) % 16 != 0 || m.stride * int64_t(size_of(m.dt)) % 16 != 0 || m.stride < len;
   };
-  return (need(x, l.K) ? 1 : 0) | (need(w, l.K) ? 2 : 0) | (dy.p && need(dy, l.N) ? 4 : 0);
+  return (need(x, l.K) ? COPY_X : 0) | (need(w, l.K) ? COPY_W : 0) | (dy.p && need(dy, l.N) ? COPY_DY : 0);
+}
+
+// A product's operand: the rows as they are, or their copy (made here) at `at`.
+cudaError_t operand(const Mat& m, int64_t rows, int64_t cols, bool copy, void* at, cudaStream_t st, int* launches,
+                    sa::dense::TcOperand* o) {
+  *o = sa::dense::TcOperand{m.p, rows, cols, m.stride};
+  if (!copy && m.dt == SA_BF16) return cudaSuccess;
+  o->p = at;
+  o->pitch = pitch_of(cols);
+  ++*launches;
+  return sa::dense::launch_repack(m, rows, int(cols), at, o->pitch, st);
 }
 
 }  // namespace
@@ -180,29 +213,51 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* w, int64_t 
   SA_TRY(check_mat(mw, true));
   SA_TRY(check_mat(mr, false));
   if ((M > 0 && !y) || !to_element(y, dt) || !to_element(z, dt) || !to_element(b, dt)) return SA_ERR_INVALID_ARG;
-  const Layout lay = linear_layout(l, false, repack_bits(mx, mw, Mat{nullptr, 0, dt}, l));
+  const int copies = repack_bits(mx, mw, Mat{nullptr, 0, dt}, l);
+  const Layout lay = linear_layout(l, false, copies);
   SA_TRY(check_workspace(workspace, ws_bytes, lay.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
-  if (M == 0) return SA_OK;
-  sa::dense::GemmArgs g{};
-  g.A = x;
-  g.a_m = x_stride;
-  g.a_k = 1;
-  g.B = w;
-  g.b_n = w_stride;
-  g.b_k = 1;
+  char* base = static_cast<char*>(workspace);
+  if (M == 0 || !on_tensor_cores()) {
+    if (cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
+    if (M == 0) return SA_OK;
+    sa::dense::GemmArgs g{};
+    g.A = x;
+    g.a_m = x_stride;
+    g.a_k = 1;
+    g.B = w;
+    g.b_n = w_stride;
+    g.b_k = 1;
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.bias = b;
+    g.r = mr;
+    g.act = act;
+    g.dt = dt;
+    g.y = y;
+    g.z = z;
+    sa::count_launches(1);
+    return status(sa::dense::launch_simt_gemm(g, st));
+  }
+  int launches = 0;
+  sa::dense::TcGemm g{};
+  cudaError_t e = operand(mx, M, K, copies & COPY_X, base + lay.x, st, &launches, &g.A);
+  if (e == cudaSuccess) e = operand(mw, l.Z, K, copies & COPY_W, base + lay.w, st, &launches, &g.B);
   g.M = M;
   g.N = N;
-  g.K = K;
   g.bias = b;
   g.r = mr;
   g.act = act;
   g.dt = dt;
   g.y = y;
   g.z = z;
-  const cudaError_t e = sa::dense::launch_simt_gemm(g, st);
-  sa::count_launches(1);
+  g.piece = reinterpret_cast<float*>(base + lay.piece);
+  g.ws = workspace;
+  g.clear = 1;
+  if (e == cudaSuccess)
+    e = sa::dense::launch_tc_gemm(g, sa::dense::tc_plan(M, N, K, act == SA_ACT_SWIGLU, dt == SA_F32), st, &launches);
+  sa::count_launches(launches);
   return status(e);
 }
 
@@ -218,11 +273,13 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
   if ((M > 0 && act != SA_ACT_NONE && !z) || !to_element(z, dt) || !to_element(dx, dt) || !to_element(dw, dt) ||
       !to_element(db, dt))
     return SA_ERR_INVALID_ARG;
-  const Layout lay = linear_layout(l, true, repack_bits(mx, mw, mdy, l));
+  const int copies = repack_bits(mx, mw, mdy, l);
+  const Layout lay = linear_layout(l, true, copies);
   SA_TRY(check_workspace(workspace, ws_bytes, lay.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* base = static_cast<char*>(workspace);
-  if (cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
+  const bool tc = on_tensor_cores() && M > 0 && (dx || dw);
+  if (!tc && cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
 
   // dz and the columns' sums
   sa::dense::ActGradArgs a{};
@@ -233,7 +290,7 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
   a.Z = l.Z;
   a.act = act;
   a.dz = act == SA_ACT_NONE || (!dx && !dw) ? nullptr : base + lay.dz;
-  a.pitch = lay.dz_pitch;
+  a.pitch = pitch_of(l.Z);
   a.partial = db ? reinterpret_cast<float*>(base + lay.partial) : nullptr;
   int launches = 0;
   cudaError_t e = cudaSuccess;
@@ -245,35 +302,67 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
     e = sa::dense::launch_join_columns(a.partial, sa::dense::act_grad_blocks(M, N), l.Z, l.Z, db, dt, st);
     ++launches;
   }
-  sa::dense::GemmArgs g{};
-  g.A = a.dz ? a.dz : dy;
-  const int64_t pitch = a.dz ? lay.dz_pitch : dy_stride;
-  g.dt = dt;
-  if (e == cudaSuccess && dx && M > 0) {  // dx = dz W
-    g.a_m = pitch;
-    g.a_k = 1;
-    g.B = w;
-    g.b_n = 1;
-    g.b_k = w_stride;
-    g.M = M;
-    g.N = K;
-    g.K = l.Z;
-    g.y = dx;
-    e = sa::dense::launch_simt_gemm(g, st);
-    ++launches;
-  }
-  if (e == cudaSuccess && dw) {  // dW = dz^T x
-    g.a_m = 1;
-    g.a_k = pitch;
-    g.B = x;
-    g.b_n = 1;
-    g.b_k = x_stride;
-    g.M = l.Z;
-    g.N = K;
-    g.K = M;
-    g.y = dw;
-    e = sa::dense::launch_simt_gemm(g, st);
-    ++launches;
+  const Mat dz = a.dz ? Mat{a.dz, a.pitch, dt} : mdy;
+  if (tc) {
+    sa::dense::TcOperand oz{}, ox{}, ow{};
+    if (e == cudaSuccess)
+      e = operand(dz, M, l.Z, !a.dz && (copies & COPY_DY), base + lay.dz_terms, st, &launches, &oz);
+    sa::dense::TcGemm g{};
+    g.dt = dt;
+    g.piece = reinterpret_cast<float*>(base + lay.piece);
+    g.ws = workspace;
+    g.clear = 1;
+    if (dx) {  // dx = dz W
+      if (e == cudaSuccess) e = operand(mw, l.Z, K, copies & COPY_W, base + lay.w, st, &launches, &ow);
+      g.A = oz;
+      g.B = ow;
+      g.b_mn = 1;
+      g.M = M;
+      g.N = K;
+      g.y = dx;
+      if (e == cudaSuccess) e = sa::dense::launch_tc_gemm(g, sa::dense::tc_plan(M, K, l.Z, false, dt == SA_F32), st, &launches);
+      g.clear = 0;
+    }
+    if (dw) {  // dW = dz^T x
+      if (e == cudaSuccess) e = operand(mx, M, K, copies & COPY_X, base + lay.x, st, &launches, &ox);
+      g.A = oz;
+      g.B = ox;
+      g.a_mn = g.b_mn = 1;
+      g.M = l.Z;
+      g.N = K;
+      g.y = dw;
+      if (e == cudaSuccess) e = sa::dense::launch_tc_gemm(g, sa::dense::tc_plan(l.Z, K, M, false, dt == SA_F32), st, &launches);
+    }
+  } else {
+    sa::dense::GemmArgs g{};
+    g.A = dz.p;
+    g.dt = dt;
+    if (e == cudaSuccess && dx && M > 0) {
+      g.a_m = dz.stride;
+      g.a_k = 1;
+      g.B = w;
+      g.b_n = 1;
+      g.b_k = w_stride;
+      g.M = M;
+      g.N = K;
+      g.K = l.Z;
+      g.y = dx;
+      e = sa::dense::launch_simt_gemm(g, st);
+      ++launches;
+    }
+    if (e == cudaSuccess && dw) {
+      g.a_m = 1;
+      g.a_k = dz.stride;
+      g.B = x;
+      g.b_n = 1;
+      g.b_k = x_stride;
+      g.M = l.Z;
+      g.N = K;
+      g.K = M;
+      g.y = dw;
+      e = sa::dense::launch_simt_gemm(g, st);
+      ++launches;
+    }
   }
   sa::count_launches(launches);
   return status(e);
@@ -281,7 +370,13 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
 
 const char* sa_linear_kernel_name(int64_t M, int N, int K, sa_act act, sa_dtype dt, int pass) {
   if (!linear_sizes_ok(M, N, K, act, dt) || pass < 0 || pass > 2) return "unsupported";
-  return "simt_linear";
+  if (!on_tensor_cores()) return "simt_linear";
+  const int64_t Z = act == SA_ACT_SWIGLU ? 2 * int64_t(N) : N;
+  const bool f32 = dt == SA_F32;
+  const sa::dense::TcPlan p = pass == 0   ? sa::dense::tc_plan(M, N, K, act == SA_ACT_SWIGLU, f32)
+                              : pass == 1 ? sa::dense::tc_plan(M, K, Z, false, f32)
+                                          : sa::dense::tc_plan(Z, K, M, false, f32);
+  return f32 ? "tc5_linear_f32" : p.ctas == 2 ? "tc5_linear_pair" : "tc5_linear";
 }
 
 }  // extern "C"

@@ -1,0 +1,613 @@
+// Products of the linear layers on tcgen05 (include/sa_dense.h): y = act(x W^T + b) + r, dx = dz W,
+// dW = dz^T x, one kernel for the three with operands in either order (K-major or MN-major tiles, so
+// nothing is transposed in memory).
+//
+// A tile is 256 x 256 for a pair of CTAs (cta_group::2: each holds 128 rows of A, half of B's rows and
+// 128 rows of the result) or 128 x 128 for one CTA.  Warp 0 loads (TMA, 64 deep blocks, six stages),
+// warp 1 issues the products, warps 4-11 end the tiles: two sets of accumulators in TMEM let one
+// tile's end overlap the next one's products.  SwiGLU's tile takes the same columns of both halves of
+// W, so gate and value meet in one warp.
+//
+// Work: tiles go to the workers (one CTA or pair an SM or two) in turn.  Where the last turn would leave many idle, its
+// tiles are dealt out in equal shares of blocks instead; a tile cut by shares leaves fp32 pieces that a second
+// kernel adds in worker order and ends, so results do not depend on timing.
+//
+// fp32 operands come as three bf16 terms each, and six of the nine products of terms are made.  The tensor
+// core's sums lose up to a step of fp32 an addition, always towards zero (1024 x 1024 sums of 1024 products were
+// 6.5e-6 off with eight blocks in a row), so each block starts with its small products, and its
+// accumulators are added to sums in registers, which round to nearest.
+#include "sa_dense_tc.cuh"
+
+#include <mutex>
+
+#include "sa_tc_common.cuh"
+
+namespace sa {
+namespace dense {
+namespace {
+
+using namespace ptx;
+
+constexpr int kTcThreads = 384;
+constexpr int kEpiWarp0 = 4;
+constexpr int kBlockBytes = 16384;  // 128 rows x 64 bf16
+constexpr uint32_t kWaitNs = 2000000000u;
+
+template <int CTAS, bool F32>
+struct TcCfg {
+  static constexpr int PLANES = F32 ? 3 : 1;
+  static constexpr int STAGE = 2 * PLANES * kBlockBytes;
+  static constexpr int STAGES = F32 ? 2 : 6;
+  static constexpr int BN = TileShape<CTAS>::BN;
+  static constexpr int TMEM = 2 * BN;
+  static constexpr int OFF_OUT = STAGES * STAGE;                     // the epilogue warps' stages
+  static constexpr int OFF_BIAS = OFF_OUT + 8 * (F32 ? 4096 : 2048);  // [2][BN] floats
+  static constexpr int OFF_BAR = OFF_BIAS + 2 * BN * 4;
+  static constexpr int SMEM = OFF_BAR + 256;
+};
+static_assert(TcCfg<2, false>::SMEM <= 232448 && TcCfg<1, true>::SMEM <= 232448, "shared memory of a CTA");
+
+// ------------------------------------------------------ cta_group::2 forms
+template <int CTAS>
+__device__ __forceinline__ void tc_alloc(uint32_t dst, uint32_t cols) {
+  if (CTAS == 1) {
+    tmem_alloc(dst, cols);
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+template <int CTAS>
+__device__ __forceinline__ void tc_dealloc(uint32_t t, uint32_t cols) {
+  if (CTAS == 1)
+    tmem_dealloc(t, cols);
+  else
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(t), "r"(cols) : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if (CTAS == 1)
+    umma_ss(d, a, b, idesc, accumulate);
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+}
+// arrives on the barrier at this offset in every CTA of the worker
+template <int CTAS>
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  if (CTAS == 1)
+    umma_commit(bar);
+  else
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "h"(uint16_t(3))
+        : "memory");
+}
+// `bar` is the first CTA's barrier (a shared::cluster address)
+template <int CTAS>
+__device__ __forceinline__ void tc_load(uint32_t dst, const void* map, uint32_t bar, int c0, int c1, int c2) {
+  if (CTAS == 1)
+    tma_load_3d(dst, map, bar, c0, c1, c2);
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+        : "memory");
+}
+
+// Maps: K-major operands [planes][rows][k], boxes of 64 x (A: 128, B: 64) rows; MN-major ones [planes][k][mn],
+// boxes of 64 x 64.
+template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    tc_linear_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const TcArgs a) {
+  using C = TcCfg<CTAS, F32>;
+  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+  using Shape = TileShape<CTAS>;
+  constexpr int YN = Shape::template YN<EPI>;
+  extern __shared__ __align__(1024) char smem[];
+  const uint32_t base = smem_u32(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CTAS == 2 ? cluster_rank() : 0;
+  const int worker = int(blockIdx.x) / CTAS;
+
+  auto full = [&](int s) { return base + C::OFF_BAR + 8 * s; };
+  auto empty = [&](int s) { return base + C::OFF_BAR + 64 + 8 * s; };
+  auto acc_full = [&](int s) { return base + C::OFF_BAR + 128 + 8 * s; };
+  auto acc_empty = [&](int s) { return base + C::OFF_BAR + 144 + 8 * s; };
+  const uint32_t bias_full = base + C::OFF_BAR + 192;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_BAR + 160);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 176);  // three words
+
+  if (threadIdx.x == 0) {
+    if (a.clear && blockIdx.x == 0) {
+      ws_header(a.ws)->err = 0;
+      ws_header(a.ws)->timeout_site = 0;
+    }
+    for (int s = 0; s < C::STAGES; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(acc_full(s), 1);
+      mbar_init(acc_empty(s), 8 * CTAS);
+    }
+    mbar_init(bias_full, 8);
+    abort_flag[0] = 0;
+    reinterpret_cast<volatile uint32_t*>(abort_flag)[2] = kWaitNs;
+    fence_mbar_init();
+    tma_prefetch_desc(&ta);
+    tma_prefetch_desc(&tb);
+  }
+  if (warp == 2) tc_alloc<CTAS>(smem_u32(tmem_slot), C::TMEM);
+  tc_fence_before();
+  if (CTAS == 2)
+    cluster_sync_all();
+  else
+    __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0 && lane == 0) {
+    // ------------------------------------------------------------- loads
+    const uint32_t lead = CTAS == 2 ? mapa_shared(base, 0) : base;
+    Segments seg(a, worker);
+    uint32_t n = 0;  // blocks loaded
+    bool ok = true;
+    while (ok && seg.next()) {
+      int mb, nb;
+      tile_place(a, seg.tile, &mb, &nb);
+      const int m0 = (mb * CTAS + int(rank)) * 128;
+      // this CTA's 128 rows of B: SwiGLU's halves are the pair's CTAs, or 64 rows each
+      int b0, b1;
+      if (EPI == EPI_GATED) {
+        b0 = CTAS == 2 ? int(rank * a.half) + nb * YN : nb * YN;
+        b1 = CTAS == 2 ? b0 + 64 : int(a.half) + nb * YN;
+      } else {
+        b0 = nb * YN + (CTAS == 2 ? int(rank) * 128 : 0);
+        b1 = b0 + 64;
+      }
+      for (int kb = seg.k0; kb < seg.k1; ++kb, ++n) {
+        const uint32_t s = n % C::STAGES, ph = (n / C::STAGES) & 1u;
+        ok = mbar_wait(empty(s), ph ^ 1u, abort_flag, a.ws, 0x401);
+        if (!ok) break;
+        if (rank == 0) mbar_arrive_expect_tx(full(s), CTAS * C::STAGE);
+        const uint32_t bar = lead + C::OFF_BAR + 8 * s, dst = base + s * C::STAGE;
+        const int k = kb * 64;
+#pragma unroll
+        for (int p = 0; p < C::PLANES; ++p) {
+          const uint32_t da = dst + p * kBlockBytes, db = dst + (C::PLANES + p) * kBlockBytes;
+          if (A_MN) {
+            tc_load<CTAS>(da, &ta, bar, m0, k, p);
+            tc_load<CTAS>(da + 8192, &ta, bar, m0 + 64, k, p);
+          } else {
+            tc_load<CTAS>(da, &ta, bar, k, m0, p);
+          }
+          if (B_MN) {
+            tc_load<CTAS>(db, &tb, bar, b0, k, p);
+            tc_load<CTAS>(db + 8192, &tb, bar, b1, k, p);
+          } else {
+            tc_load<CTAS>(db, &tb, bar, k, b0, p);
+            tc_load<CTAS>(db + 8192, &tb, bar, k, b1, p);
+          }
+        }
+      }
+    }
+    if (!ok && rank == 0)  // copies in flight land before the CTA ends
+      for (uint32_t i = n > C::STAGES ? n - C::STAGES : 0; i < n; ++i)
+        tcc::mbar_wait_bounded(full(i % C::STAGES), (i / C::STAGES) & 1u, kWaitNs);
+  } else if (warp == 1 && lane == 0 && rank == 0) {
+    // ---------------------------------------------------------- products
+    constexpr uint32_t idesc = idesc_bf16(128 * CTAS, C::BN, A_MN, B_MN);
+    constexpr uint32_t step_a = A_MN ? 2048 : 32, step_b = B_MN ? 2048 : 32;
+    const uint64_t d_a = sdesc(base, A_MN ? 8192 : 16, 1024);
+    const uint64_t d_b = sdesc(base + C::PLANES * kBlockBytes, B_MN ? 8192 : 16, 1024);
+    Segments seg(a, worker);
+    uint32_t n = 0, g = 0;  // blocks, sets of accumulators used
+    bool ok = true;
+    while (ok && seg.next()) {
+      for (int kb = seg.k0; ok && kb < seg.k1;) {
+        const int end = F32 ? kb + 1 : seg.k1;
+        const uint32_t set = g & 1u, d = tmem + set * C::BN;
+        ok = CTAS == 2 ? mbar_wait_cluster(acc_empty(set), ((g >> 1) & 1u) ^ 1u, abort_flag, a.ws, 0x402)
+                       : mbar_wait(acc_empty(set), ((g >> 1) & 1u) ^ 1u, abort_flag, a.ws, 0x402);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t accumulate = 0;
+        for (; kb < end; ++kb, ++n) {
+          const uint32_t s = n % C::STAGES;
+          ok = CTAS == 2 ? mbar_wait_cluster(full(s), (n / C::STAGES) & 1u, abort_flag, a.ws, 0x403)
+                         : mbar_wait(full(s), (n / C::STAGES) & 1u, abort_flag, a.ws, 0x403);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t sa = sdesc_add(d_a, s * C::STAGE), sb = sdesc_add(d_b, s * C::STAGE);
+          constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+          for (int i = F32 ? 0 : 5; i < 6; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              tc_mma<CTAS>(d, sdesc_add(sa, pa[i] * kBlockBytes + k * step_a),
+                           sdesc_add(sb, pb[i] * kBlockBytes + k * step_b), idesc, accumulate);
+              accumulate = 1;
+            }
+          tc_commit<CTAS>(empty(s));
+        }
+        if (!ok) break;
+        tc_commit<CTAS>(acc_full(set));
+        ++g;
+      }
+    }
+  } else if (warp >= kEpiWarp0) {
+    // -------------------------------------------------------- tiles' ends
+    const int e = warp - kEpiWarp0, q = e & 3, h = e >> 2;
+    char* out = smem + C::OFF_OUT + e * Stage<T>::BYTES;
+    const uint32_t lanes = uint32_t(q * 32) << 16;
+    const uint32_t lead_empty = CTAS == 2 ? mapa_shared(acc_empty(0), 0) : acc_empty(0);
+    constexpr int CH = Shape::template CHUNKS<EPI>;
+    Segments seg(a, worker);
+    uint32_t g = 0, tiles = 0;  // sets of accumulators and biases used
+    bool ok = true;
+    auto release = [&](uint32_t set) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (CTAS == 2)
+          mbar_arrive_cluster(lead_empty + 8 * set);
+        else
+          mbar_arrive(acc_empty(set));
+      }
+    };
+    while (ok && seg.next()) {
+      int mb, nb;
+      tile_place(a, seg.tile, &mb, &nb);
+      const int64_t m0 = int64_t(mb * CTAS + int(rank)) * 128 + q * 32;
+      const bool complete = seg.complete();
+      const float* bias = reinterpret_cast<const float*>(smem + C::OFF_BIAS) + (tiles & 1u) * C::BN;
+      if (EPI != EPI_PLAIN && complete) {
+        // the columns' biases: one thread each, ready for all epilogue warps behind their barrier
+        const int c = threadIdx.x - kEpiWarp0 * 32;
+        if (c < C::BN) {
+          const int in = EPI == EPI_GATED ? c % YN : c;
+          const int64_t n = int64_t(nb) * YN + in;
+          float v = 0.f;
+          if (a.bias && n < a.N) v = ld_f32(static_cast<const T*>(a.bias) + (EPI == EPI_GATED && c >= YN ? a.half : 0) + n);
+          reinterpret_cast<float*>(smem + C::OFF_BIAS)[(tiles & 1u) * C::BN + c] = v;
+        }
+        // every warp is past the tile before last, whose biases these replace, once it has arrived for the last
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bias_full);
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(bias_full, tiles & 1u, abort_flag, a.ws, 0x405));
+        if (!ok) break;
+        ++tiles;
+      }
+      float* piece = nullptr;
+      if (!complete) {
+        const int64_t total = a.cut * a.KB, first = (seg.tile - a.whole) * a.KB;
+        const int slot = partial_slot(total, a.W, worker, first);
+        piece = a.piece + (int64_t(worker * 2 + slot) * CTAS + rank) * (128 * C::BN) + (q * 32 + lane) * 4;
+      }
+      auto col = [&](int i, int half) {  // accumulator column of chunk i (SwiGLU: of either half)
+        return EPI == EPI_GATED ? half * YN + h * (YN / 2) + i * 32 : h * (C::BN / 2) + i * 32;
+      };
+      auto put_piece = [&](int c, const float* v) {
+        if (m0 + lane < a.M)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<float4*>(piece + int64_t(c / 4 + j) * 512) =
+                make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      };
+      if constexpr (F32) {
+        constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
+        float sum[CH][HALVES][32];
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+          for (int k = 0; k < HALVES; ++k)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[i][k][j] = 0.f;
+        for (int kb = seg.k0; kb < seg.k1; ++kb) {
+          const uint32_t set = g & 1u;
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), (g >> 1) & 1u, abort_flag, a.ws, 0x404));
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int k = 0; k < HALVES; ++k) {
+              float v[32];
+              tmem_ld32(tmem + lanes + set * C::BN + col(i, k), v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) sum[i][k][j] += v[j];
+            }
+          release(set);
+          ++g;
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          if (complete) {
+            const int n0 = nb * YN + h * (YN / 2) + i * 32;
+            Residual<T> res;
+            if (EPI != EPI_PLAIN && a.r) res.load(a, lane, m0, n0);
+            finish_chunk<T, EPI>(a, sum[i][0], sum[i][HALVES - 1], bias + col(i, 0), bias + col(i, 1), res, out, lane, m0,
+                                 n0);
+          } else {
+#pragma unroll
+            for (int k = 0; k < HALVES; ++k) put_piece(col(i, k), sum[i][k]);
+          }
+        }
+      } else {
+        Residual<T> res;
+        if (EPI != EPI_PLAIN && a.r && complete) res.load(a, lane, m0, nb * YN + h * (YN / 2));
+        const uint32_t set = g & 1u, acc = tmem + lanes + set * C::BN;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), (g >> 1) & 1u, abort_flag, a.ws, 0x404));
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll 1
+        for (int i = 0; i < CH; ++i) {
+          float v[32], u[EPI == EPI_GATED ? 32 : 1];
+          tmem_ld32(acc + col(i, 0), v);
+          if constexpr (EPI == EPI_GATED) tmem_ld32(acc + col(i, 1), u);
+          tmem_ld_wait();
+          if (i == CH - 1) release(set);
+          const int n0 = nb * YN + h * (YN / 2) + i * 32;
+          if (complete) {
+            finish_chunk<T, EPI>(a, v, u, bias + col(i, 0), bias + col(i, 1), res, out, lane, m0, n0);
+            if (EPI != EPI_PLAIN && a.r && i + 1 < CH) res.load(a, lane, m0, n0 + 32);
+          } else {
+            put_piece(col(i, 0), v);
+            if constexpr (EPI == EPI_GATED) put_piece(col(i, 1), u);
+          }
+        }
+        ++g;
+      }
+    }
+  }
+  __syncwarp();
+  if (CTAS == 2)
+    cluster_sync_all();  // nothing of the pair's is still read or written
+  else
+    __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    tc_dealloc<CTAS>(tmem, C::TMEM);
+  }
+  if (CTAS == 2) cluster_sync_all();
+}
+
+// Cut tiles: one block for 32 columns of each epilogue warp's rows; pieces are added in worker order.
+template <int CTAS, bool F32, int EPI>
+__global__ void __launch_bounds__(256) tc_join_kernel(const TcArgs a) {
+  using C = TcCfg<CTAS, F32>;
+  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+  using Shape = TileShape<CTAS>;
+  constexpr int YN = Shape::template YN<EPI>, CH = Shape::template CHUNKS<EPI>;
+  __shared__ __align__(128) char stage[8][Stage<T>::BYTES];
+  __shared__ __align__(16) float biases[8][64];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, h = warp >> 2;
+  const int i = int(blockIdx.x) % CH, rank = int(blockIdx.x) / CH % CTAS;
+  const int64_t rest = blockIdx.x / (CH * CTAS);
+  const int64_t total = a.cut * a.KB, first = rest * a.KB, last = first + a.KB - 1;
+  const int w0 = owner_of(total, a.W, first), w1 = owner_of(total, a.W, last);
+  if (w0 == w1) return;  // its worker ended it
+  int mb, nb;
+  tile_place(a, a.whole + rest, &mb, &nb);
+  const int64_t m0 = int64_t(mb * CTAS + rank) * 128 + q * 32;
+  if (m0 >= a.M) return;
+  const int n0 = nb * YN + h * (YN / 2) + i * 32;
+  auto col = [&](int half) { return EPI == EPI_GATED ? half * YN + h * (YN / 2) + i * 32 : h * (C::BN / 2) + i * 32; };
+  Residual<T> res;
+  if (EPI != EPI_PLAIN) {
+    if (a.r) res.load(a, lane, m0, n0);
+    const bool in = a.bias && n0 + lane < a.N;
+    const T* b = static_cast<const T*>(a.bias) + n0 + lane;
+    biases[warp][lane] = in ? ld_f32(b) : 0.f;
+    if (EPI == EPI_GATED) biases[warp][32 + lane] = in ? ld_f32(b + a.half) : 0.f;
+    __syncwarp();
+  }
+  float v[32], u[EPI == EPI_GATED ? 32 : 1];
+  auto sum = [&](float* x, int c) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) x[j] = 0.f;
+    if (m0 + lane >= a.M) return;
+    for (int w = w0; w <= w1; ++w) {
+      if (range_begin(total, a.W, w) == range_begin(total, a.W, w + 1)) continue;  // an empty share has no piece
+      const int slot = partial_slot(total, a.W, w, first);
+      const float* p = a.piece + (int64_t(w * 2 + slot) * CTAS + rank) * (128 * C::BN) + (q * 32 + lane) * 4;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float4 f = *reinterpret_cast<const float4*>(p + int64_t(c / 4 + j) * 512);
+        x[4 * j] += f.x, x[4 * j + 1] += f.y, x[4 * j + 2] += f.z, x[4 * j + 3] += f.w;
+      }
+    }
+  };
+  sum(v, col(0));
+  if constexpr (EPI == EPI_GATED) sum(u, col(1));
+  finish_chunk<T, EPI>(a, v, u, biases[warp], biases[warp] + 32, res, stage[warp], lane, m0, n0);
+}
+
+// Rows of dt into rows of bf16, `pitch` elements apart: as they are, or as three terms in three planes whose sum
+// is the value.
+template <typename T>
+__global__ void __launch_bounds__(256) repack_kernel(const T* src, int64_t stride, int64_t rows, int cols,
+                                                     __nv_bfloat16* dst, int64_t pitch) {
+  const int64_t plane = rows * pitch;
+  const int per_row = int(pitch / 8);
+  const int64_t all = rows * per_row;
+  for (int64_t e = blockIdx.x * int64_t(blockDim.x) + threadIdx.x; e < all; e += int64_t(gridDim.x) * blockDim.x) {
+    const int64_t row = e / per_row;
+    const int c = int(e - row * per_row) * 8;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? ld_f32(src + row * stride + c + j) : 0.f;
+    __nv_bfloat16* d = dst + row * pitch + c;
+    if (sizeof(T) == 2) {
+      store8(d, v);
+    } else {
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        float t[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          t[j] = __bfloat162float(__float2bfloat16_rn(v[j]));
+          v[j] -= t[j];  // exact
+        }
+        store8(d + p * plane, t);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ launch
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                             const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                             CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+  static EncodeFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeFn>(p);
+  });
+  return fn;
+}
+
+// rows of `cols` bf16, `pitch` elements apart, `planes` times
+bool make_map(CUtensorMap* m, const TcOperand& o, bool f32, int box_rows) {
+  EncodeFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {cuuint64_t(o.cols), cuuint64_t(o.rows), cuuint64_t(f32 ? 3 : 1)};
+  const cuuint64_t strides[2] = {cuuint64_t(o.pitch) * 2, cuuint64_t(o.pitch) * o.rows * 2};
+  const cuuint32_t box[3] = {64, cuuint32_t(box_rows), 1};
+  const cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.p), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
+cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaStream_t st, int* launches) {
+  using C = TcCfg<CTAS, F32>;
+  CUtensorMap ta, tb;
+  if (!make_map(&ta, g.A, F32, A_MN ? 64 : 128) || !make_map(&tb, g.B, F32, 64)) return cudaErrorInvalidValue;
+  auto fn = &tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>;
+  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(p.W * CTAS), 1, 1);
+  cfg.blockDim = dim3(kTcThreads, 1, 1);
+  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CTAS;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, fn, ta, tb, a);
+  ++*launches;
+  if (e != cudaSuccess || p.cut == 0) return e;
+  constexpr int CH = TileShape<CTAS>::template CHUNKS<EPI>;
+  tc_join_kernel<CTAS, F32, EPI><<<unsigned(p.cut * CTAS * CH), 256, 0, st>>>(a);
+  ++*launches;
+  return cudaGetLastError();
+}
+
+template <int CTAS, bool F32>
+cudaError_t launch_kind(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaStream_t st, int* launches) {
+  if (g.a_mn) return launch_one<CTAS, true, true, F32, EPI_PLAIN>(g, p, a, st, launches);
+  if (g.b_mn) return launch_one<CTAS, false, true, F32, EPI_PLAIN>(g, p, a, st, launches);
+  if (g.act == SA_ACT_SWIGLU) return launch_one<CTAS, false, false, F32, EPI_GATED>(g, p, a, st, launches);
+  return launch_one<CTAS, false, false, F32, EPI_FULL>(g, p, a, st, launches);
+}
+
+}  // namespace
+
+// What a call of these sizes runs on, by the blocks' time it would take (in units of a 64-deep block of
+// a pair's tile, 512 cycles): a pair's block makes four times a single CTA's products in the same time, both being
+// fed 32 KB a CTA; the end of a cut tile costs a launch and the pieces' way through L2.
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32) {
+  TcPlan best{};
+  double cost = 0;
+  const int sms = sm_count();
+  const int64_t KB = (K + 63) / 64;
+  for (int ctas = 1; ctas <= (f32 || sms < 2 ? 1 : 2); ++ctas) {
+    const int bn = ctas == 2 ? 256 : 128, yn = gated ? bn / 2 : bn;
+    const int64_t mt = (M + 128 * ctas - 1) / (128 * ctas), nt = (N + yn - 1) / yn, tiles = mt * nt;
+    const int W = sms / ctas;
+    const int64_t waves = tiles / W, rest = tiles % W;
+    const double block = f32 ? 3.0 : 1.0, join = 10 + (ctas == 2 ? 16.0 : 8.0);
+    for (int cut = 0; cut <= (rest ? 1 : 0); ++cut) {
+      const double blocks = cut ? double(waves) * KB + double((rest * KB + W - 1) / W) : double(waves + (rest ? 1 : 0)) * KB;
+      const double c = blocks * block + (cut ? join : 0);
+      if (best.W == 0 || c < cost) {
+        cost = c;
+        best.ctas = ctas;
+        best.W = W;
+        best.mt = mt;
+        best.nt = nt;
+        best.whole = cut ? waves * W : tiles;
+        best.cut = cut ? rest : 0;
+      }
+    }
+  }
+  best.KB = KB;
+  best.piece_bytes = best.cut ? size_t(best.W) * 2 * best.ctas * 128 * (best.ctas == 2 ? 256 : 128) * sizeof(float) : 0;
+  return best;
+}
+
+cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches) {
+  TcArgs a{};
+  a.M = g.M;
+  a.N = g.N;
+  a.KB = int(p.KB);
+  a.mt = int(p.mt);
+  a.nt = int(p.nt);
+  a.W = p.W;
+  a.whole = p.whole;
+  a.cut = p.cut;
+  a.half = g.N;
+  a.bias = g.bias;
+  a.r = g.r.p;
+  a.r_stride = g.r.stride;
+  a.act = g.act;
+  a.y = g.y;
+  a.z = g.z;
+  a.Z = g.act == SA_ACT_SWIGLU ? 2 * int64_t(g.N) : g.N;
+  const int each = g.dt == SA_BF16 ? 8 : 4;
+  auto base_ok = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
+  a.vec = (g.N % each == 0 && base_ok(g.y) && base_ok(g.z) ? 1 : 0) |
+          (g.N % each == 0 && g.r.stride % each == 0 && base_ok(g.r.p) ? 2 : 0);
+  a.piece = g.piece;
+  a.ws = g.ws;
+  a.clear = g.clear;
+  if (g.dt == SA_F32) return launch_kind<1, true>(g, p, a, st, launches);
+  return p.ctas == 2 ? launch_kind<2, false>(g, p, a, st, launches) : launch_kind<1, false>(g, p, a, st, launches);
+}
+
+cudaError_t launch_repack(const Mat& src, int64_t rows, int cols, void* dst, int64_t pitch, cudaStream_t st) {
+  const int64_t all = rows * (pitch / 8);
+  if (all == 0) return cudaSuccess;
+  const int64_t need = (all + 255) / 256, most = int64_t(sm_count()) * 16;
+  const unsigned grid = unsigned(need < most ? need : most);
+  __nv_bfloat16* d = static_cast<__nv_bfloat16*>(dst);
+  if (src.dt == SA_BF16)
+    repack_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src.p), src.stride, rows, cols, d,
+                                                       pitch);
+  else
+    repack_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(src.p), src.stride, rows, cols, d, pitch);
+  return cudaGetLastError();
+}
+
+}  // namespace dense
+}  // namespace sa
