@@ -40,6 +40,10 @@ int norm_bwd_blocks(int64_t rows, int n);  // blocks that leave partial column s
 cudaError_t launch_join_columns(const float* partial, int G, int64_t pitch, int64_t n, void* dst, sa_dtype dt,
                                 cudaStream_t st);
 
+// The same for two sets in one launch (d NULL: none).
+cudaError_t launch_join_columns2(const float* p0, int G, int64_t pitch, int64_t n0, void* d0, const float* p1, int64_t n1,
+                                 void* d1, sa_dtype dt, cudaStream_t st);
+
 // C[m, n] = sum_k A(m, k) B(n, k) and what follows it.
 struct GemmArgs {
   const void* A;

@@ -7,10 +7,14 @@
 // between the mean, the variance (of the differences from that mean, so a mean far from zero
 // costs no digits) and the result.  T threads hold a row, C chunks of 8 elements each: 8 to 32
 // lanes of a warp up to 512 features, a block above.  A block walks rows with the parameters,
-// and in the backward pass the columns' running sums, in registers (shared memory above 4096
+// and in the backward pass the columns' running sums, in registers (shared memory above 8192
 // features, whose sums would not fit); its sums leave as one partial row, and a second kernel
 // adds the partial rows in block order, so results do not depend on timing.
-#include "sa_dense.cuh"
+//
+// A row's loads, sums and stores wait for one another, so the next rows are on their way meanwhile: each
+// thread's own 16-byte pieces of the next two rows by cp.async (nobody else reads them, so nothing but the
+// thread's own copies is waited for), or, where rows are not 16-byte aligned, the next row's elements in registers.
+#include "sa_dense_act.cuh"
 #include "sa_tc_common.cuh"
 
 namespace sa {
@@ -21,6 +25,9 @@ int sm_count() { return tcc::device_sm_count(); }
 namespace {
 
 constexpr int kThreads = 256;  // of a block that holds several rows at once
+// Rows of a thread's ring: the one in work and two on their way (2 to 8 measured the same; the widest rows have room for 2).
+template <int T>
+constexpr int ring_rows() { return T == 1024 ? 2 : 3; }
 
 template <int T>
 constexpr int block_threads() { return T <= 32 ? kThreads : T; }
@@ -36,51 +43,206 @@ __device__ __forceinline__ int column(int t, int c, int j) {
 
 template <int T, int C, bool VEC>
 __device__ __forceinline__ void load_row(const void* p, sa_dtype dt, int64_t at, int t, int n, float* v) {
-  if (dt == SA_BF16) {
-    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p) + at;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (VEC) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (column<T, true>(t, c, 0) < n) u = *reinterpret_cast<const uint4*>(q + column<T, true>(t, c, 0));
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  for (int c = 0; c < C; ++c) {
+    if (VEC) {
+      const int k = column<T, true>(t, c, 0);
+      if (k >= n) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[8 * c + 2 * j] = __uint_as_float(w[j] << 16);
-          v[8 * c + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-        }
+        for (int j = 0; j < 8; ++j) v[8 * c + j] = 0.f;
+      } else if (dt == SA_BF16) {
+        load8(static_cast<const __nv_bfloat16*>(p) + at + k, v + 8 * c);
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int k = column<T, false>(t, c, j);
-          v[8 * c + j] = k < n ? __bfloat162float(q[k]) : 0.f;
-        }
+        load8(static_cast<const float*>(p) + at + k, v + 8 * c);
       }
-    }
-  } else {
-    const float* q = static_cast<const float*>(p) + at;
+    } else {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (VEC) {
-        float4 a = make_float4(0, 0, 0, 0), b = a;
-        if (column<T, true>(t, c, 0) < n) {
-          const float4* s = reinterpret_cast<const float4*>(q + column<T, true>(t, c, 0));
-          a = s[0];
-          b = s[1];
-        }
-        const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[8 * c + j] = w[j];
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int k = column<T, false>(t, c, j);
-          v[8 * c + j] = k < n ? q[k] : 0.f;
-        }
+      for (int j = 0; j < 8; ++j) {
+        const int k = column<T, false>(t, c, j);
+        v[8 * c + j] = k >= n ? 0.f : dt == SA_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at + k])
+                                                    : static_cast<const float*>(p)[at + k];
       }
     }
   }
 }
+
+// 16-byte pieces that a chunk of 8 elements takes
+__device__ __forceinline__ int pieces(const Mat& m) { return !m.p ? 0 : m.dt == SA_BF16 ? 1 : 2; }
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// ... through L1, where the neighbour's half of the same 32 bytes is found again
+__device__ __forceinline__ void copy16_l1(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// One matrix along a walk: where this thread's first element of the next row to be fetched is, and how far the row
+// after it is away.
+struct Track {
+  const char* p;
+  int64_t step;
+  bool half;  // bf16
+  __device__ __forceinline__ Track(const Mat& m, int64_t row, int64_t rows, int first)
+      : p(static_cast<const char*>(m.p)), half(m.dt == SA_BF16) {
+    p += (row * m.stride + first) << (half ? 1 : 2);
+    step = (rows * m.stride) << (half ? 1 : 2);
+  }
+};
+
+// The rows that a block walks, with the next ones on their way: VEC: each thread's slots of a ring of rows in
+// shared memory; else the next row's elements in registers, as they were read.  NEXT: false where neither fits.
+template <int T, int C, bool VEC, bool NEXT, bool GRAD>
+struct Walk {
+  const int t, n;
+  const uint32_t rows, step;
+  uint32_t row, ahead;  // this thread's row, and the next that it fetches
+  const bool sum;       // there is a second summand
+  bool in[VEC ? C : 1];
+  Track x, r, dy;
+  uint32_t raw[VEC ? 1 : (GRAD ? 3 : 2)][VEC ? 1 : 8 * C];
+  const char* ring;
+  uint32_t put, get;  // byte offsets of the rows to fetch and to take
+  uint32_t per_row, off_r, off_dy;
+
+  static constexpr uint32_t kApart = block_threads<T>() * 16;
+  static constexpr int kRing = ring_rows<T>();
+
+  __device__ Walk(const NormArgs& a, char* mem)
+      : t(threadIdx.x % T), n(a.n), rows(uint32_t(a.rows)), step(gridDim.x * rows_at_once<T>()),
+        row(blockIdx.x * rows_at_once<T>() + threadIdx.x / T), ahead(row), sum(a.r.p != nullptr),
+        x(a.x, row, step, VEC ? t * 8 : t), r(a.r, row, step, VEC ? t * 8 : t), dy(a.dy, row, step, VEC ? t * 8 : t) {
+    if (VEC) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) in[c] = column<T, true>(t, c, 0) < n;
+      ring = mem + threadIdx.x * 16;
+      off_r = C * kApart * pieces(a.x);
+      off_dy = off_r + C * kApart * pieces(a.r);
+      per_row = off_dy + (GRAD ? C * kApart * pieces(a.dy) : 0);
+      put = get = 0;
+    }
+    if (NEXT) {
+#pragma unroll
+      for (int i = 0; i < (VEC ? kRing - 1 : 1); ++i) fetch();
+    }
+  }
+  __device__ __forceinline__ void copy(const Track& m, uint32_t to) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (!in[c]) continue;
+      if (m.half) {
+        copy16(to + c * kApart, m.p + c * T * 16);
+      } else {
+        copy16_l1(to + 2 * c * kApart, m.p + c * T * 32);
+        copy16_l1(to + (2 * c + 1) * kApart, m.p + c * T * 32 + 16);
+      }
+    }
+  }
+  __device__ __forceinline__ void read(const Track& m, uint32_t* v) const {
+    if (m.half) {
+      const uint16_t* p = reinterpret_cast<const uint16_t*>(m.p);
+#pragma unroll
+      for (int i = 0; i < 8 * C; ++i) v[i] = i * T + t < n ? p[i * T] : 0;
+    } else {
+      const uint32_t* p = reinterpret_cast<const uint32_t*>(m.p);
+#pragma unroll
+      for (int i = 0; i < 8 * C; ++i) v[i] = i * T + t < n ? p[i * T] : 0;
+    }
+  }
+  // the next row's elements on their way
+  __device__ __forceinline__ void fetch() {
+    if (ahead < rows) {
+      if (VEC) {
+        const uint32_t to = ptx::smem_u32(ring) + put;
+        copy(x, to);
+        if (sum) copy(r, to + off_r);
+        if (GRAD) copy(dy, to + off_dy);
+      } else {
+        read(x, raw[0]);
+        if (sum) read(r, raw[1]);
+        if (GRAD) read(dy, raw[2]);
+      }
+    }
+    ahead += step;
+    x.p += x.step;
+    if (sum) r.p += r.step;
+    if (GRAD) dy.p += dy.step;
+    if (VEC) {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      put = put == (kRing - 1) * per_row ? 0 : put + per_row;
+    }
+  }
+  // the block's rows are not all done (the same for all of its threads)
+  __device__ __forceinline__ bool more() const { return row - threadIdx.x / T < rows; }
+  __device__ __forceinline__ bool here() const { return row < rows; }
+
+  template <bool ADD>
+  __device__ __forceinline__ void unpack(bool half, const char* from, float* v) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float q[8];
+      if (half) {
+        load8(reinterpret_cast<const __nv_bfloat16*>(from + c * kApart), q);
+      } else {
+        const float4 a = *reinterpret_cast<const float4*>(from + 2 * c * kApart);
+        const float4 b = *reinterpret_cast<const float4*>(from + (2 * c + 1) * kApart);
+        q[0] = a.x, q[1] = a.y, q[2] = a.z, q[3] = a.w, q[4] = b.x, q[5] = b.y, q[6] = b.z, q[7] = b.w;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[8 * c + j] = ADD ? v[8 * c + j] + q[j] : q[j];
+    }
+  }
+  template <bool ADD>
+  __device__ __forceinline__ void convert(bool half, const uint32_t* w, float* v) const {
+#pragma unroll
+    for (int i = 0; i < 8 * C; ++i) {
+      const float q = __uint_as_float(half ? w[i] << 16 : w[i]);
+      v[i] = ADD ? v[i] + q : q;
+    }
+  }
+  // x + r (and dy) of this thread's row; zeros behind the row's end and, in dy, behind the last row
+  __device__ __forceinline__ void take(const NormArgs& a, float* h, float* g) {
+    if (NEXT && VEC) {
+      fetch();
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      const char* from = ring + get;
+      unpack<false>(x.half, from, h);
+      if (sum) unpack<true>(r.half, from + off_r, h);
+      if (GRAD) unpack<false>(dy.half, from + off_dy, g);
+      get = get == (kRing - 1) * per_row ? 0 : get + per_row;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (!in[c] || !here()) {  // the slots hold whatever was there
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            h[8 * c + j] = 0.f;
+            if (GRAD) g[8 * c + j] = 0.f;
+          }
+        }
+    } else if (NEXT) {
+      convert<false>(x.half, raw[0], h);
+      if (sum) convert<true>(r.half, raw[1], h);
+      if (GRAD) convert<false>(dy.half, raw[2], g);
+      if (!here())
+#pragma unroll
+        for (int i = 0; i < 8 * C; ++i) {
+          h[i] = 0.f;
+          if (GRAD) g[i] = 0.f;
+        }
+      fetch();
+    } else {
+      const int end = here() ? n : 0;
+      load_row<T, C, VEC>(a.x.p, a.x.dt, int64_t(row) * a.x.stride, t, end, h);
+      if (GRAD) load_row<T, C, VEC>(a.dy.p, a.dy.dt, int64_t(row) * a.dy.stride, t, end, g);
+      if (sum) {
+        float v[8 * C];
+        load_row<T, C, VEC>(a.r.p, a.r.dt, int64_t(row) * a.r.stride, t, end, v);
+#pragma unroll
+        for (int i = 0; i < 8 * C; ++i) h[i] += v[i];
+      }
+    }
+  }
+};
 
 template <int T, int C, bool VEC>
 __device__ __forceinline__ void store_row(void* p, sa_dtype dt, int64_t at, int t, int n, const float* v) {
@@ -89,16 +251,10 @@ __device__ __forceinline__ void store_row(void* p, sa_dtype dt, int64_t at, int 
     if (VEC) {
       const int k = column<T, true>(t, c, 0);
       if (k >= n) continue;
-      if (dt == SA_BF16) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = ptx::pack_bf16(v[8 * c + 2 * j], v[8 * c + 2 * j + 1]);
-        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + at + k) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {
-        float4* s = reinterpret_cast<float4*>(static_cast<float*>(p) + at + k);
-        s[0] = make_float4(v[8 * c], v[8 * c + 1], v[8 * c + 2], v[8 * c + 3]);
-        s[1] = make_float4(v[8 * c + 4], v[8 * c + 5], v[8 * c + 6], v[8 * c + 7]);
-      }
+      if (dt == SA_BF16)
+        store8(static_cast<__nv_bfloat16*>(p) + at + k, v + 8 * c);
+      else
+        store8(static_cast<float*>(p) + at + k, v + 8 * c);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -157,63 +313,145 @@ __device__ __forceinline__ void row_sum(float (&v)[K], float* red, int& turn) {
   }
 }
 
-template <int T, int C, bool VEC>
-__global__ void __launch_bounds__(block_threads<T>()) norm_fwd_kernel(const NormArgs a) {
-  __shared__ float red[T > 32 ? 2 * T / 32 : 1];
+// Mean of a row's n elements and the sum of the squared differences from it, of the warps' own (sum, sum of
+// squared differences from the warp's mean, elements): M = sum M_w + sum n_w (mean_w - mean)^2, one barrier in all.
+template <int T>
+__device__ __forceinline__ float2 row_moments(float sum, float m2, float count, float inv_n, float* red, int& turn) {
+  constexpr int W = T / 32;
+  float* s = red + turn * W * 3;
+  turn ^= 1;
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) {
+    s[(threadIdx.x >> 5)] = sum;
+    s[W + (threadIdx.x >> 5)] = m2;
+    s[2 * W + (threadIdx.x >> 5)] = count;
+  }
+  __syncthreads();
+  const float sw = lane < W ? s[lane] : 0.f, mw = lane < W ? s[W + lane] : 0.f, cw = lane < W ? s[2 * W + lane] : 0.f;
+  float all = sw;
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+  if (W < 32) all = __shfl_sync(0xFFFFFFFFu, all, 0);
+  const float mean = all * inv_n;
+  const float d = cw > 0.f ? sw / cw - mean : 0.f;
+  float m = fmaf(cw * d, d, mw);
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, o);
+  if (W < 32) m = __shfl_sync(0xFFFFFFFFu, m, 0);
+  return make_float2(mean, m);
+}
+
+__device__ __forceinline__ float2 pair(const float* v, int i) { return make_float2(v[2 * i], v[2 * i + 1]); }
+__device__ __forceinline__ void unpair(float* v, int i, float2 x) { v[2 * i] = x.x, v[2 * i + 1] = x.y; }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Blocks an SM that the register budget is made for: 64 to 128 a thread, by what it holds.
+template <int T, int C, bool VEC, bool GRAD>
+constexpr int blocks_at_once() {
+  return T == 1024 ? 1 : (C == 2 || (GRAD && !VEC) ? 512 : GRAD || !VEC ? 768 : 1024) / block_threads<T>();
+}
+
+template <int T, int C, bool VEC, bool NEXT>
+__global__ void __launch_bounds__(block_threads<T>(), blocks_at_once<T, C, VEC, false>()) norm_fwd_kernel(const NormArgs a) {
+  extern __shared__ __align__(16) char ring[];
+  __shared__ float red[T > 32 ? 6 * T / 32 : 1];
+  constexpr int P = 4 * C;  // pairs of elements, whose arithmetic goes two at a time
   const int t = threadIdx.x % T, n = a.n;
   const float inv_n = 1.f / float(n);
   int turn = 0;
   float w[8 * C], b[8 * C];
+  Walk<T, C, VEC, NEXT, false> at(a, ring);
   if (keep_parameters<T, C>()) {
     load_factors<T, C, VEC>(a, t, n, w);
     load_row<T, C, VEC>(a.b, a.w_dt, 0, t, a.b ? n : 0, b);
   }
-  const int64_t step = int64_t(gridDim.x) * rows_at_once<T>();
-  for (int64_t base = int64_t(blockIdx.x) * rows_at_once<T>(); base < a.rows; base += step) {
-    const int64_t row = base + threadIdx.x / T;
-    const int here = row < a.rows ? n : 0;  // a warp's last rows may lie behind the end
-    float h[8 * C], s[1] = {0.f};
-    load_row<T, C, VEC>(a.x.p, a.x.dt, row * a.x.stride, t, here, h);
-    if (a.r.p) {
-      float r[8 * C];
-      load_row<T, C, VEC>(a.r.p, a.r.dt, row * a.r.stride, t, here, r);
+  auto inside = [&](int i) { return VEC ? at.in[VEC ? i / 8 : 0] : column<T, false>(t, i / 8, i % 8) < n; };
+  float count = 0.f;  // elements of this warp, in a row that is spread over several
+  if (T > 32) {
 #pragma unroll
-      for (int i = 0; i < 8 * C; ++i) h[i] += r[i];
+    for (int i = 0; i < 8 * C; ++i) count += inside(i) ? 1.f : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
+  }
+  const float inv_count = T <= 32 ? inv_n : count > 0.f ? 1.f / count : 0.f;
+  constexpr int lanes = T < 32 ? T : 32;
+  for (; at.more(); at.row += at.step) {
+    float h[8 * C];
+    at.take(a, h, nullptr);
+    float2 s2 = both(0.f);
+#pragma unroll
+    for (int i = 0; i < P; ++i) s2 = __fadd2_rn(s2, pair(h, i));
+    float sum = s2.x + s2.y;
+#pragma unroll
+    for (int o = lanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    // squared differences from the mean of what the warp holds: the row's, or the warp's own
+    float mean = sum * inv_count;
+    float2 m2 = both(0.f);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const float2 d = __fadd2_rn(pair(h, i), both(-mean));
+      if (T <= 32) unpair(h, i, d);
+      if (VEC) {
+        if (inside(2 * i)) m2 = __ffma2_rn(d, d, m2);
+      } else {
+        if (inside(2 * i)) m2.x = fmaf(d.x, d.x, m2.x);
+        if (inside(2 * i + 1)) m2.y = fmaf(d.y, d.y, m2.y);
+      }
     }
+    float m = m2.x + m2.y;
 #pragma unroll
-    for (int i = 0; i < 8 * C; ++i) s[0] += h[i];
-    row_sum<T>(s, red, turn);
-    const float mean = s[0] * inv_n;
-    s[0] = 0.f;
+    for (int o = lanes / 2; o > 0; o >>= 1) m += __shfl_xor_sync(0xFFFFFFFFu, m, o);
+    if constexpr (T > 32) {
+      const float2 all = row_moments<T>(sum, m, count, inv_n, red, turn);
+      mean = all.x;
+      m = all.y;
 #pragma unroll
-    for (int i = 0; i < 8 * C; ++i) {
-      h[i] -= mean;
-      if (column<T, VEC>(t, i / 8, i % 8) < n) s[0] = fmaf(h[i], h[i], s[0]);
+      for (int i = 0; i < P; ++i) unpair(h, i, __fadd2_rn(pair(h, i), both(-mean)));
     }
-    row_sum<T>(s, red, turn);
-    const float rstd = rsqrtf(fmaf(s[0], inv_n, a.eps));
-    if (here) {
+    const float rstd = rsqrtf(fmaf(m, inv_n, a.eps));
+    if (at.here()) {  // a warp's last rows may lie behind the end
       if (!keep_parameters<T, C>()) {
         load_factors<T, C, VEC>(a, t, n, w);
         load_row<T, C, VEC>(a.b, a.w_dt, 0, t, a.b ? n : 0, b);
       }
 #pragma unroll
-      for (int i = 0; i < 8 * C; ++i) h[i] = fmaf(h[i] * rstd, w[i], b[i]);
-      store_row<T, C, VEC>(a.y, a.y_dt, row * n, t, n, h);
-      if (a.stats && t == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(mean, rstd);
+      for (int i = 0; i < P; ++i)
+        unpair(h, i, __ffma2_rn(__fmul2_rn(pair(h, i), both(rstd)), pair(w, i), pair(b, i)));
+      store_row<T, C, VEC>(a.y, a.y_dt, int64_t(at.row) * n, t, n, h);
+      if (a.stats && t == 0) *reinterpret_cast<float2*>(a.stats + 2 * int64_t(at.row)) = make_float2(mean, rstd);
     }
   }
 }
 
+// Adds to the shared sums of pair i's columns ([2][n]; each thread has its own columns).
+template <int T, int C, bool VEC>
+__device__ __forceinline__ void add_to_sums(float* sums, int n, int t, int i, float2 w, float2 b) {
+  const int k = column<T, VEC>(t, i / 4, 2 * i % 8);
+  if (VEC) {
+    if (k >= n) return;
+    float2* p = reinterpret_cast<float2*>(sums + k);
+    *p = __fadd2_rn(*p, w);
+    p = reinterpret_cast<float2*>(sums + n + k);
+    *p = __fadd2_rn(*p, b);
+  } else {
+    const int l = column<T, VEC>(t, i / 4, 2 * i % 8 + 1);
+    if (k < n) sums[k] += w.x, sums[n + k] += b.x;
+    if (l < n) sums[l] += w.y, sums[n + l] += b.y;
+  }
+}
+
 // SUMS: where the columns' running sums are: 0 nowhere, 1 registers, 2 shared memory.
-template <int T, int C, bool VEC, int SUMS>
-__global__ void __launch_bounds__(block_threads<T>()) norm_bwd_kernel(const NormArgs a) {
-  extern __shared__ float sums[];  // SUMS = 2: [2][n]; SUMS = 1 and T <= 32: [warps][2][8 C lanes]
+template <int T, int C, bool VEC, bool NEXT, int SUMS>
+__global__ void __launch_bounds__(block_threads<T>(), blocks_at_once<T, C, VEC, true>()) norm_bwd_kernel(const NormArgs a) {
+  // SUMS = 2: [2][n] sums; SUMS = 1 and T <= 32: at the end [warps][2][8 C T]; NEXT: the ring
+  extern __shared__ __align__(16) float sums[];
   __shared__ float red[T > 32 ? 4 * T / 32 : 1];
+  constexpr int P = 4 * C;
   const int t = threadIdx.x % T, n = a.n;
   const float inv_n = 1.f / float(n);
   int turn = 0;
   float w[8 * C];
+  Walk<T, C, VEC, NEXT, true> at(a, reinterpret_cast<char*>(sums));
   if (keep_parameters<T, C>()) load_factors<T, C, VEC>(a, t, n, w);
   float sw[SUMS == 1 ? 8 * C : 1], sb[SUMS == 1 ? 8 * C : 1];
   if (SUMS == 1)
@@ -225,46 +463,38 @@ __global__ void __launch_bounds__(block_threads<T>()) norm_bwd_kernel(const Norm
       const int k = column<T, VEC>(t, i / 8, i % 8);
       if (k < n) sums[k] = sums[n + k] = 0.f;
     }
-  const int64_t step = int64_t(gridDim.x) * rows_at_once<T>();
-  for (int64_t base = int64_t(blockIdx.x) * rows_at_once<T>(); base < a.rows; base += step) {
-    const int64_t row = base + threadIdx.x / T;
-    const int here = row < a.rows ? n : 0;
+  for (; at.more(); at.row += at.step) {
+    const bool here = at.here();
     float h[8 * C], g[8 * C], s[2] = {0.f, 0.f};
-    load_row<T, C, VEC>(a.dy.p, a.dy.dt, row * a.dy.stride, t, here, g);
-    load_row<T, C, VEC>(a.x.p, a.x.dt, row * a.x.stride, t, here, h);
-    if (a.r.p) {
-      float r[8 * C];
-      load_row<T, C, VEC>(a.r.p, a.r.dt, row * a.r.stride, t, here, r);
-#pragma unroll
-      for (int i = 0; i < 8 * C; ++i) h[i] += r[i];
-    }
+    const float2 st = here ? *reinterpret_cast<const float2*>(a.stats + 2 * int64_t(at.row)) : make_float2(0.f, 0.f);
+    at.take(a, h, g);
     if (!keep_parameters<T, C>()) load_factors<T, C, VEC>(a, t, n, w);
-    const float2 st = here ? *reinterpret_cast<const float2*>(a.stats + 2 * row) : make_float2(0.f, 0.f);
+    float2 g2 = both(0.f), x2 = both(0.f);
 #pragma unroll
-    for (int i = 0; i < 8 * C; ++i) {
-      h[i] = (h[i] - st.x) * st.y;  // xh; behind the row's end g is 0, which keeps it out of both sums
-      const int k = column<T, VEC>(t, i / 8, i % 8);
-      if (k >= here) h[i] = 0.f;
+    for (int i = 0; i < P; ++i) {
+      // xh; behind the row's end dy is 0, which keeps it out of all sums
+      const float2 xh = __fmul2_rn(__fadd2_rn(pair(h, i), both(-st.x)), both(st.y)), d = pair(g, i);
+      unpair(h, i, xh);
       if (SUMS == 1) {
-        sw[i] = fmaf(g[i], h[i], sw[i]);
-        sb[i] += g[i];
-      } else if (SUMS == 2) {
-        if (k < n) {
-          sums[k] = fmaf(g[i], h[i], sums[k]);
-          sums[n + k] += g[i];
-        }
+        unpair(sw, SUMS == 1 ? i : 0, __ffma2_rn(d, xh, pair(sw, SUMS == 1 ? i : 0)));
+        unpair(sb, SUMS == 1 ? i : 0, __fadd2_rn(pair(sb, SUMS == 1 ? i : 0), d));
       }
-      g[i] *= w[i];
-      s[0] += g[i];
-      s[1] = fmaf(g[i], h[i], s[1]);
+      const float2 gw = __fmul2_rn(d, pair(w, i));
+      if (SUMS == 2) add_to_sums<T, C, VEC>(sums, n, t, i, __fmul2_rn(d, xh), d);
+      unpair(g, i, gw);
+      g2 = __fadd2_rn(g2, gw);
+      x2 = __ffma2_rn(gw, xh, x2);
     }
+    s[0] = g2.x + g2.y;
+    s[1] = x2.x + x2.y;
     row_sum<T>(s, red, turn);
     if (here) {
-      const float mg = s[0] * inv_n, mx = s[1] * inv_n;
+      const float2 mg = both(-s[0] * inv_n * st.y), mx = both(-s[1] * inv_n * st.y), rs = both(st.y);
 #pragma unroll
-      for (int i = 0; i < 8 * C; ++i) g[i] = st.y * (g[i] - fmaf(h[i], mx, mg));
-      if (a.dx) store_row<T, C, VEC>(a.dx, a.x.dt, row * n, t, n, g);
-      if (a.dr) store_row<T, C, VEC>(a.dr, a.r.dt, row * n, t, n, g);
+      for (int i = 0; i < P; ++i)
+        unpair(g, i, __ffma2_rn(pair(g, i), rs, __ffma2_rn(pair(h, i), mx, mg)));
+      if (a.dx) store_row<T, C, VEC>(a.dx, a.x.dt, int64_t(at.row) * n, t, n, g);
+      if (a.dr) store_row<T, C, VEC>(a.dr, a.r.dt, int64_t(at.row) * n, t, n, g);
     }
   }
   if (SUMS == 0) return;
@@ -297,6 +527,7 @@ __global__ void __launch_bounds__(block_threads<T>()) norm_bwd_kernel(const Norm
         sb[i] += __shfl_xor_sync(0xFFFFFFFFu, sb[i], o);
       }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();  // the ring is read out (no copy is in flight: the last rows' were waited for)
     if (lane < T)
 #pragma unroll
       for (int i = 0; i < 8 * C; ++i) {
@@ -315,21 +546,35 @@ __global__ void __launch_bounds__(block_threads<T>()) norm_bwd_kernel(const Norm
   }
 }
 
-__global__ void __launch_bounds__(1024) join_columns_kernel(const float* __restrict__ partial, int G, int64_t pitch,
-                                                            int64_t n, void* dst, sa_dtype dt) {
+// Column sums of one or two sets of partial rows (the first takes `blocks0` blocks).
+__global__ void __launch_bounds__(1024)
+    join_columns_kernel(const float* __restrict__ p0, int G, int64_t pitch, int64_t n0, void* d0,
+                        const float* __restrict__ p1, int64_t n1, void* d1, unsigned blocks0, sa_dtype dt) {
   // 32 columns a block, 32 threads a column that take every 32nd partial row, then their sums in order
   __shared__ float part[32][33];
   const int lane = threadIdx.x & 31, part_id = threadIdx.x >> 5;
-  const int64_t c = int64_t(blockIdx.x) * 32 + lane;
+  const bool second = blockIdx.x >= blocks0;
+  const float* partial = second ? p1 : p0;
+  const int64_t n = second ? n1 : n0, c = int64_t(blockIdx.x - (second ? blocks0 : 0)) * 32 + lane;
   float s = 0.f;
-  if (c < n)
-    for (int g = part_id; g < G; g += 32) s += partial[int64_t(g) * pitch + c];
+  if (c < n) {
+    int g = part_id;
+    for (; g + 96 < G; g += 128) {  // four rows in flight
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = partial[int64_t(g + 32 * i) * pitch + c];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s += v[i];
+    }
+    for (; g < G; g += 32) s += partial[int64_t(g) * pitch + c];
+  }
   part[part_id][lane] = s;
   __syncthreads();
   if (part_id == 0 && c < n) {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) sum += part[i][lane];
+    void* dst = second ? d1 : d0;
     if (dt == SA_BF16)
       static_cast<__nv_bfloat16*>(dst)[c] = __float2bfloat16_rn(sum);
     else
@@ -349,86 +594,130 @@ bool vec_ok(const NormArgs& a) {
          aligned_base(a.b) && aligned_base(a.y) && aligned_base(a.dx) && aligned_base(a.dr);
 }
 
-// Calls f with the layout for n features: (threads a row, chunks of 8 a thread, where the sums are).
+// Calls f with the layout for n features: (threads a row, chunks of 8 a thread).  Two chunks halve what a thread spends on
+// a row's sums; unaligned rows, whose next elements wait in registers, have one.
 template <class F>
-auto with_layout(int n, F f) {
+auto with_layout(int n, bool vec, F f) {
   using std::integral_constant;
-#define SA_LAYOUT(T, C, S) f(integral_constant<int, T>{}, integral_constant<int, C>{}, integral_constant<int, S>{})
-  if (n <= 64) return SA_LAYOUT(8, 1, 1);
-  if (n <= 128) return SA_LAYOUT(16, 1, 1);
-  if (n <= 256) return SA_LAYOUT(32, 1, 1);
-  if (n <= 512) return SA_LAYOUT(32, 2, 1);
-  if (n <= 1024) return SA_LAYOUT(128, 1, 1);
-  if (n <= 2048) return SA_LAYOUT(256, 1, 1);
-  if (n <= 4096) return SA_LAYOUT(512, 1, 1);
-  if (n <= 8192) return SA_LAYOUT(1024, 1, 2);
-  return SA_LAYOUT(1024, 2, 2);
+#define SA_LAYOUT(T, C, V) f(integral_constant<int, T>{}, integral_constant<int, C>{}, integral_constant<bool, V>{})
+  if (vec) {
+    if (n <= 64) return SA_LAYOUT(4, 2, true);
+    if (n <= 128) return SA_LAYOUT(8, 2, true);
+    if (n <= 256) return SA_LAYOUT(16, 2, true);
+    if (n <= 512) return SA_LAYOUT(32, 2, true);
+    if (n <= 1024) return SA_LAYOUT(64, 2, true);
+    if (n <= 2048) return SA_LAYOUT(128, 2, true);
+    if (n <= 4096) return SA_LAYOUT(256, 2, true);
+    if (n <= 8192) return SA_LAYOUT(512, 2, true);
+    return SA_LAYOUT(1024, 2, true);
+  }
+  if (n <= 64) return SA_LAYOUT(8, 1, false);
+  if (n <= 128) return SA_LAYOUT(16, 1, false);
+  if (n <= 256) return SA_LAYOUT(32, 1, false);
+  if (n <= 512) return SA_LAYOUT(64, 1, false);
+  if (n <= 1024) return SA_LAYOUT(128, 1, false);
+  if (n <= 2048) return SA_LAYOUT(256, 1, false);
+  if (n <= 4096) return SA_LAYOUT(512, 1, false);
+  if (n <= 8192) return SA_LAYOUT(1024, 1, false);
+  return SA_LAYOUT(1024, 2, false);
 #undef SA_LAYOUT
 }
 
 template <int T>
 int64_t blocks_for(int64_t rows) { return (rows + rows_at_once<T>() - 1) / rows_at_once<T>(); }
 
+// A walk's grid and the bytes of a block's ring: the blocks that are resident together, fewer where their rings need the
+// room (an SM has 227 KB, of which a little is left to the sums' exchange).
+struct Walkers {
+  int blocks;
+  size_t ring;
+};
+template <int T, int C, bool VEC, bool NEXT, bool GRAD>
+Walkers walkers(const NormArgs& a) {
+  Walkers w{blocks_at_once<T, C, VEC, GRAD>(), 0};
+  if (VEC && NEXT) {
+    auto pieces_of = [](const Mat& m) { return !m.p ? 0 : m.dt == SA_BF16 ? 1 : 2; };
+    w.ring = size_t(ring_rows<T>()) * C * (pieces_of(a.x) + pieces_of(a.r) + (GRAD ? pieces_of(a.dy) : 0)) * block_threads<T>() * 16;
+    const int fit = int(size_t(220 * 1024) / (w.ring + 2048));
+    if (w.blocks > fit) w.blocks = fit;
+  }
+  const int64_t most = int64_t(sm_count()) * w.blocks, need = blocks_for<T>(a.rows);
+  w.blocks = int(need < most ? need : most);
+  return w;
+}
+
+template <class K>
+cudaError_t launch_walk(K kernel, const Walkers& w, int threads, size_t smem, const NormArgs& a, cudaStream_t st) {
+  if (smem > 40 * 1024) {  // with the sums' exchange above what a launch may take unasked
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<w.blocks, threads, smem, st>>>(a);
+  return cudaGetLastError();
+}
+
 }  // namespace
 
 cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t st) {
-  const bool vec = vec_ok(a);
-  return with_layout(a.n, [&](auto T, auto C, auto) {
-    constexpr int threads = block_threads<T()>();
-    const int64_t most = int64_t(sm_count()) * (2048 / threads);
-    const int64_t need = blocks_for<T()>(a.rows);
-    const unsigned grid = unsigned(need < most ? need : most);
-    if (vec)
-      norm_fwd_kernel<T(), C(), true><<<grid, threads, 0, st>>>(a);
-    else
-      norm_fwd_kernel<T(), C(), false><<<grid, threads, 0, st>>>(a);
-    return cudaGetLastError();
+  return with_layout(a.n, vec_ok(a), [&](auto T, auto C, auto V) {
+    constexpr bool NEXT = T() < 1024 || V();
+    const Walkers w = walkers<T(), C(), V(), NEXT, false>(a);
+    if (T() == 1024 && (!NEXT || w.blocks == 0)) {  // no room for two rows
+      const Walkers plain = walkers<T(), C(), V(), false, false>(a);
+      return launch_walk(norm_fwd_kernel<T(), C(), V(), false>, plain, block_threads<T()>(), 0, a, st);
+    }
+    return launch_walk(norm_fwd_kernel<T(), C(), V(), NEXT>, w, block_threads<T()>(), w.ring, a, st);
   });
 }
 
 int norm_bwd_blocks(int64_t rows, int n) {
-  return with_layout(n, [&](auto T, auto, auto) {
-    const int64_t most = int64_t(sm_count()) * (1024 / block_threads<T()>());
-    const int64_t need = blocks_for<T()>(rows);
-    return int(need < most ? need : most);
-  });
+  int most = 0;
+  for (const bool vec : {false, true}) {
+    const int g = with_layout(n, vec, [&](auto T, auto C, auto V) {
+      const int64_t all = int64_t(sm_count()) * blocks_at_once<T(), C(), V(), true>(), need = blocks_for<T()>(rows);
+      return int(need < all ? need : all);
+    });
+    most = g > most ? g : most;
+  }
+  return most;
 }
 
 cudaError_t launch_norm_bwd(const NormArgs& a, cudaStream_t st, int* launches) {
-  const bool vec = vec_ok(a);
-  const int G = norm_bwd_blocks(a.rows, a.n);
+  int G = 0;
   cudaError_t e = cudaSuccess;
-  if (G > 0)
-    e = with_layout(a.n, [&](auto T, auto C, auto S) {
-      auto go = [&](auto kernel, size_t smem) {
-        if (smem > 48 * 1024) {
-          const cudaError_t s = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-          if (s != cudaSuccess) return s;
-        }
-        kernel<<<G, block_threads<T()>(), smem, st>>>(a);
-        ++*launches;
-        return cudaGetLastError();
-      };
-      if (!a.partial) return vec ? go(norm_bwd_kernel<T(), C(), true, 0>, 0) : go(norm_bwd_kernel<T(), C(), false, 0>, 0);
-      const size_t smem = S() == 2 ? size_t(2) * a.n * 4 : T() <= 32 ? size_t(kThreads / 32) * 2 * 8 * C() * T() * 4 : 0;
-      return vec ? go(norm_bwd_kernel<T(), C(), true, S()>, smem) : go(norm_bwd_kernel<T(), C(), false, S()>, smem);
+  if (a.rows > 0)
+    e = with_layout(a.n, vec_ok(a), [&](auto T, auto C, auto V) {
+      constexpr bool NEXT = T() < 1024;
+      constexpr int threads = block_threads<T()>();
+      const Walkers w = walkers<T(), C(), V(), NEXT, true>(a);
+      G = w.blocks;
+      ++*launches;
+      if (!a.partial) return launch_walk(norm_bwd_kernel<T(), C(), V(), NEXT, 0>, w, threads, w.ring, a, st);
+      constexpr int SUMS = T() == 1024 ? 2 : 1;
+      const size_t sums = SUMS == 2 ? size_t(2) * a.n * 4 : T() <= 32 ? size_t(kThreads / 32) * 2 * 8 * C() * T() * 4 : 0;
+      return launch_walk(norm_bwd_kernel<T(), C(), V(), NEXT, SUMS>, w, threads, sums > w.ring ? sums : w.ring, a, st);
     });
   if (e != cudaSuccess) return e;
-  if (a.dw) {
-    e = launch_join_columns(a.partial, G, 2 * int64_t(a.n), a.n, a.dw, a.w_dt, st);
-    ++*launches;
-  }
-  if (e == cudaSuccess && a.db) {
-    e = launch_join_columns(a.partial + a.n, G, 2 * int64_t(a.n), a.n, a.db, a.w_dt, st);
+  if (a.dw || a.db) {
+    e = launch_join_columns2(a.partial, G, 2 * int64_t(a.n), a.n, a.dw, a.partial + a.n, a.n, a.db, a.w_dt, st);
     ++*launches;
   }
   return e;
 }
 
+cudaError_t launch_join_columns2(const float* p0, int G, int64_t pitch, int64_t n0, void* d0, const float* p1, int64_t n1,
+                                 void* d1, sa_dtype dt, cudaStream_t st) {
+  if (!d0) n0 = 0;
+  if (!d1) n1 = 0;
+  const unsigned b0 = unsigned((n0 + 31) / 32), b1 = unsigned((n1 + 31) / 32);
+  if (b0 + b1 == 0) return cudaSuccess;
+  join_columns_kernel<<<b0 + b1, 1024, 0, st>>>(p0, G, pitch, n0, d0, p1, n1, d1, b0, dt);
+  return cudaGetLastError();
+}
+
 cudaError_t launch_join_columns(const float* partial, int G, int64_t pitch, int64_t n, void* dst, sa_dtype dt,
                                 cudaStream_t st) {
-  join_columns_kernel<<<unsigned((n + 31) / 32), 1024, 0, st>>>(partial, G, pitch, n, dst, dt);
-  return cudaGetLastError();
+  return launch_join_columns2(partial, G, pitch, n, dst, nullptr, 0, nullptr, dt, st);
 }
 
 }  // namespace dense

@@ -212,15 +212,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       for (int kb = seg.k0; ok && kb < seg.k1;) {
         const int end = F32 ? kb + 1 : seg.k1;
         const uint32_t set = g & 1u, d = tmem + set * C::BN;
-        ok = CTAS == 2 ? mbar_wait_cluster(acc_empty(set), ((g >> 1) & 1u) ^ 1u, abort_flag, a.ws, 0x402)
-                       : mbar_wait(acc_empty(set), ((g >> 1) & 1u) ^ 1u, abort_flag, a.ws, 0x402);
+        ok = mbar_wait(acc_empty(set), ((g >> 1) & 1u) ^ 1u, abort_flag, a.ws, 0x402);
         if (!ok) break;
         tc_fence_after();
         uint32_t accumulate = 0;
         for (; kb < end; ++kb, ++n) {
           const uint32_t s = n % C::STAGES;
-          ok = CTAS == 2 ? mbar_wait_cluster(full(s), (n / C::STAGES) & 1u, abort_flag, a.ws, 0x403)
-                         : mbar_wait(full(s), (n / C::STAGES) & 1u, abort_flag, a.ws, 0x403);
+          ok = mbar_wait(full(s), (n / C::STAGES) & 1u, abort_flag, a.ws, 0x403);
           if (!ok) break;
           tc_fence_after();
           const uint64_t sa = sdesc_add(d_a, s * C::STAGE), sb = sdesc_add(d_b, s * C::STAGE);
@@ -254,8 +252,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
+        // relaxed: only the accumulators' reads come before it, and a release would wait for this warp's stores
         if (CTAS == 2)
-          mbar_arrive_cluster(lead_empty + 8 * set);
+          mbar_arrive_relaxed_cluster(lead_empty + 8 * set);
         else
           mbar_arrive(acc_empty(set));
       }
