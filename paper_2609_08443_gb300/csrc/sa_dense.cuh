@@ -70,8 +70,9 @@ struct ActGradArgs {
   int64_t M;
   int N, Z;
   int act;
-  void* dz;
+  void* dz;        // type dt; fp32: as three planes of bf16 terms where `terms` is set
   int64_t pitch;
+  int terms;
   float* partial;
 };
 cudaError_t launch_act_grad(const ActGradArgs& a, cudaStream_t st);
@@ -88,7 +89,9 @@ struct TcOperand {
 struct TcPlan {
   int ctas, W;  // CTAs of a worker, workers
   int64_t mt, nt, KB, whole, cut;
+  int cutters;  // workers that share the cut tiles
   size_t piece_bytes;
+  double cost;
 };
 
 // C[m, n] = sum_k A(m, k) B(n, k) on tcgen05.  K-major operands have k along their rows (a_mn, b_mn 0).
@@ -108,10 +111,24 @@ struct TcGemm {
   int clear;
 };
 
-TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32);
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32, int sms = 0, int ctas_only = 0);
 cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches);
-// bf16 rows, or fp32 rows as three planes of bf16 terms
-cudaError_t launch_repack(const Mat& src, int64_t rows, int cols, void* dst, int64_t pitch, cudaStream_t st);
+// Plans of dx = dz W and dW = dz^T x (dz [M, Z], W [Z, K]) side by side (launch_tc_grads), where that is better than one
+// after the other at a cost of `apart`.
+bool tc_plan_grads(int64_t M, int64_t Z, int64_t K, bool f32, double apart, TcPlan* x, TcPlan* w);
+cudaError_t launch_tc_grads(const TcGemm& gx, const TcPlan& px, const TcGemm& gw, const TcPlan& pw, cudaStream_t st,
+                            int* launches);
+
+// A copy of rows in bf16 (fp32: three planes of terms), `pitch` elements apart, filled up with zeros.
+struct Repack {
+  Mat src;
+  int64_t rows;
+  int cols;
+  void* dst;  // NULL: nothing to copy
+  int64_t pitch;
+  int vec;
+};
+cudaError_t launch_repack(Repack r0, Repack r1, cudaStream_t st);
 
 int sm_count();
 

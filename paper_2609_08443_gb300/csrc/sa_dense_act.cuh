@@ -29,6 +29,24 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
   reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
+// Eight fp32 values as three terms of bf16 each, in planes `plane` elements apart: each term is what is left rounded to
+// nearest, and what is left after the third is nothing.
+__device__ __forceinline__ void store_terms(__nv_bfloat16* p, int64_t plane, const float* v) {
+  float left[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) left[j] = v[j];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    float t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      t[j] = __bfloat162float(__float2bfloat16_rn(left[j]));
+      left[j] -= t[j];
+    }
+    store8(p + k * plane, t);
+  }
+}
+
 // 1 / (1 + e^-z).  Results that end in bf16 take the hardware's approximations of 2^x and 1/x (a few
 // 2^-23); fp32 results the full-precision functions.
 template <bool FULL>

@@ -75,6 +75,8 @@ enum { COPY_X = 1, COPY_W = 2, COPY_DY = 4 };
 // one product at a time) and the partial column sums.
 struct Layout {
   size_t x, w, dz, dz_terms, piece, partial, total;
+  sa::dense::TcPlan plan, dx, dw, side_dx, side_dw;  // of y; of either gradient alone; of both side by side
+  bool side;
 };
 
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
@@ -92,14 +94,20 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
   const size_t each = f32 ? 6 : 2;  // bytes of an element's terms
   s.x = section(repack & COPY_X, size_t(l.M) * pitch_of(l.K) * each);
   s.w = section(repack & COPY_W, size_t(l.Z) * pitch_of(l.K) * each);
-  size_t piece = sa::dense::tc_plan(l.M, l.N, l.K, l.act == SA_ACT_SWIGLU, f32).piece_bytes;
-  if (bwd) {
+  size_t piece = 0;
+  if (!bwd) {
+    s.plan = sa::dense::tc_plan(l.M, l.N, l.K, l.act == SA_ACT_SWIGLU, f32);
+    piece = s.plan.piece_bytes;
+  } else {
     const bool act = l.act != SA_ACT_NONE;
     s.dz = section(act, size_t(l.M) * pitch_of(l.Z) * size_of(l.dt));
     s.dz_terms = section(f32 || (!act && (repack & COPY_DY)), size_t(l.M) * pitch_of(l.Z) * each);
-    const size_t dx = sa::dense::tc_plan(l.M, l.K, l.Z, false, f32).piece_bytes;
-    const size_t dw = sa::dense::tc_plan(l.Z, l.K, l.M, false, f32).piece_bytes;
-    piece = dx > dw ? dx : dw;
+    s.dx = sa::dense::tc_plan(l.M, l.K, l.Z, false, f32);
+    s.dw = sa::dense::tc_plan(l.Z, l.K, l.M, false, f32);
+    s.side = sa::dense::tc_plan_grads(l.M, l.Z, l.K, f32, s.dx.cost + s.dw.cost, &s.side_dx, &s.side_dw);
+    piece = s.dx.piece_bytes > s.dw.piece_bytes ? s.dx.piece_bytes : s.dw.piece_bytes;
+    if (s.side && s.side_dx.piece_bytes + s.side_dw.piece_bytes > piece)
+      piece = s.side_dx.piece_bytes + s.side_dw.piece_bytes;
   }
   s.piece = section(piece > 0, piece);
   s.partial = section(bwd, size_t(sa::dense::act_grad_blocks(l.M, l.N)) * size_t(l.Z) * sizeof(float));
@@ -116,15 +124,20 @@ int repack_bits(const Mat& x, const Mat& w, const Mat& dy, const Linear& l) {
   return (need(x, l.K) ? COPY_X : 0) | (need(w, l.K) ? COPY_W : 0) | (dy.p && need(dy, l.N) ? COPY_DY : 0);
 }
 
-// A product's operand: the rows as they are, or their copy (made here) at `at`.
-cudaError_t operand(const Mat& m, int64_t rows, int64_t cols, bool copy, void* at, cudaStream_t st, int* launches,
-                    sa::dense::TcOperand* o) {
-  *o = sa::dense::TcOperand{m.p, rows, cols, m.stride};
-  if (!copy && m.dt == SA_BF16) return cudaSuccess;
-  o->p = at;
-  o->pitch = pitch_of(cols);
+// A product's operand: the rows as they are, or their copy at `at`, which is made by the launch of `r`.
+sa::dense::TcOperand operand(const Mat& m, int64_t rows, int64_t cols, bool copy, void* at, sa::dense::Repack* r) {
+  sa::dense::TcOperand o{m.p, rows, cols, m.stride};
+  if (!copy && m.dt == SA_BF16) return o;
+  o.p = at;
+  o.pitch = pitch_of(cols);
+  *r = sa::dense::Repack{m, rows, int(cols), at, o.pitch, 0};
+  return o;
+}
+
+cudaError_t repack(const sa::dense::Repack& r0, const sa::dense::Repack& r1, cudaStream_t st, int* launches) {
+  if (!r0.dst && !r1.dst) return cudaSuccess;
   ++*launches;
-  return sa::dense::launch_repack(m, rows, int(cols), at, o->pitch, st);
+  return sa::dense::launch_repack(r0, r1, st);
 }
 
 }  // namespace
@@ -242,8 +255,10 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* w, int64_t 
   }
   int launches = 0;
   sa::dense::TcGemm g{};
-  cudaError_t e = operand(mx, M, K, copies & COPY_X, base + lay.x, st, &launches, &g.A);
-  if (e == cudaSuccess) e = operand(mw, l.Z, K, copies & COPY_W, base + lay.w, st, &launches, &g.B);
+  sa::dense::Repack rx{}, rw{};
+  g.A = operand(mx, M, K, copies & COPY_X, base + lay.x, &rx);
+  g.B = operand(mw, l.Z, K, copies & COPY_W, base + lay.w, &rw);
+  cudaError_t e = repack(rx, rw, st, &launches);
   g.M = M;
   g.N = N;
   g.bias = b;
@@ -256,7 +271,7 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* w, int64_t 
   g.ws = workspace;
   g.clear = 1;
   if (e == cudaSuccess)
-    e = sa::dense::launch_tc_gemm(g, sa::dense::tc_plan(M, N, K, act == SA_ACT_SWIGLU, dt == SA_F32), st, &launches);
+    e = sa::dense::launch_tc_gemm(g, lay.plan, st, &launches);
   sa::count_launches(launches);
   return status(e);
 }
@@ -289,7 +304,9 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
   a.N = N;
   a.Z = l.Z;
   a.act = act;
-  a.dz = act == SA_ACT_NONE || (!dx && !dw) ? nullptr : base + lay.dz;
+  const bool terms = tc && dt == SA_F32;  // dz goes straight into the products' terms
+  a.dz = act == SA_ACT_NONE || (!dx && !dw) ? nullptr : base + (terms ? lay.dz_terms : lay.dz);
+  a.terms = terms;
   a.pitch = pitch_of(l.Z);
   a.partial = db ? reinterpret_cast<float*>(base + lay.partial) : nullptr;
   int launches = 0;
@@ -304,34 +321,35 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
   }
   const Mat dz = a.dz ? Mat{a.dz, a.pitch, dt} : mdy;
   if (tc) {
-    sa::dense::TcOperand oz{}, ox{}, ow{};
-    if (e == cudaSuccess)
-      e = operand(dz, M, l.Z, !a.dz && (copies & COPY_DY), base + lay.dz_terms, st, &launches, &oz);
-    sa::dense::TcGemm g{};
-    g.dt = dt;
-    g.piece = reinterpret_cast<float*>(base + lay.piece);
-    g.ws = workspace;
-    g.clear = 1;
-    if (dx) {  // dx = dz W
-      if (e == cudaSuccess) e = operand(mw, l.Z, K, copies & COPY_W, base + lay.w, st, &launches, &ow);
-      g.A = oz;
-      g.B = ow;
-      g.b_mn = 1;
-      g.M = M;
-      g.N = K;
-      g.y = dx;
-      if (e == cudaSuccess) e = sa::dense::launch_tc_gemm(g, sa::dense::tc_plan(M, K, l.Z, false, dt == SA_F32), st, &launches);
-      g.clear = 0;
-    }
-    if (dw) {  // dW = dz^T x
-      if (e == cudaSuccess) e = operand(mx, M, K, copies & COPY_X, base + lay.x, st, &launches, &ox);
-      g.A = oz;
-      g.B = ox;
-      g.a_mn = g.b_mn = 1;
-      g.M = l.Z;
-      g.N = K;
-      g.y = dw;
-      if (e == cudaSuccess) e = sa::dense::launch_tc_gemm(g, sa::dense::tc_plan(l.Z, K, M, false, dt == SA_F32), st, &launches);
+    sa::dense::Repack rz{}, rx{}, rw{};
+    sa::dense::TcOperand oz{a.dz, M, l.Z, a.pitch};
+    if (!a.dz) oz = operand(dz, M, l.Z, copies & COPY_DY, base + lay.dz_terms, &rz);
+    const sa::dense::TcOperand ox = dw ? operand(mx, M, K, copies & COPY_X, base + lay.x, &rx) : sa::dense::TcOperand{};
+    const sa::dense::TcOperand ow = dx ? operand(mw, l.Z, K, copies & COPY_W, base + lay.w, &rw) : sa::dense::TcOperand{};
+    if (e == cudaSuccess) e = repack(rx, rw, st, &launches);
+    if (e == cudaSuccess) e = repack(rz, sa::dense::Repack{}, st, &launches);
+    sa::dense::TcGemm gx{}, gw{};
+    gx.dt = gw.dt = dt;
+    gx.piece = gw.piece = reinterpret_cast<float*>(base + lay.piece);
+    gx.ws = gw.ws = workspace;
+    gx.A = gw.A = oz;
+    gx.clear = 1;
+    gw.clear = !dx;
+    gx.B = ow;  // dx = dz W
+    gx.b_mn = 1;
+    gx.M = M;
+    gx.y = dx;
+    gw.B = ox;  // dW = dz^T x
+    gw.a_mn = gw.b_mn = 1;
+    gw.M = l.Z;
+    gw.y = dw;
+    gx.N = gw.N = K;
+    if (dx && dw && lay.side) {
+      gw.piece += lay.side_dx.piece_bytes / sizeof(float);
+      if (e == cudaSuccess) e = sa::dense::launch_tc_grads(gx, lay.side_dx, gw, lay.side_dw, st, &launches);
+    } else {
+      if (e == cudaSuccess && dx) e = sa::dense::launch_tc_gemm(gx, lay.dx, st, &launches);
+      if (e == cudaSuccess && dw) e = sa::dense::launch_tc_gemm(gw, lay.dw, st, &launches);
     }
   } else {
     sa::dense::GemmArgs g{};

@@ -27,7 +27,7 @@ namespace {
 constexpr int kThreads = 256;  // of a block that holds several rows at once
 // Rows of a thread's ring: the one in work and two on their way (2 to 8 measured the same; the widest rows have room for 2).
 template <int T>
-constexpr int ring_rows() { return T == 1024 ? 2 : 3; }
+constexpr int ring_rows() { return T >= 512 ? 2 : 3; }
 
 template <int T>
 constexpr int block_threads() { return T <= 32 ? kThreads : T; }
@@ -174,7 +174,7 @@ struct Walk {
   }
   // the block's rows are not all done (the same for all of its threads)
   __device__ __forceinline__ bool more() const { return row - threadIdx.x / T < rows; }
-  __device__ __forceinline__ bool here() const { return row < rows; }
+  __device__ __forceinline__ bool here() const { return T > 32 || row < rows; }
 
   template <bool ADD>
   __device__ __forceinline__ void unpack(bool half, const char* from, float* v) const {
@@ -210,15 +210,16 @@ struct Walk {
       if (sum) unpack<true>(r.half, from + off_r, h);
       if (GRAD) unpack<false>(dy.half, from + off_dy, g);
       get = get == (kRing - 1) * per_row ? 0 : get + per_row;
+      if (!in[C - 1] || !here()) {  // slots that nothing was copied to hold whatever was there
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (!in[c] || !here()) {  // the slots hold whatever was there
+        for (int c = 0; c < C; ++c)
+          if (!in[c] || !here())
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            h[8 * c + j] = 0.f;
-            if (GRAD) g[8 * c + j] = 0.f;
-          }
-        }
+            for (int j = 0; j < 8; ++j) {
+              h[8 * c + j] = 0.f;
+              if (GRAD) g[8 * c + j] = 0.f;
+            }
+      }
     } else if (NEXT) {
       convert<false>(x.half, raw[0], h);
       if (sum) convert<true>(r.half, raw[1], h);
@@ -290,6 +291,34 @@ constexpr bool keep_parameters() { return T * C < 2048; }
 template <int T, int K>
 __device__ __forceinline__ void row_sum(float (&v)[K], float* red, int& turn) {
   constexpr int lanes = T < 32 ? T : 32;
+  if constexpr (K == 2 && T > 32) {
+    // the first exchange leaves each half of the warp with one of the two sums
+    const bool high = threadIdx.x & 16;
+    float x = (high ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, high ? v[0] : v[1], 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    constexpr int W = T / 32;
+    float* s = red + turn * W * 2;
+    turn ^= 1;
+    const int lane = threadIdx.x & 31;
+    if ((lane & 15) == 0) s[(lane >> 4) * W + (threadIdx.x >> 5)] = x;
+    __syncthreads();
+    if constexpr (W <= 16) {  // likewise: the lower half of the warp adds one sum's parts, the upper the other's
+      x = (lane & 15) < W ? s[(lane >> 4) * W + (lane & 15)] : 0.f;
+#pragma unroll
+      for (int o = W / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+      v[0] = __shfl_sync(0xFFFFFFFFu, x, 0);
+      v[1] = __shfl_sync(0xFFFFFFFFu, x, 16);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        v[k] = s[k * W + lane];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int o = lanes / 2; o > 0; o >>= 1)
 #pragma unroll
@@ -348,7 +377,7 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 // Blocks an SM that the register budget is made for: 64 to 128 a thread, by what it holds.
 template <int T, int C, bool VEC, bool GRAD>
 constexpr int blocks_at_once() {
-  return T == 1024 ? 1 : (C == 2 || (GRAD && !VEC) ? 512 : GRAD || !VEC ? 768 : 1024) / block_threads<T>();
+  return T == 1024 ? 1 : (C >= 2 || (GRAD && !VEC) ? 512 : GRAD || !VEC ? 768 : 1024) / block_threads<T>();
 }
 
 template <int T, int C, bool VEC, bool NEXT>
@@ -508,6 +537,14 @@ __global__ void __launch_bounds__(block_threads<T>(), blocks_at_once<T, C, VEC, 
         out[n + k] = sums[n + k];
       }
     }
+  } else if constexpr (T > 32 && VEC) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int k = column<T, true>(t, c, 0);
+      if (k >= n) continue;
+      store8(out + k, sw + 8 * c);
+      store8(out + n + k, sb + 8 * c);
+    }
   } else if constexpr (T > 32) {
 #pragma unroll
     for (int i = 0; i < 8 * C; ++i) {
@@ -594,12 +631,21 @@ bool vec_ok(const NormArgs& a) {
          aligned_base(a.b) && aligned_base(a.y) && aligned_base(a.dx) && aligned_base(a.dr);
 }
 
-// Calls f with the layout for n features: (threads a row, chunks of 8 a thread).  Two chunks halve what a thread spends on
-// a row's sums; unaligned rows, whose next elements wait in registers, have one.
-template <class F>
-auto with_layout(int n, bool vec, F f) {
+// Calls f with the layout for n features: (threads a row, chunks of 8 a thread).  More chunks spread what a thread spends
+// on a row's sums over more elements: two (8192 x 4096 in bf16, forward and gradient 30 and 46 us; one chunk 37 and 58),
+// four in the forward of wide rows that are read in bf16 alone (26 us; but 62 with fp32 rows and a residual, for 43
+// with two).  Unaligned rows, whose next elements wait in registers, have one.
+template <bool GRAD, class F>
+auto with_layout(int n, bool vec, bool narrow, F f) {
   using std::integral_constant;
 #define SA_LAYOUT(T, C, V) f(integral_constant<int, T>{}, integral_constant<int, C>{}, integral_constant<bool, V>{})
+  if (vec && !GRAD && narrow && n > 512) {
+    if (n <= 1024) return SA_LAYOUT(32, 4, true);
+    if (n <= 2048) return SA_LAYOUT(64, 4, true);
+    if (n <= 4096) return SA_LAYOUT(128, 4, true);
+    if (n <= 8192) return SA_LAYOUT(256, 4, true);
+    return SA_LAYOUT(512, 4, true);
+  }
   if (vec) {
     if (n <= 64) return SA_LAYOUT(4, 2, true);
     if (n <= 128) return SA_LAYOUT(8, 2, true);
@@ -659,10 +705,11 @@ cudaError_t launch_walk(K kernel, const Walkers& w, int threads, size_t smem, co
 }  // namespace
 
 cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t st) {
-  return with_layout(a.n, vec_ok(a), [&](auto T, auto C, auto V) {
+  const bool narrow = a.x.dt == SA_BF16 && (!a.r.p || a.r.dt == SA_BF16);
+  return with_layout<false>(a.n, vec_ok(a), narrow, [&](auto T, auto C, auto V) {
     constexpr bool NEXT = T() < 1024 || V();
     const Walkers w = walkers<T(), C(), V(), NEXT, false>(a);
-    if (T() == 1024 && (!NEXT || w.blocks == 0)) {  // no room for two rows
+    if (T() >= 512 && (!NEXT || w.blocks == 0)) {  // no room for two rows
       const Walkers plain = walkers<T(), C(), V(), false, false>(a);
       return launch_walk(norm_fwd_kernel<T(), C(), V(), false>, plain, block_threads<T()>(), 0, a, st);
     }
@@ -673,7 +720,7 @@ cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t st) {
 int norm_bwd_blocks(int64_t rows, int n) {
   int most = 0;
   for (const bool vec : {false, true}) {
-    const int g = with_layout(n, vec, [&](auto T, auto C, auto V) {
+    const int g = with_layout<true>(n, vec, false, [&](auto T, auto C, auto V) {
       const int64_t all = int64_t(sm_count()) * blocks_at_once<T(), C(), V(), true>(), need = blocks_for<T()>(rows);
       return int(need < all ? need : all);
     });
@@ -686,7 +733,7 @@ cudaError_t launch_norm_bwd(const NormArgs& a, cudaStream_t st, int* launches) {
   int G = 0;
   cudaError_t e = cudaSuccess;
   if (a.rows > 0)
-    e = with_layout(a.n, vec_ok(a), [&](auto T, auto C, auto V) {
+    e = with_layout<true>(a.n, vec_ok(a), false, [&](auto T, auto C, auto V) {
       constexpr bool NEXT = T() < 1024;
       constexpr int threads = block_threads<T()>();
       const Walkers w = walkers<T(), C(), V(), NEXT, true>(a);

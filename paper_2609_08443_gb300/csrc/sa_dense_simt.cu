@@ -85,72 +85,103 @@ __global__ void __launch_bounds__(256) simt_gemm_kernel(const GemmArgs g) {
 
 // Columns are spread over 32 lanes x 8 (fewer lanes where there are fewer columns, and the rest of the
 // warp takes other rows); a block's eight warps and its share of the rows leave one partial row of sums.
-constexpr int kRowsPerWarpLoop = 4;
 
 template <typename T, bool VEC, bool GATED>
 __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradArgs a, int lanes) {
   constexpr int S = GATED ? 2 : 1;
   constexpr bool FULL = sizeof(T) == 4;
+  constexpr int R = VEC && !FULL ? 2 : 1;  // rows that a thread has in flight
   __shared__ float part[8][S][256];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t = lane % lanes, per_warp = 32 / lanes;
   const int c0 = blockIdx.x * 256;
   const T* dy = static_cast<const T*>(a.dy.p);
   const T* z = static_cast<const T*>(a.z);
-  T* dz = static_cast<T*>(a.dz);
   float sum[S][8] = {};
   const int64_t step = int64_t(gridDim.y) * 8 * per_warp;
   auto col = [&](int j) { return c0 + (VEC ? t * 8 + j : j * lanes + t); };
-  for (int64_t row = (int64_t(blockIdx.y) * 8 + warp) * per_warp + lane / lanes; row < a.M; row += step) {
-    float g[8], zz[S][8];
-    if (VEC) {
-      if (col(0) < a.N) {
-        load8(dy + row * a.dy.stride + col(0), g);
-        if (a.act != SA_ACT_NONE)
+  for (int64_t row0 = (int64_t(blockIdx.y) * 8 + warp) * per_warp + lane / lanes; row0 < a.M; row0 += R * step) {
+    float g[R][8], zz[R][S][8];
 #pragma unroll
-          for (int s = 0; s < S; ++s) load8(z + row * a.Z + s * a.N + col(0), zz[s]);
+    for (int i = 0; i < R; ++i) {
+      const int64_t row = row0 + i * step;
+      const bool here = row < a.M;
+      if (VEC) {
+        if (here && col(0) < a.N) {
+          load8(dy + row * a.dy.stride + col(0), g[i]);
+          if (a.act != SA_ACT_NONE)
+#pragma unroll
+            for (int s = 0; s < S; ++s) load8(z + row * a.Z + s * a.N + col(0), zz[i][s]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            g[i][j] = 0.f;
+#pragma unroll
+            for (int s = 0; s < S; ++s) zz[i][s][j] = 0.f;
+          }
+        }
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          g[j] = 0.f;
+          const bool in = here && col(j) < a.N;
+          g[i][j] = in ? ld_f32(dy + row * a.dy.stride + col(j)) : 0.f;
 #pragma unroll
-          for (int s = 0; s < S; ++s) zz[s][j] = 0.f;
+          for (int s = 0; s < S; ++s)
+            zz[i][s][j] = in && a.act != SA_ACT_NONE ? ld_f32(z + row * a.Z + int64_t(s) * a.N + col(j)) : 0.f;
         }
       }
-    } else {
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int64_t row = row0 + i * step;
+      if (R > 1 && row >= a.M) break;
+      float d[S][8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const bool in = col(j) < a.N;
-        g[j] = in ? ld_f32(dy + row * a.dy.stride + col(j)) : 0.f;
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-          zz[s][j] = in && a.act != SA_ACT_NONE ? ld_f32(z + row * a.Z + int64_t(s) * a.N + col(j)) : 0.f;
+        if (GATED) {
+          const float p = sigmoid<FULL>(zz[i][0][j]);
+          d[0][j] = g[i][j] * zz[i][S - 1][j] * (p * fmaf(zz[i][0][j], 1.f - p, 1.f));
+          d[S - 1][j] = g[i][j] * (zz[i][0][j] * p);
+        } else {
+          d[0][j] = a.act == SA_ACT_NONE   ? g[i][j]
+                    : a.act == SA_ACT_RELU ? (zz[i][0][j] > 0.f ? g[i][j] : 0.f)
+                                           : g[i][j] * slope<FULL>(a.act, zz[i][0][j]);
+        }
       }
-    }
-    float d[S][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (GATED) {
-        const float p = sigmoid<FULL>(zz[0][j]);
-        d[0][j] = g[j] * zz[S - 1][j] * (p * fmaf(zz[0][j], 1.f - p, 1.f));
-        d[S - 1][j] = g[j] * (zz[0][j] * p);
-      } else {
-        d[0][j] = a.act == SA_ACT_NONE ? g[j] : a.act == SA_ACT_RELU ? (zz[0][j] > 0.f ? g[j] : 0.f)
-                                                                     : g[j] * slope<FULL>(a.act, zz[0][j]);
-      }
-    }
+      for (int s = 0; s < S; ++s) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
+        for (int j = 0; j < 8; ++j) sum[s][j] += d[s][j];
+        if (!a.dz) continue;
+        const int64_t at = row * a.pitch + int64_t(s) * a.N;
+        if (a.terms) {
+          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.dz) + at;
+          const int64_t plane = a.M * a.pitch;
+          if (VEC) {
+            if (col(0) < a.N) store_terms(o + col(0), plane, d[s]);
+          } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[s][j] += d[s][j];
-      if (!dz) continue;
-      T* o = dz + row * a.pitch + int64_t(s) * a.N;
-      if (VEC) {
-        if (col(0) < a.N) store8(o + col(0), d[s]);
-      } else {
+            for (int j = 0; j < 8; ++j)
+              if (col(j) < a.N) {
+                float left = d[s][j];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (col(j) < a.N) st_from_f32(o + col(j), d[s][j]);
+                for (int k = 0; k < 3; ++k) {
+                  const __nv_bfloat16 term = __float2bfloat16_rn(left);
+                  o[k * plane + col(j)] = term;
+                  left -= __bfloat162float(term);
+                }
+              }
+          }
+        } else {
+          T* o = static_cast<T*>(a.dz) + at;
+          if (VEC) {
+            if (col(0) < a.N) store8(o + col(0), d[s]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (col(j) < a.N) st_from_f32(o + col(j), d[s][j]);
+          }
+        }
       }
     }
   }
@@ -190,7 +221,7 @@ int lanes_for(int N) {
 int act_grad_blocks(int64_t M, int N) {
   const int strips = (N + 255) / 256, rows = 8 * (32 / lanes_for(N));
   const int64_t most = (int64_t(sm_count()) * 8 + strips - 1) / strips;
-  const int64_t need = (M + int64_t(rows) * kRowsPerWarpLoop - 1) / (int64_t(rows) * kRowsPerWarpLoop);
+  const int64_t need = (M + rows - 1) / rows;
   const int64_t g = need < most ? need : most;
   return int(g < 65535 ? g : 65535);
 }

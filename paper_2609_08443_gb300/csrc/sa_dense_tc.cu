@@ -99,11 +99,11 @@ __device__ __forceinline__ void tc_load(uint32_t dst, const void* map, uint32_t 
         : "memory");
 }
 
-// Maps: K-major operands [planes][rows][k], boxes of 64 x (A: 128, B: 64) rows; MN-major ones [planes][k][mn],
-// boxes of 64 x 64.
+// The work of one CTA.  Maps: K-major operands [planes][rows][k], boxes of 64 x (A: 128, B: 64) rows; MN-major ones
+// [planes][k][mn], boxes of 64 x 64.
 template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
-__global__ void __launch_bounds__(kTcThreads, 1)
-    tc_linear_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const TcArgs a) {
+__device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUtensorMap& tb, const TcArgs& a,
+                                               const int worker, const bool clear) {
   using C = TcCfg<CTAS, F32>;
   using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
   using Shape = TileShape<CTAS>;
@@ -112,7 +112,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const uint32_t base = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CTAS == 2 ? cluster_rank() : 0;
-  const int worker = int(blockIdx.x) / CTAS;
 
   auto full = [&](int s) { return base + C::OFF_BAR + 8 * s; };
   auto empty = [&](int s) { return base + C::OFF_BAR + 64 + 8 * s; };
@@ -123,7 +122,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 176);  // three words
 
   if (threadIdx.x == 0) {
-    if (a.clear && blockIdx.x == 0) {
+    if (clear) {
       ws_header(a.ws)->err = 0;
       ws_header(a.ws)->timeout_site = 0;
     }
@@ -285,7 +284,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       float* piece = nullptr;
       if (!complete) {
         const int64_t total = a.cut * a.KB, first = (seg.tile - a.whole) * a.KB;
-        const int slot = partial_slot(total, a.W, worker, first);
+        const int slot = partial_slot(total, a.cutters, worker, first);
         piece = a.piece + (int64_t(worker * 2 + slot) * CTAS + rank) * (128 * C::BN) + (q * 32 + lane) * 4;
       }
       auto col = [&](int i, int half) {  // accumulator column of chunk i (SwiGLU: of either half)
@@ -378,9 +377,29 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (CTAS == 2) cluster_sync_all();
 }
 
+template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    tc_linear_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const TcArgs a) {
+  tc_linear_work<CTAS, A_MN, B_MN, F32, EPI>(ta, tb, a, int(blockIdx.x) / CTAS, a.clear && blockIdx.x == 0);
+}
+
+// dx and dW side by side, for gradients that would leave most of the GPU idle one after the other: the first
+// x.W CTAs (or pairs) make dx.
+template <int CTAS, bool F32>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    tc_linear_grads_kernel(const __grid_constant__ CUtensorMap xa, const __grid_constant__ CUtensorMap xb,
+                           const __grid_constant__ CUtensorMap wa, const __grid_constant__ CUtensorMap wb, const TcArgs x,
+                           const TcArgs w) {
+  const int worker = int(blockIdx.x) / CTAS;
+  if (worker < x.W)
+    tc_linear_work<CTAS, false, true, F32, EPI_PLAIN>(xa, xb, x, worker, blockIdx.x == 0);
+  else
+    tc_linear_work<CTAS, true, true, F32, EPI_PLAIN>(wa, wb, w, worker - x.W, false);
+}
+
 // Cut tiles: one block for 32 columns of each epilogue warp's rows; pieces are added in worker order.
 template <int CTAS, bool F32, int EPI>
-__global__ void __launch_bounds__(256) tc_join_kernel(const TcArgs a) {
+__device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   using C = TcCfg<CTAS, F32>;
   using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
   using Shape = TileShape<CTAS>;
@@ -388,10 +407,10 @@ __global__ void __launch_bounds__(256) tc_join_kernel(const TcArgs a) {
   __shared__ __align__(128) char stage[8][Stage<T>::BYTES];
   __shared__ __align__(16) float biases[8][64];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, h = warp >> 2;
-  const int i = int(blockIdx.x) % CH, rank = int(blockIdx.x) / CH % CTAS;
-  const int64_t rest = blockIdx.x / (CH * CTAS);
+  const int i = block % CH, rank = block / CH % CTAS;
+  const int64_t rest = block / (CH * CTAS);
   const int64_t total = a.cut * a.KB, first = rest * a.KB, last = first + a.KB - 1;
-  const int w0 = owner_of(total, a.W, first), w1 = owner_of(total, a.W, last);
+  const int w0 = owner_of(total, a.cutters, first), w1 = owner_of(total, a.cutters, last);
   if (w0 == w1) return;  // its worker ended it
   int mb, nb;
   tile_place(a, a.whole + rest, &mb, &nb);
@@ -409,19 +428,36 @@ __global__ void __launch_bounds__(256) tc_join_kernel(const TcArgs a) {
     __syncwarp();
   }
   float v[32], u[EPI == EPI_GATED ? 32 : 1];
+  const int64_t piece = int64_t(CTAS) * 128 * C::BN;
+  // every worker between has a piece (none has an empty share), in its first slot but for the first, whose share may
+  // begin before the tile
+  const float* p0 = a.piece + int64_t(rank) * 128 * C::BN + (q * 32 + lane) * 4;
+  auto at = [&](int w) { return p0 + (int64_t(w) * 2 + (w == w0 ? partial_slot(total, a.cutters, w0, first) : 0)) * piece; };
   auto sum = [&](float* x, int c) {
 #pragma unroll
     for (int j = 0; j < 32; ++j) x[j] = 0.f;
     if (m0 + lane >= a.M) return;
-    for (int w = w0; w <= w1; ++w) {
-      if (range_begin(total, a.W, w) == range_begin(total, a.W, w + 1)) continue;  // an empty share has no piece
-      const int slot = partial_slot(total, a.W, w, first);
-      const float* p = a.piece + (int64_t(w * 2 + slot) * CTAS + rank) * (128 * C::BN) + (q * 32 + lane) * 4;
+    auto add = [&](const float4* f) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float4 f = *reinterpret_cast<const float4*>(p + int64_t(c / 4 + j) * 512);
-        x[4 * j] += f.x, x[4 * j + 1] += f.y, x[4 * j + 2] += f.z, x[4 * j + 3] += f.w;
-      }
+      for (int j = 0; j < 8; ++j) x[4 * j] += f[j].x, x[4 * j + 1] += f[j].y, x[4 * j + 2] += f[j].z, x[4 * j + 3] += f[j].w;
+    };
+    auto read = [&](int w, float4* f) {
+      const float* p = at(w) + int64_t(c / 4) * 512;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = *reinterpret_cast<const float4*>(p + j * 512);
+    };
+    int w = w0;
+    for (; w + 2 <= w1; w += 3) {  // three pieces in flight
+      float4 f[3][8];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) read(w + k, f[k]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) add(f[k]);
+    }
+    for (; w <= w1; ++w) {
+      float4 f[8];
+      read(w, f);
+      add(f);
     }
   };
   sum(v, col(0));
@@ -429,35 +465,45 @@ __global__ void __launch_bounds__(256) tc_join_kernel(const TcArgs a) {
   finish_chunk<T, EPI>(a, v, u, biases[warp], biases[warp] + 32, res, stage[warp], lane, m0, n0);
 }
 
-// Rows of dt into rows of bf16, `pitch` elements apart: as they are, or as three terms in three planes whose sum
-// is the value.
+template <int CTAS, bool F32, int EPI>
+__global__ void __launch_bounds__(256) tc_join_kernel(const TcArgs a) {
+  tc_join_work<CTAS, F32, EPI>(a, blockIdx.x);
+}
+
+// dx's cut tiles in the first `split` blocks, dW's in the rest
+template <int CTAS, bool F32>
+__global__ void __launch_bounds__(256) tc_join_grads_kernel(const TcArgs x, const TcArgs w, const int split) {
+  const bool second = int(blockIdx.x) >= split;
+  tc_join_work<CTAS, F32, EPI_PLAIN>(second ? w : x, int(blockIdx.x) - (second ? split : 0));
+}
+
+// Rows into rows of bf16, `pitch` elements apart: as they are, or as three terms in three planes whose sum is the value.
+// One or two matrices (the first takes `blocks0` blocks).
 template <typename T>
-__global__ void __launch_bounds__(256) repack_kernel(const T* src, int64_t stride, int64_t rows, int cols,
-                                                     __nv_bfloat16* dst, int64_t pitch) {
-  const int64_t plane = rows * pitch;
-  const int per_row = int(pitch / 8);
-  const int64_t all = rows * per_row;
-  for (int64_t e = blockIdx.x * int64_t(blockDim.x) + threadIdx.x; e < all; e += int64_t(gridDim.x) * blockDim.x) {
+__global__ void __launch_bounds__(256) repack_kernel(const Repack r0, const Repack r1, unsigned blocks0) {
+  const bool second = blockIdx.x >= blocks0;
+  const Repack& r = second ? r1 : r0;
+  const T* src = static_cast<const T*>(r.src.p);
+  __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(r.dst);
+  const int64_t plane = r.rows * r.pitch, all = r.rows * (r.pitch / 8);
+  const int per_row = int(r.pitch / 8);
+  const unsigned block = blockIdx.x - (second ? blocks0 : 0), blocks = second ? gridDim.x - blocks0 : blocks0;
+  for (int64_t e = block * int64_t(blockDim.x) + threadIdx.x; e < all; e += int64_t(blocks) * blockDim.x) {
     const int64_t row = e / per_row;
     const int c = int(e - row * per_row) * 8;
     float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? ld_f32(src + row * stride + c + j) : 0.f;
-    __nv_bfloat16* d = dst + row * pitch + c;
-    if (sizeof(T) == 2) {
-      store8(d, v);
+    const T* s = src + row * r.src.stride + c;
+    if (r.vec) {
+      load8(s, v);
     } else {
 #pragma unroll
-      for (int p = 0; p < 3; ++p) {
-        float t[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          t[j] = __bfloat162float(__float2bfloat16_rn(v[j]));
-          v[j] -= t[j];  // exact
-        }
-        store8(d + p * plane, t);
-      }
+      for (int j = 0; j < 8; ++j) v[j] = c + j < r.cols ? ld_f32(s + j) : 0.f;
     }
+    __nv_bfloat16* d = dst + row * r.pitch + c;
+    if (sizeof(T) == 2)
+      store8(d, v);
+    else
+      store_terms(d, plane, v);
   }
 }
 
@@ -493,18 +539,15 @@ bool make_map(CUtensorMap* m, const TcOperand& o, bool f32, int box_rows) {
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
-cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaStream_t st, int* launches) {
-  using C = TcCfg<CTAS, F32>;
-  CUtensorMap ta, tb;
-  if (!make_map(&ta, g.A, F32, A_MN ? 64 : 128) || !make_map(&tb, g.B, F32, 64)) return cudaErrorInvalidValue;
-  auto fn = &tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>;
-  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+// A launch of `ctas` CTAs in clusters of CTAS.
+template <int CTAS, class... P, class... A>
+cudaError_t launch_cluster(void (*fn)(P...), int ctas, size_t smem, cudaStream_t st, const A&... args) {
+  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(p.W * CTAS), 1, 1);
+  cfg.gridDim = dim3(unsigned(ctas), 1, 1);
   cfg.blockDim = dim3(kTcThreads, 1, 1);
-  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -512,12 +555,38 @@ cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaSt
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, fn, ta, tb, a);
+  cfg.numAttrs = CTAS > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, fn, args...);
+}
+
+template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
+cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaStream_t st, int* launches) {
+  using C = TcCfg<CTAS, F32>;
+  CUtensorMap ta, tb;
+  if (!make_map(&ta, g.A, F32, A_MN ? 64 : 128) || !make_map(&tb, g.B, F32, 64)) return cudaErrorInvalidValue;
+  cudaError_t e = launch_cluster<CTAS>(&tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>, p.W * CTAS, C::SMEM, st, ta, tb, a);
   ++*launches;
   if (e != cudaSuccess || p.cut == 0) return e;
   constexpr int CH = TileShape<CTAS>::template CHUNKS<EPI>;
   tc_join_kernel<CTAS, F32, EPI><<<unsigned(p.cut * CTAS * CH), 256, 0, st>>>(a);
+  ++*launches;
+  return cudaGetLastError();
+}
+
+template <int CTAS, bool F32>
+cudaError_t launch_grads(const TcGemm& gx, const TcPlan& px, const TcArgs& x, const TcGemm& gw, const TcPlan& pw,
+                         const TcArgs& w, cudaStream_t st, int* launches) {
+  using C = TcCfg<CTAS, F32>;
+  CUtensorMap xa, xb, wa, wb;
+  if (!make_map(&xa, gx.A, F32, 128) || !make_map(&xb, gx.B, F32, 64) || !make_map(&wa, gw.A, F32, 64) ||
+      !make_map(&wb, gw.B, F32, 64))
+    return cudaErrorInvalidValue;
+  cudaError_t e = launch_cluster<CTAS>(&tc_linear_grads_kernel<CTAS, F32>, (px.W + pw.W) * CTAS, C::SMEM, st, xa, xb, wa, wb, x, w);
+  ++*launches;
+  if (e != cudaSuccess || px.cut + pw.cut == 0) return e;
+  constexpr int CH = TileShape<CTAS>::template CHUNKS<EPI_PLAIN>;
+  tc_join_grads_kernel<CTAS, F32>
+      <<<unsigned((px.cut + pw.cut) * CTAS * CH), 256, 0, st>>>(x, w, int(px.cut * CTAS * CH));
   ++*launches;
   return cudaGetLastError();
 }
@@ -532,40 +601,74 @@ cudaError_t launch_kind(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaS
 
 }  // namespace
 
-// What a call of these sizes runs on, by the blocks' time it would take (in units of a 64-deep block of
+// What a product of these sizes runs on, by the time its blocks would take (in units of a 64-deep block of
 // a pair's tile, 512 cycles): a pair's block makes four times a single CTA's products in the same time, both being
-// fed 32 KB a CTA; the end of a cut tile costs a launch and the pieces' way through L2.
-TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32) {
+// fed 32 KB a CTA; the end of a cut tile costs a launch and the pieces' way through L2.  `ctas_only` 0: either kind.
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32, int sms, int ctas_only) {
   TcPlan best{};
-  double cost = 0;
-  const int sms = sm_count();
+  best.cost = 0;
+  if (sms <= 0) sms = sm_count();
   const int64_t KB = (K + 63) / 64;
   for (int ctas = 1; ctas <= (f32 || sms < 2 ? 1 : 2); ++ctas) {
+    if (ctas_only && ctas != ctas_only) continue;
     const int bn = ctas == 2 ? 256 : 128, yn = gated ? bn / 2 : bn;
     const int64_t mt = (M + 128 * ctas - 1) / (128 * ctas), nt = (N + yn - 1) / yn, tiles = mt * nt;
-    const int W = sms / ctas;
-    const int64_t waves = tiles / W, rest = tiles % W;
-    const double block = f32 ? 3.0 : 1.0, join = 10 + (ctas == 2 ? 16.0 : 8.0);
-    for (int cut = 0; cut <= (rest ? 1 : 0); ++cut) {
-      const double blocks = cut ? double(waves) * KB + double((rest * KB + W - 1) / W) : double(waves + (rest ? 1 : 0)) * KB;
+    const int workers = sms / ctas;
+    const int64_t waves = tiles / workers, rest = tiles % workers;
+    const double block = f32 ? 3.0 : 1.0;
+    for (int cut = 0; cut <= (rest && KB > 1 ? 1 : 0); ++cut) {
+      int cutters = 0;
+      if (cut) {
+        const int64_t most = rest * (KB < 16 ? KB : 16);
+        cutters = int(most < workers ? most : workers);
+      }
+      const double blocks =
+          cut ? double(waves) * KB + double((rest * KB + cutters - 1) / cutters) : double(waves + (rest ? 1 : 0)) * KB;
+      const double join = 10 + (ctas == 2 ? 12.0 : 4.0) + (cut ? 0.5 * cutters / rest : 0);
       const double c = blocks * block + (cut ? join : 0);
-      if (best.W == 0 || c < cost) {
-        cost = c;
+      if (best.ctas == 0 || c < best.cost) {
+        best.cost = c;
         best.ctas = ctas;
-        best.W = W;
+        best.W = int(waves ? workers : cut ? cutters : rest);
         best.mt = mt;
         best.nt = nt;
-        best.whole = cut ? waves * W : tiles;
+        best.whole = cut ? waves * workers : tiles;
         best.cut = cut ? rest : 0;
+        best.cutters = cutters;
       }
     }
   }
   best.KB = KB;
-  best.piece_bytes = best.cut ? size_t(best.W) * 2 * best.ctas * 128 * (best.ctas == 2 ? 256 : 128) * sizeof(float) : 0;
+  best.piece_bytes =
+      best.cut ? size_t(best.cutters) * 2 * best.ctas * 128 * (best.ctas == 2 ? 256 : 128) * sizeof(float) : 0;
   return best;
 }
 
-cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches) {
+// Both gradients' products side by side, each on a share of the SMs by its work, where that is no slower than one after the
+// other on all of them with two launches more (about ten units).
+bool tc_plan_grads(int64_t M, int64_t Z, int64_t K, bool f32, double apart, TcPlan* x, TcPlan* w) {
+  const int sms = sm_count();
+  if (sms < 8 || apart > 1000) return false;  // large products fill the GPU by themselves
+  double best = apart + 10;
+  bool found = false;
+  for (int ctas = 1; ctas <= (f32 ? 1 : 2); ++ctas)
+    for (int eighths = 2; eighths <= 6; ++eighths) {
+      const int sx = sms * eighths / 8 / ctas * ctas;
+      const TcPlan px = tc_plan(M, K, Z, false, f32, sx, ctas), pw = tc_plan(Z, K, M, false, f32, sms - sx, ctas);
+      const double c = px.cost > pw.cost ? px.cost : pw.cost;
+      if (c < best) {
+        best = c;
+        *x = px;
+        *w = pw;
+        found = true;
+      }
+    }
+  return found;
+}
+
+namespace {
+
+TcArgs tc_args(const TcGemm& g, const TcPlan& p) {
   TcArgs a{};
   a.M = g.M;
   a.N = g.N;
@@ -575,6 +678,7 @@ cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, in
   a.W = p.W;
   a.whole = p.whole;
   a.cut = p.cut;
+  a.cutters = p.cutters;
   a.half = g.N;
   a.bias = g.bias;
   a.r = g.r.p;
@@ -590,21 +694,38 @@ cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, in
   a.piece = g.piece;
   a.ws = g.ws;
   a.clear = g.clear;
+  return a;
+}
+
+}  // namespace
+
+cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches) {
+  const TcArgs a = tc_args(g, p);
   if (g.dt == SA_F32) return launch_kind<1, true>(g, p, a, st, launches);
   return p.ctas == 2 ? launch_kind<2, false>(g, p, a, st, launches) : launch_kind<1, false>(g, p, a, st, launches);
 }
 
-cudaError_t launch_repack(const Mat& src, int64_t rows, int cols, void* dst, int64_t pitch, cudaStream_t st) {
-  const int64_t all = rows * (pitch / 8);
-  if (all == 0) return cudaSuccess;
-  const int64_t need = (all + 255) / 256, most = int64_t(sm_count()) * 16;
-  const unsigned grid = unsigned(need < most ? need : most);
-  __nv_bfloat16* d = static_cast<__nv_bfloat16*>(dst);
-  if (src.dt == SA_BF16)
-    repack_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src.p), src.stride, rows, cols, d,
-                                                       pitch);
+cudaError_t launch_tc_grads(const TcGemm& gx, const TcPlan& px, const TcGemm& gw, const TcPlan& pw, cudaStream_t st,
+                            int* launches) {
+  const TcArgs x = tc_args(gx, px), w = tc_args(gw, pw);
+  if (gx.dt == SA_F32) return launch_grads<1, true>(gx, px, x, gw, pw, w, st, launches);
+  return px.ctas == 2 ? launch_grads<2, false>(gx, px, x, gw, pw, w, st, launches)
+                      : launch_grads<1, false>(gx, px, x, gw, pw, w, st, launches);
+}
+
+cudaError_t launch_repack(Repack r0, Repack r1, cudaStream_t st) {
+  auto blocks = [](Repack& r) {
+    r.vec = r.cols % 8 == 0 && reinterpret_cast<uintptr_t>(r.src.p) % 16 == 0 &&
+            r.src.stride % (r.src.dt == SA_BF16 ? 8 : 4) == 0;
+    const int64_t all = r.dst ? r.rows * (r.pitch / 8) : 0, need = (all + 255) / 256, most = int64_t(sm_count()) * 16;
+    return unsigned(need < most ? need : most);
+  };
+  const unsigned b0 = blocks(r0), b1 = blocks(r1);
+  if (b0 + b1 == 0) return cudaSuccess;
+  if ((b0 ? r0 : r1).src.dt == SA_BF16)
+    repack_kernel<__nv_bfloat16><<<b0 + b1, 256, 0, st>>>(r0, r1, b0);
   else
-    repack_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(src.p), src.stride, rows, cols, d, pitch);
+    repack_kernel<float><<<b0 + b1, 256, 0, st>>>(r0, r1, b0);
   return cudaGetLastError();
 }
 

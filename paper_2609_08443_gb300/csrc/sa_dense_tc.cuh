@@ -16,6 +16,7 @@ struct TcArgs {
   int W;           // workers: CTAs or pairs
   int64_t whole;   // tiles [0, whole) go to workers in turn, the rest in equal shares of blocks
   int64_t cut;     // the rest's tiles
+  int cutters;     // workers that take a share of them (at most one a block)
   int64_t half;    // SwiGLU: rows of B before the second half
   const void* bias;
   const void* r;
@@ -48,8 +49,11 @@ struct Segments {
   int k0, k1;
   __device__ Segments(const TcArgs& a_, int w) : a(a_), t(w) {
     const int64_t total = a.cut * a.KB;
-    u = range_begin(total, a.W, w);
-    u1 = range_begin(total, a.W, w + 1);
+    u = u1 = 0;
+    if (w < a.cutters) {
+      u = range_begin(total, a.cutters, w);
+      u1 = range_begin(total, a.cutters, w + 1);
+    }
   }
   __device__ bool next() {
     if (t < a.whole) {
@@ -184,7 +188,7 @@ struct Residual {
         *reinterpret_cast<uint4*>(s + S::at(i * ROWS + lane / S::PIECES, lane % S::PIECES)) = q[i];
     } else {
       const T* r = static_cast<const T*>(a.r);
-#pragma unroll 4
+#pragma unroll 16
       for (int row = 0; row < 32; ++row) {
         T v = T(0.f);
         if (m0 + row < a.M && n0 + lane < a.N) v = r[(m0 + row) * a.r_stride + n0 + lane];
