@@ -33,19 +33,24 @@ constexpr int kEpiWarp0 = 4;
 constexpr int kBlockBytes = 16384;  // 128 rows x 64 bf16
 constexpr uint32_t kWaitNs = 2000000000u;
 
-template <int CTAS, bool F32>
+template <int CTAS, bool F32, int EPI>
 struct TcCfg {
+  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+  using End = ChunkEnd<T, EPI>;
   static constexpr int PLANES = F32 ? 3 : 1;
   static constexpr int STAGE = 2 * PLANES * kBlockBytes;
-  static constexpr int STAGES = F32 ? 2 : 6;
+  static constexpr int OUT = F32 ? kStageBytes : 4 * kOutBytes;  // of an epilogue warp
+  static constexpr int STAGES = F32 ? 2 : 5;
   static constexpr int BN = TileShape<CTAS>::BN;
   static constexpr int TMEM = 2 * BN;
-  static constexpr int OFF_OUT = STAGES * STAGE;                     // the epilogue warps' stages
-  static constexpr int OFF_BIAS = OFF_OUT + 8 * (F32 ? 4096 : 2048);  // [2][BN] floats
-  static constexpr int OFF_BAR = OFF_BIAS + 2 * BN * 4;
+  static constexpr int OFF_OUT = STAGES * STAGE;
+  static constexpr int OFF_BIAS = OFF_OUT + 8 * OUT;  // bf16: 64 floats of each epilogue warp
+  static constexpr int OFF_BAR = OFF_BIAS + (F32 ? 0 : 8 * 256);
   static constexpr int SMEM = OFF_BAR + 256;
 };
-static_assert(TcCfg<2, false>::SMEM <= 232448 && TcCfg<1, true>::SMEM <= 232448, "shared memory of a CTA");
+static_assert(TcCfg<2, false, EPI_GATED>::SMEM <= 232448 && TcCfg<2, false, EPI_FULL>::SMEM <= 232448 &&
+                  TcCfg<1, true, EPI_GATED>::SMEM <= 232448,
+              "shared memory of a CTA");
 
 // ------------------------------------------------------ cta_group::2 forms
 template <int CTAS>
@@ -102,10 +107,11 @@ __device__ __forceinline__ void tc_load(uint32_t dst, const void* map, uint32_t 
 // The work of one CTA.  Maps: K-major operands [planes][rows][k], boxes of 64 x (A: 128, B: 64) rows; MN-major ones
 // [planes][k][mn], boxes of 64 x 64.
 template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
-__device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUtensorMap& tb, const TcArgs& a,
-                                               const int worker, const bool clear) {
-  using C = TcCfg<CTAS, F32>;
-  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+__device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ty,
+                                               const CUtensorMap& tz, const TcArgs& a, const int worker,
+                                               const bool clear) {
+  using C = TcCfg<CTAS, F32, EPI>;
+  using End = typename C::End;
   using Shape = TileShape<CTAS>;
   constexpr int YN = Shape::template YN<EPI>;
   extern __shared__ __align__(1024) char smem[];
@@ -117,7 +123,6 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
   auto empty = [&](int s) { return base + C::OFF_BAR + 64 + 8 * s; };
   auto acc_full = [&](int s) { return base + C::OFF_BAR + 128 + 8 * s; };
   auto acc_empty = [&](int s) { return base + C::OFF_BAR + 144 + 8 * s; };
-  const uint32_t bias_full = base + C::OFF_BAR + 192;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_BAR + 160);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 176);  // three words
 
@@ -134,7 +139,6 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       mbar_init(acc_full(s), 1);
       mbar_init(acc_empty(s), 8 * CTAS);
     }
-    mbar_init(bias_full, 8);
     abort_flag[0] = 0;
     reinterpret_cast<volatile uint32_t*>(abort_flag)[2] = kWaitNs;
     fence_mbar_init();
@@ -240,12 +244,13 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
   } else if (warp >= kEpiWarp0) {
     // -------------------------------------------------------- tiles' ends
     const int e = warp - kEpiWarp0, q = e & 3, h = e >> 2;
-    char* out = smem + C::OFF_OUT + e * Stage<T>::BYTES;
+    char* out = smem + C::OFF_OUT + e * C::OUT;
     const uint32_t lanes = uint32_t(q * 32) << 16;
     const uint32_t lead_empty = CTAS == 2 ? mapa_shared(acc_empty(0), 0) : acc_empty(0);
     constexpr int CH = Shape::template CHUNKS<EPI>;
+    TmaOut outs(out, reinterpret_cast<float*>(smem + C::OFF_BIAS) + e * 64, lane);
     Segments seg(a, worker);
-    uint32_t g = 0, tiles = 0;  // sets of accumulators and biases used
+    uint32_t g = 0;  // sets of accumulators used
     bool ok = true;
     auto release = [&](uint32_t set) {
       tc_fence_before();
@@ -263,24 +268,6 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       tile_place(a, seg.tile, &mb, &nb);
       const int64_t m0 = int64_t(mb * CTAS + int(rank)) * 128 + q * 32;
       const bool complete = seg.complete();
-      const float* bias = reinterpret_cast<const float*>(smem + C::OFF_BIAS) + (tiles & 1u) * C::BN;
-      if (EPI != EPI_PLAIN && complete) {
-        // the columns' biases: one thread each, ready for all epilogue warps behind their barrier
-        const int c = threadIdx.x - kEpiWarp0 * 32;
-        if (c < C::BN) {
-          const int in = EPI == EPI_GATED ? c % YN : c;
-          const int64_t n = int64_t(nb) * YN + in;
-          float v = 0.f;
-          if (a.bias && n < a.N) v = ld_f32(static_cast<const T*>(a.bias) + (EPI == EPI_GATED && c >= YN ? a.half : 0) + n);
-          reinterpret_cast<float*>(smem + C::OFF_BIAS)[(tiles & 1u) * C::BN + c] = v;
-        }
-        // every warp is past the tile before last, whose biases these replace, once it has arrived for the last
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bias_full);
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(bias_full, tiles & 1u, abort_flag, a.ws, 0x405));
-        if (!ok) break;
-        ++tiles;
-      }
       float* piece = nullptr;
       if (!complete) {
         const int64_t total = a.cut * a.KB, first = (seg.tile - a.whole) * a.KB;
@@ -297,6 +284,8 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
             *reinterpret_cast<float4*>(piece + int64_t(c / 4 + j) * 512) =
                 make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
       };
+      End end;
+      const int y0 = nb * YN + h * (YN / 2);  // this warp's first column of y
       if constexpr (F32) {
         constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
         float sum[CH][HALVES][32];
@@ -325,22 +314,37 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           ++g;
         }
         if (!ok) break;
+        if (complete) {
+          // all chunks pass through one copy of their end, so the registers they are in are chosen by selects
+#pragma unroll 1
+          for (int i = 0; i < CH * 32 / End::COLS; ++i) {
+            const int n0 = y0 + i * End::COLS;
+            end.load_bias(a, lane, n0);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-          if (complete) {
-            const int n0 = nb * YN + h * (YN / 2) + i * 32;
-            Residual<T> res;
-            if (EPI != EPI_PLAIN && a.r) res.load(a, lane, m0, n0);
-            finish_chunk<T, EPI>(a, sum[i][0], sum[i][HALVES - 1], bias + col(i, 0), bias + col(i, 1), res, out, lane, m0,
-                                 n0);
-          } else {
+            for (int k = 0; k < CH * 32 / End::COLS; ++k)
+              if (k == i) {
+                stage_put<End::COLS>(out, lane, &sum[k * End::COLS / 32][0][k * End::COLS % 32]);
+                if (EPI == EPI_GATED)
+                  stage_put<End::COLS>(out, lane, &sum[k * End::COLS / 32][HALVES - 1][k * End::COLS % 32], End::COLS / 4);
+              }
+            __syncwarp();
+            end.finish(a, out, lane, m0, n0);
+            __syncwarp();
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int k = 0; k < HALVES; ++k) put_piece(col(i, k), sum[i][k]);
-          }
         }
       } else {
-        Residual<T> res;
-        if (EPI != EPI_PLAIN && a.r && complete) res.load(a, lane, m0, nb * YN + h * (YN / 2));
+        const bool tma = (a.vec & 1) != 0;
+        if (complete) {
+          if (tma)
+            outs.template load_bias<EPI>(a, y0);
+          else
+            end.load_bias(a, lane, y0);
+        }
         const uint32_t set = g & 1u, acc = tmem + lanes + set * C::BN;
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), (g >> 1) & 1u, abort_flag, a.ws, 0x404));
         if (!ok) break;
@@ -352,10 +356,16 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           if constexpr (EPI == EPI_GATED) tmem_ld32(acc + col(i, 1), u);
           tmem_ld_wait();
           if (i == CH - 1) release(set);
-          const int n0 = nb * YN + h * (YN / 2) + i * 32;
-          if (complete) {
-            finish_chunk<T, EPI>(a, v, u, bias + col(i, 0), bias + col(i, 1), res, out, lane, m0, n0);
-            if (EPI != EPI_PLAIN && a.r && i + 1 < CH) res.load(a, lane, m0, n0 + 32);
+          if (complete && tma) {
+            outs.template finish<EPI>(a, ty, tz, v, u, m0, y0 + i * 32);
+            if (i + 1 < CH) outs.template load_bias<EPI>(a, y0 + i * 32 + 32);
+          } else if (complete) {
+            stage_put<32>(out, lane, v);
+            if constexpr (EPI == EPI_GATED) stage_put<32>(out + kStageBytes, lane, u);
+            __syncwarp();
+            end.finish(a, out, lane, m0, y0 + i * 32);
+            if (i + 1 < CH) end.load_bias(a, lane, y0 + i * 32 + 32);
+            __syncwarp();
           } else {
             put_piece(col(i, 0), v);
             if constexpr (EPI == EPI_GATED) put_piece(col(i, 1), u);
@@ -364,6 +374,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         ++g;
       }
     }
+    if (!F32) outs.done();
   }
   __syncwarp();
   if (CTAS == 2)
@@ -379,8 +390,9 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
 
 template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
 __global__ void __launch_bounds__(kTcThreads, 1)
-    tc_linear_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const TcArgs a) {
-  tc_linear_work<CTAS, A_MN, B_MN, F32, EPI>(ta, tb, a, int(blockIdx.x) / CTAS, a.clear && blockIdx.x == 0);
+    tc_linear_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
+                     const __grid_constant__ CUtensorMap ty, const __grid_constant__ CUtensorMap tz, const TcArgs a) {
+  tc_linear_work<CTAS, A_MN, B_MN, F32, EPI>(ta, tb, ty, tz, a, int(blockIdx.x) / CTAS, a.clear && blockIdx.x == 0);
 }
 
 // dx and dW side by side, for gradients that would leave most of the GPU idle one after the other: the first
@@ -388,24 +400,24 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 template <int CTAS, bool F32>
 __global__ void __launch_bounds__(kTcThreads, 1)
     tc_linear_grads_kernel(const __grid_constant__ CUtensorMap xa, const __grid_constant__ CUtensorMap xb,
-                           const __grid_constant__ CUtensorMap wa, const __grid_constant__ CUtensorMap wb, const TcArgs x,
+                           const __grid_constant__ CUtensorMap wa, const __grid_constant__ CUtensorMap wb,
+                           const __grid_constant__ CUtensorMap xy, const __grid_constant__ CUtensorMap wy, const TcArgs x,
                            const TcArgs w) {
   const int worker = int(blockIdx.x) / CTAS;
   if (worker < x.W)
-    tc_linear_work<CTAS, false, true, F32, EPI_PLAIN>(xa, xb, x, worker, blockIdx.x == 0);
+    tc_linear_work<CTAS, false, true, F32, EPI_PLAIN>(xa, xb, xy, xy, x, worker, blockIdx.x == 0);
   else
-    tc_linear_work<CTAS, true, true, F32, EPI_PLAIN>(wa, wb, w, worker - x.W, false);
+    tc_linear_work<CTAS, true, true, F32, EPI_PLAIN>(wa, wb, wy, wy, w, worker - x.W, false);
 }
 
 // Cut tiles: one block for 32 columns of each epilogue warp's rows; pieces are added in worker order.
 template <int CTAS, bool F32, int EPI>
 __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
-  using C = TcCfg<CTAS, F32>;
-  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+  using C = TcCfg<CTAS, F32, EPI>;
+  using End = typename C::End;
   using Shape = TileShape<CTAS>;
   constexpr int YN = Shape::template YN<EPI>, CH = Shape::template CHUNKS<EPI>;
-  __shared__ __align__(128) char stage[8][Stage<T>::BYTES];
-  __shared__ __align__(16) float biases[8][64];
+  extern __shared__ __align__(128) char stages[];  // the warps' stages
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, h = warp >> 2;
   const int i = block % CH, rank = block / CH % CTAS;
   const int64_t rest = block / (CH * CTAS);
@@ -418,15 +430,8 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   if (m0 >= a.M) return;
   const int n0 = nb * YN + h * (YN / 2) + i * 32;
   auto col = [&](int half) { return EPI == EPI_GATED ? half * YN + h * (YN / 2) + i * 32 : h * (C::BN / 2) + i * 32; };
-  Residual<T> res;
-  if (EPI != EPI_PLAIN) {
-    if (a.r) res.load(a, lane, m0, n0);
-    const bool in = a.bias && n0 + lane < a.N;
-    const T* b = static_cast<const T*>(a.bias) + n0 + lane;
-    biases[warp][lane] = in ? ld_f32(b) : 0.f;
-    if (EPI == EPI_GATED) biases[warp][32 + lane] = in ? ld_f32(b + a.half) : 0.f;
-    __syncwarp();
-  }
+  End end;
+  end.load_bias(a, lane, n0);
   float v[32], u[EPI == EPI_GATED ? 32 : 1];
   const int64_t piece = int64_t(CTAS) * 128 * C::BN;
   // every worker between has a piece (none has an empty share), in its first slot but for the first, whose share may
@@ -462,7 +467,23 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   };
   sum(v, col(0));
   if constexpr (EPI == EPI_GATED) sum(u, col(1));
-  finish_chunk<T, EPI>(a, v, u, biases[warp], biases[warp] + 32, res, stage[warp], lane, m0, n0);
+  char* out = stages + warp * End::STAGES * kStageBytes;
+  if constexpr (End::COLS == 32) {
+    stage_put<32>(out, lane, v);
+    if constexpr (EPI == EPI_GATED) stage_put<32>(out + kStageBytes, lane, u);
+    __syncwarp();
+    end.finish(a, out, lane, m0, n0);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (k) end.load_bias(a, lane, n0 + 16);
+      stage_put<16>(out, lane, v + 16 * k);
+      stage_put<16>(out, lane, u + 16 * k, 4);
+      __syncwarp();
+      end.finish(a, out, lane, m0, n0 + 16 * k);
+      __syncwarp();
+    }
+  }
 }
 
 template <int CTAS, bool F32, int EPI>
@@ -559,16 +580,40 @@ cudaError_t launch_cluster(void (*fn)(P...), int ctas, size_t smem, cudaStream_t
   return cudaLaunchKernelEx(&cfg, fn, args...);
 }
 
+// `halves` matrices of N bf16 columns side by side in rows of halves * N: boxes of 32 x 32 to be written.
+bool make_out_map(CUtensorMap* m, const void* p, int64_t M, int N, int halves) {
+  EncodeFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {cuuint64_t(N), cuuint64_t(halves), cuuint64_t(M)};
+  const cuuint64_t strides[2] = {cuuint64_t(N) * 2, cuuint64_t(N) * halves * 2};
+  const cuuint32_t box[3] = {32, 1, 32};
+  const cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
 cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaStream_t st, int* launches) {
-  using C = TcCfg<CTAS, F32>;
+  using C = TcCfg<CTAS, F32, EPI>;
   CUtensorMap ta, tb;
   if (!make_map(&ta, g.A, F32, A_MN ? 64 : 128) || !make_map(&tb, g.B, F32, 64)) return cudaErrorInvalidValue;
-  cudaError_t e = launch_cluster<CTAS>(&tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>, p.W * CTAS, C::SMEM, st, ta, tb, a);
+  CUtensorMap ty = ta, tz = ta;
+  if (!F32 && (a.vec & 1)) {
+    if (!make_out_map(&ty, a.y, a.M, a.N, 1) || (a.z && !make_out_map(&tz, a.z, a.M, a.N, EPI == EPI_GATED ? 2 : 1)))
+      return cudaErrorInvalidValue;
+  }
+  cudaError_t e =
+      launch_cluster<CTAS>(&tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>, p.W * CTAS, C::SMEM, st, ta, tb, ty, tz, a);
   ++*launches;
   if (e != cudaSuccess || p.cut == 0) return e;
   constexpr int CH = TileShape<CTAS>::template CHUNKS<EPI>;
-  tc_join_kernel<CTAS, F32, EPI><<<unsigned(p.cut * CTAS * CH), 256, 0, st>>>(a);
+  constexpr size_t stages = 8 * C::End::STAGES * kStageBytes;
+  if (stages > 48 * 1024) {
+    e = cudaFuncSetAttribute(tc_join_kernel<CTAS, F32, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(stages));
+    if (e != cudaSuccess) return e;
+  }
+  tc_join_kernel<CTAS, F32, EPI><<<unsigned(p.cut * CTAS * CH), 256, stages, st>>>(a);
   ++*launches;
   return cudaGetLastError();
 }
@@ -576,17 +621,21 @@ cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaSt
 template <int CTAS, bool F32>
 cudaError_t launch_grads(const TcGemm& gx, const TcPlan& px, const TcArgs& x, const TcGemm& gw, const TcPlan& pw,
                          const TcArgs& w, cudaStream_t st, int* launches) {
-  using C = TcCfg<CTAS, F32>;
+  using C = TcCfg<CTAS, F32, EPI_PLAIN>;
   CUtensorMap xa, xb, wa, wb;
   if (!make_map(&xa, gx.A, F32, 128) || !make_map(&xb, gx.B, F32, 64) || !make_map(&wa, gw.A, F32, 64) ||
       !make_map(&wb, gw.B, F32, 64))
     return cudaErrorInvalidValue;
-  cudaError_t e = launch_cluster<CTAS>(&tc_linear_grads_kernel<CTAS, F32>, (px.W + pw.W) * CTAS, C::SMEM, st, xa, xb, wa, wb, x, w);
+  CUtensorMap xy = xa, wy = wa;
+  if (!F32 && ((x.vec & 1) && !make_out_map(&xy, x.y, x.M, x.N, 1))) return cudaErrorInvalidValue;
+  if (!F32 && ((w.vec & 1) && !make_out_map(&wy, w.y, w.M, w.N, 1))) return cudaErrorInvalidValue;
+  cudaError_t e = launch_cluster<CTAS>(&tc_linear_grads_kernel<CTAS, F32>, (px.W + pw.W) * CTAS, C::SMEM, st, xa, xb, wa,
+                                       wb, xy, wy, x, w);
   ++*launches;
   if (e != cudaSuccess || px.cut + pw.cut == 0) return e;
   constexpr int CH = TileShape<CTAS>::template CHUNKS<EPI_PLAIN>;
   tc_join_grads_kernel<CTAS, F32>
-      <<<unsigned((px.cut + pw.cut) * CTAS * CH), 256, 0, st>>>(x, w, int(px.cut * CTAS * CH));
+      <<<unsigned((px.cut + pw.cut) * CTAS * CH), 256, 8 * kStageBytes, st>>>(x, w, int(px.cut * CTAS * CH));
   ++*launches;
   return cudaGetLastError();
 }
@@ -615,7 +664,8 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32, int sms, i
     const int64_t mt = (M + 128 * ctas - 1) / (128 * ctas), nt = (N + yn - 1) / yn, tiles = mt * nt;
     const int workers = sms / ctas;
     const int64_t waves = tiles / workers, rest = tiles % workers;
-    const double block = f32 ? 3.0 : 1.0;
+    // the end of a worker's last tile, which nothing hides; fp32's is longer by its activation
+    const double block = f32 ? 3.0 : 1.0, end = f32 ? 24.0 : 6.0;
     for (int cut = 0; cut <= (rest && KB > 1 ? 1 : 0); ++cut) {
       int cutters = 0;
       if (cut) {
@@ -625,7 +675,7 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32, int sms, i
       const double blocks =
           cut ? double(waves) * KB + double((rest * KB + cutters - 1) / cutters) : double(waves + (rest ? 1 : 0)) * KB;
       const double join = 10 + (ctas == 2 ? 12.0 : 4.0) + (cut ? 0.5 * cutters / rest : 0);
-      const double c = blocks * block + (cut ? join : 0);
+      const double c = blocks * block + (cut ? join + end / 2 : end);
       if (best.ctas == 0 || c < best.cost) {
         best.cost = c;
         best.ctas = ctas;

@@ -87,172 +87,309 @@ struct TileShape {
   static constexpr int CHUNKS = YN<EPI> / 64;
 };
 
-// Rows' 32 columns as the warp stores them: 16-byte pieces in an order that keeps both the row-wise
-// and the column-wise access free of bank conflicts.
-template <typename T>
-struct Stage;
-template <>
-struct Stage<__nv_bfloat16> {
-  static constexpr int BYTES = 2048, PIECES = 4, EACH = 8;  // 16-byte pieces of a row, elements of a piece
-  __device__ static uint32_t at(int row, int p) { return row * 64 + ((p ^ ((row >> 1) & 3)) << 4); }
-};
-template <>
-struct Stage<float> {
-  static constexpr int BYTES = 4096, PIECES = 8, EACH = 4;
-  __device__ static uint32_t at(int row, int p) { return row * 128 + ((p ^ (row & 7)) << 4); }
-};
+// A chunk's sums on their way from one row a lane to whole rows a few lanes: 32 rows of 128 bytes, 16-byte pieces in
+// an order that keeps both directions free of bank conflicts.
+constexpr int kStageBytes = 4096;
+__device__ __forceinline__ uint32_t stage_at(int row, int p) { return row * 128 + ((p ^ (row & 7)) << 4); }
 
-// 32 values of this lane's row into the stage
-__device__ __forceinline__ void stage_put(__nv_bfloat16*, char* s, int lane, const float* v) {
+// COLS values of this lane's row into the stage, from 16-byte piece `first` on
+template <int COLS>
+__device__ __forceinline__ void stage_put(char* s, int lane, const float* v, int first = 0) {
 #pragma unroll
-  for (int p = 0; p < 4; ++p)
-    *reinterpret_cast<uint4*>(s + Stage<__nv_bfloat16>::at(lane, p)) =
-        make_uint4(ptx::pack_bf16(v[8 * p], v[8 * p + 1]), ptx::pack_bf16(v[8 * p + 2], v[8 * p + 3]),
-                   ptx::pack_bf16(v[8 * p + 4], v[8 * p + 5]), ptx::pack_bf16(v[8 * p + 6], v[8 * p + 7]));
-}
-__device__ __forceinline__ void stage_put(float*, char* s, int lane, const float* v) {
-#pragma unroll
-  for (int p = 0; p < 8; ++p)
-    *reinterpret_cast<float4*>(s + Stage<float>::at(lane, p)) =
-        make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
-}
-// v += this lane's row of the stage
-__device__ __forceinline__ void stage_add(__nv_bfloat16*, const char* s, int lane, float* v) {
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const uint4 q = *reinterpret_cast<const uint4*>(s + Stage<__nv_bfloat16>::at(lane, p));
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[8 * p + 2 * j] += __uint_as_float(w[j] << 16);
-      v[8 * p + 2 * j + 1] += __uint_as_float(w[j] & 0xFFFF0000u);
-    }
-  }
-}
-__device__ __forceinline__ void stage_add(float*, const char* s, int lane, float* v) {
-#pragma unroll
-  for (int p = 0; p < 8; ++p) {
-    const float4 q = *reinterpret_cast<const float4*>(s + Stage<float>::at(lane, p));
-    v[4 * p] += q.x, v[4 * p + 1] += q.y, v[4 * p + 2] += q.z, v[4 * p + 3] += q.w;
-  }
+  for (int p = 0; p < COLS / 4; ++p)
+    *reinterpret_cast<float4*>(s + stage_at(lane, first + p)) = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
 }
 
-// The stage's 32 x 32 values to rows m0.. and columns n0.. of a matrix of M rows and n_end columns.
-template <typename T>
-__device__ __forceinline__ void stage_store(const char* s, int lane, void* dst, int64_t pitch, int64_t m0, int64_t M,
-                                            int64_t n0, int64_t n_end, bool vec) {
-  using S = Stage<T>;
-  T* d = static_cast<T*>(dst);
-  if (vec) {
-    constexpr int ROWS = 32 / S::PIECES;
-    const int p = lane % S::PIECES;
-    const int64_t n = n0 + p * S::EACH;
-#pragma unroll
-    for (int i = 0; i < S::PIECES; ++i) {
-      const int row = i * ROWS + lane / S::PIECES;
-      const uint4 q = *reinterpret_cast<const uint4*>(s + S::at(row, p));
-      if (m0 + row < M && n < n_end) *reinterpret_cast<uint4*>(d + (m0 + row) * pitch + n) = q;
-    }
-  } else {
-#pragma unroll 4
-    for (int row = 0; row < 32; ++row) {
-      const T v = *reinterpret_cast<const T*>(s + S::at(row, lane / S::EACH) + (lane % S::EACH) * sizeof(T));
-      if (m0 + row < M && n0 + lane < n_end) d[(m0 + row) * pitch + n0 + lane] = v;
-    }
-  }
-}
-
-// A chunk's residual, read ahead: 16-byte pieces in the order in which they are stored.
-template <typename T>
-struct Residual {
-  uint4 q[Stage<T>::PIECES];
-  __device__ __forceinline__ void load(const TcArgs& a, int lane, int64_t m0, int n0) {
-    using S = Stage<T>;
-    if (!(a.vec & 2)) return;
-    const T* r = static_cast<const T*>(a.r);
-    constexpr int ROWS = 32 / S::PIECES;
-    const int n = n0 + (lane % S::PIECES) * S::EACH;
-#pragma unroll
-    for (int i = 0; i < S::PIECES; ++i) {
-      const int64_t m = m0 + i * ROWS + lane / S::PIECES;
-      q[i] = make_uint4(0, 0, 0, 0);
-      if (m < a.M && n < a.N) q[i] = *reinterpret_cast<const uint4*>(r + m * a.r_stride + n);
-    }
-  }
-  __device__ __forceinline__ void put(const TcArgs& a, char* s, int lane, int64_t m0, int n0) const {
-    using S = Stage<T>;
-    if (a.vec & 2) {
-      constexpr int ROWS = 32 / S::PIECES;
-#pragma unroll
-      for (int i = 0; i < S::PIECES; ++i)
-        *reinterpret_cast<uint4*>(s + S::at(i * ROWS + lane / S::PIECES, lane % S::PIECES)) = q[i];
-    } else {
-      const T* r = static_cast<const T*>(a.r);
-#pragma unroll 16
-      for (int row = 0; row < 32; ++row) {
-        T v = T(0.f);
-        if (m0 + row < a.M && n0 + lane < a.N) v = r[(m0 + row) * a.r_stride + n0 + lane];
-        *reinterpret_cast<T*>(s + S::at(row, lane / S::EACH) + (lane % S::EACH) * sizeof(T)) = v;
-      }
-    }
-  }
-};
-
-// The end of 32 rows (m0 + lane) x 32 columns (n0 ..) of y: v holds the sums (SwiGLU: of the gate's half, u of
-// the other's), bv and bu the biases of these columns (in shared memory), s the warp's stage.
+// How a chunk ends: EACH neighbouring values a lane, 16 bytes of T, of a row's COLS columns.  SwiGLU's fp32 chunks have
+// 16 columns, so that the gate's and the other half's share the stage; in bf16 the other half has a stage of its own.
 template <typename T, int EPI>
-__device__ __forceinline__ void finish_chunk(const TcArgs& a, float* v, float* u, const float* bv, const float* bu,
-                                             const Residual<T>& res, char* s, int lane, int64_t m0, int n0) {
-  constexpr bool FULL = sizeof(T) == 4;
-  T* tag = nullptr;
-  const bool vec = (a.vec & 1) != 0;
-  if (EPI != EPI_PLAIN) {
+struct ChunkEnd {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int COLS = F32 && EPI == EPI_GATED ? 16 : 32;
+  static constexpr int EACH = F32 ? 4 : 8;
+  static constexpr int LANES = COLS / EACH;   // lanes of a row
+  static constexpr int ROWS = 32 / LANES;     // rows at a time
+  static constexpr int STAGES = !F32 && EPI == EPI_GATED ? 2 : 1;
+
+  float bv[EACH], bu[EACH];  // biases of this lane's columns
+
+  // the biases of columns n0 ..; on their way while the products are awaited
+  __device__ __forceinline__ void load_bias(const TcArgs& a, int lane, int n0) {
+    if (EPI == EPI_PLAIN) return;
+    const T* b = static_cast<const T*>(a.bias);
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      const float4 b = *reinterpret_cast<const float4*>(bv + j);
-      v[j] += b.x, v[j + 1] += b.y, v[j + 2] += b.z, v[j + 3] += b.w;
-      if (EPI == EPI_GATED) {
-        const float4 c = *reinterpret_cast<const float4*>(bu + j);
-        u[j] += c.x, u[j + 1] += c.y, u[j + 2] += c.z, u[j + 3] += c.w;
+    for (int j = 0; j < EACH; ++j) bv[j] = bu[j] = 0.f;
+    if (!b) return;
+    if (a.vec & 1) {
+      const int n = n0 + (lane % LANES) * EACH;
+      if (n >= a.N) return;
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        bv[j] = ld_f32(b + n + j);
+        if (EPI == EPI_GATED) bu[j] = ld_f32(b + a.half + n + j);
       }
+    } else {
+      const int n = n0 + lane % COLS;
+      if (n >= a.N) return;
+      bv[0] = ld_f32(b + n);
+      if (EPI == EPI_GATED) bu[0] = ld_f32(b + a.half + n);
     }
-    if (a.z) {
-      stage_put(tag, s, lane, v);
-      __syncwarp();
-      stage_store<T>(s, lane, a.z, a.Z, m0, a.M, n0, a.N, vec);
-      __syncwarp();
-      if (EPI == EPI_GATED) {
-        stage_put(tag, s, lane, u);
-        __syncwarp();
-        stage_store<T>(s, lane, a.z, a.Z, m0, a.M, a.half + n0, a.half + a.N, vec);
-        __syncwarp();
-      }
-    }
+  }
+
+  __device__ __forceinline__ static void activate_all(int act, float* v, const float* u) {
     if (EPI == EPI_GATED) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = v[j] * sigmoid<FULL>(v[j]) * u[j];
-    } else if (a.act == SA_ACT_RELU) {
+      for (int j = 0; j < EACH; ++j) v[j] = v[j] * sigmoid<F32>(v[j]) * u[j];
+    } else if (act == SA_ACT_RELU) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = activate<FULL>(SA_ACT_RELU, v[j]);
-    } else if (a.act == SA_ACT_GELU) {
+      for (int j = 0; j < EACH; ++j) v[j] = activate<F32>(SA_ACT_RELU, v[j]);
+    } else if (act == SA_ACT_GELU) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = activate<FULL>(SA_ACT_GELU, v[j]);
-    } else if (a.act == SA_ACT_SILU) {
+      for (int j = 0; j < EACH; ++j) v[j] = activate<F32>(SA_ACT_GELU, v[j]);
+    } else if (act == SA_ACT_SILU) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = activate<FULL>(SA_ACT_SILU, v[j]);
-    }
-    if (a.r) {
-      res.put(a, s, lane, m0, n0);
-      __syncwarp();
-      stage_add(tag, s, lane, v);
-      __syncwarp();
+      for (int j = 0; j < EACH; ++j) v[j] = activate<F32>(SA_ACT_SILU, v[j]);
     }
   }
-  stage_put(tag, s, lane, v);
-  __syncwarp();
-  stage_store<T>(s, lane, a.y, a.N, m0, a.M, n0, a.N, vec);
-  __syncwarp();
-}
+
+  __device__ __forceinline__ static void read(const char* s, int row, int first, float* v) {
+#pragma unroll
+    for (int p = 0; p < EACH / 4; ++p) {
+      const float4 f = *reinterpret_cast<const float4*>(s + stage_at(row, first + p));
+      v[4 * p] = f.x, v[4 * p + 1] = f.y, v[4 * p + 2] = f.z, v[4 * p + 3] = f.w;
+    }
+  }
+
+  // Rows m0 .. m0 + 31, columns n0 .. n0 + COLS - 1 of y, of the sums in the stage(s).
+  __device__ __forceinline__ void finish(const TcArgs& a, const char* s, int lane, int64_t m0, int n0) const {
+    const char* su = STAGES == 2 ? s + kStageBytes : s;
+    constexpr int U = STAGES == 2 ? 0 : COLS / 4;  // the other half's first piece
+    if (a.vec & 1) {
+      const int p = lane % LANES, n = n0 + p * EACH;
+      const bool res = EPI != EPI_PLAIN && a.r, res_vec = (a.vec & 2) != 0;
+      int64_t m = m0 + lane / LANES;
+      T* y = static_cast<T*>(a.y) + m * a.N + n;
+      T* z = static_cast<T*>(a.z) + m * a.Z + n;
+      const T* r = static_cast<const T*>(a.r) + m * a.r_stride + n;
+      float next[EACH];  // the next row's residual, on its way
+      auto fetch = [&](int64_t at) {
+        if (at >= a.M || n >= a.N) return;
+        if (res_vec) {
+          load16(r, next);
+        } else {
+#pragma unroll
+          for (int j = 0; j < EACH; ++j) next[j] = ld_nc(r + j);
+        }
+      };
+      if (res) fetch(m);
+      // fp32 activations are long: few copies of them, or the instruction cache overflows
+#pragma unroll(F32 ? 1 : LANES)
+      for (int i = 0; i < LANES; ++i) {
+        const int row = i * ROWS + lane / LANES;
+        const bool here = m < a.M && n < a.N;
+        float v[EACH], u[EACH], rv[EACH];
+        if (EPI != EPI_PLAIN && res) {
+#pragma unroll
+          for (int j = 0; j < EACH; ++j) rv[j] = next[j];
+          r += int64_t(ROWS) * a.r_stride;
+          if (i + 1 < LANES) fetch(m + ROWS);
+        }
+        read(s, row, p * (EACH / 4), v);
+        if (EPI == EPI_GATED) read(su, row, U + p * (EACH / 4), u);
+        if (EPI != EPI_PLAIN) {
+#pragma unroll
+          for (int j = 0; j < EACH; ++j) {
+            v[j] += bv[j];
+            if (EPI == EPI_GATED) u[j] += bu[j];
+          }
+          if (a.z && here) {
+            store16(z, v);
+            if (EPI == EPI_GATED) store16(z + a.half, u);
+          }
+          activate_all(a.act, v, u);
+          if (res) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) v[j] += rv[j];
+          }
+        }
+        if (here) store16(y, v);
+        m += ROWS;
+        y += int64_t(ROWS) * a.N;
+        if (EPI != EPI_PLAIN) z += int64_t(ROWS) * a.Z;
+      }
+    } else {  // one value a lane, so that single-element accesses coalesce; four rows at a time
+      const int c = lane % COLS, n = n0 + c;
+      constexpr int AT_ONCE = 32 / COLS;
+      const bool res = EPI != EPI_PLAIN && a.r;
+      float next[4];
+      auto fetch = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t m = m0 + (i + k) * AT_ONCE + lane / COLS;
+          next[k] = m < a.M && n < a.N ? ld_nc(static_cast<const T*>(a.r) + m * a.r_stride + n) : 0.f;
+        }
+      };
+      if (res) fetch(0);
+#pragma unroll 1
+      for (int i = 0; i < COLS; i += 4) {
+        float rv[4] = {0.f, 0.f, 0.f, 0.f};
+        if (res) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) rv[k] = next[k];
+          if (i + 4 < COLS) fetch(i + 4);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int row = (i + k) * AT_ONCE + lane / COLS;
+          const int64_t m = m0 + row;
+          const bool here = m < a.M && n < a.N;
+          float v = *reinterpret_cast<const float*>(s + stage_at(row, c / 4) + c % 4 * 4), u = 0.f;
+          if (EPI == EPI_GATED) u = *reinterpret_cast<const float*>(su + stage_at(row, U + c / 4) + c % 4 * 4);
+          if (EPI != EPI_PLAIN) {
+            v += bv[0];
+            if (EPI == EPI_GATED) u += bu[0];
+            if (a.z && here) {
+              st_from_f32(static_cast<T*>(a.z) + m * a.Z + n, v);
+              if (EPI == EPI_GATED) st_from_f32(static_cast<T*>(a.z) + m * a.Z + a.half + n, u);
+            }
+            v = activate<F32>(EPI == EPI_GATED ? SA_ACT_SWIGLU : a.act, v);
+            if (EPI == EPI_GATED) v *= u;
+            v += rv[k];
+          }
+          if (here) st_from_f32(static_cast<T*>(a.y) + m * a.N + n, v);
+        }
+      }
+    }
+  }
+};
+
+// The end of bf16 chunks whose rows TMA can write: each lane keeps its row's 32 columns in registers to the end, and
+// every 32 x 32 result leaves through one of the warp's four buffers (64-byte rows, TMA's 64-byte swizzle).  That
+// takes a third of the shared-memory traffic of the way above.
+constexpr int kOutBytes = 2048;
+struct TmaOut {
+  char* ring;
+  float* bias;  // [64]
+  int lane, used;
+  float b0, b1;
+
+  __device__ __forceinline__ TmaOut(char* ring_, float* bias_, int lane_) : ring(ring_), bias(bias_), lane(lane_), used(0) {}
+
+  template <int EPI>
+  __device__ __forceinline__ void load_bias(const TcArgs& a, int n0) {
+    b0 = b1 = 0.f;
+    if (EPI == EPI_PLAIN || !a.bias || n0 + lane >= a.N) return;
+    const __nv_bfloat16* b = static_cast<const __nv_bfloat16*>(a.bias) + n0 + lane;
+    b0 = ld_nc(b);
+    if (EPI == EPI_GATED) b1 = ld_nc(b + a.half);
+  }
+  // the next buffer, once its last store has read it
+  __device__ __forceinline__ char* next() {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
+    __syncwarp();
+    return ring + (used++ & 3) * kOutBytes;
+  }
+  __device__ __forceinline__ static uint32_t at(int row, int p) { return row * 64 + ((p ^ ((row >> 1) & 3)) << 4); }
+  __device__ __forceinline__ void put(char* s, const float* v) const {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) store8(reinterpret_cast<__nv_bfloat16*>(s + at(lane, p)), v + 8 * p);
+  }
+  __device__ __forceinline__ void send(const CUtensorMap& map, const char* s, bool here, int n0, int64_t m0, int half) const {
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      if (here) ptx::tma_store_3d(&map, ptx::smem_u32(s), n0, half, int(m0));
+      ptx::bulk_commit_group();  // an empty group counts too
+    }
+  }
+
+  template <int EPI>
+  __device__ __forceinline__ void finish(const TcArgs& a, const CUtensorMap& ty, const CUtensorMap& tz, float* v, float* u,
+                                         int64_t m0, int n0) {
+    const bool here = m0 < a.M && n0 < a.N;
+    if (EPI != EPI_PLAIN) {
+      uint4 res[4];
+      const bool direct = a.r && (a.vec & 2);
+      if (direct) {  // whole rows a few lanes, on their way meanwhile
+        const int n = n0 + lane % 4 * 8;
+        const __nv_bfloat16* r = static_cast<const __nv_bfloat16*>(a.r) + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t m = m0 + i * 8 + lane / 4;
+          res[i] = make_uint4(0, 0, 0, 0);
+          if (m < a.M && n < a.N) res[i] = __ldg(reinterpret_cast<const uint4*>(r + m * a.r_stride));
+        }
+      }
+      if (a.bias) {
+        bias[lane] = b0;
+        if (EPI == EPI_GATED) bias[32 + lane] = b1;
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(bias + j);
+          v[j] += b.x, v[j + 1] += b.y, v[j + 2] += b.z, v[j + 3] += b.w;
+          if (EPI == EPI_GATED) {
+            const float4 c = *reinterpret_cast<const float4*>(bias + 32 + j);
+            u[j] += c.x, u[j + 1] += c.y, u[j + 2] += c.z, u[j + 3] += c.w;
+          }
+        }
+      }
+      if (a.z) {
+        char* s = next();
+        put(s, v);
+        send(tz, s, here, n0, m0, 0);
+        if (EPI == EPI_GATED) {
+          s = next();
+          put(s, u);
+          send(tz, s, here, n0, m0, 1);
+        }
+      }
+      if (EPI == EPI_GATED) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = v[j] * sigmoid<false>(v[j]) * u[j];
+      } else if (a.act == SA_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_RELU, v[j]);
+      } else if (a.act == SA_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_GELU, v[j]);
+      } else if (a.act == SA_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_SILU, v[j]);
+      }
+      if (a.r) {
+        char* s = next();
+        if (direct) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(s + at(i * 8 + lane / 4, lane % 4)) = res[i];
+        } else {
+          const __nv_bfloat16* r = static_cast<const __nv_bfloat16*>(a.r) + n0 + lane;
+#pragma unroll 8
+          for (int i = 0; i < 32; ++i)
+            *reinterpret_cast<__nv_bfloat16*>(s + at(i, lane / 8) + lane % 8 * 2) =
+                __float2bfloat16_rn(m0 + i < a.M && n0 + lane < a.N ? ld_nc(r + (m0 + i) * a.r_stride) : 0.f);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          float w[8];
+          load8(reinterpret_cast<const __nv_bfloat16*>(s + at(lane, p)), w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[8 * p + j] += w[j];
+        }
+        put(s, v);  // each lane its own row
+        send(ty, s, here, n0, m0, 0);
+        return;
+      }
+    }
+    char* s = next();
+    put(s, v);
+    send(ty, s, here, n0, m0, 0);
+  }
+  __device__ __forceinline__ void done() const {
+    if (lane == 0) ptx::bulk_wait_all();
+  }
+};
 
 }  // namespace dense
 }  // namespace sa
