@@ -58,9 +58,13 @@ struct GemmArgs {
   sa_dtype dt;
   void* y;
   void* z;
+  void* ws;  // launch_rows: the call's status, cleared
 };
 
 cudaError_t launch_simt_gemm(const GemmArgs& g, cudaStream_t st);
+constexpr int kMostFewRows = 16;
+// y for at most kMostFewRows rows of x
+cudaError_t launch_rows(const GemmArgs& g, cudaStream_t st);
 
 // dz = dy act'(z) as [M, Z] rows of type dt, `pitch` elements apart (dz NULL: not stored), and
 // column sums of the unrounded dz into partial[g * Z + c] (NULL: none).

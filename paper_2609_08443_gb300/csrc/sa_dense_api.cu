@@ -79,6 +79,9 @@ struct Layout {
   bool side;
 };
 
+// A product of this many rows of x is a matter of reading W (sa_dense_rows.cu), and takes no workspace on any path.
+bool few_rows(const Linear& l) { return l.M <= sa::dense::kMostFewRows; }
+
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
 
 Layout linear_layout(const Linear& l, bool bwd, int repack) {
@@ -92,10 +95,13 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
     return at;
   };
   const size_t each = f32 ? 6 : 2;  // bytes of an element's terms
+  if (!bwd && few_rows(l)) repack = 0;
   s.x = section(repack & COPY_X, size_t(l.M) * pitch_of(l.K) * each);
   s.w = section(repack & COPY_W, size_t(l.Z) * pitch_of(l.K) * each);
   size_t piece = 0;
-  if (!bwd) {
+  if (!bwd && few_rows(l)) {
+    // no workspace but the status
+  } else if (!bwd) {
     s.plan = sa::dense::tc_plan(l.M, l.N, l.K, l.act == SA_ACT_SWIGLU, f32);
     piece = s.plan.piece_bytes;
   } else {
@@ -114,6 +120,7 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
   s.total = off;
   return s;
 }
+
 
 bool on_tensor_cores() { return sa::tc_path_enabled() && sa::tcc::device_is_sm103(); }
 
@@ -231,8 +238,10 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* w, int64_t 
   SA_TRY(check_workspace(workspace, ws_bytes, lay.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* base = static_cast<char*>(workspace);
-  if (M == 0 || !on_tensor_cores()) {
-    if (cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
+  const bool few = few_rows(l);
+  if (M == 0 || few || !on_tensor_cores()) {
+    const bool rows = few && sa::tc_path_enabled();
+    if ((M == 0 || !rows) && cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
     if (M == 0) return SA_OK;
     sa::dense::GemmArgs g{};
     g.A = x;
@@ -250,8 +259,9 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* w, int64_t 
     g.dt = dt;
     g.y = y;
     g.z = z;
+    g.ws = workspace;
     sa::count_launches(1);
-    return status(sa::dense::launch_simt_gemm(g, st));
+    return status(rows ? sa::dense::launch_rows(g, st) : sa::dense::launch_simt_gemm(g, st));
   }
   int launches = 0;
   sa::dense::TcGemm g{};
@@ -388,6 +398,8 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
 
 const char* sa_linear_kernel_name(int64_t M, int N, int K, sa_act act, sa_dtype dt, int pass) {
   if (!linear_sizes_ok(M, N, K, act, dt) || pass < 0 || pass > 2) return "unsupported";
+  if (pass == 0 && M <= sa::dense::kMostFewRows && sa::tc_path_enabled())
+    return dt == SA_BF16 ? "mma_linear_rows" : "linear_rows";
   if (!on_tensor_cores()) return "simt_linear";
   const int64_t Z = act == SA_ACT_SWIGLU ? 2 * int64_t(N) : N;
   const bool f32 = dt == SA_F32;

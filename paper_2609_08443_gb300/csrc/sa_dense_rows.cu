@@ -1,0 +1,246 @@
+// Linear layers for at most 16 rows of x (single tokens, a small request): y = act(x W^T + b) + r.
+//
+// Bound by reading W once, so W goes from memory straight into registers: a block makes a few columns of y for
+// all rows of x, its eight warps each take an eighth of k (64 or 128 elements in turn), and their sums meet in
+// shared memory, in order.
+//   bf16: 16 rows of W against 8 or 16 rows of x with warp-level products (m16n8k16).  Which k an element of a fragment
+//         stands for does not matter as long as both operands agree, so a thread takes 8 neighbours of a row
+//         of W and the same 8 of a row of x, and uses them in two products.
+//   fp32: 4 (2) rows of W against 8 (16) rows of x with multiply-adds.
+#include "sa_dense_act.cuh"
+
+namespace sa {
+namespace dense {
+namespace {
+
+constexpr int kWarps = 8;
+
+// 16 bytes of W, which nobody reads again soon
+__device__ __forceinline__ uint4 stream16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+
+// Eight bf16 from k on (zeros behind K)
+template <bool VEC, bool ONCE>
+__device__ __forceinline__ uint4 take8(const __nv_bfloat16* row, int k, int K) {
+  if (VEC) {
+    if (k >= K) return make_uint4(0, 0, 0, 0);
+    return ONCE ? stream16(row + k) : __ldg(reinterpret_cast<const uint4*>(row + k));
+  }
+  const unsigned short* p = reinterpret_cast<const unsigned short*>(row) + k;
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t lo = k + 2 * j < K ? __ldg(p + 2 * j) : 0, hi = k + 2 * j + 1 < K ? __ldg(p + 2 * j + 1) : 0;
+    w[j] = lo | hi << 16;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <bool VEC, bool ONCE>
+__device__ __forceinline__ float4 take4(const float* row, int k, int K) {
+  if (VEC) {
+    if (k >= K) return make_float4(0, 0, 0, 0);
+    if (!ONCE) return __ldg(reinterpret_cast<const float4*>(row + k));
+    const uint4 u = stream16(row + k);
+    return make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+  }
+  float4 v;
+  v.x = k < K ? __ldg(row + k) : 0.f;
+  v.y = k + 1 < K ? __ldg(row + k + 1) : 0.f;
+  v.z = k + 2 < K ? __ldg(row + k + 2) : 0.f;
+  v.w = k + 3 < K ? __ldg(row + k + 3) : 0.f;
+  return v;
+}
+
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The end of y[m, n] (z: the sums of both halves for SwiGLU)
+template <typename T, bool GATED>
+__device__ __forceinline__ void end_one(const GemmArgs& a, int64_t m, int n, float z0, float z1) {
+  constexpr bool FULL = sizeof(T) == 4;
+  const int64_t Z = GATED ? 2 * int64_t(a.N) : a.N;
+  if (a.bias) {
+    z0 += ld_f32(static_cast<const T*>(a.bias) + n);
+    if (GATED) z1 += ld_f32(static_cast<const T*>(a.bias) + a.N + n);
+  }
+  if (a.z) {
+    st_from_f32(static_cast<T*>(a.z) + m * Z + n, z0);
+    if (GATED) st_from_f32(static_cast<T*>(a.z) + m * Z + a.N + n, z1);
+  }
+  float y = activate<FULL>(a.act, z0);
+  if (GATED) y *= z1;
+  if (a.r.p) y += ld_f32(static_cast<const T*>(a.r.p) + m * a.r.stride + n);
+  st_from_f32(static_cast<T*>(a.y) + m * a.N + n, y);
+}
+
+__device__ __forceinline__ void clear_status(const GemmArgs& a) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    ws_header(a.ws)->err = 0;
+    ws_header(a.ws)->timeout_site = 0;
+  }
+}
+
+// MT: tiles of 8 rows of x, RT: tiles of 16 rows of W
+template <int MT, int RT, bool GATED, bool VEC>
+__global__ void __launch_bounds__(256, 2) rows_bf16_kernel(const GemmArgs a) {
+  constexpr int S = GATED ? 2 : 1, U = RT == 1 ? 2 : 1;  // U: steps in flight
+  __shared__ float sums[kWarps][S][MT][RT * 16][8];
+  clear_status(a);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.x * 16 * RT, K = int(a.K), M = int(a.M);
+  const __nv_bfloat16* W = static_cast<const __nv_bfloat16*>(a.B);
+  const __nv_bfloat16* X = static_cast<const __nv_bfloat16*>(a.A);
+  // rows behind the last are read as the last, and not written
+  const __nv_bfloat16 *w[S][2 * RT], *x[MT];
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int i = 0; i < 2 * RT; ++i) {
+      const int n = n0 + g + 8 * i < a.N ? n0 + g + 8 * i : a.N - 1;
+      w[s][i] = W + (int64_t(s) * a.N + n) * a.b_n;
+    }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) x[i] = X + int64_t(i * 8 + g < M ? i * 8 + g : M - 1) * a.a_m;
+  float acc[S][RT][MT][4] = {};
+  for (int k0 = warp * 64; k0 < K; k0 += U * kWarps * 64) {
+    uint4 wv[U][2][S][2 * RT], xv[U][2][MT];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int k = k0 + u * kWarps * 64 + c * 32 + 8 * t;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int i = 0; i < 2 * RT; ++i) wv[u][c][s][i] = take8<VEC, true>(w[s][i], k, K);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xv[u][c][i] = take8<VEC, false>(x[i], k, K);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              const uint4 p = wv[u][c][s][2 * r], q = wv[u][c][s][2 * r + 1], b = xv[u][c][i];
+              mma16816(acc[s][r][i], p.x, q.x, p.y, q.y, b.x, b.y);
+              mma16816(acc[s][r][i], p.z, q.z, p.w, q.w, b.z, b.w);
+            }
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const float* c = acc[s][r][i];
+        *reinterpret_cast<float2*>(&sums[warp][s][i][r * 16 + g][2 * t]) = make_float2(c[0], c[1]);
+        *reinterpret_cast<float2*>(&sums[warp][s][i][r * 16 + g + 8][2 * t]) = make_float2(c[2], c[3]);
+      }
+  __syncthreads();
+  constexpr int COLS = 16 * RT;
+  for (int e = threadIdx.x; e < COLS * 8 * MT; e += 256) {
+    const int n = e % COLS, m = e / COLS;
+    if (m >= M || n0 + n >= a.N) continue;
+    float z[2] = {0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int v = 0; v < kWarps; ++v) z[s] += sums[v][s][m / 8][n][m % 8];
+    end_one<__nv_bfloat16, GATED>(a, m, n0 + n, z[0], z[1]);
+  }
+}
+
+// R rows of W (of each half) against MT rows of x
+template <int R, int MT, bool GATED, bool VEC>
+__global__ void __launch_bounds__(256, 2) rows_f32_kernel(const GemmArgs a) {
+  constexpr int S = GATED ? 2 : 1, RS = R / S;  // columns of y
+  __shared__ float sums[kWarps][R][MT];
+  clear_status(a);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n0 = blockIdx.x * RS, K = int(a.K), M = int(a.M);
+  const float *w[R], *x[MT];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int n = n0 + i % RS < a.N ? n0 + i % RS : a.N - 1;
+    w[i] = static_cast<const float*>(a.B) + (int64_t(i / RS) * a.N + n) * a.b_n;
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) x[i] = static_cast<const float*>(a.A) + int64_t(i < M ? i : M - 1) * a.a_m;
+  float acc[R][MT] = {};
+  for (int k = warp * 128 + 4 * lane; k - 4 * lane < K; k += kWarps * 128) {
+    float4 wv[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) wv[i] = take4<VEC, true>(w[i], k, K);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      const float4 xv = take4<VEC, false>(x[j], k, K);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        acc[i][j] = fmaf(wv[i].w, xv.w, fmaf(wv[i].z, xv.z, fmaf(wv[i].y, xv.y, fmaf(wv[i].x, xv.x, acc[i][j]))));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) acc[i][j] += __shfl_xor_sync(0xFFFFFFFFu, acc[i][j], o);
+      if (lane == 0) sums[warp][i][j] = acc[i][j];
+    }
+  __syncthreads();
+  const int e = threadIdx.x, n = e % RS, m = e / RS;
+  if (m < M && m < MT && n0 + n < a.N) {
+    float z[2] = {0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int v = 0; v < kWarps; ++v) z[s] += sums[v][s * RS + n][m];
+    end_one<float, GATED>(a, m, n0 + n, z[0], z[1]);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_rows(const GemmArgs& a, cudaStream_t st) {
+  const bool gated = a.act == SA_ACT_SWIGLU;
+  const int each = a.dt == SA_BF16 ? 8 : 4;
+  auto row_ok = [&](const void* p, int64_t stride) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % each == 0;
+  };
+  const bool vec = a.K % each == 0 && row_ok(a.A, a.a_m) && row_ok(a.B, a.b_n);
+  auto go = [&](auto kernel, int columns) {
+    kernel<<<unsigned((a.N + columns - 1) / columns), 256, 0, st>>>(a);
+    return cudaGetLastError();
+  };
+#define SA_PICK(K, COLS, ...)                                                                          \
+  (gated ? (vec ? go(K<__VA_ARGS__, true, true>, COLS) : go(K<__VA_ARGS__, true, false>, COLS))         \
+         : (vec ? go(K<__VA_ARGS__, false, true>, COLS) : go(K<__VA_ARGS__, false, false>, COLS)))
+  if (a.dt == SA_BF16) {
+    if (a.M <= 8) return SA_PICK(rows_bf16_kernel, 16, 1, 1);
+    // 16 rows of x are half as much to read as 32 rows of W of a SwiGLU tile: twice the rows of W where they fill the SMs
+    // (16 x 4096 -> 8192 gated: RATE)
+    return a.N >= 32 * sm_count() ? SA_PICK(rows_bf16_kernel, 32, 2, 2) : SA_PICK(rows_bf16_kernel, 16, 2, 1);
+  }
+  if (a.M <= 8) return SA_PICK(rows_f32_kernel, (gated ? 2 : 4), 4, 8);
+  return SA_PICK(rows_f32_kernel, (gated ? 1 : 2), 2, 16);
+#undef SA_PICK
+}
+
+}  // namespace dense
+}  // namespace sa

@@ -328,7 +328,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
                   stage_put<End::COLS>(out, lane, &sum[k * End::COLS / 32][HALVES - 1][k * End::COLS % 32], End::COLS / 4);
               }
             __syncwarp();
-            end.finish(a, out, lane, m0, n0);
+            end.template finish<1>(a, out, out, lane, m0, n0, 0);
             __syncwarp();
           }
         } else {
@@ -363,7 +363,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
             stage_put<32>(out, lane, v);
             if constexpr (EPI == EPI_GATED) stage_put<32>(out + kStageBytes, lane, u);
             __syncwarp();
-            end.finish(a, out, lane, m0, y0 + i * 32);
+            end.template finish<1>(a, out, out + kStageBytes, lane, m0, y0 + i * 32, 0);
             if (i + 1 < CH) end.load_bias(a, lane, y0 + i * 32 + 32);
             __syncwarp();
           } else {
@@ -410,15 +410,18 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     tc_linear_work<CTAS, true, true, F32, EPI_PLAIN>(wa, wb, wy, wy, w, worker - x.W, false);
 }
 
-// Cut tiles: one block for 32 columns of each epilogue warp's rows; pieces are added in worker order.
+// Cut tiles: a block of 16 warps ends 128 rows x 32 columns of y.  Warp (q, part) adds the pieces of the rows of q and eight
+// columns (SwiGLU: of both halves), in worker order, and after they have met in shared memory ends eight rows of q.
+constexpr int kJoinThreads = 512;
 template <int CTAS, bool F32, int EPI>
 __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   using C = TcCfg<CTAS, F32, EPI>;
   using End = typename C::End;
   using Shape = TileShape<CTAS>;
-  constexpr int YN = Shape::template YN<EPI>, CH = Shape::template CHUNKS<EPI>;
-  extern __shared__ __align__(128) char stages[];  // the warps' stages
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, h = warp >> 2;
+  constexpr int YN = Shape::template YN<EPI>, CH = 2 * Shape::template CHUNKS<EPI>;
+  constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
+  extern __shared__ __align__(128) char stages[];  // [4][HALVES][kStageBytes]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, part = warp >> 2;
   const int i = block % CH, rank = block / CH % CTAS;
   const int64_t rest = block / (CH * CTAS);
   const int64_t total = a.cut * a.KB, first = rest * a.KB, last = first + a.KB - 1;
@@ -427,73 +430,77 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   int mb, nb;
   tile_place(a, a.whole + rest, &mb, &nb);
   const int64_t m0 = int64_t(mb * CTAS + rank) * 128 + q * 32;
-  if (m0 >= a.M) return;
-  const int n0 = nb * YN + h * (YN / 2) + i * 32;
-  auto col = [&](int half) { return EPI == EPI_GATED ? half * YN + h * (YN / 2) + i * 32 : h * (C::BN / 2) + i * 32; };
+  const int n0 = nb * YN + i * 32;
+  if (m0 - q * 32 >= a.M || n0 >= a.N) return;
   End end;
   end.load_bias(a, lane, n0);
-  float v[32], u[EPI == EPI_GATED ? 32 : 1];
   const int64_t piece = int64_t(CTAS) * 128 * C::BN;
   // every worker between has a piece (none has an empty share), in its first slot but for the first, whose share may
   // begin before the tile
   const float* p0 = a.piece + int64_t(rank) * 128 * C::BN + (q * 32 + lane) * 4;
-  auto at = [&](int w) { return p0 + (int64_t(w) * 2 + (w == w0 ? partial_slot(total, a.cutters, w0, first) : 0)) * piece; };
-  auto sum = [&](float* x, int c) {
+  char* out = stages + q * HALVES * kStageBytes;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = 0.f;
-    if (m0 + lane >= a.M) return;
-    auto add = [&](const float4* f) {
+  for (int k = 0; k < HALVES; ++k) {
+    const int c = (EPI == EPI_GATED ? k * YN : 0) + i * 32 + part * 8;
+    float4 x[2] = {make_float4(0, 0, 0, 0), make_float4(0, 0, 0, 0)};
+    if (m0 + lane < a.M) {
+      auto add = [&](const float4* f) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[4 * j] += f[j].x, x[4 * j + 1] += f[j].y, x[4 * j + 2] += f[j].z, x[4 * j + 3] += f[j].w;
-    };
-    auto read = [&](int w, float4* f) {
-      const float* p = at(w) + int64_t(c / 4) * 512;
+        for (int j = 0; j < 2; ++j) x[j].x += f[j].x, x[j].y += f[j].y, x[j].z += f[j].z, x[j].w += f[j].w;
+      };
+      auto read = [&](int w, float4* f) {
+        const int slot = w == w0 ? partial_slot(total, a.cutters, w0, first) : 0;
+        const float* p = p0 + (int64_t(w) * 2 + slot) * piece + int64_t(c / 4) * 512;
+        f[0] = *reinterpret_cast<const float4*>(p);
+        f[1] = *reinterpret_cast<const float4*>(p + 512);
+      };
+      int w = w0;
+      for (; w + 7 <= w1; w += 8) {  // eight pieces in flight
+        float4 f[8][2];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = *reinterpret_cast<const float4*>(p + j * 512);
-    };
-    int w = w0;
-    for (; w + 2 <= w1; w += 3) {  // three pieces in flight
-      float4 f[3][8];
+        for (int l = 0; l < 8; ++l) read(w + l, f[l]);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) read(w + k, f[k]);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) add(f[k]);
+        for (int l = 0; l < 8; ++l) add(f[l]);
+      }
+      for (; w + 1 <= w1; w += 2) {
+        float4 f[2][2];
+        read(w, f[0]);
+        read(w + 1, f[1]);
+        add(f[0]);
+        add(f[1]);
+      }
+      if (w <= w1) {
+        float4 f[2];
+        read(w, f);
+        add(f);
+      }
     }
-    for (; w <= w1; ++w) {
-      float4 f[8];
-      read(w, f);
-      add(f);
-    }
-  };
-  sum(v, col(0));
-  if constexpr (EPI == EPI_GATED) sum(u, col(1));
-  char* out = stages + warp * End::STAGES * kStageBytes;
+    const float v[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+    if constexpr (End::COLS == 32)
+      stage_put<8>(out + k * kStageBytes, lane, v, part * 2);
+    else  // columns 0-15 of both halves in one stage, 16-31 in the next
+      stage_put<8>(out + (part >> 1) * kStageBytes, lane, v, k * 4 + (part & 1) * 2);
+  }
+  __syncthreads();
   if constexpr (End::COLS == 32) {
-    stage_put<32>(out, lane, v);
-    if constexpr (EPI == EPI_GATED) stage_put<32>(out + kStageBytes, lane, u);
-    __syncwarp();
-    end.finish(a, out, lane, m0, n0);
+    end.template finish<4>(a, out, out + kStageBytes, lane, m0, n0, part);
   } else {
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 2; ++k) {
       if (k) end.load_bias(a, lane, n0 + 16);
-      stage_put<16>(out, lane, v + 16 * k);
-      stage_put<16>(out, lane, u + 16 * k, 4);
-      __syncwarp();
-      end.finish(a, out, lane, m0, n0 + 16 * k);
-      __syncwarp();
+      end.template finish<4>(a, out + k * kStageBytes, out + k * kStageBytes, lane, m0, n0 + 16 * k, part);
     }
   }
 }
 
 template <int CTAS, bool F32, int EPI>
-__global__ void __launch_bounds__(256) tc_join_kernel(const TcArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) tc_join_kernel(const TcArgs a) {
   tc_join_work<CTAS, F32, EPI>(a, blockIdx.x);
 }
 
 // dx's cut tiles in the first `split` blocks, dW's in the rest
 template <int CTAS, bool F32>
-__global__ void __launch_bounds__(256) tc_join_grads_kernel(const TcArgs x, const TcArgs w, const int split) {
+__global__ void __launch_bounds__(kJoinThreads) tc_join_grads_kernel(const TcArgs x, const TcArgs w, const int split) {
   const bool second = int(blockIdx.x) >= split;
   tc_join_work<CTAS, F32, EPI_PLAIN>(second ? w : x, int(blockIdx.x) - (second ? split : 0));
 }
@@ -607,13 +614,9 @@ cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaSt
       launch_cluster<CTAS>(&tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>, p.W * CTAS, C::SMEM, st, ta, tb, ty, tz, a);
   ++*launches;
   if (e != cudaSuccess || p.cut == 0) return e;
-  constexpr int CH = TileShape<CTAS>::template CHUNKS<EPI>;
-  constexpr size_t stages = 8 * C::End::STAGES * kStageBytes;
-  if (stages > 48 * 1024) {
-    e = cudaFuncSetAttribute(tc_join_kernel<CTAS, F32, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(stages));
-    if (e != cudaSuccess) return e;
-  }
-  tc_join_kernel<CTAS, F32, EPI><<<unsigned(p.cut * CTAS * CH), 256, stages, st>>>(a);
+  constexpr int CH = 2 * TileShape<CTAS>::template CHUNKS<EPI>;
+  tc_join_kernel<CTAS, F32, EPI>
+      <<<unsigned(p.cut * CTAS * CH), kJoinThreads, 4 * (EPI == EPI_GATED ? 2 : 1) * kStageBytes, st>>>(a);
   ++*launches;
   return cudaGetLastError();
 }
@@ -633,9 +636,9 @@ cudaError_t launch_grads(const TcGemm& gx, const TcPlan& px, const TcArgs& x, co
                                        wb, xy, wy, x, w);
   ++*launches;
   if (e != cudaSuccess || px.cut + pw.cut == 0) return e;
-  constexpr int CH = TileShape<CTAS>::template CHUNKS<EPI_PLAIN>;
+  constexpr int CH = 2 * TileShape<CTAS>::template CHUNKS<EPI_PLAIN>;
   tc_join_grads_kernel<CTAS, F32>
-      <<<unsigned((px.cut + pw.cut) * CTAS * CH), 256, 8 * kStageBytes, st>>>(x, w, int(px.cut * CTAS * CH));
+      <<<unsigned((px.cut + pw.cut) * CTAS * CH), kJoinThreads, 4 * kStageBytes, st>>>(x, w, int(px.cut * CTAS * CH));
   ++*launches;
   return cudaGetLastError();
 }

@@ -160,14 +160,17 @@ struct ChunkEnd {
     }
   }
 
-  // Rows m0 .. m0 + 31, columns n0 .. n0 + COLS - 1 of y, of the sums in the stage(s).
-  __device__ __forceinline__ void finish(const TcArgs& a, const char* s, int lane, int64_t m0, int n0) const {
-    const char* su = STAGES == 2 ? s + kStageBytes : s;
+  // Rows m0 .. m0 + 31, columns n0 .. n0 + COLS - 1 of y, of the sums in the stage(s) (SwiGLU in bf16: the other half's in
+  // su); of PARTS, the eight rows of `part` only.
+  template <int PARTS>
+  __device__ __forceinline__ void finish(const TcArgs& a, const char* s, const char* su, int lane, int64_t m0, int n0,
+                                         int part) const {
     constexpr int U = STAGES == 2 ? 0 : COLS / 4;  // the other half's first piece
     if (a.vec & 1) {
       const int p = lane % LANES, n = n0 + p * EACH;
       const bool res = EPI != EPI_PLAIN && a.r, res_vec = (a.vec & 2) != 0;
-      int64_t m = m0 + lane / LANES;
+      const int first = part * (LANES / PARTS);
+      int64_t m = m0 + first * ROWS + lane / LANES;
       T* y = static_cast<T*>(a.y) + m * a.N + n;
       T* z = static_cast<T*>(a.z) + m * a.Z + n;
       const T* r = static_cast<const T*>(a.r) + m * a.r_stride + n;
@@ -184,15 +187,15 @@ struct ChunkEnd {
       if (res) fetch(m);
       // fp32 activations are long: few copies of them, or the instruction cache overflows
 #pragma unroll(F32 ? 1 : LANES)
-      for (int i = 0; i < LANES; ++i) {
-        const int row = i * ROWS + lane / LANES;
+      for (int i = 0; i < LANES / PARTS; ++i) {
+        const int row = (first + i) * ROWS + lane / LANES;
         const bool here = m < a.M && n < a.N;
         float v[EACH], u[EACH], rv[EACH];
         if (EPI != EPI_PLAIN && res) {
 #pragma unroll
           for (int j = 0; j < EACH; ++j) rv[j] = next[j];
           r += int64_t(ROWS) * a.r_stride;
-          if (i + 1 < LANES) fetch(m + ROWS);
+          if (i + 1 < LANES / PARTS) fetch(m + ROWS);
         }
         read(s, row, p * (EACH / 4), v);
         if (EPI == EPI_GATED) read(su, row, U + p * (EACH / 4), u);
@@ -229,14 +232,15 @@ struct ChunkEnd {
           next[k] = m < a.M && n < a.N ? ld_nc(static_cast<const T*>(a.r) + m * a.r_stride + n) : 0.f;
         }
       };
-      if (res) fetch(0);
+      const int begin = part * (COLS / PARTS), stop = begin + COLS / PARTS;
+      if (res) fetch(begin);
 #pragma unroll 1
-      for (int i = 0; i < COLS; i += 4) {
+      for (int i = begin; i < stop; i += 4) {
         float rv[4] = {0.f, 0.f, 0.f, 0.f};
         if (res) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) rv[k] = next[k];
-          if (i + 4 < COLS) fetch(i + 4);
+          if (i + 4 < stop) fetch(i + 4);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
