@@ -91,30 +91,30 @@ __device__ __forceinline__ void clear_status(const GemmArgs& a) {
   }
 }
 
-// MT: tiles of 8 rows of x, RT: tiles of 16 rows of W
-template <int MT, int RT, bool GATED, bool VEC>
+// MT: tiles of 8 rows of x
+template <int MT, bool GATED, bool VEC>
 __global__ void __launch_bounds__(256, 2) rows_bf16_kernel(const GemmArgs a) {
-  constexpr int S = GATED ? 2 : 1, U = RT == 1 ? 2 : 1;  // U: steps in flight
-  __shared__ float sums[kWarps][S][MT][RT * 16][8];
+  constexpr int S = GATED ? 2 : 1, U = 2;  // U: steps in flight
+  __shared__ float sums[kWarps][S][MT][16][8];
   clear_status(a);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int n0 = blockIdx.x * 16 * RT, K = int(a.K), M = int(a.M);
+  const int n0 = blockIdx.x * 16, K = int(a.K), M = int(a.M);
   const __nv_bfloat16* W = static_cast<const __nv_bfloat16*>(a.B);
   const __nv_bfloat16* X = static_cast<const __nv_bfloat16*>(a.A);
   // rows behind the last are read as the last, and not written
-  const __nv_bfloat16 *w[S][2 * RT], *x[MT];
+  const __nv_bfloat16 *w[S][2], *x[MT];
 #pragma unroll
   for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int i = 0; i < 2 * RT; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const int n = n0 + g + 8 * i < a.N ? n0 + g + 8 * i : a.N - 1;
       w[s][i] = W + (int64_t(s) * a.N + n) * a.b_n;
     }
 #pragma unroll
   for (int i = 0; i < MT; ++i) x[i] = X + int64_t(i * 8 + g < M ? i * 8 + g : M - 1) * a.a_m;
-  float acc[S][RT][MT][4] = {};
+  float acc[S][MT][4] = {};
   for (int k0 = warp * 64; k0 < K; k0 += U * kWarps * 64) {
-    uint4 wv[U][2][S][2 * RT], xv[U][2][MT];
+    uint4 wv[U][2][S][2], xv[U][2][MT];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(256, 2) rows_bf16_kernel(const GemmArgs a) {
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
-          for (int i = 0; i < 2 * RT; ++i) wv[u][c][s][i] = take8<VEC, true>(w[s][i], k, K);
+          for (int i = 0; i < 2; ++i) wv[u][c][s][i] = take8<VEC, true>(w[s][i], k, K);
 #pragma unroll
         for (int i = 0; i < MT; ++i) xv[u][c][i] = take8<VEC, false>(x[i], k, K);
       }
@@ -134,29 +134,23 @@ __global__ void __launch_bounds__(256, 2) rows_bf16_kernel(const GemmArgs a) {
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
-          for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-              const uint4 p = wv[u][c][s][2 * r], q = wv[u][c][s][2 * r + 1], b = xv[u][c][i];
-              mma16816(acc[s][r][i], p.x, q.x, p.y, q.y, b.x, b.y);
-              mma16816(acc[s][r][i], p.z, q.z, p.w, q.w, b.z, b.w);
-            }
+          for (int i = 0; i < MT; ++i) {
+            const uint4 p = wv[u][c][s][0], q = wv[u][c][s][1], b = xv[u][c][i];
+            mma16816(acc[s][i], p.x, q.x, p.y, q.y, b.x, b.y);
+            mma16816(acc[s][i], p.z, q.z, p.w, q.w, b.z, b.w);
+          }
   }
 #pragma unroll
   for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const float* c = acc[s][r][i];
-        *reinterpret_cast<float2*>(&sums[warp][s][i][r * 16 + g][2 * t]) = make_float2(c[0], c[1]);
-        *reinterpret_cast<float2*>(&sums[warp][s][i][r * 16 + g + 8][2 * t]) = make_float2(c[2], c[3]);
-      }
+    for (int i = 0; i < MT; ++i) {
+      const float* c = acc[s][i];
+      *reinterpret_cast<float2*>(&sums[warp][s][i][g][2 * t]) = make_float2(c[0], c[1]);
+      *reinterpret_cast<float2*>(&sums[warp][s][i][g + 8][2 * t]) = make_float2(c[2], c[3]);
+    }
   __syncthreads();
-  constexpr int COLS = 16 * RT;
-  for (int e = threadIdx.x; e < COLS * 8 * MT; e += 256) {
-    const int n = e % COLS, m = e / COLS;
-    if (m >= M || n0 + n >= a.N) continue;
+  const int e = threadIdx.x, n = e % 16, m = e / 16;  // 16 columns of up to 16 rows
+  if (m < M && m < 8 * MT && n0 + n < a.N) {
     float z[2] = {0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < S; ++s)
@@ -231,12 +225,7 @@ cudaError_t launch_rows(const GemmArgs& a, cudaStream_t st) {
 #define SA_PICK(K, COLS, ...)                                                                          \
   (gated ? (vec ? go(K<__VA_ARGS__, true, true>, COLS) : go(K<__VA_ARGS__, true, false>, COLS))         \
          : (vec ? go(K<__VA_ARGS__, false, true>, COLS) : go(K<__VA_ARGS__, false, false>, COLS)))
-  if (a.dt == SA_BF16) {
-    if (a.M <= 8) return SA_PICK(rows_bf16_kernel, 16, 1, 1);
-    // 16 rows of x are half as much to read as 32 rows of W of a SwiGLU tile: twice the rows of W where they fill the SMs
-    // (16 x 4096 -> 8192 gated: RATE)
-    return a.N >= 32 * sm_count() ? SA_PICK(rows_bf16_kernel, 32, 2, 2) : SA_PICK(rows_bf16_kernel, 16, 2, 1);
-  }
+  if (a.dt == SA_BF16) return a.M <= 8 ? SA_PICK(rows_bf16_kernel, 16, 1) : SA_PICK(rows_bf16_kernel, 16, 2);
   if (a.M <= 8) return SA_PICK(rows_f32_kernel, (gated ? 2 : 4), 4, 8);
   return SA_PICK(rows_f32_kernel, (gated ? 1 : 2), 2, 16);
 #undef SA_PICK

@@ -39,8 +39,8 @@ struct TcCfg {
   using End = ChunkEnd<T, EPI>;
   static constexpr int PLANES = F32 ? 3 : 1;
   static constexpr int STAGE = 2 * PLANES * kBlockBytes;
-  static constexpr int OUT = F32 ? kStageBytes : 4 * kOutBytes;  // of an epilogue warp
-  static constexpr int STAGES = F32 ? 2 : 5;
+  static constexpr int OUT = F32 ? kStageBytes : TmaOut<EPI>::BUFFERS * kOutBytes;  // of an epilogue warp
+  static constexpr int STAGES = F32 ? 2 : EPI == EPI_GATED ? 4 : 5;
   static constexpr int BN = TileShape<CTAS>::BN;
   static constexpr int TMEM = 2 * BN;
   static constexpr int OFF_OUT = STAGES * STAGE;
@@ -248,7 +248,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     const uint32_t lanes = uint32_t(q * 32) << 16;
     const uint32_t lead_empty = CTAS == 2 ? mapa_shared(acc_empty(0), 0) : acc_empty(0);
     constexpr int CH = Shape::template CHUNKS<EPI>;
-    TmaOut outs(out, reinterpret_cast<float*>(smem + C::OFF_BIAS) + e * 64, lane);
+    TmaOut<EPI> outs(out, reinterpret_cast<float*>(smem + C::OFF_BIAS) + e * 64, lane);
     Segments seg(a, worker);
     uint32_t g = 0;  // sets of accumulators used
     bool ok = true;
@@ -341,7 +341,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         const bool tma = (a.vec & 1) != 0;
         if (complete) {
           if (tma)
-            outs.template load_bias<EPI>(a, y0);
+            outs.load_bias(a, y0);
           else
             end.load_bias(a, lane, y0);
         }
@@ -357,8 +357,8 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           tmem_ld_wait();
           if (i == CH - 1) release(set);
           if (complete && tma) {
-            outs.template finish<EPI>(a, ty, tz, v, u, m0, y0 + i * 32);
-            if (i + 1 < CH) outs.template load_bias<EPI>(a, y0 + i * 32 + 32);
+            outs.finish(a, ty, tz, v, u, m0, y0 + i * 32);
+            if (i + 1 < CH) outs.load_bias(a, y0 + i * 32 + 32);
           } else if (complete) {
             stage_put<32>(out, lane, v);
             if constexpr (EPI == EPI_GATED) stage_put<32>(out + kStageBytes, lane, u);
@@ -455,25 +455,20 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
         f[1] = *reinterpret_cast<const float4*>(p + 512);
       };
       int w = w0;
-      for (; w + 7 <= w1; w += 8) {  // eight pieces in flight
-        float4 f[8][2];
+      for (; w + 3 <= w1; w += 4) {  // four pieces in flight
+        float4 f[4][2];
 #pragma unroll
-        for (int l = 0; l < 8; ++l) read(w + l, f[l]);
+        for (int l = 0; l < 4; ++l) read(w + l, f[l]);
 #pragma unroll
-        for (int l = 0; l < 8; ++l) add(f[l]);
+        for (int l = 0; l < 4; ++l) add(f[l]);
       }
-      for (; w + 1 <= w1; w += 2) {
-        float4 f[2][2];
-        read(w, f[0]);
-        read(w + 1, f[1]);
-        add(f[0]);
-        add(f[1]);
-      }
-      if (w <= w1) {
-        float4 f[2];
-        read(w, f);
-        add(f);
-      }
+      float4 f[3][2];
+#pragma unroll
+      for (int l = 0; l < 3; ++l)
+        if (w + l <= w1) read(w + l, f[l]);
+#pragma unroll
+      for (int l = 0; l < 3; ++l)
+        if (w + l <= w1) add(f[l]);
     }
     const float v[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
     if constexpr (End::COLS == 32)
@@ -494,13 +489,13 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
 }
 
 template <int CTAS, bool F32, int EPI>
-__global__ void __launch_bounds__(kJoinThreads) tc_join_kernel(const TcArgs a) {
+__global__ void __launch_bounds__(kJoinThreads, EPI == EPI_GATED ? 1 : 2) tc_join_kernel(const TcArgs a) {
   tc_join_work<CTAS, F32, EPI>(a, blockIdx.x);
 }
 
 // dx's cut tiles in the first `split` blocks, dW's in the rest
 template <int CTAS, bool F32>
-__global__ void __launch_bounds__(kJoinThreads) tc_join_grads_kernel(const TcArgs x, const TcArgs w, const int split) {
+__global__ void __launch_bounds__(kJoinThreads, 2) tc_join_grads_kernel(const TcArgs x, const TcArgs w, const int split) {
   const bool second = int(blockIdx.x) >= split;
   tc_join_work<CTAS, F32, EPI_PLAIN>(second ? w : x, int(blockIdx.x) - (second ? split : 0));
 }

@@ -268,10 +268,13 @@ struct ChunkEnd {
 };
 
 // The end of bf16 chunks whose rows TMA can write: each lane keeps its row's 32 columns in registers to the end, and
-// every 32 x 32 result leaves through one of the warp's four buffers (64-byte rows, TMA's 64-byte swizzle).  That
-// takes a third of the shared-memory traffic of the way above.
+// a chunk's 32 x 32 results (z, SwiGLU's other half of z, y) leave together from one of two sets of buffers (64-byte
+// rows, TMA's 64-byte swizzle).  That takes a third of the shared-memory traffic of the way above.
 constexpr int kOutBytes = 2048;
+template <int EPI>
 struct TmaOut {
+  static constexpr int SET = EPI == EPI_GATED ? 3 : EPI == EPI_FULL ? 2 : 1;  // results of a chunk
+  static constexpr int BUFFERS = EPI == EPI_GATED ? 6 : 4;  // two sets at least (and two whole stages, for unaligned rows)
   char* ring;
   float* bias;  // [64]
   int lane, used;
@@ -279,7 +282,6 @@ struct TmaOut {
 
   __device__ __forceinline__ TmaOut(char* ring_, float* bias_, int lane_) : ring(ring_), bias(bias_), lane(lane_), used(0) {}
 
-  template <int EPI>
   __device__ __forceinline__ void load_bias(const TcArgs& a, int n0) {
     b0 = b1 = 0.f;
     if (EPI == EPI_PLAIN || !a.bias || n0 + lane >= a.N) return;
@@ -287,30 +289,18 @@ struct TmaOut {
     b0 = ld_nc(b);
     if (EPI == EPI_GATED) b1 = ld_nc(b + a.half);
   }
-  // the next buffer, once its last store has read it
-  __device__ __forceinline__ char* next() {
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
-    __syncwarp();
-    return ring + (used++ & 3) * kOutBytes;
-  }
   __device__ __forceinline__ static uint32_t at(int row, int p) { return row * 64 + ((p ^ ((row >> 1) & 3)) << 4); }
   __device__ __forceinline__ void put(char* s, const float* v) const {
 #pragma unroll
     for (int p = 0; p < 4; ++p) store8(reinterpret_cast<__nv_bfloat16*>(s + at(lane, p)), v + 8 * p);
   }
-  __device__ __forceinline__ void send(const CUtensorMap& map, const char* s, bool here, int n0, int64_t m0, int half) const {
-    ptx::fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      if (here) ptx::tma_store_3d(&map, ptx::smem_u32(s), n0, half, int(m0));
-      ptx::bulk_commit_group();  // an empty group counts too
-    }
-  }
 
-  template <int EPI>
   __device__ __forceinline__ void finish(const TcArgs& a, const CUtensorMap& ty, const CUtensorMap& tz, float* v, float* u,
                                          int64_t m0, int n0) {
-    const bool here = m0 < a.M && n0 < a.N;
+    // the set of the chunk before last, once its stores have read it
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    __syncwarp();
+    char* s = ring + (used ^= 1) * SET * kOutBytes;  // y, then z's halves
     if (EPI != EPI_PLAIN) {
       uint4 res[4];
       const bool direct = a.r && (a.vec & 2);
@@ -339,14 +329,8 @@ struct TmaOut {
         }
       }
       if (a.z) {
-        char* s = next();
-        put(s, v);
-        send(tz, s, here, n0, m0, 0);
-        if (EPI == EPI_GATED) {
-          s = next();
-          put(s, u);
-          send(tz, s, here, n0, m0, 1);
-        }
+        put(s + kOutBytes, v);
+        if (EPI == EPI_GATED) put(s + 2 * kOutBytes, u);
       }
       if (EPI == EPI_GATED) {
 #pragma unroll
@@ -362,7 +346,6 @@ struct TmaOut {
         for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_SILU, v[j]);
       }
       if (a.r) {
-        char* s = next();
         if (direct) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(s + at(i * 8 + lane / 4, lane % 4)) = res[i];
@@ -381,14 +364,21 @@ struct TmaOut {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[8 * p + j] += w[j];
         }
-        put(s, v);  // each lane its own row
-        send(ty, s, here, n0, m0, 0);
-        return;
       }
     }
-    char* s = next();
-    put(s, v);
-    send(ty, s, here, n0, m0, 0);
+    put(s, v);  // over the residual: each lane its own row
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      if (m0 < a.M && n0 < a.N) {
+        if (EPI != EPI_PLAIN && a.z) {
+          ptx::tma_store_3d(&tz, ptx::smem_u32(s + kOutBytes), n0, 0, int(m0));
+          if (EPI == EPI_GATED) ptx::tma_store_3d(&tz, ptx::smem_u32(s + 2 * kOutBytes), n0, 1, int(m0));
+        }
+        ptx::tma_store_3d(&ty, ptx::smem_u32(s), n0, 0, int(m0));
+      }
+      ptx::bulk_commit_group();  // an empty group counts too
+    }
   }
   __device__ __forceinline__ void done() const {
     if (lane == 0) ptx::bulk_wait_all();
