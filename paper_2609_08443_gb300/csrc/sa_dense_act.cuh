@@ -52,6 +52,28 @@ __device__ __forceinline__ void store16(__nv_bfloat16* p, const float* v) { stor
 __device__ __forceinline__ void store16(float* p, const float* v) {
   *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
 }
+// 16 bytes of neighbours, or four bf16
+template <int N>
+__device__ __forceinline__ void load_n(const float* p, float* v) { load16(p, v); }
+template <int N>
+__device__ __forceinline__ void load_n(const __nv_bfloat16* p, float* v) {
+  if (N == 8) {
+    load16(p, v);
+  } else {
+    const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_n(float* p, const float* v) { store16(p, v); }
+template <int N>
+__device__ __forceinline__ void store_n(__nv_bfloat16* p, const float* v) {
+  if (N == 8)
+    store16(p, v);
+  else
+    *reinterpret_cast<uint2*>(p) = make_uint2(ptx::pack_bf16(v[0], v[1]), ptx::pack_bf16(v[2], v[3]));
+}
 
 // Eight fp32 values as three terms of bf16 each, in planes `plane` elements apart: each term is what is left rounded to
 // nearest, and what is left after the third is nothing.

@@ -28,7 +28,6 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kTcThreads = 384;
 constexpr int kEpiWarp0 = 4;
 constexpr int kBlockBytes = 16384;  // 128 rows x 64 bf16
 constexpr uint32_t kWaitNs = 2000000000u;
@@ -42,10 +41,11 @@ struct TcCfg {
   static constexpr int OUT = F32 ? kStageBytes : TmaOut<EPI>::BUFFERS * kOutBytes;  // of an epilogue warp
   static constexpr int STAGES = F32 ? 2 : EPI == EPI_GATED ? 4 : 5;
   static constexpr int BN = TileShape<CTAS>::BN;
+  static constexpr int WARPS = 4 * TileShape<CTAS>::GROUPS;  // that end tiles
+  static constexpr int THREADS = 128 + 32 * WARPS;
   static constexpr int TMEM = 2 * BN;
   static constexpr int OFF_OUT = STAGES * STAGE;
-  static constexpr int OFF_BIAS = OFF_OUT + 8 * OUT;  // bf16: 64 floats of each epilogue warp
-  static constexpr int OFF_BAR = OFF_BIAS + (F32 ? 0 : 8 * 256);
+  static constexpr int OFF_BAR = OFF_OUT + WARPS * OUT;
   static constexpr int SMEM = OFF_BAR + 256;
 };
 static_assert(TcCfg<2, false, EPI_GATED>::SMEM <= 232448 && TcCfg<2, false, EPI_FULL>::SMEM <= 232448 &&
@@ -137,7 +137,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(acc_full(s), 1);
-      mbar_init(acc_empty(s), 8 * CTAS);
+      mbar_init(acc_empty(s), C::WARPS * CTAS);
     }
     abort_flag[0] = 0;
     reinterpret_cast<volatile uint32_t*>(abort_flag)[2] = kWaitNs;
@@ -153,7 +153,6 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-
   if (warp == 0 && lane == 0) {
     // ------------------------------------------------------------- loads
     const uint32_t lead = CTAS == 2 ? mapa_shared(base, 0) : base;
@@ -248,7 +247,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     const uint32_t lanes = uint32_t(q * 32) << 16;
     const uint32_t lead_empty = CTAS == 2 ? mapa_shared(acc_empty(0), 0) : acc_empty(0);
     constexpr int CH = Shape::template CHUNKS<EPI>;
-    TmaOut<EPI> outs(out, reinterpret_cast<float*>(smem + C::OFF_BIAS) + e * 64, lane);
+    TmaOut<EPI> outs(out, lane);
     Segments seg(a, worker);
     uint32_t g = 0;  // sets of accumulators used
     bool ok = true;
@@ -275,7 +274,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         piece = a.piece + (int64_t(worker * 2 + slot) * CTAS + rank) * (128 * C::BN) + (q * 32 + lane) * 4;
       }
       auto col = [&](int i, int half) {  // accumulator column of chunk i (SwiGLU: of either half)
-        return EPI == EPI_GATED ? half * YN + h * (YN / 2) + i * 32 : h * (C::BN / 2) + i * 32;
+        return half * YN + h * (YN / Shape::GROUPS) + i * 32;
       };
       auto put_piece = [&](int c, const float* v) {
         if (m0 + lane < a.M)
@@ -285,7 +284,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
                 make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
       };
       End end;
-      const int y0 = nb * YN + h * (YN / 2);  // this warp's first column of y
+      const int y0 = nb * YN + h * (YN / Shape::GROUPS);  // this warp's first column of y
       if constexpr (F32) {
         constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
         float sum[CH][HALVES][32];
@@ -325,10 +324,10 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
               if (k == i) {
                 stage_put<End::COLS>(out, lane, &sum[k * End::COLS / 32][0][k * End::COLS % 32]);
                 if (EPI == EPI_GATED)
-                  stage_put<End::COLS>(out, lane, &sum[k * End::COLS / 32][HALVES - 1][k * End::COLS % 32], End::COLS / 4);
+                  stage_put<End::COLS>(out, lane, &sum[k * End::COLS / 32][HALVES - 1][k * End::COLS % 32], End::U);
               }
             __syncwarp();
-            end.template finish<1>(a, out, out, lane, m0, n0, 0);
+            end.template finish<1>(a, out, lane, m0, n0, 0);
             __syncwarp();
           }
         } else {
@@ -339,36 +338,48 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         }
       } else {
         const bool tma = (a.vec & 1) != 0;
-        if (complete) {
-          if (tma)
-            outs.load_bias(a, y0);
-          else
-            end.load_bias(a, lane, y0);
-        }
+        if (complete && tma) outs.load_bias(a, y0);
         const uint32_t set = g & 1u, acc = tmem + lanes + set * C::BN;
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), (g >> 1) & 1u, abort_flag, a.ws, 0x404));
         if (!ok) break;
         tc_fence_after();
 #pragma unroll 1
         for (int i = 0; i < CH; ++i) {
-          float v[32], u[EPI == EPI_GATED ? 32 : 1];
-          tmem_ld32(acc + col(i, 0), v);
-          if constexpr (EPI == EPI_GATED) tmem_ld32(acc + col(i, 1), u);
-          tmem_ld_wait();
-          if (i == CH - 1) release(set);
+          auto read = [&] {
+            if (i == CH - 1) release(set);
+          };
           if (complete && tma) {
-            outs.finish(a, ty, tz, v, u, m0, y0 + i * 32);
+            outs.finish(a, ty, tz, acc + col(i, 0), acc + col(i, 1), m0, y0 + i * 32, read);
             if (i + 1 < CH) outs.load_bias(a, y0 + i * 32 + 32);
           } else if (complete) {
-            stage_put<32>(out, lane, v);
-            if constexpr (EPI == EPI_GATED) stage_put<32>(out + kStageBytes, lane, u);
-            __syncwarp();
-            end.template finish<1>(a, out, out + kStageBytes, lane, m0, y0 + i * 32, 0);
-            if (i + 1 < CH) end.load_bias(a, lane, y0 + i * 32 + 32);
-            __syncwarp();
+#pragma unroll 1
+            for (int k = 0; k < 2; ++k) {  // by 16 columns
+              float v[16];
+              const int n0 = y0 + i * 32 + k * 16;
+              tmem_ld16(acc + col(i, 0) + k * 16, v);
+              tmem_ld_wait();
+              stage_put<16>(out, lane, v, End::COLS == 32 ? 4 * k : 0);
+              if (EPI == EPI_GATED) {
+                tmem_ld16(acc + col(i, 1) + k * 16, v);
+                tmem_ld_wait();
+                stage_put<16>(out, lane, v, End::U);
+              }
+              if (k == 1) read();
+              if (End::COLS == 32 && k == 0) continue;
+              __syncwarp();
+              end.load_bias(a, lane, End::COLS == 32 ? y0 + i * 32 : n0);
+              end.template finish<1>(a, out, lane, m0, End::COLS == 32 ? y0 + i * 32 : n0, 0);
+              __syncwarp();
+            }
           } else {
-            put_piece(col(i, 0), v);
-            if constexpr (EPI == EPI_GATED) put_piece(col(i, 1), u);
+#pragma unroll 1
+            for (int k = 0; k < (EPI == EPI_GATED ? 2 : 1); ++k) {
+              float v[32];
+              tmem_ld32(acc + col(i, k), v);
+              tmem_ld_wait();
+              put_piece(col(i, k), v);
+            }
+            read();
           }
         }
         ++g;
@@ -389,7 +400,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
 }
 
 template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(TcCfg<CTAS, F32, EPI>::THREADS, 1)
     tc_linear_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                      const __grid_constant__ CUtensorMap ty, const __grid_constant__ CUtensorMap tz, const TcArgs a) {
   tc_linear_work<CTAS, A_MN, B_MN, F32, EPI>(ta, tb, ty, tz, a, int(blockIdx.x) / CTAS, a.clear && blockIdx.x == 0);
@@ -398,7 +409,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 // dx and dW side by side, for gradients that would leave most of the GPU idle one after the other: the first
 // x.W CTAs (or pairs) make dx.
 template <int CTAS, bool F32>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(TcCfg<CTAS, F32, EPI_PLAIN>::THREADS, 1)
     tc_linear_grads_kernel(const __grid_constant__ CUtensorMap xa, const __grid_constant__ CUtensorMap xb,
                            const __grid_constant__ CUtensorMap wa, const __grid_constant__ CUtensorMap wb,
                            const __grid_constant__ CUtensorMap xy, const __grid_constant__ CUtensorMap wy, const TcArgs x,
@@ -418,9 +429,9 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   using C = TcCfg<CTAS, F32, EPI>;
   using End = typename C::End;
   using Shape = TileShape<CTAS>;
-  constexpr int YN = Shape::template YN<EPI>, CH = 2 * Shape::template CHUNKS<EPI>;
+  constexpr int YN = Shape::template YN<EPI>, CH = YN / 32;
   constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
-  extern __shared__ __align__(128) char stages[];  // [4][HALVES][kStageBytes]
+  extern __shared__ __align__(128) char stages[];  // [4][32 / COLS][kStageBytes]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, part = warp >> 2;
   const int i = block % CH, rank = block / CH % CTAS;
   const int64_t rest = block / (CH * CTAS);
@@ -472,19 +483,15 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
     }
     const float v[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
     if constexpr (End::COLS == 32)
-      stage_put<8>(out + k * kStageBytes, lane, v, part * 2);
+      stage_put<8>(out, lane, v, part * 2);
     else  // columns 0-15 of both halves in one stage, 16-31 in the next
-      stage_put<8>(out + (part >> 1) * kStageBytes, lane, v, k * 4 + (part & 1) * 2);
+      stage_put<8>(out + (part >> 1) * kStageBytes, lane, v, k * End::U + (part & 1) * 2);
   }
   __syncthreads();
-  if constexpr (End::COLS == 32) {
-    end.template finish<4>(a, out, out + kStageBytes, lane, m0, n0, part);
-  } else {
 #pragma unroll 1
-    for (int k = 0; k < 2; ++k) {
-      if (k) end.load_bias(a, lane, n0 + 16);
-      end.template finish<4>(a, out + k * kStageBytes, out + k * kStageBytes, lane, m0, n0 + 16 * k, part);
-    }
+  for (int k = 0; k < 32 / End::COLS; ++k) {
+    if (k) end.load_bias(a, lane, n0 + k * End::COLS);
+    end.template finish<4>(a, out + k * kStageBytes, lane, m0, n0 + k * End::COLS, part);
   }
 }
 
@@ -564,12 +571,12 @@ bool make_map(CUtensorMap* m, const TcOperand& o, bool f32, int box_rows) {
 
 // A launch of `ctas` CTAs in clusters of CTAS.
 template <int CTAS, class... P, class... A>
-cudaError_t launch_cluster(void (*fn)(P...), int ctas, size_t smem, cudaStream_t st, const A&... args) {
+cudaError_t launch_cluster(void (*fn)(P...), int ctas, int threads, size_t smem, cudaStream_t st, const A&... args) {
   cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(ctas), 1, 1);
-  cfg.blockDim = dim3(kTcThreads, 1, 1);
+  cfg.blockDim = dim3(unsigned(threads), 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -606,10 +613,11 @@ cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaSt
       return cudaErrorInvalidValue;
   }
   cudaError_t e =
-      launch_cluster<CTAS>(&tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>, p.W * CTAS, C::SMEM, st, ta, tb, ty, tz, a);
+      launch_cluster<CTAS>(&tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>, p.W * CTAS, C::THREADS, C::SMEM, st, ta,
+                           tb, ty, tz, a);
   ++*launches;
   if (e != cudaSuccess || p.cut == 0) return e;
-  constexpr int CH = 2 * TileShape<CTAS>::template CHUNKS<EPI>;
+  constexpr int CH = TileShape<CTAS>::template YN<EPI> / 32;
   tc_join_kernel<CTAS, F32, EPI>
       <<<unsigned(p.cut * CTAS * CH), kJoinThreads, 4 * (EPI == EPI_GATED ? 2 : 1) * kStageBytes, st>>>(a);
   ++*launches;
@@ -627,11 +635,11 @@ cudaError_t launch_grads(const TcGemm& gx, const TcPlan& px, const TcArgs& x, co
   CUtensorMap xy = xa, wy = wa;
   if (!F32 && ((x.vec & 1) && !make_out_map(&xy, x.y, x.M, x.N, 1))) return cudaErrorInvalidValue;
   if (!F32 && ((w.vec & 1) && !make_out_map(&wy, w.y, w.M, w.N, 1))) return cudaErrorInvalidValue;
-  cudaError_t e = launch_cluster<CTAS>(&tc_linear_grads_kernel<CTAS, F32>, (px.W + pw.W) * CTAS, C::SMEM, st, xa, xb, wa,
+  cudaError_t e = launch_cluster<CTAS>(&tc_linear_grads_kernel<CTAS, F32>, (px.W + pw.W) * CTAS, C::THREADS, C::SMEM, st, xa, xb, wa,
                                        wb, xy, wy, x, w);
   ++*launches;
   if (e != cudaSuccess || px.cut + pw.cut == 0) return e;
-  constexpr int CH = 2 * TileShape<CTAS>::template CHUNKS<EPI_PLAIN>;
+  constexpr int CH = TileShape<CTAS>::template YN<EPI_PLAIN> / 32;
   tc_join_grads_kernel<CTAS, F32>
       <<<unsigned((px.cut + pw.cut) * CTAS * CH), kJoinThreads, 4 * kStageBytes, st>>>(x, w, int(px.cut * CTAS * CH));
   ++*launches;

@@ -80,11 +80,12 @@ enum { EPI_PLAIN = 0, EPI_FULL = 1, EPI_GATED = 2 };
 template <int CTAS>
 struct TileShape {
   static constexpr int BN = CTAS == 2 ? 256 : 128;           // accumulator columns
+  static constexpr int GROUPS = 2;                            // epilogue warps of a row
   template <int EPI>
   static constexpr int YN = EPI == EPI_GATED ? BN / 2 : BN;  // columns of y
-  // chunks of 32 columns of y that an epilogue warp (of two for a row) makes, and where they begin
+  // chunks of 32 columns of y that an epilogue warp makes
   template <int EPI>
-  static constexpr int CHUNKS = YN<EPI> / 64;
+  static constexpr int CHUNKS = YN<EPI> / (32 * GROUPS);
 };
 
 // A chunk's sums on their way from one row a lane to whole rows a few lanes: 32 rows of 128 bytes, 16-byte pieces in
@@ -100,16 +101,16 @@ __device__ __forceinline__ void stage_put(char* s, int lane, const float* v, int
     *reinterpret_cast<float4*>(s + stage_at(lane, first + p)) = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
 }
 
-// How a chunk ends: EACH neighbouring values a lane, 16 bytes of T, of a row's COLS columns.  SwiGLU's fp32 chunks have
-// 16 columns, so that the gate's and the other half's share the stage; in bf16 the other half has a stage of its own.
+// How a chunk ends: EACH neighbouring values a lane of a row's COLS columns.  SwiGLU's chunks have 16 columns, so that the
+// gate's and the other half's share the stage.
 template <typename T, int EPI>
 struct ChunkEnd {
   static constexpr bool F32 = sizeof(T) == 4;
-  static constexpr int COLS = F32 && EPI == EPI_GATED ? 16 : 32;
-  static constexpr int EACH = F32 ? 4 : 8;
+  static constexpr int COLS = EPI == EPI_GATED ? 16 : 32;
+  static constexpr int EACH = F32 || EPI == EPI_GATED ? 4 : 8;
   static constexpr int LANES = COLS / EACH;   // lanes of a row
   static constexpr int ROWS = 32 / LANES;     // rows at a time
-  static constexpr int STAGES = !F32 && EPI == EPI_GATED ? 2 : 1;
+  static constexpr int U = COLS / 4;          // the other half's first 16-byte piece of the stage
 
   float bv[EACH], bu[EACH];  // biases of this lane's columns
 
@@ -160,12 +161,9 @@ struct ChunkEnd {
     }
   }
 
-  // Rows m0 .. m0 + 31, columns n0 .. n0 + COLS - 1 of y, of the sums in the stage(s) (SwiGLU in bf16: the other half's in
-  // su); of PARTS, the eight rows of `part` only.
+  // Rows m0 .. m0 + 31, columns n0 .. n0 + COLS - 1 of y, of the sums in the stage; of PARTS, the rows of `part` only.
   template <int PARTS>
-  __device__ __forceinline__ void finish(const TcArgs& a, const char* s, const char* su, int lane, int64_t m0, int n0,
-                                         int part) const {
-    constexpr int U = STAGES == 2 ? 0 : COLS / 4;  // the other half's first piece
+  __device__ __forceinline__ void finish(const TcArgs& a, const char* s, int lane, int64_t m0, int n0, int part) const {
     if (a.vec & 1) {
       const int p = lane % LANES, n = n0 + p * EACH;
       const bool res = EPI != EPI_PLAIN && a.r, res_vec = (a.vec & 2) != 0;
@@ -178,7 +176,7 @@ struct ChunkEnd {
       auto fetch = [&](int64_t at) {
         if (at >= a.M || n >= a.N) return;
         if (res_vec) {
-          load16(r, next);
+          load_n<EACH>(r, next);
         } else {
 #pragma unroll
           for (int j = 0; j < EACH; ++j) next[j] = ld_nc(r + j);
@@ -198,7 +196,7 @@ struct ChunkEnd {
           if (i + 1 < LANES / PARTS) fetch(m + ROWS);
         }
         read(s, row, p * (EACH / 4), v);
-        if (EPI == EPI_GATED) read(su, row, U + p * (EACH / 4), u);
+        if (EPI == EPI_GATED) read(s, row, U + p * (EACH / 4), u);
         if (EPI != EPI_PLAIN) {
 #pragma unroll
           for (int j = 0; j < EACH; ++j) {
@@ -206,8 +204,8 @@ struct ChunkEnd {
             if (EPI == EPI_GATED) u[j] += bu[j];
           }
           if (a.z && here) {
-            store16(z, v);
-            if (EPI == EPI_GATED) store16(z + a.half, u);
+            store_n<EACH>(z, v);
+            if (EPI == EPI_GATED) store_n<EACH>(z + a.half, u);
           }
           activate_all(a.act, v, u);
           if (res) {
@@ -215,7 +213,7 @@ struct ChunkEnd {
             for (int j = 0; j < EACH; ++j) v[j] += rv[j];
           }
         }
-        if (here) store16(y, v);
+        if (here) store_n<EACH>(y, v);
         m += ROWS;
         y += int64_t(ROWS) * a.N;
         if (EPI != EPI_PLAIN) z += int64_t(ROWS) * a.Z;
@@ -248,7 +246,7 @@ struct ChunkEnd {
           const int64_t m = m0 + row;
           const bool here = m < a.M && n < a.N;
           float v = *reinterpret_cast<const float*>(s + stage_at(row, c / 4) + c % 4 * 4), u = 0.f;
-          if (EPI == EPI_GATED) u = *reinterpret_cast<const float*>(su + stage_at(row, U + c / 4) + c % 4 * 4);
+          if (EPI == EPI_GATED) u = *reinterpret_cast<const float*>(s + stage_at(row, U + c / 4) + c % 4 * 4);
           if (EPI != EPI_PLAIN) {
             v += bv[0];
             if (EPI == EPI_GATED) u += bu[0];
@@ -267,20 +265,30 @@ struct ChunkEnd {
   }
 };
 
+// 16 columns of 32 lanes' accumulators (see ptx::tmem_ld32)
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+      "[%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+
 // The end of bf16 chunks whose rows TMA can write: each lane keeps its row's 32 columns in registers to the end, and
-// a chunk's 32 x 32 results (z, SwiGLU's other half of z, y) leave together from one of two sets of buffers (64-byte
-// rows, TMA's 64-byte swizzle).  That takes a third of the shared-memory traffic of the way above.
+// a chunk's 32 x 32 results (z, SwiGLU's other half of z, y) leave together from the warp's buffers (64-byte rows, TMA's
+// 64-byte swizzle).  That takes a third of the shared-memory traffic of the way above.
 constexpr int kOutBytes = 2048;
 template <int EPI>
 struct TmaOut {
   static constexpr int SET = EPI == EPI_GATED ? 3 : EPI == EPI_FULL ? 2 : 1;  // results of a chunk
-  static constexpr int BUFFERS = EPI == EPI_GATED ? 6 : 4;  // two sets at least (and two whole stages, for unaligned rows)
+  static constexpr int BUFFERS = 2 * SET;  // two sets in turn (unaligned rows' stage is as long as two buffers)
   char* ring;
-  float* bias;  // [64]
-  int lane, used;
+  int lane, turn;
   float b0, b1;
 
-  __device__ __forceinline__ TmaOut(char* ring_, float* bias_, int lane_) : ring(ring_), bias(bias_), lane(lane_), used(0) {}
+  __device__ __forceinline__ TmaOut(char* ring_, int lane_) : ring(ring_), lane(lane_), turn(0) {}
 
   __device__ __forceinline__ void load_bias(const TcArgs& a, int n0) {
     b0 = b1 = 0.f;
@@ -295,47 +303,72 @@ struct TmaOut {
     for (int p = 0; p < 4; ++p) store8(reinterpret_cast<__nv_bfloat16*>(s + at(lane, p)), v + 8 * p);
   }
 
-  __device__ __forceinline__ void finish(const TcArgs& a, const CUtensorMap& ty, const CUtensorMap& tz, float* v, float* u,
-                                         int64_t m0, int n0) {
+  // `acc`: this lane's accumulators of the chunk, SwiGLU's other half at `other`; read() is called once they are read.
+  template <class F>
+  __device__ __forceinline__ void finish(const TcArgs& a, const CUtensorMap& ty, const CUtensorMap& tz, uint32_t acc,
+                                         uint32_t other, int64_t m0, int n0, F read) {
+    float v[32];
+    ptx::tmem_ld32(acc, v);
     // the set of the chunk before last, once its stores have read it
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    char* s = ring + (turn ^= 1) * SET * kOutBytes;  // y, then z's halves
+    uint4 res[EPI == EPI_FULL ? 4 : 1];
+    const bool direct = EPI != EPI_PLAIN && a.r && (a.vec & 2);
+    auto load_residual = [&](uint4* q) {  // whole rows a few lanes
+      const int n = n0 + lane % 4 * 8;
+      const __nv_bfloat16* r = static_cast<const __nv_bfloat16*>(a.r) + n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t m = m0 + i * 8 + lane / 4;
+        q[i] = make_uint4(0, 0, 0, 0);
+        if (m < a.M && n < a.N) q[i] = __ldg(reinterpret_cast<const uint4*>(r + m * a.r_stride));
+      }
+    };
+    if constexpr (EPI == EPI_FULL) {
+      if (direct) load_residual(res);  // on its way meanwhile
+    }
     __syncwarp();
-    char* s = ring + (used ^= 1) * SET * kOutBytes;  // y, then z's halves
+    // y's buffer holds the biases until y itself
+    float* bias = reinterpret_cast<float*>(s);
+    auto add_bias = [&](const float* from, float* to, int count) {
+#pragma unroll
+      for (int j = 0; j < count; j += 4) {
+        const float4 b = *reinterpret_cast<const float4*>(from + j);
+        to[j] += b.x, to[j + 1] += b.y, to[j + 2] += b.z, to[j + 3] += b.w;
+      }
+    };
+    if (EPI != EPI_PLAIN && a.bias) {
+      bias[lane] = b0;
+      if (EPI == EPI_GATED) bias[32 + lane] = b1;
+      __syncwarp();
+    }
+    ptx::tmem_ld_wait();
+    if (EPI != EPI_GATED) read();
     if (EPI != EPI_PLAIN) {
-      uint4 res[4];
-      const bool direct = a.r && (a.vec & 2);
-      if (direct) {  // whole rows a few lanes, on their way meanwhile
-        const int n = n0 + lane % 4 * 8;
-        const __nv_bfloat16* r = static_cast<const __nv_bfloat16*>(a.r) + n;
+      if (a.bias) add_bias(bias, v, 32);
+      if (a.z) put(s + kOutBytes, v);
+    }
+    if constexpr (EPI == EPI_GATED) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t m = m0 + i * 8 + lane / 4;
-          res[i] = make_uint4(0, 0, 0, 0);
-          if (m < a.M && n < a.N) res[i] = __ldg(reinterpret_cast<const uint4*>(r + m * a.r_stride));
-        }
-      }
-      if (a.bias) {
-        bias[lane] = b0;
-        if (EPI == EPI_GATED) bias[32 + lane] = b1;
-        __syncwarp();
+      for (int j = 0; j < 32; ++j) v[j] *= sigmoid<false>(v[j]);
+      // the other half by 16 columns, so that the chunk's registers are few
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-          const float4 b = *reinterpret_cast<const float4*>(bias + j);
-          v[j] += b.x, v[j + 1] += b.y, v[j + 2] += b.z, v[j + 3] += b.w;
-          if (EPI == EPI_GATED) {
-            const float4 c = *reinterpret_cast<const float4*>(bias + 32 + j);
-            u[j] += c.x, u[j + 1] += c.y, u[j + 2] += c.z, u[j + 3] += c.w;
-          }
-        }
-      }
-      if (a.z) {
-        put(s + kOutBytes, v);
-        if (EPI == EPI_GATED) put(s + 2 * kOutBytes, u);
-      }
-      if (EPI == EPI_GATED) {
+      for (int k = 0; k < 2; ++k) {
+        float u[16];
+        tmem_ld16(other + 16 * k, u);
+        ptx::tmem_ld_wait();
+        if (k == 1) read();
+        if (a.bias) add_bias(bias + 32 + 16 * k, u, 16);
+        if (a.z)
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = v[j] * sigmoid<false>(v[j]) * u[j];
-      } else if (a.act == SA_ACT_RELU) {
+          for (int p = 0; p < 2; ++p)
+            store8(reinterpret_cast<__nv_bfloat16*>(s + 2 * kOutBytes + at(lane, 2 * k + p)), u + 8 * p);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[16 * k + j] *= u[j];
+      }
+    }
+    if constexpr (EPI == EPI_FULL) {
+      if (a.act == SA_ACT_RELU) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_RELU, v[j]);
       } else if (a.act == SA_ACT_GELU) {
@@ -345,10 +378,16 @@ struct TmaOut {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_SILU, v[j]);
       }
+    }
+    if (EPI != EPI_PLAIN) {
+      if (a.bias) __syncwarp();  // the biases are read
       if (a.r) {
         if (direct) {
+          uint4 late[4];
+          if constexpr (EPI == EPI_GATED) load_residual(late);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(s + at(i * 8 + lane / 4, lane % 4)) = res[i];
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(s + at(i * 8 + lane / 4, lane % 4)) = EPI == EPI_FULL ? res[EPI == EPI_FULL ? i : 0] : late[i];
         } else {
           const __nv_bfloat16* r = static_cast<const __nv_bfloat16*>(a.r) + n0 + lane;
 #pragma unroll 8
