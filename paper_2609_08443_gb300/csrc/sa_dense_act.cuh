@@ -29,6 +29,15 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
   reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
+// 16 bytes on their way from memory to this thread's place in shared memory.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// ... through L1, where the neighbour's half of the same 32 bytes is found again
+__device__ __forceinline__ void copy16_l1(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 // 16 bytes of neighbours: eight bf16 or four fp32.  Loads of what the kernel does not write, so that they may go ahead of
 // stores.
 __device__ __forceinline__ void load16(const __nv_bfloat16* p, float* v) {

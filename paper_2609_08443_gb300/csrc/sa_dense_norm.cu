@@ -69,14 +69,6 @@ __device__ __forceinline__ void load_row(const void* p, sa_dtype dt, int64_t at,
 // 16-byte pieces that a chunk of 8 elements takes
 __device__ __forceinline__ int pieces(const Mat& m) { return !m.p ? 0 : m.dt == SA_BF16 ? 1 : 2; }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-// ... through L1, where the neighbour's half of the same 32 bytes is found again
-__device__ __forceinline__ void copy16_l1(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-
 // One matrix along a walk: where this thread's first element of the next row to be fetched is, and how far the row
 // after it is away.
 struct Track {

@@ -86,12 +86,16 @@ __global__ void __launch_bounds__(256) simt_gemm_kernel(const GemmArgs g) {
 // Columns are spread over 32 lanes x 8 (fewer lanes where there are fewer columns, and the rest of the
 // warp takes other rows); a block's eight warps and its share of the rows leave one partial row of sums.
 
+// Aligned rows (VEC) come through a ring of three rows a thread in shared memory, filled by the thread's own cp.async: a
+// row's loads and its arithmetic would wait for each other (16384 x 8192 gated: 131 us with two rows in registers, RING us).
+constexpr int kRing = 3;
+
 template <typename T, bool VEC, bool GATED>
-__global__ void __launch_bounds__(256) act_grad_kernel(const ActGradArgs a, int lanes) {
+__global__ void __launch_bounds__(256, GATED && sizeof(T) == 4 ? 2 : 3) act_grad_kernel(const ActGradArgs a, int lanes) {
   constexpr int S = GATED ? 2 : 1;
   constexpr bool FULL = sizeof(T) == 4;
-  constexpr int R = VEC && !FULL ? 2 : 1;  // rows that a thread has in flight
-  __shared__ float part[8][S][256];
+  constexpr int P = int(sizeof(T)) / 2;  // 16-byte pieces of 8 values
+  extern __shared__ __align__(16) char mem[];  // VEC: the ring; at the end the warps' sums [8][S][256]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t = lane % lanes, per_warp = 32 / lanes;
   const int c0 = blockIdx.x * 256;
@@ -100,87 +104,113 @@ __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradArgs a, int 
   float sum[S][8] = {};
   const int64_t step = int64_t(gridDim.y) * 8 * per_warp;
   auto col = [&](int j) { return c0 + (VEC ? t * 8 + j : j * lanes + t); };
-  for (int64_t row0 = (int64_t(blockIdx.y) * 8 + warp) * per_warp + lane / lanes; row0 < a.M; row0 += R * step) {
-    float g[R][8], zz[R][S][8];
+  int64_t row = (int64_t(blockIdx.y) * 8 + warp) * per_warp + lane / lanes;
+
+  constexpr int kApart = 256 * 16, kRow = (S + 1) * P * kApart;  // bytes between a thread's pieces, and between rows
+  char* own = mem + threadIdx.x * 16;
+  const bool in = col(0) < a.N;
+  int64_t ahead = row;
+  int put = 0, get = 0;
+  auto copy8 = [&](int slot, const T* p) {
+    const uint32_t to = ptx::smem_u32(own) + slot;
+    if (P == 1) {
+      copy16(to, p);
+    } else {
+      copy16_l1(to, p);
+      copy16_l1(to + kApart, p + 4);
+    }
+  };
+  auto fetch = [&] {
+    if (ahead < a.M && in) {
+      copy8(put, dy + ahead * a.dy.stride + col(0));
+      if (a.act != SA_ACT_NONE)
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int64_t row = row0 + i * step;
-      const bool here = row < a.M;
-      if (VEC) {
-        if (here && col(0) < a.N) {
-          load8(dy + row * a.dy.stride + col(0), g[i]);
-          if (a.act != SA_ACT_NONE)
+        for (int s = 0; s < S; ++s) copy8(put + (s + 1) * P * kApart, z + ahead * a.Z + int64_t(s) * a.N + col(0));
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ahead += step;
+    put = put == (kRing - 1) * kRow ? 0 : put + kRow;
+  };
+  auto take8 = [&](int slot, float* v) {
+    if (P == 1) {
+      load8(reinterpret_cast<const __nv_bfloat16*>(own + slot), v);
+    } else {
+      const float4 x = *reinterpret_cast<const float4*>(own + slot), y = *reinterpret_cast<const float4*>(own + slot + kApart);
+      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+    }
+  };
+  if (VEC)
 #pragma unroll
-            for (int s = 0; s < S; ++s) load8(z + row * a.Z + s * a.N + col(0), zz[i][s]);
-        } else {
+    for (int i = 0; i < kRing - 1; ++i) fetch();
+
+  for (; row < a.M; row += step) {
+    float g[8], zz[S][8];
+    if (VEC) {
+      fetch();
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      if (in) {
+        take8(get, g);
+        if (a.act != SA_ACT_NONE)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            g[i][j] = 0.f;
+          for (int s = 0; s < S; ++s) take8(get + (s + 1) * P * kApart, zz[s]);
+      }
+      get = get == (kRing - 1) * kRow ? 0 : get + kRow;
+      if (!in) continue;
+    } else {
 #pragma unroll
-            for (int s = 0; s < S; ++s) zz[i][s][j] = 0.f;
-          }
-        }
+      for (int j = 0; j < 8; ++j) {
+        const bool inside = col(j) < a.N;
+        g[j] = inside ? ld_f32(dy + row * a.dy.stride + col(j)) : 0.f;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+          zz[s][j] = inside && a.act != SA_ACT_NONE ? ld_f32(z + row * a.Z + int64_t(s) * a.N + col(j)) : 0.f;
+      }
+    }
+    float d[S][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (GATED) {
+        const float p = sigmoid<FULL>(zz[0][j]);
+        d[0][j] = g[j] * zz[S - 1][j] * (p * fmaf(zz[0][j], 1.f - p, 1.f));
+        d[S - 1][j] = g[j] * (zz[0][j] * p);
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool in = here && col(j) < a.N;
-          g[i][j] = in ? ld_f32(dy + row * a.dy.stride + col(j)) : 0.f;
-#pragma unroll
-          for (int s = 0; s < S; ++s)
-            zz[i][s][j] = in && a.act != SA_ACT_NONE ? ld_f32(z + row * a.Z + int64_t(s) * a.N + col(j)) : 0.f;
-        }
+        d[0][j] = a.act == SA_ACT_NONE   ? g[j]
+                  : a.act == SA_ACT_RELU ? (zz[0][j] > 0.f ? g[j] : 0.f)
+                                         : g[j] * slope<FULL>(a.act, zz[0][j]);
       }
     }
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int64_t row = row0 + i * step;
-      if (R > 1 && row >= a.M) break;
-      float d[S][8];
+    for (int s = 0; s < S; ++s) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (GATED) {
-          const float p = sigmoid<FULL>(zz[i][0][j]);
-          d[0][j] = g[i][j] * zz[i][S - 1][j] * (p * fmaf(zz[i][0][j], 1.f - p, 1.f));
-          d[S - 1][j] = g[i][j] * (zz[i][0][j] * p);
+      for (int j = 0; j < 8; ++j) sum[s][j] += d[s][j];
+      if (!a.dz) continue;
+      const int64_t at = row * a.pitch + int64_t(s) * a.N;
+      if (a.terms) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.dz) + at;
+        const int64_t plane = a.M * a.pitch;
+        if (VEC) {
+          store_terms(o + col(0), plane, d[s]);
         } else {
-          d[0][j] = a.act == SA_ACT_NONE   ? g[i][j]
-                    : a.act == SA_ACT_RELU ? (zz[i][0][j] > 0.f ? g[i][j] : 0.f)
-                                           : g[i][j] * slope<FULL>(a.act, zz[i][0][j]);
-        }
-      }
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
+          for (int j = 0; j < 8; ++j)
+            if (col(j) < a.N) {
+              float left = d[s][j];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[s][j] += d[s][j];
-        if (!a.dz) continue;
-        const int64_t at = row * a.pitch + int64_t(s) * a.N;
-        if (a.terms) {
-          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.dz) + at;
-          const int64_t plane = a.M * a.pitch;
-          if (VEC) {
-            if (col(0) < a.N) store_terms(o + col(0), plane, d[s]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (col(j) < a.N) {
-                float left = d[s][j];
-#pragma unroll
-                for (int k = 0; k < 3; ++k) {
-                  const __nv_bfloat16 term = __float2bfloat16_rn(left);
-                  o[k * plane + col(j)] = term;
-                  left -= __bfloat162float(term);
-                }
+              for (int k = 0; k < 3; ++k) {
+                const __nv_bfloat16 term = __float2bfloat16_rn(left);
+                o[k * plane + col(j)] = term;
+                left -= __bfloat162float(term);
               }
-          }
+            }
+        }
+      } else {
+        T* o = static_cast<T*>(a.dz) + at;
+        if (VEC) {
+          store8(o + col(0), d[s]);
         } else {
-          T* o = static_cast<T*>(a.dz) + at;
-          if (VEC) {
-            if (col(0) < a.N) store8(o + col(0), d[s]);
-          } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (col(j) < a.N) st_from_f32(o + col(j), d[s][j]);
-          }
+          for (int j = 0; j < 8; ++j)
+            if (col(j) < a.N) st_from_f32(o + col(j), d[s][j]);
         }
       }
     }
@@ -193,6 +223,8 @@ __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradArgs a, int 
       for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[s][j] += __shfl_xor_sync(0xFFFFFFFFu, sum[s][j], o);
+  float(*part)[S][256] = reinterpret_cast<float(*)[S][256]>(mem);
+  __syncthreads();  // the ring is read out (no copy is in flight: the last rows' were waited for)
   if (lane < lanes)
 #pragma unroll
     for (int s = 0; s < S; ++s)
@@ -235,8 +267,15 @@ cudaError_t launch_act_grad(const ActGradArgs& a, cudaStream_t st) {
   auto base_ok = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
   const bool vec = a.N % 8 == 0 && base_ok(a.dy.p) && a.dy.stride % e == 0 && base_ok(a.z) && base_ok(a.dz) &&
                    a.pitch % 8 == 0;
+  const size_t sums = size_t(8) * (gated ? 2 : 1) * 256 * sizeof(float);
+  const size_t ring = vec ? size_t(kRing) * (gated ? 3 : 2) * (a.dy.dt == SA_BF16 ? 1 : 2) * 256 * 16 : 0;
+  const size_t smem = ring > sums ? ring : sums;
   auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, st>>>(a, lanes);
+    if (smem > 48 * 1024) {
+      const cudaError_t s = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+      if (s != cudaSuccess) return s;
+    }
+    kernel<<<grid, 256, smem, st>>>(a, lanes);
     return cudaGetLastError();
   };
   if (a.dy.dt == SA_BF16) {
