@@ -879,7 +879,7 @@ def sa_linear_get_device_error(device=None) -> int:
 
 def _row_stride(name: str, t: torch.Tensor, n: int, index: int, dtype=None) -> int:
     """Elements between the rows of ``t`` [..., n] (its last axis contiguous)."""
-    if not t.is_cuda or t.get_device() != index:
+    if t.get_device() != index:
         raise ValueError(f"{name} must be a CUDA tensor on the call's device")
     if t.dim() < 1 or t.shape[-1] != n or (dtype is not None and t.dtype is not dtype):
         raise ValueError(f"{name} must be {dtype or 'bf16 or fp32'} [..., {n}], not {t.dtype} {tuple(t.shape)}")
@@ -903,16 +903,16 @@ def _row_stride(name: str, t: torch.Tensor, n: int, index: int, dtype=None) -> i
 def _vector(name: str, t: Optional[torch.Tensor], n: int, index: int, dtype) -> Optional[int]:
     if t is None:
         return None
-    if not t.is_cuda or t.get_device() != index or t.dtype is not dtype or tuple(t.shape) != (n,) or \
-            not t.is_contiguous():
+    if t.get_device() != index or t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {dtype} [{n}] on the call's device")
     return t.data_ptr()
 
 
 def _on_device(name: str, t: torch.Tensor) -> int:
-    if not t.is_cuda:
+    index = t.get_device()
+    if index < 0 or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    return t.get_device()
+    return index
 
 
 def sa_layer_norm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -921,26 +921,29 @@ def sa_layer_norm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bi
     """Layer norm over the last axis of x + residual: y [..., n] of ``dtype`` (x's by default), and with
     ``want_stats`` the rows' (mean, 1/sqrt(var + eps)), fp32 [..., 2], which the gradient takes.  x, residual,
     the parameters (of one type) and y are bf16 or fp32 each."""
-    lib = load()
     index = _on_device("x", x)
-    if x.dim() < 1:
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return sa_layer_norm_fwd(x, weight, bias, residual, eps, dtype, want_stats)
+    shape = x.shape
+    if not shape:
         raise ValueError("x must be [..., n]")
-    n = x.shape[-1]
-    xs = _row_stride("x", x, n, index)
-    rs, r_dt = 0, 0
+    n = shape[-1]
+    xs, rs, r_dt = _row_stride("x", x, n, index), 0, 0
     if residual is not None:
-        if residual.shape != x.shape:
-            raise ValueError(f"residual{tuple(residual.shape)} must have the shape of x{tuple(x.shape)}")
+        if residual.shape != shape:
+            raise ValueError(f"residual{tuple(residual.shape)} must have the shape of x{tuple(shape)}")
         rs, r_dt = _row_stride("residual", residual, n, index), _dt(residual)
     w_t = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
     w, b = _vector("weight", weight, n, index, w_t), _vector("bias", bias, n, index, w_t)
-    y = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
-    stats = torch.empty((*x.shape[:-1], 2), dtype=torch.float32, device=x.device) if want_stats else None
-    with _on(index):
-        st = lib.sa_layer_norm_fwd(x.data_ptr(), xs, _dt(x), _addr(residual), rs, r_dt, w, b,
-                                   _dt_of(w_t), x.numel() // max(n, 1), n,
-                                   float(eps), y.data_ptr(), _dt(y), _addr(stats), _stream_handle(index))
-    _check(st, "sa_layer_norm_fwd")
+    device = x.device
+    y = torch.empty(shape, dtype=x.dtype if dtype is None else dtype, device=device)
+    stats = torch.empty((*shape[:-1], 2), dtype=torch.float32, device=device) if want_stats else None
+    st = load().sa_layer_norm_fwd(x.data_ptr(), xs, _dt(x), _addr(residual), rs, r_dt, w, b, _dt_of(w_t),
+                                  x.numel() // max(n, 1), n, eps, y.data_ptr(), _dt(y), _addr(stats),
+                                  _stream_handle(index))
+    if st:
+        raise SketchError(st, "sa_layer_norm_fwd")
     return (y, stats) if want_stats else y
 
 
@@ -956,8 +959,10 @@ def sa_layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, we
     """(dx, dr, dw, db) for the gradient dy of ``sa_layer_norm_fwd``'s y; ``stats`` are that call's.  dx is of x's
     type and dr of residual's (the same tensor where the types agree, None without a residual); dw and db [n] are of
     weight's type (fp32 without one).  What is not wanted is None."""
-    lib = load()
     index = _on_device("x", x)
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return sa_layer_norm_bwd(dy, x, stats, weight, residual, want_dx, want_params, ws)
     if x.dim() < 1 or dy.shape != x.shape:
         raise ValueError(f"dy{tuple(dy.shape)} must have the shape of x{tuple(x.shape)}, [..., n]")
     n = x.shape[-1]
@@ -979,18 +984,16 @@ def sa_layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, we
         dr = dx if residual.dtype is x.dtype else torch.empty(x.shape, dtype=residual.dtype, device=x.device)
     dw = torch.empty(n, dtype=w_t, device=x.device) if want_params else None
     db = torch.empty(n, dtype=w_t, device=x.device) if want_params else None
-    with _on(index):
-        stream = _stream_handle(index)
-        at, size = None, 0
-        if want_params:
-            need = _norm_workspace_size(index, rows, n)
-            if need == 0:
-                raise SketchError(2, "sa_layer_norm_workspace_size")
-            w_buf = _ws_arg(ws, index) if ws is not None else _stream_workspace(need, index, stream, _dense_ws)
-            at, size = w_buf.data_ptr(), w_buf.numel() * w_buf.element_size()
-        st = lib.sa_layer_norm_bwd(dy.data_ptr(), ys, _dt(dy), x.data_ptr(), xs, _dt(x), _addr(residual), rs, r_dt, w,
-                                   _dt_of(w_t), stats.data_ptr(), rows, n, _addr(dx), None if dr is dx else _addr(dr),
-                                   _addr(dw), _addr(db), at, size, stream)
+    stream, at, size = _stream_handle(index), None, 0
+    if want_params:
+        need = _norm_workspace_size(index, rows, n)
+        if need == 0:
+            raise SketchError(2, "sa_layer_norm_workspace_size")
+        w_buf = _ws_arg(ws, index) if ws is not None else _stream_workspace(need, index, stream, _dense_ws)
+        at, size = w_buf.data_ptr(), w_buf.numel() * w_buf.element_size()
+    st = load().sa_layer_norm_bwd(dy.data_ptr(), ys, _dt(dy), x.data_ptr(), xs, _dt(x), _addr(residual), rs, r_dt, w,
+                                  _dt_of(w_t), stats.data_ptr(), rows, n, _addr(dx), None if dr is dx else _addr(dr),
+                                  _addr(dw), _addr(db), at, size, stream)
     _check(st, "sa_layer_norm_bwd")
     return dx, dr, dw, db
 
@@ -1049,17 +1052,25 @@ def sa_linear_kernel_name(M: int, N: int, K: int, activation: Optional[str], dt:
     return load().sa_linear_kernel_name(M, N, K, _act(activation), dt, which).decode()
 
 
-def _linear_args(x, weight, activation):
-    index = _on_device("x", x)
+def _linear_args(x, weight, activation, index):
     act = _act(activation)
     if weight.dim() != 2 or x.dim() < 1 or weight.dtype is not x.dtype:
         raise ValueError("want x [..., K] and weight [N, K] (swiglu: [2 N, K]) of one dtype")
     Z, K = weight.shape
     if act == 4 and Z % 2:
         raise ValueError("swiglu takes a weight [2 N, K], the gate's N rows first")
-    dt = _dt(x)
-    xs, wt = _row_stride("x", x, K, index, x.dtype), _row_stride("weight", weight, K, index, x.dtype)
-    return index, act, dt, x.numel() // max(K, 1), Z // 2 if act == 4 else Z, Z, K, xs, wt
+    xs, wt = _row_stride("x", x, K, index), _row_stride("weight", weight, K, index)
+    copies = _repack(x, xs, K) + 2 * _repack(weight, wt, K)
+    return act, _dt(x), x.numel() // max(K, 1), Z // 2 if act == 4 else Z, Z, K, xs, wt, copies
+
+
+def _linear_workspace(ws, index: int, stream: int, *sizes) -> torch.Tensor:
+    if ws is not None:
+        return _ws_arg(ws, index)
+    need = _linear_workspace_size(index, *sizes)
+    if need == 0:
+        raise SketchError(2, "sa_linear_workspace_size")
+    return _stream_workspace(need, index, stream, _dense_ws)
 
 
 def sa_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -1069,29 +1080,25 @@ def sa_linear_fwd(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Te
     [..., N].  ``activation``: none, relu, gelu (with the normal distribution function), silu, or swiglu, where the
     weight's first half of the rows makes the gate: silu(first) * second, N = Z / 2; else N = Z.  With ``want_pre``
     also what the activation is taken of, [..., Z], which the gradient takes (None for no activation)."""
-    lib = load()
-    index, act, dt, M, N, Z, K, xs, wt = _linear_args(x, weight, activation)
-    lead = x.shape[:-1]
-    b, rs = _vector("bias", bias, Z, index, x.dtype), 0
+    index = _on_device("x", x)
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return sa_linear_fwd(x, weight, bias, activation, residual, want_pre, ws)
+    act, dt, M, N, Z, K, xs, wt, copies = _linear_args(x, weight, activation, index)
+    lead, dtype, device = x.shape[:-1], x.dtype, x.device
+    b, rs = _vector("bias", bias, Z, index, dtype), 0
     if residual is not None:
-        if tuple(residual.shape) != (*lead, N):
+        if residual.shape != (*lead, N):
             raise ValueError(f"residual{tuple(residual.shape)} must be {(*lead, N)}")
-        rs = _row_stride("residual", residual, N, index, x.dtype)
-    y = torch.empty((*lead, N), dtype=x.dtype, device=x.device)
-    z = torch.empty((*lead, Z), dtype=x.dtype, device=x.device) if want_pre and act else None
-    with _on(index):
-        stream = _stream_handle(index)
-        if ws is not None:
-            w = _ws_arg(ws, index)
-        else:
-            need = _linear_workspace_size(index, M, N, K, act, dt, 0,
-                                          _repack(x, xs, K) + 2 * _repack(weight, wt, K))
-            if need == 0:
-                raise SketchError(2, "sa_linear_workspace_size")
-            w = _stream_workspace(need, index, stream, _dense_ws)
-        st = lib.sa_linear_fwd(x.data_ptr(), xs, weight.data_ptr(), wt, b, _addr(residual), rs, M, N, K, act, dt,
-                               y.data_ptr(), _addr(z), w.data_ptr(), w.numel() * w.element_size(), stream)
-    _check(st, "sa_linear_fwd")
+        rs = _row_stride("residual", residual, N, index, dtype)
+    y = torch.empty((*lead, N), dtype=dtype, device=device)
+    z = torch.empty((*lead, Z), dtype=dtype, device=device) if want_pre and act else None
+    stream = _stream_handle(index)
+    w = _linear_workspace(ws, index, stream, M, N, K, act, dt, 0, copies)
+    st = load().sa_linear_fwd(x.data_ptr(), xs, weight.data_ptr(), wt, b, _addr(residual), rs, M, N, K, act, dt,
+                              y.data_ptr(), _addr(z), w.data_ptr(), w.nbytes, stream)
+    if st:
+        raise SketchError(st, "sa_linear_fwd")
     if ws is None:
         _note_call(w, index, stream, _dense_ws_cache)
     return (y, z) if want_pre else y
@@ -1102,32 +1109,26 @@ def sa_linear_bwd(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: 
                   ws: Optional[torch.Tensor] = None):
     """(dx [..., K], dw [Z, K], db [Z]) of x's type for the gradient dy [..., N] of ``sa_linear_fwd``'s y; ``pre`` is
     that call's.  The residual's gradient is dy itself.  What is not wanted is None."""
-    lib = load()
-    index, act, dt, M, N, Z, K, xs, wt = _linear_args(x, weight, activation)
-    lead = x.shape[:-1]
-    if tuple(dy.shape) != (*lead, N):
+    index = _on_device("x", x)
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return sa_linear_bwd(dy, x, weight, pre, activation, want_dx, want_dw, want_db, ws)
+    act, dt, M, N, Z, K, xs, wt, copies = _linear_args(x, weight, activation, index)
+    lead, dtype, device = x.shape[:-1], x.dtype, x.device
+    if dy.shape != (*lead, N):
         raise ValueError(f"dy{tuple(dy.shape)} must be {(*lead, N)}")
-    ys = _row_stride("dy", dy, N, index, x.dtype)
+    ys = _row_stride("dy", dy, N, index, dtype)
     if act:
-        if pre is None or tuple(pre.shape) != (*lead, Z) or pre.dtype is not x.dtype or not pre.is_contiguous() or \
-                not pre.is_cuda or pre.get_device() != index:
-            raise ValueError(f"pre must be contiguous {x.dtype} {(*lead, Z)} on x's device")
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
-    dw = torch.empty((Z, K), dtype=x.dtype, device=x.device) if want_dw else None
-    db = torch.empty(Z, dtype=x.dtype, device=x.device) if want_db else None
-    with _on(index):
-        stream = _stream_handle(index)
-        if ws is not None:
-            w = _ws_arg(ws, index)
-        else:
-            need = _linear_workspace_size(index, M, N, K, act, dt, 1, _repack(x, xs, K) +
-                                          2 * _repack(weight, wt, K) + 4 * _repack(dy, ys, N))
-            if need == 0:
-                raise SketchError(2, "sa_linear_workspace_size")
-            w = _stream_workspace(need, index, stream, _dense_ws)
-        st = lib.sa_linear_bwd(dy.data_ptr(), ys, x.data_ptr(), xs, weight.data_ptr(), wt, _addr(pre) if act else None,
-                               M, N, K, act, dt, _addr(dx), _addr(dw), _addr(db), w.data_ptr(),
-                               w.numel() * w.element_size(), stream)
+        if pre is None or pre.shape != (*lead, Z) or pre.dtype is not dtype or not pre.is_contiguous() or \
+                pre.get_device() != index:
+            raise ValueError(f"pre must be contiguous {dtype} {(*lead, Z)} on x's device")
+    dx = torch.empty(x.shape, dtype=dtype, device=device) if want_dx else None
+    dw = torch.empty((Z, K), dtype=dtype, device=device) if want_dw else None
+    db = torch.empty(Z, dtype=dtype, device=device) if want_db else None
+    stream = _stream_handle(index)
+    w = _linear_workspace(ws, index, stream, M, N, K, act, dt, 1, copies + 4 * _repack(dy, ys, N))
+    st = load().sa_linear_bwd(dy.data_ptr(), ys, x.data_ptr(), xs, weight.data_ptr(), wt, _addr(pre) if act else None,
+                              M, N, K, act, dt, _addr(dx), _addr(dw), _addr(db), w.data_ptr(), w.nbytes, stream)
     _check(st, "sa_linear_bwd")
     if ws is None:
         _note_call(w, index, stream, _dense_ws_cache)

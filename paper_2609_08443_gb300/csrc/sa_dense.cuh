@@ -1,5 +1,7 @@
 // Interface of the dense operators' kernels (include/sa_dense.h): layer norm and linear layers.
 #pragma once
+#include <atomic>
+
 #include "sa_common.cuh"
 
 #include "../../include/sa_dense.h"
@@ -135,6 +137,19 @@ struct Repack {
 cudaError_t launch_repack(Repack r0, Repack r1, cudaStream_t st);
 
 int sm_count();
+
+// Lets a kernel take `bytes` of dynamic shared memory on the current device; asked of the runtime once a device.
+template <auto Kernel>
+cudaError_t allow_smem(size_t bytes) {
+  static std::atomic<size_t> allowed[64];
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64 && allowed[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+  const cudaError_t s = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+  if (s == cudaSuccess && dev < 64) allowed[dev].store(bytes, std::memory_order_relaxed);
+  return s;
+}
 
 }  // namespace dense
 }  // namespace sa

@@ -122,7 +122,19 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
 }
 
 
-bool on_tensor_cores() { return sa::tc_path_enabled() && sa::tcc::device_is_sm103(); }
+bool on_tensor_cores() {
+  static std::atomic<int> known[64];  // 0: not asked yet, 1: yes, 2: no
+  if (!sa::tc_path_enabled()) return false;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (dev >= 64) return sa::tcc::device_is_sm103();
+  int k = known[dev].load(std::memory_order_relaxed);
+  if (k == 0) {
+    k = sa::tcc::device_is_sm103() ? 1 : 2;
+    known[dev].store(k, std::memory_order_relaxed);
+  }
+  return k == 1;
+}
 
 int repack_bits(const Mat& x, const Mat& w, const Mat& dy, const Linear& l) {
   auto need = [&](const Mat& m, int64_t len) {

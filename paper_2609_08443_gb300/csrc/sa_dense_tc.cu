@@ -570,9 +570,9 @@ bool make_map(CUtensorMap* m, const TcOperand& o, bool f32, int box_rows) {
 }
 
 // A launch of `ctas` CTAs in clusters of CTAS.
-template <int CTAS, class... P, class... A>
-cudaError_t launch_cluster(void (*fn)(P...), int ctas, int threads, size_t smem, cudaStream_t st, const A&... args) {
-  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+template <int CTAS, auto Kernel, class... A>
+cudaError_t launch_cluster(int ctas, int threads, size_t smem, cudaStream_t st, const A&... args) {
+  const cudaError_t e = allow_smem<Kernel>(smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(ctas), 1, 1);
@@ -586,7 +586,7 @@ cudaError_t launch_cluster(void (*fn)(P...), int ctas, int threads, size_t smem,
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CTAS > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, fn, args...);
+  return cudaLaunchKernelEx(&cfg, Kernel, args...);
 }
 
 // `halves` matrices of N bf16 columns side by side in rows of halves * N: boxes of 32 x 32 to be written.
@@ -613,8 +613,8 @@ cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaSt
       return cudaErrorInvalidValue;
   }
   cudaError_t e =
-      launch_cluster<CTAS>(&tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>, p.W * CTAS, C::THREADS, C::SMEM, st, ta,
-                           tb, ty, tz, a);
+      launch_cluster<CTAS, tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>>(p.W * CTAS, C::THREADS, C::SMEM, st, ta, tb, ty,
+                                                                         tz, a);
   ++*launches;
   if (e != cudaSuccess || p.cut == 0) return e;
   constexpr int CH = TileShape<CTAS>::template YN<EPI> / 32;
@@ -635,7 +635,7 @@ cudaError_t launch_grads(const TcGemm& gx, const TcPlan& px, const TcArgs& x, co
   CUtensorMap xy = xa, wy = wa;
   if (!F32 && ((x.vec & 1) && !make_out_map(&xy, x.y, x.M, x.N, 1))) return cudaErrorInvalidValue;
   if (!F32 && ((w.vec & 1) && !make_out_map(&wy, w.y, w.M, w.N, 1))) return cudaErrorInvalidValue;
-  cudaError_t e = launch_cluster<CTAS>(&tc_linear_grads_kernel<CTAS, F32>, (px.W + pw.W) * CTAS, C::THREADS, C::SMEM, st, xa, xb, wa,
+  cudaError_t e = launch_cluster<CTAS, tc_linear_grads_kernel<CTAS, F32>>((px.W + pw.W) * CTAS, C::THREADS, C::SMEM, st, xa, xb, wa,
                                        wb, xy, wy, x, w);
   ++*launches;
   if (e != cudaSuccess || px.cut + pw.cut == 0) return e;
