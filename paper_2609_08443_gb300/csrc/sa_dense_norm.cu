@@ -11,9 +11,10 @@
 // features, whose sums would not fit); its sums leave as one partial row, and a second kernel
 // adds the partial rows in block order, so results do not depend on timing.
 //
-// A row's loads, sums and stores wait for one another, so the next rows are on their way meanwhile: each
-// thread's own 16-byte pieces of the next two rows by cp.async (nobody else reads them, so nothing but the
-// thread's own copies is waited for), or, where rows are not 16-byte aligned, the next row's elements in registers.
+// A row's loads, sums and stores wait for one another, so the next two rows are on their way meanwhile, by cp.async
+// into a ring in shared memory: each thread's own 16-byte pieces (nobody else reads them, so nothing but the
+// thread's own copies is waited for), or, where rows are not 16-byte aligned, the 16-byte pieces that the row touches,
+// from which the row's threads pick their elements.
 #include "sa_dense_act.cuh"
 #include "sa_tc_common.cuh"
 
@@ -66,24 +67,30 @@ __device__ __forceinline__ void load_row(const void* p, sa_dtype dt, int64_t at,
   }
 }
 
+// bytes of the 16-byte pieces that a row of n elements can touch
+__host__ __device__ __forceinline__ uint32_t row_span(const Mat& m, int n) {
+  return !m.p ? 0 : ((uint32_t(n) * (m.dt == SA_BF16 ? 2 : 4) + 15) / 16 + 1) * 16;
+}
+
 // 16-byte pieces that a chunk of 8 elements takes
 __device__ __forceinline__ int pieces(const Mat& m) { return !m.p ? 0 : m.dt == SA_BF16 ? 1 : 2; }
 
-// One matrix along a walk: where this thread's first element of the next row to be fetched is, and how far the row
-// after it is away.
+// One matrix along a walk: where the next row to be fetched is (aligned rows: this thread's first element of it), and how
+// far the row after it is away.
 struct Track {
   const char* p;
   int64_t step;
-  bool half;  // bf16
+  bool half;       // bf16
+  uint32_t shift;  // of the row in work from its 16-byte boundary
   __device__ __forceinline__ Track(const Mat& m, int64_t row, int64_t rows, int first)
       : p(static_cast<const char*>(m.p)), half(m.dt == SA_BF16) {
     p += (row * m.stride + first) << (half ? 1 : 2);
     step = (rows * m.stride) << (half ? 1 : 2);
+    shift = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
   }
 };
 
-// The rows that a block walks, with the next ones on their way: VEC: each thread's slots of a ring of rows in
-// shared memory; else the next row's elements in registers, as they were read.  NEXT: false where neither fits.
+// The rows that a block walks, with the next ones on their way.  NEXT: false where the ring has no room.
 template <int T, int C, bool VEC, bool NEXT, bool GRAD>
 struct Walk {
   const int t, n;
@@ -92,7 +99,6 @@ struct Walk {
   const bool sum;       // there is a second summand
   bool in[VEC ? C : 1];
   Track x, r, dy;
-  uint32_t raw[VEC ? 1 : (GRAD ? 3 : 2)][VEC ? 1 : 8 * C];
   const char* ring;
   uint32_t put, get;  // byte offsets of the rows to fetch and to take
   uint32_t per_row, off_r, off_dy;
@@ -103,7 +109,8 @@ struct Walk {
   __device__ Walk(const NormArgs& a, char* mem)
       : t(threadIdx.x % T), n(a.n), rows(uint32_t(a.rows)), step(gridDim.x * rows_at_once<T>()),
         row(blockIdx.x * rows_at_once<T>() + threadIdx.x / T), ahead(row), sum(a.r.p != nullptr),
-        x(a.x, row, step, VEC ? t * 8 : t), r(a.r, row, step, VEC ? t * 8 : t), dy(a.dy, row, step, VEC ? t * 8 : t) {
+        x(a.x, row, step, VEC ? t * 8 : 0), r(a.r, row, step, VEC ? t * 8 : 0), dy(a.dy, row, step, VEC ? t * 8 : 0) {
+    put = get = 0;
     if (VEC) {
 #pragma unroll
       for (int c = 0; c < C; ++c) in[c] = column<T, true>(t, c, 0) < n;
@@ -111,58 +118,50 @@ struct Walk {
       off_r = C * kApart * pieces(a.x);
       off_dy = off_r + C * kApart * pieces(a.r);
       per_row = off_dy + (GRAD ? C * kApart * pieces(a.dy) : 0);
-      put = get = 0;
+    } else {
+      off_r = row_span(a.x, n);
+      off_dy = off_r + row_span(a.r, n);
+      per_row = off_dy + (GRAD ? row_span(a.dy, n) : 0);
+      ring = mem + (threadIdx.x / T) * (kRing * per_row);
     }
     if (NEXT) {
 #pragma unroll
-      for (int i = 0; i < (VEC ? kRing - 1 : 1); ++i) fetch();
+      for (int i = 0; i < kRing - 1; ++i) fetch();
     }
   }
   __device__ __forceinline__ void copy(const Track& m, uint32_t to) const {
+    if (VEC) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (!in[c]) continue;
-      if (m.half) {
-        copy16(to + c * kApart, m.p + c * T * 16);
-      } else {
-        copy16_l1(to + 2 * c * kApart, m.p + c * T * 32);
-        copy16_l1(to + (2 * c + 1) * kApart, m.p + c * T * 32 + 16);
+      for (int c = 0; c < C; ++c) {
+        if (!in[VEC ? c : 0]) continue;
+        if (m.half) {
+          copy16(to + c * kApart, m.p + c * T * 16);
+        } else {
+          copy16_l1(to + 2 * c * kApart, m.p + c * T * 32);
+          copy16_l1(to + (2 * c + 1) * kApart, m.p + c * T * 32 + 16);
+        }
       }
-    }
-  }
-  __device__ __forceinline__ void read(const Track& m, uint32_t* v) const {
-    if (m.half) {
-      const uint16_t* p = reinterpret_cast<const uint16_t*>(m.p);
-#pragma unroll
-      for (int i = 0; i < 8 * C; ++i) v[i] = i * T + t < n ? p[i * T] : 0;
     } else {
-      const uint32_t* p = reinterpret_cast<const uint32_t*>(m.p);
-#pragma unroll
-      for (int i = 0; i < 8 * C; ++i) v[i] = i * T + t < n ? p[i * T] : 0;
+      // the pieces that hold a byte of the row (the ends of the first and the last may belong to other rows)
+      const int shift = int(reinterpret_cast<uintptr_t>(m.p) & 15), bytes = shift + (n << (m.half ? 1 : 2));
+      const char* from = m.p - shift;
+      for (int at = t * 16; at < bytes; at += T * 16) copy16(to + at, from + at);
     }
   }
   // the next row's elements on their way
   __device__ __forceinline__ void fetch() {
     if (ahead < rows) {
-      if (VEC) {
-        const uint32_t to = ptx::smem_u32(ring) + put;
-        copy(x, to);
-        if (sum) copy(r, to + off_r);
-        if (GRAD) copy(dy, to + off_dy);
-      } else {
-        read(x, raw[0]);
-        if (sum) read(r, raw[1]);
-        if (GRAD) read(dy, raw[2]);
-      }
+      const uint32_t to = ptx::smem_u32(ring) + put;
+      copy(x, to);
+      if (sum) copy(r, to + off_r);
+      if (GRAD) copy(dy, to + off_dy);
     }
     ahead += step;
     x.p += x.step;
     if (sum) r.p += r.step;
     if (GRAD) dy.p += dy.step;
-    if (VEC) {
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      put = put == (kRing - 1) * per_row ? 0 : put + per_row;
-    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    put = put == (kRing - 1) * per_row ? 0 : put + per_row;
   }
   // the block's rows are not all done (the same for all of its threads)
   __device__ __forceinline__ bool more() const { return row - threadIdx.x / T < rows; }
@@ -184,11 +183,18 @@ struct Walk {
       for (int j = 0; j < 8; ++j) v[8 * c + j] = ADD ? v[8 * c + j] + q[j] : q[j];
     }
   }
+  // one element each T columns of an unaligned row
   template <bool ADD>
-  __device__ __forceinline__ void convert(bool half, const uint32_t* w, float* v) const {
+  __device__ __forceinline__ void pick(Track& m, const char* from, float* v) const {
+    from += m.shift;
+    m.shift = (m.shift + uint32_t(m.step)) & 15;
 #pragma unroll
     for (int i = 0; i < 8 * C; ++i) {
-      const float q = __uint_as_float(half ? w[i] << 16 : w[i]);
+      const int k = i * T + t;
+      float q = 0.f;
+      if (k < n)
+        q = m.half ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(from)[k]) << 16)
+                   : reinterpret_cast<const float*>(from)[k];
       v[i] = ADD ? v[i] + q : q;
     }
   }
@@ -213,16 +219,24 @@ struct Walk {
             }
       }
     } else if (NEXT) {
-      convert<false>(x.half, raw[0], h);
-      if (sum) convert<true>(r.half, raw[1], h);
-      if (GRAD) convert<false>(dy.half, raw[2], g);
-      if (!here())
+      // the slot that is filled here was read before the last row's sums, which the row's threads made together
+      fetch();
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      if (T <= 32)
+        __syncwarp();
+      else
+        __syncthreads();
+      const char* from = ring + get;
+      pick<false>(x, from, h);
+      if (sum) pick<true>(r, from + off_r, h);
+      if (GRAD) pick<false>(dy, from + off_dy, g);
+      get = get == (kRing - 1) * per_row ? 0 : get + per_row;
+      if (!here())  // the slots hold whatever was there
 #pragma unroll
         for (int i = 0; i < 8 * C; ++i) {
           h[i] = 0.f;
           if (GRAD) g[i] = 0.f;
         }
-      fetch();
     } else {
       const int end = here() ? n : 0;
       load_row<T, C, VEC>(a.x.p, a.x.dt, int64_t(row) * a.x.stride, t, end, h);
@@ -369,7 +383,7 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 // Blocks an SM that the register budget is made for: 64 to 128 a thread, by what it holds.
 template <int T, int C, bool VEC, bool GRAD>
 constexpr int blocks_at_once() {
-  return T == 1024 ? 1 : (C >= 2 || (GRAD && !VEC) ? 512 : GRAD || !VEC ? 768 : 1024) / block_threads<T>();
+  return T == 1024 ? 1 : 512 / block_threads<T>();
 }
 
 template <int T, int C, bool VEC, bool NEXT>
@@ -626,17 +640,21 @@ bool vec_ok(const NormArgs& a) {
 // Calls f with the layout for n features: (threads a row, chunks of 8 a thread).  More chunks spread what a thread spends
 // on a row's sums over more elements: two (8192 x 4096 in bf16, forward and gradient 30 and 46 us; one chunk 37 and 58),
 // four in the forward of wide rows that are read in bf16 alone (26 us; but 62 with fp32 rows and a residual, for 43
-// with two).  Unaligned rows, whose next elements wait in registers, have one.
+// with two).  Unaligned rows: two (10007 x 1001 in bf16 18 us, one 20, four 22), above 4096 features four (8000 x 8191:
+// 88 us, two 98).
 template <bool GRAD, class F>
 auto with_layout(int n, bool vec, bool narrow, F f) {
   using std::integral_constant;
 #define SA_LAYOUT(T, C, V) f(integral_constant<int, T>{}, integral_constant<int, C>{}, integral_constant<bool, V>{})
-  if (vec && !GRAD && narrow && n > 512) {
-    if (n <= 1024) return SA_LAYOUT(32, 4, true);
-    if (n <= 2048) return SA_LAYOUT(64, 4, true);
-    if (n <= 4096) return SA_LAYOUT(128, 4, true);
-    if (n <= 8192) return SA_LAYOUT(256, 4, true);
-    return SA_LAYOUT(512, 4, true);
+  if constexpr (!GRAD) {
+    if (vec && narrow && n > 512) {
+      if (n <= 1024) return SA_LAYOUT(32, 4, true);
+      if (n <= 2048) return SA_LAYOUT(64, 4, true);
+      if (n <= 4096) return SA_LAYOUT(128, 4, true);
+      if (n <= 8192) return SA_LAYOUT(256, 4, true);
+      return SA_LAYOUT(512, 4, true);
+    }
+    if (!vec && n > 4096 && n <= 8192) return SA_LAYOUT(256, 4, false);
   }
   if (vec) {
     if (n <= 64) return SA_LAYOUT(4, 2, true);
@@ -649,14 +667,14 @@ auto with_layout(int n, bool vec, bool narrow, F f) {
     if (n <= 8192) return SA_LAYOUT(512, 2, true);
     return SA_LAYOUT(1024, 2, true);
   }
-  if (n <= 64) return SA_LAYOUT(8, 1, false);
-  if (n <= 128) return SA_LAYOUT(16, 1, false);
-  if (n <= 256) return SA_LAYOUT(32, 1, false);
-  if (n <= 512) return SA_LAYOUT(64, 1, false);
-  if (n <= 1024) return SA_LAYOUT(128, 1, false);
-  if (n <= 2048) return SA_LAYOUT(256, 1, false);
-  if (n <= 4096) return SA_LAYOUT(512, 1, false);
-  if (n <= 8192) return SA_LAYOUT(1024, 1, false);
+  if (n <= 64) return SA_LAYOUT(4, 2, false);
+  if (n <= 128) return SA_LAYOUT(8, 2, false);
+  if (n <= 256) return SA_LAYOUT(16, 2, false);
+  if (n <= 512) return SA_LAYOUT(32, 2, false);
+  if (n <= 1024) return SA_LAYOUT(64, 2, false);
+  if (n <= 2048) return SA_LAYOUT(128, 2, false);
+  if (n <= 4096) return SA_LAYOUT(256, 2, false);
+  if (n <= 8192) return SA_LAYOUT(512, 2, false);
   return SA_LAYOUT(1024, 2, false);
 #undef SA_LAYOUT
 }
@@ -673,9 +691,11 @@ struct Walkers {
 template <int T, int C, bool VEC, bool NEXT, bool GRAD>
 Walkers walkers(const NormArgs& a) {
   Walkers w{blocks_at_once<T, C, VEC, GRAD>(), 0};
-  if (VEC && NEXT) {
+  if (NEXT) {
     auto pieces_of = [](const Mat& m) { return !m.p ? 0 : m.dt == SA_BF16 ? 1 : 2; };
-    w.ring = size_t(ring_rows<T>()) * C * (pieces_of(a.x) + pieces_of(a.r) + (GRAD ? pieces_of(a.dy) : 0)) * block_threads<T>() * 16;
+    const size_t row = VEC ? size_t(C) * (pieces_of(a.x) + pieces_of(a.r) + (GRAD ? pieces_of(a.dy) : 0)) * block_threads<T>() * 16
+                           : size_t(row_span(a.x, a.n) + row_span(a.r, a.n) + (GRAD ? row_span(a.dy, a.n) : 0)) * rows_at_once<T>();
+    w.ring = ring_rows<T>() * row;
     const int fit = int(size_t(220 * 1024) / (w.ring + 2048));
     if (w.blocks > fit) w.blocks = fit;
   }
@@ -684,13 +704,13 @@ Walkers walkers(const NormArgs& a) {
   return w;
 }
 
-template <class K>
-cudaError_t launch_walk(K kernel, const Walkers& w, int threads, size_t smem, const NormArgs& a, cudaStream_t st) {
+template <auto Kernel>
+cudaError_t launch_walk(const Walkers& w, int threads, size_t smem, const NormArgs& a, cudaStream_t st) {
   if (smem > 40 * 1024) {  // with the sums' exchange above what a launch may take unasked
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    const cudaError_t e = allow_smem<Kernel>(smem);
     if (e != cudaSuccess) return e;
   }
-  kernel<<<w.blocks, threads, smem, st>>>(a);
+  Kernel<<<w.blocks, threads, smem, st>>>(a);
   return cudaGetLastError();
 }
 
@@ -701,11 +721,13 @@ cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t st) {
   return with_layout<false>(a.n, vec_ok(a), narrow, [&](auto T, auto C, auto V) {
     constexpr bool NEXT = T() < 1024 || V();
     const Walkers w = walkers<T(), C(), V(), NEXT, false>(a);
-    if (T() >= 512 && (!NEXT || w.blocks == 0)) {  // no room for two rows
-      const Walkers plain = walkers<T(), C(), V(), false, false>(a);
-      return launch_walk(norm_fwd_kernel<T(), C(), V(), false>, plain, block_threads<T()>(), 0, a, st);
+    if constexpr (T() >= 512 && NEXT) {
+      if (w.blocks == 0) {  // no room for two rows
+        const Walkers plain = walkers<T(), C(), V(), false, false>(a);
+        return launch_walk<norm_fwd_kernel<T(), C(), V(), false>>(plain, block_threads<T()>(), 0, a, st);
+      }
     }
-    return launch_walk(norm_fwd_kernel<T(), C(), V(), NEXT>, w, block_threads<T()>(), w.ring, a, st);
+    return launch_walk<norm_fwd_kernel<T(), C(), V(), NEXT>>(w, block_threads<T()>(), w.ring, a, st);
   });
 }
 
@@ -731,10 +753,10 @@ cudaError_t launch_norm_bwd(const NormArgs& a, cudaStream_t st, int* launches) {
       const Walkers w = walkers<T(), C(), V(), NEXT, true>(a);
       G = w.blocks;
       ++*launches;
-      if (!a.partial) return launch_walk(norm_bwd_kernel<T(), C(), V(), NEXT, 0>, w, threads, w.ring, a, st);
+      if (!a.partial) return launch_walk<norm_bwd_kernel<T(), C(), V(), NEXT, 0>>(w, threads, w.ring, a, st);
       constexpr int SUMS = T() == 1024 ? 2 : 1;
       const size_t sums = SUMS == 2 ? size_t(2) * a.n * 4 : T() <= 32 ? size_t(kThreads / 32) * 2 * 8 * C() * T() * 4 : 0;
-      return launch_walk(norm_bwd_kernel<T(), C(), V(), NEXT, SUMS>, w, threads, sums > w.ring ? sums : w.ring, a, st);
+      return launch_walk<norm_bwd_kernel<T(), C(), V(), NEXT, SUMS>>(w, threads, sums > w.ring ? sums : w.ring, a, st);
     });
   if (e != cudaSuccess) return e;
   if (a.dw || a.db) {
