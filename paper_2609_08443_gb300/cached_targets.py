@@ -1,20 +1,21 @@
 """Sketches in a 4-bit cache and ranked targets that attend over them, as a server and a
 trainer on cache hits use them (paper Sec. 4.1 and 3.4): run
 
-    python -m paper_2609_08443_gb300.cached_targets
+    python -m paper_2609_08443_gb300.cached_targets [--refine LAYERS]
 
-One pass: the histories of a few users are sketched (Sec. 3.1), the sketches enter the
-cache in 4 bits, a request's candidates attend over their user's sketch, each user's live
+One pass: the histories of a few users are sketched (Sec. 3.1), refined by as many layers as are
+asked for (Sec. 3.3; none by default), the sketches enter the cache in 4 bits, a request's candidates attend over their user's sketch, each user's live
 history grows by a token and is attended to up to each request's own time, and the
 candidates' queries get their gradients.  Prints how far 4 bits are from the fp32 sketch.
 """
 from __future__ import annotations
 
+import argparse
 import math
 
 import torch
 
-from . import binding as b, workloads as wl
+from . import binding as b, refine, workloads as wl
 
 
 class PagePool:
@@ -52,14 +53,18 @@ def offsets(counts, device):
     return torch.tensor([0, *torch.tensor(counts).cumsum(0).tolist()], dtype=torch.int32, device=device)
 
 
-def run(lengths=(3000, 1200, 700), H=4, P=256, d=64, candidates=100, seed=0, device="cuda"):
-    """The pass described above; returns what a caller may want to check."""
+def run(lengths=(3000, 1200, 700), H=4, P=256, d=64, candidates=100, seed=0, device="cuda", layers=0):
+    """The pass described above, with ``layers`` of refinement; returns what a caller may want to check."""
     spec = wl.custom(lengths, H=H, P=P, d=d, seed=seed, bwd=False)
     t = wl.host_to_torch(spec, wl.make_host(spec), device)
     B, N = len(lengths), t["K"].shape[0]
 
     # a cache miss: sketch the histories, keep the sketches (keys and values in one) in 4 bits
     sketch = b.sa_sketch(t["K"], t["V"], t["cu_seqlens"], t["Q"])  # [B, H, P, d] fp32
+    if layers:
+        g = torch.Generator(device=device).manual_seed(seed + 2)
+        stack = [refine.random_layer(d, 4 * d, t["V"].dtype, device, g) for _ in range(layers)]
+        sketch = refine.sa_refine(sketch, t["V"], t["cu_seqlens"], stack).float()
     sketches = PagePool(B * (P // 64 + 1), B, P, H, d, device=device)
     for u in range(B):
         sketches.grow(u, P)
@@ -100,9 +105,12 @@ def run(lengths=(3000, 1200, 700), H=4, P=256, d=64, candidates=100, seed=0, dev
 
 
 def main() -> None:
-    res = run()
+    parser = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    parser.add_argument("--refine", type=int, default=0, metavar="LAYERS", help="refinement layers behind the sketch")
+    args = parser.parse_args()
+    res = run(layers=args.refine)
     torch.cuda.synchronize()
-    print(f"{res['tokens']} history rows sketched; sketches {res['bytes_fp32'] / 1e6:.2f} MB in fp32, "
+    print(f"{res['tokens']} history rows sketched, {args.refine} refinement layers; sketches {res['bytes_fp32'] / 1e6:.2f} MB in fp32, "
           f"{res['bytes_cached'] / 1e6:.2f} MB cached as keys and values")
     print(f"attention over the 4-bit sketch against fp32: relative difference {res['error']:.3f}")
     print(f"query gradient norm {float(res['dq'].float().norm()):.3e}; "
