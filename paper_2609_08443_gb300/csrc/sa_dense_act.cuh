@@ -102,11 +102,18 @@ __device__ __forceinline__ void store_terms(__nv_bfloat16* p, int64_t plane, con
   }
 }
 
-// 1 / (1 + e^-z).  Results that end in bf16 take the hardware's approximations of 2^x and 1/x (a few
-// 2^-23); fp32 results the full-precision functions.
+// 1 / (1 + e^-z), from the hardware's 2^x and 1/x (a few 2^-23).  FULL, for fp32 results: -z log2 e is kept in two
+// parts, since its rounding, times |z|, would be the largest error by far, and 1/x gets a Newton step.
 template <bool FULL>
 __device__ __forceinline__ float sigmoid(float z) {
-  return FULL ? 1.f / (1.f + expf(-z)) : ptx::rcp_approx(1.f + ptx::ex2(-1.4426950409f * z));
+  if (!FULL) return ptx::rcp_approx(1.f + ptx::ex2(-1.4426950409f * z));
+  const float t = -1.4426950409f * z;
+  // what the product and the constant were rounded by: log2 e = 1.44269502... + 1.92596e-8
+  const float low = fmaf(-1.4426950409f, z, -t) - 1.92596302e-8f * z;
+  float e = ptx::ex2(t);
+  e = isinf(e) || t < -126.f ? e : fmaf(e, 0.69314718f * low, e);
+  const float d = 1.f + e, r = ptx::rcp_approx(d);
+  return isinf(d) ? r : fmaf(r, fmaf(-d, r, 1.f), r);
 }
 
 // Phi(z) and e^(-z^2/2), Phi the normal distribution function.

@@ -172,51 +172,54 @@ struct ChunkEnd {
       T* y = static_cast<T*>(a.y) + m * a.N + n;
       T* z = static_cast<T*>(a.z) + m * a.Z + n;
       const T* r = static_cast<const T*>(a.r) + m * a.r_stride + n;
-      float next[EACH];  // the next row's residual, on its way
-      auto fetch = [&](int64_t at) {
-        if (at >= a.M || n >= a.N) return;
-        if (res_vec) {
-          load_n<EACH>(r, next);
-        } else {
-#pragma unroll
-          for (int j = 0; j < EACH; ++j) next[j] = ld_nc(r + j);
-        }
-      };
-      if (res) fetch(m);
-      // fp32 activations are long: few copies of them, or the instruction cache overflows
-#pragma unroll(F32 ? 1 : LANES)
-      for (int i = 0; i < LANES / PARTS; ++i) {
-        const int row = (first + i) * ROWS + lane / LANES;
-        const bool here = m < a.M && n < a.N;
-        float v[EACH], u[EACH], rv[EACH];
+      // rows by fours (fewer where there are fewer): their residuals are on their way together, and a long activation has
+      // four copies and not more, which the instruction cache holds
+      constexpr int COUNT = LANES / PARTS, FOUR = COUNT < 4 ? COUNT : 4;
+#pragma unroll 1
+      for (int i0 = 0; i0 < COUNT; i0 += FOUR) {
+        float rv[FOUR][EACH];
         if (EPI != EPI_PLAIN && res) {
 #pragma unroll
-          for (int j = 0; j < EACH; ++j) rv[j] = next[j];
-          r += int64_t(ROWS) * a.r_stride;
-          if (i + 1 < LANES / PARTS) fetch(m + ROWS);
-        }
-        read(s, row, p * (EACH / 4), v);
-        if (EPI == EPI_GATED) read(s, row, U + p * (EACH / 4), u);
-        if (EPI != EPI_PLAIN) {
+          for (int k = 0; k < FOUR; ++k) {
+            if (m + k * ROWS >= a.M || n >= a.N) continue;
+            const T* from = r + int64_t(k * ROWS) * a.r_stride;
+            if (res_vec) {
+              load_n<EACH>(from, rv[k]);
+            } else {
 #pragma unroll
-          for (int j = 0; j < EACH; ++j) {
-            v[j] += bv[j];
-            if (EPI == EPI_GATED) u[j] += bu[j];
+              for (int j = 0; j < EACH; ++j) rv[k][j] = ld_nc(from + j);
+            }
           }
-          if (a.z && here) {
-            store_n<EACH>(z, v);
-            if (EPI == EPI_GATED) store_n<EACH>(z + a.half, u);
-          }
-          activate_all(a.act, v, u);
-          if (res) {
-#pragma unroll
-            for (int j = 0; j < EACH; ++j) v[j] += rv[j];
-          }
+          r += int64_t(FOUR * ROWS) * a.r_stride;
         }
-        if (here) store_n<EACH>(y, v);
-        m += ROWS;
-        y += int64_t(ROWS) * a.N;
-        if (EPI != EPI_PLAIN) z += int64_t(ROWS) * a.Z;
+#pragma unroll
+        for (int k = 0; k < FOUR; ++k) {
+          const int row = (first + i0 + k) * ROWS + lane / LANES;
+          const bool here = m < a.M && n < a.N;
+          float v[EACH], u[EACH];
+          read(s, row, p * (EACH / 4), v);
+          if (EPI == EPI_GATED) read(s, row, U + p * (EACH / 4), u);
+          if (EPI != EPI_PLAIN) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+              v[j] += bv[j];
+              if (EPI == EPI_GATED) u[j] += bu[j];
+            }
+            if (a.z && here) {
+              store_n<EACH>(z, v);
+              if (EPI == EPI_GATED) store_n<EACH>(z + a.half, u);
+            }
+            activate_all(a.act, v, u);
+            if (res) {
+#pragma unroll
+              for (int j = 0; j < EACH; ++j) v[j] += rv[k][j];
+            }
+            z += int64_t(ROWS) * a.Z;
+          }
+          if (here) store_n<EACH>(y, v);
+          m += ROWS;
+          y += int64_t(ROWS) * a.N;
+        }
       }
     } else {  // one value a lane, so that single-element accesses coalesce; four rows at a time
       const int c = lane % COLS, n = n0 + c;
