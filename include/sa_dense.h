@@ -86,7 +86,8 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
                         int64_t w_stride, const void* z, int64_t M, int N, int K, sa_act act, sa_dtype dt, void* dx,
                         void* dw, void* db, void* workspace, size_t ws_bytes, void* stream);
 
-/* Name of the kernel that makes the products of a call with these sizes (pass: 0 y, 1 dx, 2 dW). */
+/* Name of the kernel that makes the products of a call with these sizes and aligned operands (pass: 0 y, 1 dx alone,
+ * 2 dW alone).  sa_select_path(1) takes plain CUDA-core kernels for every call (a cross-check). */
 const char* sa_linear_kernel_name(int64_t M, int N, int K, sa_act act, sa_dtype dt, int pass);
 
 #ifdef __cplusplus

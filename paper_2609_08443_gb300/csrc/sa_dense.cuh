@@ -68,6 +68,19 @@ constexpr int kMostFewRows = 16;
 // y for at most kMostFewRows rows of x
 cudaError_t launch_rows(const GemmArgs& g, cudaStream_t st);
 
+// Gradients for at most kMostFewRows rows, without the tensor cores: dx [M, K] from shares of W's rows
+// (partial: [rows_dx_shares][M][K]), dW [Z, K]; NULL where not wanted.
+struct RowsGradArgs {
+  const void *dz, *w, *x;  // dz [M, Z], w [Z, K], x [M, K]
+  int64_t pitch, w_stride, x_stride;
+  int M, Z, K;
+  sa_dtype dt;
+  float* partial;
+  void *dx, *dw;
+};
+int rows_dx_shares(int64_t Z, int64_t K);
+cudaError_t launch_rows_grads(const RowsGradArgs& a, cudaStream_t st, int* launches);
+
 // dz = dy act'(z) as [M, Z] rows of type dt, `pitch` elements apart (dz NULL: not stored), and
 // column sums of the unrounded dz into partial[g * Z + c] (NULL: none).
 struct ActGradArgs {

@@ -74,7 +74,7 @@ enum { COPY_X = 1, COPY_W = 2, COPY_DY = 4 };
 // Sections of a linear call's workspace: the operands' copies (fp32: their terms), dz, the pieces of cut tiles (of
 // one product at a time) and the partial column sums.
 struct Layout {
-  size_t x, w, dz, dz_terms, piece, partial, total;
+  size_t x, w, dz, dz_terms, piece, partial, dx_partial, total;
   sa::dense::TcPlan plan, dx, dw, side_dx, side_dw;  // of y; of either gradient alone; of both side by side
   bool side;
 };
@@ -83,6 +83,9 @@ struct Layout {
 bool few_rows(const Linear& l) { return l.M <= sa::dense::kMostFewRows; }
 
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
+
+// Few rows' gradients go without the tensor cores where these would want a copy of W.
+bool few_rows_grads(const Linear& l, int repack) { return few_rows(l) && l.M > 0 && (l.dt == SA_F32 || (repack & COPY_W)); }
 
 Layout linear_layout(const Linear& l, bool bwd, int repack) {
   Layout s{};
@@ -117,6 +120,8 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
   }
   s.piece = section(piece > 0, piece);
   s.partial = section(bwd, size_t(sa::dense::act_grad_blocks(l.M, l.N)) * size_t(l.Z) * sizeof(float));
+  // whichever way few rows go, which an operand's alignment has a say in, the size is enough
+  s.dx_partial = section(bwd && few_rows(l), size_t(sa::dense::rows_dx_shares(l.Z, l.K)) * size_t(l.M) * size_t(l.K) * sizeof(float));
   s.total = off;
   return s;
 }
@@ -315,7 +320,8 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
   SA_TRY(check_workspace(workspace, ws_bytes, lay.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* base = static_cast<char*>(workspace);
-  const bool tc = on_tensor_cores() && M > 0 && (dx || dw);
+  const bool few = few_rows_grads(l, copies) && sa::tc_path_enabled();
+  const bool tc = !few && on_tensor_cores() && M > 0 && (dx || dw);
   if (!tc && cudaMemsetAsync(workspace, 0, sizeof(sa::WsHeader), st) != cudaSuccess) return SA_ERR_CUDA;
 
   // dz and the columns' sums
@@ -342,7 +348,23 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
     ++launches;
   }
   const Mat dz = a.dz ? Mat{a.dz, a.pitch, dt} : mdy;
-  if (tc) {
+  if (few) {
+    sa::dense::RowsGradArgs r{};
+    r.dz = dz.p;
+    r.w = w;
+    r.x = x;
+    r.pitch = dz.stride;
+    r.w_stride = w_stride;
+    r.x_stride = x_stride;
+    r.M = int(M);
+    r.Z = l.Z;
+    r.K = K;
+    r.dt = dt;
+    r.partial = reinterpret_cast<float*>(base + lay.dx_partial);
+    r.dx = dx;
+    r.dw = dw;
+    if (e == cudaSuccess) e = sa::dense::launch_rows_grads(r, st, &launches);
+  } else if (tc) {
     sa::dense::Repack rz{}, rx{}, rw{};
     sa::dense::TcOperand oz{a.dz, M, l.Z, a.pitch};
     if (!a.dz) oz = operand(dz, M, l.Z, copies & COPY_DY, base + lay.dz_terms, &rz);
@@ -410,8 +432,8 @@ sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_
 
 const char* sa_linear_kernel_name(int64_t M, int N, int K, sa_act act, sa_dtype dt, int pass) {
   if (!linear_sizes_ok(M, N, K, act, dt) || pass < 0 || pass > 2) return "unsupported";
-  if (pass == 0 && M <= sa::dense::kMostFewRows && sa::tc_path_enabled())
-    return dt == SA_BF16 ? "mma_linear_rows" : "linear_rows";
+  if (M <= sa::dense::kMostFewRows && sa::tc_path_enabled() && (pass == 0 || (dt == SA_F32 && M > 0)))
+    return pass == 0 && dt == SA_BF16 ? "mma_linear_rows" : "linear_rows";
   if (!on_tensor_cores()) return "simt_linear";
   const int64_t Z = act == SA_ACT_SWIGLU ? 2 * int64_t(N) : N;
   const bool f32 = dt == SA_F32;

@@ -7,6 +7,12 @@
 //         stands for does not matter as long as both operands agree, so a thread takes 8 neighbours of a row
 //         of W and the same 8 of a row of x, and uses them in two products.
 //   fp32: 4 (2) rows of W against 8 (16) rows of x with multiply-adds.
+//
+// Their gradients, where the tensor cores would want a copy of W first (fp32, whose terms are three times its reading, and
+// rows that TMA cannot read):
+//   dx = dz W    bound by reading W once: a thread holds a few columns of dx for all rows and walks down its block's share of
+//                W's rows; the shares' sums are added in order by a second kernel.
+//   dW = dz^T x  bound by writing dW: a thread holds a few columns of x and walks down rows of dW.
 #include "sa_dense_act.cuh"
 
 namespace sa {
@@ -209,7 +215,163 @@ __global__ void __launch_bounds__(256, 2) rows_f32_kernel(const GemmArgs a) {
   }
 }
 
+constexpr int kCols = 4;            // columns of a thread
+constexpr int kStrip = 256 * kCols;  // and of a block
+
+// Column j of this thread in strip c0: neighbours where rows allow them to be accessed together, else one of 256 threads'.
+template <bool VEC>
+__device__ __forceinline__ int strip_column(int c0, int j) {
+  return c0 + (VEC ? int(threadIdx.x) * kCols + j : j * 256 + int(threadIdx.x));
+}
+template <bool VEC>
+__device__ __forceinline__ void load_columns(const float* row, int c0, int K, float* v) {
+  if (VEC) {
+    const int k = strip_column<VEC>(c0, 0);
+    const float4 f = k < K ? __ldg(reinterpret_cast<const float4*>(row + k)) : make_float4(0, 0, 0, 0);
+    v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) v[j] = strip_column<VEC>(c0, j) < K ? __ldg(row + strip_column<VEC>(c0, j)) : 0.f;
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load_columns(const __nv_bfloat16* row, int c0, int K, float* v) {
+  if (VEC) {
+    const int k = strip_column<VEC>(c0, 0);
+    const uint2 u = k < K ? __ldg(reinterpret_cast<const uint2*>(row + k)) : make_uint2(0, 0);
+    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) v[j] = strip_column<VEC>(c0, j) < K ? ld_nc(row + strip_column<VEC>(c0, j)) : 0.f;
+  }
+}
+
+// dz of `count` rows of W from z0 on into shared memory, [row][MT], zeros behind M.
+template <int MT, typename T>
+__device__ __forceinline__ void load_dz(const RowsGradArgs& a, int64_t z0, int count, float (*s)[MT]) {
+  for (int e = threadIdx.x; e < count * MT; e += 256) {
+    const int i = e % count, m = e / count;
+    s[i][m] = m < a.M ? ld_f32(static_cast<const T*>(a.dz) + int64_t(m) * a.pitch + z0 + i) : 0.f;
+  }
+}
+
+constexpr int kDzRows = 64;  // rows of W whose dz a block holds at a time
+
+// partial[blockIdx.y][m][k] = sum of dz[m, z] W[z, k] over the block's share of z
+template <typename T, int MT, bool VEC>
+__global__ void __launch_bounds__(256) rows_dx_kernel(const RowsGradArgs a) {
+  __shared__ __align__(16) float dz[kDzRows][MT];
+  const int c0 = blockIdx.x * kStrip;
+  const int64_t begin = range_begin(a.Z, gridDim.y, blockIdx.y), stop = range_begin(a.Z, gridDim.y, blockIdx.y + 1);
+  float acc[MT][kCols] = {};
+  for (int64_t z0 = begin; z0 < stop; z0 += kDzRows) {
+    const int count = stop - z0 < kDzRows ? int(stop - z0) : kDzRows;
+    __syncthreads();
+    load_dz<MT, T>(a, z0, count, dz);
+    __syncthreads();
+    const T* w = static_cast<const T*>(a.w) + z0 * a.w_stride;
+    for (int i = 0; i < count; i += 4) {  // four rows of W on their way
+      float v[4][kCols];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i + k < count) {
+          load_columns<VEC>(w + (i + k) * a.w_stride, c0, a.K, v[k]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) v[k][j] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i + k >= count) break;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const float d = dz[i + k][m];
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) acc[m][j] = fmaf(d, v[k][j], acc[m][j]);
+        }
+      }
+    }
+  }
+  float* out = a.partial + int64_t(blockIdx.y) * a.M * a.K;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int j = 0; j < kCols; ++j)
+      if (m < a.M && strip_column<VEC>(c0, j) < a.K) out[int64_t(m) * a.K + strip_column<VEC>(c0, j)] = acc[m][j];
+}
+
+template <typename T, int MT, bool VEC>
+__global__ void __launch_bounds__(256) rows_dw_kernel(const RowsGradArgs a) {
+  __shared__ __align__(16) float dz[kDzRows][MT];
+  const int c0 = blockIdx.x * kStrip;
+  const int64_t z0 = int64_t(blockIdx.y) * kDzRows;
+  const int count = a.Z - z0 < kDzRows ? int(a.Z - z0) : kDzRows;
+  load_dz<MT, T>(a, z0, count, dz);
+  float x[MT][kCols];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)  // behind M dz is 0: the last row again, which is there
+    load_columns<VEC>(static_cast<const T*>(a.x) + int64_t(m < a.M ? m : a.M - 1) * a.x_stride, c0, a.K, x[m]);
+  __syncthreads();
+  T* out = static_cast<T*>(a.dw) + z0 * a.K;
+#pragma unroll 2
+  for (int i = 0; i < count; ++i, out += a.K) {
+    float v[kCols] = {};
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      if (m >= a.M) break;
+      const float d = dz[i][m];
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) v[j] = fmaf(d, x[m][j], v[j]);
+    }
+    if (VEC) {
+      if (strip_column<VEC>(c0, 0) < a.K) store_n<4>(out + strip_column<VEC>(c0, 0), v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        if (strip_column<VEC>(c0, j) < a.K) st_from_f32(out + strip_column<VEC>(c0, j), v[j]);
+    }
+  }
+}
+
 }  // namespace
+
+int rows_dx_shares(int64_t Z, int64_t K) {
+  const int64_t strips = (K + kStrip - 1) / kStrip, most = (Z + 31) / 32;
+  const int64_t want = (int64_t(sm_count()) * 4 + strips - 1) / strips;
+  return int(want < most ? want : most);
+}
+
+cudaError_t launch_rows_grads(const RowsGradArgs& a, cudaStream_t st, int* launches) {
+  const size_t es = a.dt == SA_BF16 ? 2 : 4;
+  auto ok = [&](const void* p, int64_t stride) {  // rows of four neighbours
+    return reinterpret_cast<uintptr_t>(p) % (4 * es) == 0 && stride % 4 == 0;
+  };
+  const unsigned strips = unsigned((a.K + kStrip - 1) / kStrip);
+  cudaError_t e = cudaSuccess;
+  auto go = [&](auto kernel, unsigned y) {
+    kernel<<<dim3(strips, y), 256, 0, st>>>(a);
+    ++*launches;
+    e = cudaGetLastError();
+  };
+#define SA_PICK(KERNEL, VEC, Y)                                                                                   \
+  (a.dt == SA_BF16 ? (a.M <= 4 ? (VEC ? go(KERNEL<__nv_bfloat16, 4, true>, Y) : go(KERNEL<__nv_bfloat16, 4, false>, Y))   \
+                               : (VEC ? go(KERNEL<__nv_bfloat16, 16, true>, Y) : go(KERNEL<__nv_bfloat16, 16, false>, Y))) \
+                   : (a.M <= 4 ? (VEC ? go(KERNEL<float, 4, true>, Y) : go(KERNEL<float, 4, false>, Y))           \
+                               : (VEC ? go(KERNEL<float, 16, true>, Y) : go(KERNEL<float, 16, false>, Y))))
+  if (a.dx) {
+    const int G = rows_dx_shares(a.Z, a.K);
+    SA_PICK(rows_dx_kernel, a.K % 4 == 0 && ok(a.w, a.w_stride), unsigned(G));
+    const int64_t n = int64_t(a.M) * a.K;
+    if (e == cudaSuccess) e = launch_join_columns(a.partial, G, n, n, a.dx, a.dt, st);
+    ++*launches;
+  }
+  if (e == cudaSuccess && a.dw)
+    SA_PICK(rows_dw_kernel, a.K % 4 == 0 && ok(a.x, a.x_stride) && ok(a.dw, a.K), unsigned((a.Z + kDzRows - 1) / kDzRows));
+#undef SA_PICK
+  return e;
+}
 
 cudaError_t launch_rows(const GemmArgs& a, cudaStream_t st) {
   const bool gated = a.act == SA_ACT_SWIGLU;

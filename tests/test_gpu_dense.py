@@ -343,3 +343,23 @@ def test_repeated_calls_give_the_same_bits(cuda_lib):
     a = norm_call(cuda_lib, c, "f32", "bf16", "bf16")
     for _ in range(3):
         assert all(torch.equal(p, q) for p, q in zip(a, norm_call(cuda_lib, c, "f32", "bf16", "bf16")))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 70, 33), (4, 1030, 130), (5, 2052, 65), (16, 3001, 700), (16, 1024, 512), (3, 8, 4100)])
+def test_linear_grads_of_few_rows(cuda_lib, shape, dt):
+    """W read by columns and dW written row by row, over several strips and shares."""
+    for act in ("none", "swiglu"):
+        linear_check(cuda_lib, *shape, act, dt, seed=3)
+
+
+def test_linear_grads_of_few_rows_unaligned(cuda_lib):
+    """bf16 rows that TMA cannot read go the same way as fp32."""
+    b = cuda_lib
+    g = torch.Generator(device="cuda").manual_seed(6)
+    wide = torch.randn((96, 525), generator=g, device="cuda").bfloat16()
+    w, x = wide[:, 3:515], torch.randn((9, 512), generator=g, device="cuda").bfloat16()
+    dy = torch.randn((9, 96), generator=g, device="cuda").bfloat16()
+    got, want = b.sa_linear_bwd(dy, x, w), b.sa_linear_bwd(dy, x, w.contiguous())
+    for p, q in zip(got, want):  # the same sums in another order
+        assert float((p.float() - q.float()).norm()) <= 2e-3 * float(q.float().norm())
