@@ -110,7 +110,7 @@ struct TcPlan {
   int64_t mt, nt, KB, whole, cut;
   int cutters;  // workers that share the cut tiles
   size_t piece_bytes;
-  double cost;
+  double cost, bytes;  // estimated time (sa_dense_tc.cu has the unit), what has to move
 };
 
 // C[m, n] = sum_k A(m, k) B(n, k) on tcgen05.  K-major operands have k along their rows (a_mn, b_mn 0).
@@ -130,7 +130,9 @@ struct TcGemm {
   int clear;
 };
 
-TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32, int sms = 0, int ctas_only = 0);
+// How a product ends: as it is, with bias, activation and residual, or as SwiGLU.
+enum { EPI_PLAIN = 0, EPI_FULL = 1, EPI_GATED = 2 };
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int kind, bool f32, int sms = 0, int ctas_only = 0);
 cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches);
 // Plans of dx = dz W and dW = dz^T x (dz [M, Z], W [Z, K]) side by side (launch_tc_grads), where that is better than one
 // after the other at a cost of `apart`.

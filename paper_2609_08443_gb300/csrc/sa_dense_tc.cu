@@ -18,6 +18,7 @@
 // accumulators are added to sums in registers, which round to nearest.
 #include "sa_dense_tc.cuh"
 
+#include <cmath>
 #include <mutex>
 
 #include "sa_tc_common.cuh"
@@ -656,32 +657,39 @@ cudaError_t launch_kind(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaS
 
 }  // namespace
 
-// What a product of these sizes runs on, by the time its blocks would take (in units of a 64-deep block of
-// a pair's tile, 512 cycles): a pair's block makes four times a single CTA's products in the same time, both being
-// fed 32 KB a CTA; the end of a cut tile costs a launch and the pieces' way through L2.  `ctas_only` 0: either kind.
-TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32, int sms, int ctas_only) {
+// What a product of these sizes runs on, by the time that its blocks would take, in units of a 64-deep block of a pair's
+// tile: 512 cycles of products.  Measured beside that: a single CTA's block, a quarter of the products for the same
+// 32 KB a CTA, 1.4 units (L2 gives an SM about 45 bytes a cycle when all ask); of fp32 terms, 96 KB, 4.5.  A tile takes
+// no less than its end, which the next tile's products only hide; the last end is not hidden.  The end of a cut tile
+// costs a launch and the pieces' way through L2.  And memory moves 6.6 TB/s, 1.8 MB a unit.  `ctas_only` 0: either kind.
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int kind, bool f32, int sms, int ctas_only) {
   TcPlan best{};
-  best.cost = 0;
   if (sms <= 0) sms = sm_count();
   const int64_t KB = (K + 63) / 64;
+  const bool gated = kind == EPI_GATED;
+  best.KB = KB;
+  best.bytes = double(f32 ? 4 : 2) * (double(M) * K + double(N) * K * (gated ? 2 : 1) + double(M) * N * (gated ? 2 : 1));
   for (int ctas = 1; ctas <= (f32 || sms < 2 ? 1 : 2); ++ctas) {
     if (ctas_only && ctas != ctas_only) continue;
     const int bn = ctas == 2 ? 256 : 128, yn = gated ? bn / 2 : bn;
     const int64_t mt = (M + 128 * ctas - 1) / (128 * ctas), nt = (N + yn - 1) / yn, tiles = mt * nt;
     const int workers = sms / ctas;
     const int64_t waves = tiles / workers, rest = tiles % workers;
-    // the end of a worker's last tile, which nothing hides; fp32's is longer by its activation
-    const double block = f32 ? 3.0 : 1.0, end = f32 ? 24.0 : 6.0;
+    const double block = f32 ? 4.5 : ctas == 2 ? 1.0 : 1.4;
+    const double end = f32 ? (kind == EPI_PLAIN ? 8.0 : 24.0) : (kind == EPI_PLAIN ? 6.0 : 8.0) * ctas;
+    const double tile = KB * block > end ? KB * block : end;
     for (int cut = 0; cut <= (rest && KB > 1 ? 1 : 0); ++cut) {
       int cutters = 0;
       if (cut) {
-        const int64_t most = rest * (KB < 16 ? KB : 16);
+        // n shares of a tile take KB / n blocks each and half a unit each to be joined: least at sqrt(2 KB) (and never more
+        // than its blocks)
+        const int64_t each = int64_t(std::sqrt(2.0 * block * double(KB))) + 1, most = rest * (KB < each ? KB : each);
         cutters = int(most < workers ? most : workers);
       }
-      const double blocks =
-          cut ? double(waves) * KB + double((rest * KB + cutters - 1) / cutters) : double(waves + (rest ? 1 : 0)) * KB;
-      const double join = 10 + (ctas == 2 ? 12.0 : 4.0) + (cut ? 0.5 * cutters / rest : 0);
-      const double c = blocks * block + (cut ? join + end / 2 : end);
+      const double c = double(waves) * tile +
+                       (cut ? double((rest * KB + cutters - 1) / cutters) * block + 10 + (ctas == 2 ? 12.0 : 4.0) +
+                                  0.5 * cutters / rest + end / 2
+                            : (rest ? tile : 0.0) + end);
       if (best.ctas == 0 || c < best.cost) {
         best.cost = c;
         best.ctas = ctas;
@@ -694,24 +702,25 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, bool gated, bool f32, int sms, i
       }
     }
   }
-  best.KB = KB;
+  if (best.cost < best.bytes / 1.8e6) best.cost = best.bytes / 1.8e6;
   best.piece_bytes =
       best.cut ? size_t(best.cutters) * 2 * best.ctas * 128 * (best.ctas == 2 ? 256 : 128) * sizeof(float) : 0;
   return best;
 }
 
-// Both gradients' products side by side, each on a share of the SMs by its work, where that is no slower than one after the
-// other on all of them with two launches more (about ten units).
+// Both gradients' products side by side, each on a share of the SMs, where that is better than one after the other on all of
+// them with a launch or two more (about ten units).
 bool tc_plan_grads(int64_t M, int64_t Z, int64_t K, bool f32, double apart, TcPlan* x, TcPlan* w) {
   const int sms = sm_count();
-  if (sms < 8 || apart > 1000) return false;  // large products fill the GPU by themselves
+  if (sms < 8 || apart > 1500) return false;  // large products fill the GPU by themselves
   double best = apart + 10;
   bool found = false;
   for (int ctas = 1; ctas <= (f32 ? 1 : 2); ++ctas)
     for (int eighths = 2; eighths <= 6; ++eighths) {
       const int sx = sms * eighths / 8 / ctas * ctas;
-      const TcPlan px = tc_plan(M, K, Z, false, f32, sx, ctas), pw = tc_plan(Z, K, M, false, f32, sms - sx, ctas);
-      const double c = px.cost > pw.cost ? px.cost : pw.cost;
+      const TcPlan px = tc_plan(M, K, Z, EPI_PLAIN, f32, sx, ctas), pw = tc_plan(Z, K, M, EPI_PLAIN, f32, sms - sx, ctas);
+      double c = px.cost > pw.cost ? px.cost : pw.cost;
+      if (c < (px.bytes + pw.bytes) / 1.8e6) c = (px.bytes + pw.bytes) / 1.8e6;
       if (c < best) {
         best = c;
         *x = px;

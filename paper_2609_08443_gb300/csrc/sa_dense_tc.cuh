@@ -75,8 +75,6 @@ struct Segments {
   __device__ bool complete() const { return k0 == 0 && k1 == a.KB; }
 };
 
-enum { EPI_PLAIN = 0, EPI_FULL = 1, EPI_GATED = 2 };
-
 template <int CTAS>
 struct TileShape {
   static constexpr int BN = CTAS == 2 ? 256 : 128;           // accumulator columns
