@@ -132,7 +132,9 @@ struct TcGemm {
 
 // How a product ends: as it is, with bias, activation and residual, or as SwiGLU.
 enum { EPI_PLAIN = 0, EPI_FULL = 1, EPI_GATED = 2 };
-TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int kind, bool f32, int sms = 0, int ctas_only = 0);
+// `act`: kPlain for a product that ends as it is.
+constexpr int kPlain = -1;
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms = 0, int ctas_only = 0);
 cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches);
 // Plans of dx = dz W and dW = dz^T x (dz [M, Z], W [Z, K]) side by side (launch_tc_grads), where that is better than one
 // after the other at a cost of `apart`.

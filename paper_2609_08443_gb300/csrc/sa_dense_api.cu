@@ -82,8 +82,6 @@ struct Layout {
 // A product of this many rows of x is a matter of reading W (sa_dense_rows.cu), and takes no workspace on any path.
 bool few_rows(const Linear& l) { return l.M <= sa::dense::kMostFewRows; }
 
-int y_kind(int act) { return act == SA_ACT_SWIGLU ? sa::dense::EPI_GATED : sa::dense::EPI_FULL; }
-
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
 
 // Few rows' gradients go without the tensor cores where these would want a copy of W.
@@ -107,14 +105,14 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
   if (!bwd && few_rows(l)) {
     // no workspace but the status
   } else if (!bwd) {
-    s.plan = sa::dense::tc_plan(l.M, l.N, l.K, y_kind(l.act), f32);
+    s.plan = sa::dense::tc_plan(l.M, l.N, l.K, l.act, f32);
     piece = s.plan.piece_bytes;
   } else {
     const bool act = l.act != SA_ACT_NONE;
     s.dz = section(act, size_t(l.M) * pitch_of(l.Z) * size_of(l.dt));
     s.dz_terms = section(f32 || (!act && (repack & COPY_DY)), size_t(l.M) * pitch_of(l.Z) * each);
-    s.dx = sa::dense::tc_plan(l.M, l.K, l.Z, sa::dense::EPI_PLAIN, f32);
-    s.dw = sa::dense::tc_plan(l.Z, l.K, l.M, sa::dense::EPI_PLAIN, f32);
+    s.dx = sa::dense::tc_plan(l.M, l.K, l.Z, sa::dense::kPlain, f32);
+    s.dw = sa::dense::tc_plan(l.Z, l.K, l.M, sa::dense::kPlain, f32);
     s.side = sa::dense::tc_plan_grads(l.M, l.Z, l.K, f32, s.dx.cost + s.dw.cost, &s.side_dx, &s.side_dw);
     piece = s.dx.piece_bytes > s.dw.piece_bytes ? s.dx.piece_bytes : s.dw.piece_bytes;
     if (s.side && s.side_dx.piece_bytes + s.side_dw.piece_bytes > piece)
@@ -439,9 +437,9 @@ const char* sa_linear_kernel_name(int64_t M, int N, int K, sa_act act, sa_dtype 
   if (!on_tensor_cores()) return "simt_linear";
   const int64_t Z = act == SA_ACT_SWIGLU ? 2 * int64_t(N) : N;
   const bool f32 = dt == SA_F32;
-  const sa::dense::TcPlan p = pass == 0   ? sa::dense::tc_plan(M, N, K, y_kind(act), f32)
-                              : pass == 1 ? sa::dense::tc_plan(M, K, Z, sa::dense::EPI_PLAIN, f32)
-                                          : sa::dense::tc_plan(Z, K, M, sa::dense::EPI_PLAIN, f32);
+  const sa::dense::TcPlan p = pass == 0   ? sa::dense::tc_plan(M, N, K, act, f32)
+                              : pass == 1 ? sa::dense::tc_plan(M, K, Z, sa::dense::kPlain, f32)
+                                          : sa::dense::tc_plan(Z, K, M, sa::dense::kPlain, f32);
   return f32 ? "tc5_linear_f32" : p.ctas == 2 ? "tc5_linear_pair" : "tc5_linear";
 }
 

@@ -319,6 +319,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
 #pragma unroll 1
           for (int i = 0; i < CH * 32 / End::COLS; ++i) {
             const int n0 = y0 + i * End::COLS;
+            if (n0 >= a.N || m0 >= a.M) break;
             end.load_bias(a, lane, n0);
 #pragma unroll
             for (int k = 0; k < CH * 32 / End::COLS; ++k)
@@ -349,7 +350,9 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           auto read = [&] {
             if (i == CH - 1) release(set);
           };
-          if (complete && tma) {
+          if (y0 + i * 32 >= a.N || m0 >= a.M) {  // nothing of it is in y
+            read();
+          } else if (complete && tma) {
             outs.finish(a, ty, tz, acc + col(i, 0), acc + col(i, 1), m0, y0 + i * 32, read);
             if (i + 1 < CH) outs.load_bias(a, y0 + i * 32 + 32);
           } else if (complete) {
@@ -660,13 +663,17 @@ cudaError_t launch_kind(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaS
 // What a product of these sizes runs on, by the time that its blocks would take, in units of a 64-deep block of a pair's
 // tile: 512 cycles of products.  Measured beside that: a single CTA's block, a quarter of the products for the same
 // 32 KB a CTA, 1.4 units (L2 gives an SM about 45 bytes a cycle when all ask); of fp32 terms, 96 KB, 4.5.  A tile takes
-// no less than its end, which the next tile's products only hide; the last end is not hidden.  The end of a cut tile
-// costs a launch and the pieces' way through L2.  And memory moves 6.6 TB/s, 1.8 MB a unit.  `ctas_only` 0: either kind.
-TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int kind, bool f32, int sms, int ctas_only) {
+// no less than its end, which the next tile's products only hide; the last end is not hidden.  Cut tiles cost a second
+// kernel, 25 units, and their pieces' way to L2 and back (2048 x 1024 -> 1024: 9 us whole, 19 cut; 128 x 4096 -> 8192: 23
+// and 20; dx of 16384 x 8192 -> 1024: 168 and 158).  And memory moves 6.6 TB/s, 1.8 MB a unit.  `ctas_only` 0: either kind.
+TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms, int ctas_only) {
   TcPlan best{};
   if (sms <= 0) sms = sm_count();
   const int64_t KB = (K + 63) / 64;
-  const bool gated = kind == EPI_GATED;
+  const bool gated = act == SA_ACT_SWIGLU, plain = act == kPlain;
+  // the end of a tile: rows that 16-byte pieces do not fit go element by element; fp32 has CUDA's erfc in gelu
+  const double slow = N % (f32 ? 4 : 8) == 0 ? 1.0 : f32 ? 1.5 : 3.0;
+  const double end1 = slow * (!f32 ? (plain ? 6.0 : 8.0) : act == SA_ACT_GELU ? 36.0 : gated ? 20.0 : plain ? 8.0 : 12.0);
   best.KB = KB;
   best.bytes = double(f32 ? 4 : 2) * (double(M) * K + double(N) * K * (gated ? 2 : 1) + double(M) * N * (gated ? 2 : 1));
   for (int ctas = 1; ctas <= (f32 || sms < 2 ? 1 : 2); ++ctas) {
@@ -676,7 +683,7 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int kind, bool f32, int sms, int
     const int workers = sms / ctas;
     const int64_t waves = tiles / workers, rest = tiles % workers;
     const double block = f32 ? 4.5 : ctas == 2 ? 1.0 : 1.4;
-    const double end = f32 ? (kind == EPI_PLAIN ? 8.0 : 24.0) : (kind == EPI_PLAIN ? 6.0 : 8.0) * ctas;
+    const double end = end1 * (f32 ? 1 : ctas);
     const double tile = KB * block > end ? KB * block : end;
     for (int cut = 0; cut <= (rest && KB > 1 ? 1 : 0); ++cut) {
       int cutters = 0;
@@ -686,10 +693,11 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int kind, bool f32, int sms, int
         const int64_t each = int64_t(std::sqrt(2.0 * block * double(KB))) + 1, most = rest * (KB < each ? KB : each);
         cutters = int(most < workers ? most : workers);
       }
-      const double c = double(waves) * tile +
-                       (cut ? double((rest * KB + cutters - 1) / cutters) * block + 10 + (ctas == 2 ? 12.0 : 4.0) +
-                                  0.5 * cutters / rest + end / 2
-                            : (rest ? tile : 0.0) + end);
+      const double rows = M < 128 * ctas ? double(M) : 128.0 * ctas;  // of a piece
+      const double join = 25 + 0.5 * cutters / (rest ? rest : 1) + 2.0 * (cutters + rest) * rows * bn * 4 / 1.8e6;
+      const double c = double(waves) * tile + (cut ? double((rest * KB + cutters - 1) / cutters) * block + join
+                                                   : (rest ? tile : 0.0) + end) +
+                       (ctas == 2 ? 8.0 : 0.0);  // a pair's launch and its two meetings
       if (best.ctas == 0 || c < best.cost) {
         best.cost = c;
         best.ctas = ctas;
@@ -718,7 +726,7 @@ bool tc_plan_grads(int64_t M, int64_t Z, int64_t K, bool f32, double apart, TcPl
   for (int ctas = 1; ctas <= (f32 ? 1 : 2); ++ctas)
     for (int eighths = 2; eighths <= 6; ++eighths) {
       const int sx = sms * eighths / 8 / ctas * ctas;
-      const TcPlan px = tc_plan(M, K, Z, EPI_PLAIN, f32, sx, ctas), pw = tc_plan(Z, K, M, EPI_PLAIN, f32, sms - sx, ctas);
+      const TcPlan px = tc_plan(M, K, Z, kPlain, f32, sx, ctas), pw = tc_plan(Z, K, M, kPlain, f32, sms - sx, ctas);
       double c = px.cost > pw.cost ? px.cost : pw.cost;
       if (c < (px.bytes + pw.bytes) / 1.8e6) c = (px.bytes + pw.bytes) / 1.8e6;
       if (c < best) {
