@@ -440,7 +440,7 @@ const char* sa_linear_kernel_name(int64_t M, int N, int K, sa_act act, sa_dtype 
   const sa::dense::TcPlan p = pass == 0   ? sa::dense::tc_plan(M, N, K, act, f32)
                               : pass == 1 ? sa::dense::tc_plan(M, K, Z, sa::dense::kPlain, f32)
                                           : sa::dense::tc_plan(Z, K, M, sa::dense::kPlain, f32);
-  return f32 ? (p.ctas == 2 ? "tc5_linear_f32_pair" : "tc5_linear_f32") : p.ctas == 2 ? "tc5_linear_pair" : "tc5_linear";
+  return f32 ? "tc5_linear_f32" : p.ctas == 2 ? "tc5_linear_pair" : "tc5_linear";
 }
 
 }  // extern "C"

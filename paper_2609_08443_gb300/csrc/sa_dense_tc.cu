@@ -3,7 +3,7 @@
 // nothing is transposed in memory).
 //
 // A tile is 256 x 256 for a pair of CTAs (cta_group::2: each holds 128 rows of A, half of B's rows and
-// 128 rows of the result; 256 x 128 in fp32) or 128 x 128 for one CTA.  Warp 0 loads (TMA, 64 deep blocks, six stages),
+// 128 rows of the result) or 128 x 128 for one CTA.  Warp 0 loads (TMA, 64 deep blocks, up to five stages),
 // warp 1 issues the products, warps 4-11 end the tiles: two sets of accumulators in TMEM let one
 // tile's end overlap the next one's products.  SwiGLU's tile takes the same columns of both halves of
 // W, so gate and value meet in one warp.
@@ -38,13 +38,11 @@ struct TcCfg {
   using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
   using End = ChunkEnd<T, EPI>;
   static constexpr int PLANES = F32 ? 3 : 1;
-  static constexpr int B_BOXES = TileShape<CTAS, F32>::BN / CTAS / 64;  // boxes of 64 rows of B that a CTA loads
-  static constexpr int B_BYTES = B_BOXES * 8192;
-  static constexpr int STAGE = PLANES * (kBlockBytes + B_BYTES);
+  static constexpr int STAGE = 2 * PLANES * kBlockBytes;
   static constexpr int OUT = F32 ? kStageBytes : TmaOut<EPI>::BUFFERS * kOutBytes;  // of an epilogue warp
   static constexpr int STAGES = F32 ? 2 : EPI == EPI_GATED ? 4 : 5;
-  static constexpr int BN = TileShape<CTAS, F32>::BN;
-  static constexpr int WARPS = 4 * TileShape<CTAS, F32>::GROUPS;  // that end tiles
+  static constexpr int BN = TileShape<CTAS>::BN;
+  static constexpr int WARPS = 4 * TileShape<CTAS>::GROUPS;  // that end tiles
   static constexpr int THREADS = 128 + 32 * WARPS;
   static constexpr int TMEM = 2 * BN;
   static constexpr int OFF_OUT = STAGES * STAGE;
@@ -52,7 +50,7 @@ struct TcCfg {
   static constexpr int SMEM = OFF_BAR + 256;
 };
 static_assert(TcCfg<2, false, EPI_GATED>::SMEM <= 232448 && TcCfg<2, false, EPI_FULL>::SMEM <= 232448 &&
-                  TcCfg<1, true, EPI_GATED>::SMEM <= 232448 && TcCfg<2, true, EPI_GATED>::SMEM <= 232448,
+                  TcCfg<1, true, EPI_GATED>::SMEM <= 232448,
               "shared memory of a CTA");
 
 // ------------------------------------------------------ cta_group::2 forms
@@ -115,7 +113,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
                                                const bool clear) {
   using C = TcCfg<CTAS, F32, EPI>;
   using End = typename C::End;
-  using Shape = TileShape<CTAS, F32>;
+  using Shape = TileShape<CTAS>;
   constexpr int YN = Shape::template YN<EPI>;
   extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_u32(smem);
@@ -166,13 +164,13 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       int mb, nb;
       tile_place(a, seg.tile, &mb, &nb);
       const int m0 = (mb * CTAS + int(rank)) * 128;
-      // this CTA's rows of B: SwiGLU's halves are the pair's CTAs, or 64 rows each
+      // this CTA's 128 rows of B: SwiGLU's halves are the pair's CTAs, or 64 rows each
       int b0, b1;
       if (EPI == EPI_GATED) {
         b0 = CTAS == 2 ? int(rank * a.half) + nb * YN : nb * YN;
         b1 = CTAS == 2 ? b0 + 64 : int(a.half) + nb * YN;
       } else {
-        b0 = nb * YN + (CTAS == 2 ? int(rank) * 64 * C::B_BOXES : 0);
+        b0 = nb * YN + (CTAS == 2 ? int(rank) * 128 : 0);
         b1 = b0 + 64;
       }
       for (int kb = seg.k0; kb < seg.k1; ++kb, ++n) {
@@ -184,7 +182,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         const int k = kb * 64;
 #pragma unroll
         for (int p = 0; p < C::PLANES; ++p) {
-          const uint32_t da = dst + p * kBlockBytes, db = dst + C::PLANES * kBlockBytes + p * C::B_BYTES;
+          const uint32_t da = dst + p * kBlockBytes, db = dst + (C::PLANES + p) * kBlockBytes;
           if (A_MN) {
             tc_load<CTAS>(da, &ta, bar, m0, k, p);
             tc_load<CTAS>(da + 8192, &ta, bar, m0 + 64, k, p);
@@ -193,10 +191,10 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           }
           if (B_MN) {
             tc_load<CTAS>(db, &tb, bar, b0, k, p);
-            if (C::B_BOXES == 2) tc_load<CTAS>(db + 8192, &tb, bar, b1, k, p);
+            tc_load<CTAS>(db + 8192, &tb, bar, b1, k, p);
           } else {
             tc_load<CTAS>(db, &tb, bar, k, b0, p);
-            if (C::B_BOXES == 2) tc_load<CTAS>(db + 8192, &tb, bar, k, b1, p);
+            tc_load<CTAS>(db + 8192, &tb, bar, k, b1, p);
           }
         }
       }
@@ -233,7 +231,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               tc_mma<CTAS>(d, sdesc_add(sa, pa[i] * kBlockBytes + k * step_a),
-                           sdesc_add(sb, pb[i] * C::B_BYTES + k * step_b), idesc, accumulate);
+                           sdesc_add(sb, pb[i] * kBlockBytes + k * step_b), idesc, accumulate);
               accumulate = 1;
             }
           tc_commit<CTAS>(empty(s));
@@ -434,7 +432,7 @@ template <int CTAS, bool F32, int EPI>
 __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   using C = TcCfg<CTAS, F32, EPI>;
   using End = typename C::End;
-  using Shape = TileShape<CTAS, F32>;
+  using Shape = TileShape<CTAS>;
   constexpr int YN = Shape::template YN<EPI>, CH = YN / 32;
   constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
   extern __shared__ __align__(128) char stages[];  // [4][32 / COLS][kStageBytes]
@@ -623,7 +621,7 @@ cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaSt
                                                                          tz, a);
   ++*launches;
   if (e != cudaSuccess || p.cut == 0) return e;
-  constexpr int CH = TileShape<CTAS, F32>::template YN<EPI> / 32;
+  constexpr int CH = TileShape<CTAS>::template YN<EPI> / 32;
   tc_join_kernel<CTAS, F32, EPI>
       <<<unsigned(p.cut * CTAS * CH), kJoinThreads, 4 * (EPI == EPI_GATED ? 2 : 1) * kStageBytes, st>>>(a);
   ++*launches;
@@ -645,7 +643,7 @@ cudaError_t launch_grads(const TcGemm& gx, const TcPlan& px, const TcArgs& x, co
                                        wb, xy, wy, x, w);
   ++*launches;
   if (e != cudaSuccess || px.cut + pw.cut == 0) return e;
-  constexpr int CH = TileShape<CTAS, F32>::template YN<EPI_PLAIN> / 32;
+  constexpr int CH = TileShape<CTAS>::template YN<EPI_PLAIN> / 32;
   tc_join_grads_kernel<CTAS, F32>
       <<<unsigned((px.cut + pw.cut) * CTAS * CH), kJoinThreads, 4 * kStageBytes, st>>>(x, w, int(px.cut * CTAS * CH));
   ++*launches;
@@ -664,8 +662,8 @@ cudaError_t launch_kind(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaS
 
 // What a product of these sizes runs on, by the time that its blocks would take, in units of a 64-deep block of a pair's
 // tile: 512 cycles of products.  Measured beside that: a single CTA's block, a quarter of the products for the same
-// 32 KB a CTA, 1.4 units (L2 gives an SM about 45 bytes a cycle when all ask); of fp32 terms, 96 KB, 4.5 (a pair's, 72 KB
-// a CTA, 3.3).  A tile takes
+// 32 KB a CTA, 1.4 units; of fp32 terms 4.5 (24 products read 8 KB each and 96 KB are written beside them: 2304 cycles of
+// shared memory; pairs of 256 x 128 and half-deep stages measured the same or worse).  A tile takes
 // no less than its end, which the next tile's products only hide; the last end is not hidden.  Cut tiles cost a second
 // kernel, 25 units, and their pieces' way to L2 and back (2048 x 1024 -> 1024: 9 us whole, 19 cut; 128 x 4096 -> 8192: 23
 // and 20; dx of 16384 x 8192 -> 1024: 168 and 158).  And memory moves 6.6 TB/s, 1.8 MB a unit.  `ctas_only` 0: either kind.
@@ -679,14 +677,14 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms, int 
   const double end1 = slow * (!f32 ? (plain ? 6.0 : 8.0) : act == SA_ACT_GELU ? 36.0 : gated ? 20.0 : plain ? 8.0 : 12.0);
   best.KB = KB;
   best.bytes = double(f32 ? 4 : 2) * (double(M) * K + double(N) * K * (gated ? 2 : 1) + double(M) * N * (gated ? 2 : 1));
-  for (int ctas = 1; ctas <= (sms < 2 ? 1 : 2); ++ctas) {
+  for (int ctas = 1; ctas <= (f32 || sms < 2 ? 1 : 2); ++ctas) {
     if (ctas_only && ctas != ctas_only) continue;
-    const int bn = ctas == 2 && !f32 ? 256 : 128, yn = gated ? bn / 2 : bn;
+    const int bn = ctas == 2 ? 256 : 128, yn = gated ? bn / 2 : bn;
     const int64_t mt = (M + 128 * ctas - 1) / (128 * ctas), nt = (N + yn - 1) / yn, tiles = mt * nt;
     const int workers = sms / ctas;
     const int64_t waves = tiles / workers, rest = tiles % workers;
-    const double block = f32 ? (ctas == 2 ? 3.3 : 4.5) : ctas == 2 ? 1.0 : 1.4;
-    const double end = end1 * (f32 || ctas == 1 ? 1.0 : 1.8);
+    const double block = f32 ? 4.5 : ctas == 2 ? 1.0 : 1.4;
+    const double end = end1 * (ctas == 2 ? 1.8 : 1.0);
     const double tile = KB * block > end ? KB * block : end;
     for (int cut = 0; cut <= (rest && KB > 1 ? 1 : 0); ++cut) {
       int cutters = 0;
@@ -715,7 +713,7 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms, int 
   }
   if (best.cost < best.bytes / 1.8e6) best.cost = best.bytes / 1.8e6;
   best.piece_bytes =
-      best.cut ? size_t(best.cutters) * 2 * best.ctas * 128 * (best.ctas == 2 && !f32 ? 256 : 128) * sizeof(float) : 0;
+      best.cut ? size_t(best.cutters) * 2 * best.ctas * 128 * (best.ctas == 2 ? 256 : 128) * sizeof(float) : 0;
   return best;
 }
 
@@ -726,7 +724,7 @@ bool tc_plan_grads(int64_t M, int64_t Z, int64_t K, bool f32, double apart, TcPl
   if (sms < 8 || apart > 1500) return false;  // large products fill the GPU by themselves
   double best = apart + 10;
   bool found = false;
-  for (int ctas = 1; ctas <= 2; ++ctas)
+  for (int ctas = 1; ctas <= (f32 ? 1 : 2); ++ctas)
     for (int eighths = 2; eighths <= 6; ++eighths) {
       const int sx = sms * eighths / 8 / ctas * ctas;
       const TcPlan px = tc_plan(M, K, Z, kPlain, f32, sx, ctas), pw = tc_plan(Z, K, M, kPlain, f32, sms - sx, ctas);
@@ -777,17 +775,14 @@ TcArgs tc_args(const TcGemm& g, const TcPlan& p) {
 
 cudaError_t launch_tc_gemm(const TcGemm& g, const TcPlan& p, cudaStream_t st, int* launches) {
   const TcArgs a = tc_args(g, p);
-  if (g.dt == SA_F32)
-    return p.ctas == 2 ? launch_kind<2, true>(g, p, a, st, launches) : launch_kind<1, true>(g, p, a, st, launches);
+  if (g.dt == SA_F32) return launch_kind<1, true>(g, p, a, st, launches);
   return p.ctas == 2 ? launch_kind<2, false>(g, p, a, st, launches) : launch_kind<1, false>(g, p, a, st, launches);
 }
 
 cudaError_t launch_tc_grads(const TcGemm& gx, const TcPlan& px, const TcGemm& gw, const TcPlan& pw, cudaStream_t st,
                             int* launches) {
   const TcArgs x = tc_args(gx, px), w = tc_args(gw, pw);
-  if (gx.dt == SA_F32)
-    return px.ctas == 2 ? launch_grads<2, true>(gx, px, x, gw, pw, w, st, launches)
-                        : launch_grads<1, true>(gx, px, x, gw, pw, w, st, launches);
+  if (gx.dt == SA_F32) return launch_grads<1, true>(gx, px, x, gw, pw, w, st, launches);
   return px.ctas == 2 ? launch_grads<2, false>(gx, px, x, gw, pw, w, st, launches)
                       : launch_grads<1, false>(gx, px, x, gw, pw, w, st, launches);
 }

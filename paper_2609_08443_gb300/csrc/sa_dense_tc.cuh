@@ -75,9 +75,9 @@ struct Segments {
   __device__ bool complete() const { return k0 == 0 && k1 == a.KB; }
 };
 
-template <int CTAS, bool F32>
+template <int CTAS>
 struct TileShape {
-  static constexpr int BN = CTAS == 2 && !F32 ? 256 : 128;    // accumulator columns
+  static constexpr int BN = CTAS == 2 ? 256 : 128;           // accumulator columns
   static constexpr int GROUPS = 2;                            // epilogue warps of a row
   template <int EPI>
   static constexpr int YN = EPI == EPI_GATED ? BN / 2 : BN;  // columns of y
