@@ -7,12 +7,15 @@
 //         stands for does not matter as long as both operands agree, so a thread takes 8 neighbours of a row
 //         of W and the same 8 of a row of x, and uses them in two products.
 //   fp32: 4 (2) rows of W against 8 (16) rows of x with multiply-adds.
+// 1 x 4096 -> 8192 gated in bf16: 23 us (5.9 TB/s), 16 rows 26 us (x comes from L1 and L2 as well as W from memory); 1 x 1024
+// -> 4096: 2.9 us, a launch.
 //
 // Their gradients, where the tensor cores would want a copy of W first (fp32, whose terms are three times its reading, and
 // rows that TMA cannot read):
 //   dx = dz W    bound by reading W once: a thread holds a few columns of dx for all rows and walks down its block's share of
 //                W's rows; the shares' sums are added in order by a second kernel.
 //   dW = dz^T x  bound by writing dW: a thread holds a few columns of x and walks down rows of dW.
+// Both for 4 x 5954 -> 5312 in fp32: 87 us of a floor of 38 (copies for the tensor cores: 212).
 #include "sa_dense_act.cuh"
 
 namespace sa {

@@ -87,7 +87,8 @@ __global__ void __launch_bounds__(256) simt_gemm_kernel(const GemmArgs g) {
 // warp takes other rows); a block's eight warps and its share of the rows leave one partial row of sums.
 
 // Aligned rows (VEC) come through a ring of three rows a thread in shared memory, filled by the thread's own cp.async: a
-// row's loads and its arithmetic would wait for each other (16384 x 8192 gated: 131 us with two rows in registers, RING us).
+// row's loads and its arithmetic would wait for each other (the columns' sums of 16384 x 8192 gated: 107 us with two rows
+// in registers, 70 so, 5.7 TB/s).
 constexpr int kRing = 3;
 
 template <typename T, bool VEC, bool GATED>
