@@ -155,16 +155,17 @@ cudaError_t launch_repack(Repack r0, Repack r1, cudaStream_t st);
 
 int sm_count();
 
-// Lets a kernel take `bytes` of dynamic shared memory on the current device; asked of the runtime once a device.
+// Lets a kernel take `bytes` of dynamic shared memory on the current device; asked of the runtime once a device.  A kernel
+// asks for the same number at all times: threads' calls may come in any order.
 template <auto Kernel>
 cudaError_t allow_smem(size_t bytes) {
-  static std::atomic<size_t> allowed[64];
+  static std::atomic<bool> allowed[64];
   int dev = 0;
   const cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  if (dev < 64 && allowed[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+  if (dev < 64 && allowed[dev].load(std::memory_order_relaxed)) return cudaSuccess;
   const cudaError_t s = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
-  if (s == cudaSuccess && dev < 64) allowed[dev].store(bytes, std::memory_order_relaxed);
+  if (s == cudaSuccess && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
   return s;
 }
 

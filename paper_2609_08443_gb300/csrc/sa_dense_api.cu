@@ -90,7 +90,10 @@ bool few_rows_grads(const Linear& l, int repack) { return few_rows(l) && l.M > 0
 Layout linear_layout(const Linear& l, bool bwd, int repack) {
   Layout s{};
   const bool f32 = l.dt == SA_F32;
-  if (f32) repack = COPY_X | COPY_W | COPY_DY;
+  // few rows' gradients in fp32, or with a W that needs a copy, never reach the tensor cores
+  const bool few_f32 = bwd && f32 && few_rows(l);
+  if (f32) repack = few_f32 ? 0 : COPY_X | COPY_W | COPY_DY;
+  if (bwd && few_rows(l)) repack &= ~COPY_W;
   size_t off = sizeof(sa::WsHeader);
   auto section = [&](bool there, size_t bytes) {
     const size_t at = off;
@@ -110,12 +113,12 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
   } else {
     const bool act = l.act != SA_ACT_NONE;
     s.dz = section(act, size_t(l.M) * pitch_of(l.Z) * size_of(l.dt));
-    s.dz_terms = section(f32 || (!act && (repack & COPY_DY)), size_t(l.M) * pitch_of(l.Z) * each);
+    s.dz_terms = section((f32 && !few_f32) || (!act && (repack & COPY_DY)), size_t(l.M) * pitch_of(l.Z) * each);
     s.dx = sa::dense::tc_plan(l.M, l.K, l.Z, sa::dense::kPlain, f32);
     s.dw = sa::dense::tc_plan(l.Z, l.K, l.M, sa::dense::kPlain, f32);
     s.side = sa::dense::tc_plan_grads(l.M, l.Z, l.K, f32, s.dx.cost + s.dw.cost, &s.side_dx, &s.side_dw);
-    piece = s.dx.piece_bytes > s.dw.piece_bytes ? s.dx.piece_bytes : s.dw.piece_bytes;
-    if (s.side && s.side_dx.piece_bytes + s.side_dw.piece_bytes > piece)
+    piece = few_f32 ? 0 : s.dx.piece_bytes > s.dw.piece_bytes ? s.dx.piece_bytes : s.dw.piece_bytes;
+    if (s.side && !few_f32 && s.side_dx.piece_bytes + s.side_dw.piece_bytes > piece)
       piece = s.side_dx.piece_bytes + s.side_dw.piece_bytes;
   }
   s.piece = section(piece > 0, piece);

@@ -5,8 +5,8 @@
 //
 // Bound by memory: each element is read once and written once, the row stays in registers
 // between the mean, the variance (of the differences from that mean, so a mean far from zero
-// costs no digits) and the result.  T threads hold a row, C chunks of 8 elements each: 8 to 32
-// lanes of a warp up to 512 features, a block above.  A block walks rows with the parameters,
+// costs no digits) and the result.  T threads hold a row, C chunks of 8 elements each: 4 to 32
+// lanes of a warp up to 512 features (1024), a block above.  A block walks rows with the parameters,
 // and in the backward pass the columns' running sums, in registers (shared memory above 8192
 // features, whose sums would not fit); its sums leave as one partial row, and a second kernel
 // adds the partial rows in block order, so results do not depend on timing.
@@ -684,6 +684,7 @@ int64_t blocks_for(int64_t rows) { return (rows + rows_at_once<T>() - 1) / rows_
 
 // A walk's grid and the bytes of a block's ring: the blocks that are resident together, fewer where their rings need the
 // room (an SM has 227 KB, of which a little is left to the sums' exchange).
+constexpr size_t kRoom = 220 * 1024;
 struct Walkers {
   int blocks;
   size_t ring;
@@ -696,7 +697,7 @@ Walkers walkers(const NormArgs& a) {
     const size_t row = VEC ? size_t(C) * (pieces_of(a.x) + pieces_of(a.r) + (GRAD ? pieces_of(a.dy) : 0)) * block_threads<T>() * 16
                            : size_t(row_span(a.x, a.n) + row_span(a.r, a.n) + (GRAD ? row_span(a.dy, a.n) : 0)) * rows_at_once<T>();
     w.ring = ring_rows<T>() * row;
-    const int fit = int(size_t(220 * 1024) / (w.ring + 2048));
+    const int fit = int(kRoom / (w.ring + 2048));
     if (w.blocks > fit) w.blocks = fit;
   }
   const int64_t most = int64_t(sm_count()) * w.blocks, need = blocks_for<T>(a.rows);
@@ -707,7 +708,7 @@ Walkers walkers(const NormArgs& a) {
 template <auto Kernel>
 cudaError_t launch_walk(const Walkers& w, int threads, size_t smem, const NormArgs& a, cudaStream_t st) {
   if (smem > 40 * 1024) {  // with the sums' exchange above what a launch may take unasked
-    const cudaError_t e = allow_smem<Kernel>(smem);
+    const cudaError_t e = allow_smem<Kernel>(kRoom);
     if (e != cudaSuccess) return e;
   }
   Kernel<<<w.blocks, threads, smem, st>>>(a);

@@ -271,21 +271,24 @@ cudaError_t launch_act_grad(const ActGradArgs& a, cudaStream_t st) {
   const size_t sums = size_t(8) * (gated ? 2 : 1) * 256 * sizeof(float);
   const size_t ring = vec ? size_t(kRing) * (gated ? 3 : 2) * (a.dy.dt == SA_BF16 ? 1 : 2) * 256 * 16 : 0;
   const size_t smem = ring > sums ? ring : sums;
-  auto go = [&](auto kernel) {
+  // the same size for a kernel at all times
+  auto go = [&](auto type, auto aligned, auto halves) {
+    using T = decltype(type);
+    constexpr auto kernel = act_grad_kernel<T, aligned(), halves()>;
     if (smem > 48 * 1024) {
-      const cudaError_t s = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+      const cudaError_t s = allow_smem<kernel>(smem);
       if (s != cudaSuccess) return s;
     }
     kernel<<<grid, 256, smem, st>>>(a, lanes);
     return cudaGetLastError();
   };
-  if (a.dy.dt == SA_BF16) {
-    using T = __nv_bfloat16;
-    if (vec) return gated ? go(act_grad_kernel<T, true, true>) : go(act_grad_kernel<T, true, false>);
-    return gated ? go(act_grad_kernel<T, false, true>) : go(act_grad_kernel<T, false, false>);
-  }
-  if (vec) return gated ? go(act_grad_kernel<float, true, true>) : go(act_grad_kernel<float, true, false>);
-  return gated ? go(act_grad_kernel<float, false, true>) : go(act_grad_kernel<float, false, false>);
+  auto pick = [&](auto type) {
+    using std::true_type;
+    using std::false_type;
+    if (vec) return gated ? go(type, true_type{}, true_type{}) : go(type, true_type{}, false_type{});
+    return gated ? go(type, false_type{}, true_type{}) : go(type, false_type{}, false_type{});
+  };
+  return a.dy.dt == SA_BF16 ? pick(__nv_bfloat16{}) : pick(float{});
 }
 
 cudaError_t launch_simt_gemm(const GemmArgs& g, cudaStream_t st) {
