@@ -116,6 +116,15 @@ __device__ __forceinline__ float sigmoid(float z) {
   return isinf(d) ? r : fmaf(r, fmaf(-d, r, 1.f), r);
 }
 
+// z sigmoid<false>(z) of two neighbours; the products and sums go in pairs
+__device__ __forceinline__ void silu_pair(float* v) {
+  const float2 z = make_float2(v[0], v[1]);
+  const float2 t = __fmul2_rn(z, make_float2(-1.4426950409f, -1.4426950409f));
+  const float2 d = __fadd2_rn(make_float2(ptx::ex2(t.x), ptx::ex2(t.y)), make_float2(1.f, 1.f));
+  const float2 y = __fmul2_rn(z, make_float2(ptx::rcp_approx(d.x), ptx::rcp_approx(d.y)));
+  v[0] = y.x, v[1] = y.y;
+}
+
 // Phi(z) and e^(-z^2/2), Phi the normal distribution function.
 // FULL: from CUDA's erfc.  Else Phi(-x) = e^(-x^2/2) R(1 / (1 + 0.31 x)) for x >= 0, R of degree 6 without a constant
 // term: a least-squares fit with weights that level the relative error over 0 <= x <= 20 (Lawson's

@@ -10,7 +10,7 @@
 //
 // 8192 x 4096 -> 4096 with a residual: 159 us alone, 1.73 PFLOP/s, tensor pipe 82 % busy (six and three quarters waves of
 // pairs); 16384 x 4096 gated, dx and dW: 297 us, 1.85 PFLOP/s.  65536 x 128 -> 512 gated with z is bound by the tiles'
-// ends: 47 us, 21 without them.
+// ends: 44 us, 21 without them.
 //
 // Work: tiles go to the workers (one CTA or pair an SM or two) in turn.  Where the last turn would leave many idle, its
 // tiles are dealt out in equal shares of blocks instead; a tile cut by shares leaves fp32 pieces that a second

@@ -335,7 +335,9 @@ struct TmaOut {
 #pragma unroll
       for (int j = 0; j < count; j += 4) {
         const float4 b = *reinterpret_cast<const float4*>(from + j);
-        to[j] += b.x, to[j + 1] += b.y, to[j + 2] += b.z, to[j + 3] += b.w;
+        const float2 p = __fadd2_rn(make_float2(to[j], to[j + 1]), make_float2(b.x, b.y));
+        const float2 q = __fadd2_rn(make_float2(to[j + 2], to[j + 3]), make_float2(b.z, b.w));
+        to[j] = p.x, to[j + 1] = p.y, to[j + 2] = q.x, to[j + 3] = q.y;
       }
     };
     if (EPI != EPI_PLAIN && a.bias) {
@@ -345,27 +347,23 @@ struct TmaOut {
     }
     ptx::tmem_ld_wait();
     if (EPI != EPI_GATED) read();
+    float u[EPI == EPI_GATED ? 32 : 1];
+    if constexpr (EPI == EPI_GATED) ptx::tmem_ld32(other, u);  // the other half, on its way meanwhile
     if (EPI != EPI_PLAIN) {
       if (a.bias) add_bias(bias, v, 32);
       if (a.z) put(s + kOutBytes, v);
     }
     if constexpr (EPI == EPI_GATED) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] *= sigmoid<false>(v[j]);
-      // the other half by 16 columns, so that the chunk's registers are few
+      for (int j = 0; j < 32; j += 2) silu_pair(v + j);
+      ptx::tmem_ld_wait();
+      read();
+      if (a.bias) add_bias(bias + 32, u, 32);
+      if (a.z) put(s + 2 * kOutBytes, u);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float u[16];
-        tmem_ld16(other + 16 * k, u);
-        ptx::tmem_ld_wait();
-        if (k == 1) read();
-        if (a.bias) add_bias(bias + 32 + 16 * k, u, 16);
-        if (a.z)
-#pragma unroll
-          for (int p = 0; p < 2; ++p)
-            store8(reinterpret_cast<__nv_bfloat16*>(s + 2 * kOutBytes + at(lane, 2 * k + p)), u + 8 * p);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[16 * k + j] *= u[j];
+      for (int j = 0; j < 32; j += 2) {
+        const float2 p = __fmul2_rn(make_float2(v[j], v[j + 1]), make_float2(u[j], u[j + 1]));
+        v[j] = p.x, v[j + 1] = p.y;
       }
     }
     if constexpr (EPI == EPI_FULL) {
@@ -377,7 +375,7 @@ struct TmaOut {
         for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_GELU, v[j]);
       } else if (a.act == SA_ACT_SILU) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_SILU, v[j]);
+        for (int j = 0; j < 32; j += 2) silu_pair(v + j);
       }
     }
     if (EPI != EPI_PLAIN) {
