@@ -143,6 +143,24 @@ __device__ __forceinline__ float normal_cdf(float z, float* density) {
   return z < 0.f ? r : 1.f - r;
 }
 
+// z normal_cdf<false>(z) of two neighbours
+__device__ __forceinline__ void gelu_pair(float* v) {
+  auto two = [](float c) { return make_float2(c, c); };
+  const float2 z = make_float2(v[0], v[1]);
+  const float2 q = __fmul2_rn(__fmul2_rn(two(-0.72134752f), z), z);
+  const float2 d = __ffma2_rn(two(0.31f), make_float2(fabsf(z.x), fabsf(z.y)), two(1.f));
+  const float2 t = make_float2(ptx::rcp_approx(d.x), ptx::rcp_approx(d.y));
+  float2 r = __ffma2_rn(two(-0.07230377f), t, two(0.17592333f));
+  r = __ffma2_rn(r, t, two(0.020491485f));
+  r = __ffma2_rn(r, t, two(0.13110992f));
+  r = __ffma2_rn(r, t, two(0.120964423f));
+  r = __ffma2_rn(r, t, two(0.12381754f));
+  r = __fmul2_rn(__fmul2_rn(r, t), make_float2(ptx::ex2(q.x), ptx::ex2(q.y)));
+  const float2 u = __ffma2_rn(two(-1.f), r, two(1.f));
+  const float2 y = __fmul2_rn(z, make_float2(z.x < 0.f ? r.x : u.x, z.y < 0.f ? r.y : u.y));
+  v[0] = y.x, v[1] = y.y;
+}
+
 // act(z) of one value (SA_ACT_SWIGLU: of the gate's half)
 template <bool FULL>
 __device__ __forceinline__ float activate(int act, float z) {

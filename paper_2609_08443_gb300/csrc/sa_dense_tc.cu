@@ -33,7 +33,6 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kEpiWarp0 = 4;
 constexpr int kBlockBytes = 16384;  // 128 rows x 64 bf16
 constexpr uint32_t kWaitNs = 2000000000u;
 
@@ -41,20 +40,28 @@ template <int CTAS, bool F32, int EPI>
 struct TcCfg {
   using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
   using End = ChunkEnd<T, EPI>;
+  // three groups of epilogue warps take the chunks in turn (else two, each with its half of a tile's columns)
+  static constexpr bool POOL = CTAS == 1 && !F32;
+  static constexpr int GROUPS = POOL ? 3 : TileShape<CTAS>::GROUPS;
+  static constexpr int SETS = POOL ? 3 : 2;      // of accumulators
+  static constexpr int EPI0 = POOL ? 0 : 4;      // the first epilogue warp
+  static constexpr int LOAD = POOL ? 12 : 0;     // the warp that loads, before the one that issues the products
+  static constexpr int ALLOC = POOL ? 12 : 2;
   static constexpr int PLANES = F32 ? 3 : 1;
   static constexpr int STAGE = 2 * PLANES * kBlockBytes;
-  static constexpr int OUT = F32 ? kStageBytes : TmaOut<EPI>::BUFFERS * kOutBytes;  // of an epilogue warp
-  static constexpr int STAGES = F32 ? 2 : EPI == EPI_GATED ? 4 : 5;
+  static constexpr int OUT_SETS = POOL && EPI != EPI_PLAIN ? 1 : 2;
+  static constexpr int OUT = F32 ? kStageBytes : TmaOut<EPI, OUT_SETS>::BUFFERS * kOutBytes;  // of an epilogue warp
+  static constexpr int STAGES = F32 ? 2 : EPI == EPI_GATED || (POOL && EPI == EPI_FULL) ? 4 : 5;
   static constexpr int BN = TileShape<CTAS>::BN;
-  static constexpr int WARPS = 4 * TileShape<CTAS>::GROUPS;  // that end tiles
-  static constexpr int THREADS = 128 + 32 * WARPS;
-  static constexpr int TMEM = 2 * BN;
+  static constexpr int WARPS = 4 * GROUPS;  // that end tiles
+  static constexpr int THREADS = 32 * WARPS + 128;
+  static constexpr int TMEM = POOL ? 512 : 2 * BN;  // a power of two
   static constexpr int OFF_OUT = STAGES * STAGE;
   static constexpr int OFF_BAR = OFF_OUT + WARPS * OUT;
   static constexpr int SMEM = OFF_BAR + 256;
 };
 static_assert(TcCfg<2, false, EPI_GATED>::SMEM <= 232448 && TcCfg<2, false, EPI_FULL>::SMEM <= 232448 &&
-                  TcCfg<1, true, EPI_GATED>::SMEM <= 232448,
+                  TcCfg<1, true, EPI_GATED>::SMEM <= 232448 && TcCfg<1, false, EPI_GATED>::SMEM <= 232448,
               "shared memory of a CTA");
 
 // ------------------------------------------------------ cta_group::2 forms
@@ -127,7 +134,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
   auto full = [&](int s) { return base + C::OFF_BAR + 8 * s; };
   auto empty = [&](int s) { return base + C::OFF_BAR + 64 + 8 * s; };
   auto acc_full = [&](int s) { return base + C::OFF_BAR + 128 + 8 * s; };
-  auto acc_empty = [&](int s) { return base + C::OFF_BAR + 144 + 8 * s; };
+  auto acc_empty = [&](int s) { return base + C::OFF_BAR + 192 + 8 * s; };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_BAR + 160);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 176);  // three words
 
@@ -140,7 +147,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < C::SETS; ++s) {
       mbar_init(acc_full(s), 1);
       mbar_init(acc_empty(s), C::WARPS * CTAS);
     }
@@ -150,7 +157,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     tma_prefetch_desc(&ta);
     tma_prefetch_desc(&tb);
   }
-  if (warp == 2) tc_alloc<CTAS>(smem_u32(tmem_slot), C::TMEM);
+  if (warp == C::ALLOC) tc_alloc<CTAS>(smem_u32(tmem_slot), C::TMEM);
   tc_fence_before();
   if (CTAS == 2)
     cluster_sync_all();
@@ -158,101 +165,16 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  if (warp == 0 && lane == 0) {
-    // ------------------------------------------------------------- loads
-    const uint32_t lead = CTAS == 2 ? mapa_shared(base, 0) : base;
-    Segments seg(a, worker);
-    uint32_t n = 0;  // blocks loaded
-    bool ok = true;
-    while (ok && seg.next()) {
-      int mb, nb;
-      tile_place(a, seg.tile, &mb, &nb);
-      const int m0 = (mb * CTAS + int(rank)) * 128;
-      // this CTA's 128 rows of B: SwiGLU's halves are the pair's CTAs, or 64 rows each
-      int b0, b1;
-      if (EPI == EPI_GATED) {
-        b0 = CTAS == 2 ? int(rank * a.half) + nb * YN : nb * YN;
-        b1 = CTAS == 2 ? b0 + 64 : int(a.half) + nb * YN;
-      } else {
-        b0 = nb * YN + (CTAS == 2 ? int(rank) * 128 : 0);
-        b1 = b0 + 64;
-      }
-      for (int kb = seg.k0; kb < seg.k1; ++kb, ++n) {
-        const uint32_t s = n % C::STAGES, ph = (n / C::STAGES) & 1u;
-        ok = mbar_wait(empty(s), ph ^ 1u, abort_flag, a.ws, 0x401);
-        if (!ok) break;
-        if (rank == 0) mbar_arrive_expect_tx(full(s), CTAS * C::STAGE);
-        const uint32_t bar = lead + C::OFF_BAR + 8 * s, dst = base + s * C::STAGE;
-        const int k = kb * 64;
-#pragma unroll
-        for (int p = 0; p < C::PLANES; ++p) {
-          const uint32_t da = dst + p * kBlockBytes, db = dst + (C::PLANES + p) * kBlockBytes;
-          if (A_MN) {
-            tc_load<CTAS>(da, &ta, bar, m0, k, p);
-            tc_load<CTAS>(da + 8192, &ta, bar, m0 + 64, k, p);
-          } else {
-            tc_load<CTAS>(da, &ta, bar, k, m0, p);
-          }
-          if (B_MN) {
-            tc_load<CTAS>(db, &tb, bar, b0, k, p);
-            tc_load<CTAS>(db + 8192, &tb, bar, b1, k, p);
-          } else {
-            tc_load<CTAS>(db, &tb, bar, k, b0, p);
-            tc_load<CTAS>(db + 8192, &tb, bar, k, b1, p);
-          }
-        }
-      }
-    }
-    if (!ok && rank == 0)  // copies in flight land before the CTA ends
-      for (uint32_t i = n > C::STAGES ? n - C::STAGES : 0; i < n; ++i)
-        tcc::mbar_wait_bounded(full(i % C::STAGES), (i / C::STAGES) & 1u, kWaitNs);
-  } else if (warp == 1 && lane == 0 && rank == 0) {
-    // ---------------------------------------------------------- products
-    constexpr uint32_t idesc = idesc_bf16(128 * CTAS, C::BN, A_MN, B_MN);
-    constexpr uint32_t step_a = A_MN ? 2048 : 32, step_b = B_MN ? 2048 : 32;
-    const uint64_t d_a = sdesc(base, A_MN ? 8192 : 16, 1024);
-    const uint64_t d_b = sdesc(base + C::PLANES * kBlockBytes, B_MN ? 8192 : 16, 1024);
-    Segments seg(a, worker);
-    uint32_t n = 0, g = 0;  // blocks, sets of accumulators used
-    bool ok = true;
-    while (ok && seg.next()) {
-      for (int kb = seg.k0; ok && kb < seg.k1;) {
-        const int end = F32 ? kb + 1 : seg.k1;
-        const uint32_t set = g & 1u, d = tmem + set * C::BN;
-        ok = mbar_wait(acc_empty(set), ((g >> 1) & 1u) ^ 1u, abort_flag, a.ws, 0x402);
-        if (!ok) break;
-        tc_fence_after();
-        uint32_t accumulate = 0;
-        for (; kb < end; ++kb, ++n) {
-          const uint32_t s = n % C::STAGES;
-          ok = mbar_wait(full(s), (n / C::STAGES) & 1u, abort_flag, a.ws, 0x403);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t sa = sdesc_add(d_a, s * C::STAGE), sb = sdesc_add(d_b, s * C::STAGE);
-          constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
-#pragma unroll
-          for (int i = F32 ? 0 : 5; i < 6; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              tc_mma<CTAS>(d, sdesc_add(sa, pa[i] * kBlockBytes + k * step_a),
-                           sdesc_add(sb, pb[i] * kBlockBytes + k * step_b), idesc, accumulate);
-              accumulate = 1;
-            }
-          tc_commit<CTAS>(empty(s));
-        }
-        if (!ok) break;
-        tc_commit<CTAS>(acc_full(set));
-        ++g;
-      }
-    }
-  } else if (warp >= kEpiWarp0) {
+  if (warp >= C::EPI0 && warp < C::EPI0 + C::WARPS) {
+    // of the launch's 512 x 128 registers: 384 x 152 here, 128 x 56 there
+    if constexpr (C::POOL) setmaxnreg_inc<152>();
     // -------------------------------------------------------- tiles' ends
-    const int e = warp - kEpiWarp0, q = e & 3, h = e >> 2;
+    const int e = warp - C::EPI0, q = e & 3, h = e >> 2;
     char* out = smem + C::OFF_OUT + e * C::OUT;
     const uint32_t lanes = uint32_t(q * 32) << 16;
     const uint32_t lead_empty = CTAS == 2 ? mapa_shared(acc_empty(0), 0) : acc_empty(0);
-    constexpr int CH = Shape::template CHUNKS<EPI>;
-    TmaOut<EPI> outs(out, lane);
+    constexpr int CH = C::POOL ? YN / 32 : Shape::template CHUNKS<EPI>;
+    TmaOut<EPI, C::OUT_SETS> outs(out, lane);
     Segments seg(a, worker);
     uint32_t g = 0;  // sets of accumulators used
     bool ok = true;
@@ -268,6 +190,9 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       }
     };
     while (ok && seg.next()) {
+      // this warp's chunks: of a pool every third of all tiles' chunks, else half of each tile's
+      constexpr int STEP = C::POOL ? 3 : 1;
+      const int first = C::POOL ? (h + int(g % 3) * (3 - CH % 3)) % 3 : h * CH, stop = C::POOL ? CH : first + CH;
       int mb, nb;
       tile_place(a, seg.tile, &mb, &nb);
       const int64_t m0 = int64_t(mb * CTAS + int(rank)) * 128 + q * 32;
@@ -279,7 +204,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         piece = a.piece + (int64_t(worker * 2 + slot) * CTAS + rank) * (128 * C::BN) + (q * 32 + lane) * 4;
       }
       auto col = [&](int i, int half) {  // accumulator column of chunk i (SwiGLU: of either half)
-        return half * YN + h * (YN / Shape::GROUPS) + i * 32;
+        return half * YN + i * 32;
       };
       auto put_piece = [&](int c, const float* v) {
         if (m0 + lane < a.M)
@@ -289,7 +214,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
                 make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
       };
       End end;
-      const int y0 = nb * YN + h * (YN / Shape::GROUPS);  // this warp's first column of y
+      const int y0 = nb * YN;
       if constexpr (F32) {
         constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
         float sum[CH][HALVES][32];
@@ -309,7 +234,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
 #pragma unroll
             for (int k = 0; k < HALVES; ++k) {
               float v[32];
-              tmem_ld32(tmem + lanes + set * C::BN + col(i, k), v);
+              tmem_ld32(tmem + lanes + set * C::BN + col(first + i, k), v);
               tmem_ld_wait();
 #pragma unroll
               for (int j = 0; j < 32; ++j) sum[i][k][j] += v[j];
@@ -322,7 +247,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           // all chunks pass through one copy of their end, so the registers they are in are chosen by selects
 #pragma unroll 1
           for (int i = 0; i < CH * 32 / End::COLS; ++i) {
-            const int n0 = y0 + i * End::COLS;
+            const int n0 = y0 + first * 32 + i * End::COLS;
             if (n0 >= a.N || m0 >= a.M) break;
             end.load_bias(a, lane, n0);
 #pragma unroll
@@ -340,25 +265,26 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
 #pragma unroll
           for (int i = 0; i < CH; ++i)
 #pragma unroll
-            for (int k = 0; k < HALVES; ++k) put_piece(col(i, k), sum[i][k]);
+            for (int k = 0; k < HALVES; ++k) put_piece(col(first + i, k), sum[i][k]);
         }
       } else {
         const bool tma = (a.vec & 1) != 0;
-        if (complete && tma) outs.load_bias(a, y0);
-        const uint32_t set = g & 1u, acc = tmem + lanes + set * C::BN;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), (g >> 1) & 1u, abort_flag, a.ws, 0x404));
+        if (complete && tma && first < stop) outs.load_bias(a, y0 + first * 32);
+        const uint32_t set = g % C::SETS, acc = tmem + lanes + set * C::BN;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), g / C::SETS & 1u, abort_flag, a.ws, 0x404));
         if (!ok) break;
         tc_fence_after();
+        if (C::POOL && first >= stop) release(set);
 #pragma unroll 1
-        for (int i = 0; i < CH; ++i) {
+        for (int i = first; i < stop; i += STEP) {
           auto read = [&] {
-            if (i == CH - 1) release(set);
+            if (i + STEP >= stop) release(set);
           };
           if (y0 + i * 32 >= a.N || m0 >= a.M) {  // nothing of it is in y
             read();
           } else if (complete && tma) {
             outs.finish(a, ty, tz, acc + col(i, 0), acc + col(i, 1), m0, y0 + i * 32, read);
-            if (i + 1 < CH) outs.load_bias(a, y0 + i * 32 + 32);
+            if (i + STEP < stop) outs.load_bias(a, y0 + (i + STEP) * 32);
           } else if (complete) {
 #pragma unroll 1
             for (int k = 0; k < 2; ++k) {  // by 16 columns
@@ -394,13 +320,103 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       }
     }
     if (!F32) outs.done();
+  } else {
+    if constexpr (C::POOL) setmaxnreg_dec<56>();
+    if (warp == C::LOAD && lane == 0) {
+      // ------------------------------------------------------------- loads
+      const uint32_t lead = CTAS == 2 ? mapa_shared(base, 0) : base;
+      Segments seg(a, worker);
+      uint32_t n = 0;  // blocks loaded
+      bool ok = true;
+      while (ok && seg.next()) {
+        int mb, nb;
+        tile_place(a, seg.tile, &mb, &nb);
+        const int m0 = (mb * CTAS + int(rank)) * 128;
+        // this CTA's 128 rows of B: SwiGLU's halves are the pair's CTAs, or 64 rows each
+        int b0, b1;
+        if (EPI == EPI_GATED) {
+          b0 = CTAS == 2 ? int(rank * a.half) + nb * YN : nb * YN;
+          b1 = CTAS == 2 ? b0 + 64 : int(a.half) + nb * YN;
+        } else {
+          b0 = nb * YN + (CTAS == 2 ? int(rank) * 128 : 0);
+          b1 = b0 + 64;
+        }
+        for (int kb = seg.k0; kb < seg.k1; ++kb, ++n) {
+          const uint32_t s = n % C::STAGES, ph = (n / C::STAGES) & 1u;
+          ok = mbar_wait(empty(s), ph ^ 1u, abort_flag, a.ws, 0x401);
+          if (!ok) break;
+          if (rank == 0) mbar_arrive_expect_tx(full(s), CTAS * C::STAGE);
+          const uint32_t bar = lead + C::OFF_BAR + 8 * s, dst = base + s * C::STAGE;
+          const int k = kb * 64;
+  #pragma unroll
+          for (int p = 0; p < C::PLANES; ++p) {
+            const uint32_t da = dst + p * kBlockBytes, db = dst + (C::PLANES + p) * kBlockBytes;
+            if (A_MN) {
+              tc_load<CTAS>(da, &ta, bar, m0, k, p);
+              tc_load<CTAS>(da + 8192, &ta, bar, m0 + 64, k, p);
+            } else {
+              tc_load<CTAS>(da, &ta, bar, k, m0, p);
+            }
+            if (B_MN) {
+              tc_load<CTAS>(db, &tb, bar, b0, k, p);
+              tc_load<CTAS>(db + 8192, &tb, bar, b1, k, p);
+            } else {
+              tc_load<CTAS>(db, &tb, bar, k, b0, p);
+              tc_load<CTAS>(db + 8192, &tb, bar, k, b1, p);
+            }
+          }
+        }
+      }
+      if (!ok && rank == 0)  // copies in flight land before the CTA ends
+        for (uint32_t i = n > C::STAGES ? n - C::STAGES : 0; i < n; ++i)
+          tcc::mbar_wait_bounded(full(i % C::STAGES), (i / C::STAGES) & 1u, kWaitNs);
+    } else if (warp == C::LOAD + 1 && lane == 0 && rank == 0) {
+      // ---------------------------------------------------------- products
+      constexpr uint32_t idesc = idesc_bf16(128 * CTAS, C::BN, A_MN, B_MN);
+      constexpr uint32_t step_a = A_MN ? 2048 : 32, step_b = B_MN ? 2048 : 32;
+      const uint64_t d_a = sdesc(base, A_MN ? 8192 : 16, 1024);
+      const uint64_t d_b = sdesc(base + C::PLANES * kBlockBytes, B_MN ? 8192 : 16, 1024);
+      Segments seg(a, worker);
+      uint32_t n = 0, g = 0;  // blocks, sets of accumulators used
+      bool ok = true;
+      while (ok && seg.next()) {
+        for (int kb = seg.k0; ok && kb < seg.k1;) {
+          const int end = F32 ? kb + 1 : seg.k1;
+          const uint32_t set = g % C::SETS, d = tmem + set * C::BN;
+          ok = mbar_wait(acc_empty(set), (g / C::SETS & 1u) ^ 1u, abort_flag, a.ws, 0x402);
+          if (!ok) break;
+          tc_fence_after();
+          uint32_t accumulate = 0;
+          for (; kb < end; ++kb, ++n) {
+            const uint32_t s = n % C::STAGES;
+            ok = mbar_wait(full(s), (n / C::STAGES) & 1u, abort_flag, a.ws, 0x403);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t sa = sdesc_add(d_a, s * C::STAGE), sb = sdesc_add(d_b, s * C::STAGE);
+            constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
+  #pragma unroll
+            for (int i = F32 ? 0 : 5; i < 6; ++i)
+  #pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                tc_mma<CTAS>(d, sdesc_add(sa, pa[i] * kBlockBytes + k * step_a),
+                             sdesc_add(sb, pb[i] * kBlockBytes + k * step_b), idesc, accumulate);
+                accumulate = 1;
+              }
+            tc_commit<CTAS>(empty(s));
+          }
+          if (!ok) break;
+          tc_commit<CTAS>(acc_full(set));
+          ++g;
+        }
+      }
+    }
   }
   __syncwarp();
   if (CTAS == 2)
     cluster_sync_all();  // nothing of the pair's is still read or written
   else
     __syncthreads();
-  if (warp == 2) {
+  if (warp == C::ALLOC) {
     tc_fence_after();
     tc_dealloc<CTAS>(tmem, C::TMEM);
   }

@@ -281,10 +281,10 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
 // a chunk's 32 x 32 results (z, SwiGLU's other half of z, y) leave together from the warp's buffers (64-byte rows, TMA's
 // 64-byte swizzle).  That takes a third of the shared-memory traffic of the way above.
 constexpr int kOutBytes = 2048;
-template <int EPI>
+template <int EPI, int SETS>
 struct TmaOut {
   static constexpr int SET = EPI == EPI_GATED ? 3 : EPI == EPI_FULL ? 2 : 1;  // results of a chunk
-  static constexpr int BUFFERS = 2 * SET;  // two sets in turn (unaligned rows' stage is as long as two buffers)
+  static constexpr int BUFFERS = SETS * SET;  // sets in turn (unaligned rows' stage is as long as two buffers)
   char* ring;
   int lane, turn;
   float b0, b1;
@@ -310,9 +310,9 @@ struct TmaOut {
                                          uint32_t other, int64_t m0, int n0, F read) {
     float v[32];
     ptx::tmem_ld32(acc, v);
-    // the set of the chunk before last, once its stores have read it
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-    char* s = ring + (turn ^= 1) * SET * kOutBytes;  // y, then z's halves
+    // this set, once the stores of its last chunk have read it
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(SETS - 1) : "memory");
+    char* s = ring + (SETS == 2 ? turn ^= 1 : 0) * SET * kOutBytes;  // y, then z's halves
     uint4 res[EPI == EPI_FULL ? 4 : 1];
     const bool direct = EPI != EPI_PLAIN && a.r && (a.vec & 2);
     auto load_residual = [&](uint4* q) {  // whole rows a few lanes
@@ -372,7 +372,7 @@ struct TmaOut {
         for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_RELU, v[j]);
       } else if (a.act == SA_ACT_GELU) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = activate<false>(SA_ACT_GELU, v[j]);
+        for (int j = 0; j < 32; j += 2) gelu_pair(v + j);
       } else if (a.act == SA_ACT_SILU) {
 #pragma unroll
         for (int j = 0; j < 32; j += 2) silu_pair(v + j);
