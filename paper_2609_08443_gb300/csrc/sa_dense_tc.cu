@@ -769,6 +769,8 @@ TcArgs tc_args(const TcGemm& g, const TcPlan& p) {
   a.KB = int(p.KB);
   a.mt = int(p.mt);
   a.nt = int(p.nt);
+  a.by_group = Divisor(uint32_t(8 * p.nt));
+  a.by_last = Divisor(uint32_t(p.mt % 8 ? p.mt % 8 : 8));
   a.W = p.W;
   a.whole = p.whole;
   a.cut = p.cut;
