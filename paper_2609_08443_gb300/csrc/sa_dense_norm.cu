@@ -498,10 +498,16 @@ __global__ void __launch_bounds__(block_threads<T>(), blocks_at_once<T, C, VEC, 
       const int k = column<T, VEC>(t, i / 8, i % 8);
       if (k < n) sums[k] = sums[n + k] = 0.f;
     }
+  // a row's mean and 1 / sqrt(var), asked for a row ahead
+  auto stats_of = [&](uint32_t row) {
+    return row < at.rows ? __ldg(reinterpret_cast<const float2*>(a.stats) + row) : make_float2(0.f, 0.f);
+  };
+  float2 next = stats_of(at.row);
   for (; at.more(); at.row += at.step) {
     const bool here = at.here();
     float h[8 * C], g[8 * C], s[2] = {0.f, 0.f};
-    const float2 st = here ? *reinterpret_cast<const float2*>(a.stats + 2 * int64_t(at.row)) : make_float2(0.f, 0.f);
+    const float2 st = next;
+    next = stats_of(at.row + at.step);
     at.take(a, h, g);
     if (!keep_parameters<T, C>()) load_factors<T, C, VEC>(a, t, n, w);
     float2 g2 = both(0.f), x2 = both(0.f);
