@@ -684,7 +684,8 @@ cudaError_t launch_kind(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaS
 // tile: 512 cycles of products.  Measured beside that: a single CTA's block, a quarter of the products for the same
 // 32 KB a CTA, 1.4 units; of fp32 terms 4.5 (24 products read 8 KB each and 96 KB are written beside them: 2304 cycles of
 // shared memory; pairs of 256 x 128 and half-deep stages measured the same or worse).  A tile takes
-// no less than its end, which the next tile's products only hide; the last end is not hidden.  Cut tiles cost a second
+// no less than its end, which the next tile's products only hide (of a single CTA's tile 1.2 to 2.8 us, by the activation);
+// the last end is not hidden.  Cut tiles cost a second
 // kernel, 25 units, and their pieces' way to L2 and back (2048 x 1024 -> 1024: 9 us whole, 19 cut; 128 x 4096 -> 8192: 23
 // and 20; dx of 16384 x 8192 -> 1024: 168 and 158).  And memory moves 6.6 TB/s, 1.8 MB a unit.  `ctas_only` 0: either kind.
 TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms, int ctas_only) {
@@ -694,7 +695,9 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms, int 
   const bool gated = act == SA_ACT_SWIGLU, plain = act == kPlain;
   // the end of a tile: rows that 16-byte pieces do not fit go element by element; fp32 has CUDA's erfc in gelu
   const double slow = N % (f32 ? 4 : 8) == 0 ? 1.0 : f32 ? 1.5 : 3.0;
-  const double end1 = slow * (!f32 ? (plain ? 6.0 : 8.0) : act == SA_ACT_GELU ? 36.0 : gated ? 20.0 : plain ? 8.0 : 12.0);
+  const double full = act == SA_ACT_GELU ? 10.4 : act == SA_ACT_SILU ? 8.0 : act == SA_ACT_RELU ? 6.5 : 5.4;
+  const double end1 = slow * (!f32 ? (plain ? 6.0 : gated ? 5.5 : full)
+                                   : act == SA_ACT_GELU ? 36.0 : gated ? 20.0 : plain ? 8.0 : 12.0);
   best.KB = KB;
   best.bytes = double(f32 ? 4 : 2) * (double(M) * K + double(N) * K * (gated ? 2 : 1) + double(M) * N * (gated ? 2 : 1));
   for (int ctas = 1; ctas <= (f32 || sms < 2 ? 1 : 2); ++ctas) {
@@ -704,7 +707,8 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms, int 
     const int workers = sms / ctas;
     const int64_t waves = tiles / workers, rest = tiles % workers;
     const double block = f32 ? 4.5 : ctas == 2 ? 1.0 : 1.4;
-    const double end = end1 * (ctas == 2 ? 1.8 : 1.0);
+    // a pair's CTAs have twice the columns and eight warps for twelve
+    const double end = end1 * (ctas == 1 ? 1.0 : plain ? 1.8 : gated ? 1.9 : 2.2);
     const double tile = KB * block > end ? KB * block : end;
     for (int cut = 0; cut <= (rest && KB > 1 ? 1 : 0); ++cut) {
       int cutters = 0;
