@@ -12,7 +12,8 @@
 // adds the partial rows in block order, so results do not depend on timing.
 //
 // A row's loads, sums and stores wait for one another, so the next two rows are on their way meanwhile, by cp.async
-// into a ring in shared memory (8192 x 4096 in bf16, gradient: 134 us without, 46 with): each thread's own 16-byte pieces (nobody else reads them, so nothing but the
+// into a ring in shared memory (8192 x 4096 in bf16, gradient: 134 us without, 46 with; 43 with the row's statistics
+// asked for a row ahead too): each thread's own 16-byte pieces (nobody else reads them, so nothing but the
 // thread's own copies is waited for), or, where rows are not 16-byte aligned, the 16-byte pieces that the row touches,
 // from which the row's threads pick their elements.  524288 x 128, fp32 plus a bf16 residual: 81 us, 6.6 TB/s.
 #include "sa_dense_act.cuh"
@@ -644,7 +645,7 @@ bool vec_ok(const NormArgs& a) {
 }
 
 // Calls f with the layout for n features: (threads a row, chunks of 8 a thread).  More chunks spread what a thread spends
-// on a row's sums over more elements: two (8192 x 4096 in bf16, forward and gradient 30 and 46 us; one chunk 37 and 58),
+// on a row's sums over more elements: two (8192 x 4096 in bf16, forward and gradient 30 and 43 us; one chunk 37 and 58),
 // four in the forward of wide rows that are read in bf16 alone (26 us; but 62 with fp32 rows and a residual, for 43
 // with two).  Unaligned rows: two (10007 x 1001 in bf16 18 us, one 20, four 22), above 4096 features four (8000 x 8191:
 // 88 us, two 98).

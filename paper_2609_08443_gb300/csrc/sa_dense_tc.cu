@@ -3,14 +3,17 @@
 // nothing is transposed in memory).
 //
 // A tile is 256 x 256 for a pair of CTAs (cta_group::2: each holds 128 rows of A, half of B's rows and
-// 128 rows of the result) or 128 x 128 for one CTA.  Warp 0 loads (TMA, 64 deep blocks, up to five stages),
-// warp 1 issues the products, warps 4-11 end the tiles: two sets of accumulators in TMEM let one
-// tile's end overlap the next one's products.  SwiGLU's tile takes the same columns of both halves of
-// W, so gate and value meet in one warp.
+// 128 rows of the result) or 128 x 128 for one CTA.  One warp loads (TMA, 64 deep blocks, up to five stages), one issues the
+// products, and the others end tiles, 32 x 32 results at a time, while the next tile's products go to another set of
+// accumulators in TMEM.  A pair's CTA has eight of them, each with its part of every tile, and two sets.  A single CTA,
+// whose tiles have few products an element, has twelve with 152 registers, in three groups that take the chunks of all tiles
+// in turn, and three sets (65536 x 128 -> 512, eight warps and twelve: gated 44 and 40 us, silu 42 and 36, none 31 and 26;
+// without more registers for them 45, from spills).  SwiGLU's tile takes the same columns of both halves of W, so gate
+// and value meet in one warp.
 //
 // 8192 x 4096 -> 4096 with a residual: 159 us alone, 1.73 PFLOP/s, tensor pipe 82 % busy (six and three quarters waves of
-// pairs); 16384 x 4096 gated, dx and dW: 297 us, 1.85 PFLOP/s.  65536 x 128 -> 512 gated with z is bound by the tiles'
-// ends: 44 us, 21 without them.
+// pairs); 16384 x 4096 gated, dx and dW: 297 us, 1.85 PFLOP/s.  65536 x 128 -> 512 gated with z: 38 us (5.7 TB/s), of which
+// loads and products alone would take 28 and barriers alone 20.
 //
 // Work: tiles go to the workers (one CTA or pair an SM or two) in turn.  Where the last turn would leave many idle, its
 // tiles are dealt out in equal shares of blocks instead; a tile cut by shares leaves fp32 pieces that a second
@@ -51,7 +54,7 @@ struct TcCfg {
   static constexpr int STAGE = 2 * PLANES * kBlockBytes;
   static constexpr int OUT_SETS = POOL && EPI != EPI_PLAIN ? 1 : 2;
   static constexpr int OUT = F32 ? kStageBytes : TmaOut<EPI, OUT_SETS>::BUFFERS * kOutBytes;  // of an epilogue warp
-  static constexpr int STAGES = F32 ? 2 : EPI == EPI_GATED || (POOL && EPI == EPI_FULL) ? 4 : 5;
+  static constexpr int STAGES = F32 ? 2 : EPI == EPI_GATED || (POOL && EPI == EPI_FULL) ? 4 : 5;  // (five measured the same there)
   static constexpr int BN = TileShape<CTAS>::BN;
   static constexpr int WARPS = 4 * GROUPS;  // that end tiles
   static constexpr int THREADS = 32 * WARPS + 128;
@@ -61,7 +64,8 @@ struct TcCfg {
   static constexpr int SMEM = OFF_BAR + 256;
 };
 static_assert(TcCfg<2, false, EPI_GATED>::SMEM <= 232448 && TcCfg<2, false, EPI_FULL>::SMEM <= 232448 &&
-                  TcCfg<1, true, EPI_GATED>::SMEM <= 232448 && TcCfg<1, false, EPI_GATED>::SMEM <= 232448,
+                  TcCfg<1, true, EPI_GATED>::SMEM <= 232448 && TcCfg<1, false, EPI_GATED>::SMEM <= 232448 &&
+                  TcCfg<1, false, EPI_FULL>::SMEM <= 232448 && TcCfg<1, false, EPI_PLAIN>::SMEM <= 232448,
               "shared memory of a CTA");
 
 // ------------------------------------------------------ cta_group::2 forms

@@ -243,6 +243,13 @@ def test_linear_larger(cuda_lib, shape, dt):
         assert off <= most * (1.5 if k in ("dx", "dw") else 1), (k, off)
 
 
+@pytest.mark.parametrize("act", do.ACTIVATIONS)
+@pytest.mark.parametrize("shape", [(5000, 72, 520), (5000, 130, 519), (20000, 16, 40), (2500, 200, 1100)])
+def test_linear_many_tiles(cuda_lib, shape, act):
+    """Several tiles, and chunks of them, for each of the warps that end them."""
+    linear_check(cuda_lib, *shape, act, "bf16", bias=True, res=True)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_linear_large_values(cuda_lib, dt):
     """Activations far out on both sides."""
