@@ -15,7 +15,8 @@
  *   - Outputs may not overlap inputs or one another, except where a call says so.
  *   - An output pointer that may be NULL is not computed then.
  *   - All arithmetic is in fp32 or better; each output is rounded to its type once.
- *   - `workspace` is 256-byte aligned and need not be cleared.
+ *   - `workspace` is 256-byte aligned and need not be cleared.  A linear call's first 256 bytes hold its status
+ *     (sa_get_device_error): SA_ERR_TIMEOUT where a wait reached sa_set_wait_limit_ns's limit, and the outputs are undefined.
  */
 #ifndef SA_DENSE_H
 #define SA_DENSE_H

@@ -37,7 +37,8 @@ namespace {
 using namespace ptx;
 
 constexpr int kBlockBytes = 16384;  // 128 rows x 64 bf16
-constexpr uint32_t kWaitNs = 2000000000u;
+// What a worker that gave up allows its own copies and products in flight, each.
+constexpr uint64_t kDrainNs = 200000000ull;
 
 template <int CTAS, bool F32, int EPI>
 struct TcCfg {
@@ -107,6 +108,14 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
         "h"(uint16_t(3))
         : "memory");
 }
+// a word of the first CTA's or the other CTA's shared memory (a shared::cluster address)
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr_cl, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr_cl), "r"(v) : "memory");
+}
+// takes `bytes` off what a barrier of this CTA still expects
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 // `bar` is the first CTA's barrier (a shared::cluster address)
 template <int CTAS>
 __device__ __forceinline__ void tc_load(uint32_t dst, const void* map, uint32_t bar, int c0, int c1, int c2) {
@@ -139,8 +148,11 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
   auto empty = [&](int s) { return base + C::OFF_BAR + 64 + 8 * s; };
   auto acc_full = [&](int s) { return base + C::OFF_BAR + 128 + 8 * s; };
   auto acc_empty = [&](int s) { return base + C::OFF_BAR + 192 + 8 * s; };
+  const uint32_t drain = base + C::OFF_BAR + 216, never = base + C::OFF_BAR + 224;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_BAR + 160);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 176);  // three words
+  // in the first CTA: blocks that each CTA of the worker has asked for, once its loads are done
+  volatile uint32_t* loads = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_BAR + 232);
 
   if (threadIdx.x == 0) {
     if (clear) {
@@ -155,8 +167,10 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       mbar_init(acc_full(s), 1);
       mbar_init(acc_empty(s), C::WARPS * CTAS);
     }
+    mbar_init(drain, 1);
+    mbar_init(never, 1);
     abort_flag[0] = 0;
-    reinterpret_cast<volatile uint32_t*>(abort_flag)[2] = kWaitNs;
+    reinterpret_cast<volatile uint32_t*>(abort_flag)[2] = a.wait_ns;
     fence_mbar_init();
     tma_prefetch_desc(&ta);
     tma_prefetch_desc(&tb);
@@ -169,6 +183,10 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // a role that gave up: the pair's other CTA stops too
+  auto gave_up = [&] {
+    if (CTAS == 2) st_cluster_u32(mapa_shared(smem_u32(const_cast<int*>(abort_flag)), rank ^ 1u), 1u);
+  };
   if (warp >= C::EPI0 && warp < C::EPI0 + C::WARPS) {
     // of the launch's 512 x 128 registers: 384 x 152 here, 128 x 56 there
     if constexpr (C::POOL) setmaxnreg_inc<152>();
@@ -324,6 +342,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       }
     }
     if (!F32) outs.done();
+    if (!ok && lane == 0) gave_up();
   } else {
     if constexpr (C::POOL) setmaxnreg_dec<56>();
     if (warp == C::LOAD && lane == 0) {
@@ -371,9 +390,11 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           }
         }
       }
-      if (!ok && rank == 0)  // copies in flight land before the CTA ends
-        for (uint32_t i = n > C::STAGES ? n - C::STAGES : 0; i < n; ++i)
-          tcc::mbar_wait_bounded(full(i % C::STAGES), (i / C::STAGES) & 1u, kWaitNs);
+      if (CTAS == 2)
+        st_cluster_u32(lead + C::OFF_BAR + 232 + 4 * rank, n);
+      else
+        loads[0] = n;
+      if (!ok) gave_up();
     } else if (warp == C::LOAD + 1 && lane == 0 && rank == 0) {
       // ---------------------------------------------------------- products
       constexpr uint32_t idesc = idesc_bf16(128 * CTAS, C::BN, A_MN, B_MN);
@@ -382,7 +403,8 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       const uint64_t d_b = sdesc(base + C::PLANES * kBlockBytes, B_MN ? 8192 : 16, 1024);
       Segments seg(a, worker);
       uint32_t n = 0, g = 0;  // blocks, sets of accumulators used
-      bool ok = true;
+      // under a test limit (sa_set_wait_limit_ns) the first wait is for a barrier that nothing completes
+      bool ok = a.wait_ns >= kPollLimitNs || mbar_wait(never, 0, abort_flag, a.ws, 0x400);
       while (ok && seg.next()) {
         for (int kb = seg.k0; ok && kb < seg.k1;) {
           const int end = F32 ? kb + 1 : seg.k1;
@@ -413,13 +435,37 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           ++g;
         }
       }
+      if (!ok) gave_up();
     }
   }
   __syncwarp();
-  if (CTAS == 2)
-    cluster_sync_all();  // nothing of the pair's is still read or written
-  else
-    __syncthreads();
+  auto meet = [&] {
+    if (CTAS == 2)
+      cluster_sync_all();
+    else
+      __syncthreads();
+  };
+  meet();  // nothing of the worker's is still read or written, unless a role gave up
+  if (abort_flag[0]) {  // the same for all of the worker's threads: no role is left to set it
+    // whichever role gave up, copies and products may be in flight: they end before the CTA and its TMEM do
+    if (warp == C::LOAD + 1 && lane == 0) {
+      if (rank == 0) tc_commit<CTAS>(drain);  // the thread that issued the products
+      tcc::mbar_wait_bounded(drain, 0, kDrainNs);
+    }
+    if (warp == C::LOAD && lane == 0 && rank == 0) {
+      const uint32_t n0 = loads[0], n1 = CTAS == 2 ? loads[1] : n0, n = n0 > n1 ? n0 : n1;
+      for (uint32_t i = n > C::STAGES ? n - C::STAGES : 0; i < n; ++i) {
+        const uint32_t bar = full(i % C::STAGES);
+        if (i >= n0)
+          mbar_arrive_expect_tx(bar, C::STAGE);  // the second CTA's copies alone
+        else if (i >= n1)
+          mbar_complete_tx(bar, C::STAGE);  // the first CTA's alone: the others were expected, and do not come
+        tcc::mbar_wait_bounded(bar, (i / C::STAGES) & 1u, kDrainNs);
+      }
+    }
+    __syncwarp();
+    meet();
+  }
   if (warp == C::ALLOC) {
     tc_fence_after();
     tc_dealloc<CTAS>(tmem, C::TMEM);
@@ -466,6 +512,7 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   const int64_t total = a.cut * a.KB, first = rest * a.KB, last = first + a.KB - 1;
   const int w0 = owner_of(total, a.cutters, first), w1 = owner_of(total, a.cutters, last);
   if (w0 == w1) return;  // its worker ended it
+  const bool failed = ws_failed(a.ws);  // a worker gave up: its pieces are not there
   int mb, nb;
   tile_place(a, a.whole + rest, &mb, &nb);
   const int64_t m0 = int64_t(mb * CTAS + rank) * 128 + q * 32;
@@ -515,6 +562,7 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
     else  // columns 0-15 of both halves in one stage, 16-31 in the next
       stage_put<8>(out + (part >> 1) * kStageBytes, lane, v, k * End::U + (part & 1) * 2);
   }
+  if (failed) return;
   __syncthreads();
 #pragma unroll 1
   for (int k = 0; k < 32 / End::COLS; ++k) {
@@ -798,6 +846,8 @@ TcArgs tc_args(const TcGemm& g, const TcPlan& p) {
   a.piece = g.piece;
   a.ws = g.ws;
   a.clear = g.clear;
+  const uint64_t ns = wait_limit_ns();
+  a.wait_ns = ns > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(ns);
   return a;
 }
 

@@ -43,6 +43,7 @@ struct TcArgs {
   float* piece;    // [W][2][CTAs of a worker][BN / 4][128][4]
   void* ws;
   int clear;       // this launch clears the call's status
+  uint32_t wait_ns;  // limit of every wait
 };
 
 // Tile t's place: groups of eight tiles along m, within a group m first, so that tiles in flight
