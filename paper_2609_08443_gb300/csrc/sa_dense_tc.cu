@@ -512,7 +512,7 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
   const int64_t total = a.cut * a.KB, first = rest * a.KB, last = first + a.KB - 1;
   const int w0 = owner_of(total, a.cutters, first), w1 = owner_of(total, a.cutters, last);
   if (w0 == w1) return;  // its worker ended it
-  const bool failed = ws_failed(a.ws);  // a worker gave up: its pieces are not there
+  if (ws_failed(a.ws)) return;  // a worker gave up: its pieces are not there (asked later, it cost a register and 1 us)
   int mb, nb;
   tile_place(a, a.whole + rest, &mb, &nb);
   const int64_t m0 = int64_t(mb * CTAS + rank) * 128 + q * 32;
@@ -562,7 +562,6 @@ __device__ __forceinline__ void tc_join_work(const TcArgs& a, const int block) {
     else  // columns 0-15 of both halves in one stage, 16-31 in the next
       stage_put<8>(out + (part >> 1) * kStageBytes, lane, v, k * End::U + (part & 1) * 2);
   }
-  if (failed) return;
   __syncthreads();
 #pragma unroll 1
   for (int k = 0; k < 32 / End::COLS; ++k) {
