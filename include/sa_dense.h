@@ -64,7 +64,8 @@ sa_status sa_layer_norm_bwd(const void* dy, int64_t dy_stride, sa_dtype y_dt, co
  *     x : [M, K] with strides    w : [Z, K] with strides    b : [Z]
  *     r : [M, N] with strides    y : [M, N]                 z : [M, Z], or NULL
  * The activation takes z before its rounding.  K >= 1, N >= 1, Z and K at most 2^20, M < 2^31 - 256.
- * bf16 products accumulate in fp32 on the tensor cores.  fp32 factors are split into three
+ * bf16 products accumulate in fp32 on the tensor cores, whose additions round towards zero: a sum of terms of one sign
+ * comes out less than 2^-13 too small, however long it is (6e-5 measured).  fp32 factors are split into three
  * bf16 terms each (exact), of which the six largest products are taken (the rest is below
  * 2^-23 of a product's size) and summed in fp32; with more than 16 rows an infinite factor there, or one
  * above 3.38e38, gives a NaN.  y may not be r. */

@@ -109,7 +109,7 @@ struct TcPlan {
   int ctas, W;  // CTAs of a worker, workers
   int64_t mt, nt, KB, whole, cut;
   int cutters;  // workers that share the cut tiles
-  size_t piece_bytes;
+  size_t piece_bytes, sums_at;  // of cut tiles' pieces and, from sums_at on, of the sums of tiles in several runs
   double cost, bytes;  // estimated time (sa_dense_tc.cu has the unit), what has to move
 };
 

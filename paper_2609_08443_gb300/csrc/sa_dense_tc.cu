@@ -20,9 +20,12 @@
 // kernel adds in worker order and ends, so results do not depend on timing.
 //
 // fp32 operands come as three bf16 terms each, and six of the nine products of terms are made.  The tensor
-// core's sums lose up to a step of fp32 an addition, always towards zero (1024 x 1024 sums of 1024 products were
+// core's sums lose about a step of fp32 an addition, always towards zero (1024 x 1024 sums of 1024 products were
 // 6.5e-6 off with eight blocks in a row), so each block starts with its small products, and its
 // accumulators are added to sums in registers, which round to nearest.
+// bf16 sums lose as much: 200,003 products of one sign came out 7.3e-4 too small.  So a tile's blocks go in runs of at most
+// kRun, and the runs' sums are added in memory, in fp32 (a worker's own cells, which L2 holds): a run loses 6e-5, a sixtieth of
+// the largest rounding of a result, and its 68 us of products hide the 256 KB each way.
 #include "sa_dense_tc.cuh"
 
 #include <cmath>
@@ -198,7 +201,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
     constexpr int CH = C::POOL ? YN / 32 : Shape::template CHUNKS<EPI>;
     TmaOut<EPI, C::OUT_SETS> outs(out, lane);
     Segments seg(a, worker);
-    uint32_t g = 0;  // sets of accumulators used
+    uint32_t g = 0, tiles = 0;  // sets of accumulators used, tiles
     bool ok = true;
     auto release = [&](uint32_t set) {
       tc_fence_before();
@@ -211,10 +214,10 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
           mbar_arrive(acc_empty(set));
       }
     };
-    while (ok && seg.next()) {
+    for (; ok && seg.next(); ++tiles) {
       // this warp's chunks: of a pool every third of all tiles' chunks, else half of each tile's
       constexpr int STEP = C::POOL ? 3 : 1;
-      const int first = C::POOL ? (h + int(g % 3) * (3 - CH % 3)) % 3 : h * CH, stop = C::POOL ? CH : first + CH;
+      const int first = C::POOL ? (h + int(tiles % 3) * (3 - CH % 3)) % 3 : h * CH, stop = C::POOL ? CH : first + CH;
       int mb, nb;
       tile_place(a, seg.tile, &mb, &nb);
       const int64_t m0 = int64_t(mb * CTAS + int(rank)) * 128 + q * 32;
@@ -290,12 +293,60 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
             for (int k = 0; k < HALVES; ++k) put_piece(col(first + i, k), sum[i][k]);
         }
       } else {
+        // the sums of the runs so far: this thread's cells of chunk i
+        auto sums_of = [&](int i, int k) {
+          return a.sums + (int64_t(worker) * CTAS + rank) * (128 * C::BN) + (q * 32 + lane) * 4 + int64_t(col(i, k) / 4) * 512;
+        };
+        auto add_sums = [&](const float* p, float* v) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 f = *reinterpret_cast<const float4*>(p + j * 512);
+            v[4 * j] += f.x, v[4 * j + 1] += f.y, v[4 * j + 2] += f.z, v[4 * j + 3] += f.w;
+          }
+        };
+        constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
+        int kb = seg.k0;
+        for (; seg.k1 - kb > kRun; kb += kRun, ++g) {  // runs before a tile's last
+          const uint32_t set = g % C::SETS, acc = tmem + lanes + set * C::BN;
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), g / C::SETS & 1u, abort_flag, a.ws, 0x405));
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int i = first; i < stop; i += STEP)
+#pragma unroll 1
+            for (int k = 0; k < HALVES; ++k) {
+              float v[32];
+              float* p = sums_of(i, k);
+              tmem_ld32(acc + col(i, k), v);
+              tmem_ld_wait();
+              if (kb != seg.k0) add_sums(p, v);
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<float4*>(p + j * 512) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            }
+          release(set);
+        }
+        if (!ok) break;
         const bool tma = (a.vec & 1) != 0;
         if (complete && tma && first < stop) outs.load_bias(a, y0 + first * 32);
         const uint32_t set = g % C::SETS, acc = tmem + lanes + set * C::BN;
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), g / C::SETS & 1u, abort_flag, a.ws, 0x404));
         if (!ok) break;
         tc_fence_after();
+        if (kb != seg.k0) {  // the last run's accumulators become the tile's sums
+#pragma unroll 1
+          for (int i = first; i < stop; i += STEP)
+#pragma unroll 1
+            for (int k = 0; k < HALVES; ++k) {
+              float v[32];
+              tmem_ld32(acc + col(i, k), v);
+              tmem_ld_wait();
+              add_sums(sums_of(i, k), v);
+              tmem_st16(acc + col(i, k), reinterpret_cast<const uint32_t*>(v));
+              tmem_st16(acc + col(i, k) + 16, reinterpret_cast<const uint32_t*>(v) + 16);
+            }
+          tmem_st_wait();
+        }
         if (C::POOL && first >= stop) release(set);
 #pragma unroll 1
         for (int i = first; i < stop; i += STEP) {
@@ -407,7 +458,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       bool ok = a.wait_ns >= kPollLimitNs || mbar_wait(never, 0, abort_flag, a.ws, 0x400);
       while (ok && seg.next()) {
         for (int kb = seg.k0; ok && kb < seg.k1;) {
-          const int end = F32 ? kb + 1 : seg.k1;
+          const int end = F32 ? kb + 1 : seg.k1 - kb > kRun ? kb + kRun : seg.k1;
           const uint32_t set = g % C::SETS, d = tmem + set * C::BN;
           ok = mbar_wait(acc_empty(set), (g / C::SETS & 1u) ^ 1u, abort_flag, a.ws, 0x402);
           if (!ok) break;
@@ -787,8 +838,9 @@ TcPlan tc_plan(int64_t M, int64_t N, int64_t K, int act, bool f32, int sms, int 
     }
   }
   if (best.cost < best.bytes / 1.8e6) best.cost = best.bytes / 1.8e6;
-  best.piece_bytes =
-      best.cut ? size_t(best.cutters) * 2 * best.ctas * 128 * (best.ctas == 2 ? 256 : 128) * sizeof(float) : 0;
+  const size_t cells = size_t(best.ctas) * 128 * (best.ctas == 2 ? 256 : 128) * sizeof(float);  // a worker's tile
+  best.sums_at = best.cut ? size_t(best.cutters) * 2 * cells : 0;
+  best.piece_bytes = best.sums_at + (!f32 && KB > kRun ? size_t(best.W) * cells : 0);
   return best;
 }
 
@@ -843,6 +895,7 @@ TcArgs tc_args(const TcGemm& g, const TcPlan& p) {
   a.vec = (g.N % each == 0 && base_ok(g.y) && base_ok(g.z) ? 1 : 0) |
           (g.N % each == 0 && g.r.stride % each == 0 && base_ok(g.r.p) ? 2 : 0);
   a.piece = g.piece;
+  a.sums = g.piece + p.sums_at / sizeof(float);
   a.ws = g.ws;
   a.clear = g.clear;
   const uint64_t ns = wait_limit_ns();

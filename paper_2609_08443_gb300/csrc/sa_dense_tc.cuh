@@ -20,6 +20,9 @@ struct Divisor {
   __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
 };
 
+// Blocks of bf16 products that accumulate in TMEM in one go (sa_dense_tc.cu): 16384 terms a sum.
+constexpr int kRun = 256;
+
 // C[m, n] = sum over k of A[m, k] B[n, k], in tiles of 128 rows a CTA.
 struct TcArgs {
   int64_t M;       // rows of C
@@ -40,7 +43,8 @@ struct TcArgs {
   void* z;
   int64_t Z;       // columns of z
   int vec;         // rows allow 16-byte access: 1 y and z, 2 r
-  float* piece;    // [W][2][CTAs of a worker][BN / 4][128][4]
+  float* piece;    // [cutters][2][CTAs of a worker][BN / 4][128][4]
+  float* sums;     // bf16 and more than kRun blocks: [W][CTAs of a worker][BN / 4][128][4]
   void* ws;
   int clear;       // this launch clears the call's status
   uint32_t wait_ns;  // limit of every wait
