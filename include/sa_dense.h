@@ -66,9 +66,9 @@ sa_status sa_layer_norm_bwd(const void* dy, int64_t dy_stride, sa_dtype y_dt, co
  * The activation takes z before its rounding.  K >= 1, N >= 1, Z and K at most 2^20, M < 2^31 - 256.
  * bf16 products accumulate in fp32 on the tensor cores, whose additions round towards zero: a sum of terms of one sign
  * comes out less than 2^-13 too small, however long it is (6e-5 measured).  fp32 factors are split into three
- * bf16 terms each (exact), of which the six largest products are taken (the rest is below
- * 2^-23 of a product's size) and summed in fp32; with more than 16 rows an infinite factor there, or one
- * above 3.38e38, gives a NaN.  y may not be r. */
+ * bf16 terms each (exactly for sizes from 2^-110 on; of smaller ones, what lies below 2^-134 is lost), of which the six
+ * largest products are taken (the rest is below 2^-23 of a product's size) and summed in fp32; with more than 16 rows an
+ * infinite factor there gives a NaN.  y may not be r. */
 typedef enum { SA_ACT_NONE = 0, SA_ACT_RELU = 1, SA_ACT_GELU = 2, SA_ACT_SILU = 3, SA_ACT_SWIGLU = 4 } sa_act;
 
 /* `repack` says which operands need a copy in aligned rows, because their address or row

@@ -84,8 +84,17 @@ __device__ __forceinline__ void store_n(__nv_bfloat16* p, const float* v) {
     *reinterpret_cast<uint2*>(p) = make_uint2(ptx::pack_bf16(v[0], v[1]), ptx::pack_bf16(v[2], v[3]));
 }
 
-// Eight fp32 values as three terms of bf16 each, in planes `plane` elements apart: each term is what is left rounded to
-// nearest, and what is left after the third is nothing.
+// Term k of an fp32 value of which `left` is left: that rounded to nearest, but bf16's largest where a finite value would round
+// to an infinity, whose remainder would be a NaN.
+__device__ __forceinline__ __nv_bfloat16 term_of(float left, int k) {
+  const __nv_bfloat16 t = __float2bfloat16_rn(left);
+  if (k == 0 && fabsf(left) >= 3.3961775e38f && fabsf(left) <= 3.4028235e38f)
+    return __float2bfloat16_rz(left);
+  return t;
+}
+
+// Eight fp32 values as three terms of bf16 each, in planes `plane` elements apart: nothing is left after the third for sizes
+// from 2^-110 on; below, what lies under half of bf16's smallest subnormal, 2^-134, is lost.
 __device__ __forceinline__ void store_terms(__nv_bfloat16* p, int64_t plane, const float* v) {
   float left[8];
 #pragma unroll
@@ -95,7 +104,7 @@ __device__ __forceinline__ void store_terms(__nv_bfloat16* p, int64_t plane, con
     float t[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      t[j] = __bfloat162float(__float2bfloat16_rn(left[j]));
+      t[j] = __bfloat162float(term_of(left[j], k));
       left[j] -= t[j];
     }
     store8(p + k * plane, t);

@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(256, GATED && sizeof(T) == 4 ? 2 : 3) act_grad
               float left = d[s][j];
 #pragma unroll
               for (int k = 0; k < 3; ++k) {
-                const __nv_bfloat16 term = __float2bfloat16_rn(left);
+                const __nv_bfloat16 term = term_of(left, k);
                 o[k * plane + col(j)] = term;
                 left -= __bfloat162float(term);
               }
