@@ -1004,6 +1004,12 @@ def _norm_workspace_size(index: int, rows: int, n: int) -> int:
     return int(load().sa_layer_norm_workspace_size(rows, n))
 
 
+def _gradient_follows(*tensors) -> bool:
+    """Whether autograd records a call of these.  (Inside a Function's forward, where gradients are off, a parameter counts
+    as needing one under ``torch.no_grad()`` too.)"""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 class LayerNorm(torch.autograd.Function):
     """y = LN(x + residual) weight + bias over the last axis; differentiable once."""
 
@@ -1028,6 +1034,8 @@ class LayerNorm(torch.autograd.Function):
 
 def sa_layer_norm(x, weight=None, bias=None, residual=None, eps: float = 1e-5, dtype=None):
     """Differentiable layer norm of x + residual over the last axis, [..., n] of ``dtype`` (x's by default)."""
+    if not _gradient_follows(x, weight, bias, residual):
+        return sa_layer_norm_fwd(x, weight, bias, residual, eps, dtype)
     return LayerNorm.apply(x, weight, bias, residual, eps, dtype)
 
 
@@ -1160,4 +1168,6 @@ class Linear(torch.autograd.Function):
 
 def sa_linear(x, weight, bias=None, activation: Optional[str] = None, residual=None):
     """Differentiable act(x weight^T + bias) + residual (see ``sa_linear_fwd``)."""
+    if not _gradient_follows(x, weight, bias, residual):
+        return sa_linear_fwd(x, weight, bias, activation, residual)
     return Linear.apply(x, weight, bias, activation, residual)
