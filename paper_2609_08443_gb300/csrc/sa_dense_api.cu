@@ -112,8 +112,9 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
     piece = s.plan.piece_bytes;
   } else {
     const bool act = l.act != SA_ACT_NONE;
-    s.dz = section(act, size_t(l.M) * pitch_of(l.Z) * size_of(l.dt));
-    s.dz_terms = section((f32 && !few_f32) || (!act && (repack & COPY_DY)), size_t(l.M) * pitch_of(l.Z) * each);
+    // dz, or dy's copy, or fp32's terms of either: in one place, since only the CUDA-core path has an fp32 dz and no terms
+    const bool terms = f32 && !few_f32;
+    s.dz = s.dz_terms = section(act || terms || (repack & COPY_DY), size_t(l.M) * pitch_of(l.Z) * (terms ? each : size_of(l.dt)));
     s.dx = sa::dense::tc_plan(l.M, l.K, l.Z, sa::dense::kPlain, f32);
     s.dw = sa::dense::tc_plan(l.Z, l.K, l.M, sa::dense::kPlain, f32);
     s.side = sa::dense::tc_plan_grads(l.M, l.Z, l.K, f32, s.dx.cost + s.dw.cost, &s.side_dx, &s.side_dw);
