@@ -869,6 +869,9 @@ SA_ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "swiglu": 4}
 # Workspaces of these calls, apart from the cache's: reading one family's status must not depend on the other's calls.
 _dense_ws = threading.local()
 _dense_ws_cache = {}
+# Larger ones (a gradient's dz, copies of operands) are taken from torch's allocator for each call and given back with the
+# next on the stream: such a call takes tens of microseconds, an allocation two.
+_DENSE_KEPT = 32 << 20
 
 
 def sa_linear_get_device_error(device=None) -> int:
@@ -1078,6 +1081,10 @@ def _linear_workspace(ws, index: int, stream: int, *sizes) -> torch.Tensor:
     need = _linear_workspace_size(index, *sizes)
     if need == 0:
         raise SketchError(2, "sa_linear_workspace_size")
+    if need > _DENSE_KEPT:
+        with _ws_lock:
+            _dense_ws_cache.pop((index, stream), None)  # the last call's, whose status this call's replaces
+        return torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
     return _stream_workspace(need, index, stream, _dense_ws)
 
 
