@@ -134,7 +134,8 @@ __device__ __forceinline__ void tc_load(uint32_t dst, const void* map, uint32_t 
 
 // The work of one CTA.  Maps: K-major operands [planes][rows][k], boxes of 64 x (A: 128, B: 64) rows; MN-major ones
 // [planes][k][mn], boxes of 64 x 64.
-template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
+// LONG: a tile may take several runs.
+template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI, bool LONG>
 __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ty,
                                                const CUtensorMap& tz, const TcArgs& a, const int worker,
                                                const bool clear) {
@@ -306,7 +307,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         };
         constexpr int HALVES = EPI == EPI_GATED ? 2 : 1;
         int kb = seg.k0;
-        for (; seg.k1 - kb > kRun; kb += kRun, ++g) {  // runs before a tile's last
+        for (; LONG && seg.k1 - kb > kRun; kb += kRun, ++g) {  // runs before a tile's last
           const uint32_t set = g % C::SETS, acc = tmem + lanes + set * C::BN;
           ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), g / C::SETS & 1u, abort_flag, a.ws, 0x405));
           if (!ok) break;
@@ -333,7 +334,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(set), g / C::SETS & 1u, abort_flag, a.ws, 0x404));
         if (!ok) break;
         tc_fence_after();
-        if (kb != seg.k0) {  // the last run's accumulators become the tile's sums
+        if (LONG && kb != seg.k0) {  // the last run's accumulators become the tile's sums
 #pragma unroll 1
           for (int i = first; i < stop; i += STEP)
 #pragma unroll 1
@@ -458,7 +459,7 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
       bool ok = a.wait_ns >= kPollLimitNs || mbar_wait(never, 0, abort_flag, a.ws, 0x400);
       while (ok && seg.next()) {
         for (int kb = seg.k0; ok && kb < seg.k1;) {
-          const int end = F32 ? kb + 1 : seg.k1 - kb > kRun ? kb + kRun : seg.k1;
+          const int end = F32 ? kb + 1 : LONG && seg.k1 - kb > kRun ? kb + kRun : seg.k1;
           const uint32_t set = g % C::SETS, d = tmem + set * C::BN;
           ok = mbar_wait(acc_empty(set), (g / C::SETS & 1u) ^ 1u, abort_flag, a.ws, 0x402);
           if (!ok) break;
@@ -524,16 +525,16 @@ __device__ __forceinline__ void tc_linear_work(const CUtensorMap& ta, const CUte
   if (CTAS == 2) cluster_sync_all();
 }
 
-template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
+template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI, bool LONG>
 __global__ void __launch_bounds__(TcCfg<CTAS, F32, EPI>::THREADS, 1)
     tc_linear_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                      const __grid_constant__ CUtensorMap ty, const __grid_constant__ CUtensorMap tz, const TcArgs a) {
-  tc_linear_work<CTAS, A_MN, B_MN, F32, EPI>(ta, tb, ty, tz, a, int(blockIdx.x) / CTAS, a.clear && blockIdx.x == 0);
+  tc_linear_work<CTAS, A_MN, B_MN, F32, EPI, LONG>(ta, tb, ty, tz, a, int(blockIdx.x) / CTAS, a.clear && blockIdx.x == 0);
 }
 
 // dx and dW side by side, for gradients that would leave most of the GPU idle one after the other: the first
 // x.W CTAs (or pairs) make dx.
-template <int CTAS, bool F32>
+template <int CTAS, bool F32, bool LONG>
 __global__ void __launch_bounds__(TcCfg<CTAS, F32, EPI_PLAIN>::THREADS, 1)
     tc_linear_grads_kernel(const __grid_constant__ CUtensorMap xa, const __grid_constant__ CUtensorMap xb,
                            const __grid_constant__ CUtensorMap wa, const __grid_constant__ CUtensorMap wb,
@@ -541,9 +542,9 @@ __global__ void __launch_bounds__(TcCfg<CTAS, F32, EPI_PLAIN>::THREADS, 1)
                            const TcArgs w) {
   const int worker = int(blockIdx.x) / CTAS;
   if (worker < x.W)
-    tc_linear_work<CTAS, false, true, F32, EPI_PLAIN>(xa, xb, xy, xy, x, worker, blockIdx.x == 0);
+    tc_linear_work<CTAS, false, true, F32, EPI_PLAIN, LONG>(xa, xb, xy, xy, x, worker, blockIdx.x == 0);
   else
-    tc_linear_work<CTAS, true, true, F32, EPI_PLAIN>(wa, wb, wy, wy, w, worker - x.W, false);
+    tc_linear_work<CTAS, true, true, F32, EPI_PLAIN, LONG>(wa, wb, wy, wy, w, worker - x.W, false);
 }
 
 // Cut tiles: a block of 16 warps ends 128 rows x 32 columns of y.  Warp (q, part) adds the pieces of the rows of q and eight
@@ -728,6 +729,18 @@ bool make_out_map(CUtensorMap* m, const void* p, int64_t M, int N, int halves) {
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// f(LONG).  The code of several runs costs a single CTA's tiles, whose products are short, 0.3 us of 41 where it is not used
+// (65536 x 128 -> 512 gated), so they have kernels without it; pairs none.
+template <int CTAS, bool F32, class F>
+cudaError_t with_runs(bool several, F f) {
+  if constexpr (F32)
+    return f(std::false_type{});
+  else if constexpr (CTAS == 2)
+    return f(std::true_type{});
+  else
+    return several ? f(std::true_type{}) : f(std::false_type{});
+}
+
 template <int CTAS, bool A_MN, bool B_MN, bool F32, int EPI>
 cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaStream_t st, int* launches) {
   using C = TcCfg<CTAS, F32, EPI>;
@@ -738,9 +751,11 @@ cudaError_t launch_one(const TcGemm& g, const TcPlan& p, const TcArgs& a, cudaSt
     if (!make_out_map(&ty, a.y, a.M, a.N, 1) || (a.z && !make_out_map(&tz, a.z, a.M, a.N, EPI == EPI_GATED ? 2 : 1)))
       return cudaErrorInvalidValue;
   }
-  cudaError_t e =
-      launch_cluster<CTAS, tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI>>(p.W * CTAS, C::THREADS, C::SMEM, st, ta, tb, ty,
-                                                                         tz, a);
+  auto go = [&](auto runs) {
+    return launch_cluster<CTAS, tc_linear_kernel<CTAS, A_MN, B_MN, F32, EPI, runs()>>(p.W * CTAS, C::THREADS, C::SMEM, st, ta,
+                                                                                      tb, ty, tz, a);
+  };
+  const cudaError_t e = with_runs<CTAS, F32>(a.KB > kRun, go);
   ++*launches;
   if (e != cudaSuccess || p.cut == 0) return e;
   constexpr int CH = TileShape<CTAS>::template YN<EPI> / 32;
@@ -761,8 +776,11 @@ cudaError_t launch_grads(const TcGemm& gx, const TcPlan& px, const TcArgs& x, co
   CUtensorMap xy = xa, wy = wa;
   if (!F32 && ((x.vec & 1) && !make_out_map(&xy, x.y, x.M, x.N, 1))) return cudaErrorInvalidValue;
   if (!F32 && ((w.vec & 1) && !make_out_map(&wy, w.y, w.M, w.N, 1))) return cudaErrorInvalidValue;
-  cudaError_t e = launch_cluster<CTAS, tc_linear_grads_kernel<CTAS, F32>>((px.W + pw.W) * CTAS, C::THREADS, C::SMEM, st, xa, xb, wa,
-                                       wb, xy, wy, x, w);
+  auto go = [&](auto runs) {
+    return launch_cluster<CTAS, tc_linear_grads_kernel<CTAS, F32, runs()>>((px.W + pw.W) * CTAS, C::THREADS, C::SMEM, st, xa, xb,
+                                                                           wa, wb, xy, wy, x, w);
+  };
+  const cudaError_t e = with_runs<CTAS, F32>(x.KB > kRun || w.KB > kRun, go);
   ++*launches;
   if (e != cudaSuccess || px.cut + pw.cut == 0) return e;
   constexpr int CH = TileShape<CTAS>::template YN<EPI_PLAIN> / 32;
