@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(256, GATED && sizeof(T) == 4 ? 2 : 3) act_grad
       for (int j = 0; j < 8; ++j) sum[s][j] += d[s][j];
       if (!a.dz) continue;
       const int64_t at = row * a.pitch + int64_t(s) * a.N;
-      if (a.terms) {
+      if (sizeof(T) == 4 && a.terms) {  // never of bf16
         __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.dz) + at;
         const int64_t plane = a.M * a.pitch;
         if (VEC) {
