@@ -293,12 +293,16 @@ __device__ __forceinline__ void load_factors(const NormArgs& a, int t, int n, fl
 template <int T, int C>
 constexpr bool keep_parameters() { return T * C < 2048; }
 
-// Sums over the T threads of a row.  Within a warp by shuffles; over a block through `red`, whose
+// Two sums over the T threads of a row.  Within a warp by shuffles; over a block through `red`, whose
 // two halves take turns, so one barrier a sum is enough.
-template <int T, int K>
-__device__ __forceinline__ void row_sum(float (&v)[K], float* red, int& turn) {
-  constexpr int lanes = T < 32 ? T : 32;
-  if constexpr (K == 2 && T > 32) {
+template <int T>
+__device__ __forceinline__ void row_sum(float (&v)[2], float* red, int& turn) {
+  if constexpr (T <= 32) {
+#pragma unroll
+    for (int o = T / 2; o > 0; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+  } else {
     // the first exchange leaves each half of the warp with one of the two sums
     const bool high = threadIdx.x & 16;
     float x = (high ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, high ? v[0] : v[1], 16);
@@ -323,28 +327,6 @@ __device__ __forceinline__ void row_sum(float (&v)[K], float* red, int& turn) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
       }
-    }
-    return;
-  }
-#pragma unroll
-  for (int o = lanes / 2; o > 0; o >>= 1)
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-  if constexpr (T > 32) {
-    constexpr int W = T / 32;
-    float* s = red + turn * W * K;
-    turn ^= 1;
-    const int lane = threadIdx.x & 31;
-    if (lane == 0)
-#pragma unroll
-      for (int k = 0; k < K; ++k) s[(threadIdx.x >> 5) * K + k] = v[k];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      v[k] = lane < W ? s[lane * K + k] : 0.f;
-#pragma unroll
-      for (int o = W / 2; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-      if (W < 32) v[k] = __shfl_sync(0xFFFFFFFFu, v[k], 0);
     }
   }
 }
@@ -729,8 +711,8 @@ cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t st) {
   return with_layout<false>(a.n, vec_ok(a), narrow, [&](auto T, auto C, auto V) {
     constexpr bool NEXT = T() < 1024 || V();
     const Walkers w = walkers<T(), C(), V(), NEXT, false>(a);
-    if constexpr (T() >= 512 && NEXT) {
-      if (w.blocks == 0) {  // no room for two rows
+    if constexpr (T() == 1024 && NEXT) {
+      if (w.blocks == 0) {  // no room for two rows of fp32
         const Walkers plain = walkers<T(), C(), V(), false, false>(a);
         return launch_walk<norm_fwd_kernel<T(), C(), V(), false>>(plain, block_threads<T()>(), 0, a, st);
       }
