@@ -68,8 +68,9 @@ constexpr int kMostFewRows = 16;
 // y for at most kMostFewRows rows of x
 cudaError_t launch_rows(const GemmArgs& g, cudaStream_t st);
 
-// Gradients for at most kMostFewRows rows, without the tensor cores: dx [M, K] from shares of W's rows
+// Gradients for at most so many rows, without the tensor cores: dx [M, K] from shares of W's rows
 // (partial: [rows_dx_shares][M][K]), dW [Z, K]; NULL where not wanted.
+constexpr int most_few_grads(sa_dtype dt) { return dt == SA_BF16 ? 4 : kMostFewRows; }
 struct RowsGradArgs {
   const void *dz, *w, *x;  // dz [M, Z], w [Z, K], x [M, K]
   int64_t pitch, w_stride, x_stride;

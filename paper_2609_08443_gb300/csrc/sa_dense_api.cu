@@ -79,13 +79,22 @@ struct Layout {
   bool side;
 };
 
-// A product of this many rows of x is a matter of reading W (sa_dense_rows.cu), and takes no workspace on any path.
+// A product of this many rows of x is a matter of reading W (sa_dense_rows.cu), and takes no workspace on any path.  us, rows
+// kernel | tensor cores: bf16 1024 -> 1024, 1 row 2.6 | 8.8, 16 rows 3.1 | 8.9, 32 rows (in two calls) 5.6 | 9.2; 4096 -> 8192
+// gated, 16 rows 26 | 34, 17 rows 48 | 34; 8192 -> 1024, 16 rows 11.3 | 13.3, 17 rows 17.5 | 13.3.  fp32 4096 -> 8192 gated,
+// 16 rows 161 | 189, 17 rows 236 | 190; 8192 -> 1024, 16 rows 22 | 30, 17 rows 31 | 31.  The other way round: fp32 of unaligned
+// rows (4095 -> 4096), 8 rows 38 | 56, 16 rows 87 | 56.
 bool few_rows(const Linear& l) { return l.M <= sa::dense::kMostFewRows; }
 
 int64_t pitch_of(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-// Few rows' gradients go without the tensor cores where these would want a copy of W.
-bool few_rows_grads(const Linear& l, int repack) { return few_rows(l) && l.M > 0 && (l.dt == SA_F32 || (repack & COPY_W)); }
+// Few rows' gradients go without the tensor cores where these would want a copy of W: in bf16 up to 4 rows of an unaligned W
+// (us, rows kernels | tensor cores: 4095 -> 4096, 4 rows 51 | 63, 8 rows 111 | 62; aligned, 1024 -> 4096, 4 rows 27 | 18), in fp32
+// up to 16, which also keep infinite factors (1024 -> 4096, 4 rows 25 | 33, 16 rows 42 | 32; 4096 -> 8192 gated, 4 rows 111 |
+// 247, 16 rows 187 | 248; 8192 -> 1024, 4 rows 33 | 43, 16 rows 61 | 44).
+bool few_rows_grads(const Linear& l, int repack) {
+  return l.M > 0 && l.M <= sa::dense::most_few_grads(l.dt) && (l.dt == SA_F32 || (repack & COPY_W));
+}
 
 Layout linear_layout(const Linear& l, bool bwd, int repack) {
   Layout s{};
@@ -93,7 +102,7 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
   // few rows' gradients in fp32, or with a W that needs a copy, never reach the tensor cores
   const bool few_f32 = bwd && f32 && few_rows(l);
   if (f32) repack = few_f32 ? 0 : COPY_X | COPY_W | COPY_DY;
-  if (bwd && few_rows(l)) repack &= ~COPY_W;
+  if (bwd && l.M <= sa::dense::most_few_grads(l.dt)) repack &= ~COPY_W;
   size_t off = sizeof(sa::WsHeader);
   auto section = [&](bool there, size_t bytes) {
     const size_t at = off;
@@ -125,7 +134,7 @@ Layout linear_layout(const Linear& l, bool bwd, int repack) {
   s.piece = section(piece > 0, piece);
   s.partial = section(bwd, size_t(sa::dense::act_grad_blocks(l.M, l.N)) * size_t(l.Z) * sizeof(float));
   // whichever way few rows go, which an operand's alignment has a say in, the size is enough
-  s.dx_partial = section(bwd && few_rows(l), size_t(sa::dense::rows_dx_shares(l.Z, l.K)) * size_t(l.M) * size_t(l.K) * sizeof(float));
+  s.dx_partial = section(bwd && l.M <= sa::dense::most_few_grads(l.dt), size_t(sa::dense::rows_dx_shares(l.Z, l.K)) * size_t(l.M) * size_t(l.K) * sizeof(float));
   s.total = off;
   return s;
 }

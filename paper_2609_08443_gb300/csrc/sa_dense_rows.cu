@@ -11,7 +11,7 @@
 // -> 4096: 2.9 us, a launch.
 //
 // Their gradients, where the tensor cores would want a copy of W first (fp32, whose terms are three times its reading, and
-// rows that TMA cannot read):
+// up to four rows where TMA cannot read W):
 //   dx = dz W    bound by reading W once: a thread holds a few columns of dx for all rows and walks down its block's share of
 //                W's rows; the shares' sums are added in order by a second kernel.
 //   dW = dz^T x  bound by writing dW: a thread holds a few columns of x and walks down rows of dW.
@@ -375,8 +375,7 @@ cudaError_t launch_rows_grads(const RowsGradArgs& a, cudaStream_t st, int* launc
     e = cudaGetLastError();
   };
 #define SA_PICK(KERNEL, VEC, Y)                                                                                   \
-  (a.dt == SA_BF16 ? (a.M <= 4 ? (VEC ? go(KERNEL<__nv_bfloat16, 4, true>, Y) : go(KERNEL<__nv_bfloat16, 4, false>, Y))   \
-                               : (VEC ? go(KERNEL<__nv_bfloat16, 16, true>, Y) : go(KERNEL<__nv_bfloat16, 16, false>, Y))) \
+  (a.dt == SA_BF16 ? (VEC ? go(KERNEL<__nv_bfloat16, 4, true>, Y) : go(KERNEL<__nv_bfloat16, 4, false>, Y))     \
                    : (a.M <= 4 ? (VEC ? go(KERNEL<float, 4, true>, Y) : go(KERNEL<float, 4, false>, Y))           \
                                : (VEC ? go(KERNEL<float, 16, true>, Y) : go(KERNEL<float, 16, false>, Y))))
   if (a.dx) {

@@ -34,3 +34,11 @@ def test_bf16_holds_dz_or_a_copy_of_dy(size):
     M, N, K = 4000, 512, 384
     plain = size(M, N, K, NONE, BF16, 1)
     assert size(M, N, K, NONE, BF16, 1, 4) - plain == size(M, N, K, GELU, BF16, 1) - plain == M * N * 2
+
+
+def test_an_unaligned_w_is_copied_above_four_rows(size):
+    """bf16 gradients: up to four rows read W where it is, the others from aligned rows."""
+    N, K = 512, 333
+    for M, copied in ((1, 0), (4, 0), (5, 1), (16, 1), (17, 1)):
+        more = size(M, N, K, NONE, BF16, 1, 2) - size(M, N, K, NONE, BF16, 1, 0)
+        assert more == copied * (N * 336 * 2), M
