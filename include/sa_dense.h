@@ -13,6 +13,8 @@
  *     elements (any value >= 0 for inputs: rows may repeat or overlap).  Outputs are
  *     contiguous.  Base pointers are aligned to their element.
  *   - Outputs may not overlap inputs or one another, except where a call says so.
+ *   - Where a norm's rows of x, r or dy do not start on 16 bytes, the 16-byte pieces that a row begins and ends in are read
+ *     whole: up to 15 bytes beside the matrix, in the same piece as its first or last element. What they hold has no effect.
  *   - An output pointer that may be NULL is not computed then.
  *   - All arithmetic is in fp32 or better; each output is rounded to its type once.
  *   - `workspace` is 256-byte aligned and need not be cleared.  A linear call's first 256 bytes hold its status
@@ -34,7 +36,7 @@ extern "C" {
  * x, r, y and the parameters have types of their own (SA_F32 or SA_BF16).  h is not
  * rounded before it is normalised.  eps > 0.
  *     x, r  : [rows, n] with strides      w, b : [n] of type w_dt
- *     y     : [rows, n] of type y_dt      stats: fp32 [rows, 2] = (mean, rstd), or NULL
+ *     y     : [rows, n] of type y_dt      stats: fp32 [rows, 2] = (mean, rstd), 8-byte aligned, or NULL
  * y may be x or r where type and layout are the same. */
 sa_status sa_layer_norm_fwd(const void* x, int64_t x_stride, sa_dtype x_dt, const void* r, int64_t r_stride,
                             sa_dtype r_dt, const void* w, const void* b, sa_dtype w_dt, int64_t rows, int n, float eps,
@@ -81,8 +83,8 @@ sa_status sa_linear_fwd(const void* x, int64_t x_stride, const void* w, int64_t 
 
 /* Gradient: dz = dy act'(z) (the forward's z; not looked at for SA_ACT_NONE),
  *     dx = dz W,   dW = dz^T x,   db = sum_rows dz          (each NULL where not wanted)
- * relu's slope at 0 is 0.  dz is rounded to dt where it enters the products (bf16: one
- * rounding of 2^-9 relative, as of any operand there; fp32: none), db sums it unrounded.
+ * relu's slope at 0 is 0.  dz is rounded to dt where it enters the products (bf16: by up to 2^-8 relative, as any operand
+ * there: dx and dW are 2.3e-3 from 64 bits, norm-wise, of which their own rounding is 1.7e-3; fp32: not), db sums it unrounded.
  *     dy : [M, N] with strides   z : [M, Z]   dx : [M, K]   dw : [Z, K]   db : [Z] */
 sa_status sa_linear_bwd(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* w,
                         int64_t w_stride, const void* z, int64_t M, int N, int K, sa_act act, sa_dtype dt, void* dx,

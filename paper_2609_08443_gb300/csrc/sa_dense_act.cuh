@@ -137,7 +137,7 @@ __device__ __forceinline__ void silu_pair(float* v) {
 // Phi(z) and e^(-z^2/2), Phi the normal distribution function.
 // FULL: from CUDA's erfc.  Else Phi(-x) = e^(-x^2/2) R(1 / (1 + 0.31 x)) for x >= 0, R of degree 6 without a constant
 // term: a least-squares fit with weights that level the relative error over 0 <= x <= 20 (Lawson's
-// iteration), 7.5e-6 at most; bf16's half step is 2e-3.
+// iteration), 7.5e-6 at most; bf16's half step is 2e-3 to 4e-3.
 template <bool FULL>
 __device__ __forceinline__ float normal_cdf(float z, float* density) {
   const float e = FULL ? expf(-0.5f * z * z) : ptx::ex2(-0.72134752f * z * z);

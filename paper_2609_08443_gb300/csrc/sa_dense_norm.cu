@@ -5,7 +5,7 @@
 //
 // Bound by memory: each element is read once and written once, the row stays in registers
 // between the mean, the variance (of the differences from that mean, so a mean far from zero
-// costs no digits) and the result.  T threads hold a row, C chunks of 8 elements each: 4 to 32
+// costs it no digits; the mean's own rounding, 2^-24 of it, stays in y) and the result.  T threads hold a row, C chunks of 8 elements each: 4 to 32
 // lanes of a warp up to 512 features (1024), a block above.  A block walks rows with the parameters,
 // and in the backward pass the columns' running sums, in registers (shared memory above 8192
 // features, whose sums would not fit); its sums leave as one partial row, and a second kernel
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(block_threads<T>(), blocks_at_once<T, C, VEC, 
 #pragma unroll
       for (int i = 0; i < P; ++i) unpair(h, i, __fadd2_rn(pair(h, i), both(-mean)));
     }
-    const float rstd = rsqrtf(fmaf(m, inv_n, a.eps));
+    const float rstd = rsqrtf(fmaf(m, inv_n, a.eps));  // off by 2^-22 at most, of which a correct root would save a step of y's fp32
     if (at.here()) {  // a warp's last rows may lie behind the end
       if (!keep_parameters<T, C>()) {
         load_factors<T, C, VEC>(a, t, n, w);
