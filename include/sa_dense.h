@@ -34,7 +34,8 @@ extern "C" {
  *     mean = sum h / n,  rstd = 1 / sqrt(sum (h - mean)^2 / n + eps),
  *     y = (h - mean) rstd w + b            (w NULL: 1, b NULL: 0)
  * x, r, y and the parameters have types of their own (SA_F32 or SA_BF16).  h is not
- * rounded before it is normalised.  eps > 0.
+ * rounded before it is normalised.  eps > 0.  The squares are summed in fp32: a row whose sum of them exceeds 3.4e38
+ * has rstd 0.
  *     x, r  : [rows, n] with strides      w, b : [n] of type w_dt
  *     y     : [rows, n] of type y_dt      stats: fp32 [rows, 2] = (mean, rstd), 8-byte aligned, or NULL
  * y may be x or r where type and layout are the same. */
